@@ -333,6 +333,123 @@ int conv_probe_mfma_mix(int32_t dtype, int32_t block, int32_t waves_per_simd, in
                         int32_t distinct_operands, void* scratch, void* stream, double* tflops, double* ns_per_mfma);
 int conv_probe_stream_bandwidth(const void* src, void* dst, size_t bytes, void* stream, double* gbytes_per_s);
 
+/*
+ * Operators at the end of a network: from the trunk's features (or the pixels of a channel-innermost tensor) to what the
+ * network answers with, and the gradients a head is trained with.  All of them work on `rows` rows (images, tokens,
+ * pixels); element (t, j) of a tensor is at t * ld + j, with the row stride `ld` in elements.
+ *
+ * Conventions, next to those at the top of this file:
+ *   - `dtype` is the storage type of the float tensors; per-row and per-column vectors (gamma, beta, bias, scales,
+ *     statistics, log probabilities and their gradients) are fp32, dense.  Sums and statistics are fp32 or int32.
+ *   - Float tensors have to be aligned to their element only and row strides are free (>= the row's length), so a slice
+ *     of a larger tensor can be passed; 8-bit tensors start on 16 bytes and have row strides divisible by 16.
+ *   - rows = 0 is valid and enqueues nothing (layernorm_bwd still writes its zero sums).  rows < 2^31.
+ *   - Outputs alias no input, except where said.
+ *   - Results do not depend on scheduling (no floating-point atomics): the same call gives the same bits.
+ */
+
+/*
+ * Layer norm over the columns: y[t][j] = (x[t][j] - mean_t) * rstd_t * gamma[j] + beta[j], mean_t the row's mean,
+ * rstd_t = 1 / sqrt(var_t + eps) with the variance taken around that mean (in a second pass over the held row).
+ * gamma NULL = ones, beta NULL = zeros; mean and rstd (fp32 [rows], what layernorm_bwd needs) may be NULL.
+ * ldx is the row stride of x and dx, ldy that of y and dy.  CONV_EINVAL for rows < 0, cols < 1 or >= 2^30, a stride
+ * below cols, eps < 0 or NaN, NULL or misaligned pointers.
+ */
+typedef struct {
+    int64_t rows;
+    int64_t ldx, ldy; /* row strides in elements */
+    int32_t cols;
+    int32_t dtype;    /* conv_dtype of x, y, dx, dy */
+    float eps;
+} norm_desc;
+int layernorm_fwd(const norm_desc* desc, const void* x, const float* gamma, const float* beta, void* y, float* mean,
+                  float* rstd, void* stream);
+
+/*
+ * Its gradients: with xh = (x - mean) * rstd and g = dy * gamma,
+ *   dx = rstd * (g - avg_j(g) - xh * avg_j(g * xh)),   dgamma[j] = sum_t dy * xh,   dbeta[j] = sum_t dy.
+ * Any of dx, dgamma and dbeta may be NULL, not all; gamma NULL = ones.  dx may be dy itself where ldx == ldy.  The sums over the
+ * rows are formed in fp32, per workgroup first and then over the workgroups' partial sums in `workspace`
+ * (layernorm_bwd_workspace_bytes(desc) bytes, 16-byte aligned; CONV_EWORKSPACE if it is smaller; not needed, and may be NULL,
+ * when neither dgamma nor dbeta is asked for).
+ */
+size_t layernorm_bwd_workspace_bytes(const norm_desc* desc);
+int layernorm_bwd(const norm_desc* desc, const void* x, const void* dy, const float* gamma, const float* mean,
+                  const float* rstd, void* dx, float* dgamma, float* dbeta, void* workspace, size_t workspace_bytes,
+                  void* stream);
+
+/*
+ * Rows to 8 bits with a scale each: scale[t] = max(max_j |x[t][j]| * fl(1/127), 2^-126), q[t][j] = x[t][j] * fl(1/scale[t])
+ * rounded to the nearest whole number (ties to even), so that q * scale stands for x and |q| <= 127.  A row that holds a
+ * NaN or an infinity gets the scale NaN and zeros: what is computed from it is NaN.  q has the row stride ldq
+ * (divisible by 16, >= cols); the bytes from cols up to the next multiple of 16 are written as zeros, those beyond are left.
+ * Weights [N][K] are quantised by the same call, a scale for each output channel.
+ */
+typedef struct {
+    int64_t rows;
+    int64_t ldx, ldq; /* row strides in elements */
+    int32_t cols;
+    int32_t dtype;    /* conv_dtype of x */
+} quant_desc;
+int quantize_rows(const quant_desc* desc, const void* x, int8_t* q, float* scale, void* stream);
+
+/* layernorm_fwd whose result, rounded to `dtype`, is quantised as by quantize_rows without being written: q has the row
+ * stride desc->ldy (divisible by 16).  Codes and scales are bit for bit those of the two calls. */
+int layernorm_quant_fwd(const norm_desc* desc, const void* x, const float* gamma, const float* beta, int8_t* q,
+                        float* scale, void* stream);
+
+/*
+ * Matrix product in 8-bit integers: out[t][n] = act(float(sum_k a[t][k] * w[n][k]) * (a_scale[t] * w_scale[n]) + bias[n])
+ * for a [rows][K] and w [N][K]; the sum is exact (int32; K < 2^17).  a_scale is [rows], w_scale [N], bias [N] or NULL.
+ * CONV_FLAG_RELU: act(x) = max(x, 0), a NaN stays NaN.  Rows of a and w are read in pieces of 16 bytes: the bytes from K
+ * up to the next multiple of 16 have to be readable; their values do not matter.  `workspace`
+ * (int_linear_workspace_bytes(desc) bytes, which may be 0; 16-byte aligned) holds partial sums of few-row products; NULL or a smaller one gives
+ * CONV_EWORKSPACE when bytes are needed.  N, K >= 1; lda, ldw >= K and divisible by 16; ldo >= N.
+ */
+typedef struct {
+    int64_t rows;
+    int64_t lda, ldw, ldo; /* row strides in elements */
+    int32_t N, K;
+    int32_t dtype;         /* conv_dtype of out */
+    uint32_t flags;        /* CONV_FLAG_RELU or 0 */
+} int_linear_desc;
+size_t int_linear_workspace_bytes(const int_linear_desc* desc);
+int int_linear_fwd(const int_linear_desc* desc, const int8_t* a, const float* a_scale, const int8_t* w,
+                   const float* w_scale, const float* bias, void* out, void* workspace, size_t workspace_bytes,
+                   void* stream);
+
+/*
+ * Log probabilities of given tokens under softmax over the columns (classes, a vocabulary), with lse_t = log sum_j exp(x_tj):
+ *   logp[t] = x[t][target[t]] - lse_t,   entropy[t] = -sum_j p_tj log p_tj (nats; p log p = 0 where p = 0),
+ *   top_id[t][0..top), top_logp[t][0..top): the `top` likeliest columns, by value and, where values are equal, by the lower
+ *   index (+0 and -0 are equal; a NaN counts as the largest), and their log probabilities.
+ * target is int64 [rows]: a negative one stands for "no token" (logp 0, no gradient), one >= cols gives NaN.
+ * Any output may be NULL, not all; target may be NULL if logp is; top_id and top_logp are dense [rows][top] and go together;
+ * 0 <= top <= min(64, cols), ignored if both are NULL.  Masked columns are -inf; a row of -inf only has lse, logp and top_logp -inf, entropy 0 and the columns
+ * 0, 1, ... as top_id.  A row with a NaN or +inf has NaN for all values.
+ * `workspace` (logprob_workspace_bytes(desc), may be 0; 16-byte aligned) joins rows that are split over several workgroups.
+ * CONV_EINVAL for rows < 0, cols < 1 or >= 2^31 - 2^20, strides below cols, top outside its range, NULL or misaligned pointers.
+ */
+typedef struct {
+    int64_t rows;
+    int64_t ldx, ldg; /* row strides of the logits and of their gradient, in elements */
+    int32_t cols;
+    int32_t dtype;    /* conv_dtype of the logits and of their gradient */
+    int32_t top;
+} logprob_desc;
+size_t logprob_workspace_bytes(const logprob_desc* desc);
+int logprob_fwd(const logprob_desc* desc, const void* logits, const int64_t* target, float* logp, float* lse,
+                float* entropy, int64_t* top_id, float* top_logp, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * The gradient in the logits of sum_t g_logp[t] * logp[t] + g_entropy[t] * entropy[t]:
+ *   dlogits[t][j] = g_logp[t] * ([j == target[t]] - p_tj) - g_entropy[t] * p_tj * (log p_tj + entropy[t]),
+ * p from lse and entropy of the forward pass.  g_logp or g_entropy may be NULL (zeros), not both; target goes with g_logp, entropy with
+ * g_entropy.  Rows whose lse is -inf get zeros.  dlogits may be the logits themselves where ldx == ldg.  desc->top is not read.
+ */
+int logprob_bwd(const logprob_desc* desc, const void* logits, const int64_t* target, const float* lse,
+                const float* entropy, const float* g_logp, const float* g_entropy, void* dlogits, void* stream);
+
 /* Text for a conv_status; for CONV_EHIP it includes the message of the last failed HIP call of this thread. */
 const char* conv_strerror(int status);
 

@@ -45,6 +45,26 @@ class conv_op(ctypes.Structure):
                 ("workspace_bytes", ctypes.c_size_t), ("p", ctypes.c_int32 * 9)]
 
 
+class norm_desc(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("ldx", ctypes.c_int64), ("ldy", ctypes.c_int64), ("cols", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("eps", ctypes.c_float)]
+
+
+class quant_desc(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("ldx", ctypes.c_int64), ("ldq", ctypes.c_int64), ("cols", ctypes.c_int32),
+                ("dtype", ctypes.c_int32)]
+
+
+class int_linear_desc(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("lda", ctypes.c_int64), ("ldw", ctypes.c_int64), ("ldo", ctypes.c_int64),
+                ("N", ctypes.c_int32), ("K", ctypes.c_int32), ("dtype", ctypes.c_int32), ("flags", ctypes.c_uint32)]
+
+
+class logprob_desc(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("ldx", ctypes.c_int64), ("ldg", ctypes.c_int64), ("cols", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("top", ctypes.c_int32)]
+
+
 class ConvError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -125,6 +145,28 @@ def lib() -> ctypes.CDLL:
         L.conv_transformed_filter_bytes.restype = ctypes.c_size_t
         L.conv_transform_filters.argtypes = [dp, vp, vp, vp]
         L.conv_transform_filters.restype = ctypes.c_int
+        np_, qp, ip, gp = (ctypes.POINTER(t) for t in (norm_desc, quant_desc, int_linear_desc, logprob_desc))
+        sz = ctypes.c_size_t
+        L.layernorm_fwd.argtypes = [np_] + [vp] * 7
+        L.layernorm_fwd.restype = ctypes.c_int
+        L.layernorm_quant_fwd.argtypes = [np_] + [vp] * 6
+        L.layernorm_quant_fwd.restype = ctypes.c_int
+        L.layernorm_bwd_workspace_bytes.argtypes = [np_]
+        L.layernorm_bwd_workspace_bytes.restype = sz
+        L.layernorm_bwd.argtypes = [np_] + [vp] * 9 + [sz, vp]
+        L.layernorm_bwd.restype = ctypes.c_int
+        L.quantize_rows.argtypes = [qp] + [vp] * 4
+        L.quantize_rows.restype = ctypes.c_int
+        L.int_linear_workspace_bytes.argtypes = [ip]
+        L.int_linear_workspace_bytes.restype = sz
+        L.int_linear_fwd.argtypes = [ip] + [vp] * 7 + [sz, vp]
+        L.int_linear_fwd.restype = ctypes.c_int
+        L.logprob_workspace_bytes.argtypes = [gp]
+        L.logprob_workspace_bytes.restype = sz
+        L.logprob_fwd.argtypes = [gp] + [vp] * 8 + [sz, vp]
+        L.logprob_fwd.restype = ctypes.c_int
+        L.logprob_bwd.argtypes = [gp] + [vp] * 8
+        L.logprob_bwd.restype = ctypes.c_int
         L.conv_strerror.argtypes = [ctypes.c_int]
         L.conv_strerror.restype = ctypes.c_char_p
         _lib = L
@@ -335,6 +377,79 @@ def conv_transformed_filter_bytes(desc) -> int:
 def conv_transform_filters(desc, filt, out, stream=None) -> None:
     """KCRS filters -> the ahead-of-time format whose bit `desc` carries (Winograd domain, or MFMA operand order)."""
     _check(lib().conv_transform_filters(ctypes.byref(desc), _ptr(filt), _ptr(out), _stream(stream)), "conv_transform_filters")
+
+
+# ---- operators on rows: layer norm, 8-bit rows and their product, log probabilities ------------------------------------
+
+
+def row_stride(cols: int) -> int:
+    """Row stride of an 8-bit tensor with `cols` columns: the next multiple of 16."""
+    return (int(cols) + 15) // 16 * 16
+
+
+def make_norm_desc(rows, cols, dtype=CONV_F32, eps=1e-5, ldx=None, ldy=None) -> norm_desc:
+    return norm_desc(rows, cols if ldx is None else ldx, cols if ldy is None else ldy, cols, dtype, eps)
+
+
+def make_quant_desc(rows, cols, dtype=CONV_F32, ldx=None, ldq=None) -> quant_desc:
+    return quant_desc(rows, cols if ldx is None else ldx, row_stride(cols) if ldq is None else ldq, cols, dtype)
+
+
+def make_int_linear_desc(rows, N, K, dtype=CONV_F32, relu=False, lda=None, ldw=None, ldo=None) -> int_linear_desc:
+    return int_linear_desc(rows, row_stride(K) if lda is None else lda, row_stride(K) if ldw is None else ldw,
+                           N if ldo is None else ldo, N, K, dtype, CONV_FLAG_RELU if relu else 0)
+
+
+def make_logprob_desc(rows, cols, dtype=CONV_F32, top=0, ldx=None, ldg=None) -> logprob_desc:
+    return logprob_desc(rows, cols if ldx is None else ldx, cols if ldg is None else ldg, cols, dtype, top)
+
+
+def layernorm_fwd(desc, x, gamma, beta, y, mean=None, rstd=None, stream=None) -> None:
+    _check(lib().layernorm_fwd(ctypes.byref(desc), _ptr(x), _ptr(gamma), _ptr(beta), _ptr(y), _ptr(mean), _ptr(rstd),
+                               _stream(stream)), "layernorm_fwd")
+
+
+def layernorm_quant_fwd(desc, x, gamma, beta, q, scale, stream=None) -> None:
+    """layernorm_fwd with its result in 8 bits (codes and scales of quantize_rows); desc.ldy is the row stride of q."""
+    _check(lib().layernorm_quant_fwd(ctypes.byref(desc), _ptr(x), _ptr(gamma), _ptr(beta), _ptr(q), _ptr(scale),
+                                     _stream(stream)), "layernorm_quant_fwd")
+
+
+def layernorm_bwd_workspace_bytes(desc) -> int:
+    return int(lib().layernorm_bwd_workspace_bytes(ctypes.byref(desc)))
+
+
+def layernorm_bwd(desc, x, dy, gamma, mean, rstd, dx, dgamma, dbeta, workspace=None, workspace_bytes=0, stream=None) -> None:
+    _check(lib().layernorm_bwd(ctypes.byref(desc), _ptr(x), _ptr(dy), _ptr(gamma), _ptr(mean), _ptr(rstd), _ptr(dx),
+                               _ptr(dgamma), _ptr(dbeta), _ptr(workspace), int(workspace_bytes), _stream(stream)), "layernorm_bwd")
+
+
+def quantize_rows(desc, x, q, scale, stream=None) -> None:
+    _check(lib().quantize_rows(ctypes.byref(desc), _ptr(x), _ptr(q), _ptr(scale), _stream(stream)), "quantize_rows")
+
+
+def int_linear_workspace_bytes(desc) -> int:
+    return int(lib().int_linear_workspace_bytes(ctypes.byref(desc)))
+
+
+def int_linear_fwd(desc, a, a_scale, w, w_scale, bias, out, workspace=None, workspace_bytes=0, stream=None) -> None:
+    _check(lib().int_linear_fwd(ctypes.byref(desc), _ptr(a), _ptr(a_scale), _ptr(w), _ptr(w_scale), _ptr(bias), _ptr(out),
+                                _ptr(workspace), int(workspace_bytes), _stream(stream)), "int_linear_fwd")
+
+
+def logprob_workspace_bytes(desc) -> int:
+    return int(lib().logprob_workspace_bytes(ctypes.byref(desc)))
+
+
+def logprob_fwd(desc, logits, target, logp, lse=None, entropy=None, top_id=None, top_logp=None, workspace=None,
+                workspace_bytes=0, stream=None) -> None:
+    _check(lib().logprob_fwd(ctypes.byref(desc), _ptr(logits), _ptr(target), _ptr(logp), _ptr(lse), _ptr(entropy), _ptr(top_id),
+                             _ptr(top_logp), _ptr(workspace), int(workspace_bytes), _stream(stream)), "logprob_fwd")
+
+
+def logprob_bwd(desc, logits, target, lse, entropy, g_logp, g_entropy, dlogits, stream=None) -> None:
+    _check(lib().logprob_bwd(ctypes.byref(desc), _ptr(logits), _ptr(target), _ptr(lse), _ptr(entropy), _ptr(g_logp),
+                             _ptr(g_entropy), _ptr(dlogits), _stream(stream)), "logprob_bwd")
 
 
 def conv_probe_mfma_peak(dtype: int, block: int, scratch, stream=None) -> float:

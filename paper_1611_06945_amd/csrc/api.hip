@@ -128,6 +128,12 @@ int hip_fail(hipError_t e, const char* what)
     return CONV_EHIP;
 }
 
+}  // namespace
+
+int convfwd::hip_status(hipError_t e, const char* what) { return hip_fail(e, what); }
+
+namespace {
+
 constexpr uint32_t kLayoutFlags = CONV_FLAG_IN_NHWC | CONV_FLAG_OUT_NHWC | CONV_FLAG_FILT_KRSC;
 constexpr uint32_t kKnownFlags =
     CONV_FLAG_RELU | kLayoutFlags | CONV_FLAG_FILT_WINOGRAD | CONV_FLAG_MAXPOOL_3X3S2 | CONV_FLAG_FILT_PACKED;

@@ -227,6 +227,76 @@ hipError_t probe_mfma(int dtype, int block, float* sink, hipStream_t s, double* 
 hipError_t probe_mfma_mix(int dtype, int block, int wps, int nv, int distinct, float* sink, hipStream_t s, double* tflops, double* ns);
 hipError_t probe_copy(const void* src, void* dst, size_t bytes, hipStream_t s, double* gbs);
 
+// CONV_EHIP with the message of a failed HIP call kept for conv_strerror (api.hip).
+int hip_status(hipError_t e, const char* what);
+
+// Operators on rows (layer norm, row quantiser, 8-bit product, log probabilities): what the kernels need, passed by value.
+// Pointers and strides as in the functions of include/convfwd.h with the same names; null where the caller gave none.
+struct NormArgs {
+    const void* x;
+    const void* dy;      // backward
+    const float* gamma;
+    const float* beta;
+    void* y;             // forward: the result
+    int8_t* q;           // forward: the result in 8 bits, instead of y
+    float* scale;        // ... and its scales
+    float* mean;         // forward: written where not null; backward: read
+    float* rstd;
+    void* dx;
+    float* dgamma;
+    float* dbeta;
+    float* ws;           // backward: partial sums [workgroups][2][cols]
+    int64_t rows, ldx, ldy;
+    int cols;
+    float eps;
+};
+hipError_t launch_layernorm_fwd(NormArgs& a, int dtype, hipStream_t s);
+hipError_t launch_layernorm_bwd(NormArgs& a, int dtype, hipStream_t s);
+size_t layernorm_bwd_workspace(int64_t rows, int cols, int dtype);
+
+struct QuantArgs {
+    const void* x;
+    int8_t* q;
+    float* scale;
+    int64_t rows, ldx, ldq;
+    int cols;
+};
+hipError_t launch_quantize_rows(QuantArgs& a, int dtype, hipStream_t s);
+
+struct IntLinearArgs {
+    const int8_t* a;
+    const float* a_scale;
+    const int8_t* w;
+    const float* w_scale;
+    const float* bias;
+    void* out;
+    int* ws;             // partial sums
+    int64_t rows, lda, ldw, ldo;
+    int N, K;
+    int relu;
+};
+hipError_t launch_int_linear(IntLinearArgs& a, int dtype, hipStream_t s);
+size_t int_linear_workspace(int64_t rows, int N, int K);
+
+struct LogprobArgs {
+    const void* x;
+    const int64_t* target;
+    float* logp;         // forward: outputs, null where not asked for
+    float* lse;          // forward: output; backward: input
+    float* entropy;
+    int64_t* top_id;
+    float* top_logp;
+    const float* g_logp;
+    const float* g_entropy;
+    void* dx;
+    void* ws;
+    int64_t rows, ldx, ldg;
+    int cols, top;
+};
+hipError_t launch_logprob_fwd(LogprobArgs& a, int dtype, hipStream_t s);
+hipError_t launch_logprob_bwd(LogprobArgs& a, int dtype, hipStream_t s);
+size_t logprob_workspace(int64_t rows, int cols, int top);
+
 inline const char* dtype_name(int dt) { return dt == CONV_F32 ? "f32" : dt == CONV_F16 ? "f16" : "bf16"; }
 inline int dtype_size(int dt) { return dt == CONV_F32 ? 4 : 2; }
 

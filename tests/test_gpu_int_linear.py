@@ -1,0 +1,115 @@
+"""The product in 8-bit integers on the GPU: sums are exact, so only the scaling, the bias and the rounding are held to bounds."""
+import numpy as np
+import pytest
+
+from oracle import rows_oracle as ro
+from paper_1611_06945_amd import binding as B
+from paper_1611_06945_amd import workloads as wl
+
+from gpu_util import torch_mod
+from rows_util import EPS32, ROUND, TINY, Rows, assert_close, torch_type, vec
+
+pytestmark = pytest.mark.gpu
+
+DTYPES = [wl.F32, wl.F16, wl.BF16]
+
+
+def check(rows, N, K, dtype, relu=False, bias=True, pad=0, ldo=None, start=0, seed=0, extreme=False, nan_row=None):
+    torch = torch_mod()
+    rng = np.random.default_rng(seed + rows + 7 * N + 13 * K)
+    lo, hi = (-128, -128) if extreme else (-128, 127)
+    a, w = rng.integers(lo, hi + 1, size=(rows, K)).astype(np.int8), rng.integers(lo, hi + 1, size=(N, K)).astype(np.int8)
+    sa, sw = rng.uniform(0.5, 2, rows).astype(np.float32) / 1000, rng.uniform(0.5, 2, N).astype(np.float32) / 1000
+    if nan_row is not None:
+        sa[nan_row] = np.nan
+    b = rng.normal(size=N).astype(np.float32) if bias else None
+    # what lies behind the columns is read up to the next 16 bytes: its values must not matter
+    A = Rows(rows, K, torch.int8, B.row_stride(K) + pad, fill=77).set(a)
+    W = Rows(N, K, torch.int8, B.row_stride(K) + 2 * pad, fill=-55).set(w)
+    Y = Rows(rows, N, torch_type(dtype), ldo, start, fill=7.0)
+    d = B.make_int_linear_desc(rows, N, K, dtype, relu, A.ld, W.ld, Y.ld)
+    need = B.int_linear_workspace_bytes(d)
+    ws = torch.full((max(need, 16),), 0xFF, dtype=torch.uint8, device="cuda")
+    B.int_linear_fwd(d, A.ptr, vec(sa), W.ptr, vec(sw), None if b is None else vec(b), Y.ptr, ws, need)
+    torch.cuda.synchronize()
+    v, size = ro.int_linear(a, sa, w, sw, b, relu)
+    if nan_row is not None:
+        v[nan_row] = np.nan
+    tol = 5 * EPS32 * size
+    assert_close(Y.host(), v, tol + ROUND[dtype] * (np.abs(v) + tol) + TINY[dtype], "out")
+    assert Y.untouched()
+    return Y
+
+
+ROWS = [1, 2, 3, 7, 8, 15, 16, 17, 31, 33, 63, 65, 100, 129]
+
+
+@pytest.mark.parametrize("rows", ROWS)
+@pytest.mark.parametrize("N,K", [(1, 1), (10, 17), (16, 64), (33, 63), (100, 128), (130, 65), (257, 300), (64, 1001)])
+def test_small_products(rows, N, K):
+    check(rows, N, K, DTYPES[(rows + N) % 3], relu=bool(N % 2), bias=bool(K % 2), pad=16 * (rows % 3), seed=1)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rows,N,K", [(1, 4096, 4096), (1, 1000, 16384), (5, 4096, 9216), (20, 1000, 4096), (16, 16, 16384), (32, 513, 2050), (64, 2048, 1024),
+                                      (200, 1003, 999), (777, 1283, 1001), (256, 256, 128), (257, 255, 129), (512, 512, 512), (1000, 128, 4096), (129, 3000, 384),
+                                      (1024, 1024, 256), (1300, 1111, 640), (2048, 768, 1600)])
+def test_products(rows, N, K, dtype):
+    check(rows, N, K, dtype, relu=rows % 2 == 0, seed=2)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rows,N,ldo,start", [(3, 50, 53, 1), (40, 130, 131, 3), (300, 300, 311, 5), (300, 260, 264, 1), (600, 512, 520, 0), (17, 1001, 1002, 2)])
+def test_outputs_that_are_slices(rows, N, ldo, start, dtype):
+    check(rows, N, 200, dtype, ldo=ldo, start=start, pad=48, seed=3)
+
+
+@pytest.mark.parametrize("rows", [1, 20, 300])
+def test_the_largest_sums(rows):
+    check(rows, 40, (1 << 17) - 1, wl.F32, extreme=True, seed=4)
+
+
+@pytest.mark.parametrize("rows", [3, 40, 300])
+@pytest.mark.parametrize("relu", [False, True])
+def test_a_row_whose_scale_is_nan_is_nan(rows, relu):
+    check(rows, 70, 100, wl.F16, relu=relu, nan_row=rows - 1, seed=5)
+
+
+@pytest.mark.parametrize("rows", [1, 18, 130, 700])
+def test_the_same_call_gives_the_same_bits(rows):
+    a, b = (check(rows, 300, 2000, wl.F32, seed=6).host() for _ in range(2))
+    assert np.array_equal(a, b)
+
+
+def test_more_rows_than_one_launch_holds():
+    """65535 tiles of rows are one launch's; a narrow product over more of them against the sums by hand."""
+    torch = torch_mod()
+    rows, N, K = 65535 * 16 + 37, 3, 16
+    g = torch.Generator(device="cuda")
+    g.manual_seed(3)
+    a = torch.randint(-128, 128, (rows, K), generator=g, device="cuda", dtype=torch.int8)
+    w = torch.randint(-128, 128, (N, K), generator=g, device="cuda", dtype=torch.int8)
+    one_a, one_w = torch.ones(rows, device="cuda"), torch.ones(N, device="cuda")
+    out = torch.full((rows, N), float("nan"), device="cuda")
+    d = B.make_int_linear_desc(rows, N, K)
+    need = B.int_linear_workspace_bytes(d)
+    ws = torch.empty(max(need, 16), dtype=torch.uint8, device="cuda")
+    B.int_linear_fwd(d, a, one_a, w, one_w, None, out, ws, need)
+    want = (a.float()[:, None, :] * w.float()[None]).sum(2)
+    assert bool((out == want).all())
+
+
+def test_operands_beyond_four_gigabytes():
+    """Rows whose offsets pass 32 bits, in the 8-bit operand and in the output."""
+    torch = torch_mod()
+    rows, N, K, lda, ldo = 600, 130, 96, 1 << 23, 1 << 22   # 5.0e9 bytes of a, 1.0e10 bytes of an fp32 output
+    a = torch.zeros(rows * lda, dtype=torch.int8, device="cuda").view(rows, lda)
+    a[:, :K] = torch.randint(-128, 128, (rows, K), device="cuda", dtype=torch.int8)
+    w = torch.randint(-128, 128, (N, K), device="cuda", dtype=torch.int8)
+    out = torch.zeros(rows * ldo, device="cuda").view(rows, ldo)
+    d = B.make_int_linear_desc(rows, N, K, wl.F32, lda=lda, ldo=ldo)
+    need = B.int_linear_workspace_bytes(d)
+    ws = torch.empty(max(need, 16), dtype=torch.uint8, device="cuda")
+    B.int_linear_fwd(d, a, torch.ones(rows, device="cuda"), w, torch.ones(N, device="cuda"), None, out, ws, need)
+    want = a[:, :K].contiguous().float() @ w.float().t().contiguous()
+    assert bool((out[:, :N] == want).all()) and bool((out[:, N:N + 64] == 0).all())

@@ -1,0 +1,221 @@
+"""The operators on rows without a GPU: refusals of every entry point, empty calls, and the oracle against closed forms and
+differences."""
+import ctypes
+
+import numpy as np
+import pytest
+
+from oracle import rows_oracle as ro
+from paper_1611_06945_amd import binding as B
+
+P = 1 << 20  # an aligned address that is never read: every call here ends before the first HIP call
+
+
+def status(call, *args, **kw):
+    try:
+        call(*args, **kw)
+    except B.ConvError as e:
+        return e.status
+    return B.CONV_OK
+
+
+NORM_BAD = [dict(rows=-1), dict(rows=1 << 31), dict(cols=0), dict(cols=1 << 30), dict(ldx=7), dict(ldy=7), dict(eps=-1.0),
+            dict(eps=float("nan")), dict(eps=float("inf"))]
+
+
+@pytest.mark.parametrize("change", NORM_BAD)
+def test_norm_descriptors_that_are_refused(change):
+    d = B.make_norm_desc(4, 8)
+    for k, v in change.items():
+        setattr(d, k, v)
+    if change == dict(cols=1 << 30):
+        d.ldx = d.ldy = 1 << 30
+    assert status(B.layernorm_fwd, d, P, P, P, 2 * P, P, P, stream=0) == B.CONV_EINVAL
+    assert status(B.layernorm_quant_fwd, d, P, P, P, 2 * P, P, stream=0) == B.CONV_EINVAL
+    assert status(B.layernorm_bwd, d, P, 2 * P, P, P, P, 3 * P, P, P, P, 1 << 20, stream=0) == B.CONV_EINVAL
+    assert B.layernorm_bwd_workspace_bytes(d) == 0
+
+
+def test_norm_pointers_that_are_refused():
+    d = B.make_norm_desc(4, 8, B.CONV_F32)
+    assert status(B.layernorm_fwd, d, None, P, P, 2 * P, stream=0) == B.CONV_EINVAL
+    assert status(B.layernorm_fwd, d, P, P, P, None, stream=0) == B.CONV_EINVAL
+    assert status(B.layernorm_fwd, d, P, P, P, P, stream=0) == B.CONV_EINVAL                # in place
+    assert status(B.layernorm_fwd, d, P + 2, P, P, 2 * P, stream=0) == B.CONV_EINVAL        # not on an element
+    assert status(B.layernorm_fwd, d, P, P + 2, P, 2 * P, stream=0) == B.CONV_EINVAL
+    assert status(B.layernorm_fwd, d, P, P, P, 2 * P, P + 1, stream=0) == B.CONV_EINVAL
+    d.dtype = 3
+    assert status(B.layernorm_fwd, d, P, P, P, 2 * P, stream=0) == B.CONV_EDTYPE
+    assert status(B.layernorm_bwd, d, P, P, P, P, P, 2 * P, P, P, P, 1 << 20, stream=0) == B.CONV_EDTYPE
+    d = B.make_norm_desc(4, 8, ldy=16)
+    assert status(B.layernorm_quant_fwd, d, P, P, P, 2 * P + 8, P, stream=0) == B.CONV_EINVAL  # 8-bit rows start on 16 bytes
+    assert status(B.layernorm_quant_fwd, d, P, P, P, 2 * P, None, stream=0) == B.CONV_EINVAL
+    d.ldy = 24
+    assert status(B.layernorm_quant_fwd, d, P, P, P, 2 * P, P, stream=0) == B.CONV_EINVAL
+    assert B.lib().layernorm_fwd(None, P, P, P, 2 * P, P, P, None) == B.CONV_EINVAL
+    assert B.lib().layernorm_bwd_workspace_bytes(None) == 0
+
+
+def test_norm_bwd_arguments_that_are_refused():
+    d = B.make_norm_desc(40, 8)
+    ws = B.layernorm_bwd_workspace_bytes(d)
+    assert ws > 0
+    ok = dict(stream=0)
+    assert status(B.layernorm_bwd, d, P, P, P, P, P, None, None, None, P, ws, **ok) == B.CONV_EINVAL      # nothing asked for
+    assert status(B.layernorm_bwd, d, P, 2 * P, P, None, P, 3 * P, P, P, P, ws, **ok) == B.CONV_EINVAL
+    assert status(B.layernorm_bwd, d, P, 2 * P, P, P, None, 3 * P, P, P, P, ws, **ok) == B.CONV_EINVAL
+    assert status(B.layernorm_bwd, d, P, 2 * P, P, P, P, P, P, P, P, ws, **ok) == B.CONV_EINVAL           # dx over x
+    assert status(B.layernorm_bwd, d, P, 2 * P, P, P, P, 3 * P, P, P, None, 0, **ok) == B.CONV_EWORKSPACE
+    assert status(B.layernorm_bwd, d, P, 2 * P, P, P, P, 3 * P, P, P, P, ws - 1, **ok) == B.CONV_EWORKSPACE
+    assert status(B.layernorm_bwd, d, P, 2 * P, P, P, P, 3 * P, P, P, P + 8, ws, **ok) == B.CONV_EINVAL
+    d.ldx = 9
+    assert status(B.layernorm_bwd, d, P, 2 * P, P, P, P, 2 * P, P, P, P, ws, **ok) == B.CONV_EINVAL       # dx over dy, other strides
+
+
+@pytest.mark.parametrize("change", [dict(rows=-1), dict(cols=0), dict(ldx=7), dict(ldq=0), dict(ldq=24), dict(rows=1 << 31)])
+def test_quantize_descriptors_that_are_refused(change):
+    d = B.make_quant_desc(4, 8)
+    for k, v in change.items():
+        setattr(d, k, v)
+    assert status(B.quantize_rows, d, P, 2 * P, P, stream=0) == B.CONV_EINVAL
+
+
+def test_quantize_pointers_that_are_refused():
+    d = B.make_quant_desc(4, 8, B.CONV_F16)
+    for args in ((None, 2 * P, P), (P, None, P), (P, 2 * P, None), (P, P, P), (P + 1, 2 * P, P), (P, 2 * P + 4, P), (P, 2 * P, P + 2)):
+        assert status(B.quantize_rows, d, *args, stream=0) == B.CONV_EINVAL, args
+    d.dtype = -1
+    assert status(B.quantize_rows, d, P, 2 * P, P, stream=0) == B.CONV_EDTYPE
+    assert B.lib().quantize_rows(None, P, 2 * P, P, None) == B.CONV_EINVAL
+
+
+@pytest.mark.parametrize("change", [dict(rows=-1), dict(rows=1 << 31), dict(N=0), dict(K=0), dict(K=1 << 17, lda=1 << 17, ldw=1 << 17), dict(lda=16),
+                                    dict(ldw=16), dict(lda=40), dict(ldw=40), dict(ldo=9), dict(flags=2)])
+def test_int_linear_descriptors_that_are_refused(change):
+    d = B.make_int_linear_desc(4, 10, 20)
+    for k, v in change.items():
+        setattr(d, k, v)
+    assert status(B.int_linear_fwd, d, P, P, 2 * P, P, P, 3 * P, P, 1 << 20, stream=0) == B.CONV_EINVAL
+    assert B.int_linear_workspace_bytes(d) == 0
+
+
+def test_int_linear_pointers_that_are_refused():
+    d = B.make_int_linear_desc(4, 10, 20, B.CONV_BF16)
+    good = [P, P, 2 * P, P, P, 3 * P]
+    for i, bad in ((0, None), (1, None), (2, None), (3, None), (5, None), (0, P + 8), (2, P + 8), (1, P + 2), (4, P + 2), (5, P + 1), (5, P), (5, 2 * P)):
+        args = list(good)
+        args[i] = bad
+        assert status(B.int_linear_fwd, d, *args, P, 1 << 20, stream=0) == B.CONV_EINVAL, (i, bad)
+    d.dtype = 5
+    assert status(B.int_linear_fwd, d, *good, P, 1 << 20, stream=0) == B.CONV_EDTYPE
+    assert B.lib().int_linear_fwd(None, P, P, P, P, P, P, None, 0, None) == B.CONV_EINVAL
+
+
+@pytest.mark.parametrize("change", [dict(rows=-1), dict(rows=1 << 31), dict(cols=0), dict(ldx=99), dict(ldg=99), dict(top=-1), dict(top=65), dict(top=101)])
+def test_logprob_descriptors_that_are_refused(change):
+    d = B.make_logprob_desc(4, 100, top=5)
+    for k, v in change.items():
+        setattr(d, k, v)
+    assert status(B.logprob_fwd, d, P, P, P, P, P, P, P, P, 1 << 20, stream=0) == B.CONV_EINVAL
+    assert status(B.logprob_bwd, d, P, P, P, P, P, P, 2 * P, stream=0) == B.CONV_EINVAL
+    assert B.logprob_workspace_bytes(d) == 0
+
+
+def test_logprob_more_alternatives_than_columns():
+    d = B.make_logprob_desc(4, 3, top=4)
+    assert status(B.logprob_fwd, d, P, P, P, P, P, P, P, P, 1 << 20, stream=0) == B.CONV_EINVAL
+
+
+def test_logprob_pointers_that_are_refused():
+    d = B.make_logprob_desc(4, 100, B.CONV_F16, top=5)
+    good = [P, P, P, P, P, P, P]  # logits target logp lse entropy top_id top_logp
+    for i, bad in ((0, None), (1, None), (0, P + 1), (1, P + 4), (2, P + 2), (3, P + 1), (5, P + 4), (5, None), (6, None)):
+        args = list(good)
+        args[i] = bad
+        assert status(B.logprob_fwd, d, *args, P, 1 << 20, stream=0) == B.CONV_EINVAL, (i, bad)
+    assert status(B.logprob_fwd, d, P, P, None, None, None, None, None, P, 1 << 20, stream=0) == B.CONV_EINVAL  # nothing asked for
+    good = [P, P, P, P, P, P, 2 * P]  # logits target lse entropy g_logp g_entropy dlogits
+    for i, bad in ((0, None), (1, None), (2, None), (3, None), (6, None), (6, P + 1), (4, P + 2)):
+        args = list(good)
+        args[i] = bad
+        assert status(B.logprob_bwd, d, *args, stream=0) == B.CONV_EINVAL, (i, bad)
+    assert status(B.logprob_bwd, d, P, P, P, P, None, None, 2 * P, stream=0) == B.CONV_EINVAL
+    d.ldg = 104
+    assert status(B.logprob_bwd, d, P, P, P, P, P, P, P, stream=0) == B.CONV_EINVAL  # in place with other strides
+    d.dtype = 9
+    assert status(B.logprob_fwd, d, P, P, P, P, P, P, P, P, 1 << 20, stream=0) == B.CONV_EDTYPE
+    assert B.lib().logprob_fwd(None, P, P, P, P, P, P, P, P, 0, None) == B.CONV_EINVAL
+    assert B.lib().logprob_bwd(None, P, P, P, P, P, P, P, None) == B.CONV_EINVAL
+
+
+def test_no_rows_is_a_valid_call_that_enqueues_nothing():
+    assert status(B.layernorm_fwd, B.make_norm_desc(0, 8), None, None, None, None, stream=0) == B.CONV_OK
+    assert status(B.layernorm_quant_fwd, B.make_norm_desc(0, 8, ldy=16), None, None, None, None, None, stream=0) == B.CONV_OK
+    assert status(B.layernorm_bwd, B.make_norm_desc(0, 8), None, None, None, None, None, P, None, None, stream=0) == B.CONV_OK
+    assert status(B.quantize_rows, B.make_quant_desc(0, 8), None, None, None, stream=0) == B.CONV_OK
+    assert status(B.int_linear_fwd, B.make_int_linear_desc(0, 8, 8), None, None, None, None, None, None, stream=0) == B.CONV_OK
+    assert status(B.logprob_fwd, B.make_logprob_desc(0, 8), None, None, None, stream=0) == B.CONV_OK
+    assert status(B.logprob_bwd, B.make_logprob_desc(0, 8), None, P, None, None, P, None, None, stream=0) == B.CONV_OK
+
+
+def test_descriptor_sizes_match_the_header():
+    assert ctypes.sizeof(B.norm_desc) == 40 and ctypes.sizeof(B.quant_desc) == 32
+    assert ctypes.sizeof(B.int_linear_desc) == 48 and ctypes.sizeof(B.logprob_desc) == 40
+
+
+# ---- the oracle ------------------------------------------------------------------------------------------------------
+
+
+def test_oracle_layernorm_closed_forms_and_differences():
+    rng = np.random.default_rng(1)
+    y, mean, rstd = ro.layernorm(np.array([[1.0, 3.0]]), None, None, 0.0)
+    assert np.allclose(y, [[-1, 1]]) and mean[0] == 2 and rstd[0] == 1
+    x, dy = rng.normal(size=(3, 7)), rng.normal(size=(3, 7))
+    gamma, beta = rng.normal(size=7), rng.normal(size=7)
+    loss = lambda x, g, b: float((ro.layernorm(x, g, b, 1e-5)[0] * dy).sum())  # noqa: E731
+    _, mean, rstd = ro.layernorm(x, gamma, beta, 1e-5)
+    dx, dg, db = ro.layernorm_bwd(x, dy, gamma, mean, rstd)
+    h = 1e-6
+    for i in range(3):
+        for j in range(7):
+            e = np.zeros_like(x)
+            e[i, j] = h
+            assert abs((loss(x + e, gamma, beta) - loss(x - e, gamma, beta)) / (2 * h) - dx[i, j]) < 1e-7
+    for j in range(7):
+        e = np.zeros(7)
+        e[j] = h
+        assert abs((loss(x, gamma + e, beta) - loss(x, gamma - e, beta)) / (2 * h) - dg[j]) < 1e-7
+        assert abs((loss(x, gamma, beta + e) - loss(x, gamma, beta - e)) / (2 * h) - db[j]) < 1e-7
+
+
+def test_oracle_quantize_and_product():
+    q, s = ro.quantize_rows(np.array([[127.0, -63.5, 0.49, 62.5], [0, 0, 0, 0], [1, np.nan, 2, 3]], dtype=np.float32))
+    assert q[0].tolist() == [127, -64, 0, 62] and abs(s[0] - 1) < 1e-6
+    assert q[1].tolist() == [0] * 4 and s[1] == np.float32(2.0 ** -126)
+    assert q[2].tolist() == [0] * 4 and np.isnan(s[2])
+    v, _ = ro.int_linear(np.array([[1, -2]], dtype=np.int8), np.array([2.0]), np.array([[3, 4], [5, -6]], dtype=np.int8), np.array([1.0, 0.5]), np.array([1.0, 0.0]), True)
+    assert v.tolist() == [[0.0, 17.0]]
+
+
+def test_oracle_logprob_closed_forms_and_differences():
+    rng = np.random.default_rng(2)
+    r = ro.logprob(np.zeros((1, 4)), np.array([2]), 3)
+    assert np.isclose(r["logp"][0], -np.log(4)) and np.isclose(r["entropy"][0], np.log(4)) and r["top_id"][0].tolist() == [0, 1, 2]
+    r = ro.logprob(np.array([[-np.inf, 0.0, -np.inf], [-np.inf] * 3, [0, np.nan, np.inf]]), np.array([0, 1, -1]), 2)
+    assert r["logp"].tolist() == [-np.inf, -np.inf, 0.0] and r["entropy"][:2].tolist() == [0.0, 0.0] and np.isnan(r["entropy"][2])
+    assert r["top_id"].tolist() == [[1, 0], [0, 1], [1, 2]]
+    x, gl, gh = rng.normal(size=(2, 6)) * 2, rng.normal(size=2), rng.normal(size=2)
+    target = np.array([3, -1])
+
+    def loss(x):
+        r = ro.logprob(x, target, 0)
+        return float((r["logp"] * gl + r["entropy"] * gh).sum())
+
+    r = ro.logprob(x, target, 0)
+    dx = ro.logprob_bwd(x, target, r["lse"], r["entropy"], gl, gh)
+    h = 1e-6
+    for i in range(2):
+        for j in range(6):
+            e = np.zeros_like(x)
+            e[i, j] = h
+            assert abs((loss(x + e) - loss(x - e)) / (2 * h) - dx[i, j]) < 1e-7
