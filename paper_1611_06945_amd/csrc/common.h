@@ -295,7 +295,7 @@ struct LogprobArgs {
 };
 hipError_t launch_logprob_fwd(LogprobArgs& a, int dtype, hipStream_t s);
 hipError_t launch_logprob_bwd(LogprobArgs& a, int dtype, hipStream_t s);
-size_t logprob_workspace(int64_t rows, int cols, int top);
+size_t logprob_workspace(int64_t rows, int cols, int top, int dtype);
 
 inline const char* dtype_name(int dt) { return dt == CONV_F32 ? "f32" : dt == CONV_F16 ? "f16" : "bf16"; }
 inline int dtype_size(int dt) { return dt == CONV_F32 ? 4 : 2; }

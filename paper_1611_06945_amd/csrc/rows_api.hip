@@ -161,7 +161,7 @@ int int_linear_fwd(const int_linear_desc* desc, const int8_t* a, const float* a_
 
 size_t logprob_workspace_bytes(const logprob_desc* desc)
 {
-    return check_logprob(desc) ? 0 : logprob_workspace(desc->rows, desc->cols, desc->top);
+    return check_logprob(desc) ? 0 : logprob_workspace(desc->rows, desc->cols, desc->top, desc->dtype);
 }
 
 int logprob_fwd(const logprob_desc* desc, const void* logits, const int64_t* target, float* logp, float* lse, float* entropy,
@@ -175,7 +175,7 @@ int logprob_fwd(const logprob_desc* desc, const void* logits, const int64_t* tar
     const bool top = top_id && desc->top > 0;
     if (!logits || !aligned(logits, dtype_size(desc->dtype)) || (logp && !target)) return CONV_EINVAL;
     if (!logp && !lse && !entropy && !top) return CONV_EINVAL;
-    const size_t need = logprob_workspace(desc->rows, desc->cols, desc->top);
+    const size_t need = logprob_workspace(desc->rows, desc->cols, desc->top, desc->dtype);
     if (need && (!workspace || workspace_bytes < need)) return CONV_EWORKSPACE;
     if (!aligned(workspace, 16)) return CONV_EINVAL;
     LogprobArgs a = {};
