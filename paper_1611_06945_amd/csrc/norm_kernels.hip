@@ -1,4 +1,10 @@
-// Layer norm forward and backward, and the row quantiser.
+// Layer norm forward and backward, and the row quantiser: one pass over the tensors, the row held in registers.
+//
+// G neighbouring lanes share a row (16, a wave, or a workgroup of 4 or 16 waves), each holding up to NV pieces of 16 bytes.  The mean
+// comes first and the variance is summed around it, from registers.  A workgroup keeps its columns' gamma and beta in registers over
+// all its rows, and asks for its next row before it works on the present one.  Backward, a lane adds up dgamma and dbeta of its columns
+// over its rows in registers; a workgroup's lanes with the same columns are added through LDS, and a second kernel adds the
+// workgroups' sums, always in the same order.  Longer rows than 16 waves hold are read again for every pass (`_any`).
 #include <algorithm>
 
 #include "rows_common.h"
@@ -36,91 +42,401 @@ struct OpKeep {
     static __device__ __forceinline__ float of(float a, float b) { return keep(a, b); }
 };
 
-// A workgroup a row, the row read again for every pass: rows of any length.
-template <int DT>
-__global__ __launch_bounds__(256) void norm_fwd_any(NormArgs a)
-{
+// The pieces of a row that a lane holds: lane l of G has pieces l, l + G, ...
+template <int DT, int G, int NV>
+struct Held {
     typedef typename Prec<DT>::elem_t elem_t;
-    __shared__ float red[3][4];
-    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
-    __syncthreads();
-    const elem_t* x = (const elem_t*)a.x + row * a.ldx;
-    float sum = 0.0f;
-    for (int j = threadIdx.x; j < a.cols; j += 256) sum += Prec<DT>::to_f32(x[j]);
-    const float mean = block_reduce<4, OpSum>(sum, red[0]) / (float)a.cols;
-    float sq = 0.0f;
-    for (int j = threadIdx.x; j < a.cols; j += 256) {
-        const float d = Prec<DT>::to_f32(x[j]) - mean;
-        sq = __builtin_fmaf(d, d, sq);
-    }
-    const float rstd = 1.0f / sqrtf(block_reduce<4, OpSum>(sq, red[1]) / (float)a.cols + a.eps);
-    auto value = [&](int j) {
-        float v = (Prec<DT>::to_f32(x[j]) - mean) * rstd;
-        if (a.gamma) v *= a.gamma[j];
-        if (a.beta) v += a.beta[j];
-        return Prec<DT>::from_f32(v);
-    };
-    if (!a.q) {
-        elem_t* y = (elem_t*)a.y + row * a.ldy;
-        for (int j = threadIdx.x; j < a.cols; j += 256) y[j] = value(j);
-        if (threadIdx.x == 0) {
-            if (a.mean) a.mean[row] = mean;
-            if (a.rstd) a.rstd[row] = rstd;
+    typedef Piece<DT> P;
+    static constexpr int VEC = P::VEC;
+
+    // Stored values; a piece past the end is not loaded, the elements of the last one past the end are zeros.
+    static __device__ __forceinline__ void load(uint4 (&raw)[NV], const elem_t* x, int cols, int l)
+    {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int j = (i * G + l) * VEC;
+            if (j + VEC <= cols) {
+                raw[i] = P::raw(x + j);
+            } else {
+                elem_t e[VEC];
+#pragma unroll
+                for (int k = 0; k < VEC; ++k) e[k] = j + k < cols ? x[j + k] : (elem_t)0;
+                __builtin_memcpy(&raw[i], e, 16);
+            }
         }
-        continue;
     }
-    float amax = 0.0f;
-    for (int j = threadIdx.x; j < a.cols; j += 256) amax = keep(amax, Prec<DT>::to_f32(value(j)));
-    const RowScale r = row_scale(block_reduce<4, OpKeep>(amax, red[2]));
-    int8_t* q = a.q + row * a.ldy;
+    static __device__ __forceinline__ void store(elem_t* y, const float (&v)[VEC], int cols, int i, int l)
+    {
+        const int j = (i * G + l) * VEC;
+        const uint4 u = P::narrow(v);
+        if (j + VEC <= cols) {
+            P::put(y + j, u);
+        } else if (j < cols) {
+            elem_t e[VEC];
+            __builtin_memcpy(e, &u, 16);
+#pragma unroll
+            for (int k = 0; k < VEC; ++k)
+                if (j + k < cols) y[j + k] = e[k];
+        }
+    }
+    // a vector over the columns, `none` where the pointer is null or the row has ended
+    static __device__ __forceinline__ void columns(float (&v)[NV][VEC], const float* p, float none, int cols, int l)
+    {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int j = (i * G + l) * VEC;
+            if (p && j + VEC <= cols) {
+                __builtin_memcpy(v[i], p + j, 4 * VEC);
+            } else {
+#pragma unroll
+                for (int k = 0; k < VEC; ++k) v[i][k] = p && j + k < cols ? p[j + k] : none;
+            }
+        }
+    }
+};
+
+// Combines a value over the G lanes of a row; `lds` holds a float for each wave of the workgroup and call within a row.
+template <int G, typename Op>
+__device__ __forceinline__ float row_reduce(float x, float* lds)
+{
+    if constexpr (G <= 64) return lanes_reduce<G, Op>(x);
+    else return block_reduce<G / 64, Op>(x, lds);
+}
+
+// Codes of a piece to q.  Pieces past the end up to the next multiple of 16 columns get zeros.
+template <int VEC>
+__device__ __forceinline__ void store_codes(int8_t* q, const float (&v)[VEC], const RowScale& r, int j, int cols, int padded)
+{
+    if (j >= padded) return;
+    uint32_t w[VEC / 4];
+#pragma unroll
+    for (int k = 0; k < VEC / 4; ++k) w[k] = 0;
+#pragma unroll
+    for (int k = 0; k < VEC; ++k) w[k / 4] |= ((uint32_t)code(j + k < cols ? v[k] : 0.0f, r) & 0xFFu) << (8 * (k % 4));
+    __builtin_memcpy(__builtin_assume_aligned(q + j, VEC), w, VEC);
+}
+
+enum { TO_FLOAT = 0, TO_CODES = 1, QUANT_ONLY = 2 };
+
+// Layer norm (to floats or codes), or the quantiser alone, which holds rows the same way.
+template <int DT, int G, int NV, int MODE>
+__global__ __launch_bounds__(G <= 256 ? 256 : G) void norm_fwd_rows(NormArgs a)
+{
+    typedef Held<DT, G, NV> H;
+    typedef typename H::elem_t elem_t;
+    constexpr int VEC = H::VEC, NT = G <= 256 ? 256 : G, ROWS = NT / G;
+    __shared__ float red[3][NT / 64];
+    const int l = threadIdx.x % G;
+    const int64_t step = (int64_t)gridDim.x * ROWS;
+    int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / G;
     const int padded = (a.cols + 15) & ~15;
-    for (int j = threadIdx.x; j < padded; j += 256) q[j] = j < a.cols ? (int8_t)code(Prec<DT>::to_f32(value(j)), r) : (int8_t)0;
-    if (threadIdx.x == 0) a.scale[row] = r.scale;
+    const float inv_cols = 1.0f / (float)a.cols;
+    auto at = [&](int64_t r) { return (const elem_t*)a.x + (r < a.rows ? r : a.rows - 1) * a.ldx; };
+
+    uint4 next[NV];
+    H::load(next, at(row), a.cols, l);
+    float gamma[NV][VEC], beta[NV][VEC];
+    if constexpr (MODE != QUANT_ONLY) {
+        H::columns(gamma, a.gamma, 1.0f, a.cols, l);
+        H::columns(beta, a.beta, 0.0f, a.cols, l);
+    }
+    // every lane of a workgroup makes the same number of rounds: the reductions of wide rows have barriers
+    for (int64_t first = (int64_t)blockIdx.x * ROWS; first < a.rows; first += step, row += step) {
+        float x[NV][VEC];
+#pragma unroll
+        for (int i = 0; i < NV; ++i) H::P::widen(next[i], x[i]);
+        if (first + step < a.rows) H::load(next, at(row + step), a.cols, l);
+        if constexpr (MODE != QUANT_ONLY) {
+            float sum = 0.0f;
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+#pragma unroll
+                for (int k = 0; k < VEC; ++k) sum += x[i][k];
+            const float mean = row_reduce<G, OpSum>(sum, red[0]) * inv_cols;
+            float sq = 0.0f;
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const int left = a.cols - (i * G + l) * VEC;
+#pragma unroll
+                for (int k = 0; k < VEC; ++k) {
+                    x[i][k] -= mean;
+                    if (left < VEC) x[i][k] = k < left ? x[i][k] : 0.0f;
+                    sq = __builtin_fmaf(x[i][k], x[i][k], sq);
+                }
+            }
+            const float rstd = 1.0f / sqrtf(row_reduce<G, OpSum>(sq, red[1]) * inv_cols + a.eps);
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+#pragma unroll
+                for (int k = 0; k < VEC; ++k) x[i][k] = __builtin_fmaf(x[i][k] * rstd, gamma[i][k], beta[i][k]);
+            if constexpr (MODE == TO_FLOAT) {
+                if (row < a.rows) {
+#pragma unroll
+                    for (int i = 0; i < NV; ++i) H::store((elem_t*)a.y + row * a.ldy, x[i], a.cols, i, l);
+                    if (l == 0) {
+                        if (a.mean) a.mean[row] = mean;
+                        if (a.rstd) a.rstd[row] = rstd;
+                    }
+                }
+            } else {
+                // the codes are those of the rounded values
+#pragma unroll
+                for (int i = 0; i < NV; ++i) H::P::widen(H::P::narrow(x[i]), x[i]);
+            }
+        }
+        if constexpr (MODE != TO_FLOAT) {
+            float amax = 0.0f;
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const int left = a.cols - (i * G + l) * VEC;
+#pragma unroll
+                for (int k = 0; k < VEC; ++k) amax = keep(amax, k < left ? x[i][k] : 0.0f);
+            }
+            const RowScale r = row_scale(row_reduce<G, OpKeep>(amax, red[2]));
+            if (row < a.rows) {
+#pragma unroll
+                for (int i = 0; i < NV; ++i) store_codes<VEC>(a.q + row * a.ldy, x[i], r, (i * G + l) * VEC, a.cols, padded);
+                if (l == 0) a.scale[row] = r.scale;
+            }
+        }
+        if constexpr (G > 64) __syncthreads();  // the next row's reductions use the same LDS
+    }
+}
+
+// Backward.  DX: dx is asked for; DW: dgamma or dbeta is.  A workgroup's sums go to ws, or, where there is one workgroup only, to their place.
+template <int DT, int G, int NV, int NT, bool DX, bool DW>
+__global__ __launch_bounds__(NT) void norm_bwd_rows(NormArgs a)
+{
+    typedef Held<DT, G, NV> H;
+    typedef typename H::elem_t elem_t;
+    constexpr int VEC = H::VEC, ROWS = NT / G, WAVES = NT / 64, SETS = G <= 64 ? WAVES : ROWS;
+    __shared__ float red[2][WAVES];
+    __shared__ float sums[DW && SETS > 1 ? 2 * G * NV * VEC : 1];
+    const int tid = threadIdx.x, l = tid % G;
+    const int64_t step = (int64_t)gridDim.x * ROWS;
+    int64_t row = (int64_t)blockIdx.x * ROWS + tid / G;
+    const float inv_cols = 1.0f / (float)a.cols;
+    auto clamp = [&](int64_t r) { return r < a.rows ? r : a.rows - 1; };
+
+    uint4 nx[NV], ndy[NV];
+    float nmean, nrstd;
+    auto fetch = [&](int64_t r) {
+        r = clamp(r);
+        H::load(nx, (const elem_t*)a.x + r * a.ldx, a.cols, l);
+        H::load(ndy, (const elem_t*)a.dy + r * a.ldy, a.cols, l);
+        nmean = a.mean[r], nrstd = a.rstd[r];
+    };
+    if (a.rows) fetch(row);
+    float gamma[NV][VEC], dg[NV][VEC], db[NV][VEC];
+    if constexpr (DX) H::columns(gamma, a.gamma, 1.0f, a.cols, l);
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) dg[i][k] = db[i][k] = 0.0f;
+
+    for (int64_t first = (int64_t)blockIdx.x * ROWS; first < a.rows; first += step, row += step) {
+        float x[NV][VEC], dy[NV][VEC];
+        const float mean = nmean, rstd = nrstd;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            H::P::widen(nx[i], x[i]);
+            H::P::widen(ndy[i], dy[i]);
+        }
+        if (first + step < a.rows) fetch(row + step);
+        const bool in = row < a.rows;
+        float s1 = 0.0f, s2 = 0.0f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int k = 0; k < VEC; ++k) {
+                x[i][k] = (x[i][k] - mean) * rstd;  // past the end dy is 0
+                if constexpr (DW) {
+                    if (in) {
+                        dg[i][k] = __builtin_fmaf(dy[i][k], x[i][k], dg[i][k]);
+                        db[i][k] += dy[i][k];
+                    }
+                }
+                if constexpr (DX) {
+                    dy[i][k] *= gamma[i][k];
+                    s1 += dy[i][k];
+                    s2 = __builtin_fmaf(dy[i][k], x[i][k], s2);
+                }
+            }
+        if constexpr (DX) {
+            float c1, c2;
+            if constexpr (G <= 64) {
+                c1 = lanes_reduce<G, OpSum>(s1) * inv_cols, c2 = lanes_reduce<G, OpSum>(s2) * inv_cols;
+            } else {
+                // the waves of this row; other rows of the workgroup have waves of their own
+                constexpr int W = G / 64;
+                s1 = lanes_reduce<64, OpSum>(s1), s2 = lanes_reduce<64, OpSum>(s2);
+                const int wave = tid >> 6, w0 = wave / W * W;
+                if ((tid & 63) == 0) red[0][wave] = s1, red[1][wave] = s2;
+                __syncthreads();
+                s1 = red[0][w0], s2 = red[1][w0];
+#pragma unroll
+                for (int w = 1; w < W; ++w) s1 += red[0][w0 + w], s2 += red[1][w0 + w];
+                c1 = s1 * inv_cols, c2 = s2 * inv_cols;
+                __syncthreads();
+            }
+            if (in) {
+#pragma unroll
+                for (int i = 0; i < NV; ++i) {
+                    float v[VEC];
+#pragma unroll
+                    for (int k = 0; k < VEC; ++k) v[k] = rstd * (dy[i][k] - c1 - x[i][k] * c2);
+                    H::store((elem_t*)a.dx + row * a.ldx, v, a.cols, i, l);
+                }
+            }
+        }
+    }
+    if constexpr (DW) {
+        float* to_dg = gridDim.x == 1 ? a.dgamma : a.ws + (size_t)blockIdx.x * 2 * a.cols;
+        float* to_db = gridDim.x == 1 ? a.dbeta : a.ws + (size_t)blockIdx.x * 2 * a.cols + a.cols;
+        if constexpr (SETS == 1) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+#pragma unroll
+                for (int k = 0; k < VEC; ++k) {
+                    const int j = (i * G + l) * VEC + k;
+                    if (j < a.cols && to_dg) to_dg[j] = dg[i][k];
+                    if (j < a.cols && to_db) to_db[j] = db[i][k];
+                }
+            return;
+        }
+        // rows within a wave first, then wave by wave (or row by row) through LDS
+        if constexpr (G < 64) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+#pragma unroll
+                for (int k = 0; k < VEC; ++k) {
+                    dg[i][k] = across_rows<G>(dg[i][k]);
+                    db[i][k] = across_rows<G>(db[i][k]);
+                }
+        }
+        const int set = G <= 64 ? tid / 64 : tid / G;
+        const bool holder = G >= 64 || (tid & 63) < G;
+        for (int w = 0; w < SETS; ++w) {
+            if (set == w && holder) {
+#pragma unroll
+                for (int i = 0; i < NV; ++i)
+#pragma unroll
+                    for (int k = 0; k < VEC; ++k) {
+                        float* p = sums + (i * VEC + k) * G + l;  // a lane's neighbours are next to it: no bank twice
+                        p[0] = w ? p[0] + dg[i][k] : dg[i][k];
+                        p[G * NV * VEC] = w ? p[G * NV * VEC] + db[i][k] : db[i][k];
+                    }
+            }
+            __syncthreads();
+        }
+        for (int j = tid; j < a.cols; j += NT) {
+            const int piece = j / VEC;
+            const float* p = sums + ((piece / G) * VEC + j % VEC) * G + piece % G;
+            if (to_dg) to_dg[j] = p[0];
+            if (to_db) to_db[j] = p[G * NV * VEC];
+        }
+    }
+}
+
+// The sums of `parts` workgroups: 64 columns and 16 waves a workgroup, a wave every 16th part, then the waves in order.
+__global__ __launch_bounds__(1024) void norm_dw_join(NormArgs a, int parts)
+{
+    __shared__ float red[16][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t j = (int64_t)blockIdx.x * 64 + lane;  // dgamma's columns, then dbeta's
+    float s = 0.0f;
+    if (j < 2 * (int64_t)a.cols) {
+        int p = wave;
+        for (; p + 48 < parts; p += 64) {
+            float v[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) v[u] = a.ws[(size_t)(p + 16 * u) * 2 * a.cols + j];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) s += v[u];
+        }
+        for (; p < parts; p += 16) s += a.ws[(size_t)p * 2 * a.cols + j];
+    }
+    red[wave][lane] = s;
+    __syncthreads();
+    if (wave == 0 && j < 2 * (int64_t)a.cols) {
+        s = red[0][lane];
+#pragma unroll
+        for (int w = 1; w < 16; ++w) s += red[w][lane];
+        float* to = j < a.cols ? a.dgamma : a.dbeta;
+        if (to) to[j < a.cols ? j : j - a.cols] = s;
+    }
+}
+
+// ---- rows of any length: a workgroup a row, the row read again for every pass --------------------------------------------
+
+template <int DT, int MODE>
+__global__ __launch_bounds__(1024) void norm_fwd_any(NormArgs a)
+{
+    typedef typename Prec<DT>::elem_t elem_t;
+    constexpr int NT = 1024;
+    __shared__ float red[3][16];
+    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        const elem_t* x = (const elem_t*)a.x + row * a.ldx;
+        float mean = 0.0f, rstd = 1.0f;
+        if constexpr (MODE != QUANT_ONLY) {
+            float sum = 0.0f, sq = 0.0f;
+            for (int j = threadIdx.x; j < a.cols; j += NT) sum += Prec<DT>::to_f32(x[j]);
+            mean = block_reduce<16, OpSum>(sum, red[0]) / (float)a.cols;
+            for (int j = threadIdx.x; j < a.cols; j += NT) {
+                const float d = Prec<DT>::to_f32(x[j]) - mean;
+                sq = __builtin_fmaf(d, d, sq);
+            }
+            rstd = 1.0f / sqrtf(block_reduce<16, OpSum>(sq, red[1]) / (float)a.cols + a.eps);
+        }
+        auto value = [&](int j) -> elem_t {
+            if constexpr (MODE == QUANT_ONLY) return x[j];
+            return Prec<DT>::from_f32(__builtin_fmaf((Prec<DT>::to_f32(x[j]) - mean) * rstd, a.gamma ? a.gamma[j] : 1.0f, a.beta ? a.beta[j] : 0.0f));
+        };
+        if constexpr (MODE == TO_FLOAT) {
+            elem_t* y = (elem_t*)a.y + row * a.ldy;
+            for (int j = threadIdx.x; j < a.cols; j += NT) y[j] = value(j);
+            if (threadIdx.x == 0) {
+                if (a.mean) a.mean[row] = mean;
+                if (a.rstd) a.rstd[row] = rstd;
+            }
+        } else {
+            float amax = 0.0f;
+            for (int j = threadIdx.x; j < a.cols; j += NT) amax = keep(amax, Prec<DT>::to_f32(value(j)));
+            const RowScale r = row_scale(block_reduce<16, OpKeep>(amax, red[2]));
+            int8_t* q = a.q + row * a.ldy;
+            const int padded = (a.cols + 15) & ~15;
+            for (int j = threadIdx.x; j < padded; j += NT) q[j] = j < a.cols ? (int8_t)code(Prec<DT>::to_f32(value(j)), r) : (int8_t)0;
+            if (threadIdx.x == 0) a.scale[row] = r.scale;
+        }
+        __syncthreads();
     }
 }
 
 template <int DT>
-__global__ __launch_bounds__(256) void quant_any(QuantArgs a)
+__global__ __launch_bounds__(1024) void norm_dx_any(NormArgs a)
 {
     typedef typename Prec<DT>::elem_t elem_t;
-    __shared__ float red[4];
+    constexpr int NT = 1024;
+    __shared__ float red[2][16];
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
-    __syncthreads();
-    const elem_t* x = (const elem_t*)a.x + row * a.ldx;
-    float amax = 0.0f;
-    for (int j = threadIdx.x; j < a.cols; j += 256) amax = keep(amax, Prec<DT>::to_f32(x[j]));
-    const RowScale r = row_scale(block_reduce<4, OpKeep>(amax, red));
-    int8_t* q = a.q + row * a.ldq;
-    const int padded = (a.cols + 15) & ~15;
-    for (int j = threadIdx.x; j < padded; j += 256) q[j] = j < a.cols ? (int8_t)code(Prec<DT>::to_f32(x[j]), r) : (int8_t)0;
-    if (threadIdx.x == 0) a.scale[row] = r.scale;
-    }
-}
-
-template <int DT>
-__global__ __launch_bounds__(256) void norm_dx_any(NormArgs a)
-{
-    typedef typename Prec<DT>::elem_t elem_t;
-    __shared__ float red[2][4];
-    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
-    __syncthreads();
-    const elem_t* x = (const elem_t*)a.x + row * a.ldx;
-    const elem_t* dy = (const elem_t*)a.dy + row * a.ldy;
-    elem_t* dx = (elem_t*)a.dx + row * a.ldx;
-    const float mean = a.mean[row], rstd = a.rstd[row];
-    float s1 = 0.0f, s2 = 0.0f;
-    for (int j = threadIdx.x; j < a.cols; j += 256) {
-        const float g = Prec<DT>::to_f32(dy[j]) * (a.gamma ? a.gamma[j] : 1.0f);
-        s1 += g;
-        s2 = __builtin_fmaf(g, (Prec<DT>::to_f32(x[j]) - mean) * rstd, s2);
-    }
-    const float c1 = block_reduce<4, OpSum>(s1, red[0]) / (float)a.cols;
-    const float c2 = block_reduce<4, OpSum>(s2, red[1]) / (float)a.cols;
-    for (int j = threadIdx.x; j < a.cols; j += 256) {
-        const float g = Prec<DT>::to_f32(dy[j]) * (a.gamma ? a.gamma[j] : 1.0f);
-        const float xh = (Prec<DT>::to_f32(x[j]) - mean) * rstd;
-        dx[j] = Prec<DT>::from_f32(rstd * (g - c1 - xh * c2));
-    }
+        const elem_t* x = (const elem_t*)a.x + row * a.ldx;
+        const elem_t* dy = (const elem_t*)a.dy + row * a.ldy;
+        elem_t* dx = (elem_t*)a.dx + row * a.ldx;
+        const float mean = a.mean[row], rstd = a.rstd[row];
+        float s1 = 0.0f, s2 = 0.0f;
+        for (int j = threadIdx.x; j < a.cols; j += NT) {
+            const float g = Prec<DT>::to_f32(dy[j]) * (a.gamma ? a.gamma[j] : 1.0f);
+            s1 += g;
+            s2 = __builtin_fmaf(g, (Prec<DT>::to_f32(x[j]) - mean) * rstd, s2);
+        }
+        const float c1 = block_reduce<16, OpSum>(s1, red[0]) / (float)a.cols;
+        const float c2 = block_reduce<16, OpSum>(s2, red[1]) / (float)a.cols;
+        for (int j = threadIdx.x; j < a.cols; j += NT) {
+            const float g = Prec<DT>::to_f32(dy[j]) * (a.gamma ? a.gamma[j] : 1.0f);
+            const float xh = (Prec<DT>::to_f32(x[j]) - mean) * rstd;
+            dx[j] = Prec<DT>::from_f32(rstd * (g - c1 - xh * c2));
+        }
+        __syncthreads();
     }
 }
 
@@ -141,58 +457,128 @@ __global__ __launch_bounds__(256) void norm_dw_any(NormArgs a)
     a.ws[((size_t)blockIdx.y * 2 + 1) * a.cols + j] = db;
 }
 
-// The partial sums of `parts` workgroups, in order.
-__global__ __launch_bounds__(256) void norm_dw_join(NormArgs a, int parts)
+// ---- which form -------------------------------------------------------------------------------------------------------
+
+constexpr int kCUs = 256;
+
+// Lanes a row and pieces a lane: the fewest lanes that hold the row in `most` pieces each.  lanes 0: the row is too long.
+struct Form {
+    int lanes, pieces;
+};
+Form form_of(int cols, int dtype, int most)
 {
-    const int j = blockIdx.x * 256 + threadIdx.x;
-    if (j >= a.cols) return;
-    float dg = 0.0f, db = 0.0f;
-    for (int p = 0; p < parts; ++p) {
-        dg += a.ws[((size_t)p * 2) * a.cols + j];
-        db += a.ws[((size_t)p * 2 + 1) * a.cols + j];
+    const int vec = dtype == CONV_F32 ? 4 : 8, pieces = (cols + vec - 1) / vec;
+    for (int lanes : {16, 64, 256, 1024}) {
+        const int n = (pieces + lanes - 1) / lanes;
+        if (n <= most) return Form{lanes, n <= 1 ? 1 : n <= 2 ? 2 : 4};
     }
-    if (a.dgamma) a.dgamma[j] = dg;
-    if (a.dbeta) a.dbeta[j] = db;
+    return Form{0, 0};
 }
 
-// one workgroup a row up to 2^20 of them, which then take several
-unsigned row_grid(int64_t rows) { return (unsigned)std::min<int64_t>(rows, 1 << 20); }
+template <int DT, int G, int NV, int MODE>
+void fwd_launch(const NormArgs& a, hipStream_t s)
+{
+    constexpr int NT = G <= 256 ? 256 : G, ROWS = NT / G;
+    const int64_t blocks = std::min<int64_t>((a.rows + ROWS - 1) / ROWS, G == 1024 ? kCUs * 2 : kCUs * 8);
+    hipLaunchKernelGGL((norm_fwd_rows<DT, G, NV, MODE>), dim3((unsigned)blocks), dim3(NT), 0, s, a);
+}
 
-int dw_parts(int64_t rows) { return (int)std::min<int64_t>(64, (rows + 15) / 16); }
+template <int DT, int G, int MODE>
+void fwd_pieces(const NormArgs& a, int nv, hipStream_t s)
+{
+    if (nv == 1) fwd_launch<DT, G, 1, MODE>(a, s);
+    else if (nv == 2) fwd_launch<DT, G, 2, MODE>(a, s);
+    else fwd_launch<DT, G, 4, MODE>(a, s);
+}
+
+template <int DT, int MODE>
+hipError_t fwd(const NormArgs& a, hipStream_t s)
+{
+    const Form f = form_of(a.cols, DT, 4);
+    if (f.lanes == 16) fwd_pieces<DT, 16, MODE>(a, f.pieces, s);
+    else if (f.lanes == 64) fwd_pieces<DT, 64, MODE>(a, f.pieces, s);
+    else if (f.lanes == 256) fwd_pieces<DT, 256, MODE>(a, f.pieces, s);
+    else if (f.lanes == 1024) fwd_pieces<DT, 1024, MODE>(a, f.pieces, s);
+    else hipLaunchKernelGGL((norm_fwd_any<DT, MODE>), dim3((unsigned)std::min<int64_t>(a.rows, 1 << 20)), dim3(1024), 0, s, a);
+    return hipGetLastError();
+}
+
+template <int MODE>
+hipError_t fwd_type(const NormArgs& a, int dtype, hipStream_t s)
+{
+    return dtype == CONV_F32 ? fwd<CONV_F32, MODE>(a, s) : dtype == CONV_F16 ? fwd<CONV_F16, MODE>(a, s) : fwd<CONV_BF16, MODE>(a, s);
+}
+
+// Backward a lane holds 16 elements at most: with their gradients, sums and the next row that is what 16 waves have registers for.
+Form bwd_form(int cols, int dtype) { return form_of(cols, dtype, dtype == CONV_F32 ? 4 : 2); }
+
+// Workgroups of the backward kernel: a sum of 2 * cols floats each is written and read again.
+int bwd_threads(int lanes) { return lanes == 1024 ? 1024 : 512; }
+int bwd_parts(int64_t rows, int cols, int dtype)
+{
+    const Form f = bwd_form(cols, dtype);
+    if (!f.lanes) return (int)std::max<int64_t>(1, std::min<int64_t>(64, (rows + 15) / 16));
+    const int here = bwd_threads(f.lanes) / f.lanes;
+    return (int)std::max<int64_t>(1, std::min<int64_t>(cols <= 1024 ? 2 * kCUs : kCUs, (rows + here - 1) / here));
+}
+
+template <int DT, int G, int NV>
+void bwd_launch(const NormArgs& a, int parts, hipStream_t s)
+{
+    constexpr int NT = G == 1024 ? 1024 : 512;
+    const dim3 grid((unsigned)parts), block(NT);
+    const bool dw = a.dgamma || a.dbeta;
+    if (a.dx && dw) hipLaunchKernelGGL((norm_bwd_rows<DT, G, NV, NT, true, true>), grid, block, 0, s, a);
+    else if (a.dx) hipLaunchKernelGGL((norm_bwd_rows<DT, G, NV, NT, true, false>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((norm_bwd_rows<DT, G, NV, NT, false, true>), grid, block, 0, s, a);
+}
+
+template <int DT, int G>
+void bwd_pieces(const NormArgs& a, int nv, int parts, hipStream_t s)
+{
+    if (nv == 1) bwd_launch<DT, G, 1>(a, parts, s);
+    else if (nv == 2) bwd_launch<DT, G, 2>(a, parts, s);
+    else if constexpr (DT == CONV_F32) bwd_launch<DT, G, 4>(a, parts, s);
+}
 
 template <int DT>
-hipError_t bwd(NormArgs& a, hipStream_t s)
+hipError_t bwd(const NormArgs& a, hipStream_t s)
 {
-    if (a.dgamma || a.dbeta) {
-        const int parts = dw_parts(a.rows);
-        const unsigned cb = (unsigned)((a.cols + 255) / 256);
-        if (parts) hipLaunchKernelGGL((norm_dw_any<DT>), dim3(cb, parts), dim3(256), 0, s, a);
-        hipLaunchKernelGGL(norm_dw_join, dim3(cb), dim3(256), 0, s, a, parts);
+    const Form f = bwd_form(a.cols, DT);
+    const int parts = bwd_parts(a.rows, a.cols, DT);
+    const bool dw = a.dgamma || a.dbeta;
+    if (f.lanes) {
+        if (f.lanes == 16) bwd_pieces<DT, 16>(a, f.pieces, parts, s);
+        else if (f.lanes == 64) bwd_pieces<DT, 64>(a, f.pieces, parts, s);
+        else if (f.lanes == 256) bwd_pieces<DT, 256>(a, f.pieces, parts, s);
+        else bwd_pieces<DT, 1024>(a, f.pieces, parts, s);
+    } else {
+        if (dw) hipLaunchKernelGGL((norm_dw_any<DT>), dim3((unsigned)((a.cols + 255) / 256), parts), dim3(256), 0, s, a);
+        if (a.dx && a.rows) hipLaunchKernelGGL((norm_dx_any<DT>), dim3((unsigned)std::min<int64_t>(a.rows, 1 << 20)), dim3(1024), 0, s, a);
     }
-    if (a.dx && a.rows) hipLaunchKernelGGL((norm_dx_any<DT>), dim3(row_grid(a.rows)), dim3(256), 0, s, a);
+    if (dw && (parts > 1 || !f.lanes))
+        hipLaunchKernelGGL(norm_dw_join, dim3((unsigned)((2 * (int64_t)a.cols + 63) / 64)), dim3(1024), 0, s, a, parts);
     return hipGetLastError();
 }
 
 }  // namespace
 
-size_t layernorm_bwd_workspace(int64_t rows, int cols, int dtype) { return (size_t)dw_parts(rows) * 2 * cols * 4; }
+size_t layernorm_bwd_workspace(int64_t rows, int cols, int dtype)
+{
+    const int parts = bwd_parts(rows, cols, dtype);
+    return parts == 1 && bwd_form(cols, dtype).lanes ? 0 : (size_t)parts * 2 * cols * 4;
+}
 
 hipError_t launch_layernorm_fwd(NormArgs& a, int dtype, hipStream_t s)
 {
-    const dim3 grid(row_grid(a.rows)), block(256);
-    if (dtype == CONV_F32) hipLaunchKernelGGL((norm_fwd_any<CONV_F32>), grid, block, 0, s, a);
-    else if (dtype == CONV_F16) hipLaunchKernelGGL((norm_fwd_any<CONV_F16>), grid, block, 0, s, a);
-    else hipLaunchKernelGGL((norm_fwd_any<CONV_BF16>), grid, block, 0, s, a);
-    return hipGetLastError();
+    return a.q ? fwd_type<TO_CODES>(a, dtype, s) : fwd_type<TO_FLOAT>(a, dtype, s);
 }
 
-hipError_t launch_quantize_rows(QuantArgs& a, int dtype, hipStream_t s)
+hipError_t launch_quantize_rows(QuantArgs& q, int dtype, hipStream_t s)
 {
-    const dim3 grid(row_grid(a.rows)), block(256);
-    if (dtype == CONV_F32) hipLaunchKernelGGL((quant_any<CONV_F32>), grid, block, 0, s, a);
-    else if (dtype == CONV_F16) hipLaunchKernelGGL((quant_any<CONV_F16>), grid, block, 0, s, a);
-    else hipLaunchKernelGGL((quant_any<CONV_BF16>), grid, block, 0, s, a);
-    return hipGetLastError();
+    NormArgs a = {};
+    a.x = q.x, a.q = q.q, a.scale = q.scale, a.rows = q.rows, a.ldx = q.ldx, a.ldy = q.ldq, a.cols = q.cols;
+    return fwd_type<QUANT_ONLY>(a, dtype, s);
 }
 
 hipError_t launch_layernorm_bwd(NormArgs& a, int dtype, hipStream_t s)

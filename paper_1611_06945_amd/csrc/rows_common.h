@@ -74,6 +74,20 @@ __device__ __forceinline__ float lanes_reduce(float x)
     return x;
 }
 
+// The sum over the lanes of a wave that are G apart (G = 16 or 32); every lane gets it.
+template <int G>
+__device__ __forceinline__ float across_rows(float x)
+{
+    if constexpr (G <= 16) {
+        const uint32_t u = __builtin_bit_cast(uint32_t, x);
+        const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+        x = __builtin_bit_cast(float, (uint32_t)r[0]) + __builtin_bit_cast(float, (uint32_t)r[1]);
+    }
+    const uint32_t u = __builtin_bit_cast(uint32_t, x);
+    const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    return __builtin_bit_cast(float, (uint32_t)r[0]) + __builtin_bit_cast(float, (uint32_t)r[1]);
+}
+
 // ... over a workgroup of W waves; `lds` holds W floats and is free again after the next barrier of the caller's.
 template <int W, typename Op>
 __device__ __forceinline__ float block_reduce(float x, float* lds)
