@@ -404,7 +404,7 @@ int layernorm_quant_fwd(const norm_desc* desc, const void* x, const float* gamma
  * CONV_FLAG_RELU: act(x) = max(x, 0), a NaN stays NaN.  Rows of a and w are read in pieces of 16 bytes: the bytes from K
  * up to the next multiple of 16 have to be readable; their values do not matter.  `workspace`
  * (int_linear_workspace_bytes(desc) bytes, which may be 0; 16-byte aligned) holds partial sums of few-row products; NULL or a smaller one gives
- * CONV_EWORKSPACE when bytes are needed.  N, K >= 1; lda, ldw >= K and divisible by 16; ldo >= N.
+ * CONV_EWORKSPACE when bytes are needed.  1 <= N < 2^24, K >= 1; lda, ldw >= K and divisible by 16; ldo >= N.
  */
 typedef struct {
     int64_t rows;

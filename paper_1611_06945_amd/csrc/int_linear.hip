@@ -1,5 +1,7 @@
 // Matrix product in 8-bit integers with scales for each row and output channel.
 #include <algorithm>
+#include <cmath>
+#include <type_traits>
 
 #include "rows_common.h"
 
@@ -10,6 +12,9 @@ namespace {
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x16 __attribute__((ext_vector_type(16)));
 typedef __attribute__((address_space(3))) void lds_void;
+
+// Added to an offset within a tile (below 2^31), puts it past the end of any descriptor here.
+constexpr uint32_t kFar = 0x80000000u;
 
 // The first `n` bytes of a 16-byte piece (n may be <= 0 or >= 16), the others zero.
 __device__ __forceinline__ i32x4 first_bytes(i32x4 v, int n)
@@ -28,9 +33,18 @@ __device__ __forceinline__ float finish(int acc, float scale, float bias, int re
     return relu && v < 0.0f ? 0.0f : v;  // a NaN stays
 }
 
-// A wave 16 channels x 16 rows, operands from memory straight into registers: any strides.
+template <int N, typename F>
+__device__ __forceinline__ void for_each(F f)
+{
+    if constexpr (N > 0) {
+        for_each<N - 1>(f);
+        f(std::integral_constant<int, N - 1>());
+    }
+}
+
+// Any strides: a wave 16 channels x 16 rows, operands from memory straight into registers.
 template <int DT>
-__global__ __launch_bounds__(256) void int_linear_tile16(IntLinearArgs g)
+__global__ __launch_bounds__(256) void int_linear_any(IntLinearArgs g)
 {
     typedef typename Prec<DT>::elem_t elem_t;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -39,7 +53,7 @@ __global__ __launch_bounds__(256) void int_linear_tile16(IntLinearArgs g)
     if (n0 >= g.N) return;
     const int i = lane & 15, kq = (lane >> 4) * 16;
     const int8_t* w = g.w + (int64_t)min(n0 + i, g.N - 1) * g.ldw;
-    const int8_t* a = g.a + (t0 + i < g.rows ? t0 + i : g.rows - 1) * g.lda;
+    const int8_t* a = g.a + min(t0 + i, g.rows - 1) * g.lda;
     i32x4 acc = {0, 0, 0, 0};
     for (int k = kq; k - kq < g.K; k += 64) {
         i32x4 wv = {0, 0, 0, 0}, av = wv;
@@ -60,19 +74,111 @@ __global__ __launch_bounds__(256) void int_linear_tile16(IntLinearArgs g)
     }
 }
 
-// Tiles of BT rows x BN channels, both operands staged through LDS by loads that write it directly, two stages.
-//   * A stage holds 128 bytes of each row; a row's eight 16-byte pieces are stored at piece ^ (row / 2 % 8), by choosing which piece
-//     a lane loads: the 16 lanes that LDS serves together then read 16 different groups of four banks.
+// Few rows: a workgroup 16 channels x 16 RB rows, its W waves share the reduction: wave w takes every W-th run of 64 U bytes.  The
+// weights' stream is what counts, so loads are made of four lanes a 64-byte stretch of a row (a lane a row, as the matrix
+// instruction wants them, is served 16 bytes a clock: 64 x 100 x 16384 took 20 us instead of 12), straight into LDS the wave has for
+// itself, no barrier; a row's four pieces lie at piece ^ (row / 4 % 4) there, so that no two of 16 lanes read a bank.  The
+// waves' exact sums meet in LDS.  Where there are few workgroups and a long reduction, gridDim.z of them share it (int_linear_join).
+template <int DT, int RB, int W, int U>
+__global__ __launch_bounds__(64 * W) void int_linear_rows(IntLinearArgs g)
+{
+    typedef typename Prec<DT>::elem_t elem_t;
+    constexpr int NT = 64 * W, RUN = 64 * U, OWN = (1 + RB) * U * 1024;
+    extern __shared__ __attribute__((aligned(16))) char smem[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int n0 = blockIdx.x * 16;
+    const int64_t t0 = (int64_t)blockIdx.y * (16 * RB);
+    const int Kr = (g.K + 15) & ~15;
+    const int rows_here = (int)min((int64_t)(16 * RB), g.rows - t0), outs_here = min(16, g.N - n0);
+    const __amdgpu_buffer_rsrc_t ra = make_rsrc(g.a + t0 * g.lda, (uint32_t)((rows_here - 1) * g.lda + Kr));
+    const __amdgpu_buffer_rsrc_t rw = make_rsrc(g.w + (int64_t)n0 * g.ldw, (uint32_t)((outs_here - 1) * g.ldw + Kr));
+    const int row = lane >> 2, piece = (lane & 3) ^ ((row >> 2) & 3);
+    const uint32_t woff = (uint32_t)row * (uint32_t)g.ldw + piece * 16, aoff = (uint32_t)row * (uint32_t)g.lda + piece * 16;
+    char* const own = smem + wave * OWN;
+    const char* const mine = own + (lane & 15) * 64 + (((lane >> 4) ^ ((lane >> 2) & 3)) << 4);
+
+    i32x4 acc[RB];
+#pragma unroll
+    for (int j = 0; j < RB; ++j) acc[j] = i32x4{0, 0, 0, 0};
+    for (int k = (blockIdx.z * W + wave) * RUN; k < g.K; k += gridDim.z * W * RUN) {
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rw, (lds_void*)(own + u * 1024), 16, (int)(woff + k + u * 64), 0, 0, 0);
+#pragma unroll
+        for (int j = 0; j < RB; ++j)
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (lds_void*)(own + ((1 + j) * U + u) * 1024), 16,
+                                                         (int)(aoff + (uint32_t)(j * 16) * (uint32_t)g.lda + k + u * 64), 0, 0, 0);
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        i32x4 wv[U], av[RB][U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) wv[u] = *(const i32x4*)(mine + u * 1024);
+#pragma unroll
+        for (int j = 0; j < RB; ++j)
+#pragma unroll
+            for (int u = 0; u < U; ++u) av[j][u] = *(const i32x4*)(mine + ((1 + j) * U + u) * 1024);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // read before the next run's loads may land
+        if (k + RUN > g.K) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) wv[u] = first_bytes(wv[u], g.K - k - u * 64 - (lane >> 4) * 16);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int j = 0; j < RB; ++j) acc[j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wv[u], av[j][u], acc[j], 0, 0, 0);
+    }
+    __syncthreads();
+    i32x4* const part = (i32x4*)smem;
+#pragma unroll
+    for (int j = 0; j < RB; ++j) part[(wave * RB + j) * 64 + lane] = acc[j];
+    __syncthreads();
+    for (int o = threadIdx.x; o < 256 * RB; o += NT) {
+        const int n = n0 + (o & 15), r = o >> 4;  // channel; row among the workgroup's
+        if (n >= g.N || r >= rows_here) continue;
+        int sum = 0;
+#pragma unroll
+        for (int v = 0; v < W; ++v) sum += ((const int*)&part[(v * RB + (r >> 4)) * 64 + ((o & 15) >> 2) * 16 + (r & 15)])[o & 3];
+        if (gridDim.z > 1)
+            g.ws[(blockIdx.z * g.rows + t0 + r) * g.N + n] = sum;
+        else
+            ((elem_t*)g.out)[(t0 + r) * g.ldo + n] =
+                Prec<DT>::from_f32(finish(sum, g.a_scale[t0 + r] * g.w_scale[n], g.bias ? g.bias[n] : 0.0f, g.relu));
+    }
+}
+
+// Adds the sums of `splits` workgroups that shared a reduction.
+template <int DT>
+__global__ __launch_bounds__(256) void int_linear_join(IntLinearArgs g, int splits)
+{
+    const int64_t o = (int64_t)blockIdx.x * 256 + threadIdx.x, all = g.rows * g.N;
+    if (o >= all) return;
+    const int64_t t = o / g.N;
+    const int n = (int)(o - t * g.N);
+    int sum = 0;
+    for (int z = 0; z < splits; ++z) sum += g.ws[z * all + o];
+    ((typename Prec<DT>::elem_t*)g.out)[t * g.ldo + n] =
+        Prec<DT>::from_f32(finish(sum, g.a_scale[t] * g.w_scale[n], g.bias ? g.bias[n] : 0.0f, g.relu));
+}
+
+// Tiles of BT rows x BN channels, both operands staged through LDS by loads that write it directly, a ring of S stages of 128 bytes
+// of each row: while one is multiplied, S - 1 are on their way or there.
+//   * A row's eight 16-byte pieces are stored at piece ^ (row / 2 % 8), by choosing which piece a lane loads: the 16 lanes that LDS
+//     serves together then read 16 different groups of four banks (no conflict counted).
 //   * Rows past the last one, and pieces past the end of the tensor, are read as zeros by the bounds check of the buffer
 //     descriptor; the bytes of a row past K belong to what follows and are cleared in one operand on the last step.
-template <int WT_, int WN_, int FT_, int FN_>
+//   * Products are 16x16x64: on random operands the register-only loop reaches 3970 TOP/s with two waves a SIMD, 32x32x32 3480
+//     (on zeros both 4600: the card's power sets the clock).
+template <int WT_, int WN_, int FT_, int FN_, int S_>
 struct IntTile {
-    static constexpr int WT = WT_, WN = WN_, FT = FT_, FN = FN_;  // waves and 32-wide blocks a wave, along rows and channels
-    static constexpr int BT = 32 * WT * FT, BN = 32 * WN * FN, NT = 64 * WT * WN;
-    static constexpr int KB = 128;
+    static constexpr int WT = WT_, WN = WN_, FT = FT_, FN = FN_;  // waves and 16-wide blocks a wave, along rows and channels
+    static constexpr int BT = 16 * WT * FT, BN = 16 * WN * FN, NT = 64 * WT * WN;
+    static constexpr int KB = 128, S = S_, PIECES = KB / 16;
     static constexpr int STAGE = (BT + BN) * KB;
-    static constexpr size_t LDS = 2 * STAGE;
-    static constexpr int LA = BT * 8 / NT, LW = BN * 8 / NT;  // 16-byte loads a thread and stage
+    static constexpr size_t LDS = (size_t)S * STAGE + (BT + 2 * BN) * 4;
+    static constexpr int LA = BT * PIECES / NT, LW = BN * PIECES / NT;  // 16-byte loads a thread and stage
+    static constexpr int H = FT > 4 ? 2 : 1, HB = FT / H;               // the blocks of rows go in H portions
+    static_assert(LA * NT == BT * PIECES && LW * NT == BN * PIECES && FN % 2 == 0 && HB * H == FT, "whole loads and portions");
 };
 
 template <int DT, typename T>
@@ -80,7 +186,7 @@ __global__ __launch_bounds__(T::NT) void int_linear_tiles(IntLinearArgs g, int t
 {
     typedef typename Prec<DT>::elem_t elem_t;
     extern __shared__ __attribute__((aligned(16))) char smem[];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wt = wave % T::WT, wn = wave / T::WT;
 
     // consecutive workgroups go to different XCDs: each XCD takes a run of tiles, in bands of eight tiles of channels
@@ -97,22 +203,25 @@ __global__ __launch_bounds__(T::NT) void int_linear_tiles(IntLinearArgs g, int t
     const int n0 = tn * T::BN;
 
     const int Kr = (g.K + 15) & ~15;
-    const int64_t rows_here = min((int64_t)T::BT, g.rows - t0);
-    const int outs_here = min(T::BN, g.N - n0);
+    const int rows_here = (int)min((int64_t)T::BT, g.rows - t0), outs_here = min(T::BN, g.N - n0);
     const __amdgpu_buffer_rsrc_t ra = make_rsrc(g.a + t0 * g.lda, (uint32_t)((rows_here - 1) * g.lda + Kr));
     const __amdgpu_buffer_rsrc_t rw = make_rsrc(g.w + (int64_t)n0 * g.ldw, (uint32_t)((outs_here - 1) * g.ldw + Kr));
     uint32_t aoff[T::LA], woff[T::LW];
+    constexpr int P = T::PIECES;
 #pragma unroll
     for (int i = 0; i < T::LA; ++i) {
-        const int p = i * T::NT + tid, row = p >> 3;
-        aoff[i] = (uint32_t)row * (uint32_t)g.lda + (((p & 7) ^ ((row >> 1) & 7)) << 4);
+        const int p = i * T::NT + tid, row = p / P;
+        aoff[i] = (uint32_t)row * (uint32_t)g.lda + (((p % P) ^ ((row >> 1) % P)) << 4);
     }
 #pragma unroll
     for (int i = 0; i < T::LW; ++i) {
-        const int p = i * T::NT + tid, row = p >> 3;
-        woff[i] = (uint32_t)row * (uint32_t)g.ldw + (((p & 7) ^ ((row >> 1) & 7)) << 4);
+        const int p = i * T::NT + tid, row = p / P;
+        woff[i] = (uint32_t)row * (uint32_t)g.ldw + (((p % P) ^ ((row >> 1) % P)) << 4);
     }
-    auto stage = [&](int buf, int k0) {
+    const int steps = (g.K + T::KB - 1) / T::KB;
+    // Steps past the last are asked for as well, out of range, so that the count of loads on their way is always the same.
+    auto stage = [&](int buf, int k) {
+        const uint32_t k0 = k < steps ? (uint32_t)k * T::KB : kFar;
         char* base = smem + buf * T::STAGE + wave * 1024;
 #pragma unroll
         for (int i = 0; i < T::LA; ++i)
@@ -121,105 +230,140 @@ __global__ __launch_bounds__(T::NT) void int_linear_tiles(IntLinearArgs g, int t
         for (int i = 0; i < T::LW; ++i)
             __builtin_amdgcn_raw_ptr_buffer_load_lds(rw, (lds_void*)(base + T::BT * T::KB + i * T::NT * 16), 16, (int)(woff[i] + k0), 0, 0, 0);
     };
-    int frag[4];  // LDS offset of this lane's piece for each step of 32 bytes, without the block
-#pragma unroll
-    for (int s = 0; s < 4; ++s) frag[s] = (lane & 31) * T::KB + (((s * 2 + (lane >> 5)) ^ ((lane >> 1) & 7)) << 4);
 
-    i32x16 acc[T::FN][T::FT];
+    // the tile's scales and biases wait in LDS for the end
+    float* const sc_a = (float*)(smem + T::S * T::STAGE);
+    float* const sc_w = sc_a + T::BT;
+    float* const bias = sc_w + T::BN;
+    for (int i = tid; i < T::BT; i += T::NT) sc_a[i] = i < rows_here ? g.a_scale[t0 + i] : 0.0f;
+    for (int i = tid; i < T::BN; i += T::NT) {
+        sc_w[i] = i < outs_here ? g.w_scale[n0 + i] : 0.0f;
+        bias[i] = g.bias && i < outs_here ? g.bias[n0 + i] : 0.0f;
+    }
+
+    int frag[2];  // LDS offset of this lane's piece for each half of a stage, without the block
+#pragma unroll
+    for (int s = 0; s < 2; ++s) frag[s] = (lane & 15) * T::KB + (((s * 4 + (lane >> 4)) ^ ((lane >> 1) & 7)) << 4);
+    const int wave_a = wt * T::FT * 16 * T::KB, wave_w = (T::BT + wn * T::FN * 16) * T::KB;
+
+    i32x4 acc[T::FN][T::FT];
 #pragma unroll
     for (int i = 0; i < T::FN; ++i)
 #pragma unroll
-        for (int j = 0; j < T::FT; ++j)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) acc[i][j][r] = 0;
+        for (int j = 0; j < T::FT; ++j) acc[i][j] = i32x4{0, 0, 0, 0};
 
-    const int steps = (g.K + T::KB - 1) / T::KB;
-    auto multiply = [&](int buf, int left, auto last) {
-        const char* pa = smem + buf * T::STAGE + wt * T::FT * 32 * T::KB;
-        const char* pw = smem + buf * T::STAGE + (T::BT + wn * T::FN * 32) * T::KB;
+    i32x4 av[2][T::HB], wv[2][T::FN];
+    // The operands of phase p of a stage (half p / H, portion p % H of the rows) to the registers of its parity.
+    auto fetch = [&](int buf, auto phase) {
+        constexpr int p = decltype(phase)::value, s = p / T::H, h = p % T::H;
+        const char* base = smem + buf * T::STAGE + frag[s];
+        if constexpr (h == 0) {
 #pragma unroll
-        for (int s = 0; s < 4; ++s) {
-            i32x4 av[T::FT], wv[T::FN];
+            for (int i = 0; i < T::FN; ++i) wv[s][i] = *(const i32x4*)(base + wave_w + i * 16 * T::KB);
+        }
 #pragma unroll
-            for (int i = 0; i < T::FN; ++i) {
-                wv[i] = *(const i32x4*)(pw + frag[s] + i * 32 * T::KB);
-                if constexpr (decltype(last)::value) wv[i] = first_bytes(wv[i], left - (s * 2 + (lane >> 5)) * 16);
-            }
+        for (int j = 0; j < T::HB; ++j) av[p & 1][j] = *(const i32x4*)(base + wave_a + (h * T::HB + j) * 16 * T::KB);
+    };
+    auto products = [&](auto phase) {
+        constexpr int p = decltype(phase)::value, s = p / T::H, h = p % T::H;
 #pragma unroll
-            for (int j = 0; j < T::FT; ++j) av[j] = *(const i32x4*)(pa + frag[s] + j * 32 * T::KB);
+        for (int j = 0; j < T::HB; ++j)
 #pragma unroll
             for (int i = 0; i < T::FN; ++i)
-#pragma unroll
-                for (int j = 0; j < T::FT; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(wv[i], av[j], acc[i][j], 0, 0, 0);
-        }
+                acc[i][h * T::HB + j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wv[s][i], av[p & 1][j], acc[i][h * T::HB + j], 0, 0, 0);
     };
-    stage(0, 0);
-    __syncthreads();
+    constexpr int PHASES = 2 * T::H, LOADS = T::LA + T::LW;
+    typedef std::integral_constant<int, 0> First;
+    typedef std::integral_constant<int, PHASES - 1> Last;
+    // Operands are read one phase ahead of their products, across the turn to the next stage too; the scheduling barriers keep the
+    // compiler from reading them where they are used.
+#pragma unroll
+    for (int k = 0; k < T::S; ++k) stage(k, k);
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((T::S - 1) * LOADS) : "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    fetch(0, First());
+    int buf = 0;
     for (int k = 0; k < steps - 1; ++k) {
-        stage((k + 1) & 1, (k + 1) * T::KB);
-        multiply(k & 1, 0, std::false_type());
-        __syncthreads();  // waits for the loads of this wave as well
-    }
-    multiply((steps - 1) & 1, g.K - (steps - 1) * T::KB, std::true_type());
-
-    // lane: row (lane & 31) of a block of rows; channels 8 q + 4 (lane / 32) + 0..3 in accumulators 4 q ..  Two q at a time, so that
-    // few scales are held; in 16 bits the halves of the wave then trade, and a lane has eight channels in a row: lanes below 32
-    // those of q, the others those of q + 1.
-    const int half = lane >> 5;
-    float sa[T::FT];
-    const int64_t t_lane = t0 + wt * T::FT * 32 + (lane & 31);
-#pragma unroll
-    for (int j = 0; j < T::FT; ++j) sa[j] = g.a_scale[min(t_lane + j * 32, g.rows - 1)];
-#pragma unroll
-    for (int i = 0; i < T::FN; ++i)
-#pragma unroll
-        for (int q = 0; q < 4; q += 2) {
-            const int nb = n0 + (wn * T::FN + i) * 32 + q * 8;
-            float sw[8], b[8];
-#pragma unroll
-            for (int r = 0; r < 8; ++r) {
-                const int n = min(nb + (r >> 2) * 8 + half * 4 + (r & 3), g.N - 1);
-                sw[r] = g.w_scale[n];
-                b[r] = g.bias ? g.bias[n] : 0.0f;
-            }
-#pragma unroll
-            for (int j = 0; j < T::FT; ++j) {
-                const int64_t t = t_lane + j * 32;
-                elem_t* out = (elem_t*)g.out + t * g.ldo;
-                float v[8];
-#pragma unroll
-                for (int r = 0; r < 8; ++r) v[r] = finish(acc[i][j][4 * q + r], sa[j] * sw[r], b[r], g.relu);
-                constexpr int LEN = 16 / sizeof(elem_t);
-                uint32_t w4[8 / LEN][4];
-                int n[8 / LEN];
-                if constexpr (DT == CONV_F32) {
-                    __builtin_memcpy(w4, v, 32);
-                    n[0] = nb + half * 4, n[1] = nb + 8 + half * 4;
-                } else {
-                    const auto r0 = __builtin_amdgcn_permlane32_swap(Prec<DT>::pack2_from_f32(v[0], v[1]), Prec<DT>::pack2_from_f32(v[4], v[5]), false, false);
-                    const auto r1 = __builtin_amdgcn_permlane32_swap(Prec<DT>::pack2_from_f32(v[2], v[3]), Prec<DT>::pack2_from_f32(v[6], v[7]), false, false);
-                    w4[0][0] = r0[0], w4[0][1] = r1[0], w4[0][2] = r0[1], w4[0][3] = r1[1];
-                    n[0] = nb + half * 8;
-                }
-#pragma unroll
-                for (int c = 0; c < 8 / LEN; ++c) {
-                    if (t < g.rows && n[c] + LEN <= g.N) {
-                        __builtin_memcpy(out + n[c], w4[c], 16);
-                    } else if (t < g.rows) {
-                        elem_t e[LEN];
-                        __builtin_memcpy(e, w4[c], 16);
-#pragma unroll
-                        for (int r = 0; r < LEN; ++r)
-                            if (n[c] + r < g.N) out[n[c] + r] = e[r];
-                    }
-                }
-            }
+        for_each<PHASES - 1>([&](auto p) {
+            fetch(buf, std::integral_constant<int, decltype(p)::value + 1>());
             __builtin_amdgcn_sched_barrier(0);
+            products(p);
+            __builtin_amdgcn_sched_barrier(0);
+        });
+        // this wave's loads of the next stage have landed and its reads of the present one are done; then so are everybody's
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((T::S - 2) * LOADS) : "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        const int next = buf + 1 == T::S ? 0 : buf + 1;
+        fetch(next, First());
+        stage(buf, k + T::S);
+        __builtin_amdgcn_sched_barrier(0);
+        products(Last());
+        __builtin_amdgcn_sched_barrier(0);
+        buf = next;
+    }
+    for_each<PHASES>([&](auto p) {
+        constexpr int q = decltype(p)::value;
+        if constexpr (q + 1 < PHASES) fetch(buf, std::integral_constant<int, q + 1>());
+        if constexpr (q % T::H == 0) {
+#pragma unroll
+            for (int i = 0; i < T::FN; ++i)
+                wv[q / T::H][i] = first_bytes(wv[q / T::H][i], g.K - (steps - 1) * T::KB - (q / T::H * 4 + (lane >> 4)) * 16);
         }
-}
+        products(p);
+    });
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // nothing may land in LDS after the end
 
-typedef IntTile<2, 4, 4, 2> Tile256;  // 256 x 256
-typedef IntTile<2, 2, 2, 2> Tile128;  // 128 x 128
+    // A lane has four channels 4 (lane / 16) .. of a block and row lane % 16 of a block of rows.  In 16 bits neighbouring groups of 16
+    // lanes trade between two blocks of channels, so that a lane has eight channels in a row: the groups 0 .. 3 those of block i from
+    // 0, of block i + 1 from 0, of block i from 8, of block i + 1 from 8.
+    const int grp = lane >> 4;
+#pragma unroll
+    for (int i = 0; i < T::FN; i += 2) {
+        const int nl = (wn * T::FN + i) * 16;
+        float sw[8], b[8];
+        __builtin_memcpy(sw, sc_w + nl + grp * 4, 16);
+        __builtin_memcpy(sw + 4, sc_w + nl + 16 + grp * 4, 16);
+        __builtin_memcpy(b, bias + nl + grp * 4, 16);
+        __builtin_memcpy(b + 4, bias + nl + 16 + grp * 4, 16);
+#pragma unroll
+        for (int j = 0; j < T::FT; ++j) {
+            const int tl = (wt * T::FT + j) * 16 + (lane & 15);
+            const float sa = sc_a[tl];
+            const bool in = tl < rows_here;
+            elem_t* out = (elem_t*)g.out + (t0 + tl) * g.ldo + n0;
+            float v[8];
+#pragma unroll
+            for (int r = 0; r < 8; ++r) v[r] = finish(acc[i + (r >> 2)][j][r & 3], sa * sw[r], b[r], g.relu);
+            constexpr int LEN = 16 / sizeof(elem_t);
+            uint32_t w4[8 / LEN][4];
+            int n[8 / LEN];
+            if constexpr (DT == CONV_F32) {
+                __builtin_memcpy(w4, v, 32);
+                n[0] = nl + grp * 4, n[1] = nl + 16 + grp * 4;
+            } else {
+                const auto r0 = __builtin_amdgcn_permlane16_swap(Prec<DT>::pack2_from_f32(v[0], v[1]), Prec<DT>::pack2_from_f32(v[4], v[5]), false, false);
+                const auto r1 = __builtin_amdgcn_permlane16_swap(Prec<DT>::pack2_from_f32(v[2], v[3]), Prec<DT>::pack2_from_f32(v[6], v[7]), false, false);
+                w4[0][0] = r0[0], w4[0][1] = r1[0], w4[0][2] = r0[1], w4[0][3] = r1[1];
+                n[0] = nl + (grp & 1) * 16 + (grp >> 1) * 8;
+            }
+#pragma unroll
+            for (int c = 0; c < 8 / LEN; ++c) {
+                if (in && n[c] + LEN <= outs_here) {
+                    __builtin_memcpy(out + n[c], w4[c], 16);
+                } else if (in) {
+                    elem_t e[LEN];
+                    __builtin_memcpy(e, w4[c], 16);
+#pragma unroll
+                    for (int r = 0; r < LEN; ++r)
+                        if (n[c] + r < outs_here) out[n[c] + r] = e[r];
+                }
+            }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    }
+}
 
 template <int DT, typename T>
 hipError_t launch_tiles(const IntLinearArgs& g, hipStream_t s)
@@ -227,38 +371,132 @@ hipError_t launch_tiles(const IntLinearArgs& g, hipStream_t s)
     const void* f = (const void*)int_linear_tiles<DT, T>;
     const hipError_t e = ensure_dynamic_lds(f, T::LDS);
     if (e != hipSuccess) return e;
-    const int tt = (int)((g.rows + T::BT - 1) / T::BT), tn = (g.N + T::BN - 1) / T::BN;
-    hipLaunchKernelGGL((int_linear_tiles<DT, T>), dim3((unsigned)(tt * tn)), dim3(T::NT), T::LDS, s, g, tt, tn);
+    const int tn = (g.N + T::BN - 1) / T::BN;
+    // a launch holds less than 2^32 threads: the rows go in portions of so many bands
+    const int64_t bands = std::max<int64_t>(1, (1 << 21) / tn);
+    for (int64_t skip = 0; skip < g.rows; skip += bands * T::BT) {
+        IntLinearArgs p = g;
+        p.rows = std::min(bands * T::BT, g.rows - skip);
+        p.a += skip * g.lda, p.a_scale += skip, p.out = (char*)g.out + skip * g.ldo * dtype_size(DT);
+        const int tt = (int)((p.rows + T::BT - 1) / T::BT);
+        hipLaunchKernelGGL((int_linear_tiles<DT, T>), dim3((unsigned)tt * (unsigned)tn), dim3(T::NT), T::LDS, s, p, tt, tn);
+    }
     return hipGetLastError();
 }
+
+// gridDim.y is at most 65535: the rows go in portions of that many workgroups.
+template <int DT, typename F>
+hipError_t in_portions(const IntLinearArgs& g, int rows_each, F launch)
+{
+    const int64_t portion = 65535 * (int64_t)rows_each;
+    for (int64_t skip = 0; skip < g.rows; skip += portion) {
+        IntLinearArgs p = g;
+        p.rows = std::min(portion, g.rows - skip);
+        p.a += skip * g.lda, p.a_scale += skip, p.out = (char*)g.out + skip * g.ldo * dtype_size(DT);
+        const hipError_t e = launch(p, (unsigned)((p.rows + rows_each - 1) / rows_each));
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
+// The forms and what a launch of them is expected to take, in us, from calls measured alone (8-bit codes at random, bf16 out):
+//   tiles: ceil(tiles / 256) rounds of `step` for every 128 bytes of the reduction and `own`;
+//   rows:  see rows_plan().
+// Measured (us), 64x64 / 64x128 / 128x128 / 128x256 / 256x256 (rows: int_linear_rows):
+//   256 x 4096 x 4096 9.5 / 12.4 / 17 / - / 47;  777 x 1283 x 1001 7.3 / 6.7 / 9.2 / - / 25;  1024 x 4096 x 4096 30 / 23 / 21 / 30 / 48;
+//   2048 x 4096 x 1024 - / - / 17.7 / 13.8 / 20.6;  2048 x 2048 x 2048 20 / 15 / 13 / 18 / 28;  4096 x 4096 x 4096 - / - / 80 / 71 / 61;
+//   33 x 4096 x 4096 8.4 (rows 7.1), 33 x 16384 x 4096 12.3 (rows 24), 64 x 100 x 16384 23 (rows 12).
+template <int WT, int WN, int FT, int FN, int S, int StepNs, int OwnNs>
+struct Costed : IntTile<WT, WN, FT, FN, S> {
+    static double us(const IntLinearArgs& g)
+    {
+        typedef IntTile<WT, WN, FT, FN, S> T;
+        const double tiles = (double)((g.rows + T::BT - 1) / T::BT) * ((g.N + T::BN - 1) / T::BN), steps = (g.K + T::KB - 1) / T::KB;
+        return std::ceil(tiles / 256) * (steps * StepNs + OwnNs) * 1e-3;
+    }
+};
+typedef Costed<4, 2, 1, 2, 4, 200, 3000> Tile64x64;
+typedef Costed<2, 4, 2, 2, 3, 330, 3000> Tile64x128;
+typedef Costed<4, 4, 2, 2, 4, 570, 3500> Tile128x128;
+typedef Costed<4, 4, 2, 4, 2, 1050, 5000> Tile128x256;
+typedef Costed<4, 2, 4, 8, 2, 1730, 10000> Tile256x256;
+
+// Few rows: blocks of 16 rows a workgroup, workgroups that share a reduction, expected us.  A workgroup reads 120 KB in a us, all of
+// them 15 TB/s (from the caches mostly); a second launch to add shares costs about 5 us of a call, so it has to save more (64 x 100 x 16384 11.9 -> 9.2, but
+// 128 x 128 x 8192 7.8 -> 8.1).
+struct RowsPlan {
+    int rb, splits;
+    double us;
+};
+RowsPlan rows_plan(int64_t rows, int N, int K)
+{
+    RowsPlan p;
+    p.rb = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+    const double groups = (double)((rows + 16 * p.rb - 1) / (16 * p.rb)) * ((N + 15) / 16);
+    const double bytes = 16.0 * (1 + p.rb) * K, alone = bytes / 120e3 * std::ceil(groups / 256);
+    p.splits = 1;
+    p.us = 3 + std::max(alone, groups * bytes / 15e6);
+    if (groups <= 64) {
+        const int most = std::min({16, (int)(256 / groups), (K + 1023) / 1024});
+        if (alone - alone / most > 6) p.splits = most, p.us = 8 + alone / most;
+    }
+    return p;
+}
+
+template <int DT, int RB, int W, int U>
+hipError_t launch_rows(const IntLinearArgs& g, int splits, hipStream_t s)
+{
+    constexpr size_t LDS = (size_t)W * (1 + RB) * U * 1024;
+    const hipError_t e = ensure_dynamic_lds((const void*)int_linear_rows<DT, RB, W, U>, LDS);
+    if (e != hipSuccess) return e;
+    return in_portions<DT>(g, 16 * RB, [&](const IntLinearArgs& p, unsigned y) {
+        hipLaunchKernelGGL((int_linear_rows<DT, RB, W, U>), dim3((unsigned)((g.N + 15) / 16), y, (unsigned)splits), dim3(64 * W), LDS, s, p);
+        if (splits > 1) hipLaunchKernelGGL((int_linear_join<DT>), dim3((unsigned)((p.rows * p.N + 255) / 256)), dim3(256), 0, s, p, splits);
+        return hipGetLastError();
+    });
+}
+
+// Waves a workgroup: a wave has a run of 256 bytes or more up to 1024 and 2048 bytes; 16 waves were no better at 4096 and 16384.
+template <int DT, int RB>
+hipError_t launch_rows(const IntLinearArgs& g, int splits, hipStream_t s)
+{
+    constexpr int U = RB == 1 ? 4 : 2;
+    return g.K <= 1024 ? launch_rows<DT, RB, 4, U>(g, splits, s) : launch_rows<DT, RB, 8, U>(g, splits, s);
+}
+
+// The tiles' offsets are 32 bits; longer strides go to int_linear_any.
+bool long_strides(int64_t lda, int64_t ldw) { return std::max(lda, ldw) >= (1 << 23); }
 
 template <int DT>
 hipError_t launch(IntLinearArgs& g, hipStream_t s)
 {
-    // offsets within a tile are 32 bits
-    const int64_t most = std::max(g.lda, g.ldw);
-    const int64_t tiles = ((g.rows + 255) / 256) * ((g.N + 255) / 256);
-    if (most < (1 << 23) && g.rows > 64 && tiles < (1 << 20)) {
-        if (tiles >= 192) return launch_tiles<DT, Tile256>(g, s);
-        return launch_tiles<DT, Tile128>(g, s);
+    if (long_strides(g.lda, g.ldw))
+        return in_portions<DT>(g, 16, [&](const IntLinearArgs& p, unsigned y) {
+            hipLaunchKernelGGL((int_linear_any<DT>), dim3((unsigned)((g.N + 63) / 64), y), dim3(256), 0, s, p);
+            return hipGetLastError();
+        });
+    const RowsPlan rows = rows_plan(g.rows, g.N, g.K);
+    if (rows.rb == 1) return launch_rows<DT, 1>(g, rows.splits, s);
+    const double us[] = {rows.us, Tile64x64::us(g), Tile64x128::us(g), Tile128x128::us(g), Tile128x256::us(g), Tile256x256::us(g)};
+    switch ((int)(std::min_element(us, us + 6) - us)) {
+        case 0: return rows.rb == 2 ? launch_rows<DT, 2>(g, rows.splits, s) : launch_rows<DT, 4>(g, rows.splits, s);
+        case 1: return launch_tiles<DT, Tile64x64>(g, s);
+        case 2: return launch_tiles<DT, Tile64x128>(g, s);
+        case 3: return launch_tiles<DT, Tile128x128>(g, s);
+        case 4: return launch_tiles<DT, Tile128x256>(g, s);
+        default: return launch_tiles<DT, Tile256x256>(g, s);
     }
-    const int64_t nt = (g.rows + 15) / 16;
-    const dim3 block(256);
-    // gridDim.y is at most 65535: the rows go in portions
-    for (int64_t t = 0; t < nt; t += 65535) {
-        IntLinearArgs p = g;
-        const int64_t skip = t * 16, left = g.rows - skip;
-        p.rows = left < 65535 * 16 ? left : 65535 * 16;
-        p.a += skip * g.lda, p.a_scale += skip, p.out = (char*)g.out + skip * g.ldo * dtype_size(DT);
-        const dim3 grid((unsigned)((g.N + 63) / 64), (unsigned)((p.rows + 15) / 16));
-        hipLaunchKernelGGL((int_linear_tile16<DT>), grid, block, 0, s, p);
-    }
-    return hipGetLastError();
 }
 
 }  // namespace
 
-size_t int_linear_workspace(int64_t rows, int N, int K) { return 0; }
+// (also where another form or the strides turn out to need none: what a caller keeps depends on the sizes alone)
+size_t int_linear_workspace(int64_t rows, int N, int K)
+{
+    if (rows == 0) return 0;
+    const RowsPlan p = rows_plan(rows, N, K);
+    return p.splits > 1 ? (size_t)p.splits * rows * N * 4 : 0;
+}
 
 hipError_t launch_int_linear(IntLinearArgs& g, int dtype, hipStream_t s)
 {

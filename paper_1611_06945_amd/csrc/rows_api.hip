@@ -41,7 +41,7 @@ int check_int_linear(const int_linear_desc* d)
     if (!d) return CONV_EINVAL;
     if (!known(d->dtype)) return CONV_EDTYPE;
     if (d->rows < 0 || d->rows > kMostRows || d->N < 1 || d->K < 1 || d->K >= (1 << 17)) return CONV_EINVAL;
-    if (d->N > INT32_MAX - (1 << 20)) return CONV_EINVAL;
+    if (d->N >= (1 << 24)) return CONV_EINVAL;  // tiles of one band of rows fit a launch
     if (d->lda < d->K || d->ldw < d->K || d->ldo < d->N || d->lda % 16 || d->ldw % 16) return CONV_EINVAL;
     if (d->lda > kMostStride / 256 || d->ldw > kMostStride / 256 || d->ldo > kMostStride / 256) return CONV_EINVAL;
     if (d->flags & ~(uint32_t)CONV_FLAG_RELU) return CONV_EINVAL;

@@ -58,6 +58,13 @@ def test_products(rows, N, K, dtype):
     check(rows, N, K, dtype, relu=rows % 2 == 0, seed=2)
 
 
+@pytest.mark.parametrize("relu", [False, True])
+@pytest.mark.parametrize("rows,N,K", [(1, 10, 40000), (3, 7, 65001), (20, 30, 30000), (64, 100, 16384), (33, 17, 13001), (128, 128, 12000), (100, 1, 100003)])
+def test_reductions_that_workgroups_share(rows, N, K, relu):
+    assert B.int_linear_workspace_bytes(B.make_int_linear_desc(rows, N, K)) > 0
+    check(rows, N, K, DTYPES[K % 3], relu=relu, pad=32, ldo=N + 3, start=1, seed=7)
+
+
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("rows,N,ldo,start", [(3, 50, 53, 1), (40, 130, 131, 3), (300, 300, 311, 5), (300, 260, 264, 1), (600, 512, 520, 0), (17, 1001, 1002, 2)])
 def test_outputs_that_are_slices(rows, N, ldo, start, dtype):
@@ -81,10 +88,11 @@ def test_the_same_call_gives_the_same_bits(rows):
     assert np.array_equal(a, b)
 
 
-def test_more_rows_than_one_launch_holds():
+@pytest.mark.parametrize("rows", [65535 * 16 + 37, 65535 * 64 + 37])
+def test_more_rows_than_one_launch_holds(rows):
     """65535 tiles of rows are one launch's; a narrow product over more of them against the sums by hand."""
     torch = torch_mod()
-    rows, N, K = 65535 * 16 + 37, 3, 16
+    N, K = 3, 16
     g = torch.Generator(device="cuda")
     g.manual_seed(3)
     a = torch.randint(-128, 128, (rows, K), generator=g, device="cuda", dtype=torch.int8)
@@ -113,3 +121,25 @@ def test_operands_beyond_four_gigabytes():
     B.int_linear_fwd(d, a, torch.ones(rows, device="cuda"), w, torch.ones(N, device="cuda"), None, out, ws, need)
     want = a[:, :K].contiguous().float() @ w.float().t().contiguous()
     assert bool((out[:, :N] == want).all()) and bool((out[:, N:N + 64] == 0).all())
+
+
+@pytest.mark.parametrize("dtype", [wl.F32, wl.BF16])
+@pytest.mark.parametrize("rows,N,K", [(40, 9000, 500), (300, 1100, 1300), (900, 1300, 1000), (1100, 4000, 2100), (2100, 4000, 1000), (4200, 4300, 1100), (8300, 500, 260),
+                                      (300, 20000, 130)])
+def test_products_of_every_form(rows, N, K, dtype):
+    """Sums small enough to be whole numbers in the output type are compared bit for bit; each case is another form's."""
+    torch = torch_mod()
+    g = torch.Generator(device="cuda")
+    g.manual_seed(rows)
+    lim = 120 if dtype == wl.F32 else 1
+    A = torch.randint(-lim, lim + 1, (rows, B.row_stride(K) + 16), generator=g, device="cuda", dtype=torch.int8)
+    W = torch.randint(-lim, lim + 1, (N, B.row_stride(K)), generator=g, device="cuda", dtype=torch.int8)
+    sa = torch.randint(1, 3, (rows,), generator=g, device="cuda").float()
+    sw = torch.randint(1, 3, (N,), generator=g, device="cuda").float()
+    out = torch.full((rows, N), float("nan"), device="cuda", dtype=torch_type(dtype))
+    d = B.make_int_linear_desc(rows, N, K, dtype, lda=A.shape[1], ldw=W.shape[1])
+    need = B.int_linear_workspace_bytes(d)
+    ws = torch.empty(max(need, 16), dtype=torch.uint8, device="cuda")
+    B.int_linear_fwd(d, A, sa, W, sw, None, out, ws, need)
+    want = (A[:, :K].double() @ W[:, :K].double().t().contiguous()) * sa.double()[:, None] * sw.double()[None, :]
+    assert bool((out.double() == want.to(out.dtype).double()).all())

@@ -90,7 +90,7 @@ def test_quantize_pointers_that_are_refused():
 
 
 @pytest.mark.parametrize("change", [dict(rows=-1), dict(rows=1 << 31), dict(N=0), dict(K=0), dict(K=1 << 17, lda=1 << 17, ldw=1 << 17), dict(lda=16),
-                                    dict(ldw=16), dict(lda=40), dict(ldw=40), dict(ldo=9), dict(flags=2)])
+                                    dict(ldw=16), dict(lda=40), dict(ldw=40), dict(ldo=9), dict(flags=2), dict(N=1 << 24, ldo=1 << 24)])
 def test_int_linear_descriptors_that_are_refused(change):
     d = B.make_int_linear_desc(4, 10, 20)
     for k, v in change.items():
@@ -106,6 +106,12 @@ def test_int_linear_pointers_that_are_refused():
         args = list(good)
         args[i] = bad
         assert status(B.int_linear_fwd, d, *args, P, 1 << 20, stream=0) == B.CONV_EINVAL, (i, bad)
+    few = B.make_int_linear_desc(4, 10, 1 << 16)
+    need = B.int_linear_workspace_bytes(few)
+    assert need > 0
+    assert status(B.int_linear_fwd, few, *good, None, 0, stream=0) == B.CONV_EWORKSPACE
+    assert status(B.int_linear_fwd, few, *good, P, need - 1, stream=0) == B.CONV_EWORKSPACE
+    assert status(B.int_linear_fwd, few, *good, P + 8, need, stream=0) == B.CONV_EINVAL
     d.dtype = 5
     assert status(B.int_linear_fwd, d, *good, P, 1 << 20, stream=0) == B.CONV_EDTYPE
     assert B.lib().int_linear_fwd(None, P, P, P, P, P, P, None, 0, None) == B.CONV_EINVAL
