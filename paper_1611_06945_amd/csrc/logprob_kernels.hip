@@ -348,23 +348,67 @@ __global__ __launch_bounds__(256) void logprob_join(LogprobArgs a, int splits)
     }
 }
 
+// The gradient: a piece of 16 bytes is read, and written, by one thread.  `per_row` threads (a power of two up to 256) share a row,
+// or, for longer rows, a workgroup has 1024 pieces of one.  x - lse = log p, so with c = g_logp + g_entropy (log p + entropy) every
+// element is -p c, and the target's g_logp more.
 template <int DT>
-__global__ __launch_bounds__(256) void logprob_bwd_any(LogprobArgs a)
+__global__ __launch_bounds__(256) void logprob_bwd_rows(LogprobArgs a, int per_row)
 {
     typedef typename Prec<DT>::elem_t elem_t;
-    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+    typedef Piece<DT> P;
+    constexpr int VEC = P::VEC, U = 4;
+    const int rows_here = 256 / per_row, l = threadIdx.x & (per_row - 1);
+    const int pieces = (a.cols + VEC - 1) / VEC, first = blockIdx.y * (per_row * U);
+    for (int64_t row = (int64_t)blockIdx.x * rows_here + threadIdx.x / per_row; row < a.rows; row += (int64_t)gridDim.x * rows_here) {
         const elem_t* x = (const elem_t*)a.x + row * a.ldx;
         elem_t* dx = (elem_t*)a.dx + row * a.ldg;
+        uint4 raw[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int64_t j = (int64_t)(first + u * per_row + l) * VEC;
+            if (j + VEC <= a.cols) {
+                raw[u] = P::raw(x + j);
+            } else {
+                elem_t e[VEC];
+#pragma unroll
+                for (int k = 0; k < VEC; ++k) e[k] = j + k < a.cols ? x[j + k] : (elem_t)0;
+                __builtin_memcpy(&raw[u], e, 16);
+            }
+        }
         const float lse = a.lse[row];
+        const bool empty = lse == -kInf;
         const int64_t t = a.g_logp ? a.target[row] : -1;
         float g = t >= 0 ? a.g_logp[row] : 0.0f;
         if (t >= a.cols) g = __builtin_nanf("");
         const float gh = a.g_entropy ? a.g_entropy[row] : 0.0f, h = a.g_entropy ? a.entropy[row] : 0.0f;
-        for (int j = threadIdx.x; j < a.cols; j += 256) {
-            const float lp = Prec<DT>::to_f32(x[j]) - lse, p = expf(lp);
-            float v = g * ((j == t ? 1.0f : 0.0f) - p);
-            if (p > 0.0f) v -= gh * (p * (lp + h));
-            dx[j] = Prec<DT>::from_f32(lse == -kInf ? 0.0f : v);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int q = first + u * per_row + l;
+            if (q >= pieces) break;
+            const int64_t j = (int64_t)q * VEC;
+            float f[VEC];
+            P::widen(raw[u], f);
+#pragma unroll
+            for (int k = 0; k < VEC; ++k) {
+                const float lp = f[k] - lse, p = exp_of(lp);
+                f[k] = -p * __builtin_fmaf(gh, fmaxf(lp, -1e20f) + h, g);  // -inf: p is 0
+            }
+            if (t >= j && t < j + VEC) {
+#pragma unroll
+                for (int k = 0; k < VEC; ++k) f[k] += t == j + k ? g : 0.0f;
+            }
+#pragma unroll
+            for (int k = 0; k < VEC; ++k) f[k] = empty ? 0.0f : f[k];
+            const uint4 out = P::narrow(f);
+            if (j + VEC <= a.cols) {
+                P::put(dx + j, out);
+            } else {
+                elem_t e[VEC];
+                __builtin_memcpy(e, &out, 16);
+#pragma unroll
+                for (int k = 0; k < VEC; ++k)
+                    if (j + k < a.cols) dx[j + k] = e[k];
+            }
         }
     }
 }
@@ -425,13 +469,22 @@ hipError_t launch_logprob_fwd(LogprobArgs& a, int dtype, hipStream_t s)
     return dtype == CONV_F32 ? fwd<CONV_F32>(a, s) : dtype == CONV_F16 ? fwd<CONV_F16>(a, s) : fwd<CONV_BF16>(a, s);
 }
 
+template <int DT>
+static hipError_t bwd(const LogprobArgs& a, hipStream_t s)
+{
+    constexpr int VEC = Piece<DT>::VEC;
+    const int pieces = (a.cols + VEC - 1) / VEC;
+    int per_row = 4;  // threads a row: four pieces a thread, up to a workgroup
+    while (per_row < 256 && per_row * 4 < pieces) per_row *= 2;
+    const int64_t blocks = (a.rows + 256 / per_row - 1) / (256 / per_row);
+    const dim3 grid((unsigned)std::min<int64_t>(blocks, 1 << 20), (unsigned)((pieces + per_row * 4 - 1) / (per_row * 4)));
+    hipLaunchKernelGGL((logprob_bwd_rows<DT>), grid, dim3(256), 0, s, a, per_row);
+    return hipGetLastError();
+}
+
 hipError_t launch_logprob_bwd(LogprobArgs& a, int dtype, hipStream_t s)
 {
-    const dim3 grid((unsigned)(a.rows < (1 << 20) ? a.rows : 1 << 20)), block(256);
-    if (dtype == CONV_F32) hipLaunchKernelGGL((logprob_bwd_any<CONV_F32>), grid, block, 0, s, a);
-    else if (dtype == CONV_F16) hipLaunchKernelGGL((logprob_bwd_any<CONV_F16>), grid, block, 0, s, a);
-    else hipLaunchKernelGGL((logprob_bwd_any<CONV_BF16>), grid, block, 0, s, a);
-    return hipGetLastError();
+    return dtype == CONV_F32 ? bwd<CONV_F32>(a, s) : dtype == CONV_F16 ? bwd<CONV_F16>(a, s) : bwd<CONV_BF16>(a, s);
 }
 
 }  // namespace convfwd
