@@ -99,20 +99,31 @@ __device__ __forceinline__ Part block_join(Part p, float* lds)  // lds: 2 * W fl
     return p;
 }
 
-// The rank-th largest (from 0) of 64 keys, one a lane; keys that are not 0 are distinct.  0 if there are not as many.
-__device__ __forceinline__ uint64_t nth_of_wave(uint64_t key, int rank)
+__device__ __forceinline__ uint64_t lane_key(uint64_t key, int l)
+{
+    return ((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(key >> 32), l) << 32) | (uint32_t)__builtin_amdgcn_readlane((int)key, l);
+}
+template <int N>
+__device__ __forceinline__ uint64_t nth_of_lanes(uint64_t key, int rank)
 {
     int before = 0;
-    const uint32_t lo = (uint32_t)key, hi = (uint32_t)(key >> 32);
-#pragma unroll 8
-    for (int l = 0; l < 64; ++l) {
-        const uint64_t o = ((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)hi, l) << 32) | (uint32_t)__builtin_amdgcn_readlane((int)lo, l);
-        before += o > key;
-    }
+#pragma unroll
+    for (int l = 0; l < N; ++l) before += lane_key(key, l) > key;
     const uint64_t hit = __ballot(before == rank && key != 0);
-    if (!hit) return 0;
-    const int l = __builtin_ctzll(hit);
-    return ((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)hi, l) << 32) | (uint32_t)__builtin_amdgcn_readlane((int)lo, l);
+    return hit ? lane_key(key, __builtin_ctzll(hit)) : 0;
+}
+// A bound for the `top` largest of 64 lanes' sets of keys, given each set's largest: the top-th largest of these, or of the largest
+// of two or four lanes where `top` is small beside 16 or 32 (fewer comparisons; for keys in no order 5 of 16 let 6 through, 20 of 32 31).  Keys
+// that are not 0 are distinct; 0 if there are not as many.
+__device__ __forceinline__ uint64_t bound_of_wave(uint64_t key, int top)
+{
+    if (top > 20) return nth_of_lanes<64>(key, top - 1);
+    uint64_t o = __shfl_xor(key, 32, 64);
+    key = o > key ? o : key;
+    if (top > 8) return nth_of_lanes<32>(key, top - 1);
+    o = __shfl_xor(key, 16, 64);
+    key = o > key ? o : key;
+    return nth_of_lanes<16>(key, top - 1);
 }
 
 // The first `top` of n keys in LDS, in order, to best[0..top) (0 where there are fewer): an element's place is the number of greater ones.
@@ -121,8 +132,12 @@ __device__ __forceinline__ void rank_keys(const uint64_t* keys, int n, uint64_t*
 {
     for (int i = threadIdx.x; i < n; i += NT) {
         const uint64_t k = keys[i];
-        int r = 0;
-        for (int j = 0; j < n; ++j) r += keys[j] > k;
+        int r = 0, j = 0;
+        for (; j + 8 <= n; j += 8) {
+#pragma unroll
+            for (int u = 0; u < 8; ++u) r += keys[j + u] > k;
+        }
+        for (; j < n; ++j) r += keys[j] > k;
         if (r < top) best[r] = k;
     }
 }
@@ -141,22 +156,34 @@ __device__ __forceinline__ RowResult result_of(const Part& p)
     return r;
 }
 
-// What a row's results are written from, by the workgroup that has them.
-template <int DT, int NT>
-__device__ __forceinline__ void write_row(const LogprobArgs& a, int64_t row, const Part& p, const uint64_t* best)
+// The target of a row and its logit (NaN where there is no such column), asked for by one thread ahead of the work on the row.
+struct Given {
+    bool any;
+    float logit;
+};
+template <int DT>
+__device__ __forceinline__ Given given_of(const LogprobArgs& a, int64_t row)
 {
-    typedef typename Prec<DT>::elem_t elem_t;
+    Given g = {false, 0.0f};
+    if (a.logp) {
+        const int64_t t = a.target[row];
+        g.any = t >= 0;
+        g.logit = __builtin_nanf("");
+        if (t >= 0 && t < a.cols) g.logit = Prec<DT>::to_f32(((const typename Prec<DT>::elem_t*)a.x)[row * a.ldx + t]);
+    }
+    return g;
+}
+
+// Writes a row's results, by the workgroup that has them; `given` counts in thread 0.
+template <int NT>
+__device__ __forceinline__ void write_row(const LogprobArgs& a, int64_t row, const Given& given, const Part& p, const uint64_t* best)
+{
     const RowResult r = result_of(p);
     if (threadIdx.x == 0) {
         if (a.lse) a.lse[row] = r.lse;
         if (a.entropy) a.entropy[row] = r.h;
-        if (a.logp) {
-            const int64_t t = a.target[row];
-            float v = 0.0f;
-            if (t >= a.cols) v = __builtin_nanf("");
-            else if (t >= 0) v = r.empty ? -kInf : Prec<DT>::to_f32(((const elem_t*)a.x)[row * a.ldx + t]) - r.lse;
-            a.logp[row] = v;
-        }
+        // (a logit of NaN without a NaN in the row: no such column)
+        if (a.logp) a.logp[row] = !given.any ? 0.0f : r.empty && given.logit == given.logit ? -kInf : given.logit - r.lse;
     }
     for (int i = threadIdx.x; i < a.top; i += NT) {
         const uint64_t k = best[i];
@@ -168,99 +195,171 @@ __device__ __forceinline__ void write_row(const LogprobArgs& a, int64_t row, con
 // Partial results of a row that several workgroups share: `splits` parts, then `splits` lists of `top` keys (16 bytes each row's start).
 __host__ __device__ __forceinline__ size_t part_bytes(int top) { return 16 + 8 * (size_t)((top + 1) & ~1); }
 
-// One row, or one of `splits` shares of `share` pieces of it, a workgroup of W waves.  TOP: alternatives are asked for.
-template <int DT, int W, bool TOP>
-__global__ __launch_bounds__(64 * W) void logprob_rows(LogprobArgs a, int splits, int share)
+// One row, or one of `splits` shares of `share` pieces of it, a workgroup of W waves.  Pieces begin at multiples of 16 bytes in memory:
+// the first and the last of a row can be short (its edges); these are left to one thread each, stay out of the maxima, and go to
+// the list element by element.  HELD: a share is at most U pieces a thread, which stay in registers; else pieces are read again
+// for the list.  TOP: alternatives are asked for.
+template <int DT, int W, bool HELD, bool TOP>
+__global__ __launch_bounds__(64 * W, TOP ? 1 : 8) void logprob_rows(LogprobArgs a, int splits, int share)
 {
     typedef typename Prec<DT>::elem_t elem_t;
     typedef Piece<DT> P;
     constexpr int VEC = P::VEC, NT = 64 * W, U = 4;
-    constexpr int LIST = W == 1 ? 640 : 1024;  // at least 64 pieces of 8: rows of so few pieces go there whole
+    constexpr int LIST = W == 1 ? 640 : 1024;  // at least 64 pieces of 8, and the edges: rows of so few pieces go there whole
     __shared__ float red[2 * W];
     __shared__ uint64_t maxima[TOP ? NT : 1], list[TOP ? LIST : 1], best[TOP ? kMostTop : 1], bound;
-    __shared__ uint16_t winner[TOP ? NT : 1];
+    __shared__ uint16_t winner[TOP && !HELD ? NT : 1];
     __shared__ int listed, winners;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int full = a.cols / VEC, rest = a.cols % VEC;  // whole pieces, and elements behind the last
-    const int v0 = blockIdx.y * share, v1 = min(full, v0 + share);
-    const bool has_rest = rest && blockIdx.y == splits - 1;
-
+    
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
-        const elem_t* x = (const elem_t*)a.x + row * a.ldx;
+        const int tid = threadIdx.x;
+        const elem_t* const x = (const elem_t*)a.x + row * a.ldx;
+        const int shift = (int)(((uintptr_t)x / sizeof(elem_t)) % VEC);  // elements of the row's first 16 bytes that are not its own
+        const elem_t* const base = x - shift;                            // element j is base[shift + j]; pieces start at base
+        const int whole_end = (int)(((int64_t)a.cols + shift) / VEC);    // whole pieces: shift > 0 .. whole_end
+        const int v0 = max((int)blockIdx.y * share, shift > 0 ? 1 : 0), v1 = min(whole_end, ((int)blockIdx.y + 1) * share);
+        const int head = shift ? min(VEC - shift, a.cols) : 0, tail = max(whole_end * VEC - shift, head);  // edges: [0, head), [tail, cols)
+        // the first share has the first edge, the last one the last
+        const int e0 = blockIdx.y == 0 && tid == 0 ? 0 : tail, e0_end = blockIdx.y == 0 && tid == 0 ? head : tail;
+        const int e1 = blockIdx.y == splits - 1 && tid == NT - 1 ? tail : a.cols;
+        Given given = {false, 0.0f};
+        if (tid == 0 && splits == 1) given = given_of<DT>(a, row);
+
         Part p = {kLowest, 0.0f, 0.0f};
         float most = -kInf;
         int at = -1;  // the piece with `most`
-        auto rest_piece = [&](float (&f)[VEC]) {
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) f[i] = i < rest ? Prec<DT>::to_f32(x[(int64_t)full * VEC + (i < rest ? i : 0)]) : -kInf;
-        };
+        uint4 raw[U];
+        auto whole = [&](int v) { return P::raw((const elem_t*)__builtin_assume_aligned(base + (int64_t)v * VEC, 16)); };
         auto note = [&](float m, int v) {
             if (TOP && m > most) most = m, at = v;
         };
-        int v = v0 + tid;
-        for (; v + (U - 1) * NT < v1; v += U * NT) {
-            uint4 raw[U];
-#pragma unroll
-            for (int u = 0; u < U; ++u) raw[u] = P::raw(x + (int64_t)(v + u * NT) * VEC);
-            float f[U][VEC], m[U];
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                P::widen(raw[u], f[u]);
-                m[u] = piece_max(f[u]);
-                note(m[u], v + u * NT);
-            }
-            const float mm = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
-            if (mm > p.m) rebase(p, mm);
-#pragma unroll
-            for (int u = 0; u < U; ++u) add_piece(p, f[u]);
-        }
-        for (; v < v1 || (has_rest && v == full); v += NT) {
-            float f[VEC];
-            if (v < v1) P::widen(P::raw(x + (int64_t)v * VEC), f);
-            else rest_piece(f);
-            const float m = piece_max(f);
-            note(m, v);
-            if (m > p.m) rebase(p, m);
+        auto element = [&](int j) {
+            const float f[2] = {Prec<DT>::to_f32(x[j]), -kInf};
+            if (f[0] > p.m) rebase(p, f[0]);
             add_piece(p, f);
+        };
+        int v = v0 + tid;
+        if constexpr (HELD) {
+            float m = -kInf;
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (v + u * NT < v1) raw[u] = whole(v + u * NT);
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (v + u * NT < v1) {
+                    float f[VEC];
+                    P::widen(raw[u], f);
+                    const float mu = piece_max(f);
+                    note(mu, v + u * NT);
+                    m = fmaxf(m, mu);
+                }
+            p.m = fmaxf(p.m, m);
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (v + u * NT < v1) {
+                    float f[VEC];
+                    P::widen(raw[u], f);
+                    add_piece(p, f);
+                }
+        } else {
+            for (; v + (U - 1) * NT < v1; v += U * NT) {
+                float m[U];
+#pragma unroll
+                for (int u = 0; u < U; ++u) raw[u] = whole(v + u * NT);
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    float f[VEC];
+                    P::widen(raw[u], f);
+                    m[u] = piece_max(f);
+                    note(m[u], v + u * NT);
+                }
+                const float mm = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
+                if (mm > p.m) rebase(p, mm);
+                // (widened again: 32 floats kept from above would cost a third of the waves)
+#pragma unroll
+                for (int u = 0; u < U; ++u) asm volatile("" : "+v"(raw[u].x), "+v"(raw[u].y), "+v"(raw[u].z), "+v"(raw[u].w));
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    float f[VEC];
+                    P::widen(raw[u], f);
+                    add_piece(p, f);
+                }
+            }
+            for (; v < v1; v += NT) {
+                float f[VEC];
+                P::widen(whole(v), f);
+                const float m = piece_max(f);
+                note(m, v);
+                if (m > p.m) rebase(p, m);
+                add_piece(p, f);
+            }
         }
+        for (int j = e0; j < e0_end; ++j) element(j);
+        for (int j = e1; j < a.cols; ++j) element(j);
         __syncthreads();  // the previous row's LDS is free
+        // (made unknown here, or what the selection computes from it would be kept in registers while the row is read)
+        int sel = threadIdx.x;
+        asm volatile("" : "+v"(sel));
+        const int lane = sel & 63, wave = sel >> 6;
+        if constexpr (TOP) {
+            if (at < 0 && v0 + sel < v1) at = v0 + sel;  // nothing but -inf
+            maxima[sel] = at < 0 ? 0 : key_of(most, (uint32_t)at);
+            for (int i = sel; i < kMostTop; i += NT) best[i] = 0;
+            if (sel == 0) listed = 0, winners = 0;
+        }
         p = block_join<W>(p, red);
         if constexpr (TOP) {
-            const int end = v1 + (has_rest ? 1 : 0);  // pieces of this workgroup, the last one short
-            if (at < 0 && v0 + tid < end) at = v0 + tid;  // nothing but -inf
-            const uint64_t mine = at < 0 ? 0 : key_of(most, (uint32_t)at);
-            maxima[tid] = mine;
-            for (int i = tid; i < kMostTop; i += NT) best[i] = 0;
-            if (tid == 0) listed = 0, winners = 0;
-            __syncthreads();
+            if constexpr (W == 1) __syncthreads();
             if (wave == 0) {
                 uint64_t k = maxima[lane];
 #pragma unroll
                 for (int w = 1; w < W; ++w) k = maxima[w * 64 + lane] > k ? maxima[w * 64 + lane] : k;
-                const uint64_t b = nth_of_wave(k, a.top - 1);
+                const uint64_t b = bound_of_wave(k, a.top);
                 if (lane == 0) bound = b;
             }
             __syncthreads();
-            const uint64_t b = bound;
+            const uint64_t b = bound, mine = maxima[sel];
             const uint32_t b_order = (uint32_t)(b >> 32), b_piece = b ? index_of(b) : 0xFFFFFFFFu;
             const bool odd = !(p.s >= 0.0f);  // a NaN or an infinity
-            if (!odd) {
-                if (mine && mine >= b) winner[atomicAdd(&winners, 1)] = (uint16_t)tid;
-                __syncthreads();
-                const int n = winners;
-                for (int i = wave; i < n; i += W) {
-                    for (int q = v0 + winner[i] + lane * NT; q < end; q += 64 * NT) {
-                        float f[VEC];
-                        if (q < v1) P::widen(P::raw(x + (int64_t)q * VEC), f);
-                        else rest_piece(f);
+            // (value, piece) not below the bound: an element of piece q goes to the list
+            auto offer = [&](float f, int q, int j) {
+                const uint32_t o = order_of(f);
+                if (o > b_order || (o == b_order && (uint32_t)q <= b_piece)) {
+                    const int to = atomicAdd(&listed, 1);
+                    if (to < LIST) list[to] = key_of(f, (uint32_t)j);
+                }
+            };
+            auto offer_piece = [&](const uint4& r, int q) {
+                float f[VEC];
+                P::widen(r, f);
 #pragma unroll
-                        for (int e = 0; e < VEC; ++e) {
-                            const uint32_t o = order_of(f[e]);
-                            if ((o > b_order || (o == b_order && (uint32_t)q <= b_piece)) && q * VEC + e < a.cols) {
-                                const int to = atomicAdd(&listed, 1);
-                                if (to < LIST) list[to] = key_of(f[e], (uint32_t)(q * VEC + e));
-                            }
-                        }
+                for (int e = 0; e < VEC; ++e) offer(f[e], q, q * VEC - shift + e);
+            };
+            if (!odd) {
+                for (int j = e0; j < e0_end; ++j) offer(Prec<DT>::to_f32(x[j]), 0, j);
+                for (int j = e1; j < a.cols; ++j) offer(Prec<DT>::to_f32(x[j]), whole_end, j);
+                if constexpr (HELD) {
+                    if (mine && mine >= b) {
+#pragma unroll
+                        for (int u = 0; u < U; ++u)
+                            if (v + u * NT < v1) offer_piece(raw[u], v + u * NT);
+                    }
+                } else {
+                    if (mine && mine >= b) winner[atomicAdd(&winners, 1)] = (uint16_t)sel;
+                    __syncthreads();
+                    // the winners' pieces, 2^log of them each, dealt to all threads; the next one is on its way while one is looked at
+                    const int log = 32 - __builtin_clz(max(v1 - v0 - 1, 0) / NT);
+                    const int all = winners << log;
+                    auto piece = [&](int i) { return i < all ? v0 + winner[i >> log] + (i & ((1 << log) - 1)) * NT : v1; };
+                    int q = piece(sel);
+                    uint4 r;
+                    if (q < v1) r = whole(q);
+                    for (int i = sel; i < all; i += NT) {
+                        const int q_now = q;
+                        const uint4 now = r;
+                        q = piece(i + NT);
+                        if (q < v1) r = whole(q);
+                        if (q_now < v1) offer_piece(now, q_now);
                     }
                 }
                 __syncthreads();
@@ -268,11 +367,11 @@ __global__ __launch_bounds__(64 * W) void logprob_rows(LogprobArgs a, int splits
             if (!odd && listed <= LIST) {
                 rank_keys<NT>(list, listed, best, a.top);
             } else {
-                const int j0 = v0 * VEC, j1 = has_rest ? a.cols : v1 * VEC;
+                const int j0 = blockIdx.y == 0 ? 0 : min(v0 * VEC - shift, tail), j1 = blockIdx.y == splits - 1 ? a.cols : v1 * VEC - shift;
                 uint64_t last = ~0ull;
                 for (int i = 0; i < a.top; ++i) {
                     uint64_t k = 0;
-                    for (int j = j0 + tid; j < j1; j += NT) {
+                    for (int j = j0 + sel; j < j1; j += NT) {
                         const uint64_t c = key_of(Prec<DT>::to_f32(x[j]), (uint32_t)j);
                         if (c < last && c > k) k = c;
                     }
@@ -283,19 +382,19 @@ __global__ __launch_bounds__(64 * W) void logprob_rows(LogprobArgs a, int splits
                     k = list[0];
 #pragma unroll
                     for (int w = 1; w < W; ++w) k = list[w] > k ? list[w] : k;
-                    if (tid == 0) best[i] = k;
+                    if (sel == 0) best[i] = k;
                     last = k;
                 }
             }
             __syncthreads();
         }
         if (splits == 1) {
-            write_row<DT, NT>(a, row, p, best);
+            write_row<NT>(a, row, given, p, best);
         } else {
             char* ws = (char*)a.ws + (size_t)row * splits * part_bytes(a.top);
-            if (tid == 0) ((float4*)ws)[blockIdx.y] = make_float4(p.m, p.s, p.sd, 0.0f);
+            if (sel == 0) ((float4*)ws)[blockIdx.y] = make_float4(p.m, p.s, p.sd, 0.0f);
             uint64_t* keys = (uint64_t*)(ws + 16 * (size_t)splits) + (size_t)blockIdx.y * a.top;
-            for (int i = tid; i < a.top; i += NT) keys[i] = best[i];
+            for (int i = sel; i < a.top; i += NT) keys[i] = best[i];
         }
     }
 }
@@ -306,46 +405,53 @@ constexpr int kMostSplits = 64;
 template <int DT>
 __global__ __launch_bounds__(256) void logprob_join(LogprobArgs a, int splits)
 {
-    constexpr int NT = 256;
+    constexpr int NT = 256, MOST = kMostSplits * kMostTop / NT;
     __shared__ float red[8];
     __shared__ uint64_t maxima[NT], list[kMostSplits * kMostTop], best[kMostTop], bound;
     __shared__ int listed;
     const int tid = threadIdx.x, lane = tid & 63;
-    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
-        const char* ws = (const char*)a.ws + (size_t)row * splits * part_bytes(a.top);
-        Part p = {kLowest, 0.0f, 0.0f};
-        if (tid < splits) {
-            const float4 f = ((const float4*)ws)[tid];
-            p.m = f.x, p.s = f.y, p.sd = f.z;
+    const int64_t row = blockIdx.x;
+    const char* ws = (const char*)a.ws + (size_t)row * splits * part_bytes(a.top);
+    const uint64_t* keys = (const uint64_t*)(ws + 16 * (size_t)splits);
+    const int n = splits * a.top;
+    Given given = {false, 0.0f};
+    if (tid == 0) given = given_of<DT>(a, row);
+    uint64_t mine[MOST], most = 0;
+#pragma unroll
+    for (int i = 0; i < MOST; ++i) {
+        mine[i] = 0;
+        if (i * NT < n && i * NT + tid < n) mine[i] = keys[i * NT + tid];
+    }
+    Part p = {kLowest, 0.0f, 0.0f};
+    if (tid < splits) {
+        const float4 f = ((const float4*)ws)[tid];
+        p.m = f.x, p.s = f.y, p.sd = f.z;
+    }
+    if (tid == 0) listed = 0;
+    for (int i = tid; i < kMostTop; i += NT) best[i] = 0;
+    p = block_join<4>(p, red);
+    if (a.top) {
+#pragma unroll
+        for (int i = 0; i < MOST; ++i) most = mine[i] > most ? mine[i] : most;
+        maxima[tid] = most;
+        __syncthreads();
+        if (tid < 64) {
+            uint64_t k = maxima[lane];
+#pragma unroll
+            for (int w = 1; w < 4; ++w) k = maxima[w * 64 + lane] > k ? maxima[w * 64 + lane] : k;
+            const uint64_t b = bound_of_wave(k, a.top);
+            if (lane == 0) bound = b ? b : 1;  // a key of 0 stands for no element
         }
         __syncthreads();
-        p = block_join<4>(p, red);
-        if (a.top) {
-            const uint64_t* keys = (const uint64_t*)(ws + 16 * (size_t)splits);
-            const int n = splits * a.top;
-            uint64_t most = 0;
-            for (int i = tid; i < n; i += NT) most = keys[i] > most ? keys[i] : most;
-            maxima[tid] = most;
-            for (int i = tid; i < kMostTop; i += NT) best[i] = 0;
-            if (tid == 0) listed = 0;
-            __syncthreads();
-            if (tid < 64) {
-                uint64_t k = maxima[lane];
+        const uint64_t b = bound;
 #pragma unroll
-                for (int w = 1; w < 4; ++w) k = maxima[w * 64 + lane] > k ? maxima[w * 64 + lane] : k;
-                const uint64_t b = nth_of_wave(k, a.top - 1);
-                if (lane == 0) bound = b;
-            }
-            __syncthreads();
-            const uint64_t b = bound ? bound : 1;  // 0 stands for no element
-            for (int i = tid; i < n; i += NT)
-                if (keys[i] >= b) list[atomicAdd(&listed, 1)] = keys[i];
-            __syncthreads();
-            rank_keys<NT>(list, listed, best, a.top);
-            __syncthreads();
-        }
-        write_row<DT, NT>(a, row, p, best);
+        for (int i = 0; i < MOST; ++i)
+            if (mine[i] >= b) list[atomicAdd(&listed, 1)] = mine[i];
+        __syncthreads();
+        rank_keys<NT>(list, listed, best, a.top);
+        __syncthreads();
     }
+    write_row<NT>(a, row, given, p, best);
 }
 
 // The gradient: a piece of 16 bytes is read, and written, by one thread.  `per_row` threads (a power of two up to 256) share a row,
@@ -413,45 +519,45 @@ __global__ __launch_bounds__(256) void logprob_bwd_rows(LogprobArgs a, int per_r
     }
 }
 
-// How a row is shared: one workgroup where the rows alone fill the GPU (two workgroups a CU), else as many as leave each of them
-// two pieces a thread, up to 64.
+// How a row is shared.  Waves a workgroup: one for rows of up to 256 pieces, which it holds; four up to 8192, so that several
+// workgroups of a CU cover each other's selections; eight beyond (2048 rows, 5 alternatives, us with four / eight waves: 50257 bf16 53 / 61,
+// 131072 bf16 110 / 104, 50257 fp32 81 / 79).  Fewer rows than CUs are shared by 256 / rows workgroups, as far as that leaves each of
+// them two pieces a thread, up to 64 (256 rows of 50257 fp16 in one each 14 us, in two 17).  A row that starts within 16 bytes
+// can touch a piece more than its length says: `pieces` is the most.
 struct Shares {
     int waves, splits, share;
+    bool held;
 };
 Shares shares_of(int64_t rows, int cols, int dtype)
 {
-    const int vec = dtype == CONV_F32 ? 4 : 8, full = cols / vec;
+    const int vec = dtype == CONV_F32 ? 4 : 8, pieces = cols / vec + 2;
     Shares s;
-    s.waves = full <= 256 ? 1 : full <= 1024 ? 4 : 8;
-    int64_t want = (512 + rows - 1) / std::max<int64_t>(rows, 1);
-    want = std::min<int64_t>(want, kMostSplits);
-    if (want > 1 && full > 1024) {
-        s.waves = 4;
-        want = std::min<int64_t>(want, full / 512);
-    } else {
-        want = 1;
-    }
-    s.share = (int)((full + want - 1) / want);
-    s.splits = s.share ? (full + s.share - 1) / s.share : 1;
-    if (s.splits < 1) s.splits = 1;
+    s.waves = pieces <= 256 ? 1 : pieces <= 8192 ? 4 : 8;
+    int64_t want = pieces > 1024 ? (256 + rows - 1) / std::max<int64_t>(rows, 1) : 1;
+    want = std::max<int64_t>(1, std::min<int64_t>({want, kMostSplits, pieces / 512}));
+    if (want > 1) s.waves = 4;
+    s.share = (int)((pieces + want - 1) / want);
+    s.splits = (pieces + s.share - 1) / s.share;
+    s.held = s.share <= 4 * 64 * s.waves;
     return s;
 }
 
-template <int DT, int W>
-void launch_w(LogprobArgs& a, const Shares& sh, hipStream_t s)
+template <int DT, int W, bool HELD>
+void launch_w(const LogprobArgs& a, const Shares& sh, hipStream_t s)
 {
     const dim3 grid((unsigned)std::min<int64_t>(a.rows, 1 << 18), (unsigned)sh.splits), block(64 * W);
-    if (a.top) hipLaunchKernelGGL((logprob_rows<DT, W, true>), grid, block, 0, s, a, sh.splits, sh.share);
-    else hipLaunchKernelGGL((logprob_rows<DT, W, false>), grid, block, 0, s, a, sh.splits, sh.share);
+    if (a.top) hipLaunchKernelGGL((logprob_rows<DT, W, HELD, true>), grid, block, 0, s, a, sh.splits, sh.share);
+    else hipLaunchKernelGGL((logprob_rows<DT, W, HELD, false>), grid, block, 0, s, a, sh.splits, sh.share);
 }
 
 template <int DT>
-hipError_t fwd(LogprobArgs& a, hipStream_t s)
+hipError_t fwd(const LogprobArgs& a, hipStream_t s)
 {
     const Shares sh = shares_of(a.rows, a.cols, DT);
-    if (sh.waves == 1) launch_w<DT, 1>(a, sh, s);
-    else if (sh.waves == 4) launch_w<DT, 4>(a, sh, s);
-    else launch_w<DT, 8>(a, sh, s);
+    if (sh.waves == 1) launch_w<DT, 1, true>(a, sh, s);
+    else if (sh.waves == 4 && sh.held) launch_w<DT, 4, true>(a, sh, s);
+    else if (sh.waves == 4) launch_w<DT, 4, false>(a, sh, s);
+    else launch_w<DT, 8, false>(a, sh, s);
     if (sh.splits > 1) hipLaunchKernelGGL((logprob_join<DT>), dim3((unsigned)a.rows), dim3(256), 0, s, a, sh.splits);
     return hipGetLastError();
 }

@@ -133,8 +133,9 @@ __global__ __launch_bounds__(G <= 256 ? 256 : G) void norm_fwd_rows(NormArgs a)
     const float inv_cols = 1.0f / (float)a.cols;
     auto at = [&](int64_t r) { return (const elem_t*)a.x + (r < a.rows ? r : a.rows - 1) * a.ldx; };
 
+    constexpr bool AHEAD = G < 1024 || NV * VEC < 32;  // (no registers for the next row: 16 waves with 32 elements a lane)
     uint4 next[NV];
-    H::load(next, at(row), a.cols, l);
+    if (AHEAD) H::load(next, at(row), a.cols, l);
     float gamma[NV][VEC], beta[NV][VEC];
     if constexpr (MODE != QUANT_ONLY) {
         H::columns(gamma, a.gamma, 1.0f, a.cols, l);
@@ -142,10 +143,11 @@ __global__ __launch_bounds__(G <= 256 ? 256 : G) void norm_fwd_rows(NormArgs a)
     }
     // every lane of a workgroup makes the same number of rounds: the reductions of wide rows have barriers
     for (int64_t first = (int64_t)blockIdx.x * ROWS; first < a.rows; first += step, row += step) {
+        if (!AHEAD) H::load(next, at(row), a.cols, l);
         float x[NV][VEC];
 #pragma unroll
         for (int i = 0; i < NV; ++i) H::P::widen(next[i], x[i]);
-        if (first + step < a.rows) H::load(next, at(row + step), a.cols, l);
+        if (AHEAD && first + step < a.rows) H::load(next, at(row + step), a.cols, l);
         if constexpr (MODE != QUANT_ONLY) {
             float sum = 0.0f;
 #pragma unroll
@@ -226,7 +228,9 @@ __global__ __launch_bounds__(NT) void norm_bwd_rows(NormArgs a)
         H::load(ndy, (const elem_t*)a.dy + r * a.ldy, a.cols, l);
         nmean = a.mean[r], nrstd = a.rstd[r];
     };
-    if (a.rows) fetch(row);
+    // (16 waves with 16 elements a lane have no registers left for the next row: they spilled 50 .. 70)
+    constexpr bool AHEAD = G < 1024 || NV * VEC < 16;
+    if (AHEAD && a.rows) fetch(row);
     float gamma[NV][VEC], dg[NV][VEC], db[NV][VEC];
     if constexpr (DX) H::columns(gamma, a.gamma, 1.0f, a.cols, l);
 #pragma unroll
@@ -235,6 +239,7 @@ __global__ __launch_bounds__(NT) void norm_bwd_rows(NormArgs a)
         for (int k = 0; k < VEC; ++k) dg[i][k] = db[i][k] = 0.0f;
 
     for (int64_t first = (int64_t)blockIdx.x * ROWS; first < a.rows; first += step, row += step) {
+        if (!AHEAD) fetch(row);
         float x[NV][VEC], dy[NV][VEC];
         const float mean = nmean, rstd = nrstd;
 #pragma unroll
@@ -242,7 +247,7 @@ __global__ __launch_bounds__(NT) void norm_bwd_rows(NormArgs a)
             H::P::widen(nx[i], x[i]);
             H::P::widen(ndy[i], dy[i]);
         }
-        if (first + step < a.rows) fetch(row + step);
+        if (AHEAD && first + step < a.rows) fetch(row + step);
         const bool in = row < a.rows;
         float s1 = 0.0f, s2 = 0.0f;
 #pragma unroll
@@ -338,30 +343,37 @@ __global__ __launch_bounds__(NT) void norm_bwd_rows(NormArgs a)
     }
 }
 
-// The sums of `parts` workgroups: 64 columns and 16 waves a workgroup, a wave every 16th part, then the waves in order.
+// The sums of `parts` workgroups: C columns and 1024 / C groups of lanes a workgroup, a group every so many parts, then the groups in order.
+template <int C>
 __global__ __launch_bounds__(1024) void norm_dw_join(NormArgs a, int parts)
 {
-    __shared__ float red[16][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t j = (int64_t)blockIdx.x * 64 + lane;  // dgamma's columns, then dbeta's
+    constexpr int GROUPS = 1024 / C;
+    __shared__ float red[GROUPS][C];
+    const int l = threadIdx.x % C, group = threadIdx.x / C;
+    const int64_t j = (int64_t)blockIdx.x * C + l;  // dgamma's columns, then dbeta's
     float s = 0.0f;
     if (j < 2 * (int64_t)a.cols) {
-        int p = wave;
-        for (; p + 48 < parts; p += 64) {
+        int p = group;
+        for (; p + 3 * GROUPS < parts; p += 4 * GROUPS) {
             float v[4];
 #pragma unroll
-            for (int u = 0; u < 4; ++u) v[u] = a.ws[(size_t)(p + 16 * u) * 2 * a.cols + j];
+            for (int u = 0; u < 4; ++u) v[u] = a.ws[(size_t)(p + GROUPS * u) * 2 * a.cols + j];
 #pragma unroll
             for (int u = 0; u < 4; ++u) s += v[u];
         }
-        for (; p < parts; p += 16) s += a.ws[(size_t)p * 2 * a.cols + j];
+        for (; p < parts; p += GROUPS) s += a.ws[(size_t)p * 2 * a.cols + j];
     }
-    red[wave][lane] = s;
+    red[group][l] = s;
     __syncthreads();
-    if (wave == 0 && j < 2 * (int64_t)a.cols) {
-        s = red[0][lane];
+    if (group == 0 && j < 2 * (int64_t)a.cols) {
+        float v[16];
 #pragma unroll
-        for (int w = 1; w < 16; ++w) s += red[w][lane];
+        for (int g = 0; g < GROUPS; g += 16) {
+#pragma unroll
+            for (int u = 0; u < 16; ++u) v[u] = red[g + u][l];
+#pragma unroll
+            for (int u = 0; u < 16; ++u) s = g + u ? s + v[u] : v[u];
+        }
         float* to = j < a.cols ? a.dgamma : a.dbeta;
         if (to) to[j < a.cols ? j : j - a.cols] = s;
     }
@@ -512,14 +524,15 @@ hipError_t fwd_type(const NormArgs& a, int dtype, hipStream_t s)
 // Backward a lane holds 16 elements at most: with their gradients, sums and the next row that is what 16 waves have registers for.
 Form bwd_form(int cols, int dtype) { return form_of(cols, dtype, dtype == CONV_F32 ? 4 : 2); }
 
-// Workgroups of the backward kernel: a sum of 2 * cols floats each is written and read again.
+// Workgroups of the backward kernel: one a CU, as a sum of 2 * cols floats each is written and read again, or two where a lane has
+// one piece only (us with 256 / 512: 16384 x 4096 bf16 79 / 84, 200704 x 192 fp32 95 / 101, 200704 x 64 fp16 42 / 31, 20000 x 384 fp16 23 / 19).
 int bwd_threads(int lanes) { return lanes == 1024 ? 1024 : 512; }
 int bwd_parts(int64_t rows, int cols, int dtype)
 {
     const Form f = bwd_form(cols, dtype);
     if (!f.lanes) return (int)std::max<int64_t>(1, std::min<int64_t>(64, (rows + 15) / 16));
     const int here = bwd_threads(f.lanes) / f.lanes;
-    return (int)std::max<int64_t>(1, std::min<int64_t>(cols <= 1024 ? 2 * kCUs : kCUs, (rows + here - 1) / here));
+    return (int)std::max<int64_t>(1, std::min<int64_t>(f.pieces == 1 && f.lanes < 256 ? 2 * kCUs : kCUs, (rows + here - 1) / here));
 }
 
 template <int DT, int G, int NV>
@@ -541,6 +554,14 @@ void bwd_pieces(const NormArgs& a, int nv, int parts, hipStream_t s)
     else if constexpr (DT == CONV_F32) bwd_launch<DT, G, 4>(a, parts, s);
 }
 
+// 64 columns a workgroup where that makes a workgroup a CU, else 16: 423 sums of 2 x 384 columns took 4.7 us with 64.
+void join(const NormArgs& a, int parts, hipStream_t s)
+{
+    const int64_t cols = 2 * (int64_t)a.cols;
+    if (cols >= 64 * kCUs) hipLaunchKernelGGL((norm_dw_join<64>), dim3((unsigned)((cols + 63) / 64)), dim3(1024), 0, s, a, parts);
+    else hipLaunchKernelGGL((norm_dw_join<16>), dim3((unsigned)((cols + 15) / 16)), dim3(1024), 0, s, a, parts);
+}
+
 template <int DT>
 hipError_t bwd(const NormArgs& a, hipStream_t s)
 {
@@ -557,7 +578,7 @@ hipError_t bwd(const NormArgs& a, hipStream_t s)
         if (a.dx && a.rows) hipLaunchKernelGGL((norm_dx_any<DT>), dim3((unsigned)std::min<int64_t>(a.rows, 1 << 20)), dim3(1024), 0, s, a);
     }
     if (dw && (parts > 1 || !f.lanes))
-        hipLaunchKernelGGL(norm_dw_join, dim3((unsigned)((2 * (int64_t)a.cols + 63) / 64)), dim3(1024), 0, s, a, parts);
+        join(a, parts, s);
     return hipGetLastError();
 }
 
