@@ -1,0 +1,146 @@
+"""The operators on rows run together: the scoring head in 8 bits and the training head against the same layers in 64 bits, on
+streams, from threads, and from a recorded graph."""
+import threading
+
+import numpy as np
+import pytest
+
+from oracle import rows_oracle as ro
+from paper_1611_06945_amd import binding as B
+from paper_1611_06945_amd import workloads as wl
+from paper_1611_06945_amd.head import ScoringHead, TrainingHead, demo
+
+from gpu_util import torch_mod
+from rows_util import ROUND, stored, torch_type
+
+pytestmark = pytest.mark.gpu
+
+
+def case(T, D, V, dtype, seed):
+    torch = torch_mod()
+    rng = np.random.default_rng(seed)
+    c = {"x": stored(rng.normal(size=(T, D)) * 2 + 0.5, dtype), "w": stored(rng.normal(size=(V, D)) * 2 * D ** -0.5, dtype),
+         "gamma": rng.normal(1, 0.2, D).astype(np.float32).astype(np.float64), "beta": rng.normal(0, 0.2, D).astype(np.float32).astype(np.float64),
+         "bias": rng.normal(0, 0.2, V).astype(np.float32).astype(np.float64), "target": rng.integers(0, V, T)}
+    d = {k: torch.from_numpy(c[k]).cuda().to(torch_type(dtype)) for k in ("x", "w")}
+    d.update({k: torch.from_numpy(c[k].astype(np.float32)).cuda() for k in ("gamma", "beta", "bias")})
+    d["target"] = torch.from_numpy(c["target"]).cuda()
+    return c, d
+
+
+@pytest.mark.parametrize("dtype", [wl.F32, wl.F16, wl.BF16])
+@pytest.mark.parametrize("T,D,V", [(1, 64, 1000), (20, 384, 1000), (3, 100, 9001), (130, 256, 333)])
+def test_scoring_head(T, D, V, dtype):
+    """The 8-bit layers' logits as stored, then the exact operators: the head's answers are those of its own logits; the logits
+    are those of the unquantised layers within the error of the 8-bit codes."""
+    c, d = case(T, D, V, dtype, T)
+    head = ScoringHead(d["gamma"], d["beta"], d["w"], d["bias"], max_rows=T + 3, top=5)
+    r = head.score(d["x"], d["target"])
+    logits = head.logits[:T].double().cpu().numpy()
+    want = ro.logprob(logits, c["target"], 5)
+    for k in ("logp", "lse", "entropy", "top_logp"):
+        assert np.allclose(r[k].cpu().numpy(), want[k], atol=2e-5, rtol=2e-5), k
+    assert np.array_equal(r["top_id"].cpu().numpy(), want["top_id"])
+    y = ro.layernorm(c["x"], c["gamma"], c["beta"], 1e-5)[0]
+    exact = y @ c["w"].T + c["bias"]
+    # a code is off by half a step of amax / 127 at most on either side; the roundings of a row's products are independent, of
+    # random sign: six standard deviations of sum(dy w + y dw) over D, and the storage type's roundings of y and of the logits
+    step_y, step_w = np.abs(y).max(1) / 127, np.abs(c["w"]).max(1) / 127
+    sd = np.sqrt((step_y ** 2 / 12)[:, None] * (c["w"] ** 2).sum(1)[None] + (step_w ** 2 / 12)[None] * (y ** 2).sum(1)[:, None]
+                 + ROUND[dtype] ** 2 * (y ** 2) @ (c["w"] ** 2).T)
+    off = np.abs(logits - exact)
+    assert (off > 6 * sd + ROUND[dtype] * np.abs(exact) + 1e-5).sum() <= 1e-6 * off.size
+    assert head.score(d["x"])["logp"] is None
+
+
+@pytest.mark.parametrize("dtype", [wl.F32, wl.F16])
+@pytest.mark.parametrize("T,D,V", [(1, 32, 10), (48, 96, 1000), (33, 100, 130)])
+def test_training_head(T, D, V, dtype):
+    c, d = case(T, D, V, dtype, T + D)
+    torch = torch_mod()
+    head = TrainingHead(T, D, V, torch_type(dtype))
+    logp, entropy = head.forward(d["x"], d["gamma"], d["beta"], d["w"], d["target"])
+    rng = np.random.default_rng(5)
+    gl, gh = rng.normal(size=T).astype(np.float32), rng.normal(size=T).astype(np.float32)
+    y, mean, rstd = ro.layernorm(c["x"], c["gamma"], c["beta"], 1e-5)
+    logits = y @ c["w"].T
+    r = ro.logprob(logits, c["target"], 0)
+    # activations and logits are stored in 8 or 11 or 24 bits: errors relative to each tensor's size, a few roundings deep
+    u = 8 * ROUND[dtype] + 2e-5
+
+    def near(got, want, what):
+        got = got.double().cpu().numpy()
+        assert np.linalg.norm(got - want) <= u * np.linalg.norm(want) + u * 1e-3, what
+
+    near(logp, r["logp"], "logp")
+    near(entropy, r["entropy"], "entropy")
+    dx, dgamma, dbeta, dw = head.backward(torch.from_numpy(gl).cuda(), torch.from_numpy(gh).cuda())
+    dl = ro.logprob_bwd(logits, c["target"], r["lse"], r["entropy"], gl.astype(np.float64), gh.astype(np.float64))
+    want_dx, want_dg, want_db = ro.layernorm_bwd(c["x"], dl @ c["w"], c["gamma"], mean, rstd)
+    near(dw, dl.T @ y, "dweight")
+    near(dx, want_dx, "dfeatures")
+    near(dgamma, want_dg, "dgamma")
+    near(dbeta, want_db, "dbeta")
+
+
+def test_demo_learns_and_the_8_bit_head_agrees():
+    first, last, hit = demo(rows=256, D=128, V=200, steps=30, log=lambda *_: None)
+    assert last > first + 2.0 and hit > 0.95
+
+
+def test_scoring_on_streams_from_threads_equals_the_serial_calls():
+    torch = torch_mod()
+    shapes = [(1, 512, 20000), (20, 384, 1000), (64, 100, 3001), (300, 256, 700)]
+    jobs = [(ScoringHead(d["gamma"], d["beta"], d["w"], d["bias"], max_rows=s[0], top=5), d) for s, (_, d) in ((s, case(*s, wl.F16, 40 + i)) for i, s in enumerate(shapes))]
+    serial = [{k: v.clone() for k, v in h.score(d["x"], d["target"]).items()} for h, d in jobs]
+    torch.cuda.synchronize()
+    bad = []
+
+    def work(i):
+        h, d = jobs[i]
+        stream = torch.cuda.Stream()
+        for _ in range(20):
+            r = h.score(d["x"], d["target"], stream)
+            stream.synchronize()
+            if not all(torch.equal(r[k], serial[i][k]) for k in serial[i]):
+                bad.append(i)
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(len(jobs))]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not bad
+
+
+@pytest.mark.parametrize("T,D,V", [(1, 256, 40000), (20, 384, 1000)])
+def test_scoring_head_in_a_graph(T, D, V):
+    torch = torch_mod()
+    _, d = case(T, D, V, wl.BF16, 9)
+    head = ScoringHead(d["gamma"], d["beta"], d["w"], max_rows=T, top=5)
+    x, target = d["x"].clone(), d["target"].clone()
+    head.plan(T, D)
+    head.score(x, target)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = head.score(x, target)
+    for seed in range(5):
+        c2, d2 = case(T, D, V, wl.BF16, 90 + seed)
+        x.copy_(d2["x"]), target.copy_(d2["target"])
+        graph.replay()
+        torch.cuda.synchronize()
+        got = {k: v.clone() for k, v in out.items()}
+        eager = head.score(x, target)
+        torch.cuda.synchronize()
+        assert all(torch.equal(got[k], eager[k]) for k in got), seed
+
+
+def test_refusals_of_the_heads_own():
+    _, d = case(4, 64, 100, wl.F16, 1)
+    head = ScoringHead(d["gamma"], d["beta"], d["w"], max_rows=4, top=3)
+    for x in (d["x"].float(), d["x"][:, :32], torch_mod().cat([d["x"], d["x"]])):
+        with pytest.raises(ValueError):
+            head.score(x)
+    with pytest.raises(B.ConvError):
+        ScoringHead(d["gamma"], d["beta"], d["w"], max_rows=4, top=101).score(d["x"])
