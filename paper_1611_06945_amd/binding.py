@@ -191,9 +191,10 @@ def desc_of(shape, dtype=CONV_F32, relu=True, in_nhwc=False, out_nhwc=False, fil
 def _ptr(x) -> Optional[int]:
     if x is None:
         return None
-    data_ptr = getattr(x, "data_ptr", None)
-    if data_ptr is not None:
-        return int(data_ptr())
+    try:
+        return x.data_ptr()  # (0.16 us; a small call has up to ten of these)
+    except AttributeError:
+        pass
     if isinstance(x, int):
         return x
     raise TypeError("expected a torch tensor, an int device address or None, got %r" % type(x))
