@@ -5,7 +5,7 @@
 // workgroups that share a row, are joined by the same rule; lse = m + log s, entropy = log s - sd / s.
 //
 // Alternatives are found without sorting: a thread also keeps its largest 16-byte piece (value, and the lower piece where values
-// are equal).  The `top`-th largest of 64 such maxima is a bound below which no alternative lies, and only about `top` threads
+// are equal).  The `top`-th largest of 16 to 128 such maxima is a bound below which no alternative lies, and only about `top` threads
 // hold anything above it; their pieces are read once more (from cache), what reaches the bound goes to a list in LDS, and its
 // elements are ranked by counting.  For logits in no particular order the list has little more than `top` entries.  Rows where it
 // would overflow, and rows with a NaN or +inf, take the alternatives one by one instead, a pass over the row for each.
@@ -112,12 +112,26 @@ __device__ __forceinline__ uint64_t nth_of_lanes(uint64_t key, int rank)
     const uint64_t hit = __ballot(before == rank && key != 0);
     return hit ? lane_key(key, __builtin_ctzll(hit)) : 0;
 }
-// A bound for the `top` largest of 64 lanes' sets of keys, given each set's largest: the top-th largest of these, or of the largest
-// of two or four lanes where `top` is small beside 16 or 32 (fewer comparisons; for keys in no order 5 of 16 let 6 through, 20 of 32 31).  Keys
-// that are not 0 are distinct; 0 if there are not as many.
-__device__ __forceinline__ uint64_t bound_of_wave(uint64_t key, int top)
+// ... of 128 keys, two a lane
+__device__ __forceinline__ uint64_t nth_of_pairs(uint64_t k0, uint64_t k1, int rank)
 {
-    if (top > 20) return nth_of_lanes<64>(key, top - 1);
+    int before0 = 0, before1 = 0;
+#pragma unroll 4
+    for (int l = 0; l < 64; ++l) {
+        const uint64_t o0 = lane_key(k0, l), o1 = lane_key(k1, l);
+        before0 += (o0 > k0) + (o1 > k0);
+        before1 += (o0 > k1) + (o1 > k1);
+    }
+    const uint64_t hit0 = __ballot(before0 == rank && k0 != 0), hit1 = __ballot(before1 == rank && k1 != 0);
+    return hit0 ? lane_key(k0, __builtin_ctzll(hit0)) : hit1 ? lane_key(k1, __builtin_ctzll(hit1)) : 0;
+}
+// A bound for the `top` largest of 128 sets of keys, given each set's largest, two a lane: the top-th largest of these, or, where `top`
+// is small beside 16 or 32, of the largest of four or eight of them (fewer comparisons; for keys in no order 5 of 16 let 6 through, 20 of
+// 32 31, 64 of 128 89).  Keys that are not 0 are distinct; 0 if there are not as many.
+__device__ __forceinline__ uint64_t bound_of_wave(uint64_t k0, uint64_t k1, int top)
+{
+    if (top > 20) return nth_of_pairs(k0, k1, top - 1);
+    uint64_t key = k0 > k1 ? k0 : k1;
     uint64_t o = __shfl_xor(key, 32, 64);
     key = o > key ? o : key;
     if (top > 8) return nth_of_lanes<32>(key, top - 1);
@@ -126,20 +140,42 @@ __device__ __forceinline__ uint64_t bound_of_wave(uint64_t key, int top)
     return nth_of_lanes<16>(key, top - 1);
 }
 
-// The first `top` of n keys in LDS, in order, to best[0..top) (0 where there are fewer): an element's place is the number of greater ones.
+// The first `top` of n keys in LDS, in order, to best[0..top): an element's place is the number of greater ones, counted by eight
+// lanes.
 template <int NT>
 __device__ __forceinline__ void rank_keys(const uint64_t* keys, int n, uint64_t* best, int top)
 {
-    for (int i = threadIdx.x; i < n; i += NT) {
+    const int part = threadIdx.x & 7;
+    for (int i = threadIdx.x >> 3; i < n; i += NT / 8) {
         const uint64_t k = keys[i];
-        int r = 0, j = 0;
-        for (; j + 8 <= n; j += 8) {
-#pragma unroll
-            for (int u = 0; u < 8; ++u) r += keys[j + u] > k;
-        }
-        for (; j < n; ++j) r += keys[j] > k;
-        if (r < top) best[r] = k;
+        int r = 0;
+        for (int j = part; j < n; j += 8) r += keys[j] > k;
+        r += __builtin_amdgcn_mov_dpp(r, 0xB1, 0xF, 0xF, false);   // the eight lanes' counts: quad_perm [1,0,3,2], [2,3,0,1],
+        r += __builtin_amdgcn_mov_dpp(r, 0x4E, 0xF, 0xF, false);
+        r += __builtin_amdgcn_mov_dpp(r, 0x141, 0xF, 0xF, false);  // row_half_mirror
+        if (part == 0 && r < top) best[r] = k;
     }
+}
+
+// The sum of `n` over the lanes up to and with this one.
+__device__ __forceinline__ int wave_scan(int n)
+{
+    n += __builtin_amdgcn_update_dpp(0, n, 0x111, 0xF, 0xF, false);  // row_shr 1, 2, 4, 8: within 16 lanes
+    n += __builtin_amdgcn_update_dpp(0, n, 0x112, 0xF, 0xF, false);
+    n += __builtin_amdgcn_update_dpp(0, n, 0x114, 0xF, 0xF, false);
+    n += __builtin_amdgcn_update_dpp(0, n, 0x118, 0xF, 0xF, false);
+    n += __builtin_amdgcn_update_dpp(0, n, 0x142, 0xA, 0xF, false);  // lane 15 to row 1, lane 47 to row 3
+    n += __builtin_amdgcn_update_dpp(0, n, 0x143, 0xC, 0xF, false);  // lane 31 to rows 2 and 3
+    return n;
+}
+// Room in a list for `n` entries of each lane, by one addition a wave (left to the compiler, lanes are added one after the other):
+// where this lane's begin.  Every lane of the wave calls; `counter` is LDS.
+__device__ __forceinline__ int take_room(int n, int* counter)
+{
+    const int upto = wave_scan(n), total = __builtin_amdgcn_readlane(upto, 63);
+    int base = 0;
+    if ((threadIdx.x & 63) == 0) base = atomicAdd(counter, total);
+    return __builtin_amdgcn_readfirstlane(base) + upto - n;
 }
 
 struct RowResult {
@@ -196,9 +232,9 @@ __device__ __forceinline__ void write_row(const LogprobArgs& a, int64_t row, con
 __host__ __device__ __forceinline__ size_t part_bytes(int top) { return 16 + 8 * (size_t)((top + 1) & ~1); }
 
 // One row, or one of `splits` shares of `share` pieces of it, a workgroup of W waves.  Pieces begin at multiples of 16 bytes in memory:
-// the first and the last of a row can be short (its edges); these are left to one thread each, stay out of the maxima, and go to
-// the list element by element.  HELD: a share is at most U pieces a thread, which stay in registers; else pieces are read again
-// for the list.  TOP: alternatives are asked for.
+// the first and the last of a row can be short (its edges); their elements are a thread's each, stay out of the maxima, and go to
+// the list on their own.  HELD: a share is at most U pieces a thread, so that its
+// maximum is known before its sums.  TOP: alternatives are asked for.
 template <int DT, int W, bool HELD, bool TOP>
 __global__ __launch_bounds__(64 * W, TOP ? 1 : 8) void logprob_rows(LogprobArgs a, int splits, int share)
 {
@@ -208,7 +244,7 @@ __global__ __launch_bounds__(64 * W, TOP ? 1 : 8) void logprob_rows(LogprobArgs 
     constexpr int LIST = W == 1 ? 640 : 1024;  // at least 64 pieces of 8, and the edges: rows of so few pieces go there whole
     __shared__ float red[2 * W];
     __shared__ uint64_t maxima[TOP ? NT : 1], list[TOP ? LIST : 1], best[TOP ? kMostTop : 1], bound;
-    __shared__ uint16_t winner[TOP && !HELD ? NT : 1];
+    __shared__ uint16_t winner[TOP ? NT : 1];
     __shared__ int listed, winners;
     
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
@@ -219,9 +255,11 @@ __global__ __launch_bounds__(64 * W, TOP ? 1 : 8) void logprob_rows(LogprobArgs 
         const int whole_end = (int)(((int64_t)a.cols + shift) / VEC);    // whole pieces: shift > 0 .. whole_end
         const int v0 = max((int)blockIdx.y * share, shift > 0 ? 1 : 0), v1 = min(whole_end, ((int)blockIdx.y + 1) * share);
         const int head = shift ? min(VEC - shift, a.cols) : 0, tail = max(whole_end * VEC - shift, head);  // edges: [0, head), [tail, cols)
-        // the first share has the first edge, the last one the last
-        const int e0 = blockIdx.y == 0 && tid == 0 ? 0 : tail, e0_end = blockIdx.y == 0 && tid == 0 ? head : tail;
-        const int e1 = blockIdx.y == splits - 1 && tid == NT - 1 ? tail : a.cols;
+        // ... an element a thread: the first edge's by the first eight threads of the first share, the last one's by the next eight of the last
+        int edge = -1;
+        if (tid < 8 && tid < head && blockIdx.y == 0) edge = tid;
+        if (tid >= 8 && tid < 16 && blockIdx.y == splits - 1 && tail + tid - 8 < a.cols) edge = tail + tid - 8;
+        const float edge_x = edge >= 0 ? Prec<DT>::to_f32(x[edge]) : -kInf;
         Given given = {false, 0.0f};
         if (tid == 0 && splits == 1) given = given_of<DT>(a, row);
 
@@ -232,11 +270,6 @@ __global__ __launch_bounds__(64 * W, TOP ? 1 : 8) void logprob_rows(LogprobArgs 
         auto whole = [&](int v) { return P::raw((const elem_t*)__builtin_assume_aligned(base + (int64_t)v * VEC, 16)); };
         auto note = [&](float m, int v) {
             if (TOP && m > most) most = m, at = v;
-        };
-        auto element = [&](int j) {
-            const float f[2] = {Prec<DT>::to_f32(x[j]), -kInf};
-            if (f[0] > p.m) rebase(p, f[0]);
-            add_piece(p, f);
         };
         int v = v0 + tid;
         if constexpr (HELD) {
@@ -294,8 +327,11 @@ __global__ __launch_bounds__(64 * W, TOP ? 1 : 8) void logprob_rows(LogprobArgs 
                 add_piece(p, f);
             }
         }
-        for (int j = e0; j < e0_end; ++j) element(j);
-        for (int j = e1; j < a.cols; ++j) element(j);
+        if (edge >= 0) {
+            const float f[2] = {edge_x, -kInf};
+            if (edge_x > p.m) rebase(p, edge_x);
+            add_piece(p, f);
+        }
         __syncthreads();  // the previous row's LDS is free
         // (made unknown here, or what the selection computes from it would be kept in registers while the row is read)
         int sel = threadIdx.x;
@@ -311,55 +347,57 @@ __global__ __launch_bounds__(64 * W, TOP ? 1 : 8) void logprob_rows(LogprobArgs 
         if constexpr (TOP) {
             if constexpr (W == 1) __syncthreads();
             if (wave == 0) {
-                uint64_t k = maxima[lane];
+                uint64_t k[2] = {maxima[lane], 0};
 #pragma unroll
-                for (int w = 1; w < W; ++w) k = maxima[w * 64 + lane] > k ? maxima[w * 64 + lane] : k;
-                const uint64_t b = bound_of_wave(k, a.top);
+                for (int w = 1; w < W; ++w) k[w & 1] = maxima[w * 64 + lane] > k[w & 1] ? maxima[w * 64 + lane] : k[w & 1];
+                const uint64_t b = bound_of_wave(k[0], k[1], a.top);
                 if (lane == 0) bound = b;
             }
             __syncthreads();
             const uint64_t b = bound, mine = maxima[sel];
-            const uint32_t b_order = (uint32_t)(b >> 32), b_piece = b ? index_of(b) : 0xFFFFFFFFu;
             const bool odd = !(p.s >= 0.0f);  // a NaN or an infinity
-            // (value, piece) not below the bound: an element of piece q goes to the list
-            auto offer = [&](float f, int q, int j) {
-                const uint32_t o = order_of(f);
-                if (o > b_order || (o == b_order && (uint32_t)q <= b_piece)) {
-                    const int to = atomicAdd(&listed, 1);
-                    if (to < LIST) list[to] = key_of(f, (uint32_t)j);
-                }
-            };
-            auto offer_piece = [&](const uint4& r, int q) {
-                float f[VEC];
-                P::widen(r, f);
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) offer(f[e], q, q * VEC - shift + e);
-            };
+            // what is not below the bound in (value, piece) goes to the list
+            const float b_value = b ? value_of((uint32_t)(b >> 32)) : -kInf;
+            const uint32_t b_piece = b ? index_of(b) : 0xFFFFFFFFu;
+            auto passes = [&](float f, int q) { return f > b_value || (f == b_value && (uint32_t)q <= b_piece); };
             if (!odd) {
-                for (int j = e0; j < e0_end; ++j) offer(Prec<DT>::to_f32(x[j]), 0, j);
-                for (int j = e1; j < a.cols; ++j) offer(Prec<DT>::to_f32(x[j]), whole_end, j);
-                if constexpr (HELD) {
-                    if (mine && mine >= b) {
-#pragma unroll
-                        for (int u = 0; u < U; ++u)
-                            if (v + u * NT < v1) offer_piece(raw[u], v + u * NT);
+                if (mine && mine >= b) winner[atomicAdd(&winners, 1)] = (uint16_t)sel;
+                if (wave == 0) {
+                    const bool in = edge >= 0 && passes(edge_x, edge < head ? 0 : whole_end);
+                    if (__any(in)) {
+                        const int to = take_room(in, &listed);
+                        if (in && to < LIST) list[to] = key_of(edge_x, (uint32_t)edge);
                     }
-                } else {
-                    if (mine && mine >= b) winner[atomicAdd(&winners, 1)] = (uint16_t)sel;
-                    __syncthreads();
-                    // the winners' pieces, 2^log of them each, dealt to all threads; the next one is on its way while one is looked at
-                    const int log = 32 - __builtin_clz(max(v1 - v0 - 1, 0) / NT);
-                    const int all = winners << log;
-                    auto piece = [&](int i) { return i < all ? v0 + winner[i >> log] + (i & ((1 << log) - 1)) * NT : v1; };
-                    int q = piece(sel);
-                    uint4 r;
-                    if (q < v1) r = whole(q);
-                    for (int i = sel; i < all; i += NT) {
-                        const int q_now = q;
-                        const uint4 now = r;
-                        q = piece(i + NT);
-                        if (q < v1) r = whole(q);
-                        if (q_now < v1) offer_piece(now, q_now);
+                }
+                __syncthreads();
+                // the winners' pieces, `each` of them a winner, dealt to all threads, two at a time
+                const int each = max(v1 - v0 + NT - 1, 0) / NT, all = winners * each;
+                for (int i0 = 0; i0 < all; i0 += 2 * NT) {  // (all lanes: they count their entries together)
+                    int q[2];
+                    uint4 r[2];
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) {
+                        const int i = i0 + u * NT + sel, w = (int)((unsigned)i / (unsigned)each);
+                        q[u] = i < all ? v0 + winner[w] + (i - w * each) * NT : v1;
+                        if (q[u] < v1) r[u] = whole(q[u]);
+                    }
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) {
+                        float f[VEC];
+                        uint32_t m = 0;
+                        P::widen(r[u], f);
+                        if (q[u] < v1) {
+#pragma unroll
+                            for (int e = 0; e < VEC; ++e) m |= (passes(f[e], q[u]) ? 1u : 0u) << e;
+                        }
+                        if (!__any(m != 0)) continue;
+                        int to = take_room(__builtin_popcount(m), &listed);
+#pragma unroll
+                        for (int e = 0; e < VEC; ++e)
+                            if ((m >> e) & 1) {
+                                if (to < LIST) list[to] = key_of(f[e], (uint32_t)(q[u] * VEC - shift + e));
+                                ++to;
+                            }
                     }
                 }
                 __syncthreads();
@@ -405,9 +443,9 @@ constexpr int kMostSplits = 64;
 template <int DT>
 __global__ __launch_bounds__(256) void logprob_join(LogprobArgs a, int splits)
 {
-    constexpr int NT = 256, MOST = kMostSplits * kMostTop / NT;
+    constexpr int NT = 256;
     __shared__ float red[8];
-    __shared__ uint64_t maxima[NT], list[kMostSplits * kMostTop], best[kMostTop], bound;
+    __shared__ uint64_t all[kMostSplits * kMostTop], list[kMostSplits * kMostTop], best[kMostTop], bound;
     __shared__ int listed;
     const int tid = threadIdx.x, lane = tid & 63;
     const int64_t row = blockIdx.x;
@@ -416,12 +454,16 @@ __global__ __launch_bounds__(256) void logprob_join(LogprobArgs a, int splits)
     const int n = splits * a.top;
     Given given = {false, 0.0f};
     if (tid == 0) given = given_of<DT>(a, row);
-    uint64_t mine[MOST], most = 0;
+    // The lists are in order, so the first of each, or the first few where there are fewer than 128 lists, are the likeliest: their
+    // top-th largest is the bound.  (Keys dealt to the lanes as they come put the firsts of 64 lists of 20 into 8 of 32 sets.)
+    uint64_t first[2] = {0, 0};
 #pragma unroll
-    for (int i = 0; i < MOST; ++i) {
-        mine[i] = 0;
-        if (i * NT < n && i * NT + tid < n) mine[i] = keys[i * NT + tid];
+    for (int i = 0; i < 2; ++i) {
+        const int o = tid + 64 * i;
+        if (tid < 64 && o / splits < a.top) first[i] = keys[(o % splits) * a.top + o / splits];
     }
+#pragma unroll 4
+    for (int i = tid; i < n; i += NT) all[i] = keys[i];
     Part p = {kLowest, 0.0f, 0.0f};
     if (tid < splits) {
         const float4 f = ((const float4*)ws)[tid];
@@ -431,22 +473,18 @@ __global__ __launch_bounds__(256) void logprob_join(LogprobArgs a, int splits)
     for (int i = tid; i < kMostTop; i += NT) best[i] = 0;
     p = block_join<4>(p, red);
     if (a.top) {
-#pragma unroll
-        for (int i = 0; i < MOST; ++i) most = mine[i] > most ? mine[i] : most;
-        maxima[tid] = most;
-        __syncthreads();
         if (tid < 64) {
-            uint64_t k = maxima[lane];
-#pragma unroll
-            for (int w = 1; w < 4; ++w) k = maxima[w * 64 + lane] > k ? maxima[w * 64 + lane] : k;
-            const uint64_t b = bound_of_wave(k, a.top);
+            const uint64_t b = bound_of_wave(first[0], first[1], a.top);
             if (lane == 0) bound = b ? b : 1;  // a key of 0 stands for no element
         }
         __syncthreads();
         const uint64_t b = bound;
-#pragma unroll
-        for (int i = 0; i < MOST; ++i)
-            if (mine[i] >= b) list[atomicAdd(&listed, 1)] = mine[i];
+        for (int i = tid; i - tid < n; i += NT) {
+            const uint64_t k = i < n ? all[i] : 0;
+            if (!__any(k >= b)) continue;
+            const int to = take_room(k >= b, &listed);
+            if (k >= b) list[to] = k;
+        }
         __syncthreads();
         rank_keys<NT>(list, listed, best, a.top);
         __syncthreads();
@@ -523,19 +561,19 @@ __global__ __launch_bounds__(256) void logprob_bwd_rows(LogprobArgs a, int per_r
 // workgroups of a CU cover each other's selections; eight beyond (2048 rows, 5 alternatives, us with four / eight waves: 50257 bf16 53 / 61,
 // 131072 bf16 110 / 104, 50257 fp32 81 / 79).  Fewer rows than CUs are shared by 256 / rows workgroups, as far as that leaves each of
 // them two pieces a thread, up to 64 (256 rows of 50257 fp16 in one each 14 us, in two 17).  A row that starts within 16 bytes
-// can touch a piece more than its length says: `pieces` is the most.
+// can touch a piece more than its length says: `pieces` is the most.  (More than 20 alternatives need the maxima of four waves.)
 struct Shares {
     int waves, splits, share;
     bool held;
 };
-Shares shares_of(int64_t rows, int cols, int dtype)
+Shares shares_of(int64_t rows, int cols, int dtype, int top)
 {
     const int vec = dtype == CONV_F32 ? 4 : 8, pieces = cols / vec + 2;
     Shares s;
     s.waves = pieces <= 256 ? 1 : pieces <= 8192 ? 4 : 8;
     int64_t want = pieces > 1024 ? (256 + rows - 1) / std::max<int64_t>(rows, 1) : 1;
     want = std::max<int64_t>(1, std::min<int64_t>({want, kMostSplits, pieces / 512}));
-    if (want > 1) s.waves = 4;
+    if (want > 1 || (top > 20 && s.waves == 1)) s.waves = 4;
     s.share = (int)((pieces + want - 1) / want);
     s.splits = (pieces + s.share - 1) / s.share;
     s.held = s.share <= 4 * 64 * s.waves;
@@ -553,7 +591,7 @@ void launch_w(const LogprobArgs& a, const Shares& sh, hipStream_t s)
 template <int DT>
 hipError_t fwd(const LogprobArgs& a, hipStream_t s)
 {
-    const Shares sh = shares_of(a.rows, a.cols, DT);
+    const Shares sh = shares_of(a.rows, a.cols, DT, a.top);
     if (sh.waves == 1) launch_w<DT, 1, true>(a, sh, s);
     else if (sh.waves == 4 && sh.held) launch_w<DT, 4, true>(a, sh, s);
     else if (sh.waves == 4) launch_w<DT, 4, false>(a, sh, s);
@@ -566,7 +604,7 @@ hipError_t fwd(const LogprobArgs& a, hipStream_t s)
 
 size_t logprob_workspace(int64_t rows, int cols, int top, int dtype)
 {
-    const Shares sh = shares_of(rows, cols, dtype);
+    const Shares sh = shares_of(rows, cols, dtype, top);
     return sh.splits > 1 ? (size_t)rows * sh.splits * part_bytes(top) : 0;
 }
 
