@@ -275,6 +275,20 @@ __global__ __launch_bounds__(T::NT) void int_linear_tiles(IntLinearArgs g, int t
     constexpr int PHASES = 2 * T::H, LOADS = T::LA + T::LW;
     typedef std::integral_constant<int, 0> First;
     typedef std::integral_constant<int, PHASES - 1> Last;
+    typedef std::integral_constant<int, 0> Zero;
+    // the order of a phase: after every few products one of its LDS reads, then one of its loads
+    auto interleave = [&](auto reads, auto loads) {
+        constexpr int R = decltype(reads)::value, L = decltype(loads)::value, M = T::HB * T::FN, EACH = M / (R + L) > 0 ? M / (R + L) : 1;
+        for_each<R>([&](auto) {
+            __builtin_amdgcn_sched_group_barrier(0x008, EACH, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        });
+        for_each<L>([&](auto) {
+            __builtin_amdgcn_sched_group_barrier(0x008, EACH, 0);
+            __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
+        });
+        if constexpr (M > EACH * (R + L)) __builtin_amdgcn_sched_group_barrier(0x008, M - EACH * (R + L), 0);
+    };
     // Operands are read one phase ahead of their products, across the turn to the next stage too; the scheduling barriers keep the
     // compiler from reading them where they are used.
 #pragma unroll
@@ -287,8 +301,8 @@ __global__ __launch_bounds__(T::NT) void int_linear_tiles(IntLinearArgs g, int t
     for (int k = 0; k < steps - 1; ++k) {
         for_each<PHASES - 1>([&](auto p) {
             fetch(buf, std::integral_constant<int, decltype(p)::value + 1>());
-            __builtin_amdgcn_sched_barrier(0);
             products(p);
+            interleave(std::integral_constant<int, T::HB + ((decltype(p)::value + 1) % T::H == 0 ? T::FN : 0)>(), Zero());
             __builtin_amdgcn_sched_barrier(0);
         });
         // this wave's loads of the next stage have landed and its reads of the present one are done; then so are everybody's
@@ -298,8 +312,8 @@ __global__ __launch_bounds__(T::NT) void int_linear_tiles(IntLinearArgs g, int t
         const int next = buf + 1 == T::S ? 0 : buf + 1;
         fetch(next, First());
         stage(buf, k + T::S);
-        __builtin_amdgcn_sched_barrier(0);
         products(Last());
+        interleave(std::integral_constant<int, T::HB + T::FN>(), std::integral_constant<int, LOADS>());
         __builtin_amdgcn_sched_barrier(0);
         buf = next;
     }
@@ -335,7 +349,11 @@ __global__ __launch_bounds__(T::NT) void int_linear_tiles(IntLinearArgs g, int t
             elem_t* out = (elem_t*)g.out + (t0 + tl) * g.ldo + n0;
             float v[8];
 #pragma unroll
-            for (int r = 0; r < 8; ++r) v[r] = finish(acc[i + (r >> 2)][j][r & 3], sa * sw[r], b[r], g.relu);
+            for (int r = 0; r < 8; ++r) v[r] = finish(acc[i + (r >> 2)][j][r & 3], sa * sw[r], b[r], 0);
+            if (g.relu) {
+#pragma unroll
+                for (int r = 0; r < 8; ++r) v[r] = v[r] < 0.0f ? 0.0f : v[r];
+            }
             constexpr int LEN = 16 / sizeof(elem_t);
             uint32_t w4[8 / LEN][4];
             int n[8 / LEN];
