@@ -276,21 +276,29 @@ __global__ __launch_bounds__(T::NT) void int_linear_tiles(IntLinearArgs g, int t
     typedef std::integral_constant<int, 0> First;
     typedef std::integral_constant<int, PHASES - 1> Last;
     typedef std::integral_constant<int, 0> Zero;
-    // the order of a phase: after every few products one of its LDS reads, then one of its loads
+    // Order of a phase of many products: after every few one of its LDS reads, then one of its loads, so that products begin at once
+    // (256 x 256: 229 -> 225 us at 8192 x 8192 x 4096).  With few products the reads come first, or they would be late (64 x 64: 10.1 -> 9.5).
+    constexpr bool MIXED = T::HB * T::FN >= 16;
     auto interleave = [&](auto reads, auto loads) {
-        constexpr int R = decltype(reads)::value, L = decltype(loads)::value, M = T::HB * T::FN, EACH = M / (R + L) > 0 ? M / (R + L) : 1;
-        for_each<R>([&](auto) {
-            __builtin_amdgcn_sched_group_barrier(0x008, EACH, 0);
-            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-        });
-        for_each<L>([&](auto) {
-            __builtin_amdgcn_sched_group_barrier(0x008, EACH, 0);
-            __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
-        });
-        if constexpr (M > EACH * (R + L)) __builtin_amdgcn_sched_group_barrier(0x008, M - EACH * (R + L), 0);
+        constexpr int R = decltype(reads)::value, L = decltype(loads)::value, M = T::HB * T::FN, EACH = MIXED ? M / (R + L) : 1;
+        if constexpr (MIXED) {
+            for_each<R>([&](auto) {
+                __builtin_amdgcn_sched_group_barrier(0x008, EACH, 0);  // products
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);     // an LDS read
+            });
+            for_each<L>([&](auto) {
+                __builtin_amdgcn_sched_group_barrier(0x008, EACH, 0);
+                __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);     // a load
+            });
+            if constexpr (M > EACH * (R + L)) __builtin_amdgcn_sched_group_barrier(0x008, M - EACH * (R + L), 0);
+        }
+        __builtin_amdgcn_sched_barrier(0);
     };
-    // Operands are read one phase ahead of their products, across the turn to the next stage too; the scheduling barriers keep the
-    // compiler from reading them where they are used.
+    auto reads_first = [&]() {
+        if constexpr (!MIXED) __builtin_amdgcn_sched_barrier(0);
+    };
+    // Operands are read one phase ahead of their products, across the turn to the next stage too; left to itself the compiler reads
+    // them where they are used.
 #pragma unroll
     for (int k = 0; k < T::S; ++k) stage(k, k);
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((T::S - 1) * LOADS) : "memory");
@@ -301,9 +309,9 @@ __global__ __launch_bounds__(T::NT) void int_linear_tiles(IntLinearArgs g, int t
     for (int k = 0; k < steps - 1; ++k) {
         for_each<PHASES - 1>([&](auto p) {
             fetch(buf, std::integral_constant<int, decltype(p)::value + 1>());
+            reads_first();
             products(p);
             interleave(std::integral_constant<int, T::HB + ((decltype(p)::value + 1) % T::H == 0 ? T::FN : 0)>(), Zero());
-            __builtin_amdgcn_sched_barrier(0);
         });
         // this wave's loads of the next stage have landed and its reads of the present one are done; then so are everybody's
         asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((T::S - 2) * LOADS) : "memory");
@@ -312,9 +320,9 @@ __global__ __launch_bounds__(T::NT) void int_linear_tiles(IntLinearArgs g, int t
         const int next = buf + 1 == T::S ? 0 : buf + 1;
         fetch(next, First());
         stage(buf, k + T::S);
+        reads_first();
         products(Last());
         interleave(std::integral_constant<int, T::HB + T::FN>(), std::integral_constant<int, LOADS>());
-        __builtin_amdgcn_sched_barrier(0);
         buf = next;
     }
     for_each<PHASES>([&](auto p) {
@@ -420,10 +428,11 @@ hipError_t in_portions(const IntLinearArgs& g, int rows_each, F launch)
 // The forms and what a launch of them is expected to take, in us, from calls measured alone (8-bit codes at random, bf16 out):
 //   tiles: ceil(tiles / 256) rounds of `step` for every 128 bytes of the reduction and `own`;
 //   rows:  see rows_plan().
-// Measured (us), 64x64 / 64x128 / 128x128 / 128x256 / 256x256 (rows: int_linear_rows):
-//   256 x 4096 x 4096 9.5 / 12.4 / 17 / - / 47;  777 x 1283 x 1001 7.3 / 6.7 / 9.2 / - / 25;  1024 x 4096 x 4096 30 / 23 / 21 / 30 / 48;
-//   2048 x 4096 x 1024 - / - / 17.7 / 13.8 / 20.6;  2048 x 2048 x 2048 20 / 15 / 13 / 18 / 28;  4096 x 4096 x 4096 - / - / 80 / 71 / 61;
-//   33 x 4096 x 4096 8.4 (rows 7.1), 33 x 16384 x 4096 12.3 (rows 24), 64 x 100 x 16384 23 (rows 12).
+// Measured (us of the GPU, bf16 out), rows / 64x64 / 64x128 / 128x128 / 128x256 / 256x256:
+//   33 x 4096 x 4096 6.6 / 8.5 / 12 / 16 / 27 / 38;  33 x 16384 x 4096 19 / 12 / 13 / 17 / 28 / 39;  128 x 128 x 8192 7.3 / 13 / 17 / 27 / 45 / 71;
+//   256 x 4096 x 4096 23 / 9.8 / 13 / 17 / 29 / 40;  777 x 1283 x 1001 9.6 / 7.5 / 7.5 / 9.0 / 15 / 22;  1024 x 4096 x 4096 70 / 31 / 25 / 24 / 31 / 43;
+//   2048 x 4096 x 1024 39 / 22 / 17 / 16 / 14 / 18;  2048 x 2048 x 2048 38 / 18 / 14 / 13 / 18 / 25;  4096 x 4096 x 4096 255 / 112 / 94 / 88 / 75 / 60;
+//   8192 x 8192 x 4096 1010 / 418 / 344 / 318 / 273 / 219 (2510 TOP/s; 3260 on zeros: the card's power holds the clock down).
 template <int WT, int WN, int FT, int FN, int S, int StepNs, int OwnNs>
 struct Costed : IntTile<WT, WN, FT, FN, S> {
     static double us(const IntLinearArgs& g)
@@ -437,7 +446,7 @@ typedef Costed<4, 2, 1, 2, 4, 200, 3000> Tile64x64;
 typedef Costed<2, 4, 2, 2, 3, 330, 3000> Tile64x128;
 typedef Costed<4, 4, 2, 2, 4, 570, 3500> Tile128x128;
 typedef Costed<4, 4, 2, 4, 2, 1050, 5000> Tile128x256;
-typedef Costed<4, 2, 4, 8, 2, 1730, 10000> Tile256x256;
+typedef Costed<4, 2, 4, 8, 2, 1690, 5000> Tile256x256;
 
 // Few rows: blocks of 16 rows a workgroup, workgroups that share a reduction, expected us.  A workgroup reads 120 KB in a us, all of
 // them 15 TB/s (from the caches mostly); a second launch to add shares costs about 5 us of a call, so it has to save more (64 x 100 x 16384 11.9 -> 9.2, but
