@@ -213,7 +213,7 @@ __global__ __launch_bounds__(NT) void norm_bwd_rows(NormArgs a)
     typedef typename H::elem_t elem_t;
     constexpr int VEC = H::VEC, ROWS = NT / G, WAVES = NT / 64, SETS = G <= 64 ? WAVES : ROWS;
     __shared__ float red[2][WAVES];
-    __shared__ float sums[DW && SETS > 1 ? 2 * G * NV * VEC : 1];
+    __shared__ float sums[DW && SETS > 1 ? SETS / 2 * 2 * G * NV * VEC : 1];
     const int tid = threadIdx.x, l = tid % G;
     const int64_t step = (int64_t)gridDim.x * ROWS;
     int64_t row = (int64_t)blockIdx.x * ROWS + tid / G;
@@ -296,20 +296,7 @@ __global__ __launch_bounds__(NT) void norm_bwd_rows(NormArgs a)
         }
     }
     if constexpr (DW) {
-        float* to_dg = gridDim.x == 1 ? a.dgamma : a.ws + (size_t)blockIdx.x * 2 * a.cols;
-        float* to_db = gridDim.x == 1 ? a.dbeta : a.ws + (size_t)blockIdx.x * 2 * a.cols + a.cols;
-        if constexpr (SETS == 1) {
-#pragma unroll
-            for (int i = 0; i < NV; ++i)
-#pragma unroll
-                for (int k = 0; k < VEC; ++k) {
-                    const int j = (i * G + l) * VEC + k;
-                    if (j < a.cols && to_dg) to_dg[j] = dg[i][k];
-                    if (j < a.cols && to_db) to_db[j] = db[i][k];
-                }
-            return;
-        }
-        // rows within a wave first, then wave by wave (or row by row) through LDS
+        // rows within a wave first, then halves of the waves (or rows) hand theirs to the others through LDS
         if constexpr (G < 64) {
 #pragma unroll
             for (int i = 0; i < NV; ++i)
@@ -321,24 +308,47 @@ __global__ __launch_bounds__(NT) void norm_bwd_rows(NormArgs a)
         }
         const int set = G <= 64 ? tid / 64 : tid / G;
         const bool holder = G >= 64 || (tid & 63) < G;
-        for (int w = 0; w < SETS; ++w) {
-            if (set == w && holder) {
+#pragma unroll
+        for (int half = SETS / 2; half >= 1; half /= 2) {
+            float* p = sums + (set % half) * (2 * G * NV * VEC) + l;  // a lane's neighbours are next to it: no bank twice
+            if (set >= half && set < 2 * half && holder) {
 #pragma unroll
                 for (int i = 0; i < NV; ++i)
 #pragma unroll
                     for (int k = 0; k < VEC; ++k) {
-                        float* p = sums + (i * VEC + k) * G + l;  // a lane's neighbours are next to it: no bank twice
-                        p[0] = w ? p[0] + dg[i][k] : dg[i][k];
-                        p[G * NV * VEC] = w ? p[G * NV * VEC] + db[i][k] : db[i][k];
+                        p[(i * VEC + k) * G] = dg[i][k];
+                        p[((NV + i) * VEC + k) * G] = db[i][k];
                     }
             }
             __syncthreads();
+            if (set < half && holder) {
+#pragma unroll
+                for (int i = 0; i < NV; ++i)
+#pragma unroll
+                    for (int k = 0; k < VEC; ++k) {
+                        dg[i][k] += p[(i * VEC + k) * G];
+                        db[i][k] += p[((NV + i) * VEC + k) * G];
+                    }
+            }
+            if (half > 1) __syncthreads();
         }
-        for (int j = tid; j < a.cols; j += NT) {
-            const int piece = j / VEC;
-            const float* p = sums + ((piece / G) * VEC + j % VEC) * G + piece % G;
-            if (to_dg) to_dg[j] = p[0];
-            if (to_db) to_db[j] = p[G * NV * VEC];
+        if (set == 0 && holder) {
+            float* to_dg = gridDim.x == 1 ? a.dgamma : a.ws + (size_t)blockIdx.x * 2 * a.cols;
+            float* to_db = gridDim.x == 1 ? a.dbeta : a.ws + (size_t)blockIdx.x * 2 * a.cols + a.cols;
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const int j = (i * G + l) * VEC;
+                if (j + VEC <= a.cols) {
+                    if (to_dg) __builtin_memcpy(to_dg + j, dg[i], 4 * VEC);
+                    if (to_db) __builtin_memcpy(to_db + j, db[i], 4 * VEC);
+                } else {
+#pragma unroll
+                    for (int k = 0; k < VEC; ++k) {
+                        if (j + k < a.cols && to_dg) to_dg[j + k] = dg[i][k];
+                        if (j + k < a.cols && to_db) to_db[j + k] = db[i][k];
+                    }
+                }
+            }
         }
     }
 }
