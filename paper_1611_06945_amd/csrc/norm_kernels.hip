@@ -1,6 +1,6 @@
 // Layer norm forward and backward, and the row quantiser: one pass over the tensors, the row held in registers.
 //
-// G neighbouring lanes share a row (16, a wave, or a workgroup of 4 or 16 waves), each holding up to NV pieces of 16 bytes.  The mean
+// G neighbouring lanes share a row (8, 16, a wave, or a workgroup of 4 or 16 waves), each holding up to NV pieces of 16 bytes.  The mean
 // comes first and the variance is summed around it, from registers.  A workgroup keeps its columns' gamma and beta in registers over
 // all its rows, and asks for its next row before it works on the present one.  Backward, a lane adds up dgamma and dbeta of its columns
 // over its rows in registers; a workgroup's lanes with the same columns are added through LDS, and a second kernel adds the
@@ -483,16 +483,18 @@ __global__ __launch_bounds__(256) void norm_dw_any(NormArgs a)
 
 constexpr int kCUs = 256;
 
-// Lanes a row and pieces a lane: the fewest lanes that hold the row in `most` pieces each.  lanes 0: the row is too long.
+// Lanes a row and pieces a lane: the fewest lanes that hold the row with 16 elements each; `last` pieces with 16 waves.  lanes 0: the
+// row is too long.  Backward, 16 elements with their gradients, sums and the next row are what a lane has registers for; forward, 32 were no
+// faster (16384 x 4096 bf16 46 us either way) and later for few rows (64 x 384 fp16 4.3 -> 3.3 us).
 struct Form {
     int lanes, pieces;
 };
-Form form_of(int cols, int dtype, int most)
+Form form_of(int cols, int dtype, int last)
 {
-    const int vec = dtype == CONV_F32 ? 4 : 8, pieces = (cols + vec - 1) / vec;
-    for (int lanes : {16, 64, 256, 1024}) {
+    const int vec = dtype == CONV_F32 ? 4 : 8, most = 16 / vec, pieces = (cols + vec - 1) / vec;
+    for (int lanes : {8, 16, 64, 256, 1024}) {
         const int n = (pieces + lanes - 1) / lanes;
-        if (n <= most) return Form{lanes, n <= 1 ? 1 : n <= 2 ? 2 : 4};
+        if (n <= (lanes == 1024 ? last : most)) return Form{lanes, n <= 1 ? 1 : n <= 2 ? 2 : 4};
     }
     return Form{0, 0};
 }
@@ -510,14 +512,15 @@ void fwd_pieces(const NormArgs& a, int nv, hipStream_t s)
 {
     if (nv == 1) fwd_launch<DT, G, 1, MODE>(a, s);
     else if (nv == 2) fwd_launch<DT, G, 2, MODE>(a, s);
-    else fwd_launch<DT, G, 4, MODE>(a, s);
+    else if constexpr (DT == CONV_F32 || G == 1024) fwd_launch<DT, G, 4, MODE>(a, s);
 }
 
 template <int DT, int MODE>
 hipError_t fwd(const NormArgs& a, hipStream_t s)
 {
     const Form f = form_of(a.cols, DT, 4);
-    if (f.lanes == 16) fwd_pieces<DT, 16, MODE>(a, f.pieces, s);
+    if (f.lanes == 8) fwd_pieces<DT, 8, MODE>(a, f.pieces, s);
+    else if (f.lanes == 16) fwd_pieces<DT, 16, MODE>(a, f.pieces, s);
     else if (f.lanes == 64) fwd_pieces<DT, 64, MODE>(a, f.pieces, s);
     else if (f.lanes == 256) fwd_pieces<DT, 256, MODE>(a, f.pieces, s);
     else if (f.lanes == 1024) fwd_pieces<DT, 1024, MODE>(a, f.pieces, s);
@@ -531,7 +534,6 @@ hipError_t fwd_type(const NormArgs& a, int dtype, hipStream_t s)
     return dtype == CONV_F32 ? fwd<CONV_F32, MODE>(a, s) : dtype == CONV_F16 ? fwd<CONV_F16, MODE>(a, s) : fwd<CONV_BF16, MODE>(a, s);
 }
 
-// Backward a lane holds 16 elements at most: with their gradients, sums and the next row that is what 16 waves have registers for.
 Form bwd_form(int cols, int dtype) { return form_of(cols, dtype, dtype == CONV_F32 ? 4 : 2); }
 
 // Workgroups of the backward kernel: one a CU, as a sum of 2 * cols floats each is written and read again, or two where a lane has
@@ -542,7 +544,7 @@ int bwd_parts(int64_t rows, int cols, int dtype)
     const Form f = bwd_form(cols, dtype);
     if (!f.lanes) return (int)std::max<int64_t>(1, std::min<int64_t>(64, (rows + 15) / 16));
     const int here = bwd_threads(f.lanes) / f.lanes;
-    return (int)std::max<int64_t>(1, std::min<int64_t>(f.pieces == 1 && f.lanes < 256 ? 2 * kCUs : kCUs, (rows + here - 1) / here));
+    return (int)std::max<int64_t>(1, std::min<int64_t>(f.pieces == 1 && f.lanes < 1024 ? 2 * kCUs : kCUs, (rows + here - 1) / here));
 }
 
 template <int DT, int G, int NV>
@@ -579,7 +581,8 @@ hipError_t bwd(const NormArgs& a, hipStream_t s)
     const int parts = bwd_parts(a.rows, a.cols, DT);
     const bool dw = a.dgamma || a.dbeta;
     if (f.lanes) {
-        if (f.lanes == 16) bwd_pieces<DT, 16>(a, f.pieces, parts, s);
+        if (f.lanes == 8) bwd_pieces<DT, 8>(a, f.pieces, parts, s);
+        else if (f.lanes == 16) bwd_pieces<DT, 16>(a, f.pieces, parts, s);
         else if (f.lanes == 64) bwd_pieces<DT, 64>(a, f.pieces, parts, s);
         else if (f.lanes == 256) bwd_pieces<DT, 256>(a, f.pieces, parts, s);
         else bwd_pieces<DT, 1024>(a, f.pieces, parts, s);

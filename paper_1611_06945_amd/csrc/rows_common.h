@@ -74,10 +74,11 @@ __device__ __forceinline__ float lanes_reduce(float x)
     return x;
 }
 
-// The sum over the lanes of a wave that are G apart (G = 16 or 32); every lane gets it.
+// The sum over the lanes of a wave that are G apart (G = 8, 16 or 32); every lane gets it.
 template <int G>
 __device__ __forceinline__ float across_rows(float x)
 {
+    if constexpr (G <= 8) x += __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x), 0x128, 0xF, 0xF, false));  // row_ror 8
     if constexpr (G <= 16) {
         const uint32_t u = __builtin_bit_cast(uint32_t, x);
         const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
