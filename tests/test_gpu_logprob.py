@@ -278,3 +278,25 @@ def test_offsets_beyond_32_bits():
         got.append(o + [z[:, :cols].contiguous()])
     for a, b in zip(*got):
         assert torch.equal(a, b)
+
+
+def test_more_rows_than_workgroups():
+    torch = torch_mod()
+    rows, cols, top = 300_001, 9, 2
+    g = torch.Generator(device="cuda")
+    g.manual_seed(2)
+    x = torch.randint(-3, 4, (rows, cols), generator=g, device="cuda").float()
+    t = torch.randint(0, cols, (rows,), generator=g, device="cuda")
+    d = B.make_logprob_desc(rows, cols, wl.F32, top)
+    o = [torch.empty(rows, device="cuda") for _ in range(3)] + [torch.empty(rows, top, dtype=torch.int64, device="cuda"), torch.empty(rows, top, device="cuda")]
+    B.logprob_fwd(d, x, t, *o, None, 0)
+    lse = torch.logsumexp(x.double(), 1)
+    assert torch.allclose(o[1].double(), lse, atol=1e-5, rtol=1e-5)
+    assert torch.allclose(o[0].double(), x.double().gather(1, t[:, None])[:, 0] - lse, atol=1e-5, rtol=1e-5)
+    order = torch.sort(x, dim=1, descending=True, stable=True).indices[:, :top]
+    assert torch.equal(o[3], order)
+    dx = torch.empty_like(x)
+    B.logprob_bwd(d, x, t, o[1], None, torch.ones(rows, device="cuda"), None, dx)
+    want = -torch.exp(x.double() - o[1].double()[:, None])
+    want.scatter_add_(1, t[:, None], torch.ones(rows, 1, dtype=torch.float64, device="cuda"))
+    assert torch.allclose(dx.double(), want, atol=1e-5)

@@ -270,3 +270,36 @@ def test_layernorm_quant_is_the_two_calls(rows, cols, dtype):
     B.layernorm_fwd(B.make_norm_desc(rows, cols, dtype, EPS, cols + 1, cols), X.ptr, gamma, beta, Y.ptr)
     B.layernorm_quant_fwd(B.make_norm_desc(rows, cols, dtype, EPS, cols + 1, Q.ld), X.ptr, gamma, beta, Q.ptr, scale)
     same_codes(Q, scale, *ro.quantize_rows(Y.host()), cols)
+
+
+def test_offsets_beyond_32_bits():
+    """Rows of tensors of 2.2e9 elements against the same rows on their own."""
+    torch = torch_mod()
+    rows, cols, ld = 20, 777, 110_000_000
+    free, _ = torch.cuda.mem_get_info()
+    assert free > 20 * 2 ** 30
+    g = torch.Generator(device="cuda")
+    g.manual_seed(1)
+    own = torch.randn(rows, cols, generator=g, device="cuda").half()
+    dy = torch.randn(rows, cols, generator=g, device="cuda").half()
+    gamma, beta = torch.rand(cols, generator=g, device="cuda"), torch.rand(cols, generator=g, device="cuda")
+    far, out = (torch.zeros(rows * ld, dtype=torch.float16, device="cuda").view(rows, ld) for _ in range(2))
+    far[:, :cols] = own
+    mean, rstd = nan_vec(rows), nan_vec(rows)
+    near = torch.empty_like(own)
+    B.layernorm_fwd(B.make_norm_desc(rows, cols, wl.F16, EPS), own, gamma, beta, near, mean, rstd)
+    B.layernorm_fwd(B.make_norm_desc(rows, cols, wl.F16, EPS, ld, ld), far, gamma, beta, out)
+    assert torch.equal(out[:, :cols], near)
+    q = [torch.zeros(rows, B.row_stride(cols), dtype=torch.int8, device="cuda") for _ in range(2)]
+    s = [nan_vec(rows) for _ in range(2)]
+    B.quantize_rows(B.make_quant_desc(rows, cols, wl.F16), own, q[0], s[0])
+    B.quantize_rows(B.make_quant_desc(rows, cols, wl.F16, ld), far, q[1], s[1])
+    assert torch.equal(q[0], q[1]) and torch.equal(s[0], s[1])
+    dx, res = torch.empty_like(own), []
+    for x, d, o, l in ((own, dy, dx, cols), (far, dy, out, ld)):
+        desc = B.make_norm_desc(rows, cols, wl.F16, EPS, l, cols)
+        ws = torch.empty(max(16, B.layernorm_bwd_workspace_bytes(desc)), dtype=torch.uint8, device="cuda")
+        dg, db = nan_vec(cols), nan_vec(cols)
+        B.layernorm_bwd(desc, x, d, gamma, mean, rstd, o, dg, db, ws, ws.numel())
+        res.append((o[:, :cols].clone(), dg, db))
+    assert all(torch.equal(a, b) for a, b in zip(*res))
