@@ -165,17 +165,24 @@ __global__ __launch_bounds__(256) void int_linear_join(IntLinearArgs g, int spli
 // of each row: while one is multiplied, S - 1 are on their way or there.
 //   * A row's eight 16-byte pieces are stored at piece ^ (row / 2 % 8), by choosing which piece a lane loads: the 16 lanes that LDS
 //     serves together then read 16 different groups of four banks (no conflict counted).
+//   * LATE, for rows that begin inside a line of 128 bytes: the 128 bytes of a step would lie in two lines, and every line be asked
+//     for twice.  A row's load of step k is the line that its bytes of step k begin in; the pieces behind them come with the load of
+//     step k + 1, so a step reads two stages of the ring, each lane its pieces of the one or the other.
 //   * Rows past the last one, and pieces past the end of the tensor, are read as zeros by the bounds check of the buffer
 //     descriptor; the bytes of a row past K belong to what follows and are cleared in one operand on the last step.
 //   * Products are 16x16x64: on random operands the register-only loop reaches 3970 TOP/s with two waves a SIMD, 32x32x32 3480
 //     (on zeros both 4600: the card's power sets the clock).
-template <int WT_, int WN_, int FT_, int FN_, int S_>
+template <int WT_, int WN_, int FT_, int FN_, int S_, bool LATE_>
 struct IntTile {
     static constexpr int WT = WT_, WN = WN_, FT = FT_, FN = FN_;  // waves and 16-wide blocks a wave, along rows and channels
     static constexpr int BT = 16 * WT * FT, BN = 16 * WN * FN, NT = 64 * WT * WN;
     static constexpr int KB = 128, S = S_, PIECES = KB / 16;
+    static constexpr bool LATE = LATE_;
+    static_assert(S >= 2 + LATE, "a stage to multiply, one to load");
     static constexpr int STAGE = (BT + BN) * KB;
-    static constexpr size_t LDS = (size_t)S * STAGE + (BT + 2 * BN) * 4;
+    static constexpr int PITCH = BN * 2 + 16;  // of a row of 16-bit outputs in LDS
+    static constexpr int RING = S * STAGE > BT * PITCH ? S * STAGE : BT * PITCH;
+    static constexpr size_t LDS = (size_t)RING + (BT + 2 * BN) * 4;
     static constexpr int LA = BT * PIECES / NT, LW = BN * PIECES / NT;  // 16-byte loads a thread and stage
     static constexpr int H = FT > 4 ? 2 : 1, HB = FT / H;               // the blocks of rows go in H portions
     static_assert(LA * NT == BT * PIECES && LW * NT == BN * PIECES && FN % 2 == 0 && HB * H == FT, "whole loads and portions");
@@ -207,32 +214,37 @@ __global__ __launch_bounds__(T::NT) void int_linear_tiles(IntLinearArgs g, int t
     const __amdgpu_buffer_rsrc_t ra = make_rsrc(g.a + t0 * g.lda, (uint32_t)((rows_here - 1) * g.lda + Kr));
     const __amdgpu_buffer_rsrc_t rw = make_rsrc(g.w + (int64_t)n0 * g.ldw, (uint32_t)((outs_here - 1) * g.ldw + Kr));
     uint32_t aoff[T::LA], woff[T::LW];
+    bool alate[T::LA], wlate[T::LW];
     constexpr int P = T::PIECES;
+    // the distance of a row's start to the last multiple of 128 bytes, in pieces; the same in rows 16 apart
+    auto shift = [](const int8_t* p, int64_t ld, int row) { return T::LATE ? (int)(((uint32_t)((uintptr_t)p >> 4) + row * (uint32_t)(ld >> 4)) % P) : 0; };
 #pragma unroll
     for (int i = 0; i < T::LA; ++i) {
-        const int p = i * T::NT + tid, row = p / P;
-        aoff[i] = (uint32_t)row * (uint32_t)g.lda + (((p % P) ^ ((row >> 1) % P)) << 4);
+        const int p = i * T::NT + tid, row = p / P, piece = (p % P) ^ ((row >> 1) % P);
+        alate[i] = piece + shift(g.a, g.lda, row) >= P;
+        aoff[i] = (uint32_t)row * (uint32_t)g.lda + (piece << 4) - (alate[i] ? T::KB : 0);
     }
 #pragma unroll
     for (int i = 0; i < T::LW; ++i) {
-        const int p = i * T::NT + tid, row = p / P;
-        woff[i] = (uint32_t)row * (uint32_t)g.ldw + (((p % P) ^ ((row >> 1) % P)) << 4);
+        const int p = i * T::NT + tid, row = p / P, piece = (p % P) ^ ((row >> 1) % P);
+        wlate[i] = piece + shift(g.w, g.ldw, row) >= P;
+        woff[i] = (uint32_t)row * (uint32_t)g.ldw + (piece << 4) - (wlate[i] ? T::KB : 0);
     }
     const int steps = (g.K + T::KB - 1) / T::KB;
     // Steps past the last are asked for as well, out of range, so that the count of loads on their way is always the same.
-    auto stage = [&](int buf, int k) {
-        const uint32_t k0 = k < steps ? (uint32_t)k * T::KB : kFar;
+    auto stage = [&](int buf, int k, auto first) {
+        const uint32_t k0 = k < steps + T::LATE ? (uint32_t)k * T::KB : kFar;
         char* base = smem + buf * T::STAGE + wave * 1024;
 #pragma unroll
         for (int i = 0; i < T::LA; ++i)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (lds_void*)(base + i * T::NT * 16), 16, (int)(aoff[i] + k0), 0, 0, 0);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (lds_void*)(base + i * T::NT * 16), 16, (int)(first() && alate[i] ? kFar : aoff[i] + k0), 0, 0, 0);
 #pragma unroll
         for (int i = 0; i < T::LW; ++i)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rw, (lds_void*)(base + T::BT * T::KB + i * T::NT * 16), 16, (int)(woff[i] + k0), 0, 0, 0);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rw, (lds_void*)(base + T::BT * T::KB + i * T::NT * 16), 16, (int)(first() && wlate[i] ? kFar : woff[i] + k0), 0, 0, 0);
     };
 
     // the tile's scales and biases wait in LDS for the end
-    float* const sc_a = (float*)(smem + T::S * T::STAGE);
+    float* const sc_a = (float*)(smem + T::RING);
     float* const sc_w = sc_a + T::BT;
     float* const bias = sc_w + T::BN;
     for (int i = tid; i < T::BT; i += T::NT) sc_a[i] = i < rows_here ? g.a_scale[t0 + i] : 0.0f;
@@ -244,6 +256,13 @@ __global__ __launch_bounds__(T::NT) void int_linear_tiles(IntLinearArgs g, int t
     int frag[2];  // LDS offset of this lane's piece for each half of a stage, without the block
 #pragma unroll
     for (int s = 0; s < 2; ++s) frag[s] = (lane & 15) * T::KB + (((s * 4 + (lane >> 4)) ^ ((lane >> 1) & 7)) << 4);
+    // whether that piece is one of the next stage
+    bool a_next[2], w_next[2];
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+        a_next[s] = s * 4 + (lane >> 4) + shift(g.a, g.lda, lane & 15) >= P;
+        w_next[s] = s * 4 + (lane >> 4) + shift(g.w, g.ldw, lane & 15) >= P;
+    }
     const int wave_a = wt * T::FT * 16 * T::KB, wave_w = (T::BT + wn * T::FN * 16) * T::KB;
 
     i32x4 acc[T::FN][T::FT];
@@ -256,10 +275,11 @@ __global__ __launch_bounds__(T::NT) void int_linear_tiles(IntLinearArgs g, int t
     // The operands of phase p of a stage (half p / H, portion p % H of the rows) to the registers of its parity.
     auto fetch = [&](int buf, auto phase) {
         constexpr int p = decltype(phase)::value, s = p / T::H, h = p % T::H;
-        const char* base = smem + buf * T::STAGE + frag[s];
+        const int here = buf * T::STAGE + frag[s], there = buf + 1 == T::S ? frag[s] : here + T::STAGE;
+        const char *base = smem + (T::LATE && a_next[s] ? there : here), *base_w = smem + (T::LATE && w_next[s] ? there : here);
         if constexpr (h == 0) {
 #pragma unroll
-            for (int i = 0; i < T::FN; ++i) wv[s][i] = *(const i32x4*)(base + wave_w + i * 16 * T::KB);
+            for (int i = 0; i < T::FN; ++i) wv[s][i] = *(const i32x4*)(base_w + wave_w + i * 16 * T::KB);
         }
 #pragma unroll
         for (int j = 0; j < T::HB; ++j) av[p & 1][j] = *(const i32x4*)(base + wave_a + (h * T::HB + j) * 16 * T::KB);
@@ -300,8 +320,8 @@ __global__ __launch_bounds__(T::NT) void int_linear_tiles(IntLinearArgs g, int t
     // Operands are read one phase ahead of their products, across the turn to the next stage too; left to itself the compiler reads
     // them where they are used.
 #pragma unroll
-    for (int k = 0; k < T::S; ++k) stage(k, k);
-    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((T::S - 1) * LOADS) : "memory");
+    for (int k = 0; k < T::S; ++k) k == 0 ? stage(k, k, std::bool_constant<T::LATE>()) : stage(k, k, std::false_type());
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((T::S - 1 - T::LATE) * LOADS) : "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
     fetch(0, First());
@@ -314,12 +334,12 @@ __global__ __launch_bounds__(T::NT) void int_linear_tiles(IntLinearArgs g, int t
             interleave(std::integral_constant<int, T::HB + ((decltype(p)::value + 1) % T::H == 0 ? T::FN : 0)>(), Zero());
         });
         // this wave's loads of the next stage have landed and its reads of the present one are done; then so are everybody's
-        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((T::S - 2) * LOADS) : "memory");
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((T::S - 2 - T::LATE) * LOADS) : "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
         const int next = buf + 1 == T::S ? 0 : buf + 1;
         fetch(next, First());
-        stage(buf, k + T::S);
+        stage(buf, k + T::S, std::false_type());
         reads_first();
         products(Last());
         interleave(std::integral_constant<int, T::HB + T::FN>(), std::integral_constant<int, LOADS>());
@@ -341,6 +361,10 @@ __global__ __launch_bounds__(T::NT) void int_linear_tiles(IntLinearArgs g, int t
     // lanes trade between two blocks of channels, so that a lane has eight channels in a row: the groups 0 .. 3 those of block i from
     // 0, of block i + 1 from 0, of block i from 8, of block i + 1 from 8.
     const int grp = lane >> 4;
+    // An odd row length puts every other row's elements across words, and a store of half a word is slow: such tiles are turned in LDS and
+    // leave in aligned pieces of 16 bytes (4096 x 11009 x 512 71 -> 52 us, 8192 x 50257 x 768 600 -> 567, against stores as they come).
+    const bool staged = DT != CONV_F32 && ((g.ldo | (int64_t)((uintptr_t)g.out >> 1)) & 1);
+    if (staged) __syncthreads();
 #pragma unroll
     for (int i = 0; i < T::FN; i += 2) {
         const int nl = (wn * T::FN + i) * 16;
@@ -376,7 +400,9 @@ __global__ __launch_bounds__(T::NT) void int_linear_tiles(IntLinearArgs g, int t
             }
 #pragma unroll
             for (int c = 0; c < 8 / LEN; ++c) {
-                if (in && n[c] + LEN <= outs_here) {
+                if (staged) {
+                    __builtin_memcpy(smem + tl * T::PITCH + n[c] * 2, w4[c], 16);
+                } else if (in && n[c] + LEN <= outs_here) {
                     __builtin_memcpy(out + n[c], w4[c], 16);
                 } else if (in) {
                     elem_t e[LEN];
@@ -388,6 +414,35 @@ __global__ __launch_bounds__(T::NT) void int_linear_tiles(IntLinearArgs g, int t
             }
         }
         __builtin_amdgcn_sched_barrier(0);
+    }
+    if constexpr (DT != CONV_F32) {
+        if (!staged) return;
+        __syncthreads();
+        constexpr int EACH = T::BN / 8 + 1;  // aligned pieces that a row of the tile touches
+        for (int i = tid; i < T::BT * EACH; i += T::NT) {
+            const int tl = i / EACH, piece = i - tl * EACH;
+            if (tl >= rows_here) break;
+            elem_t* out = (elem_t*)g.out + (t0 + tl) * g.ldo + n0;
+            const int e0 = piece * 8 - (int)((uintptr_t)out / 2 % 8);
+            if (e0 >= 0 && e0 + 8 <= outs_here) {
+                const uint32_t* from = (const uint32_t*)(smem + tl * T::PITCH + (e0 & ~1) * 2);
+                uint32_t w[5];
+#pragma unroll
+                for (int k = 0; k < 5; ++k) w[k] = from[k];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) w[k] = e0 & 1 ? __builtin_amdgcn_alignbyte(w[k + 1], w[k], 2) : w[k];
+                *(uint4*)(out + e0) = make_uint4(w[0], w[1], w[2], w[3]);
+            }
+        }
+        // the pieces that a row's tile shares with its neighbours, an element a lane
+        for (int i = tid; i < T::BT * 16; i += T::NT) {
+            const int tl = i / 16, half = i / 8 % 2;
+            if (tl >= rows_here) break;
+            elem_t* out = (elem_t*)g.out + (t0 + tl) * g.ldo + n0;
+            const int at = (int)((uintptr_t)out / 2 % 8), last = (outs_here + at) / 8;  // the piece that ends behind the tile
+            const int e = (half ? last * 8 : 0) - at + i % 8;
+            if (half ? e >= 0 && e < outs_here : at && last && e >= 0) out[e] = *(const elem_t*)(smem + tl * T::PITCH + e * 2);
+        }
     }
 }
 
@@ -425,32 +480,31 @@ hipError_t in_portions(const IntLinearArgs& g, int rows_each, F launch)
     return hipSuccess;
 }
 
-// The forms and what a launch of them is expected to take, in us, from calls measured alone (8-bit codes at random, bf16 out):
-//   tiles: ceil(tiles / 256) rounds of `step` for every 128 bytes of the reduction and `own`;
-//   rows:  see rows_plan().
-// Measured (us of the GPU, bf16 out), rows / 64x64 / 64x128 / 128x128 / 128x256 / 256x256:
-//   33 x 4096 x 4096 6.6 / 8.5 / 12 / 16 / 27 / 38;  33 x 16384 x 4096 19 / 12 / 13 / 17 / 28 / 39;  128 x 128 x 8192 7.3 / 13 / 17 / 27 / 45 / 71;
-//   256 x 4096 x 4096 23 / 9.8 / 13 / 17 / 29 / 40;  777 x 1283 x 1001 9.6 / 7.5 / 7.5 / 9.0 / 15 / 22;  1024 x 4096 x 4096 70 / 31 / 25 / 24 / 31 / 43;
-//   2048 x 4096 x 1024 39 / 22 / 17 / 16 / 14 / 18;  2048 x 2048 x 2048 38 / 18 / 14 / 13 / 18 / 25;  4096 x 4096 x 4096 255 / 112 / 94 / 88 / 75 / 60;
-//   8192 x 8192 x 4096 1010 / 418 / 344 / 318 / 273 / 219 (2510 TOP/s; 3260 on zeros: the card's power holds the clock down).
-template <int WT, int WN, int FT, int FN, int S, int StepNs, int OwnNs>
-struct Costed : IntTile<WT, WN, FT, FN, S> {
-    static double us(const IntLinearArgs& g)
-    {
-        typedef IntTile<WT, WN, FT, FN, S> T;
-        const double tiles = (double)((g.rows + T::BT - 1) / T::BT) * ((g.N + T::BN - 1) / T::BN), steps = (g.K + T::KB - 1) / T::KB;
-        return std::ceil(tiles / 256) * (steps * StepNs + OwnNs) * 1e-3;
-    }
-};
-typedef Costed<4, 2, 1, 2, 4, 200, 3000> Tile64x64;
-typedef Costed<2, 4, 2, 2, 3, 330, 3000> Tile64x128;
-typedef Costed<4, 4, 2, 2, 4, 570, 3500> Tile128x128;
-typedef Costed<4, 4, 2, 4, 2, 1050, 5000> Tile128x256;
-typedef Costed<4, 2, 4, 8, 2, 1690, 5000> Tile256x256;
+// Tiles, and what a launch of them is expected to take, in us: `once` and for every round of 256 tiles `own` and `step` for every 128
+// bytes of the reduction.  The figures were fitted to calls of 134 sizes, 10 to 50257 channels, rows of 32 to 16384 bytes aligned
+// and not, each in every form (8-bit codes at random, bf16 out): what the rule below takes was 1.8 % slower than the best form on
+// average, 20 % at most.  LATE: see IntTile; 64x64 at 256 x 13632 x 16287 193 -> 147 us, 128x128 121 -> 96, 256x256 has no room for
+// a third stage.
+template <bool LATE> using Tile64x64 = IntTile<4, 2, 1, 2, 4, LATE>;
+template <bool LATE> using Tile64x128 = IntTile<2, 4, 2, 2, LATE ? 4 : 3, LATE>;
+template <bool LATE> using Tile128x128 = IntTile<4, 4, 2, 2, 4, LATE>;
+typedef IntTile<2, 4, 4, 2, 2, false> Pair128x128;  // two workgroups a CU: one stores its tile while the other multiplies
+typedef IntTile<4, 2, 4, 8, 2, false> Tile256x256;
+// Measured (us of the GPU, bf16 out), rows / 64x64 / 64x128 / 128x128 / two 128x128 a CU / 256x256:
+//   512 x 4096 x 4096 37 / 19 / 16 / 19 / 23 / 42;  1024 x 4096 x 1024 22 / 12 / 15 / 9.7 / 9.4 / 17;  2048 x 2048 x 2048 38 / 19 / 16 / 17 / 16 / 26;
+//   5298 x 608 x 5120 79 / 36 / 28 / 25 / 33 / 56;  8192 x 1024 x 4096 123 / 61 / 46 / 44 / 38 / 46;  4096 x 4096 x 4096 263 / 114 / 90 / 85 / 71 / 57;
+//   8192 x 50256 x 768 1780 / 816 / 611 / 618 / 489 / 526;  8192 x 8192 x 64 161 / 87 / 57 / 60 / 41 / 38;
+//   8192 x 8192 x 4096 1030 / 443 / 371 / 345 / 304 / 242 (2270 TOP/s; 3260 on zeros: the card's power holds the clock down).
+template <typename T>
+double tiles_us(const IntLinearArgs& g, double once, double own, double step)
+{
+    const double tiles = (double)((g.rows + T::BT - 1) / T::BT) * ((g.N + T::BN - 1) / T::BN), steps = (g.K + T::KB - 1) / T::KB;
+    return once + std::ceil(tiles / 256) * (own + steps * step);
+}
 
 // Few rows: blocks of 16 rows a workgroup, workgroups that share a reduction, expected us.  A workgroup reads 120 KB in a us, all of
-// them 15 TB/s (from the caches mostly); a second launch to add shares costs about 5 us of a call, so it has to save more (64 x 100 x 16384 11.9 -> 9.2, but
-// 128 x 128 x 8192 7.8 -> 8.1).
+// them 33 TB/s (from the caches mostly), and one takes 0.16 us of a CU a block at least; a second launch to add shares costs about 5 us of a
+// call, so it has to save more (64 x 100 x 16384 11.9 -> 9.2, but 128 x 128 x 8192 7.8 -> 8.1).
 struct RowsPlan {
     int rb, splits;
     double us;
@@ -462,7 +516,7 @@ RowsPlan rows_plan(int64_t rows, int N, int K)
     const double groups = (double)((rows + 16 * p.rb - 1) / (16 * p.rb)) * ((N + 15) / 16);
     const double bytes = 16.0 * (1 + p.rb) * K, alone = bytes / 120e3 * std::ceil(groups / 256);
     p.splits = 1;
-    p.us = 3 + std::max(alone, groups * bytes / 15e6);
+    p.us = 2.8 + alone + std::max(groups * bytes / 33e6, groups / 256 * 0.16 * p.rb);
     if (groups <= 64) {
         const int most = std::min({16, (int)(256 / groups), (K + 1023) / 1024});
         if (alone - alone / most > 6) p.splits = most, p.us = 8 + alone / most;
@@ -505,13 +559,18 @@ hipError_t launch(IntLinearArgs& g, hipStream_t s)
         });
     const RowsPlan rows = rows_plan(g.rows, g.N, g.K);
     if (rows.rb == 1) return launch_rows<DT, 1>(g, rows.splits, s);
-    const double us[] = {rows.us, Tile64x64::us(g), Tile64x128::us(g), Tile128x128::us(g), Tile128x256::us(g), Tile256x256::us(g)};
-    switch ((int)(std::min_element(us, us + 6) - us)) {
+    const bool late = (g.lda | g.ldw | (int64_t)(uintptr_t)g.a | (int64_t)(uintptr_t)g.w) % 128 != 0;
+    const bool alone = (g.rows + 127) / 128 * ((g.N + 127) / 128) <= 256;
+    const double us[] = {rows.us, tiles_us<Tile64x64<false>>(g, 2.0, 1.2, 0.2), tiles_us<Tile64x128<false>>(g, 1.5, 2.8, 0.33),
+                         alone ? tiles_us<Tile128x128<false>>(g, 0, 4.2, 0.49) : tiles_us<Pair128x128>(g, 1.8, 1.5, 0.52),
+                         tiles_us<Tile256x256>(g, 0, 11, 1.4)};
+    switch ((int)(std::min_element(us, us + 5) - us)) {
         case 0: return rows.rb == 2 ? launch_rows<DT, 2>(g, rows.splits, s) : launch_rows<DT, 4>(g, rows.splits, s);
-        case 1: return launch_tiles<DT, Tile64x64>(g, s);
-        case 2: return launch_tiles<DT, Tile64x128>(g, s);
-        case 3: return launch_tiles<DT, Tile128x128>(g, s);
-        case 4: return launch_tiles<DT, Tile128x256>(g, s);
+        case 1: return late ? launch_tiles<DT, Tile64x64<true>>(g, s) : launch_tiles<DT, Tile64x64<false>>(g, s);
+        case 2: return late ? launch_tiles<DT, Tile64x128<true>>(g, s) : launch_tiles<DT, Tile64x128<false>>(g, s);
+        case 3:
+            if (!alone) return launch_tiles<DT, Pair128x128>(g, s);
+            return late ? launch_tiles<DT, Tile128x128<true>>(g, s) : launch_tiles<DT, Tile128x128<false>>(g, s);
         default: return launch_tiles<DT, Tile256x256>(g, s);
     }
 }

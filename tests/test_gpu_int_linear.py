@@ -71,6 +71,34 @@ def test_outputs_that_are_slices(rows, N, ldo, start, dtype):
     check(rows, N, 200, dtype, ldo=ldo, start=start, pad=48, seed=3)
 
 
+@pytest.mark.parametrize("a_start,w_start", [(0, 0), (16, 0), (48, 112), (96, 80)])
+@pytest.mark.parametrize("pad", [0, 16, 48, 112])
+@pytest.mark.parametrize("rows,N,K", [(70, 70, 1), (64, 300, 128), (130, 1000, 129), (600, 900, 300), (260, 1500, 500), (1500, 1500, 260), (600, 513, 1040)])
+def test_rows_that_begin_anywhere_in_a_line(rows, N, K, pad, a_start, w_start):
+    torch = torch_mod()
+    rng = np.random.default_rng(rows + N + K + pad)
+    a, w = rng.integers(-128, 128, size=(rows, K)).astype(np.int8), rng.integers(-128, 128, size=(N, K)).astype(np.int8)
+    A = Rows(rows, K, torch.int8, B.row_stride(K) + pad, a_start, fill=-99).set(a)
+    W = Rows(N, K, torch.int8, B.row_stride(K) + 3 * pad, w_start, fill=101).set(w)
+    one_a, one_w = np.full(rows, 2.0 ** -3, np.float32), np.full(N, 2.0, np.float32)
+    Y = Rows(rows, N, torch.float32, N + 1, 1, fill=7.0)
+    d = B.make_int_linear_desc(rows, N, K, wl.F32, False, A.ld, W.ld, Y.ld)
+    need = B.int_linear_workspace_bytes(d)
+    ws = torch.full((max(need, 16),), 0xFF, dtype=torch.uint8, device="cuda")
+    B.int_linear_fwd(d, A.ptr, vec(one_a), W.ptr, vec(one_w), None, Y.ptr, ws, need)
+    torch.cuda.synchronize()
+    # sums below 2^24 in steps of a quarter: exact
+    assert np.array_equal(Y.host(), (a.astype(np.float64) @ w.astype(np.float64).T) / 4)
+    assert Y.untouched()
+
+
+@pytest.mark.parametrize("dtype", [wl.F16, wl.BF16])
+@pytest.mark.parametrize("rows,N,K,ldo,start", [(600, 900, 300, 901, 0), (600, 901, 300, 904, 3), (260, 4097, 200, 4097, 0), (1500, 1511, 260, 1511, 5),
+                                                (3000, 1537, 130, 1537, 1), (3001, 1543, 128, 1544, 7), (4000, 4001, 2000, 4001, 0), (600, 833, 300, 835, 2)])
+def test_odd_row_lengths(rows, N, K, ldo, start, dtype):
+    check(rows, N, K, dtype, ldo=ldo, start=start, relu=bool(N % 4 == 1), seed=8)
+
+
 @pytest.mark.parametrize("rows", [1, 20, 300])
 def test_the_largest_sums(rows):
     check(rows, 40, (1 << 17) - 1, wl.F32, extreme=True, seed=4)
