@@ -1,6 +1,7 @@
 // Layer norm forward and backward, and the row quantiser: one pass over the tensors, the row held in registers.
 //
-// G neighbouring lanes share a row (8, 16, a wave, or a workgroup of 4 or 16 waves), each holding up to NV pieces of 16 bytes.  The mean
+// G neighbouring lanes share a row (8, 16, a wave, or a workgroup: forward of as many waves as the row takes, G = 0, backward of 4
+// or 16), each holding up to NV pieces of 16 bytes.  The mean
 // comes first and the variance is summed around it, from registers.  A workgroup keeps its columns' gamma and beta in registers over
 // all its rows, and asks for its next row before it works on the present one.  Backward, a lane adds up dgamma and dbeta of its columns
 // over its rows in registers; a workgroup's lanes with the same columns are added through LDS, and a second kernel adds the
@@ -48,26 +49,52 @@ struct Held {
     typedef typename Prec<DT>::elem_t elem_t;
     typedef Piece<DT> P;
     static constexpr int VEC = P::VEC;
+    static __device__ __forceinline__ int lanes() { return G ? G : (int)blockDim.x; }
 
-    // Stored values; a piece past the end is not loaded, the elements of the last one past the end are zeros.
+    // Stored values, one load for every piece and no branch around it: a piece that would pass the row's end is read at the end, and
+    // clear() puts it right.  (With a branch for the pieces at the end, which loaded element by element, a wave waited there for all
+    // its loads: backward, 65536 x 768 bf16 90 us against 58.)
     static __device__ __forceinline__ void load(uint4 (&raw)[NV], const elem_t* x, int cols, int l)
     {
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int j = (i * G + l) * VEC;
-            if (j + VEC <= cols) {
-                raw[i] = P::raw(x + j);
-            } else {
+        if constexpr (G == 8 && NV == 1) {
+            if (cols < VEC) {
                 elem_t e[VEC];
 #pragma unroll
-                for (int k = 0; k < VEC; ++k) e[k] = j + k < cols ? x[j + k] : (elem_t)0;
-                __builtin_memcpy(&raw[i], e, 16);
+                for (int k = 0; k < VEC; ++k) e[k] = k < cols ? x[k] : (elem_t)0;
+                __builtin_memcpy(&raw[0], e, 16);
+                return;
             }
+        }
+#pragma unroll
+        for (int i = 0; i < NV; ++i) raw[i] = P::raw(x + min((i * lanes() + l) * VEC, cols - VEC));
+    }
+    // Zeros past the end of the row.  The last piece of a row that is no multiple of VEC has elements in front that are another
+    // piece's: it is shifted down by as many.
+    static __device__ __forceinline__ void clear(uint4 (&raw)[NV], int cols, int l)
+    {
+        const int past = -cols & (VEC - 1), words = past * (int)sizeof(elem_t) / 4;  // the same in all lanes
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int left = cols - (i * lanes() + l) * VEC;
+            uint32_t w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
+            if (past && cols >= VEC) {
+                uint32_t v[5] = {w[0], w[1], w[2], w[3], 0};
+                if (words & 2) v[0] = v[2], v[1] = v[3], v[2] = v[3] = 0;
+                if (words & 1) v[0] = v[1], v[1] = v[2], v[2] = v[3], v[3] = 0;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    if (VEC == 8 && (past & 1)) v[k] = __builtin_amdgcn_alignbit(v[k + 1], v[k], 16);
+                    w[k] = left < VEC ? v[k] : w[k];
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k) w[k] = left > 0 ? w[k] : 0;
+            raw[i] = make_uint4(w[0], w[1], w[2], w[3]);
         }
     }
     static __device__ __forceinline__ void store(elem_t* y, const float (&v)[VEC], int cols, int i, int l)
     {
-        const int j = (i * G + l) * VEC;
+        const int j = (i * lanes() + l) * VEC;
         const uint4 u = P::narrow(v);
         if (j + VEC <= cols) {
             P::put(y + j, u);
@@ -84,7 +111,7 @@ struct Held {
     {
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int j = (i * G + l) * VEC;
+            const int j = (i * lanes() + l) * VEC;
             if (p && j + VEC <= cols) {
                 __builtin_memcpy(v[i], p + j, 4 * VEC);
             } else {
@@ -95,24 +122,63 @@ struct Held {
     }
 };
 
-// Combines a value over the G lanes of a row; `lds` holds a float for each wave of the workgroup and call within a row.
+// Combines a value over the lanes of a row; `lds` holds a float for each wave of the workgroup and call within a row.  (Sums or largest
+// magnitudes: zero is neutral.)
 template <int G, typename Op>
 __device__ __forceinline__ float row_reduce(float x, float* lds)
 {
-    if constexpr (G <= 64) return lanes_reduce<G, Op>(x);
-    else return block_reduce<G / 64, Op>(x, lds);
+    if constexpr (G > 0) {
+        return lanes_reduce<G, Op>(x);
+    } else {
+        // waves as many as the workgroup has, up to 16: each reads what all left behind
+        x = lanes_reduce<64, Op>(x);
+        if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = x;
+        __syncthreads();
+        const int w = threadIdx.x & 15;
+        return lanes_reduce<16, Op>(w < (int)(blockDim.x >> 6) ? lds[w] : 0.0f);
+    }
 }
 
-// Codes of a piece to q.  Pieces past the end up to the next multiple of 16 columns get zeros.
-template <int VEC>
-__device__ __forceinline__ void store_codes(int8_t* q, const float (&v)[VEC], const RowScale& r, int j, int cols, int padded)
+// The largest magnitude among stored values, as `keep` has it.  In 16 bits two at a time: without the sign the bits of numbers, inf
+// and NaN are in order.
+template <int DT, int NV>
+__device__ __forceinline__ float largest(const uint4 (&raw)[NV])
 {
+    typedef unsigned short us2 __attribute__((ext_vector_type(2)));
+    const uint32_t clear = DT == CONV_F32 ? 0x7FFFFFFFu : 0x7FFF7FFFu;
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const uint32_t w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if constexpr (DT == CONV_F32) m = max(m, w[k] & clear);
+            else m = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(us2, m), __builtin_bit_cast(us2, w[k] & clear)));
+        }
+    }
+    if constexpr (DT == CONV_F32) return __builtin_bit_cast(float, m);
+    else return Prec<DT>::to_f32((typename Prec<DT>::elem_t)max(m & 0xFFFFu, m >> 16));
+}
+
+// Codes of a piece to q.  Pieces past the end up to the next multiple of 16 columns get zeros.  The codes are rint(v * inv): added to
+// 1.5 * 2^23, the product is rounded to the integers and its low byte is the code.
+template <int VEC>
+__device__ __forceinline__ void store_codes(int8_t* q, const float (&v)[VEC], const RowScale& r, int j, int padded)
+{
+#pragma clang fp contract(off)
     if (j >= padded) return;
     uint32_t w[VEC / 4];
 #pragma unroll
-    for (int k = 0; k < VEC / 4; ++k) w[k] = 0;
+    for (int k = 0; k < VEC / 4; ++k) {
+        uint32_t u[4];
 #pragma unroll
-    for (int k = 0; k < VEC; ++k) w[k / 4] |= ((uint32_t)code(j + k < cols ? v[k] : 0.0f, r) & 0xFFu) << (8 * (k % 4));
+        for (int e = 0; e < 4; ++e) {
+            const float p = v[k * 4 + e] * r.inv;
+            u[e] = __builtin_bit_cast(uint32_t, p + 0x1.8p23f);
+        }
+        const uint32_t all = __builtin_amdgcn_perm(__builtin_amdgcn_perm(u[3], u[2], 0x0C0C0400), __builtin_amdgcn_perm(u[1], u[0], 0x0C0C0400), 0x05040100);
+        w[k] = r.good ? all : 0;
+    }
     __builtin_memcpy(__builtin_assume_aligned(q + j, VEC), w, VEC);
 }
 
@@ -120,22 +186,22 @@ enum { TO_FLOAT = 0, TO_CODES = 1, QUANT_ONLY = 2 };
 
 // Layer norm (to floats or codes), or the quantiser alone, which holds rows the same way.
 template <int DT, int G, int NV, int MODE>
-__global__ __launch_bounds__(G <= 256 ? 256 : G) void norm_fwd_rows(NormArgs a)
+__global__ __launch_bounds__(G ? 256 : 1024) void norm_fwd_rows(NormArgs a)
 {
     typedef Held<DT, G, NV> H;
     typedef typename H::elem_t elem_t;
-    constexpr int VEC = H::VEC, NT = G <= 256 ? 256 : G, ROWS = NT / G;
-    __shared__ float red[3][NT / 64];
-    const int l = threadIdx.x % G;
+    constexpr int VEC = H::VEC, ROWS = G ? 256 / G : 1;
+    __shared__ float red[3][G ? 1 : 16];
+    const int l = G ? threadIdx.x % G : threadIdx.x;
     const int64_t step = (int64_t)gridDim.x * ROWS;
-    int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / G;
+    int64_t row = (int64_t)blockIdx.x * ROWS + (G ? threadIdx.x / G : 0);
     const int padded = (a.cols + 15) & ~15;
     const float inv_cols = 1.0f / (float)a.cols;
-    auto at = [&](int64_t r) { return (const elem_t*)a.x + (r < a.rows ? r : a.rows - 1) * a.ldx; };
+    auto load = [&](uint4 (&raw)[NV], int64_t r) { H::load(raw, (const elem_t*)a.x + (r < a.rows ? r : a.rows - 1) * a.ldx, a.cols, l); };
 
-    constexpr bool AHEAD = G < 1024 || NV * VEC < 32;  // (no registers for the next row: 16 waves with 32 elements a lane)
+    constexpr bool AHEAD = NV * VEC < 32;  // (no registers for the next row: 16 waves with 32 elements a lane)
     uint4 next[NV];
-    if (AHEAD) H::load(next, at(row), a.cols, l);
+    if (AHEAD) load(next, row);
     float gamma[NV][VEC], beta[NV][VEC];
     if constexpr (MODE != QUANT_ONLY) {
         H::columns(gamma, a.gamma, 1.0f, a.cols, l);
@@ -143,11 +209,15 @@ __global__ __launch_bounds__(G <= 256 ? 256 : G) void norm_fwd_rows(NormArgs a)
     }
     // every lane of a workgroup makes the same number of rounds: the reductions of wide rows have barriers
     for (int64_t first = (int64_t)blockIdx.x * ROWS; first < a.rows; first += step, row += step) {
-        if (!AHEAD) H::load(next, at(row), a.cols, l);
+        if (!AHEAD) load(next, row);
         float x[NV][VEC];
+        uint4 raw[NV];
 #pragma unroll
-        for (int i = 0; i < NV; ++i) H::P::widen(next[i], x[i]);
-        if (AHEAD && first + step < a.rows) H::load(next, at(row + step), a.cols, l);
+        for (int i = 0; i < NV; ++i) raw[i] = next[i];
+        H::clear(raw, a.cols, l);
+        if (AHEAD && first + step < a.rows) load(next, row + step);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) H::P::widen(raw[i], x[i]);
         if constexpr (MODE != QUANT_ONLY) {
             float sum = 0.0f;
 #pragma unroll
@@ -158,7 +228,7 @@ __global__ __launch_bounds__(G <= 256 ? 256 : G) void norm_fwd_rows(NormArgs a)
             float sq = 0.0f;
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
-                const int left = a.cols - (i * G + l) * VEC;
+                const int left = a.cols - (i * H::lanes() + l) * VEC;
 #pragma unroll
                 for (int k = 0; k < VEC; ++k) {
                     x[i][k] -= mean;
@@ -183,25 +253,22 @@ __global__ __launch_bounds__(G <= 256 ? 256 : G) void norm_fwd_rows(NormArgs a)
             } else {
                 // the codes are those of the rounded values
 #pragma unroll
-                for (int i = 0; i < NV; ++i) H::P::widen(H::P::narrow(x[i]), x[i]);
+                for (int i = 0; i < NV; ++i) {
+                    raw[i] = H::P::narrow(x[i]);
+                    H::P::widen(raw[i], x[i]);
+                }
             }
         }
         if constexpr (MODE != TO_FLOAT) {
-            float amax = 0.0f;
-#pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                const int left = a.cols - (i * G + l) * VEC;
-#pragma unroll
-                for (int k = 0; k < VEC; ++k) amax = keep(amax, k < left ? x[i][k] : 0.0f);
-            }
-            const RowScale r = row_scale(row_reduce<G, OpKeep>(amax, red[2]));
+            // (past the end gamma is 1 and beta 0, so zeros have stayed zeros)
+            const RowScale r = row_scale(row_reduce<G, OpKeep>(largest<DT>(raw), red[2]));
             if (row < a.rows) {
 #pragma unroll
-                for (int i = 0; i < NV; ++i) store_codes<VEC>(a.q + row * a.ldy, x[i], r, (i * G + l) * VEC, a.cols, padded);
+                for (int i = 0; i < NV; ++i) store_codes<VEC>(a.q + row * a.ldy, x[i], r, (i * H::lanes() + l) * VEC, padded);
                 if (l == 0) a.scale[row] = r.scale;
             }
         }
-        if constexpr (G > 64) __syncthreads();  // the next row's reductions use the same LDS
+        if constexpr (G == 0) __syncthreads();  // the next row's reductions use the same LDS
     }
 }
 
@@ -242,6 +309,8 @@ __global__ __launch_bounds__(NT) void norm_bwd_rows(NormArgs a)
         if (!AHEAD) fetch(row);
         float x[NV][VEC], dy[NV][VEC];
         const float mean = nmean, rstd = nrstd;
+        H::clear(nx, a.cols, l);
+        H::clear(ndy, a.cols, l);
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             H::P::widen(nx[i], x[i]);
@@ -337,7 +406,7 @@ __global__ __launch_bounds__(NT) void norm_bwd_rows(NormArgs a)
             float* to_db = gridDim.x == 1 ? a.dbeta : a.ws + (size_t)blockIdx.x * 2 * a.cols + a.cols;
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
-                const int j = (i * G + l) * VEC;
+                const int j = (i * H::lanes() + l) * VEC;
                 if (j + VEC <= a.cols) {
                     if (to_dg) __builtin_memcpy(to_dg + j, dg[i], 4 * VEC);
                     if (to_db) __builtin_memcpy(to_db + j, db[i], 4 * VEC);
@@ -483,47 +552,66 @@ __global__ __launch_bounds__(256) void norm_dw_any(NormArgs a)
 
 constexpr int kCUs = 256;
 
-// Lanes a row and pieces a lane: the fewest lanes that hold the row with 16 elements each; `last` pieces with 16 waves.  lanes 0: the
-// row is too long.  Backward, 16 elements with their gradients, sums and the next row are what a lane has registers for; forward, 32 were no
-// faster (16384 x 4096 bf16 46 us either way) and later for few rows (64 x 384 fp16 4.3 -> 3.3 us).
+// Backward: the fewest lanes that hold the row with 16 elements each, which is what a lane has registers for with their gradients, sums
+// and the next row.  lanes 0: the row is too long.
 struct Form {
     int lanes, pieces;
 };
-Form form_of(int cols, int dtype, int last)
+Form bwd_form(int cols, int dtype)
 {
     const int vec = dtype == CONV_F32 ? 4 : 8, most = 16 / vec, pieces = (cols + vec - 1) / vec;
     for (int lanes : {8, 16, 64, 256, 1024}) {
         const int n = (pieces + lanes - 1) / lanes;
-        if (n <= (lanes == 1024 ? last : most)) return Form{lanes, n <= 1 ? 1 : n <= 2 ? 2 : 4};
+        if (n <= most) return Form{lanes, n <= 1 ? 1 : n <= 2 ? 2 : 4};
     }
     return Form{0, 0};
 }
 
-template <int DT, int G, int NV, int MODE>
-void fwd_launch(const NormArgs& a, hipStream_t s)
+// Forward: as above up to a wave; then waves as many as the row takes, up to 16, with 16 elements a lane (or 32, where 16 waves would
+// not do).  Against 4 or 16 waves, whose lanes were partly idle (us): 19660 x 2560 bf16 43 -> 35, 9830 x 5120 bf16 55 -> 35, codes alone
+// 40 -> 28.  With few rows half of that a lane: 300 x 1536 bf16 3.7 -> 3.0; with many it costs, 12288 x 4096 bf16 34 -> 41.
+struct FwdForm {
+    int lanes, pieces, waves;
+};
+FwdForm fwd_form(int64_t rows, int cols, int dtype)
 {
-    constexpr int NT = G <= 256 ? 256 : G, ROWS = NT / G;
-    const int64_t blocks = std::min<int64_t>((a.rows + ROWS - 1) / ROWS, G == 1024 ? kCUs * 2 : kCUs * 8);
-    hipLaunchKernelGGL((norm_fwd_rows<DT, G, NV, MODE>), dim3((unsigned)blocks), dim3(NT), 0, s, a);
+    const int vec = dtype == CONV_F32 ? 4 : 8, most = 16 / vec, pieces = (cols + vec - 1) / vec;
+    for (int lanes : {8, 16, 64}) {
+        const int n = (pieces + lanes - 1) / lanes;
+        if (n <= most) return {lanes, n <= 1 ? 1 : n <= 2 ? 2 : 4, 0};
+    }
+    for (int n = rows <= 2 * kCUs ? most / 2 : most; n <= 4; n *= 2)
+        if ((pieces + 64 * n - 1) / (64 * n) <= 16) return {0, n, (pieces + 64 * n - 1) / (64 * n)};
+    return {0, 0, 0};
+}
+
+template <int DT, int G, int NV, int MODE>
+void fwd_launch(const NormArgs& a, int waves, hipStream_t s)
+{
+    const int rows = G ? 256 / G : 1;
+    // a workgroup a row: no more than the registers leave room for at once (5225 x 9632 bf16 56 us with 32 waves a CU, 35 with 20); where
+    // workgroups are small a few more do no harm (196608 x 256 bf16 34 us with 8, 36 with 6)
+    const int room = G || MODE == QUANT_ONLY || NV * (16 / (int)dtype_size(DT)) < 16 ? 32 : DT == CONV_F32 ? 20 : 24;
+    const int64_t blocks = std::min<int64_t>((a.rows + rows - 1) / rows, kCUs * (room / waves));
+    hipLaunchKernelGGL((norm_fwd_rows<DT, G, NV, MODE>), dim3((unsigned)blocks), dim3(64 * waves), 0, s, a);
 }
 
 template <int DT, int G, int MODE>
-void fwd_pieces(const NormArgs& a, int nv, hipStream_t s)
+void fwd_pieces(const NormArgs& a, int nv, int waves, hipStream_t s)
 {
-    if (nv == 1) fwd_launch<DT, G, 1, MODE>(a, s);
-    else if (nv == 2) fwd_launch<DT, G, 2, MODE>(a, s);
-    else if constexpr (DT == CONV_F32 || G == 1024) fwd_launch<DT, G, 4, MODE>(a, s);
+    if (nv == 1) fwd_launch<DT, G, 1, MODE>(a, waves, s);
+    else if (nv == 2) fwd_launch<DT, G, 2, MODE>(a, waves, s);
+    else if constexpr (DT == CONV_F32 || G == 0) fwd_launch<DT, G, 4, MODE>(a, waves, s);
 }
 
 template <int DT, int MODE>
 hipError_t fwd(const NormArgs& a, hipStream_t s)
 {
-    const Form f = form_of(a.cols, DT, 4);
-    if (f.lanes == 8) fwd_pieces<DT, 8, MODE>(a, f.pieces, s);
-    else if (f.lanes == 16) fwd_pieces<DT, 16, MODE>(a, f.pieces, s);
-    else if (f.lanes == 64) fwd_pieces<DT, 64, MODE>(a, f.pieces, s);
-    else if (f.lanes == 256) fwd_pieces<DT, 256, MODE>(a, f.pieces, s);
-    else if (f.lanes == 1024) fwd_pieces<DT, 1024, MODE>(a, f.pieces, s);
+    const FwdForm f = fwd_form(a.rows, a.cols, DT);
+    if (f.lanes == 8) fwd_pieces<DT, 8, MODE>(a, f.pieces, 4, s);
+    else if (f.lanes == 16) fwd_pieces<DT, 16, MODE>(a, f.pieces, 4, s);
+    else if (f.lanes == 64) fwd_pieces<DT, 64, MODE>(a, f.pieces, 4, s);
+    else if (f.waves) fwd_pieces<DT, 0, MODE>(a, f.pieces, f.waves, s);
     else hipLaunchKernelGGL((norm_fwd_any<DT, MODE>), dim3((unsigned)std::min<int64_t>(a.rows, 1 << 20)), dim3(1024), 0, s, a);
     return hipGetLastError();
 }
@@ -533,8 +621,6 @@ hipError_t fwd_type(const NormArgs& a, int dtype, hipStream_t s)
 {
     return dtype == CONV_F32 ? fwd<CONV_F32, MODE>(a, s) : dtype == CONV_F16 ? fwd<CONV_F16, MODE>(a, s) : fwd<CONV_BF16, MODE>(a, s);
 }
-
-Form bwd_form(int cols, int dtype) { return form_of(cols, dtype, dtype == CONV_F32 ? 4 : 2); }
 
 // Workgroups of the backward kernel: one a CU, as a sum of 2 * cols floats each is written and read again, or two where a lane has
 // one piece only (us with 256 / 512: 16384 x 4096 bf16 79 / 84, 200704 x 192 fp32 95 / 101, 200704 x 64 fp16 42 / 31, 20000 x 384 fp16 23 / 19).

@@ -272,6 +272,45 @@ def test_layernorm_quant_is_the_two_calls(rows, cols, dtype):
     same_codes(Q, scale, *ro.quantize_rows(Y.host()), cols)
 
 
+# many rows and few take different numbers of waves for a row; around the ends of waves and of pieces
+WIDE = [(3, 1025), (600, 1025), (600, 1152), (514, 1537), (513, 2563), (5, 5120), (520, 5121), (515, 8193), (513, 9637), (2, 12289), (600, 1031), (2, 16383), (2, 17000), (1, 32768)]
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rows,cols", WIDE)
+def test_rows_of_any_number_of_waves(rows, cols, dtype):
+    torch = torch_mod()
+    check_fwd(rows, cols, dtype, cols + cols % 3, cols + 1, 1, seed=cols)
+    x = random_x(rows, cols, dtype, rows + 2 * cols)
+    x[rows // 2, cols - 1] = np.nan
+    X = Rows(rows, cols, torch_type(dtype), cols + 1, 1, fill=float("inf")).set(x)
+    Q = Rows(rows, cols, torch.int8, B.row_stride(cols) + 16, fill=99)
+    scale = nan_vec(rows)
+    B.quantize_rows(B.make_quant_desc(rows, cols, dtype, X.ld, Q.ld), X.ptr, Q.ptr, scale)
+    same_codes(Q, scale, *ro.quantize_rows(x), cols)
+    rng = np.random.default_rng(cols)
+    gamma, beta = vec(rng.normal(1, 0.3, cols)), vec(rng.normal(0, 0.3, cols))
+    Y = Rows(rows, cols, torch_type(dtype))
+    B.layernorm_fwd(B.make_norm_desc(rows, cols, dtype, EPS, X.ld, cols), X.ptr, gamma, beta, Y.ptr)
+    B.layernorm_quant_fwd(B.make_norm_desc(rows, cols, dtype, EPS, X.ld, Q.ld), X.ptr, gamma, beta, Q.ptr, scale)
+    same_codes(Q, scale, *ro.quantize_rows(Y.host()), cols)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rows,cols", [(600, 1025), (300, 2563), (70, 9637), (40, 16383)])
+def test_layernorm_bwd_of_wide_rows(rows, cols, dtype):
+    check_bwd(rows, cols, dtype, cols + 1, cols + 3, 1, seed=cols)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rows", [1, 2, 40])
+@pytest.mark.parametrize("cols", [1, 3, 4, 5, 7, 8, 9, 11])
+def test_rows_of_less_than_a_piece_that_fill_their_tensor(rows, cols, dtype):
+    """Nothing lies behind the last row, nor before the first."""
+    check_fwd(rows, cols, dtype, seed=cols)
+    check_bwd(rows, cols, dtype, seed=cols)
+
+
 def test_offsets_beyond_32_bits():
     """Rows of tensors of 2.2e9 elements against the same rows on their own."""
     torch = torch_mod()
