@@ -68,28 +68,20 @@ struct Held {
 #pragma unroll
         for (int i = 0; i < NV; ++i) raw[i] = P::raw(x + min((i * lanes() + l) * VEC, cols - VEC));
     }
-    // Zeros past the end of the row.  The last piece of a row that is no multiple of VEC has elements in front that are another
-    // piece's: it is shifted down by as many.
+    // zeros past the end of the row
     static __device__ __forceinline__ void clear(uint4 (&raw)[NV], int cols, int l)
     {
-        const int past = -cols & (VEC - 1), words = past * (int)sizeof(elem_t) / 4;  // the same in all lanes
+        const int past = cols < VEC ? 0 : -cols & (VEC - 1);
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int left = cols - (i * lanes() + l) * VEC;
-            uint32_t w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
-            if (past && cols >= VEC) {
-                uint32_t v[5] = {w[0], w[1], w[2], w[3], 0};
-                if (words & 2) v[0] = v[2], v[1] = v[3], v[2] = v[3] = 0;
-                if (words & 1) v[0] = v[1], v[1] = v[2], v[2] = v[3], v[3] = 0;
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    if (VEC == 8 && (past & 1)) v[k] = __builtin_amdgcn_alignbit(v[k + 1], v[k], 16);
-                    w[k] = left < VEC ? v[k] : w[k];
-                }
+            uint4 w = raw[i];
+            if (past) {
+                const uint4 v = P::shifted(w, past);
+                w.x = left < VEC ? v.x : w.x, w.y = left < VEC ? v.y : w.y, w.z = left < VEC ? v.z : w.z, w.w = left < VEC ? v.w : w.w;
             }
-#pragma unroll
-            for (int k = 0; k < 4; ++k) w[k] = left > 0 ? w[k] : 0;
-            raw[i] = make_uint4(w[0], w[1], w[2], w[3]);
+            w.x = left > 0 ? w.x : 0, w.y = left > 0 ? w.y : 0, w.z = left > 0 ? w.z : 0, w.w = left > 0 ? w.w : 0;
+            raw[i] = w;
         }
     }
     static __device__ __forceinline__ void store(elem_t* y, const float (&v)[VEC], int cols, int i, int l)
@@ -622,21 +614,23 @@ hipError_t fwd_type(const NormArgs& a, int dtype, hipStream_t s)
     return dtype == CONV_F32 ? fwd<CONV_F32, MODE>(a, s) : dtype == CONV_F16 ? fwd<CONV_F16, MODE>(a, s) : fwd<CONV_BF16, MODE>(a, s);
 }
 
-// Workgroups of the backward kernel: one a CU, as a sum of 2 * cols floats each is written and read again, or two where a lane has
-// one piece only (us with 256 / 512: 16384 x 4096 bf16 79 / 84, 200704 x 192 fp32 95 / 101, 200704 x 64 fp16 42 / 31, 20000 x 384 fp16 23 / 19).
-int bwd_threads(int lanes) { return lanes == 1024 ? 1024 : 512; }
+// Workgroups of the backward kernel: one of 512 threads a CU, as a sum of 2 * cols floats each is written and read again, or two where a
+// lane has one piece only (us with 256 / 512 workgroups: 16384 x 4096 bf16 79 / 84, 200704 x 192 fp32 95 / 101, 200704 x 64 fp16 42 / 31,
+// 20000 x 384 fp16 23 / 19).  Rows of eight lanes go to twice as many of 256 threads (us with 512 / 256 threads: 24 x 64 fp32 3.6 / 3.1,
+// 200 x 64 fp32 5.8 / 5.3, 1000 x 100 bf16 8.7 / 7.7, but 393216 x 128 bf16 57.2 / 57.9).
+constexpr int bwd_threads(int lanes) { return lanes == 1024 ? 1024 : lanes == 8 ? 256 : 512; }
 int bwd_parts(int64_t rows, int cols, int dtype)
 {
     const Form f = bwd_form(cols, dtype);
     if (!f.lanes) return (int)std::max<int64_t>(1, std::min<int64_t>(64, (rows + 15) / 16));
     const int here = bwd_threads(f.lanes) / f.lanes;
-    return (int)std::max<int64_t>(1, std::min<int64_t>(f.pieces == 1 && f.lanes < 1024 ? 2 * kCUs : kCUs, (rows + here - 1) / here));
+    return (int)std::max<int64_t>(1, std::min<int64_t>((f.pieces == 1 && f.lanes < 1024 ? 2 * kCUs : kCUs) * (f.lanes == 8 ? 2 : 1), (rows + here - 1) / here));
 }
 
 template <int DT, int G, int NV>
 void bwd_launch(const NormArgs& a, int parts, hipStream_t s)
 {
-    constexpr int NT = G == 1024 ? 1024 : 512;
+    constexpr int NT = bwd_threads(G);
     const dim3 grid((unsigned)parts), block(NT);
     const bool dw = a.dgamma || a.dbeta;
     if (a.dx && dw) hipLaunchKernelGGL((norm_bwd_rows<DT, G, NV, NT, true, true>), grid, block, 0, s, a);

@@ -41,6 +41,20 @@ struct Piece {
                               Prec<DT>::pack2_from_f32(x[4], x[5]), Prec<DT>::pack2_from_f32(x[6], x[7]));
     }
     static __device__ __forceinline__ void put(elem_t* p, const uint4& v) { __builtin_memcpy(p, &v, 16); }
+    // A row's last piece, where it is short, is read so that it ends with the row, without a branch.  Its first `past` elements are then
+    // another piece's: the others come to the front, zeros follow.  (`past` is the same in all lanes: 0 .. VEC - 1.)
+    static __device__ __forceinline__ uint4 shifted(const uint4& u, int past)
+    {
+        const int words = past * (int)sizeof(elem_t) / 4;
+        uint32_t v[5] = {u.x, u.y, u.z, u.w, 0};
+        if (words & 2) v[0] = v[2], v[1] = v[3], v[2] = v[3] = 0;
+        if (words & 1) v[0] = v[1], v[1] = v[2], v[2] = v[3], v[3] = 0;
+        if (VEC == 8 && (past & 1)) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[k] = __builtin_amdgcn_alignbit(v[k + 1], v[k], 16);
+        }
+        return make_uint4(v[0], v[1], v[2], v[3]);
+    }
 };
 
 struct OpSum {
