@@ -1,11 +1,11 @@
 // Layer norm forward and backward, and the row quantiser: one pass over the tensors, the row held in registers.
 //
-// G neighbouring lanes share a row (8, 16, a wave, or a workgroup: forward of as many waves as the row takes, G = 0, backward of 4
-// or 16), each holding up to NV pieces of 16 bytes.  The mean
-// comes first and the variance is summed around it, from registers.  A workgroup keeps its columns' gamma and beta in registers over
-// all its rows, and asks for its next row before it works on the present one.  Backward, a lane adds up dgamma and dbeta of its columns
+// G neighbouring lanes share a row (8, 16, a wave, or several: forward a workgroup of as many as the row takes, G = 0, backward 4 or 8),
+// each holding up to NV pieces of 16 bytes.  The mean comes first and the variance is summed around it, from registers.  A workgroup keeps
+// its columns' gamma and beta in registers over all its rows, and asks for its next row before it works on the present one.  Backward, a lane adds up dgamma and dbeta of its columns
 // over its rows in registers; a workgroup's lanes with the same columns are added through LDS, and a second kernel adds the
-// workgroups' sums, always in the same order.  Longer rows than 16 waves hold are read again for every pass (`_any`).
+// workgroups' sums, always in the same order.  Longer rows (forward 32 elements a lane of 16 waves, backward of 8) are read again for
+// every pass (`_any`).
 #include <algorithm>
 
 #include "rows_common.h"
@@ -287,8 +287,7 @@ __global__ __launch_bounds__(NT) void norm_bwd_rows(NormArgs a)
         H::load(ndy, (const elem_t*)a.dy + r * a.ldy, a.cols, l);
         nmean = a.mean[r], nrstd = a.rstd[r];
     };
-    // (16 waves with 16 elements a lane have no registers left for the next row: they spilled 50 .. 70)
-    constexpr bool AHEAD = G < 1024 || NV * VEC < 16;
+    constexpr bool AHEAD = NV * VEC < 32;
     if (AHEAD && a.rows) fetch(row);
     float gamma[NV][VEC], dg[NV][VEC], db[NV][VEC];
     if constexpr (DX) H::columns(gamma, a.gamma, 1.0f, a.cols, l);
@@ -544,17 +543,22 @@ __global__ __launch_bounds__(256) void norm_dw_any(NormArgs a)
 
 constexpr int kCUs = 256;
 
-// Backward: the fewest lanes that hold the row with 16 elements each, which is what a lane has registers for with their gradients, sums
-// and the next row.  lanes 0: the row is too long.
+// Backward: the fewest lanes that hold the row with 16 elements each; a wave and more of 16-bit rows 24, so that fewer are idle (us with 16 / 24:
+// 43690 x 1152 bf16 77 / 61, 2000 x 1536 bf16 14 / 12; fp32, whose next row takes twice the registers, 32768 x 1536 108 / 124).  The longest
+// have 512 lanes with up to 32, the 32 without the next row (which spilled 90 registers): 5225 x 9632 bf16 65 us, 4096 x 12288
+// 67, 3072 x 16384 75, where 16 waves with 16 a lane took 87, 77 and 78.  lanes 0: the row is too long.
 struct Form {
     int lanes, pieces;
 };
 Form bwd_form(int cols, int dtype)
 {
     const int vec = dtype == CONV_F32 ? 4 : 8, most = 16 / vec, pieces = (cols + vec - 1) / vec;
-    for (int lanes : {8, 16, 64, 256, 1024}) {
+    for (int lanes : {8, 16, 64, 256, 512}) {
         const int n = (pieces + lanes - 1) / lanes;
-        if (n <= most) return Form{lanes, n <= 1 ? 1 : n <= 2 ? 2 : 4};
+        if (n <= most && lanes < 512) return Form{lanes, n <= 1 ? 1 : n <= 2 ? 2 : 4};
+        if (n <= most) return Form{lanes, most};
+        if (n <= most * 3 / 2 && (lanes == 512 || (lanes >= 64 && vec == 8))) return Form{lanes, most * 3 / 2};
+        if (n <= most * 2 && lanes == 512) return Form{lanes, most * 2};
     }
     return Form{0, 0};
 }
@@ -618,13 +622,13 @@ hipError_t fwd_type(const NormArgs& a, int dtype, hipStream_t s)
 // lane has one piece only (us with 256 / 512 workgroups: 16384 x 4096 bf16 79 / 84, 200704 x 192 fp32 95 / 101, 200704 x 64 fp16 42 / 31,
 // 20000 x 384 fp16 23 / 19).  Rows of eight lanes go to twice as many of 256 threads (us with 512 / 256 threads: 24 x 64 fp32 3.6 / 3.1,
 // 200 x 64 fp32 5.8 / 5.3, 1000 x 100 bf16 8.7 / 7.7, but 393216 x 128 bf16 57.2 / 57.9).
-constexpr int bwd_threads(int lanes) { return lanes == 1024 ? 1024 : lanes == 8 ? 256 : 512; }
+constexpr int bwd_threads(int lanes) { return lanes == 8 ? 256 : 512; }
 int bwd_parts(int64_t rows, int cols, int dtype)
 {
     const Form f = bwd_form(cols, dtype);
     if (!f.lanes) return (int)std::max<int64_t>(1, std::min<int64_t>(64, (rows + 15) / 16));
     const int here = bwd_threads(f.lanes) / f.lanes;
-    return (int)std::max<int64_t>(1, std::min<int64_t>((f.pieces == 1 && f.lanes < 1024 ? 2 * kCUs : kCUs) * (f.lanes == 8 ? 2 : 1), (rows + here - 1) / here));
+    return (int)std::max<int64_t>(1, std::min<int64_t>((f.pieces == 1 ? 2 * kCUs : kCUs) * (f.lanes == 8 ? 2 : 1), (rows + here - 1) / here));
 }
 
 template <int DT, int G, int NV>
@@ -641,9 +645,16 @@ void bwd_launch(const NormArgs& a, int parts, hipStream_t s)
 template <int DT, int G>
 void bwd_pieces(const NormArgs& a, int nv, int parts, hipStream_t s)
 {
-    if (nv == 1) bwd_launch<DT, G, 1>(a, parts, s);
-    else if (nv == 2) bwd_launch<DT, G, 2>(a, parts, s);
-    else if constexpr (DT == CONV_F32) bwd_launch<DT, G, 4>(a, parts, s);
+    constexpr int MOST = DT == CONV_F32 ? 4 : 2;
+    if (nv == MOST) bwd_launch<DT, G, MOST>(a, parts, s);
+    if constexpr (G < 512) {
+        if (nv == 1) bwd_launch<DT, G, 1>(a, parts, s);
+        if (MOST == 4 && nv == 2) bwd_launch<DT, G, 2>(a, parts, s);
+    }
+    if constexpr (G == 512 || (G >= 64 && DT != CONV_F32))
+        if (nv == MOST * 3 / 2) bwd_launch<DT, G, MOST * 3 / 2>(a, parts, s);
+    if constexpr (G == 512)
+        if (nv == MOST * 2) bwd_launch<DT, G, MOST * 2>(a, parts, s);
 }
 
 // 64 columns a workgroup where that makes a workgroup a CU, else 16: 423 sums of 2 x 384 columns took 4.7 us with 64.
@@ -665,7 +676,7 @@ hipError_t bwd(const NormArgs& a, hipStream_t s)
         else if (f.lanes == 16) bwd_pieces<DT, 16>(a, f.pieces, parts, s);
         else if (f.lanes == 64) bwd_pieces<DT, 64>(a, f.pieces, parts, s);
         else if (f.lanes == 256) bwd_pieces<DT, 256>(a, f.pieces, parts, s);
-        else bwd_pieces<DT, 1024>(a, f.pieces, parts, s);
+        else bwd_pieces<DT, 512>(a, f.pieces, parts, s);
     } else {
         if (dw) hipLaunchKernelGGL((norm_dw_any<DT>), dim3((unsigned)((a.cols + 255) / 256), parts), dim3(256), 0, s, a);
         if (a.dx && a.rows) hipLaunchKernelGGL((norm_dx_any<DT>), dim3((unsigned)std::min<int64_t>(a.rows, 1 << 20)), dim3(1024), 0, s, a);

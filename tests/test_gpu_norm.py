@@ -303,6 +303,13 @@ def test_layernorm_bwd_of_wide_rows(rows, cols, dtype):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rows,cols", [(600, 1152), (530, 1536), (270, 4097), (270, 5120), (260, 6143), (300, 8192), (257, 8193), (300, 12288), (258, 12289), (3, 16384), (2, 16385)])
+def test_layernorm_bwd_of_rows_of_any_number_of_waves(rows, cols, dtype):
+    check_bwd(rows, cols, dtype, seed=cols)
+    check_bwd(min(rows, 5), cols, dtype, cols + 8, cols + 8, 0, seed=cols + 1, want=1, in_place=True)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("rows", [1, 2, 40])
 @pytest.mark.parametrize("cols", [1, 3, 4, 5, 7, 8, 9, 11])
 def test_rows_of_less_than_a_piece_that_fill_their_tensor(rows, cols, dtype):
