@@ -44,19 +44,26 @@ class ScoringHead:
         self.logp, self.lse, self.entropy = (torch.empty(self.max_rows, **f32) for _ in range(3))
         self.top_id = torch.empty(self.max_rows, self.top, dtype=torch.int64, device=dev)
         self.top_logp = torch.empty(self.max_rows, self.top, **f32)
-        self._plans, self._ws = {}, torch.empty(256, dtype=torch.uint8, device=dev)
+        # One workspace for the head's whole life: recorded graphs and calls on other streams hold its address.  What is needed goes up
+        # and down with the rows (workgroups that share a row or a reduction become fewer), so every number of them is asked.
+        need = 256
+        for rows in range(1, self.max_rows + 1):
+            linear, logprob = self._products(rows)
+            need = max(need, B.int_linear_workspace_bytes(linear), B.logprob_workspace_bytes(logprob))
+        self._plans, self._ws = {}, torch.empty(need, dtype=torch.uint8, device=dev)
+
+    def _products(self, rows: int):
+        code = _code(self.torch, self.logits_dtype)
+        return (B.make_int_linear_desc(rows, self.V, self.D, code, lda=self.q.stride(0), ldw=self.w.stride(0)),
+                B.make_logprob_desc(rows, self.V, code, self.top))
 
     def plan(self, rows: int, ldx: int):
-        """The three descriptors for a number of rows, and a workspace that serves them; call it ahead of a graph's capture."""
+        """The three descriptors for a number of rows and a row stride of the features, made once."""
+        if not 0 <= rows <= self.max_rows:
+            raise ValueError("a head of %d rows cannot score %d" % (self.max_rows, rows))
         key = (rows, ldx)
         if key not in self._plans:
-            norm = B.make_norm_desc(rows, self.D, self.code, self.eps, ldx, self.q.stride(0))
-            linear = B.make_int_linear_desc(rows, self.V, self.D, _code(self.torch, self.logits_dtype), lda=self.q.stride(0), ldw=self.w.stride(0))
-            logprob = B.make_logprob_desc(rows, self.V, _code(self.torch, self.logits_dtype), self.top)
-            need = max(B.int_linear_workspace_bytes(linear), B.logprob_workspace_bytes(logprob))
-            if need > self._ws.numel():
-                self._ws = self.torch.empty(need, dtype=self.torch.uint8, device=self.w.device)
-            self._plans[key] = (norm, linear, logprob)
+            self._plans[key] = (B.make_norm_desc(rows, self.D, self.code, self.eps, ldx, self.q.stride(0)), *self._products(rows))
         return self._plans[key]
 
     def score(self, features, target=None, stream=None):

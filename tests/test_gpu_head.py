@@ -144,3 +144,30 @@ def test_refusals_of_the_heads_own():
             head.score(x)
     with pytest.raises(B.ConvError):
         ScoringHead(d["gamma"], d["beta"], d["w"], max_rows=4, top=101).score(d["x"])
+
+
+def test_a_recorded_graph_outlives_scores_of_other_sizes():
+    """One row is recorded; batches of sizes that need more workspace are scored and memory is taken in between; the graph still
+    writes only to the head's own buffers."""
+    torch = torch_mod()
+    D, V = 256, 50257
+    _, d = case(20, D, V, wl.BF16, 31)
+    head = ScoringHead(d["gamma"], d["beta"], d["w"], max_rows=20, top=5)
+    x, target = d["x"][:1].clone(), d["target"][:1].clone()
+    head.score(x, target)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = head.score(x, target)
+    want = []
+    for i in range(20):
+        want.append({k: v.clone() for k, v in head.score(d["x"][i:i + 1], d["target"][i:i + 1]).items()})
+    held = []
+    for i, rows in enumerate((2, 4, 8, 20, 3, 1)):
+        head.score(d["x"][:rows], d["target"][:rows])
+        held += [torch.full((n,), 77, dtype=torch.uint8, device="cuda") for n in (256, 768, 1536, 6144, 12288)]
+        x.copy_(d["x"][i:i + 1]), target.copy_(d["target"][i:i + 1])
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(out[k], want[i][k]) for k in out), i
+        assert all(bool((h == 77).all()) for h in held), i

@@ -1,0 +1,47 @@
+"""The heads without a GPU: what they hand to the library, and what they refuse before anything is launched.
+
+The binding's launching functions are replaced by ones that write down their arguments, so tensors can lie in host memory; descriptors
+and workspace sizes are the library's own."""
+import pytest
+import torch
+
+from paper_1611_06945_amd import binding as B
+from paper_1611_06945_amd import head as H
+
+LAUNCHES = ("quantize_rows", "layernorm_quant_fwd", "int_linear_fwd", "logprob_fwd", "layernorm_fwd", "conv_fwd_ws", "logprob_bwd",
+            "conv_convert_layout", "layernorm_bwd")
+
+
+@pytest.fixture
+def calls(monkeypatch):
+    made = []
+    for name in LAUNCHES:
+        monkeypatch.setattr(B, name, lambda *args, name=name: made.append((name, args)))
+    return made
+
+
+def scoring_head(D=64, V=100, dtype=torch.float16, **kw):
+    return H.ScoringHead(torch.ones(D), torch.zeros(D), torch.randn(V, D).to(dtype), **kw)
+
+
+@pytest.mark.parametrize("D,V,max_rows,top", [(64, 50257, 8, 5), (64, 40000, 300, 20), (40000, 10, 140, 0)])
+def test_scoring_head_keeps_one_workspace_for_all_rows(calls, D, V, max_rows, top):
+    """A recorded graph holds the workspace's address, so no later call may replace it; it has to do for every number of rows."""
+    head = scoring_head(D, V, max_rows=max_rows, top=top)
+    most = 0
+    for rows in (1, max_rows, 2, 4, 20, 100, 250):
+        if rows > max_rows:
+            continue
+        del calls[:]
+        head.score(torch.randn(rows, D).half())
+        for name, args in calls:
+            if name in ("int_linear_fwd", "logprob_fwd"):
+                ws, size = args[-3:-1]
+                need = (B.int_linear_workspace_bytes if name == "int_linear_fwd" else B.logprob_workspace_bytes)(args[0])
+                most = max(most, need)
+                assert ws is head._ws and size == ws.numel() >= need
+                first = ws.data_ptr() if rows == 1 else first
+                assert ws.data_ptr() == first, (name, rows)
+    assert most > 256  # the sizes are ones at which a workspace is needed
+    with pytest.raises(ValueError):
+        head.plan(max_rows + 1, D)
