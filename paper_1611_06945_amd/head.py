@@ -70,8 +70,8 @@ class ScoringHead:
         """features [T][D] (rows may be strided), target int64 [T] or None (negative: no token).  Returns views of the head's own
         buffers, valid until the next call: logp (None without target), lse, entropy, top_id, top_logp."""
         rows = features.shape[0]
-        if features.shape[1] != self.D or features.dtype != self.dtype or (rows > 1 and features.stride(1) != 1) or rows > self.max_rows:
-            raise ValueError("features must be [T <= %d][%d] of %s, rows contiguous" % (self.max_rows, self.D, self.dtype))
+        if features.shape[1] != self.D or features.dtype != self.dtype or (rows and self.D > 1 and features.stride(1) != 1) or rows > self.max_rows:
+            raise ValueError("features must be [T <= %d][%d] of %s, the columns of a row next to each other" % (self.max_rows, self.D, self.dtype))
         norm, linear, logprob = self.plan(rows, features.stride(0) if rows > 1 else self.D)
         ws, n = self._ws, self._ws.numel()
         B.layernorm_quant_fwd(norm, features, self.gamma, self.beta, self.q, self.q_scale, stream)

@@ -171,3 +171,17 @@ def test_a_recorded_graph_outlives_scores_of_other_sizes():
         torch.cuda.synchronize()
         assert all(torch.equal(out[k], want[i][k]) for k in out), i
         assert all(bool((h == 77).all()) for h in held), i
+
+
+def test_one_row_out_of_a_channel_plane():
+    """The features of one image as a slice of its channel planes are refused, as those of two are; made dense they are scored."""
+    torch = torch_mod()
+    _, d = case(1, 64, 100, wl.F16, 3)
+    head = ScoringHead(d["gamma"], d["beta"], d["w"], max_rows=4, top=3)
+    planes = torch.zeros(1, 64, 2, 2, dtype=torch.float16, device="cuda")
+    planes[:, :, 0, 0] = d["x"]
+    with pytest.raises(ValueError):
+        head.score(planes[:, :, 0, 0])
+    got = {k: v.clone() for k, v in head.score(planes[:, :, 0, 0].contiguous(), d["target"]).items()}
+    want = head.score(d["x"], d["target"])
+    assert all(torch.equal(got[k], want[k]) for k in got)

@@ -45,3 +45,25 @@ def test_scoring_head_keeps_one_workspace_for_all_rows(calls, D, V, max_rows, to
     assert most > 256  # the sizes are ones at which a workspace is needed
     with pytest.raises(ValueError):
         head.plan(max_rows + 1, D)
+
+
+@pytest.mark.parametrize("rows", [1, 3])
+def test_features_whose_columns_are_not_neighbours_are_refused(calls, rows):
+    """The kernels read rows; [1][D] of a channel plane, or a transposed tensor's first row, has its columns elsewhere."""
+    head = scoring_head(max_rows=4)
+    for x in (torch.randn(rows, 64, 3, 3).half()[:, :, 0, 0], torch.randn(64, 5).half().t()[:rows], torch.randn(rows, 128).half()[:, ::2]):
+        del calls[:]
+        with pytest.raises(ValueError):
+            head.score(x)
+        assert not calls
+    x = torch.randn(rows, 1, 64).half().expand(rows, 2, 64)[:, 1]  # rows of any stride, and of any start, are fine
+    head.score(x)
+    assert calls[-3][1][0].ldx == 64 and calls[-3][1][1] is x
+
+
+def test_features_of_one_column(calls):
+    head = scoring_head(D=1, max_rows=4)
+    head.score(torch.randn(4, 7).half()[:, 2:3])
+    assert calls[-3][1][0].ldx == 7
+    head.score(torch.randn(1, 7).half()[:, 2:3])
+    assert calls[-3][1][0].ldx == 1
