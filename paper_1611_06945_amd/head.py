@@ -31,13 +31,15 @@ class ScoringHead:
 
         self.torch, self.gamma, self.beta, self.bias, self.eps = torch, gamma, beta, bias, eps
         self.V, self.D = weight.shape
+        if self.D > 1 and weight.stride(1) != 1:
+            raise ValueError("the columns of a weight's row have to be next to each other")
         self.max_rows, self.top = int(max_rows), int(top)
         self.code, self.logits_dtype = _code(torch, weight.dtype), logits_dtype or weight.dtype
         self.dtype = weight.dtype
         dev, ld = weight.device, B.row_stride(self.D)
         self.w = torch.empty(self.V, ld, dtype=torch.int8, device=dev)
         self.w_scale = torch.empty(self.V, dtype=torch.float32, device=dev)
-        B.quantize_rows(B.make_quant_desc(self.V, self.D, self.code, weight.stride(0)), weight, self.w, self.w_scale)
+        B.quantize_rows(B.make_quant_desc(self.V, self.D, self.code, weight.stride(0) if self.V > 1 else self.D), weight, self.w, self.w_scale)
         f32 = dict(dtype=torch.float32, device=dev)
         self.q, self.q_scale = torch.empty(self.max_rows, ld, dtype=torch.int8, device=dev), torch.empty(self.max_rows, **f32)
         self.logits = torch.empty(self.max_rows, self.V, dtype=self.logits_dtype, device=dev)

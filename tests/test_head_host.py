@@ -67,3 +67,16 @@ def test_features_of_one_column(calls):
     assert calls[-3][1][0].ldx == 7
     head.score(torch.randn(1, 7).half()[:, 2:3])
     assert calls[-3][1][0].ldx == 1
+
+
+def test_weights_whose_columns_are_not_neighbours_are_refused(calls):
+    for w in (torch.randn(100, 128).half()[:, ::2], torch.randn(64, 100).half().t(), torch.randn(1, 64, 2).half()[:, :, 0]):
+        with pytest.raises(ValueError):
+            H.ScoringHead(None, None, w)
+    assert not calls
+    w = torch.randn(100, 80).half()[:, :64]  # a row stride of its own is fine
+    H.ScoringHead(None, None, w)
+    assert calls[-1][1][0].ldx == 80
+    w = torch.randn(64, 1).half().t()  # one row: its stride says nothing
+    H.ScoringHead(None, None, w, top=1)
+    assert w.stride(0) == 1 and calls[-1][1][0].ldx == 64
