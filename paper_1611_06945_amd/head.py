@@ -23,6 +23,13 @@ def _code(torch, dtype):
     return {torch.float32: B.CONV_F32, torch.float16: B.CONV_F16, torch.bfloat16: B.CONV_BF16}[dtype]
 
 
+def _check(name, t, dtype, shape, device):
+    """The kernels are handed addresses: a tensor of another type, size, layout or place would be read as what it is not."""
+    if t.dtype != dtype or t.shape != shape or t.device != device or not t.is_contiguous():
+        raise ValueError("%s must be %s %s, dense, on %s; it is %s %s with strides %s on %s" % (
+            name, dtype, list(shape), device, t.dtype, list(t.shape), list(t.stride()), t.device))
+
+
 class ScoringHead:
     def __init__(self, gamma, beta, weight, bias=None, max_rows: int = 64, top: int = 5, eps: float = 1e-5, logits_dtype=None):
         """gamma, beta: fp32 [D] or None; weight: [V][D] in fp32, fp16 or bf16 on the GPU, which is also the type of the
@@ -74,6 +81,8 @@ class ScoringHead:
         rows = features.shape[0]
         if features.shape[1] != self.D or features.dtype != self.dtype or (rows and self.D > 1 and features.stride(1) != 1) or rows > self.max_rows:
             raise ValueError("features must be [T <= %d][%d] of %s, the columns of a row next to each other" % (self.max_rows, self.D, self.dtype))
+        if target is not None:
+            _check("target", target, self.torch.int64, (rows,), self.w.device)
         norm, linear, logprob = self.plan(rows, features.stride(0) if rows > 1 else self.D)
         ws, n = self._ws, self._ws.numel()
         B.layernorm_quant_fwd(norm, features, self.gamma, self.beta, self.q, self.q_scale, stream)

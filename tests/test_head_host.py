@@ -80,3 +80,19 @@ def test_weights_whose_columns_are_not_neighbours_are_refused(calls):
     w = torch.randn(64, 1).half().t()  # one row: its stride says nothing
     H.ScoringHead(None, None, w, top=1)
     assert w.stride(0) == 1 and calls[-1][1][0].ldx == 64
+
+
+BAD_TARGETS = [torch.zeros(3, dtype=torch.int32), torch.zeros(3), torch.zeros(2, dtype=torch.int64), torch.zeros(0, dtype=torch.int64),
+               torch.zeros(6, dtype=torch.int64)[::2], torch.zeros(1, dtype=torch.int64).expand(3), torch.zeros(3, 2, dtype=torch.int64),
+               torch.zeros(3, dtype=torch.int64, device="meta")]
+
+
+@pytest.mark.parametrize("target", BAD_TARGETS)
+def test_targets_that_are_not_one_whole_number_a_row_are_refused(calls, target):
+    head = scoring_head(max_rows=4)
+    del calls[:]
+    with pytest.raises(ValueError):
+        head.score(torch.randn(3, 64).half(), target)
+    assert not calls
+    head.score(torch.randn(3, 64).half(), torch.zeros(3, dtype=torch.int64))
+    head.score(torch.randn(1, 64).half(), torch.zeros(6, dtype=torch.int64)[::6])  # one number has no neighbours
