@@ -40,6 +40,9 @@ class ScoringHead:
         self.V, self.D = weight.shape
         if self.D > 1 and weight.stride(1) != 1:
             raise ValueError("the columns of a weight's row have to be next to each other")
+        for name, t, n in (("gamma", gamma, self.D), ("beta", beta, self.D), ("bias", bias, self.V)):
+            if t is not None:
+                _check(name, t, torch.float32, (n,), weight.device)
         self.max_rows, self.top = int(max_rows), int(top)
         self.code, self.logits_dtype = _code(torch, weight.dtype), logits_dtype or weight.dtype
         self.dtype = weight.dtype

@@ -96,3 +96,16 @@ def test_targets_that_are_not_one_whole_number_a_row_are_refused(calls, target):
     assert not calls
     head.score(torch.randn(3, 64).half(), torch.zeros(3, dtype=torch.int64))
     head.score(torch.randn(1, 64).half(), torch.zeros(6, dtype=torch.int64)[::6])  # one number has no neighbours
+
+
+@pytest.mark.parametrize("bad", [lambda n: torch.ones(n).bfloat16(), lambda n: torch.ones(n).double(), lambda n: torch.ones(n - 1), lambda n: torch.ones(1),
+                                 lambda n: torch.ones(2 * n)[::2], lambda n: torch.ones(n, 1), lambda n: torch.ones(n, device="meta")])
+def test_vectors_that_are_not_fp32_are_refused(calls, bad):
+    """gamma, beta and bias are read as dense fp32 of the row's, or the vocabulary's, length."""
+    w = torch.randn(100, 64).half()
+    for gamma, beta, bias in ((bad(64), None, None), (None, bad(64), None), (None, None, bad(100))):
+        with pytest.raises(ValueError):
+            H.ScoringHead(gamma, beta, w, bias)
+    assert not calls
+    H.ScoringHead(torch.ones(64), torch.ones(64), w, torch.ones(100))
+    H.ScoringHead(None, None, w, None)
