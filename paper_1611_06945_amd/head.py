@@ -18,6 +18,8 @@ from __future__ import annotations
 
 from . import binding as B
 
+GPU = "cuda"  # where every tensor here lives
+
 
 def _code(torch, dtype):
     return {torch.float32: B.CONV_F32, torch.float16: B.CONV_F16, torch.bfloat16: B.CONV_BF16}[dtype]
@@ -40,6 +42,8 @@ class ScoringHead:
         self.V, self.D = weight.shape
         if self.D > 1 and weight.stride(1) != 1:
             raise ValueError("the columns of a weight's row have to be next to each other")
+        if weight.device.type != GPU:
+            raise ValueError("the weight is on %s, not on the GPU" % weight.device)
         for name, t, n in (("gamma", gamma, self.D), ("beta", beta, self.D), ("bias", bias, self.V)):
             if t is not None:
                 _check(name, t, torch.float32, (n,), weight.device)
@@ -82,6 +86,8 @@ class ScoringHead:
         """features [T][D] (rows may be strided), target int64 [T] or None (negative: no token).  Returns views of the head's own
         buffers, valid until the next call: logp (None without target), lse, entropy, top_id, top_logp."""
         rows = features.shape[0]
+        if features.device != self.w.device:
+            raise ValueError("the features are on %s, the head on %s" % (features.device, self.w.device))
         if features.shape[1] != self.D or features.dtype != self.dtype or (rows and self.D > 1 and features.stride(1) != 1) or rows > self.max_rows:
             raise ValueError("features must be [T <= %d][%d] of %s, the columns of a row next to each other" % (self.max_rows, self.D, self.dtype))
         if target is not None:

@@ -15,6 +15,7 @@ LAUNCHES = ("quantize_rows", "layernorm_quant_fwd", "int_linear_fwd", "logprob_f
 @pytest.fixture
 def calls(monkeypatch):
     made = []
+    monkeypatch.setattr(H, "GPU", "cpu", raising=False)
     for name in LAUNCHES:
         monkeypatch.setattr(B, name, lambda *args, name=name: made.append((name, args)))
     return made
@@ -109,3 +110,15 @@ def test_vectors_that_are_not_fp32_are_refused(calls, bad):
     assert not calls
     H.ScoringHead(torch.ones(64), torch.ones(64), w, torch.ones(100))
     H.ScoringHead(None, None, w, None)
+
+
+def test_tensors_that_are_not_on_the_gpu_are_refused(calls, monkeypatch):
+    """An address in host memory would be handed to a kernel."""
+    head = scoring_head(max_rows=4)
+    del calls[:]
+    with pytest.raises(ValueError):
+        head.score(torch.empty(3, 64, dtype=torch.float16, device="meta"))
+    monkeypatch.setattr(H, "GPU", "cuda")
+    with pytest.raises(ValueError):
+        H.ScoringHead(None, None, torch.randn(100, 64).half())
+    assert not calls
