@@ -124,20 +124,26 @@ class TrainingHead:
         need = max([B.layernorm_bwd_workspace_bytes(self.norm), B.logprob_workspace_bytes(self.logprob)] +
                    [B.conv_workspace_bytes(d) for d in (self.to_logits, self.to_dy, self.to_dw)])
         self.ws = torch.empty(max(256, need), dtype=torch.uint8, device=device)
+        self.saved = None
 
     def forward(self, features, gamma, beta, weight, target, stream=None):
         """-> (logp, entropy) of the batch, fp32 [rows]; keeps what backward() needs."""
         ws, n = self.ws, self.ws.numel()
-        self.saved = (features, gamma, weight, target)
+        self.saved = None
         B.layernorm_fwd(self.norm, features, gamma, beta, self.y, self.mean, self.rstd, stream)
         B.conv_fwd_ws(self.to_logits, self.y, weight, None, self.logits, ws, n, stream)
         B.logprob_fwd(self.logprob, self.logits, target, self.logp, self.lse, self.entropy, None, None, ws, n, stream)
+        self.saved = (features, gamma, weight, target)
         return self.logp, self.entropy
 
     def backward(self, g_logp, g_entropy=None, stream=None):
-        """-> (dfeatures, dgamma, dbeta, dweight); the logits' gradient takes the logits' place."""
+        """-> (dfeatures, dgamma, dbeta, dweight), once for each forward(): the logits' gradient takes the logits' place.  Give both
+        gradients to one call; features, gamma and weight have to be those of forward() still."""
+        if self.saved is None:
+            raise RuntimeError("backward() needs a forward() of its own: the logits are no longer there")
         features, gamma, weight, target = self.saved
         ws, n = self.ws, self.ws.numel()
+        self.saved = None
         B.logprob_bwd(self.logprob, self.logits, target, self.lse, self.entropy, g_logp, g_entropy, self.logits, stream)
         B.conv_convert_layout(1, self.V, self.D, self.code, weight, self.w_t, stream)
         B.conv_fwd_ws(self.to_dy, self.logits, self.w_t, None, self.dy, ws, n, stream)

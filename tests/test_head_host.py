@@ -122,3 +122,43 @@ def test_tensors_that_are_not_on_the_gpu_are_refused(calls, monkeypatch):
     with pytest.raises(ValueError):
         H.ScoringHead(None, None, torch.randn(100, 64).half())
     assert not calls
+
+
+def training_head(T=3, D=64, V=100, dtype=torch.float16):
+    head = H.TrainingHead(T, D, V, dtype, device="cpu")
+    batch = (torch.randn(T, D).to(dtype), torch.ones(D), torch.zeros(D), torch.randn(V, D).to(dtype), torch.zeros(T, dtype=torch.int64))
+    return head, batch, torch.ones(T)
+
+
+def test_a_second_backward_is_refused(calls):
+    """The first one puts the gradient in the logits' place."""
+    head, batch, g = training_head()
+    with pytest.raises(RuntimeError):
+        head.backward(g)
+    assert not calls
+    for _ in range(2):
+        head.forward(*batch)
+        head.backward(g)
+        del calls[:]
+        with pytest.raises(RuntimeError):
+            head.backward(g)
+        with pytest.raises(RuntimeError):
+            head.backward(None, g)
+        assert not calls
+
+
+def test_backward_after_a_forward_that_failed_is_refused(calls, monkeypatch):
+    head, batch, g = training_head()
+    head.forward(*batch)
+
+    def fail(*_):
+        raise B.ConvError(B.CONV_EHIP, "conv_fwd_ws")
+
+    with monkeypatch.context() as m:
+        m.setattr(B, "conv_fwd_ws", fail)
+        with pytest.raises(B.ConvError):
+            head.forward(*batch)
+    del calls[:]
+    with pytest.raises(RuntimeError):
+        head.backward(g)
+    assert not calls
