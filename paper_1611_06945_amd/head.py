@@ -127,7 +127,13 @@ class TrainingHead:
         self.saved = None
 
     def forward(self, features, gamma, beta, weight, target, stream=None):
-        """-> (logp, entropy) of the batch, fp32 [rows]; keeps what backward() needs."""
+        """features [rows][D] and weight [V][D] of the head's type, gamma and beta fp32 [D] or None, target int64 [rows], all dense
+        -> (logp, entropy) of the batch, fp32 [rows]; keeps what backward() needs.  There is no bias."""
+        f32, dev = self.torch.float32, self.logits.device
+        for name, t, dtype, shape in (("features", features, self.dtype, (self.rows, self.D)), ("gamma", gamma, f32, (self.D,)), ("beta", beta, f32, (self.D,)),
+                                      ("weight", weight, self.dtype, (self.V, self.D)), ("target", target, self.torch.int64, (self.rows,))):
+            if t is not None:
+                _check(name, t, dtype, shape, dev)
         ws, n = self.ws, self.ws.numel()
         self.saved = None
         B.layernorm_fwd(self.norm, features, gamma, beta, self.y, self.mean, self.rstd, stream)
@@ -137,14 +143,18 @@ class TrainingHead:
         return self.logp, self.entropy
 
     def backward(self, g_logp, g_entropy=None, stream=None):
-        """-> (dfeatures, dgamma, dbeta, dweight), once for each forward(): the logits' gradient takes the logits' place.  Give both
-        gradients to one call; features, gamma and weight have to be those of forward() still."""
+        """g_logp, g_entropy: fp32 [rows], one may be None -> (dfeatures, dgamma, dbeta, dweight).  Once for each forward(), since the
+        logits' gradient takes the logits' place: give both gradients to one call.  Features, gamma and weight have to be those of
+        forward() still."""
         if self.saved is None:
             raise RuntimeError("backward() needs a forward() of its own: the logits are no longer there")
+        for name, t in (("g_logp", g_logp), ("g_entropy", g_entropy)):
+            if t is not None:
+                _check(name, t, self.torch.float32, (self.rows,), self.logits.device)
         features, gamma, weight, target = self.saved
         ws, n = self.ws, self.ws.numel()
-        self.saved = None
         B.logprob_bwd(self.logprob, self.logits, target, self.lse, self.entropy, g_logp, g_entropy, self.logits, stream)
+        self.saved = None
         B.conv_convert_layout(1, self.V, self.D, self.code, weight, self.w_t, stream)
         B.conv_fwd_ws(self.to_dy, self.logits, self.w_t, None, self.dy, ws, n, stream)
         B.conv_convert_layout(1, self.rows, self.V, self.code, self.logits, self.dlogits_t, stream)

@@ -162,3 +162,31 @@ def test_backward_after_a_forward_that_failed_is_refused(calls, monkeypatch):
     with pytest.raises(RuntimeError):
         head.backward(g)
     assert not calls
+
+
+@pytest.mark.parametrize("place,bad", [
+    (0, lambda t: t[:2]), (0, lambda t: t.float()), (0, lambda t: torch.cat([t, t], 1)[:, :64]), (0, lambda t: t.repeat(1, 2)[:, ::2]), (0, lambda t: t[:, :32]),
+    (0, lambda t: t.to("meta")), (1, lambda t: t.half()), (1, lambda t: t[:8]), (2, lambda t: t.bfloat16()), (2, lambda t: torch.zeros(128)[::2]),
+    (3, lambda t: t.float()), (3, lambda t: t[:99]), (3, lambda t: t.t().contiguous().t()), (3, lambda t: torch.cat([t, t], 1)[:, :64]),
+    (4, lambda t: t.int()), (4, lambda t: t[:2]), (4, lambda t: torch.zeros(6, dtype=torch.int64)[::2])])
+def test_batches_that_do_not_fit_the_training_head_are_refused(calls, place, bad):
+    """A smaller last batch, a strided view or another type would be read as what the head was made for."""
+    head, batch, g = training_head()
+    args = list(batch)
+    args[place] = bad(args[place])
+    with pytest.raises(ValueError):
+        head.forward(*args)
+    assert not calls
+    head.forward(batch[0], None, None, *batch[3:])
+
+
+@pytest.mark.parametrize("bad", [lambda t: t[:2], lambda t: t.half(), lambda t: t.double(), lambda t: torch.zeros(6)[::2], lambda t: t[:1].expand(3), lambda t: t.to("meta")])
+def test_gradients_that_do_not_fit_the_batch_are_refused(calls, bad):
+    head, batch, g = training_head()
+    for args in ((bad(g), None), (g, bad(g)), (None, bad(g))):
+        head.forward(*batch)
+        del calls[:]
+        with pytest.raises(ValueError):
+            head.backward(*args)
+        assert not calls
+        head.backward(g, g)  # the logits are still there
