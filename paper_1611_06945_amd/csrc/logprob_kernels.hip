@@ -493,16 +493,16 @@ __global__ __launch_bounds__(256) void logprob_join(LogprobArgs a, int splits)
 }
 
 // The gradient: a piece of 16 bytes is read, and written, by one thread.  `per_row` threads (a power of two up to 256) share a row,
-// or, for longer rows, a workgroup has 1024 pieces of one.  x - lse = log p, so with c = g_logp + g_entropy (log p + entropy) every
+// or, for longer rows, a workgroup has 1024 pieces of one (`from`: such runs ahead of this launch's first).  x - lse = log p, so with c = g_logp + g_entropy (log p + entropy) every
 // element is -p c, and the target's g_logp more.
 template <int DT>
-__global__ __launch_bounds__(256) void logprob_bwd_rows(LogprobArgs a, int per_row)
+__global__ __launch_bounds__(256) void logprob_bwd_rows(LogprobArgs a, int per_row, int from)
 {
     typedef typename Prec<DT>::elem_t elem_t;
     typedef Piece<DT> P;
     constexpr int VEC = P::VEC, U = 4;
     const int rows_here = 256 / per_row, l = threadIdx.x & (per_row - 1);
-    const int pieces = (a.cols + VEC - 1) / VEC, first = blockIdx.y * (per_row * U);
+    const int pieces = (a.cols + VEC - 1) / VEC, first = (from + (int)blockIdx.y) * (per_row * U);
     for (int64_t row = (int64_t)blockIdx.x * rows_here + threadIdx.x / per_row; row < a.rows; row += (int64_t)gridDim.x * rows_here) {
         const elem_t* x = (const elem_t*)a.x + row * a.ldx;
         elem_t* dx = (elem_t*)a.dx + row * a.ldg;
@@ -621,8 +621,12 @@ static hipError_t bwd(const LogprobArgs& a, hipStream_t s)
     int per_row = 4;  // threads a row: four pieces a thread, up to a workgroup
     while (per_row < 256 && per_row * 4 < pieces) per_row *= 2;
     const int64_t blocks = (a.rows + 256 / per_row - 1) / (256 / per_row);
-    const dim3 grid((unsigned)std::min<int64_t>(blocks, 1 << 20), (unsigned)((pieces + per_row * 4 - 1) / (per_row * 4)));
-    hipLaunchKernelGGL((logprob_bwd_rows<DT>), grid, dim3(256), 0, s, a, per_row);
+    const int runs = (pieces + per_row * 4 - 1) / (per_row * 4);
+    // gridDim.y is at most 65535: rows of more than 65535 x 1024 pieces (fp32 from 268 million columns) take several launches
+    for (int from = 0; from < runs; from += 65535) {
+        const dim3 grid((unsigned)std::min<int64_t>(blocks, 1 << 20), (unsigned)std::min(runs - from, 65535));
+        hipLaunchKernelGGL((logprob_bwd_rows<DT>), grid, dim3(256), 0, s, a, per_row, from);
+    }
     return hipGetLastError();
 }
 

@@ -300,3 +300,30 @@ def test_more_rows_than_workgroups():
     want = -torch.exp(x.double() - o[1].double()[:, None])
     want.scatter_add_(1, t[:, None], torch.ones(rows, 1, dtype=torch.float64, device="cuda"))
     assert torch.allclose(dx.double(), want, atol=1e-5)
+
+
+def test_gradient_of_a_row_of_more_columns_than_a_launch_holds():
+    """A launch has 65535 runs of 1024 pieces of a row; the gradient of a longer one, against the formula in 64 bits by slices."""
+    torch = torch_mod()
+    cols = 65535 * 1024 * 4 + 4099
+    g = torch.Generator(device="cuda")
+    g.manual_seed(5)
+    x = torch.randn(1, cols, generator=g, device="cuda")
+    lse, target = torch.logsumexp(x.double(), 1).float(), torch.tensor([cols - 3], device="cuda")
+    entropy, gl, gh = torch.full((1,), 3.0, device="cuda"), torch.full((1,), -1.5, device="cuda"), torch.full((1,), 0.5, device="cuda")
+    dx = torch.full_like(x, float("nan"))
+    B.logprob_bwd(B.make_logprob_desc(1, cols), x, target, lse, entropy, gl, gh, dx)
+    ends = sorted({0, 1 << 20, cols // 2, 65535 * 1024 * 4 - 1024, cols - 4099 - 5000, cols - 4099, cols - 1500, cols})
+    assert bool(torch.isfinite(dx).all())
+    for j0, j1 in zip(ends, ends[1:]):
+        j1 = min(j1, j0 + (1 << 24))
+        lp = x[0, j0:j1].double() - lse.double()
+        p = torch.exp(lp)
+        want = -p * (-1.5 + 0.5 * (lp + 3.0))
+        if j0 <= cols - 3 < j1:
+            want[cols - 3 - j0] += -1.5
+        # |lp| below 32, in units of 2^-24: x - lse is off by 16, its product with log2 e by 22 and by 7 for the constant, which the
+        # exponential passes on, with two of its own; the factor and the products by a few
+        size = p * (1.5 + 0.5 * (lp.abs() + 3.0))
+        off = (dx[0, j0:j1].double() - want).abs()
+        assert bool((off <= 2.0 ** -24 * (64 * size + 2 * want.abs() + 4 * (want.abs() > 1))).all()), (j0, j1)
