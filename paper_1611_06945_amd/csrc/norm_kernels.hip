@@ -415,12 +415,12 @@ __global__ __launch_bounds__(NT) void norm_bwd_rows(NormArgs a)
 
 // The sums of `parts` workgroups: C columns and 1024 / C groups of lanes a workgroup, a group every so many parts, then the groups in order.
 template <int C>
-__global__ __launch_bounds__(1024) void norm_dw_join(NormArgs a, int parts)
+__global__ __launch_bounds__(1024) void norm_dw_join(NormArgs a, int parts, int64_t from)
 {
     constexpr int GROUPS = 1024 / C;
     __shared__ float red[GROUPS][C];
     const int l = threadIdx.x % C, group = threadIdx.x / C;
-    const int64_t j = (int64_t)blockIdx.x * C + l;  // dgamma's columns, then dbeta's
+    const int64_t j = from + (int64_t)blockIdx.x * C + l;  // dgamma's columns, then dbeta's
     float s = 0.0f;
     if (j < 2 * (int64_t)a.cols) {
         int p = group;
@@ -658,11 +658,17 @@ void bwd_pieces(const NormArgs& a, int nv, int parts, hipStream_t s)
 }
 
 // 64 columns a workgroup where that makes a workgroup a CU, else 16: 423 sums of 2 x 384 columns took 4.7 us with 64.
+// A launch holds less than 2^32 threads, 16 a column here: rows of more than 2^25 columns take several.
 void join(const NormArgs& a, int parts, hipStream_t s)
 {
+    constexpr int64_t PORTION = (int64_t)1 << 26;
     const int64_t cols = 2 * (int64_t)a.cols;
-    if (cols >= 64 * kCUs) hipLaunchKernelGGL((norm_dw_join<64>), dim3((unsigned)((cols + 63) / 64)), dim3(1024), 0, s, a, parts);
-    else hipLaunchKernelGGL((norm_dw_join<16>), dim3((unsigned)((cols + 15) / 16)), dim3(1024), 0, s, a, parts);
+    if (cols < 64 * kCUs) {
+        hipLaunchKernelGGL((norm_dw_join<16>), dim3((unsigned)((cols + 15) / 16)), dim3(1024), 0, s, a, parts, 0);
+        return;
+    }
+    for (int64_t from = 0; from < cols; from += PORTION)
+        hipLaunchKernelGGL((norm_dw_join<64>), dim3((unsigned)((std::min(cols - from, PORTION) + 63) / 64)), dim3(1024), 0, s, a, parts, from);
 }
 
 template <int DT>

@@ -349,3 +349,21 @@ def test_offsets_beyond_32_bits():
         B.layernorm_bwd(desc, x, d, gamma, mean, rstd, o, dg, db, ws, ws.numel())
         res.append((o[:, :cols].clone(), dg, db))
     assert all(torch.equal(a, b) for a, b in zip(*res))
+
+
+def test_gradients_of_a_row_of_more_columns_than_a_launch_joins():
+    """2^27 columns: 16 threads for each of twice as many sums would be 2^32.  One row, so every sum is one product."""
+    torch = torch_mod()
+    cols = (1 << 27) + 70
+    g = torch.Generator(device="cuda")
+    g.manual_seed(2)
+    x, dy = (torch.randn(1, cols, generator=g, device="cuda").half() for _ in range(2))
+    mean, rstd = torch.full((1,), 0.25, device="cuda"), torch.full((1,), 1.5, device="cuda")
+    d = B.make_norm_desc(1, cols, wl.F16, EPS)
+    ws = torch.empty(B.layernorm_bwd_workspace_bytes(d), dtype=torch.uint8, device="cuda")
+    dgamma, dbeta = nan_vec(cols), nan_vec(cols)
+    B.layernorm_bwd(d, x, dy, None, mean, rstd, None, dgamma, dbeta, ws, ws.numel())
+    assert torch.equal(dbeta, dy[0].float())
+    # fp16 less a quarter has 24 bits at most, times 1.5 a rounding, times dy another
+    want = dy[0].double() * ((x[0].double() - 0.25) * 1.5)
+    assert bool(((dgamma.double() - want).abs() <= 4 * EPS32 * want.abs()).all())
