@@ -343,7 +343,8 @@ int conv_probe_stream_bandwidth(const void* src, void* dst, size_t bytes, void* 
  *     statistics, log probabilities and their gradients) are fp32, dense.  Sums and statistics are fp32 or int32.
  *   - Float tensors have to be aligned to their element only and row strides are free (>= the row's length), so a slice
  *     of a larger tensor can be passed; 8-bit tensors start on 16 bytes and have row strides divisible by 16.
- *   - rows = 0 is valid and enqueues nothing (layernorm_bwd still writes its zero sums).  rows < 2^31.
+ *   - rows = 0 is valid and enqueues nothing (layernorm_bwd still writes its zero sums).  rows < 2^31; a tensor spans at most 2^62
+ *     bytes (row stride times rows), CONV_EINVAL beyond.
  *   - Outputs alias no input, except where said.
  *   - Results do not depend on scheduling (no floating-point atomics): the same call gives the same bits.
  */
@@ -353,7 +354,7 @@ int conv_probe_stream_bandwidth(const void* src, void* dst, size_t bytes, void* 
  * rstd_t = 1 / sqrt(var_t + eps) with the variance taken around that mean (in a second pass over the held row).
  * gamma NULL = ones, beta NULL = zeros; mean and rstd (fp32 [rows], what layernorm_bwd needs) may be NULL.
  * ldx is the row stride of x and dx, ldy that of y and dy.  CONV_EINVAL for rows < 0, cols < 1 or >= 2^30, a stride
- * below cols, eps < 0 or NaN, NULL or misaligned pointers.
+ * below cols, eps < 0, infinite or NaN, NULL or misaligned pointers.
  */
 typedef struct {
     int64_t rows;
@@ -383,7 +384,7 @@ int layernorm_bwd(const norm_desc* desc, const void* x, const void* dy, const fl
  * rounded to the nearest whole number (ties to even), so that q * scale stands for x and |q| <= 127.  A row that holds a
  * NaN or an infinity gets the scale NaN and zeros: what is computed from it is NaN.  q has the row stride ldq
  * (divisible by 16, >= cols); the bytes from cols up to the next multiple of 16 are written as zeros, those beyond are left.
- * Weights [N][K] are quantised by the same call, a scale for each output channel.
+ * 1 <= cols < 2^30.  Weights [N][K] are quantised by the same call, a scale for each output channel.
  */
 typedef struct {
     int64_t rows;

@@ -1,5 +1,6 @@
 // C entry points of the operators on rows: layer norm, row quantiser, 8-bit product, log probabilities.  Arguments are
 // checked before the first HIP call; the kernels' launchers choose among their forms.
+#include <algorithm>
 #include <climits>
 #include <cmath>
 
@@ -14,14 +15,16 @@ bool aligned(const void* p, uintptr_t to) { return ((uintptr_t)p & (to - 1)) == 
 // a float vector: NULL allowed
 bool vec_ok(const void* p) { return aligned(p, 4); }
 constexpr int64_t kMostRows = INT32_MAX;
-constexpr int64_t kMostStride = (int64_t)1 << 40;  // rows * stride * 4 bytes stays below 2^63 ... and beyond any memory
+// A tensor spans at most 2^62 bytes, so that no offset in it, in elements or bytes, passes 63 bits.
+bool spans(int64_t rows, int64_t stride, int size) { return stride <= ((int64_t)1 << 62) / size / std::max<int64_t>(rows, 1); }
 
 int check_norm(const norm_desc* d)
 {
     if (!d) return CONV_EINVAL;
     if (!known(d->dtype)) return CONV_EDTYPE;
     if (d->rows < 0 || d->rows > kMostRows || d->cols < 1 || d->cols >= (1 << 30)) return CONV_EINVAL;
-    if (d->ldx < d->cols || d->ldy < d->cols || d->ldx > kMostStride / 2048 || d->ldy > kMostStride / 2048) return CONV_EINVAL;
+    const int es = dtype_size(d->dtype);
+    if (d->ldx < d->cols || d->ldy < d->cols || !spans(d->rows, d->ldx, es) || !spans(d->rows, d->ldy, es)) return CONV_EINVAL;
     if (!(d->eps >= 0.0f) || std::isinf(d->eps)) return CONV_EINVAL;
     return CONV_OK;
 }
@@ -30,8 +33,9 @@ int check_logprob(const logprob_desc* d)
 {
     if (!d) return CONV_EINVAL;
     if (!known(d->dtype)) return CONV_EDTYPE;
-    if (d->rows < 0 || d->rows > kMostRows || d->cols < 1 || d->cols >= INT32_MAX - (1 << 20)) return CONV_EINVAL;
-    if (d->ldx < d->cols || d->ldg < d->cols || d->ldx > kMostStride / 256 || d->ldg > kMostStride / 256) return CONV_EINVAL;
+    if (d->rows < 0 || d->rows > kMostRows || d->cols < 1 || d->cols > INT32_MAX - (1 << 20)) return CONV_EINVAL;
+    const int es = dtype_size(d->dtype);
+    if (d->ldx < d->cols || d->ldg < d->cols || !spans(d->rows, d->ldx, es) || !spans(d->rows, d->ldg, es)) return CONV_EINVAL;
     if (d->top < 0 || d->top > 64 || d->top > d->cols) return CONV_EINVAL;
     return CONV_OK;
 }
@@ -43,7 +47,7 @@ int check_int_linear(const int_linear_desc* d)
     if (d->rows < 0 || d->rows > kMostRows || d->N < 1 || d->K < 1 || d->K >= (1 << 17)) return CONV_EINVAL;
     if (d->N >= (1 << 24)) return CONV_EINVAL;  // tiles of one band of rows fit a launch
     if (d->lda < d->K || d->ldw < d->K || d->ldo < d->N || d->lda % 16 || d->ldw % 16) return CONV_EINVAL;
-    if (d->lda > kMostStride / 256 || d->ldw > kMostStride / 256 || d->ldo > kMostStride / 256) return CONV_EINVAL;
+    if (!spans(d->rows, d->lda, 1) || !spans(d->N, d->ldw, 1) || !spans(d->rows, d->ldo, dtype_size(d->dtype))) return CONV_EINVAL;
     if (d->flags & ~(uint32_t)CONV_FLAG_RELU) return CONV_EINVAL;
     return CONV_OK;
 }
@@ -130,7 +134,7 @@ int quantize_rows(const quant_desc* desc, const void* x, int8_t* q, float* scale
     if (!known(desc->dtype)) return CONV_EDTYPE;
     if (desc->rows < 0 || desc->rows > kMostRows || desc->cols < 1 || desc->cols >= (1 << 30)) return CONV_EINVAL;
     if (desc->ldx < desc->cols || desc->ldq < desc->cols || desc->ldq % 16) return CONV_EINVAL;
-    if (desc->ldx > kMostStride / 256 || desc->ldq > kMostStride / 256) return CONV_EINVAL;
+    if (!spans(desc->rows, desc->ldx, dtype_size(desc->dtype)) || !spans(desc->rows, desc->ldq, 1)) return CONV_EINVAL;
     if (desc->rows == 0) return CONV_OK;
     if (!x || !q || !scale || (const void*)q == x || !aligned(x, dtype_size(desc->dtype)) || !aligned(q, 16) || !vec_ok(scale)) return CONV_EINVAL;
     QuantArgs a = {x, q, scale, desc->rows, desc->ldx, desc->ldq, desc->cols};

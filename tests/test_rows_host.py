@@ -225,3 +225,41 @@ def test_oracle_logprob_closed_forms_and_differences():
             e = np.zeros_like(x)
             e[i, j] = h
             assert abs((loss(x + e) - loss(x - e)) / (2 * h) - dx[i, j]) < 1e-7
+
+
+def accepted(call, desc, nulls, **kw):
+    """Whether an empty call with this descriptor is valid: the descriptor's checks come first."""
+    return status(call, desc, *[None] * nulls, stream=0, **kw) == B.CONV_OK
+
+
+def test_columns_and_strides_are_accepted_up_to_the_stated_limits():
+    for ok, cols in ((True, (1 << 30) - 1), (False, 1 << 30)):
+        for extra in (0, 1, 1 << 33):  # whatever the strides
+            ld = (cols + 15) // 16 * 16 + 16 * extra
+            assert accepted(B.layernorm_fwd, B.make_norm_desc(0, cols, ldx=ld, ldy=ld), 4) == ok, (cols, extra)
+            assert accepted(B.layernorm_quant_fwd, B.make_norm_desc(0, cols, ldx=ld, ldy=ld), 5) == ok, (cols, extra)
+            assert accepted(B.quantize_rows, B.make_quant_desc(0, cols, ldx=ld, ldq=ld), 3) == ok, (cols, extra)
+            assert (B.layernorm_bwd_workspace_bytes(B.make_norm_desc(40, cols, ldx=ld, ldy=ld)) > 0) == ok, (cols, extra)
+    for ok, cols in ((True, (1 << 31) - (1 << 20) - 1), (False, (1 << 31) - (1 << 20))):
+        for ld in (cols, cols + 1, 1 << 33):
+            assert accepted(B.logprob_fwd, B.make_logprob_desc(0, cols, ldx=ld, ldg=ld), 3) == ok, (cols, ld)
+    assert accepted(B.int_linear_fwd, B.make_int_linear_desc(0, (1 << 24) - 1, (1 << 17) - 1, lda=1 << 33, ldw=1 << 33, ldo=1 << 33), 6)
+
+
+@pytest.mark.parametrize("dtype,es", [(B.CONV_F32, 4), (B.CONV_BF16, 2)])
+def test_tensors_whose_offsets_would_overflow_are_refused(dtype, es):
+    """A tensor spans at most 2^62 bytes."""
+    rows = (1 << 31) - 1
+    ld = (1 << 62) // es // rows // 16 * 16
+    assert B.layernorm_bwd_workspace_bytes(B.make_norm_desc(rows, 8, dtype, ldx=ld, ldy=ld)) > 0
+    assert B.layernorm_bwd_workspace_bytes(B.make_norm_desc(rows, 8, dtype, ldx=ld + 16, ldy=8)) == 0
+    assert B.layernorm_bwd_workspace_bytes(B.make_norm_desc(rows, 8, dtype, ldx=8, ldy=ld + 16)) == 0
+    assert B.logprob_workspace_bytes(B.make_logprob_desc(1, 1 << 20, dtype, ldx=1 << 40, ldg=1 << 40)) > 0
+    assert B.logprob_workspace_bytes(B.make_logprob_desc(2, 1 << 20, dtype, ldx=(1 << 61) // es + 1)) == 0
+    assert B.logprob_workspace_bytes(B.make_logprob_desc(2, 1 << 20, dtype, ldg=(1 << 61) // es + 1)) == 0
+    few = dict(rows=4, N=10, K=1 << 16, dtype=dtype)
+    assert B.int_linear_workspace_bytes(B.make_int_linear_desc(**few, lda=1 << 40, ldw=1 << 40, ldo=1 << 40)) > 0
+    for k, n in (("lda", 4), ("ldw", 10), ("ldo", 4 * es)):
+        assert B.int_linear_workspace_bytes(B.make_int_linear_desc(**few, **{k: (1 << 62) // n // 16 * 16 + 16})) == 0
+    for strides in (dict(ldx=ld + 16), dict(ldq=(1 << 62) // rows // 16 * 16 + 16)):
+        assert status(B.quantize_rows, B.make_quant_desc(rows, 8, dtype, **strides), P, 2 * P, P, stream=0) == B.CONV_EINVAL
