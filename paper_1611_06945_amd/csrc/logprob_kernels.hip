@@ -535,7 +535,7 @@ __global__ __launch_bounds__(256) void logprob_bwd_rows(LogprobArgs a, int per_r
 #pragma unroll
             for (int k = 0; k < VEC; ++k) {
                 const float lp = f[k] - lse, p = exp_of(lp);
-                f[k] = -p * __builtin_fmaf(gh, fmaxf(lp, -1e20f) + h, g);  // -inf: p is 0
+                f[k] = -p * __builtin_fmaf(gh, fmaxf(lp, -128.0f) + h, g);  // where p is 0, -inf and all below -88, the factor stays finite
             }
             if (t >= j && t < j + VEC) {
 #pragma unroll

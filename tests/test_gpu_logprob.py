@@ -327,3 +327,30 @@ def test_gradient_of_a_row_of_more_columns_than_a_launch_holds():
         size = p * (1.5 + 0.5 * (lp.abs() + 3.0))
         off = (dx[0, j0:j1].double() - want).abs()
         assert bool((off <= 2.0 ** -24 * (64 * size + 2 * want.abs() + 4 * (want.abs() > 1))).all()), (j0, j1)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("gh", [1e19, -1e25, 1e36])
+def test_gradient_of_masked_columns_is_zero_however_large_that_of_the_entropy(dtype, gh):
+    """p log p is 0 where p is 0; with a scaled loss the factor of p there must not overflow."""
+    torch = torch_mod()
+    rng = np.random.default_rng(3)
+    x = stored(rng.normal(size=(3, 77)), dtype)
+    x[:, 5::7] = -np.inf
+    x[1, 6::7] = stored(np.array([-6e4]), dtype)[0]
+    x[2, :] = -np.inf
+    x[2, 9] = 0.0
+    lse, h = (ro.logprob(x, None, 0)[k] for k in ("lse", "entropy"))
+    X = Rows(3, 77, torch_type(dtype)).set(x)
+    out = torch.full((3, 77), float("nan"), device="cuda", dtype=torch_type(dtype))
+    B.logprob_bwd(B.make_logprob_desc(3, 77, dtype), X.ptr, None, vec(lse), vec(h), None, vec(np.full(3, gh)), out)
+    got = out.double().cpu().numpy()
+    p = np.exp(x - lse[:, None])
+    assert (got[p == 0] == 0).all()
+    assert not np.isnan(got).any()
+    if dtype == wl.F32:
+        # (the entropy as rounded to fp32: off by 2^-24 of itself)
+        h32, l32 = h.astype(np.float32).astype(np.float64), lse.astype(np.float32).astype(np.float64)
+        want = ro.logprob_bwd(x, None, l32, h32, None, np.full(3, gh))
+        lp = np.where(p > 0, x - l32[:, None], 0.0)
+        assert (np.abs(got - want) <= EPS32 * 16 * (1 + np.abs(lp)) * abs(gh) * p * (np.abs(lp) + h32[:, None] + 1)).all()
