@@ -169,6 +169,31 @@ def test_descriptor_sizes_match_the_header():
     assert ctypes.sizeof(B.int_linear_desc) == 48 and ctypes.sizeof(B.logprob_desc) == 40
 
 
+class Buffer:
+    """What another library's array looks like to the binding."""
+
+    def __init__(self, address):
+        self.address = address
+
+    def data_ptr(self):
+        if isinstance(self.address, Exception):
+            raise self.address
+        return self.address
+
+
+def test_addresses_of_other_kinds_of_whole_numbers():
+    d = B.make_norm_desc(4, 8)
+    for address in (P, np.int64(P), np.uint64(P)):
+        assert status(B.layernorm_fwd, d, Buffer(address), None, None, Buffer(address), stream=0) == B.CONV_EINVAL  # in place
+    with pytest.raises(TypeError):
+        B.layernorm_fwd(d, Buffer(None), None, None, Buffer(P), stream=0)
+    with pytest.raises(AttributeError, match="gone"):
+        B.layernorm_fwd(d, Buffer(AttributeError("gone")), None, None, Buffer(P), stream=0)
+    for other in ("x", 1.5, np.zeros(3)):
+        with pytest.raises(TypeError, match="expected a torch tensor"):
+            B.layernorm_fwd(d, other, None, None, Buffer(P), stream=0)
+
+
 # ---- the oracle ------------------------------------------------------------------------------------------------------
 
 
