@@ -418,6 +418,9 @@ size_t int_linear_workspace_bytes(const int_linear_desc* desc);
 int int_linear_fwd(const int_linear_desc* desc, const int8_t* a, const float* a_scale, const int8_t* w,
                    const float* w_scale, const float* bias, void* out, void* workspace, size_t workspace_bytes,
                    void* stream);
+/* Name of the form that int_linear_fwd takes for this descriptor and these operands' addresses (which count modulo 128; NULL counts
+ * as a multiple), NUL-terminated in buf[0..n), e.g. "rows32_split3" or "tile64x128_lines"; empty for no rows.  Pure host code. */
+int int_linear_form(const int_linear_desc* desc, const int8_t* a, const int8_t* w, char* buf, size_t n);
 
 /*
  * Log probabilities of given tokens under softmax over the columns (classes, a vocabulary), with lse_t = log sum_j exp(x_tj):

@@ -159,6 +159,8 @@ def lib() -> ctypes.CDLL:
         L.quantize_rows.restype = ctypes.c_int
         L.int_linear_workspace_bytes.argtypes = [ip]
         L.int_linear_workspace_bytes.restype = sz
+        L.int_linear_form.argtypes = [ip, vp, vp, ctypes.c_char_p, sz]
+        L.int_linear_form.restype = ctypes.c_int
         L.int_linear_fwd.argtypes = [ip] + [vp] * 7 + [sz, vp]
         L.int_linear_fwd.restype = ctypes.c_int
         L.logprob_workspace_bytes.argtypes = [gp]
@@ -431,6 +433,13 @@ def quantize_rows(desc, x, q, scale, stream=None) -> None:
 
 def int_linear_workspace_bytes(desc) -> int:
     return int(lib().int_linear_workspace_bytes(ctypes.byref(desc)))
+
+
+def int_linear_form(desc, a=None, w=None) -> str:
+    """Name of the form that int_linear_fwd takes for these sizes, strides and addresses."""
+    buf = ctypes.create_string_buffer(64)
+    _check(lib().int_linear_form(ctypes.byref(desc), _ptr(a), _ptr(w), buf, len(buf)), "int_linear_form")
+    return buf.value.decode()
 
 
 def int_linear_fwd(desc, a, a_scale, w, w_scale, bias, out, workspace=None, workspace_bytes=0, stream=None) -> None:

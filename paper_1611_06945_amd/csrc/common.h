@@ -277,6 +277,7 @@ struct IntLinearArgs {
 };
 hipError_t launch_int_linear(IntLinearArgs& a, int dtype, hipStream_t s);
 size_t int_linear_workspace(int64_t rows, int N, int K);
+int int_linear_form_name(const IntLinearArgs& a, char* buf, size_t n);  // as snprintf
 
 struct LogprobArgs {
     const void* x;

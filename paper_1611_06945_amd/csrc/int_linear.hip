@@ -1,6 +1,7 @@
 // Matrix product in 8-bit integers with scales for each row and output channel.
 #include <algorithm>
 #include <cmath>
+#include <cstdio>
 #include <type_traits>
 
 #include "rows_common.h"
@@ -549,28 +550,50 @@ hipError_t launch_rows(const IntLinearArgs& g, int splits, hipStream_t s)
 // The tiles' offsets are 32 bits; longer strides go to int_linear_any.
 bool long_strides(int64_t lda, int64_t ldw) { return std::max(lda, ldw) >= (1 << 23); }
 
-template <int DT>
-hipError_t launch(IntLinearArgs& g, hipStream_t s)
+// The form of a call.
+enum FormId { ANY, ROWS16, ROWS32, ROWS64, T64X64, T64X128, T128X128, PAIR128X128, T256X256 };
+struct IntForm {
+    FormId id;
+    int splits;  // of the few-row forms
+    bool late;   // of the first three tiles
+};
+IntForm form_of(const IntLinearArgs& g)
 {
-    if (long_strides(g.lda, g.ldw))
-        return in_portions<DT>(g, 16, [&](const IntLinearArgs& p, unsigned y) {
-            hipLaunchKernelGGL((int_linear_any<DT>), dim3((unsigned)((g.N + 63) / 64), y), dim3(256), 0, s, p);
-            return hipGetLastError();
-        });
+    if (long_strides(g.lda, g.ldw)) return {ANY, 1, false};
     const RowsPlan rows = rows_plan(g.rows, g.N, g.K);
-    if (rows.rb == 1) return launch_rows<DT, 1>(g, rows.splits, s);
+    const IntForm few = {rows.rb == 1 ? ROWS16 : rows.rb == 2 ? ROWS32 : ROWS64, rows.splits, false};
+    if (rows.rb == 1) return few;
     const bool late = (g.lda | g.ldw | (int64_t)(uintptr_t)g.a | (int64_t)(uintptr_t)g.w) % 128 != 0;
     const bool alone = (g.rows + 127) / 128 * ((g.N + 127) / 128) <= 256;
     const double us[] = {rows.us, tiles_us<Tile64x64<false>>(g, 2.0, 1.2, 0.2), tiles_us<Tile64x128<false>>(g, 1.5, 2.8, 0.33),
                          alone ? tiles_us<Tile128x128<false>>(g, 0, 4.2, 0.49) : tiles_us<Pair128x128>(g, 1.8, 1.5, 0.52),
                          tiles_us<Tile256x256>(g, 0, 11, 1.4)};
     switch ((int)(std::min_element(us, us + 5) - us)) {
-        case 0: return rows.rb == 2 ? launch_rows<DT, 2>(g, rows.splits, s) : launch_rows<DT, 4>(g, rows.splits, s);
-        case 1: return late ? launch_tiles<DT, Tile64x64<true>>(g, s) : launch_tiles<DT, Tile64x64<false>>(g, s);
-        case 2: return late ? launch_tiles<DT, Tile64x128<true>>(g, s) : launch_tiles<DT, Tile64x128<false>>(g, s);
-        case 3:
-            if (!alone) return launch_tiles<DT, Pair128x128>(g, s);
-            return late ? launch_tiles<DT, Tile128x128<true>>(g, s) : launch_tiles<DT, Tile128x128<false>>(g, s);
+        case 0: return few;
+        case 1: return {T64X64, 1, late};
+        case 2: return {T64X128, 1, late};
+        case 3: return alone ? IntForm{T128X128, 1, late} : IntForm{PAIR128X128, 1, false};
+        default: return {T256X256, 1, false};
+    }
+}
+
+template <int DT>
+hipError_t launch(IntLinearArgs& g, hipStream_t s)
+{
+    const IntForm f = form_of(g);
+    switch (f.id) {
+        case ANY:
+            return in_portions<DT>(g, 16, [&](const IntLinearArgs& p, unsigned y) {
+                hipLaunchKernelGGL((int_linear_any<DT>), dim3((unsigned)((g.N + 63) / 64), y), dim3(256), 0, s, p);
+                return hipGetLastError();
+            });
+        case ROWS16: return launch_rows<DT, 1>(g, f.splits, s);
+        case ROWS32: return launch_rows<DT, 2>(g, f.splits, s);
+        case ROWS64: return launch_rows<DT, 4>(g, f.splits, s);
+        case T64X64: return f.late ? launch_tiles<DT, Tile64x64<true>>(g, s) : launch_tiles<DT, Tile64x64<false>>(g, s);
+        case T64X128: return f.late ? launch_tiles<DT, Tile64x128<true>>(g, s) : launch_tiles<DT, Tile64x128<false>>(g, s);
+        case T128X128: return f.late ? launch_tiles<DT, Tile128x128<true>>(g, s) : launch_tiles<DT, Tile128x128<false>>(g, s);
+        case PAIR128X128: return launch_tiles<DT, Pair128x128>(g, s);
         default: return launch_tiles<DT, Tile256x256>(g, s);
     }
 }
@@ -583,6 +606,14 @@ size_t int_linear_workspace(int64_t rows, int N, int K)
     if (rows == 0) return 0;
     const RowsPlan p = rows_plan(rows, N, K);
     return p.splits > 1 ? (size_t)p.splits * rows * N * 4 : 0;
+}
+
+int int_linear_form_name(const IntLinearArgs& g, char* buf, size_t n)
+{
+    static const char* const names[] = {"any", "rows16", "rows32", "rows64", "tile64x64", "tile64x128", "tile128x128", "tile128x128_two_a_cu", "tile256x256"};
+    const IntForm f = form_of(g);
+    if (f.splits > 1) return std::snprintf(buf, n, "%s_split%d", names[f.id], f.splits);
+    return std::snprintf(buf, n, "%s%s", names[f.id], f.late ? "_lines" : "");
 }
 
 hipError_t launch_int_linear(IntLinearArgs& g, int dtype, hipStream_t s)

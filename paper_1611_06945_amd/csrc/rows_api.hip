@@ -146,6 +146,19 @@ size_t int_linear_workspace_bytes(const int_linear_desc* desc)
     return check_int_linear(desc) ? 0 : int_linear_workspace(desc->rows, desc->N, desc->K);
 }
 
+int int_linear_form(const int_linear_desc* desc, const int8_t* a, const int8_t* w, char* buf, size_t n)
+{
+    const int rc = check_int_linear(desc);
+    if (rc) return rc;
+    if (!buf || n == 0 || !aligned(a, 16) || !aligned(w, 16)) return CONV_EINVAL;
+    buf[0] = 0;
+    if (desc->rows == 0) return CONV_OK;
+    IntLinearArgs g = {};
+    g.a = a, g.w = w, g.rows = desc->rows, g.lda = desc->lda, g.ldw = desc->ldw, g.ldo = desc->ldo, g.N = desc->N, g.K = desc->K;
+    int_linear_form_name(g, buf, n);
+    return CONV_OK;
+}
+
 int int_linear_fwd(const int_linear_desc* desc, const int8_t* a, const float* a_scale, const int8_t* w, const float* w_scale,
                    const float* bias, void* out, void* workspace, size_t workspace_bytes, void* stream)
 {

@@ -171,3 +171,63 @@ def test_products_of_every_form(rows, N, K, dtype):
     B.int_linear_fwd(d, A, sa, W, sw, None, out, ws, need)
     want = (A[:, :K].double() @ W[:, :K].double().t().contiguous()) * sa.double()[:, None] * sw.double()[None, :]
     assert bool((out.double() == want.to(out.dtype).double()).all())
+
+
+def exact_product(rows, N, K, dtype, lda, ldw, ldo, start=0, relu=False, a_start=0, splits=None):
+    """Whole-number scales and biases and codes small enough that every sum is a whole number below 2^24: bit for bit, whatever the
+    form, with what lies around the output untouched.  Returns the form's name."""
+    torch = torch_mod()
+    g = torch.Generator(device="cuda")
+    g.manual_seed(rows + N + K)
+    lim = 50 if dtype == wl.F32 else 1
+    assert lim * lim * K ** 0.5 * 4 * 8 < 1 << 24  # eight standard deviations and more
+
+    def codes(n, ld, start):
+        flat = torch.empty(start + n * ld, dtype=torch.int8, device="cuda")
+        view = flat[start:].view(n, ld)
+        view[:, :B.row_stride(K)] = torch.randint(-128, 128, (n, B.row_stride(K)), generator=g, device="cuda", dtype=torch.int8)
+        view[:, :K] = torch.randint(-lim, lim + 1, (n, K), generator=g, device="cuda", dtype=torch.int8)
+        return view
+
+    A, W = codes(rows, lda, a_start), codes(N, ldw, 0)
+    sa, sw = (torch.randint(1, 3, (n,), generator=g, device="cuda").float() for n in (rows, N))
+    bias = torch.randint(-9, 10, (N,), generator=g, device="cuda").float()
+    Y = Rows(rows, N, torch_type(dtype), ldo, start, fill=7.0)
+    d = B.make_int_linear_desc(rows, N, K, dtype, relu, lda, ldw, ldo)
+    need = B.int_linear_workspace_bytes(d)
+    ws = torch.full((max(need, 16),), 0xFF, dtype=torch.uint8, device="cuda")
+    B.int_linear_fwd(d, A, sa, W, sw, bias, Y.ptr, ws, need)
+    want = (A[:, :K].double() @ W[:, :K].double().t().contiguous()) * sa.double()[:, None] * sw.double()[None, :] + bias.double()
+    want = torch.relu(want) if relu else want
+    assert torch.equal(Y.view.double(), want.to(Y.view.dtype).double())
+    assert Y.untouched()
+    return B.int_linear_form(d, A, W)
+
+
+# rows, channels, reduction, strides of the codes past the next 16 bytes, the form that takes them
+FORMS = [(9, 300, 700, 0, "rows16"), (3, 20, 30000, 16, "rows16_split16"), (20, 1000, 4096, 0, "rows32"), (30, 100, 20000, 48, "rows32_split16"),
+         (60, 500, 2000, 16, "rows64"), (130, 257, 16000, 0, "rows64_split5"), (260, 1500, 512, 0, "tile64x64"), (600, 900, 300, 16, "tile64x64_lines"),
+         (900, 1300, 1024, 0, "tile64x128"), (900, 1300, 1000, 16, "tile64x128_lines"), (1500, 1500, 256, 0, "tile128x128"), (1500, 1500, 260, 80, "tile128x128_lines"),
+         (2100, 4000, 1024, 0, "tile128x128_two_a_cu"), (2100, 4001, 1000, 16, "tile128x128_two_a_cu"), (4000, 4000, 2048, 0, "tile256x256"),
+         (4001, 4003, 2000, 32, "tile256x256"), (5, 70, 100, (1 << 23) - 112, "any")]
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("odd", [False, True])
+@pytest.mark.parametrize("rows,N,K,pad,form", FORMS)
+def test_each_form_with_each_way_out(rows, N, K, pad, form, odd, dtype):
+    """Every form, in every output type, with rows of outputs that begin on words and with rows that do not."""
+    ldo = N + (N % 2 == 0) if odd else (N + 8) // 8 * 8
+    assert exact_product(rows, N, K, dtype, B.row_stride(K) + pad, B.row_stride(K) + 2 * pad if form != "any" else B.row_stride(K), ldo, int(odd), relu=odd) == form
+
+
+@pytest.mark.parametrize("rows,N,K,less,form", [(64, 64, 100, 16, "rows64"), (257, 700, 100, 16, "tile64x64_lines"), (257, 700, 100, 128, "tile64x64"),
+                                                (700, 1500, 100, 16, "tile64x128_lines"), (1500, 1500, 100, 16, "tile128x128_lines"),
+                                                (1500, 1500, 100, 128, "tile128x128"), (1500, 3000, 100, 48, "tile128x128_two_a_cu"), (3000, 3000, 4000, 16, "tile256x256")])
+def test_tiles_of_the_longest_strides(rows, N, K, less, form):
+    """Row strides just below the 2^23 from which on another kernel takes the product: the largest offsets within a tile."""
+    torch = torch_mod()
+    ld = (1 << 23) - less
+    assert torch.cuda.mem_get_info()[0] > (rows + N) * ld + (8 << 30)
+    assert exact_product(rows, N, K, wl.F32, ld, ld, N) == form
+    torch.cuda.empty_cache()

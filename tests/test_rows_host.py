@@ -117,6 +117,22 @@ def test_int_linear_pointers_that_are_refused():
     assert B.lib().int_linear_fwd(None, P, P, P, P, P, P, None, 0, None) == B.CONV_EINVAL
 
 
+def test_int_linear_form_by_name():
+    form = lambda rows, N, K, a=P, w=P, **kw: B.int_linear_form(B.make_int_linear_desc(rows, N, K, **kw), a, w)  # noqa: E731
+    assert form(1, 4096, 4096) == "rows16" and form(3, 20, 30000) == "rows16_split16"
+    assert form(4000, 4000, 2048) == "tile256x256"
+    # rows that begin inside a line of 128 bytes, by their stride or by where they start
+    assert form(1500, 1500, 256) == "tile128x128" == form(1500, 1500, 256, None, None)
+    assert {form(1500, 1500, 256, P + 16), form(1500, 1500, 256, P, P + 48), form(1500, 1500, 256, lda=272)} == {"tile128x128_lines"}
+    assert form(5, 70, 100, lda=1 << 23) == "any" and form(0, 8, 8) == ""
+    # a workspace is asked for where the form's name says that a reduction is shared
+    for size in ((3, 20, 30000), (130, 257, 16000), (1, 4096, 4096), (1500, 1500, 260)):
+        assert (B.int_linear_workspace_bytes(B.make_int_linear_desc(*size)) > 0) == ("split" in form(*size))
+    for bad in (dict(a=P + 8), dict(w=P + 8), dict(lda=40), dict(rows=-1)):
+        with pytest.raises(B.ConvError):
+            form(**{**dict(rows=4, N=8, K=16), **bad})
+
+
 @pytest.mark.parametrize("change", [dict(rows=-1), dict(rows=1 << 31), dict(cols=0), dict(ldx=99), dict(ldg=99), dict(top=-1), dict(top=65), dict(top=101)])
 def test_logprob_descriptors_that_are_refused(change):
     d = B.make_logprob_desc(4, 100, top=5)
