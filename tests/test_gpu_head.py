@@ -185,3 +185,48 @@ def test_one_row_out_of_a_channel_plane():
     got = {k: v.clone() for k, v in head.score(planes[:, :, 0, 0].contiguous(), d["target"]).items()}
     want = head.score(d["x"], d["target"])
     assert all(torch.equal(got[k], want[k]) for k in got)
+
+
+@pytest.mark.parametrize("T,D,V", [(1, 32, 10), (48, 96, 1000), (33, 100, 130), (300, 384, 1000)])
+def test_training_head_in_bf16(T, D, V):
+    """Tensors on the way (the normalised rows y, the logits z, their gradient dz, the product dy = dz w) are stored in bf16, so each
+    carries an error of 2^-8 of an element; what follows is linear in them but for the softmax.  Bounds in the 2-norm: u = 2^-8,
+    du(t) the norm of t's stored error."""
+    c, d = case(T, D, V, wl.BF16, 3 * T + D)
+    torch = torch_mod()
+    head = TrainingHead(T, D, V, torch.bfloat16)
+    rng = np.random.default_rng(6)
+    gl, gh = rng.normal(size=T).astype(np.float32), rng.normal(size=T).astype(np.float32)
+    head.forward(d["x"], d["gamma"], d["beta"], d["w"], d["target"])
+    # what the head stored, taken as the exact inputs of the next step: each step is held to its own roundings
+    y = head.y.double().cpu().numpy()
+    z = head.logits.double().cpu().numpy()
+    u, n, f32 = 2.0 ** -8, np.linalg.norm, 2.0 ** -24
+    want_y, mean, rstd = ro.layernorm(c["x"], c["gamma"], c["beta"], 1e-5)
+    assert (np.abs(y - want_y) <= u * np.abs(want_y) + 1e-4).all()
+    want_z = y @ c["w"].T
+    assert (np.abs(z - want_z) <= 1.01 * u * np.abs(want_z) + (D + 8) * f32 * (np.abs(y) @ np.abs(c["w"]).T) + 1e-6).all()
+    r = ro.logprob(z, c["target"], 0)
+    assert np.allclose(head.logp.cpu().numpy(), r["logp"], atol=2e-5, rtol=2e-5) and np.allclose(head.entropy.cpu().numpy(), r["entropy"], atol=5e-5, rtol=5e-5)
+    dx, dgamma, dbeta, dw = head.backward(torch.from_numpy(gl).cuda(), torch.from_numpy(gh).cuda())
+    dz = head.logits.double().cpu().numpy()
+    want_dz = ro.logprob_bwd(z, c["target"], r["lse"], r["entropy"], gl.astype(np.float64), gh.astype(np.float64))
+    p = np.exp(z - r["lse"][:, None])
+    size = p * (np.abs(gl)[:, None] + np.abs(gh)[:, None] * (np.abs(z - r["lse"][:, None]) + r["entropy"][:, None] + 1))
+    assert (np.abs(dz - want_dz) <= 1.01 * u * np.abs(want_dz) + 1e-4 * size + 1e-30).all()
+    dy = head.dy.double().cpu().numpy()
+    near = lambda got, a, b, k: (np.abs(got - a @ b) <= 1.01 * u * np.abs(a @ b) + (k + 8) * f32 * (np.abs(a) @ np.abs(b)) + 1e-30).all()  # noqa: E731
+    assert near(dy, dz, c["w"], V)
+    assert near(dw.double().cpu().numpy(), dz.T, y, T)
+    want_dx, want_dg, want_db = ro.layernorm_bwd(c["x"], dy, c["gamma"], mean, rstd)
+    # (statistics of 32 bits: a part in 10^5 of the sizes that enter, as in the layers' own tests)
+    xh = np.abs((c["x"] - mean[:, None]) * rstd[:, None])
+    g = np.abs(dy * c["gamma"])
+    sizes = rstd[:, None] * (g + g.mean(1)[:, None] + xh * (g * xh).mean(1)[:, None])
+    assert (np.abs(dx.double().cpu().numpy() - want_dx) <= 1.01 * u * np.abs(want_dx) + 1e-5 * sizes).all()
+    assert (np.abs(dgamma.double().cpu().numpy() - want_dg) <= 1e-5 * (np.abs(dy) * (xh + 1)).sum(0) + 1e-30).all()
+    assert (np.abs(dbeta.double().cpu().numpy() - want_db) <= 1e-5 * np.abs(dy).sum(0) + 1e-30).all()
+    # and the whole of it near the gradients without any rounding: a few roundings deep
+    full = ro.logprob_bwd(want_y @ c["w"].T, c["target"], *(ro.logprob(want_y @ c["w"].T, c["target"], 0)[k] for k in ("lse", "entropy")), gl.astype(np.float64), gh.astype(np.float64))
+    want = full.T @ want_y
+    assert n(dw.double().cpu().numpy() - want) <= 0.1 * n(want)
