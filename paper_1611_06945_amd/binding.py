@@ -194,12 +194,14 @@ def _ptr(x) -> Optional[int]:
     if x is None:
         return None
     try:
-        data_ptr = x.data_ptr  # (looked up once: a small call has up to ten of these)
+        address = x.data_ptr()  # (without a look-up ahead: a small call has up to ten of these)
     except AttributeError:
+        if hasattr(x, "data_ptr"):
+            raise
         if isinstance(x, int):
             return x
         raise TypeError("expected a torch tensor, an int device address or None, got %r" % type(x)) from None
-    return int(data_ptr())
+    return address if address.__class__ is int else int(address)
 
 
 _raw_stream = None  # () -> handle of torch's current stream, once torch has initialised the GPU
