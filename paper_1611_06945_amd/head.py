@@ -67,6 +67,8 @@ class ScoringHead:
             linear, logprob = self._products(rows)
             need = max(need, B.int_linear_workspace_bytes(linear), B.logprob_workspace_bytes(logprob))
         self._plans, self._ws = {}, torch.empty(need, dtype=torch.uint8, device=dev)
+        if GPU == "cuda" and not torch.cuda.is_current_stream_capturing():
+            torch.cuda.current_stream(dev).synchronize()  # the 8-bit weights are there for whatever stream scores first
 
     def _products(self, rows: int):
         code = _code(self.torch, self.logits_dtype)
@@ -84,7 +86,8 @@ class ScoringHead:
 
     def score(self, features, target=None, stream=None):
         """features [T][D] (rows may be strided), target int64 [T] or None (negative: no token).  Returns views of the head's own
-        buffers, valid until the next call: logp (None without target), lse, entropy, top_id, top_logp."""
+        buffers, valid until the next call: logp (None without target), lse, entropy, top_id, top_logp.  Calls of one head share
+        its buffers, so on several streams they have to be put in order."""
         rows = features.shape[0]
         if features.device != self.w.device:
             raise ValueError("the features are on %s, the head on %s" % (features.device, self.w.device))

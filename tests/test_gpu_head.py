@@ -230,3 +230,20 @@ def test_training_head_in_bf16(T, D, V):
     full = ro.logprob_bwd(want_y @ c["w"].T, c["target"], *(ro.logprob(want_y @ c["w"].T, c["target"], 0)[k] for k in ("lse", "entropy")), gl.astype(np.float64), gh.astype(np.float64))
     want = full.T @ want_y
     assert n(dw.double().cpu().numpy() - want) <= 0.1 * n(want)
+
+
+def test_a_new_head_scores_on_any_stream():
+    """The weights are quantised when the head is made; a first score on another stream finds them done."""
+    torch = torch_mod()
+    _, d = case(8, 512, 30000, wl.F16, 77)
+    want = {k: v.clone() for k, v in ScoringHead(d["gamma"], d["beta"], d["w"], max_rows=8, top=5).score(d["x"], d["target"]).items()}
+    busy = torch.randn(4096, 4096, device="cuda")
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for _ in range(20):
+            busy = torch.tanh(busy @ busy)  # the current stream is behind
+        head = ScoringHead(d["gamma"], d["beta"], d["w"], max_rows=8, top=5)
+        got = head.score(d["x"], d["target"], side)
+        side.synchronize()
+        assert all(torch.equal(got[k], want[k]) for k in want)
