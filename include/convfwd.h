@@ -427,6 +427,7 @@ int int_linear_form(const int_linear_desc* desc, const int8_t* a, const int8_t* 
  *   logp[t] = x[t][target[t]] - lse_t,   entropy[t] = -sum_j p_tj log p_tj (nats; p log p = 0 where p = 0),
  *   top_id[t][0..top), top_logp[t][0..top): the `top` likeliest columns, by value and, where values are equal, by the lower
  *   index (+0 and -0 are equal; a NaN counts as the largest), and their log probabilities.
+ * Log probabilities are taken from the distance to the row's largest logit, so they do not lose bits where lse is large.
  * target is int64 [rows]: a negative one stands for "no token" (logp 0, no gradient), one >= cols gives NaN.
  * Any output may be NULL, not all; target may be NULL if logp is; top_id and top_logp are dense [rows][top] and go together;
  * 0 <= top <= min(64, cols), ignored if both are NULL.  Masked columns are -inf; a row of -inf only has lse, logp and top_logp -inf, entropy 0 and the columns
@@ -448,7 +449,7 @@ int logprob_fwd(const logprob_desc* desc, const void* logits, const int64_t* tar
 /*
  * The gradient in the logits of sum_t g_logp[t] * logp[t] + g_entropy[t] * entropy[t]:
  *   dlogits[t][j] = g_logp[t] * ([j == target[t]] - p_tj) - g_entropy[t] * p_tj * (log p_tj + entropy[t]),
- * p from lse and entropy of the forward pass.  g_logp or g_entropy may be NULL (zeros), not both; target goes with g_logp, entropy with
+ * p from lse and entropy of the forward pass (so it is off by |lse| units of 2^-24, as lse is).  g_logp or g_entropy may be NULL (zeros), not both; target goes with g_logp, entropy with
  * g_entropy.  Rows whose lse is -inf get zeros.  dlogits may be the logits themselves where ldx == ldg.  desc->top is not read.
  */
 int logprob_bwd(const logprob_desc* desc, const void* logits, const int64_t* target, const float* lse,

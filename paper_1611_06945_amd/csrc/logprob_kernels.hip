@@ -178,16 +178,19 @@ __device__ __forceinline__ int take_room(int n, int* counter)
     return __builtin_amdgcn_readfirstlane(base) + upto - n;
 }
 
+// A log probability is taken as (x - m) - log s, not as x - lse: lse is rounded to units of its own size, and a row of the lowest
+// value only would have the log probability 0 throughout.
 struct RowResult {
-    float lse, h;
+    float m, log_s, lse, h;
     bool empty;
+    __device__ __forceinline__ float logp(float x) const { return empty ? -kInf : (x - m) - log_s; }
 };
 __device__ __forceinline__ RowResult result_of(const Part& p)
 {
     RowResult r;
     r.empty = p.s == 0.0f;
-    const float l = logf(p.s);
-    r.lse = p.m + l, r.h = l - p.sd / p.s;
+    r.m = p.m, r.log_s = logf(p.s);
+    r.lse = p.m + r.log_s, r.h = r.log_s - p.sd / p.s;
     if (r.empty) r.lse = -kInf, r.h = 0.0f;
     return r;
 }
@@ -219,12 +222,12 @@ __device__ __forceinline__ void write_row(const LogprobArgs& a, int64_t row, con
         if (a.lse) a.lse[row] = r.lse;
         if (a.entropy) a.entropy[row] = r.h;
         // (a logit of NaN without a NaN in the row: no such column)
-        if (a.logp) a.logp[row] = !given.any ? 0.0f : r.empty && given.logit == given.logit ? -kInf : given.logit - r.lse;
+        if (a.logp) a.logp[row] = !given.any ? 0.0f : given.logit == given.logit ? r.logp(given.logit) : given.logit;
     }
     for (int i = threadIdx.x; i < a.top; i += NT) {
         const uint64_t k = best[i];
         a.top_id[row * a.top + i] = (int64_t)index_of(k);
-        a.top_logp[row * a.top + i] = r.empty ? -kInf : value_of((uint32_t)(k >> 32)) - r.lse;
+        a.top_logp[row * a.top + i] = r.logp(value_of((uint32_t)(k >> 32)));
     }
 }
 

@@ -354,3 +354,23 @@ def test_gradient_of_masked_columns_is_zero_however_large_that_of_the_entropy(dt
         want = ro.logprob_bwd(x, None, l32, h32, None, np.full(3, gh))
         lp = np.where(p > 0, x - l32[:, None], 0.0)
         assert (np.abs(got - want) <= EPS32 * 16 * (1 + np.abs(lp)) * abs(gh) * p * (np.abs(lp) + h32[:, None] + 1)).all()
+
+
+@pytest.mark.parametrize("cols", [5, 1000, 70001])
+def test_log_probabilities_do_not_depend_on_where_the_logits_lie(cols):
+    """Rows around a large value, and of the lowest value only: log probabilities are those of the differences to the largest logit,
+    with the bounds of logits around 0."""
+    rng = np.random.default_rng(cols)
+    for dtype, rows in ((wl.F16, [np.full(cols, -65504.0), 32768 + 32.0 * rng.integers(-1, 2, cols), -60000.0 - 32 * rng.integers(0, 2, cols)]),
+                        (wl.BF16, [np.full(cols, -(2.0 - 2.0 ** -7) * 2.0 ** 127), 2.0 ** 10 + 8 * rng.integers(-1, 2, cols), np.full(cols, 1e30)]),
+                        (wl.F32, [np.full(cols, -(2.0 - 2.0 ** -23) * 2.0 ** 127), 1e7 + rng.integers(-5, 6, cols), -1e5 - rng.integers(0, 900, cols) / 128])):
+        x = stored(np.stack(rows), dtype)
+        t = rng.integers(0, cols, 3)
+        _, (logp, _, h, ids, lps) = forward(x, dtype, t, 3)
+        shifted = x - x.max(1, keepdims=True)  # exact in 64 bits
+        r = ro.logprob(shifted, t, 3)
+        e_lse, e_h, _ = bounds(shifted, r)
+        assert_close(logp, r["logp"], e_lse + 2 * EPS32 * np.abs(r["logp"]), "logp")
+        assert_close(lps, r["top_logp"], (e_lse + 4 * EPS32 * np.abs(r["lse"]))[:, None], "top_logp")
+        assert_close(h, r["entropy"], e_h, "entropy")
+        assert np.array_equal(ids, r["top_id"])
