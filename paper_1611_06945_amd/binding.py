@@ -76,7 +76,7 @@ _lib = None
 
 def lib() -> ctypes.CDLL:
     """Load libconvfwd.so (raises OSError with a build hint if it is not there)."""
-    global _lib
+    global _lib, _tensor, _tensor_address
     if _lib is None:
         if not os.path.exists(LIB_PATH):
             raise OSError("%s not found: build it with `python -m paper_1611_06945_amd.build`" % LIB_PATH)
@@ -84,8 +84,9 @@ def lib() -> ctypes.CDLL:
         # context).  PyTorch ships its own copy of the runtime; loading it first makes the dynamic loader resolve the
         # library's dependency to that copy.  Loaded the other way round, two runtimes end up in the process and the
         # second one finds no device.
-        import torch  # noqa: F401
+        import torch
 
+        _tensor, _tensor_address = torch.Tensor, torch.Tensor.data_ptr
         L = ctypes.CDLL(LIB_PATH)
         dp = ctypes.POINTER(conv_desc)
         vp, i32p = ctypes.c_void_p, ctypes.POINTER(ctypes.c_int32)
@@ -190,18 +191,20 @@ def desc_of(shape, dtype=CONV_F32, relu=True, in_nhwc=False, out_nhwc=False, fil
                      flags=flags)
 
 
+_tensor, _tensor_address = None, None  # torch.Tensor and its data_ptr, once the library is loaded
+
+
 def _ptr(x) -> Optional[int]:
+    if type(x) is _tensor:
+        return _tensor_address(x)  # (a small call has up to ten of these: 0.14 us, by its name 0.17)
     if x is None:
         return None
-    try:
-        address = x.data_ptr()  # (without a look-up ahead: a small call has up to ten of these)
-    except AttributeError:
-        if hasattr(x, "data_ptr"):
-            raise
-        if isinstance(x, int):
-            return x
-        raise TypeError("expected a torch tensor, an int device address or None, got %r" % type(x)) from None
-    return address if address.__class__ is int else int(address)
+    data_ptr = getattr(x, "data_ptr", None)
+    if data_ptr is not None:
+        return int(data_ptr())
+    if isinstance(x, int):
+        return x
+    raise TypeError("expected a torch tensor, an int device address or None, got %r" % type(x))
 
 
 _raw_stream = None  # () -> handle of torch's current stream, once torch has initialised the GPU
