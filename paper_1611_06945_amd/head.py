@@ -76,12 +76,13 @@ class ScoringHead:
                 B.make_logprob_desc(rows, self.V, code, self.top))
 
     def plan(self, rows: int, ldx: int):
-        """The three descriptors for a number of rows and a row stride of the features, made once."""
+        """The three descriptors for a number of rows and a row stride of the features, and the answers' places, made once."""
         if not 0 <= rows <= self.max_rows:
             raise ValueError("a head of %d rows cannot score %d" % (self.max_rows, rows))
         key = (rows, ldx)
         if key not in self._plans:
-            self._plans[key] = (B.make_norm_desc(rows, self.D, self.code, self.eps, ldx, self.q.stride(0)), *self._products(rows))
+            answers = {k: getattr(self, k)[:rows] for k in ("logp", "lse", "entropy", "top_id", "top_logp")}
+            self._plans[key] = (B.make_norm_desc(rows, self.D, self.code, self.eps, ldx, self.q.stride(0)), *self._products(rows), answers)
         return self._plans[key]
 
     def score(self, features, target=None, stream=None):
@@ -95,15 +96,14 @@ class ScoringHead:
             raise ValueError("features must be [T <= %d][%d] of %s, the columns of a row next to each other" % (self.max_rows, self.D, self.dtype))
         if target is not None:
             _check("target", target, self.torch.int64, (rows,), self.w.device)
-        norm, linear, logprob = self.plan(rows, features.stride(0) if rows > 1 else self.D)
+        norm, linear, logprob, answers = self.plan(rows, features.stride(0) if rows > 1 else self.D)
         ws, n = self._ws, self._ws.numel()
         B.layernorm_quant_fwd(norm, features, self.gamma, self.beta, self.q, self.q_scale, stream)
         B.int_linear_fwd(linear, self.q, self.q_scale, self.w, self.w_scale, self.bias, self.logits, ws, n, stream)
         logp = None if target is None else self.logp
         tops = (self.top_id, self.top_logp) if self.top else (None, None)
         B.logprob_fwd(logprob, self.logits, target, logp, self.lse, self.entropy, *tops, ws, n, stream)
-        return {"logp": None if logp is None else logp[:rows], "lse": self.lse[:rows], "entropy": self.entropy[:rows],
-                "top_id": self.top_id[:rows], "top_logp": self.top_logp[:rows]}
+        return dict(answers) if logp is not None else {**answers, "logp": None}
 
 
 class TrainingHead:
