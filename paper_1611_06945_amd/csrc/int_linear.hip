@@ -495,7 +495,9 @@ typedef IntTile<4, 2, 4, 8, 2, false> Tile256x256;
 //   512 x 4096 x 4096 37 / 19 / 16 / 19 / 23 / 42;  1024 x 4096 x 1024 22 / 12 / 15 / 9.7 / 9.4 / 17;  2048 x 2048 x 2048 38 / 19 / 16 / 17 / 16 / 26;
 //   5298 x 608 x 5120 79 / 36 / 28 / 25 / 33 / 56;  8192 x 1024 x 4096 123 / 61 / 46 / 44 / 38 / 46;  4096 x 4096 x 4096 263 / 114 / 90 / 85 / 71 / 57;
 //   8192 x 50256 x 768 1780 / 816 / 611 / 618 / 489 / 526;  8192 x 8192 x 64 161 / 87 / 57 / 60 / 41 / 38;
-//   8192 x 8192 x 4096 1030 / 443 / 371 / 345 / 304 / 242 (2270 TOP/s; 3260 on zeros: the card's power holds the clock down).
+//   8192 x 8192 x 4096 1030 / 443 / 371 / 345 / 304 / 242 (in later runs 217 to 221, 2500 TOP/s, and 3300 on zeros: the card's power holds
+//   the clock down.  The register-only loop has 3970 and 4600: what is missing on zeros too is no power but the ring of two stages, which
+//   waits for all its loads at every step with no other workgroup on the CU; waves wait for 32 % of their cycles.)
 template <typename T>
 double tiles_us(const IntLinearArgs& g, double once, double own, double step)
 {

@@ -8,7 +8,8 @@
 // are equal).  The `top`-th largest of 16 to 128 such maxima is a bound below which no alternative lies, and only about `top` threads
 // hold anything above it; their pieces are read once more (from cache), what reaches the bound goes to a list in LDS, and its
 // elements are ranked by counting.  For logits in no particular order the list has little more than `top` entries.  Rows where it
-// would overflow, and rows with a NaN or +inf, take the alternatives one by one instead, a pass over the row for each.
+// would overflow, and rows with a NaN or +inf, take the alternatives one by one instead, a pass over the row for each (2048 x 50257 bf16
+// whose large logits all lie in the pieces of six threads: 2.7 ms with 20 alternatives, 8.5 with 64, instead of 55 and 74 us).
 #include <algorithm>
 
 #include "rows_common.h"
@@ -47,7 +48,8 @@ __device__ __forceinline__ uint64_t wave_max(uint64_t k)
     return k;
 }
 
-// e^d; d * log2 e is rounded once, so the result is off by |d| units of 2^-24 at most, and 0 below 2^-126
+// e^d, off by 1.25 |d| units of 2^-24 at most, for the rounding of the product (1) and of log2 e (0.23), and by the instruction's own
+// error; 0 below 2^-126
 __device__ __forceinline__ float exp_of(float d) { return __builtin_amdgcn_exp2f(d * kLog2e); }
 
 // Sums over part of a row, relative to e^m.  m starts at the lowest number, not at -inf, so that m - m is a number.
@@ -127,7 +129,9 @@ __device__ __forceinline__ uint64_t nth_of_pairs(uint64_t k0, uint64_t k1, int r
 }
 // A bound for the `top` largest of 128 sets of keys, given each set's largest, two a lane: the top-th largest of these, or, where `top`
 // is small beside 16 or 32, of the largest of four or eight of them (fewer comparisons; for keys in no order 5 of 16 let 6 through, 20 of
-// 32 31, 64 of 128 89).  Keys that are not 0 are distinct; 0 if there are not as many.
+// 32 31, 64 of 128 89).  Keys that are not 0 are distinct; 0 if there are not as many.  The steps (us with 8 / 9 and with 20 / 21
+// alternatives): 2048 x 50257 bf16 46.0 / 46.0 and 54.9 / 55.6, 20 x 1000 fp32 5.8 / 5.9 and 7.8 / 7.9, 1 x 131072 fp32, which has the chain twice,
+// 9.7 / 9.9 and 11.7 / 15.6.
 __device__ __forceinline__ uint64_t bound_of_wave(uint64_t k0, uint64_t k1, int top)
 {
     if (top > 20) return nth_of_pairs(k0, k1, top - 1);

@@ -4,8 +4,8 @@
 // each holding up to NV pieces of 16 bytes.  The mean comes first and the variance is summed around it, from registers.  A workgroup keeps
 // its columns' gamma and beta in registers over all its rows, and asks for its next row before it works on the present one.  Backward, a lane adds up dgamma and dbeta of its columns
 // over its rows in registers; a workgroup's lanes with the same columns are added through LDS, and a second kernel adds the
-// workgroups' sums, always in the same order.  Longer rows (forward 32 elements a lane of 16 waves, backward of 8) are read again for
-// every pass (`_any`).
+// workgroups' sums, always in the same order.  Longer rows are read again for every pass (`_any`): forward from 32768 columns of
+// 16 bits and 16384 of fp32 on (32 and 16 elements a lane of 16 waves), backward from 16384 (32 of 8 waves).
 #include <algorithm>
 
 #include "rows_common.h"
@@ -450,6 +450,8 @@ __global__ __launch_bounds__(1024) void norm_dw_join(NormArgs a, int parts, int6
 }
 
 // ---- rows of any length: a workgroup a row, the row read again for every pass --------------------------------------------
+// An element a load, three passes forward and two backward (and one more for the columns' sums), most of them from cache: 1310 x 20000 fp32
+// forward 67 us (3.1 TB/s of what has to be read and written), to 8 bits 85, backward 122; 1310 x 40000 bf16 115, 158 and 171.
 
 template <int DT, int MODE>
 __global__ __launch_bounds__(1024) void norm_fwd_any(NormArgs a)
@@ -546,7 +548,7 @@ constexpr int kCUs = 256;
 // Backward: the fewest lanes that hold the row with 16 elements each; a wave and more of 16-bit rows 24, so that fewer are idle (us with 16 / 24:
 // 43690 x 1152 bf16 77 / 61, 2000 x 1536 bf16 14 / 12; fp32, whose next row takes twice the registers, 32768 x 1536 108 / 124).  The longest
 // have 512 lanes with up to 32, the 32 without the next row (which spilled 90 registers): 5225 x 9632 bf16 65 us, 4096 x 12288
-// 67, 3072 x 16384 75, where 16 waves with 16 a lane took 87, 77 and 78.  lanes 0: the row is too long.
+// 67, where 16 waves with 16 a lane took 87 and 77.  lanes 0: the row is too long.
 struct Form {
     int lanes, pieces;
 };
@@ -563,8 +565,8 @@ Form bwd_form(int cols, int dtype)
     return Form{0, 0};
 }
 
-// Forward: as above up to a wave; then waves as many as the row takes, up to 16, with 16 elements a lane (or 32, where 16 waves would
-// not do).  Against 4 or 16 waves, whose lanes were partly idle (us): 19660 x 2560 bf16 43 -> 35, 9830 x 5120 bf16 55 -> 35, codes alone
+// Forward: as above up to a wave; then waves as many as the row takes, up to 16, with 16 elements a lane (in 16 bits 32, where 16 waves
+// would not do).  Against 4 or 16 waves, whose lanes were partly idle (us): 19660 x 2560 bf16 43 -> 35, 9830 x 5120 bf16 55 -> 35, codes alone
 // 40 -> 28.  With few rows half of that a lane: 300 x 1536 bf16 3.7 -> 3.0; with many it costs, 12288 x 4096 bf16 34 -> 41.
 struct FwdForm {
     int lanes, pieces, waves;

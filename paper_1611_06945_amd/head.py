@@ -4,11 +4,11 @@
 
 `ScoringHead` is the serving form: the layer norm writes 8-bit rows, the product multiplies them with weights that were
 quantised when the head was made, and the answers are log probabilities of given tokens, entropies and the likeliest
-alternatives.  It allocates everything up front, so a call is three launches (four or five for few rows of a long vocabulary)
-and can be recorded into a HIP graph.
+alternatives.  It allocates everything up front, for any number of rows up to its own, so a call is three launches (four or five
+for few rows of a long vocabulary) and can be recorded into a HIP graph.
 
 `TrainingHead` is the training form of the same layers in their storage type: log probabilities and entropies of a batch, and
-the gradients of  sum_t g_logp[t] logp[t] + g_entropy[t] entropy[t]  in the features, gamma, beta and the weight.  Its dense products
+the gradients of  sum_t g_logp[t] logp[t] + g_entropy[t] entropy[t]  in the features, gamma, beta and the weight (there is no bias).  Its dense products
 are the library's 1x1 convolutions: T rows are T images of one pixel, and the two products of the backward pass are convolutions of
 transposed tensors.
 
