@@ -111,6 +111,8 @@ class TrainingHead:
         """Buffers and descriptors for batches of `rows` features [rows][D] over V tokens, in `dtype`."""
         import torch
 
+        if torch.device(device).type != GPU:
+            raise ValueError("a head on %s: its kernels run on the GPU" % device)
         self.torch, self.rows, self.D, self.V, self.dtype = torch, rows, D, V, dtype
         self.code = _code(torch, dtype)
         new = lambda *shape: torch.empty(*shape, dtype=dtype, device=device)  # noqa: E731

@@ -190,3 +190,10 @@ def test_gradients_that_do_not_fit_the_batch_are_refused(calls, bad):
             head.backward(*args)
         assert not calls
         head.backward(g, g)  # the logits are still there
+
+
+def test_a_training_head_off_the_gpu_is_refused(monkeypatch):
+    with pytest.raises(ValueError):
+        H.TrainingHead(3, 64, 100, torch.float16, device="cpu")
+    monkeypatch.setattr(H, "GPU", "cpu")
+    H.TrainingHead(3, 64, 100, torch.float16, device="cpu")
