@@ -455,6 +455,48 @@ int logprob_fwd(const logprob_desc* desc, const void* logits, const int64_t* tar
 int logprob_bwd(const logprob_desc* desc, const void* logits, const int64_t* target, const float* lse,
                 const float* entropy, const float* g_logp, const float* g_entropy, void* dlogits, void* stream);
 
+/*
+ * Linear layers in float types: out[t][n] = act(z[t][n]) + residual[t][n],  z[t][n] = sum_k x[t][k] * w[n][k] + bias[n],
+ * for x [rows][K] and w [N][K].  act is nothing, CONV_FLAG_RELU (max(z, 0), a NaN stays NaN), LINEAR_FLAG_GELU (z Phi(z), Phi the
+ * normal distribution) or LINEAR_FLAG_SILU (z / (1 + exp(-z))).  bias (fp32 [N]) and residual may be NULL; pre, where it is not NULL, receives z
+ * (what linear_bwd needs where there is an activation).  ldr is the row stride of the residual, ldo that of out, pre and dout; the
+ * residual may be out itself where ldr == ldo.  All sums are fp32; out and pre are each rounded once.
+ * fp32 products of more than a few rows are formed from three bf16 parts of each operand, six products of them: what is left out is below 2^-23 of each
+ * term.  There an operand's infinity, NaN or magnitude above 0x1.FEp127 makes NaN of the outputs it reaches, and parts below 2^-126 count as zero.
+ * `workspace` (linear_workspace_bytes(desc), may be 0; 16-byte aligned) holds those parts and partial sums of shared reductions; NULL or a smaller one gives
+ * CONV_EWORKSPACE when bytes are needed.  Operands whose rows start on 16 bytes are loaded faster.
+ * CONV_EINVAL for rows < 0, N or K outside [1, 2^24), strides below the row's length, unknown flags or more than one activation, NULL or misaligned
+ * pointers, outputs that are inputs.
+ */
+#define LINEAR_FLAG_GELU 0x100u
+#define LINEAR_FLAG_SILU 0x200u
+typedef struct {
+    int64_t rows;
+    int64_t ldx, ldw, ldr, ldo; /* row strides in elements */
+    int32_t N, K;
+    int32_t dtype;              /* conv_dtype of all but bias and dbias */
+    uint32_t flags;
+} linear_desc;
+size_t linear_workspace_bytes(const linear_desc* desc);
+int linear_fwd(const linear_desc* desc, const void* x, const void* w, const float* bias, const void* residual, void* out,
+               void* pre, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Its gradients: with dz = dout * act'(pre) (the slope of ReLU at 0 is 0),
+ *   dx[t][k] = sum_n dz[t][n] * w[n][k],   dw[n][k] = sum_t dz[t][n] * x[t][k],   dbias[n] = sum_t dz[t][n];
+ * the residual's gradient is dout.  Any of dx (row stride ldx), dw (ldw) and dbias (fp32 [N]) may be NULL, not all; x is read for dw, w for dx, pre
+ * where there is an activation: each may be NULL otherwise.  In 16-bit types dz is rounded to the type before the products (dbias adds it
+ * unrounded).  rows = 0 gives zero dw and dbias.  `workspace`: linear_bwd_workspace_bytes(desc), as above.
+ */
+size_t linear_bwd_workspace_bytes(const linear_desc* desc);
+int linear_bwd(const linear_desc* desc, const void* x, const void* w, const void* pre, const void* dout, void* dx, void* dw,
+               float* dbias, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Name of the form that a product takes for this descriptor and these operands' addresses (which count modulo 16), NUL-terminated in
+ * buf[0..n), e.g. "rows16", "tile256x256" or "planes_tile64x64_split4"; `which`: 0 the product of linear_fwd, 1 and 2 those of linear_bwd for dx and
+ * dw.  Empty for no rows.  Pure host code. */
+int linear_form(const linear_desc* desc, const void* x, const void* w, int which, char* buf, size_t n);
+
 /* Text for a conv_status; for CONV_EHIP it includes the message of the last failed HIP call of this thread. */
 const char* conv_strerror(int status);
 

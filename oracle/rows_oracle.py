@@ -98,3 +98,34 @@ def logprob_bwd(x, target, lse, entropy, g_logp, g_entropy):
         if g_entropy is not None:
             dx[t] -= g_entropy[t] * np.where(p > 0, p * (np.where(p > 0, lp, 0.0) + entropy[t]), 0.0)
     return dx
+
+
+def activation(z, act):
+    """-> (act(z), its slope); the slope of ReLU at 0 is 0."""
+    from scipy.special import erfc
+
+    if act == "relu":
+        return np.where(z < 0, 0.0, z), np.where(z > 0, 1.0, np.where(z <= 0, 0.0, z))
+    if act == "gelu":
+        phi = 0.5 * erfc(-z * np.sqrt(0.5))
+        return z * phi, phi + z * np.exp(-0.5 * z * z) / np.sqrt(2.0 * np.pi)
+    if act == "silu":
+        with np.errstate(over="ignore"):
+            p = 1.0 / (1.0 + np.exp(-z))
+        return z * p, p * (1.0 + z * (1.0 - p))
+    return z, np.ones_like(z)
+
+
+def linear(x, w, bias, residual, act):
+    """-> (out, pre, size): size is the sum of the magnitudes that pre adds up."""
+    z, size = x @ w.T, np.abs(x) @ np.abs(w).T
+    if bias is not None:
+        z, size = z + bias, size + np.abs(bias)
+    out = activation(z, act)[0]
+    return (out if residual is None else out + residual), z, size
+
+
+def linear_bwd(x, w, pre, dout, act):
+    """-> (dx, dw, dbias)."""
+    dz = dout if act == "none" else dout * activation(pre, act)[1]
+    return dz @ w, dz.T @ x, dz.sum(0)

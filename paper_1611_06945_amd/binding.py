@@ -22,6 +22,7 @@ CONV_F32, CONV_F16, CONV_BF16 = 0, 1, 2
 CONV_FLAG_RELU, CONV_FLAG_IN_NHWC, CONV_FLAG_OUT_NHWC, CONV_FLAG_FILT_KRSC, CONV_FLAG_FILT_WINOGRAD = 1, 2, 4, 8, 16
 CONV_FLAG_MAXPOOL_3X3S2 = 32
 CONV_FLAG_FILT_PACKED = 64
+LINEAR_FLAG_GELU, LINEAR_FLAG_SILU = 0x100, 0x200
 CONV_STATIC_SCRATCH_BYTES = 32 << 20
 CONV_OK, CONV_EINVAL, CONV_EDTYPE, CONV_EWORKSPACE, CONV_EHIP, CONV_ENOVARIANT, CONV_EIO = 0, -1, -2, -3, -4, -5, -6
 
@@ -63,6 +64,11 @@ class int_linear_desc(ctypes.Structure):
 class logprob_desc(ctypes.Structure):
     _fields_ = [("rows", ctypes.c_int64), ("ldx", ctypes.c_int64), ("ldg", ctypes.c_int64), ("cols", ctypes.c_int32),
                 ("dtype", ctypes.c_int32), ("top", ctypes.c_int32)]
+
+
+class linear_desc(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("ldx", ctypes.c_int64), ("ldw", ctypes.c_int64), ("ldr", ctypes.c_int64), ("ldo", ctypes.c_int64),
+                ("N", ctypes.c_int32), ("K", ctypes.c_int32), ("dtype", ctypes.c_int32), ("flags", ctypes.c_uint32)]
 
 
 class ConvError(RuntimeError):
@@ -170,6 +176,17 @@ def lib() -> ctypes.CDLL:
         L.logprob_fwd.restype = ctypes.c_int
         L.logprob_bwd.argtypes = [gp] + [vp] * 8
         L.logprob_bwd.restype = ctypes.c_int
+        lp = ctypes.POINTER(linear_desc)
+        L.linear_workspace_bytes.argtypes = [lp]
+        L.linear_workspace_bytes.restype = sz
+        L.linear_fwd.argtypes = [lp] + [vp] * 7 + [sz, vp]
+        L.linear_fwd.restype = ctypes.c_int
+        L.linear_bwd_workspace_bytes.argtypes = [lp]
+        L.linear_bwd_workspace_bytes.restype = sz
+        L.linear_bwd.argtypes = [lp] + [vp] * 8 + [sz, vp]
+        L.linear_bwd.restype = ctypes.c_int
+        L.linear_form.argtypes = [lp, vp, vp, ctypes.c_int, ctypes.c_char_p, sz]
+        L.linear_form.restype = ctypes.c_int
         L.conv_strerror.argtypes = [ctypes.c_int]
         L.conv_strerror.restype = ctypes.c_char_p
         _lib = L
@@ -465,6 +482,40 @@ def logprob_fwd(desc, logits, target, logp, lse=None, entropy=None, top_id=None,
 def logprob_bwd(desc, logits, target, lse, entropy, g_logp, g_entropy, dlogits, stream=None) -> None:
     _check(lib().logprob_bwd(ctypes.byref(desc), _ptr(logits), _ptr(target), _ptr(lse), _ptr(entropy), _ptr(g_logp),
                              _ptr(g_entropy), _ptr(dlogits), _stream(stream)), "logprob_bwd")
+
+
+_ACTIVATIONS = {"none": 0, "relu": CONV_FLAG_RELU, "gelu": LINEAR_FLAG_GELU, "silu": LINEAR_FLAG_SILU}
+
+
+def make_linear_desc(rows, N, K, dtype=CONV_F32, act="none", ldx=None, ldw=None, ldr=None, ldo=None) -> linear_desc:
+    """act: "none", "relu", "gelu" or "silu"."""
+    return linear_desc(rows, K if ldx is None else ldx, K if ldw is None else ldw, N if ldr is None else ldr, N if ldo is None else ldo,
+                       N, K, dtype, _ACTIVATIONS[act])
+
+
+def linear_workspace_bytes(desc) -> int:
+    return int(lib().linear_workspace_bytes(ctypes.byref(desc)))
+
+
+def linear_fwd(desc, x, w, bias, residual, out, pre=None, workspace=None, workspace_bytes=0, stream=None) -> None:
+    _check(lib().linear_fwd(ctypes.byref(desc), _ptr(x), _ptr(w), _ptr(bias), _ptr(residual), _ptr(out), _ptr(pre), _ptr(workspace),
+                            int(workspace_bytes), _stream(stream)), "linear_fwd")
+
+
+def linear_bwd_workspace_bytes(desc) -> int:
+    return int(lib().linear_bwd_workspace_bytes(ctypes.byref(desc)))
+
+
+def linear_bwd(desc, x, w, pre, dout, dx, dw, dbias, workspace=None, workspace_bytes=0, stream=None) -> None:
+    _check(lib().linear_bwd(ctypes.byref(desc), _ptr(x), _ptr(w), _ptr(pre), _ptr(dout), _ptr(dx), _ptr(dw), _ptr(dbias), _ptr(workspace),
+                            int(workspace_bytes), _stream(stream)), "linear_bwd")
+
+
+def linear_form(desc, x=None, w=None, which=0) -> str:
+    """Name of the form of a product for these sizes, strides and addresses: 0 that of linear_fwd, 1 and 2 those of linear_bwd for dx and dw."""
+    buf = ctypes.create_string_buffer(64)
+    _check(lib().linear_form(ctypes.byref(desc), _ptr(x), _ptr(w), int(which), buf, len(buf)), "linear_form")
+    return buf.value.decode()
 
 
 def conv_probe_mfma_peak(dtype: int, block: int, scratch, stream=None) -> float:

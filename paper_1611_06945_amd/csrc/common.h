@@ -298,6 +298,25 @@ hipError_t launch_logprob_fwd(LogprobArgs& a, int dtype, hipStream_t s);
 hipError_t launch_logprob_bwd(LogprobArgs& a, int dtype, hipStream_t s);
 size_t logprob_workspace(int64_t rows, int cols, int top, int dtype);
 
+// Linear layers, forward and backward.
+struct LinearArgs {
+    const void *x, *w;
+    const float* bias;
+    const void* residual;
+    void *out, *pre;       // forward; pre null where it is not asked for
+    const void *pre_in, *dout;  // backward
+    void *dx, *dw;
+    float* dbias;
+    void* ws;
+    int64_t rows, ldx, ldw, ldr, ldo;
+    int N, K, act;
+};
+hipError_t launch_linear_fwd(const LinearArgs& a, int dtype, hipStream_t s);
+hipError_t launch_linear_bwd(const LinearArgs& a, int dtype, hipStream_t s);
+size_t linear_fwd_workspace(int64_t rows, int N, int K, int dtype);
+size_t linear_bwd_workspace(int64_t rows, int N, int K, int dtype);
+int linear_form_name(const LinearArgs& a, int dtype, int which, char* buf, size_t n);  // as snprintf; which: out, dx, dw
+
 inline const char* dtype_name(int dt) { return dt == CONV_F32 ? "f32" : dt == CONV_F16 ? "f16" : "bf16"; }
 inline int dtype_size(int dt) { return dt == CONV_F32 ? 4 : 2; }
 

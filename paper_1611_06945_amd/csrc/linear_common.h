@@ -1,0 +1,134 @@
+// What the files of the linear layers share: the activations, what becomes of a sum, the launchers of products by operand type.
+#pragma once
+
+#include "product_kernel.h"
+
+namespace convfwd {
+
+enum { ACT_NONE = 0, ACT_RELU = 1, ACT_GELU = 2, ACT_SILU = 3 };
+
+__device__ __forceinline__ float act_of(float z, int act)
+{
+    if (act == ACT_RELU) return z < 0.0f ? 0.0f : z;  // a NaN stays
+    if (act == ACT_GELU) return 0.5f * z * (1.0f + erff(z * 0.70710678118654752f));
+    if (act == ACT_SILU) return z / (1.0f + __expf(-z));
+    return z;
+}
+// its derivative; 0 at the corner of ReLU
+__device__ __forceinline__ float act_slope(float z, int act)
+{
+    if (act == ACT_RELU) return z > 0.0f ? 1.0f : z <= 0.0f ? 0.0f : z;
+    if (act == ACT_GELU) return 0.5f * (1.0f + erff(z * 0.70710678118654752f)) + z * __expf(-0.5f * z * z) * 0.39894228040143268f;
+    if (act == ACT_SILU) {
+        const float p = 1.0f / (1.0f + __expf(-z));
+        return p * (1.0f + z * (1.0f - p));
+    }
+    return 1.0f;
+}
+
+// out = act(sum + bias) + residual, and the sum with its bias where it is asked for.
+struct LinearOut {
+    const float* bias;
+    const void* residual;
+    void* pre;
+    void* out;
+    int64_t ldr, ldo;
+    int act;
+};
+
+template <int DT>
+struct LinearEpi {
+    typedef LinearOut Args;
+    static constexpr bool SYMMETRIC = false;
+    static __device__ __forceinline__ void prepare(const Args& e, float* bias, int64_t n0, int here, int width, int threads)
+    {
+        for (int i = threadIdx.x; i < width; i += threads) bias[i] = e.bias && i < here ? e.bias[n0 + i] : 0.0f;
+    }
+    static __device__ __forceinline__ void finish(const ProductArgs&, const Args& e, float (&v)[8], int64_t m, int64_t n, int have, const float* bias)
+    {
+        if (e.bias) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] += bias[k];
+        }
+        if (e.pre) put8<DT>(e.pre, m * e.ldo + n, v, have);
+        if (e.act) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = act_of(v[k], e.act);
+        }
+        if (e.residual) {
+            float r[8];
+            get8<DT>(e.residual, m * e.ldr + n, r, have);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] += r[k];
+        }
+        put8<DT>(e.out, m * e.ldo + n, v, have);
+    }
+};
+
+// Tiles of a product; the last two are for operands that start anywhere.
+enum ProductForm { P64, P128, P256, P64_ANY, P128_ANY };
+typedef ProductTile<4, 2, 1, 2, 4> Tile64;
+typedef ProductTile<2, 4, 4, 2, 2> Tile128;  // two workgroups a CU
+typedef ProductTile<4, 2, 4, 8, 2> Tile256;
+typedef ProductTile<4, 2, 1, 2, 2> Tile64Any;
+
+enum ProductLayout { LAYOUT_NT, LAYOUT_NN, LAYOUT_TN };  // which operand lies across the reduction: none, the second, both
+
+// The products of bf16 and fp16 rows, and of bf16 planes with an fp32 result.  splits > 1: partial sums to g.partial.
+hipError_t launch_product_f16(const ProductArgs& g, const LinearOut& e, ProductLayout layout, ProductForm form, int splits, hipStream_t s);
+hipError_t launch_product_bf16(const ProductArgs& g, const LinearOut& e, ProductLayout layout, ProductForm form, int splits, hipStream_t s);
+hipError_t launch_product_f32(const ProductArgs& g, const LinearOut& e, ProductLayout layout, ProductForm form, int splits, hipStream_t s);
+
+// (DT: of the operands, ODT: of the result)
+template <int DT, typename T, bool A_ACROSS, bool B_ACROSS, bool DIRECT, typename Epi>
+hipError_t launch_product_tiles(ProductArgs g, const typename Epi::Args& e, int batch, int splits, hipStream_t s)
+{
+    const void* f = (const void*)product_kernel<DT, T, A_ACROSS, B_ACROSS, DIRECT, Epi>;
+    const hipError_t err = ensure_dynamic_lds(f, T::LDS);
+    if (err != hipSuccess) return err;
+    g.tiles_n = (int)((g.N + T::BN - 1) / T::BN);
+    g.each = (g.ksteps + splits - 1) / splits;
+    // a launch holds less than 2^32 threads: the rows go in portions of so many tiles
+    const int64_t all = g.M, bands = std::max<int64_t>(1, (1 << 21) / ((int64_t)g.tiles_n * batch * splits));
+    for (int64_t skip = 0; skip < all; skip += bands * T::BT) {
+        ProductArgs p = g;
+        p.M = std::min(bands * T::BT, all - skip), p.m_first = skip;
+        p.a += A_ACROSS ? skip : skip * g.lda;
+        p.tiles_m = (int)((p.M + T::BT - 1) / T::BT);
+        const unsigned tiles = Epi::SYMMETRIC ? (unsigned)((int64_t)p.tiles_m * (p.tiles_m + 1) / 2) : (unsigned)p.tiles_m * (unsigned)p.tiles_n;
+        hipLaunchKernelGGL((product_kernel<DT, T, A_ACROSS, B_ACROSS, DIRECT, Epi>), dim3(tiles, (unsigned)batch, (unsigned)splits), dim3(T::NT), T::LDS, s, p, e);
+    }
+    return hipGetLastError();
+}
+
+template <int DT, bool A_ACROSS, bool B_ACROSS, typename Epi>
+hipError_t launch_product_form(const ProductArgs& g, const typename Epi::Args& e, ProductForm form, int batch, int splits, hipStream_t s)
+{
+    switch (form) {
+        case P64: return launch_product_tiles<DT, Tile64, A_ACROSS, B_ACROSS, true, Epi>(g, e, batch, splits, s);
+        case P128: return launch_product_tiles<DT, Tile128, A_ACROSS, B_ACROSS, true, Epi>(g, e, batch, splits, s);
+        case P256: return launch_product_tiles<DT, Tile256, A_ACROSS, B_ACROSS, true, Epi>(g, e, batch, splits, s);
+        case P64_ANY: return launch_product_tiles<DT, Tile64Any, A_ACROSS, B_ACROSS, false, Epi>(g, e, batch, splits, s);
+        default: return launch_product_tiles<DT, Tile128, A_ACROSS, B_ACROSS, false, Epi>(g, e, batch, splits, s);
+    }
+}
+
+// Planes always start on 16 bytes: no forms for other operands.
+template <int DT, bool A_ACROSS, bool B_ACROSS, typename Epi>
+hipError_t launch_product_direct(const ProductArgs& g, const typename Epi::Args& e, ProductForm form, int batch, int splits, hipStream_t s)
+{
+    switch (form) {
+        case P64: return launch_product_tiles<DT, Tile64, A_ACROSS, B_ACROSS, true, Epi>(g, e, batch, splits, s);
+        case P128: return launch_product_tiles<DT, Tile128, A_ACROSS, B_ACROSS, true, Epi>(g, e, batch, splits, s);
+        default: return launch_product_tiles<DT, Tile256, A_ACROSS, B_ACROSS, true, Epi>(g, e, batch, splits, s);
+    }
+}
+
+#define CONVFWD_PRODUCT_LAYOUTS(launch, DT, Epi)                                                   \
+    switch (layout) {                                                                              \
+        case LAYOUT_NT: return launch<DT, false, false, Epi>(g, arg, form, 1, splits, s);          \
+        case LAYOUT_NN: return launch<DT, false, true, Epi>(g, arg, form, 1, splits, s);           \
+        default: return launch<DT, true, true, Epi>(g, arg, form, 1, splits, s);                   \
+    }
+
+}  // namespace convfwd

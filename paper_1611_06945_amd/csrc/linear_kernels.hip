@@ -1,0 +1,627 @@
+// Linear layers: out = act(x w^T + bias) + residual, and the gradients.  Which kernels a call takes, the form for few rows, and what stands
+// around the products: planes of fp32 operands, the gradient of the activation with its column sums, the join of shared reductions.
+#include <cstdio>
+
+#include "linear_common.h"
+#include "split_products.h"
+
+namespace convfwd {
+
+namespace {
+
+// ---- few rows -------------------------------------------------------------------------------------------------------------
+
+struct LinearRows {
+    const void *x, *w;
+    int64_t ldx, ldw;
+    int64_t rows;
+    int N, K;
+    LinearOut out;
+    float* partial;
+};
+
+template <int DT>
+__device__ __forceinline__ float finish_one(const LinearOut& e, float z, int64_t t, int n)
+{
+    typedef typename Prec<DT>::elem_t elem_t;
+    if (e.bias) z += e.bias[n];
+    if (e.pre) ((elem_t*)e.pre)[t * e.ldo + n] = Prec<DT>::from_f32(z);
+    float v = act_of(z, e.act);
+    if (e.residual) v += Prec<DT>::to_f32(((const elem_t*)e.residual)[t * e.ldr + n]);
+    return v;
+}
+
+// One 16-byte piece of 16 rows of either operand, a lane four bytes times four of row lane % 16.  fp32: a lane's four values go to four
+// instructions, each of which takes one k of every lane; the order of a sum's terms is free.
+template <int DT>
+__device__ __forceinline__ f32x4 multiply_pieces(u32x4 w, u32x4 x, f32x4 c)
+{
+    if constexpr (DT == CONV_F32) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const uint32_t wk = w[k], xk = x[k];  // (a cast of a vector's element itself takes the first one)
+            c = __builtin_amdgcn_mfma_f32_16x16x4f32(__builtin_bit_cast(float, wk), __builtin_bit_cast(float, xk), c, 0, 0, 0);
+        }
+        return c;
+    } else {
+        return multiply16<DT>(w, x, c);
+    }
+}
+
+// The first `n` elements of a piece (n may be <= 0 or more than it has), the others zero.
+template <int DT>
+__device__ __forceinline__ u32x4 first_of_piece(u32x4 v, int n)
+{
+    if constexpr (DT == CONV_F32) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = k < n ? v[k] : 0u;
+        return v;
+    } else {
+        return first_elems(v, n);
+    }
+}
+
+// A workgroup 16 outputs x 16 RB rows, its W waves share the reduction: wave w takes every W-th run of 64 U bytes.  The weights' stream is what
+// counts, so loads are made of four lanes a 64-byte stretch of a row (a lane a row, as the matrix instruction wants them, is
+// served 16 bytes a clock), straight into LDS the wave has for itself, no barrier; a row's four pieces lie at piece ^ (row / 4 % 4) there, so
+// that no two of 16 lanes read a bank.  The waves' sums meet in LDS.  gridDim.z workgroups may share a long reduction (linear_join).
+// DIRECT: rows start on 16 bytes; otherwise pieces go through registers.
+template <int DT, int RB, int W, int U, bool DIRECT>
+__global__ __launch_bounds__(64 * W) void linear_rows(LinearRows g)
+{
+    typedef typename Prec<DT>::elem_t elem_t;
+    constexpr int NT = 64 * W, ES = sizeof(elem_t), VEC = 16 / ES, RUN = 64 * U / ES, OWN = (1 + RB) * U * 1024;
+    extern __shared__ __attribute__((aligned(16))) char smem[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int n0 = blockIdx.x * 16;
+    const int64_t t0 = (int64_t)blockIdx.y * (16 * RB);
+    const int rows_here = (int)min((int64_t)(16 * RB), g.rows - t0), outs_here = min(16, g.N - n0);
+    const elem_t *const x = (const elem_t*)g.x + t0 * g.ldx, *const w = (const elem_t*)g.w + (int64_t)n0 * g.ldw;
+    const int row = lane >> 2, piece = (lane & 3) ^ ((row >> 2) & 3);
+    char* const own = smem + wave * OWN;
+    const char* const mine = own + (lane & 15) * 64 + (((lane >> 4) ^ ((lane >> 2) & 3)) << 4);
+    // (whole pieces: rows start on 16 bytes, so what the last one holds past the end lies in the same 16 bytes as an element)
+    const __amdgpu_buffer_rsrc_t rx = make_rsrc(x, DIRECT ? (uint32_t)(((rows_here - 1) * g.ldx + g.K) * ES + 15) & ~15u : 0u);
+    const __amdgpu_buffer_rsrc_t rw = make_rsrc(w, DIRECT ? (uint32_t)(((outs_here - 1) * g.ldw + g.K) * ES + 15) & ~15u : 0u);
+    const uint32_t woff = DIRECT ? (uint32_t)row * (uint32_t)(g.ldw * ES) + piece * 16 : 0u;
+    const uint32_t xoff = DIRECT ? (uint32_t)row * (uint32_t)(g.ldx * ES) + piece * 16 : 0u;
+    // a piece from any address
+    auto through = [&](const elem_t* p, bool in, int k, char* to) {
+        const int n = in ? g.K - k : 0;
+        u32x4 v = {0, 0, 0, 0};
+        if (n >= VEC) {
+            __builtin_memcpy(&v, p + k, 16);
+        } else if (n > 0) {
+            elem_t e[VEC];
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) e[j] = j < n ? p[k + j] : (elem_t)0;
+            __builtin_memcpy(&v, e, 16);
+        }
+        *(u32x4*)(to + lane * 16) = v;
+    };
+
+    f32x4 acc[RB];
+#pragma unroll
+    for (int j = 0; j < RB; ++j) acc[j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int k = (blockIdx.z * W + wave) * RUN; k < g.K; k += gridDim.z * W * RUN) {
+        if constexpr (DIRECT) {
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(rw, (lds_void_t*)(own + u * 1024), 16, (int)(woff + (uint32_t)k * ES + u * 64), 0, 0, 0);
+#pragma unroll
+            for (int j = 0; j < RB; ++j)
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+                    __builtin_amdgcn_raw_ptr_buffer_load_lds(rx, (lds_void_t*)(own + ((1 + j) * U + u) * 1024), 16,
+                                                             (int)(xoff + (uint32_t)(j * 16) * (uint32_t)(g.ldx * ES) + (uint32_t)k * ES + u * 64), 0, 0, 0);
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        } else {
+#pragma unroll
+            for (int u = 0; u < U; ++u) through(w + (int64_t)row * g.ldw, row < outs_here, k + u * (64 / ES) + piece * VEC, own + u * 1024);
+#pragma unroll
+            for (int j = 0; j < RB; ++j)
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+                    through(x + (int64_t)(j * 16 + row) * g.ldx, j * 16 + row < rows_here, k + u * (64 / ES) + piece * VEC, own + ((1 + j) * U + u) * 1024);
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        }
+        u32x4 wv[U], xv[RB][U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) wv[u] = *(const u32x4*)(mine + u * 1024);
+#pragma unroll
+        for (int j = 0; j < RB; ++j)
+#pragma unroll
+            for (int u = 0; u < U; ++u) xv[j][u] = *(const u32x4*)(mine + ((1 + j) * U + u) * 1024);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // read before the next run's loads may land
+        if (DIRECT && k + RUN > g.K) {
+            // what follows a row's end is another row's, or nobody's
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int n = g.K - k - u * (64 / ES) - (lane >> 4) * VEC;
+                wv[u] = first_of_piece<DT>(wv[u], n);
+#pragma unroll
+                for (int j = 0; j < RB; ++j) xv[j][u] = first_of_piece<DT>(xv[j][u], n);
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int j = 0; j < RB; ++j) acc[j] = multiply_pieces<DT>(wv[u], xv[j][u], acc[j]);
+    }
+    __syncthreads();
+    f32x4* const part = (f32x4*)smem;
+#pragma unroll
+    for (int j = 0; j < RB; ++j) part[(wave * RB + j) * 64 + lane] = acc[j];
+    __syncthreads();
+    for (int o = threadIdx.x; o < 256 * RB; o += NT) {
+        const int n = n0 + (o & 15), r = o >> 4;  // output; row among the workgroup's
+        if (n >= g.N || r >= rows_here) continue;
+        float sum = 0.0f;
+#pragma unroll
+        for (int v = 0; v < W; ++v) sum += ((const float*)&part[(v * RB + (r >> 4)) * 64 + ((o & 15) >> 2) * 16 + (r & 15)])[o & 3];
+        if (gridDim.z > 1)
+            g.partial[((int64_t)blockIdx.z * g.rows + t0 + r) * g.N + n] = sum;
+        else
+            ((elem_t*)g.out.out)[(t0 + r) * g.out.ldo + n] = Prec<DT>::from_f32(finish_one<DT>(g.out, sum, t0 + r, n));
+    }
+}
+
+// Adds the sums of `splits` workgroups that shared a reduction, in their order.
+template <int DT>
+__global__ __launch_bounds__(256) void linear_join(LinearOut e, const float* partial, int64_t rows, int N, int splits)
+{
+    const int64_t o = (int64_t)blockIdx.x * 256 + threadIdx.x, all = rows * N;
+    if (o >= all) return;
+    const int64_t t = o / N;
+    const int n = (int)(o - t * N);
+    float sum = 0.0f;
+    for (int z = 0; z < splits; ++z) sum += partial[z * all + o];
+    ((typename Prec<DT>::elem_t*)e.out)[t * e.ldo + n] = Prec<DT>::from_f32(finish_one<DT>(e, sum, t, n));
+}
+
+// ---- around the products --------------------------------------------------------------------------------------------------
+
+// eight fp32 values as three pieces of bf16 each
+__device__ __forceinline__ void put_planes(uint16_t* p, int64_t plane, const float (&v)[8])
+{
+    uint32_t w[3][4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) split3_pair(v[2 * j], v[2 * j + 1], w[0][j], w[1][j], w[2][j]);
+#pragma unroll
+    for (int q = 0; q < 3; ++q) *(uint4*)(p + q * plane) = make_uint4(w[q][0], w[q][1], w[q][2], w[q][3]);
+}
+
+// fp32 [rows][cols] to three bf16 planes [rows][ldp] that add up to it, zeros from cols to ldp.
+__global__ __launch_bounds__(256) void linear_planes(const float* x, int64_t ldx, int64_t rows, int cols, uint16_t* out, int64_t ldp)
+{
+    const int64_t each = ldp / 8, all = rows * each, step = (int64_t)gridDim.x * 256;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += step) {
+        const int64_t t = all <= UINT32_MAX ? (uint32_t)i / (uint32_t)each : i / each;
+        const int j = (int)(i - t * each) * 8;
+        float v[8];
+        get8<CONV_F32>(x, t * ldx + j, v, cols - j);
+        put_planes(out + t * ldp + j, rows * ldp, v);
+    }
+}
+
+// The gradient at the sum: dz = dout act'(pre), with its sums over the rows.  A workgroup has 256 columns and `each` rows, eight lanes of
+// rows; the sums are of the values before they are rounded.
+// TO: 0 only the sums, 1 dz in the storage type with the row stride ldz, 2 three planes.
+template <int DT, int TO>
+__global__ __launch_bounds__(256) void linear_dz(const void* dout, const void* pre, int64_t ld, int64_t rows, int N, int act, uint16_t* dz, int64_t ldz,
+                                                 float* sums, int64_t each)
+{
+    __shared__ float lds[8][32 * 8 + 8];
+    const int col = threadIdx.x & 31, r = threadIdx.x >> 5;
+    const int64_t j = ((int64_t)blockIdx.x * 32 + col) * 8;
+    const int have = (int)min((int64_t)8, N - j);
+    const int64_t first = blockIdx.y * each, last = min(first + each, rows);
+    float sum[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) sum[k] = 0.0f;
+    if (j < (TO ? ldz : (int64_t)N)) {
+        for (int64_t t = first + r; t < last; t += 8) {
+            float v[8];
+            get8<DT>(dout, t * ld + j, v, have);
+            if (act) {
+                float z[8];
+                get8<DT>(pre, t * ld + j, z, have);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) v[k] *= act_slope(z[k], act);
+            }
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                if (k >= have) v[k] = 0.0f;
+                sum[k] += v[k];
+            }
+            if constexpr (TO == 1) put8<DT>(dz, t * ldz + j, v, 8);
+            if constexpr (TO == 2) put_planes(dz + t * ldz + j, rows * ldz, v);
+        }
+    }
+    if (!sums) return;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) lds[r][k * 33 + col] = sum[k];
+    __syncthreads();
+    const int64_t n = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (n >= N) return;
+    float all = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) all += lds[i][(threadIdx.x & 7) * 33 + (threadIdx.x >> 3)];
+    sums[(int64_t)blockIdx.y * N + n] = all;
+}
+
+// Adds `parts` rows of partial sums, always in the same order: a workgroup 32 columns, eight lanes of rows.
+__global__ __launch_bounds__(256) void linear_sums(const float* part, int parts, int N, float* out)
+{
+    __shared__ float lds[8][32];
+    const int col = threadIdx.x & 31, r = threadIdx.x >> 5, n = blockIdx.x * 32 + col;
+    float sum = 0.0f;
+    if (n < N)
+        for (int i = r; i < parts; i += 8) sum += part[(int64_t)i * N + n];
+    lds[r][col] = sum;
+    __syncthreads();
+    if (threadIdx.x >= 32 || n >= N) return;
+#pragma unroll
+    for (int i = 1; i < 8; ++i) sum += lds[i][col];
+    out[n] = sum;
+}
+
+// What no row adds anything to.
+__global__ __launch_bounds__(256) void linear_zero(char* out, int64_t ld_bytes, int64_t rows, int64_t cols_bytes)
+{
+    const int64_t words = cols_bytes / 2, all = rows * words, step = (int64_t)gridDim.x * 256;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += step) *(uint16_t*)(out + i / words * ld_bytes + i % words * 2) = 0;
+}
+
+// ---- plans ----------------------------------------------------------------------------------------------------------------
+
+constexpr int64_t kLongStride = 1 << 22;  // from here on a tile's offsets may pass 31 bits
+
+int64_t round_up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
+
+// Tiles, and what a launch of them is expected to take, in us: `once` and for every round of 256 tiles `own` and `step` for every 64 of the
+// reduction.
+struct TileCost {
+    int bt, bn;
+    double once, own, step;
+};
+constexpr TileCost kTiles[] = {{64, 64, 2.0, 1.2, 0.2}, {128, 128, 1.8, 1.5, 0.52}, {256, 256, 0, 11, 1.4}, {64, 64, 2.0, 1.5, 0.4}, {128, 128, 1.8, 1.5, 1.0}};
+
+struct ProductPlan {
+    ProductForm form;
+    int splits;
+    double us;
+};
+ProductPlan plan_product(int64_t M, int64_t N, int64_t K, int segments, bool direct)
+{
+    ProductPlan best = {P64, 1, 1e30};
+    const int64_t ksteps = (K + 63) / 64;
+    for (int f = direct ? P64 : P64_ANY; f <= (direct ? P256 : P128_ANY); ++f) {
+        const TileCost& c = kTiles[f];
+        const double tiles = (double)((M + c.bt - 1) / c.bt) * ((N + c.bn - 1) / c.bn);
+        for (int splits = 1; splits <= 32; splits *= 2) {
+            if (splits > 1 && (splits * 4 > ksteps || tiles * splits > 1024)) break;
+            const int64_t each = (ksteps + splits - 1) / splits;
+            const int shares = (int)((ksteps + each - 1) / each);  // none without a step
+            double us = c.once + std::ceil(tiles * shares / 256) * (c.own + each * segments * c.step);
+            if (shares > 1) us += 5 + 8.0 * shares * M * N / 4e6;  // written, read and added by a second launch
+            if (us < best.us) best = {(ProductForm)f, shares, us};
+        }
+    }
+    return best;
+}
+
+// Few rows: blocks of 16 rows a workgroup, workgroups that share a reduction, expected us.  A workgroup reads 120 KB in a us, all of them
+// 33 TB/s (from the caches mostly), and one takes 0.16 us of a CU a block at least; a second launch to add shares costs about 5 us of a call.
+struct RowsPlan {
+    int rb, splits;
+    double us;
+};
+RowsPlan plan_rows(int64_t rows, int N, int K, int dtype)
+{
+    RowsPlan p;
+    const double size = dtype_size(dtype);
+    p.rb = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+    const double groups = (double)((rows + 16 * p.rb - 1) / (16 * p.rb)) * ((N + 15) / 16);
+    const double bytes = 16.0 * (1 + p.rb) * K * size, alone = bytes / 120e3 * std::ceil(groups / 256);
+    p.splits = 1;
+    p.us = 2.8 + alone + std::max(groups * bytes / 33e6, groups / 256 * 0.16 * p.rb);
+    if (groups <= 64) {
+        const int most = std::min({16, (int)(256 / groups), (int)((K * size + 1023) / 1024)});
+        if (alone - alone / most > 6) p.splits = most, p.us = 8 + alone / most;
+    }
+    return p;
+}
+
+bool on_16(const void* p, int64_t ld, int size) { return ((uintptr_t)p & 15) == 0 && ld * size % 16 == 0 && ld < kLongStride; }
+
+// A forward call: few rows, or tiles (fp32: of planes).
+struct LinearForm {
+    bool rows, direct;
+    RowsPlan few;
+    ProductPlan tiles;
+};
+LinearForm form_of(int64_t rows, int N, int K, int dtype, bool direct)
+{
+    LinearForm f;
+    f.direct = direct;
+    f.few = plan_rows(rows, N, K, dtype);
+    const bool planes = dtype == CONV_F32;
+    f.tiles = plan_product(rows, N, K, planes ? 6 : 1, planes || direct);
+    if (planes) f.tiles.us += 5 + 10.0 * ((double)rows + N) * K / 4e6;
+    f.rows = rows <= 16 || f.few.us <= f.tiles.us;
+    return f;
+}
+
+struct Carve {  // pieces of a workspace
+    char* at;
+    size_t used = 0;
+    explicit Carve(void* p) : at((char*)p) {}
+    void* take(size_t bytes)
+    {
+        void* p = at ? at + used : nullptr;
+        used += (bytes + 255) & ~(size_t)255;
+        return p;
+    }
+};
+
+int64_t plane_stride(int64_t cols) { return round_up(cols, 64); }
+size_t plane_bytes(int64_t rows, int64_t cols) { return (size_t)(6 * rows * plane_stride(cols)); }
+
+unsigned grid_of(int64_t threads) { return (unsigned)std::min<int64_t>((threads + 255) / 256, 1 << 16); }
+
+hipError_t to_planes(const void* x, int64_t ld, int64_t rows, int cols, uint16_t* out, hipStream_t s)
+{
+    hipLaunchKernelGGL(linear_planes, dim3(grid_of(rows * plane_stride(cols) / 8)), dim3(256), 0, s, (const float*)x, ld, rows, cols, out, plane_stride(cols));
+    return hipGetLastError();
+}
+
+template <int DT>
+hipError_t join_as(const LinearOut& e, const float* partial, int64_t rows, int N, int splits, hipStream_t s)
+{
+    hipLaunchKernelGGL((linear_join<DT>), dim3((unsigned)((rows * N + 255) / 256)), dim3(256), 0, s, e, partial, rows, N, splits);
+    return hipGetLastError();
+}
+hipError_t join(int dtype, const LinearOut& e, const float* partial, int64_t rows, int N, int splits, hipStream_t s)
+{
+    return dtype == CONV_F32 ? join_as<CONV_F32>(e, partial, rows, N, splits, s)
+                             : dtype == CONV_F16 ? join_as<CONV_F16>(e, partial, rows, N, splits, s) : join_as<CONV_BF16>(e, partial, rows, N, splits, s);
+}
+
+// C = A B of 16-bit rows or of planes, and the join where a reduction is shared.
+struct Factor {
+    const void* p;
+    int64_t ld, plane;
+};
+hipError_t multiply(int dtype, ProductLayout layout, const Factor& a, const Factor& b, int64_t M, int64_t N, int64_t K, const LinearOut& e,
+                    const ProductPlan& plan, float* partial, hipStream_t s)
+{
+    ProductArgs g = {};
+    g.a = (const uint16_t*)a.p, g.b = (const uint16_t*)b.p, g.lda = a.ld, g.ldb = b.ld, g.plane_a = a.plane, g.plane_b = b.plane;
+    g.M = M, g.N = N, g.K = K, g.partial = partial;
+    g.ksteps = (int)((K + 63) / 64), g.segments = 1;
+    if (dtype == CONV_F32) {
+        // planes 2 0, 1 1, 0 2, 1 0, 0 1, 0 0: what is left out is below 2^-23 of a product
+        g.segments = 6;
+        g.seg_a = 2 | 1 << 2 | 0 << 4 | 1 << 6 | 0 << 8 | 0 << 10;
+        g.seg_b = 0 | 1 << 2 | 2 << 4 | 0 << 6 | 1 << 8 | 0 << 10;
+    }
+    const auto launch = dtype == CONV_F32 ? launch_product_f32 : dtype == CONV_F16 ? launch_product_f16 : launch_product_bf16;
+    const hipError_t err = launch(g, e, layout, plan.form, plan.splits, s);
+    if (err != hipSuccess || plan.splits == 1) return err;
+    return join(dtype, e, partial, M, (int)N, plan.splits, s);
+}
+size_t partial_bytes(const ProductPlan& p, int64_t M, int64_t N) { return p.splits > 1 ? (size_t)p.splits * M * N * 4 : 0; }
+
+template <int DT, int RB, int W, int U, bool DIRECT>
+hipError_t launch_rows(const LinearRows& g, int splits, hipStream_t s)
+{
+    constexpr size_t LDS = (size_t)W * (1 + RB) * U * 1024;
+    const hipError_t e = ensure_dynamic_lds((const void*)linear_rows<DT, RB, W, U, DIRECT>, LDS);
+    if (e != hipSuccess) return e;
+    // gridDim.y is at most 65535, and a launch holds less than 2^32 threads: the rows go in portions
+    const int64_t across = (g.N + 15) / 16, portion = std::min<int64_t>(65535, std::max<int64_t>(1, (1 << 22) / across)) * (16 * RB);
+    for (int64_t skip = 0; skip < g.rows; skip += portion) {
+        LinearRows p = g;
+        constexpr int ES = sizeof(typename Prec<DT>::elem_t);
+        p.rows = std::min(portion, g.rows - skip);
+        p.x = (const char*)g.x + skip * g.ldx * ES, p.out.out = (char*)g.out.out + skip * g.out.ldo * ES;
+        if (g.out.pre) p.out.pre = (char*)g.out.pre + skip * g.out.ldo * ES;
+        if (g.out.residual) p.out.residual = (const char*)g.out.residual + skip * g.out.ldr * ES;
+        hipLaunchKernelGGL((linear_rows<DT, RB, W, U, DIRECT>), dim3((unsigned)((g.N + 15) / 16), (unsigned)((p.rows + 16 * RB - 1) / (16 * RB)), (unsigned)splits),
+                           dim3(64 * W), LDS, s, p);
+        if (splits > 1) {
+            const hipError_t j = join_as<DT>(p.out, g.partial, p.rows, g.N, splits, s);
+            if (j != hipSuccess) return j;
+        }
+    }
+    return hipGetLastError();
+}
+// Waves a workgroup: a wave has a run of 256 bytes or more up to 1024 and 2048 bytes.
+template <int DT, bool DIRECT>
+hipError_t launch_rows(const LinearRows& g, const RowsPlan& p, hipStream_t s)
+{
+    const bool narrow = (int64_t)g.K * (int)sizeof(typename Prec<DT>::elem_t) <= 1024;
+    switch (p.rb) {
+        case 1: return narrow ? launch_rows<DT, 1, 4, 4, DIRECT>(g, p.splits, s) : launch_rows<DT, 1, 8, 4, DIRECT>(g, p.splits, s);
+        case 2: return narrow ? launch_rows<DT, 2, 4, 2, DIRECT>(g, p.splits, s) : launch_rows<DT, 2, 8, 2, DIRECT>(g, p.splits, s);
+        default: return narrow ? launch_rows<DT, 4, 4, 2, DIRECT>(g, p.splits, s) : launch_rows<DT, 4, 8, 2, DIRECT>(g, p.splits, s);
+    }
+}
+template <int DT>
+hipError_t launch_rows(const LinearRows& g, const LinearForm& f, hipStream_t s)
+{
+    return f.direct ? launch_rows<DT, true>(g, f.few, s) : launch_rows<DT, false>(g, f.few, s);
+}
+
+// ---- the backward pass ----------------------------------------------------------------------------------------------------
+
+// Rows a workgroup of linear_dz takes: as many as give some 1024 workgroups, 64 at least.
+int64_t dz_rows(int64_t rows, int N)
+{
+    const int64_t across = (N + 255) / 256, parts = std::max<int64_t>(1, std::min<int64_t>((1024 + across - 1) / across, rows / 64));
+    return std::max<int64_t>(round_up((rows + parts - 1) / parts, 8), 8);
+}
+int dz_parts(int64_t rows, int N) { return rows == 0 ? 0 : (int)((rows + dz_rows(rows, N) - 1) / dz_rows(rows, N)); }
+
+struct BwdSpace {
+    uint16_t *dz, *x, *w;  // dz in the storage type or in planes; planes of x and w
+    float *sums, *partial;
+    size_t bytes;
+};
+// dz has a place of its own whatever the call needs: the sizes alone say how much a caller keeps.
+BwdSpace bwd_space(const LinearArgs& a, int dtype, void* ws)
+{
+    BwdSpace s = {};
+    Carve c(ws);
+    const bool planes = dtype == CONV_F32;
+    s.dz = (uint16_t*)c.take(planes ? plane_bytes(a.rows, a.N) : (size_t)(2 * a.rows * round_up(a.N, 8)));
+    if (planes) {
+        s.x = (uint16_t*)c.take(plane_bytes(a.rows, a.K));
+        s.w = (uint16_t*)c.take(plane_bytes(a.N, a.K));
+    }
+    s.sums = (float*)c.take((size_t)dz_parts(a.rows, a.N) * a.N * 4);
+    size_t most = 0;
+    for (const bool direct : {true, false}) {
+        most = std::max(most, partial_bytes(plan_product(a.rows, a.K, a.N, planes ? 6 : 1, direct), a.rows, a.K));
+        most = std::max(most, partial_bytes(plan_product(a.N, a.K, a.rows, planes ? 6 : 1, direct), a.N, a.K));
+    }
+    s.partial = (float*)c.take(most);
+    s.bytes = c.used;
+    return s;
+}
+
+template <int DT>
+hipError_t launch_dz(const LinearArgs& a, int to, uint16_t* dz, int64_t ldz, float* sums, hipStream_t s)
+{
+    const int64_t width = to ? ldz : a.N;
+    const int64_t each = dz_rows(a.rows, a.N);
+    const int parts = dz_parts(a.rows, a.N);
+    const dim3 grid((unsigned)((width + 255) / 256), (unsigned)parts);
+    float* const at = !a.dbias ? nullptr : parts == 1 ? a.dbias : sums;
+    if (to == 0) hipLaunchKernelGGL((linear_dz<DT, 0>), grid, dim3(256), 0, s, a.dout, a.pre_in, a.ldo, a.rows, a.N, a.act, dz, ldz, at, each);
+    else if (DT == CONV_F32) hipLaunchKernelGGL((linear_dz<DT, DT == CONV_F32 ? 2 : 1>), grid, dim3(256), 0, s, a.dout, a.pre_in, a.ldo, a.rows, a.N, a.act, dz, ldz, at, each);
+    else hipLaunchKernelGGL((linear_dz<DT, 1>), grid, dim3(256), 0, s, a.dout, a.pre_in, a.ldo, a.rows, a.N, a.act, dz, ldz, at, each);
+    if (a.dbias && parts > 1) hipLaunchKernelGGL(linear_sums, dim3((unsigned)((a.N + 31) / 32)), dim3(256), 0, s, sums, parts, a.N, a.dbias);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+// (the larger of what operands on 16 bytes and others need: what a caller keeps depends on the sizes alone)
+size_t linear_fwd_workspace(int64_t rows, int N, int K, int dtype)
+{
+    if (rows == 0) return 0;
+    size_t most = 0;
+    for (const bool direct : {true, false}) {
+        const LinearForm f = form_of(rows, N, K, dtype, direct);
+        size_t n = 0;
+        if (f.rows) n = f.few.splits > 1 ? (size_t)f.few.splits * rows * N * 4 : 0;
+        else {
+            Carve c(nullptr);
+            if (dtype == CONV_F32) c.take(plane_bytes(rows, K)), c.take(plane_bytes(N, K));
+            c.take(partial_bytes(f.tiles, rows, N));
+            n = c.used;
+        }
+        most = std::max(most, n);
+    }
+    return most;
+}
+size_t linear_bwd_workspace(int64_t rows, int N, int K, int dtype)
+{
+    if (rows == 0) return 0;
+    LinearArgs a = {};
+    a.rows = rows, a.N = N, a.K = K;
+    return bwd_space(a, dtype, nullptr).bytes;
+}
+
+hipError_t launch_linear_fwd(const LinearArgs& a, int dtype, hipStream_t s)
+{
+    const int es = dtype_size(dtype);
+    const LinearForm f = form_of(a.rows, a.N, a.K, dtype, on_16(a.x, a.ldx, es) && on_16(a.w, a.ldw, es));
+    const LinearOut out = {a.bias, a.residual, a.pre, a.out, a.ldr, a.ldo, a.act};
+    if (f.rows) {
+        const LinearRows g = {a.x, a.w, a.ldx, a.ldw, a.rows, a.N, a.K, out, (float*)a.ws};
+        return dtype == CONV_F32 ? launch_rows<CONV_F32>(g, f, s) : dtype == CONV_F16 ? launch_rows<CONV_F16>(g, f, s) : launch_rows<CONV_BF16>(g, f, s);
+    }
+    Carve c(a.ws);
+    Factor x = {a.x, a.ldx, 0}, w = {a.w, a.ldw, 0};
+    if (dtype == CONV_F32) {
+        x.p = c.take(plane_bytes(a.rows, a.K)), w.p = c.take(plane_bytes(a.N, a.K));
+        x.ld = w.ld = plane_stride(a.K), x.plane = a.rows * x.ld, w.plane = a.N * w.ld;
+        hipError_t e = to_planes(a.x, a.ldx, a.rows, a.K, (uint16_t*)x.p, s);
+        if (e == hipSuccess) e = to_planes(a.w, a.ldw, a.N, a.K, (uint16_t*)w.p, s);
+        if (e != hipSuccess) return e;
+    }
+    return multiply(dtype, LAYOUT_NT, x, w, a.rows, a.N, a.K, out, f.tiles, (float*)c.take(partial_bytes(f.tiles, a.rows, a.N)), s);
+}
+
+hipError_t launch_linear_bwd(const LinearArgs& a, int dtype, hipStream_t s)
+{
+    const int es = dtype_size(dtype);
+    if (a.rows == 0) {
+        if (a.dw) hipLaunchKernelGGL(linear_zero, dim3(grid_of((int64_t)a.N * a.K)), dim3(256), 0, s, (char*)a.dw, a.ldw * es, (int64_t)a.N, (int64_t)a.K * es);
+        if (a.dbias) hipLaunchKernelGGL(linear_zero, dim3(grid_of(a.N)), dim3(256), 0, s, (char*)a.dbias, (int64_t)a.N * 4, (int64_t)1, (int64_t)a.N * 4);
+        return hipGetLastError();
+    }
+    const BwdSpace space = bwd_space(a, dtype, a.ws);
+    const bool planes = dtype == CONV_F32, products = a.dx || a.dw;
+    Factor dz = {a.dout, a.ldo, 0}, x = {a.x, a.ldx, 0}, w = {a.w, a.ldw, 0};
+    // dout is dz where there is no activation and its rows start on 16 bytes
+    const bool make = products && (planes || a.act || !on_16(a.dout, a.ldo, es));
+    if (make) {
+        dz.p = space.dz, dz.ld = planes ? plane_stride(a.N) : round_up(a.N, 8), dz.plane = a.rows * dz.ld;
+    }
+    if (make || a.dbias) {
+        const int to = !make ? 0 : planes ? 2 : 1;
+        const hipError_t e = planes ? launch_dz<CONV_F32>(a, to, space.dz, dz.ld, space.sums, s)
+                                    : dtype == CONV_F16 ? launch_dz<CONV_F16>(a, to, space.dz, dz.ld, space.sums, s) : launch_dz<CONV_BF16>(a, to, space.dz, dz.ld, space.sums, s);
+        if (e != hipSuccess) return e;
+    }
+    if (planes && a.dx) {
+        w = {space.w, plane_stride(a.K), (int64_t)a.N * plane_stride(a.K)};
+        const hipError_t e = to_planes(a.w, a.ldw, a.N, a.K, space.w, s);
+        if (e != hipSuccess) return e;
+    }
+    if (planes && a.dw) {
+        x = {space.x, plane_stride(a.K), a.rows * plane_stride(a.K)};
+        const hipError_t e = to_planes(a.x, a.ldx, a.rows, a.K, space.x, s);
+        if (e != hipSuccess) return e;
+    }
+    const int segments = planes ? 6 : 1;
+    if (a.dx) {
+        const ProductPlan p = plan_product(a.rows, a.K, a.N, segments, planes || (on_16(w.p, w.ld, es) && on_16(dz.p, dz.ld, es)));
+        const hipError_t e = multiply(dtype, LAYOUT_NN, dz, w, a.rows, a.K, a.N, {nullptr, nullptr, nullptr, a.dx, 0, a.ldx, ACT_NONE}, p, space.partial, s);
+        if (e != hipSuccess) return e;
+    }
+    if (a.dw) {
+        const ProductPlan p = plan_product(a.N, a.K, a.rows, segments, planes || (on_16(x.p, x.ld, es) && on_16(dz.p, dz.ld, es)));
+        const hipError_t e = multiply(dtype, LAYOUT_TN, dz, x, a.N, a.K, a.rows, {nullptr, nullptr, nullptr, a.dw, 0, a.ldw, ACT_NONE}, p, space.partial, s);
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
+int linear_form_name(const LinearArgs& a, int dtype, int which, char* buf, size_t n)
+{
+    static const char* const tiles[] = {"tile64x64", "tile128x128", "tile256x256", "tile64x64_any", "tile128x128_any"};
+    const int es = dtype_size(dtype);
+    const bool planes = dtype == CONV_F32, x16 = on_16(a.x, a.ldx, es), w16 = on_16(a.w, a.ldw, es);
+    ProductPlan p;
+    if (which == 0) {
+        const LinearForm f = form_of(a.rows, a.N, a.K, dtype, x16 && w16);
+        if (f.rows) {
+            const int len = std::snprintf(buf, n, "rows%d%s", 16 * f.few.rb, f.direct ? "" : "_any");
+            return f.few.splits > 1 && len > 0 && (size_t)len < n ? std::snprintf(buf + len, n - len, "_split%d", f.few.splits) : len;
+        }
+        p = f.tiles;
+    } else if (which == 1) {
+        p = plan_product(a.rows, a.K, a.N, planes ? 6 : 1, planes || w16);
+    } else {
+        p = plan_product(a.N, a.K, a.rows, planes ? 6 : 1, planes || x16);
+    }
+    const int len = std::snprintf(buf, n, "%s%s", planes ? "planes_" : "", tiles[p.form]);
+    return p.splits > 1 && len > 0 && (size_t)len < n ? std::snprintf(buf + len, n - len, "_split%d", p.splits) : len;
+}
+
+}  // namespace convfwd

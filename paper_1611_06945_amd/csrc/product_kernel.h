@@ -1,0 +1,466 @@
+// Matrix products in 16 bits with fp32 sums, and what is done with a tile of sums before it leaves: the core of the linear layers, their
+// gradients and the Newton-Schulz update.
+//
+//   C[m][n] = sum_k A(m, k) B(n, k)
+//
+// Either operand lies along the reduction (ALONG: A(m, k) at m ld + k, as x and w do forward) or across it (ACROSS: at k ld + m, as w does in
+// the gradient of x, and both do in the gradient of w).  Tiles of BT x BN, both operands staged through LDS in steps of 64 of the
+// reduction (128 bytes), multiplied by 16x16x32 matrix instructions, with n along the registers: a lane has 4 consecutive n of row m = lane % 16.
+//   * ALONG: a stage holds 128 bytes of each row, its eight 16-byte pieces at piece ^ (row / 2 % 8), so that the 16 lanes that LDS serves
+//     together read 16 different groups of four banks.
+//   * ACROSS: a stage holds 64 rows of BT elements; an operand is read by two transposing LDS reads of 4 k x 16 m, each lane 8 bytes.  Such a
+//     read of a wave touches 32 bytes of 16 rows; pairs of pieces are stored at pair ^ swizzle(k), so that 8 rows lie in all 64 banks.
+//   * DIRECT: loads that write LDS themselves, from operands whose rows start on 16 bytes; what is past an operand's end is read as zeros by
+//     the bounds check of the buffer descriptor, which moves along with the reduction, so that offsets stay below 2^31 however long it is.  A row's
+//     bytes past K belong to what follows and are cleared in both operands on the last step.  Otherwise pieces go
+//     through registers, from any address, and their ends are cleared on the way.
+//   * fp32 operands are sums of three bf16 planes each, of which six products count; a product over planes is a reduction of `segments` times
+//     the length, the smallest terms first.
+#pragma once
+
+#include <algorithm>
+#include <cmath>
+#include <type_traits>
+
+#include "rows_common.h"
+
+namespace convfwd {
+
+typedef __attribute__((address_space(3))) void lds_void_t;
+
+template <int N, typename F>
+__device__ __forceinline__ void count_to(F f)
+{
+    if constexpr (N > 0) {
+        count_to<N - 1>(f);
+        f(std::integral_constant<int, N - 1>());
+    }
+}
+
+template <int WT_, int WN_, int FT_, int FN_, int S_>
+struct ProductTile {
+    static constexpr int WT = WT_, WN = WN_, FT = FT_, FN = FN_, S = S_;  // waves and 16-wide blocks a wave, along m and n; stages
+    static constexpr int BT = 16 * WT * FT, BN = 16 * WN * FN, NT = 64 * WT * WN;
+    static constexpr int KB = 128, KE = KB / 2;  // of a step, bytes and elements
+    static constexpr int STAGE = (BT + BN) * KB;
+    static constexpr size_t LDS = (size_t)S * STAGE + BN * 4;
+    static constexpr int LA = BT * 8 / NT, LW = BN * 8 / NT;  // 16-byte loads a thread and stage
+    static constexpr int H = FT > 4 ? 2 : 1, HB = FT / H;     // the blocks of m go in H portions
+    static_assert(S >= 2, "a stage to multiply, one to load");
+    static_assert(LA * NT == BT * 8 && LW * NT == BN * 8 && FN % 2 == 0 && HB * H == FT, "whole loads and portions");
+};
+
+// Where pair p of 16-byte pieces of row k is stored in a stage of an operand that lies across the reduction: 2 p ^ this.
+template <int W>
+__device__ __forceinline__ int across_swizzle(int k)
+{
+    return W >= 128 ? ((k & 3) | ((k >> 3) & 1) << 2) * 2 : (((k >> 1) & 1) | ((k >> 3) & 1) << 1) * 2;
+}
+
+// The first `n` elements of 8 (n may be <= 0 or >= 8), the others zero.
+__device__ __forceinline__ u32x4 first_elems(u32x4 v, int n)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int have = n - 2 * i;
+        v[i] = have >= 2 ? v[i] : have <= 0 ? 0u : v[i] & 0xFFFFu;
+    }
+    return v;
+}
+
+template <int DT>
+__device__ __forceinline__ f32x4 multiply16(u32x4 b, u32x4 a, f32x4 c)
+{
+    if constexpr (DT == CONV_F16)
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, b), __builtin_bit_cast(f16x8, a), c, 0, 0, 0);
+    else
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, b), __builtin_bit_cast(bf16x8, a), c, 0, 0, 0);
+}
+
+// 16 bytes a lane from offset `off` of a descriptor to LDS, the wave's 1024 bytes from `to`.  It is the instruction of
+// __builtin_amdgcn_raw_ptr_buffer_load_lds, written out because the compiler lets no transposing LDS read (a builtin that may read anything)
+// pass such a builtin without waiting for all of them: a step's loads would have a quarter of the step to arrive.  It has no
+// output register; what it writes is waited for by count and barrier below, and its operands are read when it is issued.
+__device__ __forceinline__ void load_to_lds(u32x4 r, uint32_t to, uint32_t off)
+{
+    asm volatile("s_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"{m0}"(to), "v"(off), "s"(r));
+}
+
+// One operand of a tile.  W: its width (BT or BN), L: pieces a thread and stage.
+template <typename T, int W, int L, bool ACROSS, bool DIRECT>
+struct Operand {
+    const uint16_t* base;  // the tile's first element, k = 0, first plane
+    int64_t ld, plane, K;
+    int here;              // rows (ALONG) or columns (ACROSS) of the tile that exist
+    const uint16_t* from;  // the next step
+    int64_t left;          // DIRECT: bytes from there to the operand's end, in whole pieces; otherwise steps of the reduction
+    uint32_t off[DIRECT ? L : 1];
+    u32x4 held[DIRECT ? 1 : L];
+
+    static __device__ __forceinline__ void place(int i, int& row, int& piece)
+    {
+        const int p = i * T::NT + (int)threadIdx.x;
+        if constexpr (ACROSS) {
+            row = p / (W / 8), piece = (p % (W / 8)) ^ across_swizzle<W>(row);
+        } else {
+            row = p / 8, piece = (p % 8) ^ ((row >> 1) & 7);
+        }
+    }
+    __device__ __forceinline__ void begin(const uint16_t* p, int64_t stride, int64_t plane_, int64_t K_, int64_t first, int64_t all)
+    {
+        ld = stride, plane = plane_, K = K_;
+        here = (int)min((int64_t)W, all - first);
+        base = p + (ACROSS ? first : first * stride);
+        if constexpr (DIRECT) {
+#pragma unroll
+            for (int i = 0; i < L; ++i) {
+                int row, piece;
+                place(i, row, piece);
+                off[i] = (uint32_t)row * (uint32_t)(stride * 2) + piece * 16;
+            }
+        }
+    }
+    // the next step is step k of plane q
+    __device__ __forceinline__ void seek(int k, int q)
+    {
+        const int64_t k0 = (int64_t)k * T::KE;
+        from = base + q * plane + (ACROSS ? k0 * ld : k0);
+        // (the rows start on 16 bytes, so what the last piece holds past the end lies in the same 16 bytes as an element)
+        if constexpr (DIRECT) left = ((ACROSS ? (K - 1 - k0) * ld + here : (here - 1) * ld + (K - k0)) * 2 + 15) & ~(int64_t)15;
+        else left = K - k0;
+    }
+    __device__ __forceinline__ void advance()
+    {
+        const int64_t by = ACROSS ? T::KE * ld : T::KE;
+        from += by;
+        left -= DIRECT ? by * 2 : T::KE;
+    }
+    // the next step to the stage at `lds` (DIRECT; no step: nothing but zeros), or to registers
+    __device__ __forceinline__ void load(char* lds, bool step)
+    {
+        if constexpr (DIRECT) {
+            const uint64_t at = (uint64_t)(uintptr_t)from;
+            const uint32_t bytes = !step || left <= 0 ? 0u : (uint32_t)min(left, (int64_t)0x7FFFFFF0);
+            const u32x4 r = {(uint32_t)at, (uint32_t)(at >> 32), bytes, 0x00020000u};
+            const uint32_t to = (uint32_t)(uintptr_t)(lds_void_t*)lds + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * 1024;
+#pragma unroll
+            for (int i = 0; i < L; ++i) load_to_lds(r, to + i * T::NT * 16, off[i]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < L; ++i) {
+                int row, piece;
+                place(i, row, piece);
+                const uint16_t* p = from + (int64_t)row * ld + piece * 8;
+                const int64_t n = !step ? 0 : ACROSS ? (row < left ? here - piece * 8 : 0) : (row < here ? left - piece * 8 : 0);
+                u32x4 v = {0, 0, 0, 0};
+                if (n >= 8) {
+                    __builtin_memcpy(&v, p, 16);
+                } else if (n > 0) {
+                    uint16_t e[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) e[j] = j < n ? p[j] : (uint16_t)0;
+                    __builtin_memcpy(&v, e, 16);
+                }
+                held[i] = v;
+            }
+        }
+    }
+    __device__ __forceinline__ void commit(char* lds) const
+    {
+        if constexpr (!DIRECT) {
+#pragma unroll
+            for (int i = 0; i < L; ++i) *(u32x4*)(lds + (i * T::NT + (int)threadIdx.x) * 16) = held[i];
+        }
+    }
+    // the matrix operand of block `block` (16 wide) for half s of a stage
+    static __device__ __forceinline__ u32x4 fragment(const char* lds, int block, int s)
+    {
+        const int lane = threadIdx.x & 63;
+        if constexpr (ACROSS) {
+            typedef short s16x4 __attribute__((ext_vector_type(4)));
+            typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+            const int k = (lane >> 4) * 8 + ((lane & 15) >> 2);
+            const char* p = lds + (s * 32 + k) * (W * 2) + ((block * 2) ^ across_swizzle<W>(k)) * 16 + (lane & 3) * 8;
+            union {
+                s16x4 h[2];
+                u32x4 v;
+            } u;
+            u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)p);
+            u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 4 * W * 2));
+            return u.v;
+        } else {
+            return *(const u32x4*)(lds + block * 16 * T::KB + (lane & 15) * T::KB + (((s * 4 + (lane >> 4)) ^ ((lane >> 1) & 7)) << 4));
+        }
+    }
+};
+
+struct ProductArgs {
+    const uint16_t *a, *b;
+    int64_t lda, ldb;             // of operands, in elements of 16 bits
+    int64_t plane_a, plane_b;     // distance of an operand's planes
+    int64_t M, N, K;
+    int64_t m_first;              // what the first row of these M is in the whole product
+    uint32_t seg_a, seg_b;        // plane of each segment, two bits each
+    int segments;
+    int ksteps, each;             // steps of a segment, and of a workgroup that shares it with others (gridDim.z)
+    int64_t batch_a, batch_b;     // distances of the batch's matrices (gridDim.y)
+    int tiles_m, tiles_n;
+    float* partial;               // sums of gridDim.z workgroups, [z][M][N]
+};
+
+// Epi: what becomes of the sums.  symmetric: only the tiles with n >= m are formed.
+template <int DT, typename T, bool A_ACROSS, bool B_ACROSS, bool DIRECT, typename Epi>
+__global__ __launch_bounds__(T::NT) void product_kernel(ProductArgs g, typename Epi::Args e)
+{
+    extern __shared__ __attribute__((aligned(16))) char smem[];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wt = wave % T::WT, wn = wave / T::WT;
+
+    // consecutive workgroups go to different XCDs: each XCD takes a run of tiles, in bands of eight tiles of n
+    int tm, tn;
+    {
+        const int total = gridDim.x;
+        int tile = blockIdx.x;
+        const int q = total / 8, r = total % 8, x = tile % 8, i = tile / 8;
+        tile = x * q + min(x, r) + i;
+        if constexpr (Epi::SYMMETRIC) {
+            // row tm has the tiles tm .. tiles_m - 1
+            tm = 0;
+            for (int left = g.tiles_m; tile >= left; --left) tile -= left, ++tm;
+            tn = tm + tile;
+        } else {
+            const int band = tile / (8 * g.tiles_m), in_band = tile - band * 8 * g.tiles_m;
+            const int width = min(8, g.tiles_n - band * 8);
+            tn = band * 8 + in_band % width, tm = in_band / width;
+        }
+    }
+    const int64_t m0 = (int64_t)tm * T::BT, n0 = (int64_t)tn * T::BN;
+    const int ks0 = blockIdx.z * g.each, ks1 = min(ks0 + g.each, g.ksteps);
+
+    Operand<T, T::BT, T::LA, A_ACROSS, DIRECT> a;
+    Operand<T, T::BN, T::LW, B_ACROSS, DIRECT> b;
+    a.begin(g.a + blockIdx.y * g.batch_a, g.lda, g.plane_a, g.K, m0, g.M);
+    b.begin(g.b + blockIdx.y * g.batch_b, g.ldb, g.plane_b, g.K, n0, g.N);
+    float* const bias = (float*)(smem + T::S * T::STAGE);
+    Epi::prepare(e, bias, n0, b.here, T::BN, T::NT);
+
+    const int steps = (ks1 - ks0) * g.segments;
+    int ks = ks0, seg = 0;  // the next step to load
+    a.seek(ks, g.seg_a & 3), b.seek(ks, g.seg_b & 3);
+    auto load = [&](int buf) {
+        char* const to = smem + buf * T::STAGE;
+        const bool step = ks < ks1;
+        a.load(to, step);
+        b.load(to + T::BT * T::KB, step);
+    };
+    auto move = [&]() {  // (apart from load(): its branch would end the stretch of code in which loads and products are interleaved)
+        ++ks;
+        if (ks == ks1 && seg + 1 < g.segments) {
+            ks = ks0, ++seg;
+            a.seek(ks, (g.seg_a >> (2 * seg)) & 3), b.seek(ks, (g.seg_b >> (2 * seg)) & 3);
+        } else {
+            a.advance(), b.advance();
+        }
+    };
+
+    f32x4 acc[T::FN][T::FT];
+#pragma unroll
+    for (int i = 0; i < T::FN; ++i)
+#pragma unroll
+        for (int j = 0; j < T::FT; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+
+    u32x4 av[2][T::HB], bv[2][T::FN];
+    // The operands of phase p of a stage (half p / H, portion p % H of the rows) to the registers of its parity.
+    auto fetch = [&](int buf, auto phase) {
+        constexpr int p = decltype(phase)::value, s = p / T::H, h = p % T::H;
+        const char* const at = smem + buf * T::STAGE;
+        if constexpr (h == 0) {
+#pragma unroll
+            for (int i = 0; i < T::FN; ++i) bv[s][i] = b.fragment(at + T::BT * T::KB, wn * T::FN + i, s);
+        }
+#pragma unroll
+        for (int j = 0; j < T::HB; ++j) av[p & 1][j] = a.fragment(at, wt * T::FT + h * T::HB + j, s);
+    };
+    auto products = [&](auto phase) {
+        constexpr int p = decltype(phase)::value, s = p / T::H, h = p % T::H;
+#pragma unroll
+        for (int j = 0; j < T::HB; ++j)
+#pragma unroll
+            for (int i = 0; i < T::FN; ++i) acc[i][h * T::HB + j] = multiply16<DT>(bv[s][i], av[p & 1][j], acc[i][h * T::HB + j]);
+    };
+    constexpr int PHASES = 2 * T::H, LOADS = T::LA + T::LW;
+    typedef std::integral_constant<int, 0> First;
+    typedef std::integral_constant<int, PHASES - 1> Last;
+
+    if constexpr (DIRECT) {
+        // Order of a phase of many products: after every few one of its LDS reads, then one of its loads, so that products begin at
+        // once.  With few products the reads come first, or they would be late.
+        constexpr bool MIXED = T::HB * T::FN >= 16;
+        constexpr int READS_A = T::HB * (A_ACROSS ? 2 : 1), READS_B = T::FN * (B_ACROSS ? 2 : 1);
+        auto interleave = [&](auto reads, auto loads) {
+            constexpr int R = decltype(reads)::value, L = decltype(loads)::value, M = T::HB * T::FN, EACH = MIXED ? M / (R + L) : 1;
+            if constexpr (MIXED && EACH > 0) {
+                count_to<R>([&](auto) {
+                    __builtin_amdgcn_sched_group_barrier(0x008, EACH, 0);  // products
+                    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);     // an LDS read
+                });
+                count_to<L>([&](auto) {
+                    __builtin_amdgcn_sched_group_barrier(0x008, EACH, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);     // a load
+                });
+                if constexpr (M > EACH * (R + L)) __builtin_amdgcn_sched_group_barrier(0x008, M - EACH * (R + L), 0);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        auto reads_first = [&]() {
+            if constexpr (!MIXED) __builtin_amdgcn_sched_barrier(0);
+        };
+        // Steps past the last are asked for as well, without a byte in range, so that the count of loads on their way is always the same.
+#pragma unroll
+        for (int k = 0; k < T::S; ++k) load(k), move();
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((T::S - 1) * LOADS) : "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        fetch(0, First());
+        int buf = 0;
+        for (int k = 0; k < steps - 1; ++k) {
+            count_to<PHASES - 1>([&](auto p) {
+                fetch(buf, std::integral_constant<int, decltype(p)::value + 1>());
+                reads_first();
+                products(p);
+                interleave(std::integral_constant<int, READS_A + ((decltype(p)::value + 1) % T::H == 0 ? READS_B : 0)>(), std::integral_constant<int, 0>());
+            });
+            // this wave's loads of the next stage have landed and its reads of the present one are done; then so are everybody's
+            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((T::S - 2) * LOADS) : "memory");
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            const int next = buf + 1 == T::S ? 0 : buf + 1;
+            fetch(next, First());
+            load(buf);
+            reads_first();
+            products(Last());
+            interleave(std::integral_constant<int, READS_A + READS_B>(), std::integral_constant<int, LOADS>());
+            move();
+            buf = next;
+        }
+        // (planes end with zeros up to a whole step)
+        const int tail = g.segments > 1 || ks1 < g.ksteps ? T::KE : (int)(g.K - (int64_t)(g.ksteps - 1) * T::KE);
+        count_to<PHASES>([&](auto p) {
+            constexpr int q = decltype(p)::value, s = q / T::H;
+            if constexpr (q + 1 < PHASES) fetch(buf, std::integral_constant<int, q + 1>());
+            const int left = tail - (s * 4 + (lane >> 4)) * 8;
+            if constexpr (q % T::H == 0 && !B_ACROSS) {
+#pragma unroll
+                for (int i = 0; i < T::FN; ++i) bv[s][i] = first_elems(bv[s][i], left);
+            }
+            if constexpr (!A_ACROSS) {
+#pragma unroll
+                for (int j = 0; j < T::HB; ++j) av[q & 1][j] = first_elems(av[q & 1][j], left);
+            }
+            products(p);
+        });
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // nothing may land in LDS after the end
+    } else {
+        static_assert(DIRECT || T::S == 2, "one stage is multiplied, the other written");
+        auto commit = [&](int buf) {
+            a.commit(smem + buf * T::STAGE);
+            b.commit(smem + buf * T::STAGE + T::BT * T::KB);
+        };
+        load(0), move();
+        commit(0);
+        load(1), move();
+        __syncthreads();
+        for (int k = 0; k < steps; ++k) {
+            fetch(k & 1, First());
+            count_to<PHASES>([&](auto p) {
+                constexpr int q = decltype(p)::value;
+                if constexpr (q + 1 < PHASES) fetch(k & 1, std::integral_constant<int, q + 1>());
+                products(p);
+            });
+            if (k + 1 < steps) {
+                commit((k + 1) & 1);
+                load(k & 1), move();
+            }
+            __syncthreads();
+        }
+    }
+
+    // A lane has four n 4 (lane / 16) .. of a block and m = lane % 16 of a block of rows.  Neighbouring groups of 16 lanes trade between two
+    // blocks of n, so that a lane has eight n in a row: the groups 0 .. 3 those of block i from 0, of block i + 1 from 0, of block i from 8,
+    // of block i + 1 from 8.
+    const int grp = lane >> 4;
+#pragma unroll
+    for (int i = 0; i < T::FN; i += 2) {
+        const int nl = (wn * T::FN + i) * 16 + (grp & 1) * 16 + (grp >> 1) * 8;
+#pragma unroll
+        for (int j = 0; j < T::FT; ++j) {
+            const int ml = (wt * T::FT + j) * 16 + (lane & 15);
+            float v[8];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const float here = acc[i][j][r], there = acc[i + 1][j][r];  // (a cast of a vector's element itself takes the first one)
+                const auto two = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, here), __builtin_bit_cast(uint32_t, there), false, false);
+                v[r] = __builtin_bit_cast(float, (uint32_t)two[0]), v[4 + r] = __builtin_bit_cast(float, (uint32_t)two[1]);
+            }
+            if (ml < a.here && nl < b.here) Epi::finish(g, e, v, g.m_first + m0 + ml, n0 + nl, min(8, b.here - nl), bias + nl);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    }
+}
+
+// Eight neighbouring elements (n of them exist), to or from a row that starts at any element.
+template <int DT>
+__device__ __forceinline__ void put8(void* row, int64_t at, const float (&v)[8], int n)
+{
+    typedef Piece<DT> P;
+    typename P::elem_t* p = (typename P::elem_t*)row + at;
+    constexpr int VEC = P::VEC;
+#pragma unroll
+    for (int c = 0; c < 8 / VEC; ++c) {
+        float part[VEC];
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) part[k] = v[c * VEC + k];
+        const uint4 u = P::narrow(part);
+        if (n >= (c + 1) * VEC) {
+            P::put(p + c * VEC, u);
+        } else {
+            typename P::elem_t e[VEC];
+            __builtin_memcpy(e, &u, 16);
+#pragma unroll
+            for (int k = 0; k < VEC; ++k)
+                if (c * VEC + k < n) p[c * VEC + k] = e[k];
+        }
+    }
+}
+template <int DT>
+__device__ __forceinline__ void get8(const void* row, int64_t at, float (&v)[8], int n)
+{
+    typedef Piece<DT> P;
+    const typename P::elem_t* p = (const typename P::elem_t*)row + at;
+    constexpr int VEC = P::VEC;
+#pragma unroll
+    for (int c = 0; c < 8 / VEC; ++c) {
+        if (n >= (c + 1) * VEC) {
+            float part[VEC];
+            P::widen(P::raw(p + c * VEC), part);
+#pragma unroll
+            for (int k = 0; k < VEC; ++k) v[c * VEC + k] = part[k];
+        } else {
+#pragma unroll
+            for (int k = 0; k < VEC; ++k) v[c * VEC + k] = c * VEC + k < n ? Prec<DT>::to_f32(p[c * VEC + k]) : 0.0f;
+        }
+    }
+}
+
+// The sums of workgroups that share a reduction, as they are.
+struct PartialSums {
+    struct Args {};
+    static constexpr bool SYMMETRIC = false;
+    static __device__ __forceinline__ void prepare(const Args&, float*, int64_t, int, int, int) {}
+    static __device__ __forceinline__ void finish(const ProductArgs& g, const Args&, const float (&v)[8], int64_t m, int64_t n, int have, const float*)
+    {
+        put8<CONV_F32>(g.partial, ((int64_t)blockIdx.z * g.M + m) * g.N + n, v, have);
+    }
+};
+
+}  // namespace convfwd

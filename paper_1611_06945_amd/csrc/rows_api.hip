@@ -1,4 +1,4 @@
-// C entry points of the operators on rows: layer norm, row quantiser, 8-bit product, log probabilities.  Arguments are
+// C entry points of the operators on rows: layer norm, row quantiser, 8-bit product, log probabilities, linear layers.  Arguments are
 // checked before the first HIP call; the kernels' launchers choose among their forms.
 #include <algorithm>
 #include <climits>
@@ -50,6 +50,27 @@ int check_int_linear(const int_linear_desc* d)
     if (!spans(d->rows, d->lda, 1) || !spans(d->N, d->ldw, 1) || !spans(d->rows, d->ldo, dtype_size(d->dtype))) return CONV_EINVAL;
     if (d->flags & ~(uint32_t)CONV_FLAG_RELU) return CONV_EINVAL;
     return CONV_OK;
+}
+
+int check_linear(const linear_desc* d)
+{
+    if (!d) return CONV_EINVAL;
+    if (!known(d->dtype)) return CONV_EDTYPE;
+    if (d->rows < 0 || d->rows > kMostRows || d->N < 1 || d->K < 1 || d->N >= (1 << 24) || d->K >= (1 << 24)) return CONV_EINVAL;
+    const int es = dtype_size(d->dtype);
+    if (d->ldx < d->K || d->ldw < d->K || d->ldr < d->N || d->ldo < d->N) return CONV_EINVAL;
+    if (!spans(d->rows, d->ldx, es) || !spans(d->N, d->ldw, es) || !spans(d->rows, d->ldr, es) || !spans(d->rows, d->ldo, es)) return CONV_EINVAL;
+    const uint32_t act = d->flags & (CONV_FLAG_RELU | LINEAR_FLAG_GELU | LINEAR_FLAG_SILU);
+    if (d->flags != act || (act & (act - 1))) return CONV_EINVAL;
+    return CONV_OK;
+}
+
+LinearArgs linear_args(const linear_desc* d)
+{
+    LinearArgs a = {};
+    a.rows = d->rows, a.ldx = d->ldx, a.ldw = d->ldw, a.ldr = d->ldr, a.ldo = d->ldo, a.N = d->N, a.K = d->K;
+    a.act = d->flags & CONV_FLAG_RELU ? 1 : d->flags & LINEAR_FLAG_GELU ? 2 : d->flags & LINEAR_FLAG_SILU ? 3 : 0;
+    return a;
 }
 
 // Runs a launcher; nothing it throws leaves the C interface.
@@ -218,6 +239,66 @@ int logprob_bwd(const logprob_desc* desc, const void* logits, const int64_t* tar
     a.g_logp = g_logp, a.g_entropy = g_entropy, a.dx = dlogits;
     a.rows = desc->rows, a.ldx = desc->ldx, a.ldg = desc->ldg, a.cols = desc->cols;
     return guarded("logprob_bwd", [&] { return launch_logprob_bwd(a, desc->dtype, (hipStream_t)stream); });
+}
+
+size_t linear_workspace_bytes(const linear_desc* desc)
+{
+    return check_linear(desc) ? 0 : linear_fwd_workspace(desc->rows, desc->N, desc->K, desc->dtype);
+}
+
+int linear_fwd(const linear_desc* desc, const void* x, const void* w, const float* bias, const void* residual, void* out, void* pre,
+               void* workspace, size_t workspace_bytes, void* stream)
+{
+    const int rc = check_linear(desc);
+    if (rc) return rc;
+    if (desc->rows == 0) return CONV_OK;
+    const int es = dtype_size(desc->dtype);
+    if (!x || !w || !out || !aligned(x, es) || !aligned(w, es) || !aligned(out, es) || !aligned(residual, es) || !aligned(pre, es) || !vec_ok(bias)) return CONV_EINVAL;
+    if (out == x || out == w || pre == x || pre == w || pre == out || (pre && pre == residual) || (residual == out && desc->ldr != desc->ldo)) return CONV_EINVAL;
+    const size_t need = linear_fwd_workspace(desc->rows, desc->N, desc->K, desc->dtype);
+    if (need && (!workspace || workspace_bytes < need)) return CONV_EWORKSPACE;
+    if (!aligned(workspace, 16)) return CONV_EINVAL;
+    LinearArgs a = linear_args(desc);
+    a.x = x, a.w = w, a.bias = bias, a.residual = residual, a.out = out, a.pre = pre, a.ws = workspace;
+    return guarded("linear_fwd", [&] { return launch_linear_fwd(a, desc->dtype, (hipStream_t)stream); });
+}
+
+size_t linear_bwd_workspace_bytes(const linear_desc* desc)
+{
+    return check_linear(desc) ? 0 : linear_bwd_workspace(desc->rows, desc->N, desc->K, desc->dtype);
+}
+
+int linear_bwd(const linear_desc* desc, const void* x, const void* w, const void* pre, const void* dout, void* dx, void* dw, float* dbias,
+               void* workspace, size_t workspace_bytes, void* stream)
+{
+    const int rc = check_linear(desc);
+    if (rc) return rc;
+    const int es = dtype_size(desc->dtype);
+    LinearArgs a = linear_args(desc);
+    if (!dx && !dw && !dbias) return CONV_EINVAL;
+    if (!aligned(x, es) || !aligned(w, es) || !aligned(pre, es) || !aligned(dout, es) || !aligned(dx, es) || !aligned(dw, es) || !vec_ok(dbias)) return CONV_EINVAL;
+    if (desc->rows > 0) {
+        if (!dout || (dw && !x) || (dx && !w) || (a.act && !pre)) return CONV_EINVAL;
+        if ((dx && (dx == x || dx == w || dx == pre || dx == dout || dx == dw)) || (dw && (dw == x || dw == w || dw == pre || dw == dout))) return CONV_EINVAL;
+        const size_t need = linear_bwd_workspace(desc->rows, desc->N, desc->K, desc->dtype);
+        if (need && (!workspace || workspace_bytes < need)) return CONV_EWORKSPACE;
+        if (!aligned(workspace, 16)) return CONV_EINVAL;
+    }
+    a.x = x, a.w = w, a.pre_in = pre, a.dout = dout, a.dx = dx, a.dw = dw, a.dbias = dbias, a.ws = workspace;
+    return guarded("linear_bwd", [&] { return launch_linear_bwd(a, desc->dtype, (hipStream_t)stream); });
+}
+
+int linear_form(const linear_desc* desc, const void* x, const void* w, int which, char* buf, size_t n)
+{
+    const int rc = check_linear(desc);
+    if (rc) return rc;
+    if (!buf || n == 0 || which < 0 || which > 2) return CONV_EINVAL;
+    buf[0] = 0;
+    if (desc->rows == 0) return CONV_OK;
+    LinearArgs a = linear_args(desc);
+    a.x = x, a.w = w;
+    linear_form_name(a, desc->dtype, which, buf, n);
+    return CONV_OK;
 }
 
 }  // extern "C"
