@@ -79,7 +79,7 @@ def test_linear_bwd_pointers_that_are_refused():
 
 
 def test_linear_workspaces_that_are_refused():
-    d = B.make_linear_desc(3380, 1536, 384)
+    d = B.make_linear_desc(8192, 8192, 4096)
     for call, need in ((fwd, B.linear_workspace_bytes(d)), (bwd, B.linear_bwd_workspace_bytes(d))):
         assert need > 0
         assert call(d, ws=None, n=need) == B.CONV_EWORKSPACE
