@@ -497,6 +497,52 @@ int linear_bwd(const linear_desc* desc, const void* x, const void* w, const void
  * dw.  Empty for no rows.  Pure host code. */
 int linear_form(const linear_desc* desc, const void* x, const void* w, int which, char* buf, size_t n);
 
+/*
+ * What stands between two blocks of rows, in one call: the norm behind a block, its gate and scale, the residual sum, and the norm before the
+ * next block.
+ *   u = norm(h) * gamma_h + beta_h  with RESIDUAL_NORM_POST, else h
+ *   sum[t][j] = r[t][j] + scale[j] * gate[t / gate_rows][j] * u[t][j],   r_out = sum rounded,   y = norm(sum) * gamma + beta
+ * norm is layer norm's (x - mean) * rstd, or with RESIDUAL_NORM_RMS x * rstd with rstd = 1 / sqrt(mean of x^2 + eps); y is formed from the sum before it
+ * is rounded.  gate has a row of `cols` for every gate_rows rows (1: each row its own; the last may stand for fewer; 0: no gate,
+ * and the pointer is NULL); with RESIDUAL_NORM_SIGMOID it multiplies as 1 / (1 + exp(-gate)).  gamma_h, beta_h (NULL without RESIDUAL_NORM_POST), scale,
+ * gamma, beta: fp32 [cols], NULL = ones, zeros, ones, ones, zeros.  y may be NULL (no norm behind).  stats: fp32 [rows][4], 16-byte aligned,
+ * receives mean and rstd of h and mean and rstd of the sum (0 and 1 where there is no norm, 0 for means under RMS); may be NULL.
+ * r_out may be r.  Row strides: ldr of r, r_out, dr, dr_out; ldh of h, dh; ldg of gate, dgate; ldy of y, dy.
+ * CONV_EINVAL for rows or gate_rows < 0, cols < 1 or >= 2^30, strides below cols (ldg only with a gate), eps < 0, infinite or NaN, unknown flags, a gate without gate_rows
+ * or the reverse, NULL or misaligned pointers, other outputs that are inputs.
+ */
+#define RESIDUAL_NORM_RMS 1u
+#define RESIDUAL_NORM_POST 2u
+#define RESIDUAL_NORM_SIGMOID 4u
+typedef struct {
+    int64_t rows;
+    int64_t ldr, ldh, ldg, ldy; /* row strides in elements */
+    int32_t gate_rows;
+    int32_t cols;
+    int32_t dtype;              /* conv_dtype of r, r_out, h, gate, y and their gradients */
+    float eps;
+    uint32_t flags;
+} residual_norm_desc;
+int residual_norm_fwd(const residual_norm_desc* desc, const void* r, const void* h, const void* gate, const float* gamma_h,
+                      const float* beta_h, const float* scale, const float* gamma, const float* beta, void* r_out, void* y,
+                      float* stats, void* stream);
+
+/*
+ * Its gradients from dr_out and dy (either may be NULL: zeros) with r_out and stats as the forward pass left them: with xh and hh the normed rows,
+ *   dr = dr_out + rstd * (dy gamma - avg(dy gamma) - xh avg(dy gamma xh)),   p = dr * gate,
+ *   dh = rstd_h * (g - avg(g) - hh avg(g hh)) with g = p * scale * gamma_h  (p * scale without RESIDUAL_NORM_POST; no avg(.) of its own under RMS),
+ *   dgate = sum over the rows that share it of dr * scale * u (times s (1 - s) for a sigmoid s),
+ *   dgamma_h = sum_t p scale hh,  dbeta_h = sum_t p scale,  dscale = sum_t p u,  dgamma = sum_t dy xh,  dbeta = sum_t dy.
+ * Any output may be NULL, not all; no output is an input.  r_out is read where dy is given, stats there and with RESIDUAL_NORM_POST.  Sums over rows are
+ * fp32, in `workspace` (residual_norm_bwd_workspace_bytes(desc), 16-byte aligned; CONV_EWORKSPACE if it is smaller).  rows = 0 gives zero sums.
+ * Gradients of the vectors go with what they belong to: dgamma_h and dbeta_h with RESIDUAL_NORM_POST, dgate with a gate.
+ */
+size_t residual_norm_bwd_workspace_bytes(const residual_norm_desc* desc);
+int residual_norm_bwd(const residual_norm_desc* desc, const void* r_out, const void* h, const void* gate, const float* gamma_h,
+                      const float* beta_h, const float* scale, const float* gamma, const float* stats, const void* dr_out,
+                      const void* dy, void* dr, void* dh, void* dgate, float* dgamma_h, float* dbeta_h, float* dscale,
+                      float* dgamma, float* dbeta, void* workspace, size_t workspace_bytes, void* stream);
+
 /* Text for a conv_status; for CONV_EHIP it includes the message of the last failed HIP call of this thread. */
 const char* conv_strerror(int status);
 

@@ -129,3 +129,54 @@ def linear_bwd(x, w, pre, dout, act):
     """-> (dx, dw, dbias)."""
     dz = dout if act == "none" else dout * activation(pre, act)[1]
     return dz @ w, dz.T @ x, dz.sum(0)
+
+
+def row_norm(x, rms, eps):
+    """-> (normed rows, mean, rstd)."""
+    mean = np.zeros(len(x)) if rms else x.mean(1)
+    rstd = 1.0 / np.sqrt(((x - mean[:, None]) ** 2).mean(1) + eps)
+    return (x - mean[:, None]) * rstd[:, None], mean, rstd
+
+
+def residual_norm(r, h, gate, gate_rows, sigmoid, gamma_h, beta_h, scale, gamma, beta, post, rms, eps):
+    """-> (sum, y, stats, branch): branch is what was added to r.  gamma_h .. beta are arrays, or None for ones or zeros."""
+    one = lambda v: 1.0 if v is None else v  # noqa: E731
+    zero = lambda v: 0.0 if v is None else v  # noqa: E731
+    u, mean_h, rstd_h = row_norm(h, rms, eps) if post else (h, np.zeros(len(h)), np.ones(len(h)))
+    if post:
+        u = u * one(gamma_h) + zero(beta_h)
+    if gate is not None:
+        g = gate[np.arange(len(h)) // gate_rows]
+        u = u * (1.0 / (1.0 + np.exp(-g)) if sigmoid else g)
+    branch = u * one(scale)
+    xh, mean, rstd = row_norm(r + branch, rms, eps)
+    return r + branch, xh * one(gamma) + zero(beta), np.stack([mean_h, rstd_h, mean, rstd], 1), branch
+
+
+def residual_norm_bwd(x, h, gate, gate_rows, sigmoid, gamma_h, beta_h, scale, gamma, stats, dr_out, dy, post, rms):
+    """-> dict of dr, dh, dgate, dgamma_h, dbeta_h, dscale, dgamma, dbeta."""
+    one = lambda v: 1.0 if v is None else v  # noqa: E731
+    zero = lambda v: 0.0 if v is None else v  # noqa: E731
+
+    def through(g, xh, rstd):
+        return rstd[:, None] * (g - (0.0 if rms else g.mean(1)[:, None]) - xh * (g * xh).mean(1)[:, None])
+
+    out = {}
+    xh = (x - stats[:, 2:3]) * stats[:, 3:4]
+    out["dr"] = dr = dr_out + through(dy * one(gamma), xh, stats[:, 3])
+    out["dgamma"], out["dbeta"] = (dy * xh).sum(0), dy.sum(0)
+    hh = (h - stats[:, 0:1]) * stats[:, 1:2] if post else h
+    u = hh * one(gamma_h) + zero(beta_h) if post else h
+    p = dr
+    if gate is not None:
+        at = np.arange(len(h)) // gate_rows
+        s = 1.0 / (1.0 + np.exp(-gate)) if sigmoid else gate
+        d = np.zeros_like(gate)
+        np.add.at(d, at, dr * u * one(scale))
+        out["dgate"] = d * s * (1.0 - s) if sigmoid else d
+        p = dr * s[at]
+    du = p * one(scale)
+    out["dscale"] = (p * u).sum(0)
+    out["dgamma_h"], out["dbeta_h"] = (du * hh).sum(0), du.sum(0)
+    out["dh"] = through(du * one(gamma_h), hh, stats[:, 1]) if post else du
+    return out

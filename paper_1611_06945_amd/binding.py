@@ -23,6 +23,7 @@ CONV_FLAG_RELU, CONV_FLAG_IN_NHWC, CONV_FLAG_OUT_NHWC, CONV_FLAG_FILT_KRSC, CONV
 CONV_FLAG_MAXPOOL_3X3S2 = 32
 CONV_FLAG_FILT_PACKED = 64
 LINEAR_FLAG_GELU, LINEAR_FLAG_SILU = 0x100, 0x200
+RESIDUAL_NORM_RMS, RESIDUAL_NORM_POST, RESIDUAL_NORM_SIGMOID = 1, 2, 4
 CONV_STATIC_SCRATCH_BYTES = 32 << 20
 CONV_OK, CONV_EINVAL, CONV_EDTYPE, CONV_EWORKSPACE, CONV_EHIP, CONV_ENOVARIANT, CONV_EIO = 0, -1, -2, -3, -4, -5, -6
 
@@ -69,6 +70,11 @@ class logprob_desc(ctypes.Structure):
 class linear_desc(ctypes.Structure):
     _fields_ = [("rows", ctypes.c_int64), ("ldx", ctypes.c_int64), ("ldw", ctypes.c_int64), ("ldr", ctypes.c_int64), ("ldo", ctypes.c_int64),
                 ("N", ctypes.c_int32), ("K", ctypes.c_int32), ("dtype", ctypes.c_int32), ("flags", ctypes.c_uint32)]
+
+
+class residual_norm_desc(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("ldr", ctypes.c_int64), ("ldh", ctypes.c_int64), ("ldg", ctypes.c_int64), ("ldy", ctypes.c_int64),
+                ("gate_rows", ctypes.c_int32), ("cols", ctypes.c_int32), ("dtype", ctypes.c_int32), ("eps", ctypes.c_float), ("flags", ctypes.c_uint32)]
 
 
 class ConvError(RuntimeError):
@@ -187,6 +193,13 @@ def lib() -> ctypes.CDLL:
         L.linear_bwd.restype = ctypes.c_int
         L.linear_form.argtypes = [lp, vp, vp, ctypes.c_int, ctypes.c_char_p, sz]
         L.linear_form.restype = ctypes.c_int
+        rp = ctypes.POINTER(residual_norm_desc)
+        L.residual_norm_fwd.argtypes = [rp] + [vp] * 12
+        L.residual_norm_fwd.restype = ctypes.c_int
+        L.residual_norm_bwd_workspace_bytes.argtypes = [rp]
+        L.residual_norm_bwd_workspace_bytes.restype = sz
+        L.residual_norm_bwd.argtypes = [rp] + [vp] * 19 + [sz, vp]
+        L.residual_norm_bwd.restype = ctypes.c_int
         L.conv_strerror.argtypes = [ctypes.c_int]
         L.conv_strerror.restype = ctypes.c_char_p
         _lib = L
@@ -516,6 +529,29 @@ def linear_form(desc, x=None, w=None, which=0) -> str:
     buf = ctypes.create_string_buffer(64)
     _check(lib().linear_form(ctypes.byref(desc), _ptr(x), _ptr(w), int(which), buf, len(buf)), "linear_form")
     return buf.value.decode()
+
+
+def make_residual_norm_desc(rows, cols, dtype=CONV_F32, eps=1e-5, rms=False, post=True, gate_rows=0, sigmoid=False, ldr=None, ldh=None, ldg=None,
+                            ldy=None) -> residual_norm_desc:
+    """post: h is normed; gate_rows: rows that share a row of gates (0: no gate)."""
+    flags = (RESIDUAL_NORM_RMS if rms else 0) | (RESIDUAL_NORM_POST if post else 0) | (RESIDUAL_NORM_SIGMOID if sigmoid else 0)
+    return residual_norm_desc(rows, *(cols if ld is None else ld for ld in (ldr, ldh, ldg, ldy)), gate_rows, cols, dtype, eps, flags)
+
+
+def residual_norm_fwd(desc, r, h, gate, gamma_h, beta_h, scale, gamma, beta, r_out, y=None, stats=None, stream=None) -> None:
+    _check(lib().residual_norm_fwd(ctypes.byref(desc), _ptr(r), _ptr(h), _ptr(gate), _ptr(gamma_h), _ptr(beta_h), _ptr(scale), _ptr(gamma),
+                                   _ptr(beta), _ptr(r_out), _ptr(y), _ptr(stats), _stream(stream)), "residual_norm_fwd")
+
+
+def residual_norm_bwd_workspace_bytes(desc) -> int:
+    return int(lib().residual_norm_bwd_workspace_bytes(ctypes.byref(desc)))
+
+
+def residual_norm_bwd(desc, r_out, h, gate, gamma_h, beta_h, scale, gamma, stats, dr_out, dy, dr, dh, dgate=None, dgamma_h=None, dbeta_h=None,
+                      dscale=None, dgamma=None, dbeta=None, workspace=None, workspace_bytes=0, stream=None) -> None:
+    _check(lib().residual_norm_bwd(ctypes.byref(desc), _ptr(r_out), _ptr(h), _ptr(gate), _ptr(gamma_h), _ptr(beta_h), _ptr(scale), _ptr(gamma),
+                                   _ptr(stats), _ptr(dr_out), _ptr(dy), _ptr(dr), _ptr(dh), _ptr(dgate), _ptr(dgamma_h), _ptr(dbeta_h),
+                                   _ptr(dscale), _ptr(dgamma), _ptr(dbeta), _ptr(workspace), int(workspace_bytes), _stream(stream)), "residual_norm_bwd")
 
 
 def conv_probe_mfma_peak(dtype: int, block: int, scratch, stream=None) -> float:

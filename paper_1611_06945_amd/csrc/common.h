@@ -317,6 +317,40 @@ size_t linear_fwd_workspace(int64_t rows, int N, int K, int dtype);
 size_t linear_bwd_workspace(int64_t rows, int N, int K, int dtype);
 int linear_form_name(const LinearArgs& a, int dtype, int which, char* buf, size_t n);  // as snprintf; which: out, dx, dw
 
+// The norms around a block, forward and backward.
+struct ResidualNormArgs {
+    const void *r, *h, *gate;            // r: forward
+    const float *gamma_h, *beta_h, *scale, *gamma, *beta;
+    void *r_out, *y;                     // forward; y null where there is no norm behind
+    float* stats_out;
+    const void *x, *dr_out, *dy;         // backward: r_out as it was stored, and the gradients (either null)
+    const float* stats;
+    void *dr, *dh, *dgate;
+    float *dgamma_h, *dbeta_h, *dscale, *dgamma, *dbeta;
+    void* ws;
+    float *sums, *sums_h, *averages;     // in ws: dgamma and dbeta of each workgroup; the sums of each item; a row's averages
+    int64_t rows, ldr, ldh, ldg, ldy;
+    int64_t stretch, each, items;        // runs of rows (item_rows)
+    int32_t gate_rows;
+    int cols, per;
+    float eps;
+    int rms, post, sigmoid;
+};
+struct ResidualNormForm {
+    int lanes, most, waves;              // lanes of a row (0: none hold it), elements a lane holds, forward waves a workgroup
+    int64_t stretch, each, items;        // backward: as above, and workgroups
+    int per, groups;
+};
+hipError_t launch_residual_norm_fwd(const ResidualNormArgs& a, int dtype, hipStream_t s);
+hipError_t launch_residual_norm_bwd(ResidualNormArgs& a, int dtype, hipStream_t s);
+size_t residual_norm_bwd_workspace(int64_t rows, int cols, int64_t gate_rows, int dtype);
+hipError_t residual_norm_fwd_f32(const ResidualNormArgs& a, const ResidualNormForm& f, hipStream_t s);
+hipError_t residual_norm_fwd_f16(const ResidualNormArgs& a, const ResidualNormForm& f, hipStream_t s);
+hipError_t residual_norm_fwd_bf16(const ResidualNormArgs& a, const ResidualNormForm& f, hipStream_t s);
+hipError_t residual_norm_bwd_f32(const ResidualNormArgs& a, const ResidualNormForm& f, hipStream_t s);
+hipError_t residual_norm_bwd_f16(const ResidualNormArgs& a, const ResidualNormForm& f, hipStream_t s);
+hipError_t residual_norm_bwd_bf16(const ResidualNormArgs& a, const ResidualNormForm& f, hipStream_t s);
+
 inline const char* dtype_name(int dt) { return dt == CONV_F32 ? "f32" : dt == CONV_F16 ? "f16" : "bf16"; }
 inline int dtype_size(int dt) { return dt == CONV_F32 ? 4 : 2; }
 

@@ -1,0 +1,334 @@
+// The norms around a block: which form a call takes, rows that no registers hold, and the joins of the backward pass.
+#include "residual_norm_kernel.h"
+
+namespace convfwd {
+
+namespace {
+
+constexpr int kCUs = 256;
+
+// ---- rows of any length: a workgroup a row, an element a load, the row read again for every pass ---------------------------------
+
+template <int DT>
+__global__ __launch_bounds__(1024) void residual_norm_fwd_any(ResidualNormArgs a)
+{
+    typedef typename Prec<DT>::elem_t elem_t;
+    constexpr int NT = 1024;
+    __shared__ float red[4][16];
+    for (int64_t t = blockIdx.x; t < a.rows; t += gridDim.x) {
+        const elem_t *r = (const elem_t*)a.r + t * a.ldr, *h = (const elem_t*)a.h + t * a.ldh;
+        const elem_t* gate = a.gate ? (const elem_t*)a.gate + t / a.gate_rows * a.ldg : nullptr;
+        float mean_h = 0.0f, rstd_h = 1.0f, mean = 0.0f, rstd = 1.0f;
+        if (a.post) {
+            float sum = 0.0f, sq = 0.0f;
+            if (!a.rms) {
+                for (int j = threadIdx.x; j < a.cols; j += NT) sum += Prec<DT>::to_f32(h[j]);
+                mean_h = block_reduce<16, OpSum>(sum, red[0]) / (float)a.cols;
+            }
+            for (int j = threadIdx.x; j < a.cols; j += NT) {
+                const float d = Prec<DT>::to_f32(h[j]) - mean_h;
+                sq = __builtin_fmaf(d, d, sq);
+            }
+            rstd_h = 1.0f / sqrtf(block_reduce<16, OpSum>(sq, red[1]) / (float)a.cols + a.eps);
+        }
+        auto sum_at = [&](int j) {
+            float v = Prec<DT>::to_f32(h[j]), s = a.scale ? a.scale[j] : 1.0f;
+            if (a.post) v = __builtin_fmaf((v - mean_h) * rstd_h, s * (a.gamma_h ? a.gamma_h[j] : 1.0f), s * (a.beta_h ? a.beta_h[j] : 0.0f));
+            else v *= s;
+            if (gate) v *= gate_of(Prec<DT>::to_f32(gate[j]), a.sigmoid);
+            return Prec<DT>::to_f32(r[j]) + v;
+        };
+        if (a.y) {
+            float sum = 0.0f, sq = 0.0f;
+            if (!a.rms) {
+                for (int j = threadIdx.x; j < a.cols; j += NT) sum += sum_at(j);
+                mean = block_reduce<16, OpSum>(sum, red[2]) / (float)a.cols;
+            }
+            for (int j = threadIdx.x; j < a.cols; j += NT) {
+                const float d = sum_at(j) - mean;
+                sq = __builtin_fmaf(d, d, sq);
+            }
+            rstd = 1.0f / sqrtf(block_reduce<16, OpSum>(sq, red[3]) / (float)a.cols + a.eps);
+        }
+        for (int j = threadIdx.x; j < a.cols; j += NT) {
+            const float x = sum_at(j);
+            ((elem_t*)a.r_out)[t * a.ldr + j] = Prec<DT>::from_f32(x);
+            if (a.y)
+                ((elem_t*)a.y)[t * a.ldy + j] = Prec<DT>::from_f32(__builtin_fmaf((x - mean) * rstd, a.gamma ? a.gamma[j] : 1.0f, a.beta ? a.beta[j] : 0.0f));
+        }
+        if (threadIdx.x == 0 && a.stats_out) *(float4*)(a.stats_out + t * 4) = make_float4(mean_h, rstd_h, mean, rstd);
+        __syncthreads();
+    }
+}
+
+// The gradient at the sum at one element; c1, c2: the averages of the row that the norm's gradient takes away.
+template <int DT>
+__device__ __forceinline__ float grad_at(const ResidualNormArgs& a, int64_t t, int j, float4 st, float c1, float c2)
+{
+    typedef typename Prec<DT>::elem_t elem_t;
+    float q = a.dr_out ? Prec<DT>::to_f32(((const elem_t*)a.dr_out)[t * a.ldr + j]) : 0.0f;
+    if (a.dy) {
+        const float xh = (Prec<DT>::to_f32(((const elem_t*)a.x)[t * a.ldr + j]) - st.z) * st.w;
+        const float g = Prec<DT>::to_f32(((const elem_t*)a.dy)[t * a.ldy + j]) * (a.gamma ? a.gamma[j] : 1.0f);
+        q += st.w * (g - c1 - xh * c2);
+    }
+    return q;
+}
+__device__ __forceinline__ float4 stats_of(const ResidualNormArgs& a, int64_t t)
+{
+    return a.stats ? *(const float4*)(a.stats + t * 4) : make_float4(0.0f, 1.0f, 0.0f, 1.0f);
+}
+
+// dr, dh and the gradients of gates of a row's own; leaves the averages of each row for the column sums.
+template <int DT>
+__global__ __launch_bounds__(1024) void residual_norm_bwd_any(ResidualNormArgs a)
+{
+    typedef typename Prec<DT>::elem_t elem_t;
+    constexpr int NT = 1024;
+    __shared__ float red[4][16];
+    const float inv_cols = 1.0f / (float)a.cols;
+    for (int64_t t = blockIdx.x; t < a.rows; t += gridDim.x) {
+        const float4 st = stats_of(a, t);
+        const elem_t* h = (const elem_t*)a.h + t * a.ldh;
+        const elem_t* gate = a.gate ? (const elem_t*)a.gate + t / a.gate_rows * a.ldg : nullptr;
+        float c1 = 0.0f, c2 = 0.0f, d1 = 0.0f, d2 = 0.0f;
+        if (a.dy) {
+            for (int j = threadIdx.x; j < a.cols; j += NT) {
+                const float xh = (Prec<DT>::to_f32(((const elem_t*)a.x)[t * a.ldr + j]) - st.z) * st.w;
+                const float g = Prec<DT>::to_f32(((const elem_t*)a.dy)[t * a.ldy + j]) * (a.gamma ? a.gamma[j] : 1.0f);
+                c1 += g, c2 = __builtin_fmaf(g, xh, c2);
+            }
+            c1 = block_reduce<16, OpSum>(c1, red[0]), c2 = block_reduce<16, OpSum>(c2, red[1]) * inv_cols;
+            c1 = a.rms ? 0.0f : c1 * inv_cols;
+        }
+        auto at_hh = [&](int j, float q, float gv) {  // the gradient at the normed h
+            const float s = a.scale ? a.scale[j] : 1.0f;
+            return q * gv * (a.post && a.gamma_h ? s * a.gamma_h[j] : s);
+        };
+        if (a.post && a.dh) {
+            for (int j = threadIdx.x; j < a.cols; j += NT) {
+                const float g = at_hh(j, grad_at<DT>(a, t, j, st, c1, c2), gate ? gate_of(Prec<DT>::to_f32(gate[j]), a.sigmoid) : 1.0f);
+                d1 += g, d2 = __builtin_fmaf(g, (Prec<DT>::to_f32(h[j]) - st.x) * st.y, d2);
+            }
+            d1 = block_reduce<16, OpSum>(d1, red[2]), d2 = block_reduce<16, OpSum>(d2, red[3]) * inv_cols;
+            d1 = a.rms ? 0.0f : d1 * inv_cols;
+        }
+        for (int j = threadIdx.x; j < a.cols; j += NT) {
+            const float q = grad_at<DT>(a, t, j, st, c1, c2), gv = gate ? gate_of(Prec<DT>::to_f32(gate[j]), a.sigmoid) : 1.0f;
+            const float hh = a.post ? (Prec<DT>::to_f32(h[j]) - st.x) * st.y : Prec<DT>::to_f32(h[j]);
+            if (a.dr) ((elem_t*)a.dr)[t * a.ldr + j] = Prec<DT>::from_f32(q);
+            if (a.dh) {
+                const float g = at_hh(j, q, gv);
+                ((elem_t*)a.dh)[t * a.ldh + j] = Prec<DT>::from_f32(a.post ? st.y * (g - d1 - hh * d2) : g);
+            }
+            if (gate && a.gate_rows == 1 && a.dgate) {
+                const float s = a.scale ? a.scale[j] : 1.0f;
+                float d = q * s * (a.post ? __builtin_fmaf(hh, a.gamma_h ? a.gamma_h[j] : 1.0f, a.beta_h ? a.beta_h[j] : 0.0f) : hh);
+                if (a.sigmoid) d *= gv * (1.0f - gv);
+                ((elem_t*)a.dgate)[t * a.ldg + j] = Prec<DT>::from_f32(d);
+            }
+        }
+        if (threadIdx.x == 0) a.averages[t * 2] = c1, a.averages[t * 2 + 1] = c2;
+        __syncthreads();
+    }
+}
+
+// The four column sums of each item: a thread a column.
+template <int DT>
+__global__ __launch_bounds__(256) void residual_norm_sums_any(ResidualNormArgs a)
+{
+    typedef typename Prec<DT>::elem_t elem_t;
+    const int j = blockIdx.x * 256 + threadIdx.x;
+    if (j >= a.cols) return;
+    float dg = 0.0f, db = 0.0f;
+    for (int64_t item = blockIdx.y; item < a.items; item += gridDim.y) {
+        int64_t first, last;
+        item_rows(a, item, first, last);
+        float s1 = 0.0f, s2 = 0.0f;
+        for (int64_t t = first; t < last; ++t) {
+            const float4 st = stats_of(a, t);
+            float q = grad_at<DT>(a, t, j, st, a.averages[t * 2], a.averages[t * 2 + 1]);
+            const float hv = Prec<DT>::to_f32(((const elem_t*)a.h)[t * a.ldh + j]);
+            if (a.gate && a.gate_rows == 1) q *= gate_of(Prec<DT>::to_f32(((const elem_t*)a.gate)[t * a.ldg + j]), a.sigmoid);
+            s1 += q, s2 = __builtin_fmaf(q, a.post ? (hv - st.x) * st.y : hv, s2);
+            if (a.dy) {
+                const float dy = Prec<DT>::to_f32(((const elem_t*)a.dy)[t * a.ldy + j]);
+                dg = __builtin_fmaf(dy, (Prec<DT>::to_f32(((const elem_t*)a.x)[t * a.ldr + j]) - st.z) * st.w, dg);
+                db += dy;
+            }
+        }
+        if (a.sums_h) a.sums_h[item * 2 * a.cols + j] = s1, a.sums_h[item * 2 * a.cols + a.cols + j] = s2;
+    }
+    if (a.sums) a.sums[(int64_t)blockIdx.y * 2 * a.cols + j] = dg, a.sums[(int64_t)blockIdx.y * 2 * a.cols + a.cols + j] = db;
+}
+
+// ---- joins ----------------------------------------------------------------------------------------------------------------
+
+// Gates that rows share: their gradient from the sums of their rows, which then become those times the gate, at the gate's first item.
+template <int DT>
+__global__ __launch_bounds__(256) void residual_norm_gates(ResidualNormArgs a)
+{
+    typedef typename Prec<DT>::elem_t elem_t;
+    const int j = blockIdx.x * 256 + threadIdx.x;
+    if (j >= a.cols) return;
+    const float s = a.scale ? a.scale[j] : 1.0f, ga = a.post && a.gamma_h ? a.gamma_h[j] : 1.0f, gb = a.post && a.beta_h ? a.beta_h[j] : 0.0f;
+    const int64_t gates = a.items / a.per;
+    for (int64_t g = blockIdx.y; g < gates; g += gridDim.y) {
+        float s1 = 0.0f, s2 = 0.0f;
+        for (int p = 0; p < a.per; ++p) s1 += a.sums_h[(g * a.per + p) * 2 * a.cols + j], s2 += a.sums_h[(g * a.per + p) * 2 * a.cols + a.cols + j];
+        const float gate = gate_of(Prec<DT>::to_f32(((const elem_t*)a.gate)[g * a.ldg + j]), a.sigmoid);
+        if (a.dgate) {
+            float d = s * __builtin_fmaf(ga, s2, gb * s1);
+            if (a.sigmoid) d *= gate * (1.0f - gate);
+            ((elem_t*)a.dgate)[g * a.ldg + j] = Prec<DT>::from_f32(d);
+        }
+        a.sums_h[g * a.per * 2 * a.cols + j] = gate * s1, a.sums_h[g * a.per * 2 * a.cols + a.cols + j] = gate * s2;
+    }
+}
+
+// Sums of `parts` and of `items`, 16 columns and 64 lanes of rows a workgroup, and from them the gradients of the vectors.
+__global__ __launch_bounds__(1024) void residual_norm_join(ResidualNormArgs a, int parts, int64_t items, int per)
+{
+    __shared__ float red[4][64][16];
+    const int l = threadIdx.x & 15, lane = threadIdx.x >> 4;
+    const int j = blockIdx.x * 16 + l;
+    float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (j < a.cols) {
+        if (a.sums)
+            for (int p = lane; p < parts; p += 64) s[0] += a.sums[(int64_t)p * 2 * a.cols + j], s[1] += a.sums[(int64_t)p * 2 * a.cols + a.cols + j];
+        if (a.sums_h)
+            for (int64_t p = lane; p < items; p += 64) s[2] += a.sums_h[p * per * 2 * a.cols + j], s[3] += a.sums_h[p * per * 2 * a.cols + a.cols + j];
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) red[i][lane][l] = s[i];
+    __syncthreads();
+    if (lane >= 4) return;
+    float sum = 0.0f;  // lane i: sum i (one wave is left, so the four sums of a column are in its lanes)
+#pragma unroll 8
+    for (int p = 0; p < 64; ++p) sum += red[lane][p][l];
+    const float dg = __shfl(sum, l), db = __shfl(sum, 16 + l), s1 = __shfl(sum, 32 + l), s2 = __shfl(sum, 48 + l);
+    if (lane || j >= a.cols) return;
+    if (a.dgamma) a.dgamma[j] = dg;
+    if (a.dbeta) a.dbeta[j] = db;
+    const float scale = a.scale ? a.scale[j] : 1.0f;
+    if (a.dgamma_h) a.dgamma_h[j] = scale * s2;
+    if (a.dbeta_h) a.dbeta_h[j] = scale * s1;
+    if (a.dscale) a.dscale[j] = a.post ? __builtin_fmaf(a.gamma_h ? a.gamma_h[j] : 1.0f, s2, (a.beta_h ? a.beta_h[j] : 0.0f) * s1) : s2;
+}
+
+// ---- forms ----------------------------------------------------------------------------------------------------------------
+
+ResidualNormForm fwd_form(int cols, int dtype)
+{
+    const int vec = dtype == CONV_F32 ? 4 : 8;
+    ResidualNormForm f = {};
+    if (vec == 4 && cols <= 32) f.lanes = 8, f.most = 4, f.waves = 4;
+    for (int lanes : {8, 16, 64})
+        for (int most : {8, 16})
+            if (cols <= lanes * most && !f.lanes) f.lanes = lanes, f.most = most, f.waves = 4;
+    if (f.lanes) return f;
+    const int pieces = (cols + vec - 1) / vec;
+    for (int most : {8, 16}) {
+        const int waves = (pieces + 64 * (most / vec) - 1) / (64 * (most / vec));
+        if (waves <= (most == 8 ? 8 : 16)) {
+            f.lanes = 64 * waves, f.most = most, f.waves = waves;
+            return f;
+        }
+    }
+    return f;  // none
+}
+
+// Backward: lanes a row and elements a lane; workgroups, and the runs of rows that they take.
+ResidualNormForm bwd_form(int64_t rows, int cols, int64_t gate_rows, int dtype)
+{
+    ResidualNormForm f = {};
+    if (dtype == CONV_F32 && cols <= 32) f.lanes = 8, f.most = 4;
+    for (int lanes : {8, 16, 64, 256, 512})
+        for (int most : {8, 16})
+            if (cols <= lanes * most && !f.lanes && !(lanes == 512 && most == 8)) f.lanes = lanes, f.most = most;
+    const int here = f.lanes ? (f.lanes <= 16 ? 256 : 512) / f.lanes : 1;  // rows at once
+    const int64_t most = f.lanes ? (f.most <= 8 ? 4 * kCUs : 2 * kCUs) : 64;
+    f.stretch = gate_rows > 1 ? gate_rows : std::max<int64_t>(rows, 1);
+    const int64_t stretches = (rows + f.stretch - 1) / f.stretch;
+    // as many runs as workgroups, of whole rounds; at least eight rows each, lest their sums cost more than they
+    const int64_t want = stretches ? std::max<int64_t>(1, most / stretches) : 1;
+    const int64_t least = std::max(here, 8);
+    f.each = std::max((f.stretch + want - 1) / want, least);
+    f.each = (f.each + here - 1) / here * here;
+    f.per = (int)((f.stretch + f.each - 1) / f.each);
+    f.items = stretches * f.per;
+    f.groups = (int)std::min<int64_t>(std::max<int64_t>(f.items, 1), most);
+    return f;
+}
+
+struct Space {
+    float *sums, *sums_h, *averages;
+    size_t bytes;
+};
+Space space_of(const ResidualNormForm& f, int64_t rows, int cols, void* ws)
+{
+    Space s = {};
+    char* at = (char*)ws;
+    auto take = [&](size_t n) {
+        float* p = at ? (float*)(at + s.bytes) : nullptr;
+        s.bytes += (n + 255) & ~(size_t)255;
+        return p;
+    };
+    s.sums = take((size_t)f.groups * 2 * cols * 4);
+    s.sums_h = take((size_t)f.items * 2 * cols * 4);
+    if (!f.lanes) s.averages = take((size_t)rows * 2 * 4);
+    return s;
+}
+
+template <int DT>
+hipError_t bwd(ResidualNormArgs a, const ResidualNormForm& f, hipStream_t s)
+{
+    if (a.rows > 0) {
+        if (f.lanes) {
+            const hipError_t e = DT == CONV_F32 ? residual_norm_bwd_f32(a, f, s) : DT == CONV_F16 ? residual_norm_bwd_f16(a, f, s) : residual_norm_bwd_bf16(a, f, s);
+            if (e != hipSuccess) return e;
+        } else {
+            hipLaunchKernelGGL((residual_norm_bwd_any<DT>), dim3((unsigned)std::min<int64_t>(a.rows, 1 << 20)), dim3(1024), 0, s, a);
+            if (a.sums || a.sums_h) hipLaunchKernelGGL((residual_norm_sums_any<DT>), dim3((unsigned)((a.cols + 255) / 256), (unsigned)f.groups), dim3(256), 0, s, a);
+        }
+        if (a.gate && a.gate_rows > 1 && a.sums_h)
+            hipLaunchKernelGGL((residual_norm_gates<DT>), dim3((unsigned)((a.cols + 255) / 256), (unsigned)std::min<int64_t>(f.items / f.per, 4096)), dim3(256), 0, s, a);
+    }
+    if (a.dgamma || a.dbeta || a.dgamma_h || a.dbeta_h || a.dscale) {
+        const bool shared = a.gate && a.gate_rows > 1;
+        hipLaunchKernelGGL(residual_norm_join, dim3((unsigned)((a.cols + 15) / 16)), dim3(1024), 0, s, a, a.rows ? f.groups : 0, shared ? f.items / f.per : f.items,
+                           shared ? f.per : 1);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace
+
+size_t residual_norm_bwd_workspace(int64_t rows, int cols, int64_t gate_rows, int dtype)
+{
+    return space_of(bwd_form(rows, cols, gate_rows, dtype), rows, cols, nullptr).bytes;
+}
+
+hipError_t launch_residual_norm_fwd(const ResidualNormArgs& a, int dtype, hipStream_t s)
+{
+    const ResidualNormForm f = fwd_form(a.cols, dtype);
+    if (f.lanes) return dtype == CONV_F32 ? residual_norm_fwd_f32(a, f, s) : dtype == CONV_F16 ? residual_norm_fwd_f16(a, f, s) : residual_norm_fwd_bf16(a, f, s);
+    const dim3 grid((unsigned)std::min<int64_t>(a.rows, 1 << 20));
+    if (dtype == CONV_F32) hipLaunchKernelGGL((residual_norm_fwd_any<CONV_F32>), grid, dim3(1024), 0, s, a);
+    else if (dtype == CONV_F16) hipLaunchKernelGGL((residual_norm_fwd_any<CONV_F16>), grid, dim3(1024), 0, s, a);
+    else hipLaunchKernelGGL((residual_norm_fwd_any<CONV_BF16>), grid, dim3(1024), 0, s, a);
+    return hipGetLastError();
+}
+
+hipError_t launch_residual_norm_bwd(ResidualNormArgs& a, int dtype, hipStream_t s)
+{
+    const ResidualNormForm f = bwd_form(a.rows, a.cols, a.gate ? a.gate_rows : 0, dtype);
+    const Space space = space_of(f, a.rows, a.cols, a.ws);
+    a.stretch = f.stretch, a.each = f.each, a.items = f.items, a.per = f.per;
+    a.sums = a.dgamma || a.dbeta ? space.sums : nullptr;
+    a.sums_h = a.dgamma_h || a.dbeta_h || a.dscale || (a.dgate && a.gate_rows > 1) ? space.sums_h : nullptr;
+    a.averages = space.averages;
+    return dtype == CONV_F32 ? bwd<CONV_F32>(a, f, s) : dtype == CONV_F16 ? bwd<CONV_F16>(a, f, s) : bwd<CONV_BF16>(a, f, s);
+}
+
+}  // namespace convfwd

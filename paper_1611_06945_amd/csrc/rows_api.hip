@@ -1,8 +1,10 @@
-// C entry points of the operators on rows: layer norm, row quantiser, 8-bit product, log probabilities, linear layers.  Arguments are
+// C entry points of the operators on rows: layer norm, row quantiser, 8-bit product, log probabilities, linear layers, the norms around a
+// block.  Arguments are
 // checked before the first HIP call; the kernels' launchers choose among their forms.
 #include <algorithm>
 #include <climits>
 #include <cmath>
+#include <initializer_list>
 
 #include "common.h"
 
@@ -71,6 +73,41 @@ LinearArgs linear_args(const linear_desc* d)
     a.rows = d->rows, a.ldx = d->ldx, a.ldw = d->ldw, a.ldr = d->ldr, a.ldo = d->ldo, a.N = d->N, a.K = d->K;
     a.act = d->flags & CONV_FLAG_RELU ? 1 : d->flags & LINEAR_FLAG_GELU ? 2 : d->flags & LINEAR_FLAG_SILU ? 3 : 0;
     return a;
+}
+
+int check_residual_norm(const residual_norm_desc* d)
+{
+    if (!d) return CONV_EINVAL;
+    if (!known(d->dtype)) return CONV_EDTYPE;
+    if (d->rows < 0 || d->rows > kMostRows || d->cols < 1 || d->cols >= (1 << 30) || d->gate_rows < 0) return CONV_EINVAL;
+    const int es = dtype_size(d->dtype);
+    for (const int64_t ld : {d->ldr, d->ldh, d->ldy})
+        if (ld < d->cols || !spans(d->rows, ld, es)) return CONV_EINVAL;
+    if (d->gate_rows && (d->ldg < d->cols || !spans(d->rows, d->ldg, es))) return CONV_EINVAL;
+    if (!(d->eps >= 0.0f) || std::isinf(d->eps)) return CONV_EINVAL;
+    if (d->flags & ~(RESIDUAL_NORM_RMS | RESIDUAL_NORM_POST | RESIDUAL_NORM_SIGMOID)) return CONV_EINVAL;
+    return CONV_OK;
+}
+
+ResidualNormArgs residual_norm_args(const residual_norm_desc* d)
+{
+    ResidualNormArgs a = {};
+    a.rows = d->rows, a.ldr = d->ldr, a.ldh = d->ldh, a.ldg = d->ldg, a.ldy = d->ldy, a.gate_rows = d->gate_rows, a.cols = d->cols, a.eps = d->eps;
+    a.rms = (d->flags & RESIDUAL_NORM_RMS) != 0, a.post = (d->flags & RESIDUAL_NORM_POST) != 0, a.sigmoid = (d->flags & RESIDUAL_NORM_SIGMOID) != 0;
+    return a;
+}
+
+// Whether an output is one of the inputs, or another output.
+bool overlaps(std::initializer_list<const void*> outputs, std::initializer_list<const void*> inputs)
+{
+    for (auto o = outputs.begin(); o != outputs.end(); ++o) {
+        if (!*o) continue;
+        for (const void* i : inputs)
+            if (*o == i) return true;
+        for (auto p = outputs.begin(); p != o; ++p)
+            if (*o == *p) return true;
+    }
+    return false;
 }
 
 // Runs a launcher; nothing it throws leaves the C interface.
@@ -299,6 +336,58 @@ int linear_form(const linear_desc* desc, const void* x, const void* w, int which
     a.x = x, a.w = w;
     linear_form_name(a, desc->dtype, which, buf, n);
     return CONV_OK;
+}
+
+int residual_norm_fwd(const residual_norm_desc* desc, const void* r, const void* h, const void* gate, const float* gamma_h, const float* beta_h,
+                      const float* scale, const float* gamma, const float* beta, void* r_out, void* y, float* stats, void* stream)
+{
+    const int rc = check_residual_norm(desc);
+    if (rc) return rc;
+    ResidualNormArgs a = residual_norm_args(desc);
+    const int es = dtype_size(desc->dtype);
+    for (const float* v : {gamma_h, beta_h, scale, gamma, beta})
+        if (!vec_ok(v)) return CONV_EINVAL;
+    if (!aligned(r, es) || !aligned(h, es) || !aligned(gate, es) || !aligned(r_out, es) || !aligned(y, es) || !aligned(stats, 16)) return CONV_EINVAL;
+    if (!a.post && (gamma_h || beta_h)) return CONV_EINVAL;
+    if (desc->rows == 0) return CONV_OK;
+    if (!r || !h || !r_out || (gate != nullptr) != (desc->gate_rows > 0)) return CONV_EINVAL;
+    if (overlaps({r_out, y, stats}, {h, gate}) || y == r || (const void*)stats == r) return CONV_EINVAL;
+    a.r = r, a.h = h, a.gate = gate, a.gamma_h = gamma_h, a.beta_h = beta_h, a.scale = scale, a.gamma = gamma, a.beta = beta;
+    a.r_out = r_out, a.y = y, a.stats_out = stats;
+    return guarded("residual_norm_fwd", [&] { return launch_residual_norm_fwd(a, desc->dtype, (hipStream_t)stream); });
+}
+
+size_t residual_norm_bwd_workspace_bytes(const residual_norm_desc* desc)
+{
+    return check_residual_norm(desc) ? 0 : residual_norm_bwd_workspace(desc->rows, desc->cols, desc->gate_rows, desc->dtype);
+}
+
+int residual_norm_bwd(const residual_norm_desc* desc, const void* r_out, const void* h, const void* gate, const float* gamma_h, const float* beta_h,
+                      const float* scale, const float* gamma, const float* stats, const void* dr_out, const void* dy, void* dr, void* dh, void* dgate,
+                      float* dgamma_h, float* dbeta_h, float* dscale, float* dgamma, float* dbeta, void* workspace, size_t workspace_bytes, void* stream)
+{
+    const int rc = check_residual_norm(desc);
+    if (rc) return rc;
+    ResidualNormArgs a = residual_norm_args(desc);
+    const int es = dtype_size(desc->dtype);
+    for (const float* v : {gamma_h, beta_h, scale, gamma, (const float*)dgamma_h, (const float*)dbeta_h, (const float*)dscale, (const float*)dgamma, (const float*)dbeta})
+        if (!vec_ok(v)) return CONV_EINVAL;
+    for (const void* p : {r_out, h, gate, dr_out, dy, (const void*)dr, (const void*)dh, (const void*)dgate})
+        if (!aligned(p, es)) return CONV_EINVAL;
+    if (!aligned(stats, 16) || !aligned(workspace, 16)) return CONV_EINVAL;
+    if (!dr && !dh && !dgate && !dgamma_h && !dbeta_h && !dscale && !dgamma && !dbeta) return CONV_EINVAL;
+    if (!a.post && (gamma_h || beta_h || dgamma_h || dbeta_h)) return CONV_EINVAL;
+    if (desc->rows > 0) {
+        if (!h || (!dr_out && !dy) || (dy && !r_out) || ((dy || a.post) && !stats)) return CONV_EINVAL;
+        if ((gate != nullptr) != (desc->gate_rows > 0) || (dgate && !gate)) return CONV_EINVAL;
+        if (overlaps({dr, dh, dgate, dgamma_h, dbeta_h, dscale, dgamma, dbeta}, {r_out, h, gate, gamma_h, beta_h, scale, gamma, stats, dr_out, dy})) return CONV_EINVAL;
+    }
+    const size_t need = residual_norm_bwd_workspace(desc->rows, desc->cols, desc->gate_rows, desc->dtype);
+    if (need && (!workspace || workspace_bytes < need)) return CONV_EWORKSPACE;
+    a.x = r_out, a.h = h, a.gate = gate, a.gamma_h = gamma_h, a.beta_h = beta_h, a.scale = scale, a.gamma = gamma, a.stats = stats;
+    a.dr_out = dr_out, a.dy = dy, a.dr = dr, a.dh = dh, a.dgate = dgate;
+    a.dgamma_h = dgamma_h, a.dbeta_h = dbeta_h, a.dscale = dscale, a.dgamma = dgamma, a.dbeta = dbeta, a.ws = workspace;
+    return guarded("residual_norm_bwd", [&] { return launch_residual_norm_bwd(a, desc->dtype, (hipStream_t)stream); });
 }
 
 }  // extern "C"

@@ -119,3 +119,99 @@ def test_oracle_gradients_against_differences(act):
             up = value(*args)
             args[at][i] -= 2 * h
             assert abs((up - value(*args)) / (2 * h) - d[i]) < 1e-6
+
+
+# ---- the norms around a block ------------------------------------------------------------------------------------------
+
+
+def nfwd(d, r=P, h=2 * P, gate=3 * P, gamma_h=P, beta_h=P, scale=P, gamma=P, beta=P, r_out=4 * P, y=5 * P, stats=6 * P):
+    return status(B.residual_norm_fwd, d, r, h, gate, gamma_h, beta_h, scale, gamma, beta, r_out, y, stats, stream=0)
+
+
+def nbwd(d, r_out=P, h=2 * P, gate=3 * P, gamma_h=P + 64, beta_h=P + 64, scale=P + 64, gamma=P + 64, stats=4 * P, dr_out=5 * P, dy=6 * P, dr=7 * P, dh=8 * P, dgate=9 * P,
+         dgamma_h=10 * P, dbeta_h=11 * P, dscale=12 * P, dgamma=13 * P, dbeta=14 * P, ws=P, n=1 << 40):
+    return status(B.residual_norm_bwd, d, r_out, h, gate, gamma_h, beta_h, scale, gamma, stats, dr_out, dy, dr, dh, dgate, dgamma_h, dbeta_h, dscale, dgamma, dbeta,
+                  ws, n, stream=0)
+
+
+@pytest.mark.parametrize("change", [dict(rows=-1), dict(rows=1 << 31), dict(cols=0), dict(cols=1 << 30), dict(ldr=7), dict(ldh=7), dict(ldy=7), dict(ldg=7), dict(gate_rows=-1),
+                                    dict(eps=-1.0), dict(eps=float("nan")), dict(eps=float("inf")), dict(flags=8), dict(ldr=1 << 62), dict(ldg=1 << 62)])
+def test_residual_norm_descriptors_that_are_refused(change):
+    d = B.make_residual_norm_desc(4, 8, B.CONV_BF16, gate_rows=2)
+    for k, v in change.items():
+        setattr(d, k, v)
+    if change == dict(cols=1 << 30):
+        d.ldr = d.ldh = d.ldy = d.ldg = 1 << 30
+    assert nfwd(d) == B.CONV_EINVAL and nbwd(d) == B.CONV_EINVAL
+    assert B.residual_norm_bwd_workspace_bytes(d) == 0
+
+
+def test_residual_norm_pointers_that_are_refused():
+    d = B.make_residual_norm_desc(4, 8, B.CONV_BF16, gate_rows=2)
+    for name in ("r", "h", "r_out", "gate"):
+        assert nfwd(d, **{name: None}) == B.CONV_EINVAL
+    for name in ("r", "h", "gate", "r_out", "y", "gamma_h", "beta_h", "scale", "gamma", "beta", "stats"):
+        assert nfwd(d, **{name: 17 * P + 1}) == B.CONV_EINVAL
+    assert nfwd(d, stats=17 * P + 4) == B.CONV_EINVAL                       # its rows are read four floats at a time
+    assert nfwd(d, r_out=2 * P) == B.CONV_EINVAL and nfwd(d, r_out=3 * P) == B.CONV_EINVAL
+    assert nfwd(d, y=P) == B.CONV_EINVAL and nfwd(d, y=2 * P) == B.CONV_EINVAL and nfwd(d, y=4 * P) == B.CONV_EINVAL
+    assert nfwd(d, stats=P) == B.CONV_EINVAL
+    d.dtype = 3
+    assert nfwd(d) == B.CONV_EDTYPE and nbwd(d) == B.CONV_EDTYPE
+    d = B.make_residual_norm_desc(4, 8, post=False)
+    assert nfwd(d, gate=None) == B.CONV_EINVAL                              # a norm's vectors without the norm
+    assert nfwd(d, gamma_h=None, beta_h=None) == B.CONV_EINVAL              # a gate without rows that share it
+    assert B.lib().residual_norm_fwd(None, *[P] * 12) == B.CONV_EINVAL
+
+
+def test_residual_norm_bwd_pointers_that_are_refused():
+    d = B.make_residual_norm_desc(4, 8, B.CONV_BF16, gate_rows=2)
+    outs = ("dr", "dh", "dgate", "dgamma_h", "dbeta_h", "dscale", "dgamma", "dbeta")
+    assert nbwd(d, **{k: None for k in outs}) == B.CONV_EINVAL              # nothing asked for
+    assert nbwd(d, dr_out=None, dy=None) == B.CONV_EINVAL                   # nothing to go by
+    for name in ("r_out", "h", "gate", "stats"):
+        assert nbwd(d, **{name: None}) == B.CONV_EINVAL
+    for name in outs + ("r_out", "h", "gate", "dr_out", "dy", "gamma_h", "scale", "stats"):
+        assert nbwd(d, **{name: 17 * P + 1}) == B.CONV_EINVAL
+    for name in outs:
+        for taken in (P, 2 * P, 3 * P, 4 * P, 5 * P, 6 * P, (8 if name == "dr" else 7) * P):
+            assert nbwd(d, **{name: taken}) == B.CONV_EINVAL
+    need = B.residual_norm_bwd_workspace_bytes(d)
+    assert need > 0
+    assert nbwd(d, n=need - 1) == B.CONV_EWORKSPACE and nbwd(d, ws=None, n=need) == B.CONV_EWORKSPACE
+    assert nbwd(d, ws=P + 8, n=need) == B.CONV_EINVAL
+    d = B.make_residual_norm_desc(4, 8, post=False)
+    free = dict(gate=None, gamma_h=None, beta_h=None)
+    assert nbwd(d, **free, dgate=None) == B.CONV_EINVAL                     # gradients of vectors that are not there
+    assert nbwd(d, **free, dgamma_h=None, dbeta_h=None) == B.CONV_EINVAL    # ... and of gates
+    assert B.lib().residual_norm_bwd(None, *[P] * 19, P, 0, None) == B.CONV_EINVAL
+
+
+def test_residual_norm_without_rows():
+    d = B.make_residual_norm_desc(0, 8)
+    assert nfwd(d, None, None, None, r_out=None, y=None, stats=None) == B.CONV_OK
+
+
+@pytest.mark.parametrize("post,rms,gate_rows,sigmoid", [(True, False, 0, False), (True, True, 2, True), (False, False, 1, False), (True, False, 3, True)])
+def test_oracle_gradients_of_the_norms_against_differences(post, rms, gate_rows, sigmoid):
+    rng = np.random.default_rng(5)
+    t = dict(r=rng.normal(size=(5, 6)), h=rng.normal(size=(5, 6)), gate=rng.normal(size=(-(-5 // gate_rows), 6)) if gate_rows else None)
+    v = {k: rng.normal(size=6) for k in ("gamma_h", "beta_h", "scale", "gamma", "beta")}
+    if not post:
+        v["gamma_h"] = v["beta_h"] = None
+    gr, gy = rng.normal(size=(5, 6)), rng.normal(size=(5, 6))
+
+    def value(a):
+        x, y, _, _ = ro.residual_norm(a["r"], a["h"], a["gate"], gate_rows, sigmoid, a["gamma_h"], a["beta_h"], a["scale"], a["gamma"], a["beta"], post, rms, 1e-3)
+        return float((gr * x + gy * y).sum())
+
+    a = {**t, **v}
+    x, _, st, _ = ro.residual_norm(a["r"], a["h"], a["gate"], gate_rows, sigmoid, a["gamma_h"], a["beta_h"], a["scale"], a["gamma"], a["beta"], post, rms, 1e-3)
+    got = ro.residual_norm_bwd(x, a["h"], a["gate"], gate_rows, sigmoid, a["gamma_h"], a["beta_h"], a["scale"], a["gamma"], st, gr, gy, post, rms)
+    e = 1e-6
+    for k in a:
+        if a[k] is None:
+            continue
+        for i in np.ndindex(a[k].shape):
+            moved = [value({**a, k: a[k] + s * e * (np.indices(a[k].shape) == np.array(i).reshape(-1, *[1] * a[k].ndim)).all(0)}) for s in (1, -1)]
+            assert abs((moved[0] - moved[1]) / (2 * e) - got["d" + k][i]) < 1e-6, (k, i)
