@@ -543,6 +543,30 @@ int residual_norm_bwd(const residual_norm_desc* desc, const void* r_out, const v
                       const void* dy, void* dr, void* dh, void* dgate, float* dgamma_h, float* dbeta_h, float* dscale,
                       float* dgamma, float* dbeta, void* workspace, size_t workspace_bytes, void* stream);
 
+/*
+ * The direction of an update made orthogonal by Newton-Schulz steps, for each of `batch` matrices x [rows][cols]:
+ *   X = x / (|x| + eps), |x| the root of the sum of the squares;  `steps` times  X <- a X + (b X X^T + c (X X^T)^2) X;  out = X.
+ * The polynomial a s + b s^3 + c s^5 moves every singular value s of X towards one; e.g. 3.4445, -4.7750, 2.0315 and five steps.  Coefficients have to keep
+ * the elements of X and of b X X^T + c (X X^T)^2 below 15 (any that keep the singular values below 1.5 with |b|, |c| <= 5 do); beyond, results may be infinite or NaN.
+ * X is held in fp32 and multiplied in fp16 with fp32 sums: in one part for bf16, whose results are off by some 2e-3 of their norm with the rounding to the
+ * type, in two parts of 11 bits for fp16 and fp32 (some 2e-6).  A matrix with a NaN or an infinity gives NaN; one of zeros stays zero where eps > 0.
+ * Matrix i starts stride_x (stride_o) elements behind matrix i - 1, its rows ldx (ldo) apart; out may be x where the strides are the same.  `workspace`:
+ * orthogonalize_workspace_bytes(desc), 16-byte aligned, CONV_EWORKSPACE if it is smaller.  batch = 0 enqueues nothing.
+ * CONV_EINVAL for batch < 0 or >= 2^31, rows or cols outside [1, 2^20] or both above 2^17, steps outside [1, 100], strides below a row's length, matrices that overlap in out (stride_o below
+ * rows * ldo for batch > 1), coefficients that are not finite, eps < 0, infinite or NaN, NULL or misaligned pointers.
+ */
+typedef struct {
+    int64_t batch;
+    int64_t ldx, ldo;           /* row strides in elements */
+    int64_t stride_x, stride_o; /* from a matrix to the next, in elements */
+    int32_t rows, cols;
+    int32_t dtype;              /* conv_dtype of x and out */
+    int32_t steps;
+    float a, b, c, eps;
+} orthogonal_desc;
+size_t orthogonalize_workspace_bytes(const orthogonal_desc* desc);
+int orthogonalize(const orthogonal_desc* desc, const void* x, void* out, void* workspace, size_t workspace_bytes, void* stream);
+
 /* Text for a conv_status; for CONV_EHIP it includes the message of the last failed HIP call of this thread. */
 const char* conv_strerror(int status);
 

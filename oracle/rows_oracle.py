@@ -180,3 +180,13 @@ def residual_norm_bwd(x, h, gate, gate_rows, sigmoid, gamma_h, beta_h, scale, ga
     out["dgamma_h"], out["dbeta_h"] = (du * hh).sum(0), du.sum(0)
     out["dh"] = through(du * one(gamma_h), hh, stats[:, 1]) if post else du
     return out
+
+
+def newton_schulz(x, steps, coefficients, eps):
+    """One matrix."""
+    a, b, c = coefficients
+    x = x / (np.sqrt((x * x).sum()) + eps)
+    for _ in range(steps):
+        m = x @ x.T
+        x = a * x + (b * m + c * (m @ m)) @ x
+    return x

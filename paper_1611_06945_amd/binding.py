@@ -77,6 +77,12 @@ class residual_norm_desc(ctypes.Structure):
                 ("gate_rows", ctypes.c_int32), ("cols", ctypes.c_int32), ("dtype", ctypes.c_int32), ("eps", ctypes.c_float), ("flags", ctypes.c_uint32)]
 
 
+class orthogonal_desc(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int64), ("ldx", ctypes.c_int64), ("ldo", ctypes.c_int64), ("stride_x", ctypes.c_int64), ("stride_o", ctypes.c_int64),
+                ("rows", ctypes.c_int32), ("cols", ctypes.c_int32), ("dtype", ctypes.c_int32), ("steps", ctypes.c_int32), ("a", ctypes.c_float), ("b", ctypes.c_float),
+                ("c", ctypes.c_float), ("eps", ctypes.c_float)]
+
+
 class ConvError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -200,6 +206,11 @@ def lib() -> ctypes.CDLL:
         L.residual_norm_bwd_workspace_bytes.restype = sz
         L.residual_norm_bwd.argtypes = [rp] + [vp] * 19 + [sz, vp]
         L.residual_norm_bwd.restype = ctypes.c_int
+        op = ctypes.POINTER(orthogonal_desc)
+        L.orthogonalize_workspace_bytes.argtypes = [op]
+        L.orthogonalize_workspace_bytes.restype = sz
+        L.orthogonalize.argtypes = [op, vp, vp, vp, sz, vp]
+        L.orthogonalize.restype = ctypes.c_int
         L.conv_strerror.argtypes = [ctypes.c_int]
         L.conv_strerror.restype = ctypes.c_char_p
         _lib = L
@@ -552,6 +563,21 @@ def residual_norm_bwd(desc, r_out, h, gate, gamma_h, beta_h, scale, gamma, stats
     _check(lib().residual_norm_bwd(ctypes.byref(desc), _ptr(r_out), _ptr(h), _ptr(gate), _ptr(gamma_h), _ptr(beta_h), _ptr(scale), _ptr(gamma),
                                    _ptr(stats), _ptr(dr_out), _ptr(dy), _ptr(dr), _ptr(dh), _ptr(dgate), _ptr(dgamma_h), _ptr(dbeta_h),
                                    _ptr(dscale), _ptr(dgamma), _ptr(dbeta), _ptr(workspace), int(workspace_bytes), _stream(stream)), "residual_norm_bwd")
+
+
+def make_orthogonal_desc(rows, cols, dtype=CONV_F32, batch=1, steps=5, coefficients=(3.4445, -4.7750, 2.0315), eps=1e-7, ldx=None, ldo=None, stride_x=None,
+                         stride_o=None) -> orthogonal_desc:
+    ldx, ldo = cols if ldx is None else ldx, cols if ldo is None else ldo
+    return orthogonal_desc(batch, ldx, ldo, rows * ldx if stride_x is None else stride_x, rows * ldo if stride_o is None else stride_o, rows, cols, dtype, steps,
+                           *coefficients, eps)
+
+
+def orthogonalize_workspace_bytes(desc) -> int:
+    return int(lib().orthogonalize_workspace_bytes(ctypes.byref(desc)))
+
+
+def orthogonalize(desc, x, out, workspace=None, workspace_bytes=0, stream=None) -> None:
+    _check(lib().orthogonalize(ctypes.byref(desc), _ptr(x), _ptr(out), _ptr(workspace), int(workspace_bytes), _stream(stream)), "orthogonalize")
 
 
 def conv_probe_mfma_peak(dtype: int, block: int, scratch, stream=None) -> float:

@@ -351,6 +351,17 @@ hipError_t residual_norm_bwd_f32(const ResidualNormArgs& a, const ResidualNormFo
 hipError_t residual_norm_bwd_f16(const ResidualNormArgs& a, const ResidualNormForm& f, hipStream_t s);
 hipError_t residual_norm_bwd_bf16(const ResidualNormArgs& a, const ResidualNormForm& f, hipStream_t s);
 
+// Newton-Schulz steps on a batch of matrices.
+struct OrthogonalArgs {
+    const void* x;
+    void *out, *ws;
+    int64_t batch, rows, cols, ldx, ldo, stride_x, stride_o;
+    int steps;
+    float a, b, c, eps;
+};
+hipError_t launch_orthogonalize(const OrthogonalArgs& a, int dtype, hipStream_t s);
+size_t orthogonal_workspace(const OrthogonalArgs& a, int dtype);
+
 inline const char* dtype_name(int dt) { return dt == CONV_F32 ? "f32" : dt == CONV_F16 ? "f16" : "bf16"; }
 inline int dtype_size(int dt) { return dt == CONV_F32 ? 4 : 2; }
 

@@ -1,5 +1,5 @@
 // C entry points of the operators on rows: layer norm, row quantiser, 8-bit product, log probabilities, linear layers, the norms around a
-// block.  Arguments are
+// block, Newton-Schulz steps.  Arguments are
 // checked before the first HIP call; the kernels' launchers choose among their forms.
 #include <algorithm>
 #include <climits>
@@ -94,6 +94,31 @@ ResidualNormArgs residual_norm_args(const residual_norm_desc* d)
     ResidualNormArgs a = {};
     a.rows = d->rows, a.ldr = d->ldr, a.ldh = d->ldh, a.ldg = d->ldg, a.ldy = d->ldy, a.gate_rows = d->gate_rows, a.cols = d->cols, a.eps = d->eps;
     a.rms = (d->flags & RESIDUAL_NORM_RMS) != 0, a.post = (d->flags & RESIDUAL_NORM_POST) != 0, a.sigmoid = (d->flags & RESIDUAL_NORM_SIGMOID) != 0;
+    return a;
+}
+
+int check_orthogonal(const orthogonal_desc* d)
+{
+    if (!d) return CONV_EINVAL;
+    if (!known(d->dtype)) return CONV_EDTYPE;
+    if (d->batch < 0 || d->batch > kMostRows || d->rows < 1 || d->cols < 1 || d->rows > (1 << 20) || d->cols > (1 << 20)) return CONV_EINVAL;
+    if (std::min(d->rows, d->cols) > (1 << 17)) return CONV_EINVAL;
+    if (d->steps < 1 || d->steps > 100 || d->ldx < d->cols || d->ldo < d->cols || d->stride_x < 0 || d->stride_o < 0) return CONV_EINVAL;
+    const int es = dtype_size(d->dtype);
+    if (!spans(d->rows, d->ldx, es) || !spans(d->rows, d->ldo, es) || !spans(d->batch, d->stride_x, es) || !spans(d->batch, d->stride_o, es)) return CONV_EINVAL;
+    if (d->batch > 1 && d->stride_o < d->rows * d->ldo) return CONV_EINVAL;
+    if (!std::isfinite(d->a) || !std::isfinite(d->b) || !std::isfinite(d->c) || !(d->eps >= 0.0f) || std::isinf(d->eps)) return CONV_EINVAL;
+    // the workspace of a batch, too, is below 2^62 bytes
+    const double side = std::min(d->rows, d->cols);
+    if ((double)d->batch * (20.0 * d->rows * (d->cols + 64.0) + 16.0 * side * (side + 64.0)) > 0x1p61) return CONV_EINVAL;
+    return CONV_OK;
+}
+
+OrthogonalArgs orthogonal_args(const orthogonal_desc* d)
+{
+    OrthogonalArgs a = {};
+    a.batch = d->batch, a.rows = d->rows, a.cols = d->cols, a.ldx = d->ldx, a.ldo = d->ldo, a.stride_x = d->stride_x, a.stride_o = d->stride_o;
+    a.steps = d->steps, a.a = d->a, a.b = d->b, a.c = d->c, a.eps = d->eps;
     return a;
 }
 
@@ -388,6 +413,26 @@ int residual_norm_bwd(const residual_norm_desc* desc, const void* r_out, const v
     a.dr_out = dr_out, a.dy = dy, a.dr = dr, a.dh = dh, a.dgate = dgate;
     a.dgamma_h = dgamma_h, a.dbeta_h = dbeta_h, a.dscale = dscale, a.dgamma = dgamma, a.dbeta = dbeta, a.ws = workspace;
     return guarded("residual_norm_bwd", [&] { return launch_residual_norm_bwd(a, desc->dtype, (hipStream_t)stream); });
+}
+
+size_t orthogonalize_workspace_bytes(const orthogonal_desc* desc)
+{
+    return check_orthogonal(desc) ? 0 : orthogonal_workspace(orthogonal_args(desc), desc->dtype);
+}
+
+int orthogonalize(const orthogonal_desc* desc, const void* x, void* out, void* workspace, size_t workspace_bytes, void* stream)
+{
+    const int rc = check_orthogonal(desc);
+    if (rc) return rc;
+    if (desc->batch == 0) return CONV_OK;
+    const int es = dtype_size(desc->dtype);
+    if (!x || !out || !aligned(x, es) || !aligned(out, es)) return CONV_EINVAL;
+    if (x == out && (desc->ldx != desc->ldo || (desc->batch > 1 && desc->stride_x != desc->stride_o))) return CONV_EINVAL;
+    OrthogonalArgs a = orthogonal_args(desc);
+    if (!workspace || workspace_bytes < orthogonal_workspace(a, desc->dtype)) return CONV_EWORKSPACE;
+    if (!aligned(workspace, 16)) return CONV_EINVAL;
+    a.x = x, a.out = out, a.ws = workspace;
+    return guarded("orthogonalize", [&] { return launch_orthogonalize(a, desc->dtype, (hipStream_t)stream); });
 }
 
 }  // extern "C"

@@ -215,3 +215,43 @@ def test_oracle_gradients_of_the_norms_against_differences(post, rms, gate_rows,
         for i in np.ndindex(a[k].shape):
             moved = [value({**a, k: a[k] + s * e * (np.indices(a[k].shape) == np.array(i).reshape(-1, *[1] * a[k].ndim)).all(0)}) for s in (1, -1)]
             assert abs((moved[0] - moved[1]) / (2 * e) - got["d" + k][i]) < 1e-6, (k, i)
+
+
+# ---- Newton-Schulz steps -----------------------------------------------------------------------------------------------
+
+
+def ns(d, x=P, out=2 * P, ws=P, n=1 << 62):
+    return status(B.orthogonalize, d, x, out, ws, n, stream=0)
+
+
+@pytest.mark.parametrize("change", [dict(batch=-1), dict(batch=1 << 31), dict(rows=0), dict(cols=0), dict(rows=(1 << 20) + 1), dict(steps=0), dict(steps=101), dict(ldx=7), dict(ldo=7),
+                                    dict(stride_x=-1), dict(stride_o=31), dict(a=float("nan")), dict(b=float("inf")), dict(c=float("nan")), dict(eps=-1.0), dict(eps=float("nan")),
+                                    dict(stride_o=1 << 62), dict(rows=1 << 18, cols=1 << 18, ldx=1 << 18, ldo=1 << 18, stride_o=1 << 36)])
+def test_orthogonal_descriptors_that_are_refused(change):
+    d = B.make_orthogonal_desc(4, 8, B.CONV_BF16, batch=2)
+    for k, v in change.items():
+        setattr(d, k, v)
+    assert ns(d) == B.CONV_EINVAL and B.orthogonalize_workspace_bytes(d) == 0
+
+
+def test_orthogonal_arguments_that_are_refused():
+    d = B.make_orthogonal_desc(4, 8, B.CONV_F32, batch=2)
+    need = B.orthogonalize_workspace_bytes(d)
+    assert need > 0
+    assert ns(d, x=None) == B.CONV_EINVAL and ns(d, out=None) == B.CONV_EINVAL and ns(d, x=P + 2) == B.CONV_EINVAL and ns(d, out=P + 1) == B.CONV_EINVAL
+    assert ns(d, n=need - 1) == B.CONV_EWORKSPACE and ns(d, ws=None) == B.CONV_EWORKSPACE and ns(d, ws=P + 8) == B.CONV_EINVAL
+    d.ldx, d.stride_x = 9, 36
+    assert ns(d, out=P) == B.CONV_EINVAL                  # in place with other strides
+    d.dtype = 3
+    assert ns(d) == B.CONV_EDTYPE
+    assert ns(B.make_orthogonal_desc(4, 8, batch=0), None, None, None, 0) == B.CONV_OK
+    assert B.lib().orthogonalize(None, P, P, P, 0, None) == B.CONV_EINVAL
+    assert B.lib().orthogonalize_workspace_bytes(None) == 0
+
+
+def test_oracle_of_the_steps_against_singular_values():
+    x = np.random.default_rng(1).normal(size=(6, 9))
+    u, s, v = np.linalg.svd(x / np.linalg.norm(x), full_matrices=False)
+    for _ in range(3):
+        s = 3.4445 * s - 4.7750 * s ** 3 + 2.0315 * s ** 5
+    assert np.allclose(ro.newton_schulz(x, 3, (3.4445, -4.7750, 2.0315), 0.0), u * s @ v, atol=1e-12)
