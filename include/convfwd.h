@@ -461,9 +461,9 @@ int logprob_bwd(const logprob_desc* desc, const void* logits, const int64_t* tar
  * normal distribution) or LINEAR_FLAG_SILU (z / (1 + exp(-z))).  bias (fp32 [N]) and residual may be NULL; pre, where it is not NULL, receives z
  * (what linear_bwd needs where there is an activation).  ldr is the row stride of the residual, ldo that of out, pre and dout; the
  * residual may be out itself where ldr == ldo.  All sums are fp32; out and pre are each rounded once.
- * fp32 products of more than a few rows are formed from three bf16 parts of each operand, six products of them: what is left out is below 2^-23 of each
+ * fp32 products of more than a few rows are formed from three bf16 parts of each operand, six products of them: what is left out is below 2^-25 of each
  * term.  There an operand's infinity, NaN or magnitude above 0x1.FEp127 makes NaN of the outputs it reaches, and parts below 2^-126 count as zero.
- * `workspace` (linear_workspace_bytes(desc), may be 0; 16-byte aligned) holds those parts and partial sums of shared reductions; NULL or a smaller one gives
+ * `workspace` (linear_workspace_bytes(desc), may be 0; 16-byte aligned) holds partial sums of shared reductions; NULL or a smaller one gives
  * CONV_EWORKSPACE when bytes are needed.  Operands whose rows start on 16 bytes are loaded faster.
  * CONV_EINVAL for rows < 0, N or K outside [1, 2^24), strides below the row's length, unknown flags or more than one activation, NULL or misaligned
  * pointers, outputs that are inputs.
@@ -493,7 +493,7 @@ int linear_bwd(const linear_desc* desc, const void* x, const void* w, const void
                float* dbias, void* workspace, size_t workspace_bytes, void* stream);
 
 /* Name of the form that a product takes for this descriptor and these operands' addresses (which count modulo 16), NUL-terminated in
- * buf[0..n), e.g. "rows16", "tile256x256" or "planes_tile64x64_split4"; `which`: 0 the product of linear_fwd, 1 and 2 those of linear_bwd for dx and
+ * buf[0..n), e.g. "rows16", "tile256x256" or "split_tile64x64_split4"; `which`: 0 the product of linear_fwd, 1 and 2 those of linear_bwd for dx and
  * dw.  Empty for no rows.  Pure host code. */
 int linear_form(const linear_desc* desc, const void* x, const void* w, int which, char* buf, size_t n);
 

@@ -74,7 +74,7 @@ typedef ProductTile<4, 2, 1, 2, 2> Tile64Any;
 
 enum ProductLayout { LAYOUT_NT, LAYOUT_NN, LAYOUT_TN };  // which operand lies across the reduction: none, the second, both
 
-// The products of bf16 and fp16 rows, and of bf16 planes with an fp32 result.  splits > 1: partial sums to g.partial.
+// The products of fp16, bf16 and fp32 rows (fp32: strides in elements of four bytes, tiles of 64 and 128).  splits > 1: partial sums to g.partial.
 hipError_t launch_product_f16(const ProductArgs& g, const LinearOut& e, ProductLayout layout, ProductForm form, int splits, hipStream_t s);
 hipError_t launch_product_bf16(const ProductArgs& g, const LinearOut& e, ProductLayout layout, ProductForm form, int splits, hipStream_t s);
 hipError_t launch_product_f32(const ProductArgs& g, const LinearOut& e, ProductLayout layout, ProductForm form, int splits, hipStream_t s);

@@ -1,9 +1,8 @@
 // Linear layers: out = act(x w^T + bias) + residual, and the gradients.  Which kernels a call takes, the form for few rows, and what stands
-// around the products: planes of fp32 operands, the gradient of the activation with its column sums, the join of shared reductions.
+// around the products: the gradient of the activation with its column sums, the join of shared reductions.
 #include <cstdio>
 
 #include "linear_common.h"
-#include "split_products.h"
 
 namespace convfwd {
 
@@ -181,34 +180,11 @@ __global__ __launch_bounds__(256) void linear_join(LinearOut e, const float* par
 
 // ---- around the products --------------------------------------------------------------------------------------------------
 
-// eight fp32 values as three pieces of bf16 each
-__device__ __forceinline__ void put_planes(uint16_t* p, int64_t plane, const float (&v)[8])
-{
-    uint32_t w[3][4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) split3_pair(v[2 * j], v[2 * j + 1], w[0][j], w[1][j], w[2][j]);
-#pragma unroll
-    for (int q = 0; q < 3; ++q) *(uint4*)(p + q * plane) = make_uint4(w[q][0], w[q][1], w[q][2], w[q][3]);
-}
-
-// fp32 [rows][cols] to three bf16 planes [rows][ldp] that add up to it, zeros from cols to ldp.
-__global__ __launch_bounds__(256) void linear_planes(const float* x, int64_t ldx, int64_t rows, int cols, uint16_t* out, int64_t ldp)
-{
-    const int64_t each = ldp / 8, all = rows * each, step = (int64_t)gridDim.x * 256;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += step) {
-        const int64_t t = all <= UINT32_MAX ? (uint32_t)i / (uint32_t)each : i / each;
-        const int j = (int)(i - t * each) * 8;
-        float v[8];
-        get8<CONV_F32>(x, t * ldx + j, v, cols - j);
-        put_planes(out + t * ldp + j, rows * ldp, v);
-    }
-}
-
 // The gradient at the sum: dz = dout act'(pre), with its sums over the rows.  A workgroup has 256 columns and `each` rows, eight lanes of
 // rows; the sums are of the values before they are rounded.
-// TO: 0 only the sums, 1 dz in the storage type with the row stride ldz, 2 three planes.
-template <int DT, int TO>
-__global__ __launch_bounds__(256) void linear_dz(const void* dout, const void* pre, int64_t ld, int64_t rows, int N, int act, uint16_t* dz, int64_t ldz,
+// TO: whether dz is written, in the storage type with the row stride ldz.
+template <int DT, bool TO>
+__global__ __launch_bounds__(256) void linear_dz(const void* dout, const void* pre, int64_t ld, int64_t rows, int N, int act, void* dz, int64_t ldz,
                                                  float* sums, int64_t each)
 {
     __shared__ float lds[8][32 * 8 + 8];
@@ -234,8 +210,7 @@ __global__ __launch_bounds__(256) void linear_dz(const void* dout, const void* p
                 if (k >= have) v[k] = 0.0f;
                 sum[k] += v[k];
             }
-            if constexpr (TO == 1) put8<DT>(dz, t * ldz + j, v, 8);
-            if constexpr (TO == 2) put_planes(dz + t * ldz + j, rows * ldz, v);
+            if constexpr (TO) put8<DT>(dz, t * ldz + j, v, (int)min((int64_t)8, ldz - j));
         }
     }
     if (!sums) return;
@@ -286,24 +261,26 @@ struct TileCost {
     double once, own, step;
 };
 constexpr TileCost kTiles[] = {{64, 64, 2.0, 1.2, 0.2}, {128, 128, 1.8, 1.5, 0.52}, {256, 256, 0, 11, 1.4}, {64, 64, 2.0, 1.5, 0.4}, {128, 128, 1.8, 1.5, 1.0}};
+constexpr TileCost kTilesF32[] = {{64, 64, 2.0, 1.2, 0.8}, {128, 128, 1.8, 1.5, 2.4}};
 
 struct ProductPlan {
     ProductForm form;
     int splits;
     double us;
 };
-ProductPlan plan_product(int64_t M, int64_t N, int64_t K, int segments, bool direct)
+ProductPlan plan_product(int64_t M, int64_t N, int64_t K, int dtype, bool direct)
 {
     ProductPlan best = {P64, 1, 1e30};
     const int64_t ksteps = (K + 63) / 64;
-    for (int f = direct ? P64 : P64_ANY; f <= (direct ? P256 : P128_ANY); ++f) {
-        const TileCost& c = kTiles[f];
+    const bool f32 = dtype == CONV_F32;
+    for (int f = f32 || direct ? P64 : P64_ANY; f <= (f32 ? P128 : direct ? P256 : P128_ANY); ++f) {
+        const TileCost& c = f32 ? kTilesF32[f] : kTiles[f];
         const double tiles = (double)((M + c.bt - 1) / c.bt) * ((N + c.bn - 1) / c.bn);
-        for (int splits = 1; splits <= 32; splits *= 2) {
-            if (splits > 1 && (splits * 4 > ksteps || tiles * splits > 1024)) break;
+        for (int splits = 1; splits <= 64; splits *= 2) {
+            if (splits > 1 && (splits * 4 > ksteps || tiles * splits > 2048)) break;
             const int64_t each = (ksteps + splits - 1) / splits;
             const int shares = (int)((ksteps + each - 1) / each);  // none without a step
-            double us = c.once + std::ceil(tiles * shares / 256) * (c.own + each * segments * c.step);
+            double us = c.once + std::ceil(tiles * shares / 256) * (c.own + each * c.step);
             if (shares > 1) us += 5 + 8.0 * shares * M * N / 4e6;  // written, read and added by a second launch
             if (us < best.us) best = {(ProductForm)f, shares, us};
         }
@@ -335,7 +312,7 @@ RowsPlan plan_rows(int64_t rows, int N, int K, int dtype)
 
 bool on_16(const void* p, int64_t ld, int size) { return ((uintptr_t)p & 15) == 0 && ld * size % 16 == 0 && ld < kLongStride; }
 
-// A forward call: few rows, or tiles (fp32: of planes).
+// A forward call: few rows, or tiles.
 struct LinearForm {
     bool rows, direct;
     RowsPlan few;
@@ -346,9 +323,7 @@ LinearForm form_of(int64_t rows, int N, int K, int dtype, bool direct)
     LinearForm f;
     f.direct = direct;
     f.few = plan_rows(rows, N, K, dtype);
-    const bool planes = dtype == CONV_F32;
-    f.tiles = plan_product(rows, N, K, planes ? 6 : 1, planes || direct);
-    if (planes) f.tiles.us += 5 + 10.0 * ((double)rows + N) * K / 4e6;
+    f.tiles = plan_product(rows, N, K, dtype, direct);
     f.rows = rows <= 16 || f.few.us <= f.tiles.us;
     return f;
 }
@@ -365,16 +340,7 @@ struct Carve {  // pieces of a workspace
     }
 };
 
-int64_t plane_stride(int64_t cols) { return round_up(cols, 64); }
-size_t plane_bytes(int64_t rows, int64_t cols) { return (size_t)(6 * rows * plane_stride(cols)); }
-
 unsigned grid_of(int64_t threads) { return (unsigned)std::min<int64_t>((threads + 255) / 256, 1 << 16); }
-
-hipError_t to_planes(const void* x, int64_t ld, int64_t rows, int cols, uint16_t* out, hipStream_t s)
-{
-    hipLaunchKernelGGL(linear_planes, dim3(grid_of(rows * plane_stride(cols) / 8)), dim3(256), 0, s, (const float*)x, ld, rows, cols, out, plane_stride(cols));
-    return hipGetLastError();
-}
 
 template <int DT>
 hipError_t join_as(const LinearOut& e, const float* partial, int64_t rows, int N, int splits, hipStream_t s)
@@ -388,24 +354,17 @@ hipError_t join(int dtype, const LinearOut& e, const float* partial, int64_t row
                              : dtype == CONV_F16 ? join_as<CONV_F16>(e, partial, rows, N, splits, s) : join_as<CONV_BF16>(e, partial, rows, N, splits, s);
 }
 
-// C = A B of 16-bit rows or of planes, and the join where a reduction is shared.
+// C = A B, and the join where a reduction is shared.
 struct Factor {
     const void* p;
-    int64_t ld, plane;
+    int64_t ld;
 };
 hipError_t multiply(int dtype, ProductLayout layout, const Factor& a, const Factor& b, int64_t M, int64_t N, int64_t K, const LinearOut& e,
                     const ProductPlan& plan, float* partial, hipStream_t s)
 {
     ProductArgs g = {};
-    g.a = (const uint16_t*)a.p, g.b = (const uint16_t*)b.p, g.lda = a.ld, g.ldb = b.ld, g.plane_a = a.plane, g.plane_b = b.plane;
-    g.M = M, g.N = N, g.K = K, g.partial = partial;
+    g.a = (const uint16_t*)a.p, g.b = (const uint16_t*)b.p, g.lda = a.ld, g.ldb = b.ld, g.M = M, g.N = N, g.K = K, g.partial = partial;
     g.ksteps = (int)((K + 63) / 64), g.segments = 1;
-    if (dtype == CONV_F32) {
-        // planes 2 0, 1 1, 0 2, 1 0, 0 1, 0 0: what is left out is below 2^-23 of a product
-        g.segments = 6;
-        g.seg_a = 2 | 1 << 2 | 0 << 4 | 1 << 6 | 0 << 8 | 0 << 10;
-        g.seg_b = 0 | 1 << 2 | 2 << 4 | 0 << 6 | 1 << 8 | 0 << 10;
-    }
     const auto launch = dtype == CONV_F32 ? launch_product_f32 : dtype == CONV_F16 ? launch_product_f16 : launch_product_bf16;
     const hipError_t err = launch(g, e, layout, plan.form, plan.splits, s);
     if (err != hipSuccess || plan.splits == 1) return err;
@@ -464,8 +423,11 @@ int64_t dz_rows(int64_t rows, int N)
 }
 int dz_parts(int64_t rows, int N) { return rows == 0 ? 0 : (int)((rows + dz_rows(rows, N) - 1) / dz_rows(rows, N)); }
 
+// Rows of dz start on 16 bytes in 16-bit types.
+int64_t dz_stride(int N, int dtype) { return dtype == CONV_F32 ? N : round_up(N, 8); }
+
 struct BwdSpace {
-    uint16_t *dz, *x, *w;  // dz in the storage type or in planes; planes of x and w
+    void* dz;
     float *sums, *partial;
     size_t bytes;
 };
@@ -474,17 +436,12 @@ BwdSpace bwd_space(const LinearArgs& a, int dtype, void* ws)
 {
     BwdSpace s = {};
     Carve c(ws);
-    const bool planes = dtype == CONV_F32;
-    s.dz = (uint16_t*)c.take(planes ? plane_bytes(a.rows, a.N) : (size_t)(2 * a.rows * round_up(a.N, 8)));
-    if (planes) {
-        s.x = (uint16_t*)c.take(plane_bytes(a.rows, a.K));
-        s.w = (uint16_t*)c.take(plane_bytes(a.N, a.K));
-    }
+    s.dz = c.take((size_t)(a.rows * dz_stride(a.N, dtype)) * dtype_size(dtype));
     s.sums = (float*)c.take((size_t)dz_parts(a.rows, a.N) * a.N * 4);
     size_t most = 0;
     for (const bool direct : {true, false}) {
-        most = std::max(most, partial_bytes(plan_product(a.rows, a.K, a.N, planes ? 6 : 1, direct), a.rows, a.K));
-        most = std::max(most, partial_bytes(plan_product(a.N, a.K, a.rows, planes ? 6 : 1, direct), a.N, a.K));
+        most = std::max(most, partial_bytes(plan_product(a.rows, a.K, a.N, dtype, direct), a.rows, a.K));
+        most = std::max(most, partial_bytes(plan_product(a.N, a.K, a.rows, dtype, direct), a.N, a.K));
     }
     s.partial = (float*)c.take(most);
     s.bytes = c.used;
@@ -492,16 +449,14 @@ BwdSpace bwd_space(const LinearArgs& a, int dtype, void* ws)
 }
 
 template <int DT>
-hipError_t launch_dz(const LinearArgs& a, int to, uint16_t* dz, int64_t ldz, float* sums, hipStream_t s)
+hipError_t launch_dz(const LinearArgs& a, void* dz, int64_t ldz, float* sums, hipStream_t s)
 {
-    const int64_t width = to ? ldz : a.N;
     const int64_t each = dz_rows(a.rows, a.N);
     const int parts = dz_parts(a.rows, a.N);
-    const dim3 grid((unsigned)((width + 255) / 256), (unsigned)parts);
+    const dim3 grid((unsigned)(((dz ? ldz : a.N) + 255) / 256), (unsigned)parts);
     float* const at = !a.dbias ? nullptr : parts == 1 ? a.dbias : sums;
-    if (to == 0) hipLaunchKernelGGL((linear_dz<DT, 0>), grid, dim3(256), 0, s, a.dout, a.pre_in, a.ldo, a.rows, a.N, a.act, dz, ldz, at, each);
-    else if (DT == CONV_F32) hipLaunchKernelGGL((linear_dz<DT, DT == CONV_F32 ? 2 : 1>), grid, dim3(256), 0, s, a.dout, a.pre_in, a.ldo, a.rows, a.N, a.act, dz, ldz, at, each);
-    else hipLaunchKernelGGL((linear_dz<DT, 1>), grid, dim3(256), 0, s, a.dout, a.pre_in, a.ldo, a.rows, a.N, a.act, dz, ldz, at, each);
+    if (dz) hipLaunchKernelGGL((linear_dz<DT, true>), grid, dim3(256), 0, s, a.dout, a.pre_in, a.ldo, a.rows, a.N, a.act, dz, ldz, at, each);
+    else hipLaunchKernelGGL((linear_dz<DT, false>), grid, dim3(256), 0, s, a.dout, a.pre_in, a.ldo, a.rows, a.N, a.act, dz, ldz, at, each);
     if (a.dbias && parts > 1) hipLaunchKernelGGL(linear_sums, dim3((unsigned)((a.N + 31) / 32)), dim3(256), 0, s, sums, parts, a.N, a.dbias);
     return hipGetLastError();
 }
@@ -517,12 +472,7 @@ size_t linear_fwd_workspace(int64_t rows, int N, int K, int dtype)
         const LinearForm f = form_of(rows, N, K, dtype, direct);
         size_t n = 0;
         if (f.rows) n = f.few.splits > 1 ? (size_t)f.few.splits * rows * N * 4 : 0;
-        else {
-            Carve c(nullptr);
-            if (dtype == CONV_F32) c.take(plane_bytes(rows, K)), c.take(plane_bytes(N, K));
-            c.take(partial_bytes(f.tiles, rows, N));
-            n = c.used;
-        }
+        else n = partial_bytes(f.tiles, rows, N);
         most = std::max(most, n);
     }
     return most;
@@ -544,16 +494,7 @@ hipError_t launch_linear_fwd(const LinearArgs& a, int dtype, hipStream_t s)
         const LinearRows g = {a.x, a.w, a.ldx, a.ldw, a.rows, a.N, a.K, out, (float*)a.ws};
         return dtype == CONV_F32 ? launch_rows<CONV_F32>(g, f, s) : dtype == CONV_F16 ? launch_rows<CONV_F16>(g, f, s) : launch_rows<CONV_BF16>(g, f, s);
     }
-    Carve c(a.ws);
-    Factor x = {a.x, a.ldx, 0}, w = {a.w, a.ldw, 0};
-    if (dtype == CONV_F32) {
-        x.p = c.take(plane_bytes(a.rows, a.K)), w.p = c.take(plane_bytes(a.N, a.K));
-        x.ld = w.ld = plane_stride(a.K), x.plane = a.rows * x.ld, w.plane = a.N * w.ld;
-        hipError_t e = to_planes(a.x, a.ldx, a.rows, a.K, (uint16_t*)x.p, s);
-        if (e == hipSuccess) e = to_planes(a.w, a.ldw, a.N, a.K, (uint16_t*)w.p, s);
-        if (e != hipSuccess) return e;
-    }
-    return multiply(dtype, LAYOUT_NT, x, w, a.rows, a.N, a.K, out, f.tiles, (float*)c.take(partial_bytes(f.tiles, a.rows, a.N)), s);
+    return multiply(dtype, LAYOUT_NT, {a.x, a.ldx}, {a.w, a.ldw}, a.rows, a.N, a.K, out, f.tiles, (float*)a.ws, s);
 }
 
 hipError_t launch_linear_bwd(const LinearArgs& a, int dtype, hipStream_t s)
@@ -565,37 +506,24 @@ hipError_t launch_linear_bwd(const LinearArgs& a, int dtype, hipStream_t s)
         return hipGetLastError();
     }
     const BwdSpace space = bwd_space(a, dtype, a.ws);
-    const bool planes = dtype == CONV_F32, products = a.dx || a.dw;
-    Factor dz = {a.dout, a.ldo, 0}, x = {a.x, a.ldx, 0}, w = {a.w, a.ldw, 0};
-    // dout is dz where there is no activation and its rows start on 16 bytes
-    const bool make = products && (planes || a.act || !on_16(a.dout, a.ldo, es));
-    if (make) {
-        dz.p = space.dz, dz.ld = planes ? plane_stride(a.N) : round_up(a.N, 8), dz.plane = a.rows * dz.ld;
-    }
+    const Factor x = {a.x, a.ldx}, w = {a.w, a.ldw};
+    Factor dz = {a.dout, a.ldo};
+    // dout is dz where there is no activation and its rows start on 16 bytes (in fp32 anywhere)
+    const bool make = (a.dx || a.dw) && (a.act || (dtype != CONV_F32 && !on_16(a.dout, a.ldo, es)));
+    if (make) dz = {space.dz, dz_stride(a.N, dtype)};
     if (make || a.dbias) {
-        const int to = !make ? 0 : planes ? 2 : 1;
-        const hipError_t e = planes ? launch_dz<CONV_F32>(a, to, space.dz, dz.ld, space.sums, s)
-                                    : dtype == CONV_F16 ? launch_dz<CONV_F16>(a, to, space.dz, dz.ld, space.sums, s) : launch_dz<CONV_BF16>(a, to, space.dz, dz.ld, space.sums, s);
+        void* const to = make ? space.dz : nullptr;
+        const hipError_t e = dtype == CONV_F32 ? launch_dz<CONV_F32>(a, to, dz.ld, space.sums, s)
+                                               : dtype == CONV_F16 ? launch_dz<CONV_F16>(a, to, dz.ld, space.sums, s) : launch_dz<CONV_BF16>(a, to, dz.ld, space.sums, s);
         if (e != hipSuccess) return e;
     }
-    if (planes && a.dx) {
-        w = {space.w, plane_stride(a.K), (int64_t)a.N * plane_stride(a.K)};
-        const hipError_t e = to_planes(a.w, a.ldw, a.N, a.K, space.w, s);
-        if (e != hipSuccess) return e;
-    }
-    if (planes && a.dw) {
-        x = {space.x, plane_stride(a.K), a.rows * plane_stride(a.K)};
-        const hipError_t e = to_planes(a.x, a.ldx, a.rows, a.K, space.x, s);
-        if (e != hipSuccess) return e;
-    }
-    const int segments = planes ? 6 : 1;
     if (a.dx) {
-        const ProductPlan p = plan_product(a.rows, a.K, a.N, segments, planes || (on_16(w.p, w.ld, es) && on_16(dz.p, dz.ld, es)));
+        const ProductPlan p = plan_product(a.rows, a.K, a.N, dtype, on_16(w.p, w.ld, es) && on_16(dz.p, dz.ld, es));
         const hipError_t e = multiply(dtype, LAYOUT_NN, dz, w, a.rows, a.K, a.N, {nullptr, nullptr, nullptr, a.dx, 0, a.ldx, ACT_NONE}, p, space.partial, s);
         if (e != hipSuccess) return e;
     }
     if (a.dw) {
-        const ProductPlan p = plan_product(a.N, a.K, a.rows, segments, planes || (on_16(x.p, x.ld, es) && on_16(dz.p, dz.ld, es)));
+        const ProductPlan p = plan_product(a.N, a.K, a.rows, dtype, on_16(x.p, x.ld, es) && on_16(dz.p, dz.ld, es));
         const hipError_t e = multiply(dtype, LAYOUT_TN, dz, x, a.N, a.K, a.rows, {nullptr, nullptr, nullptr, a.dw, 0, a.ldw, ACT_NONE}, p, space.partial, s);
         if (e != hipSuccess) return e;
     }
@@ -606,7 +534,7 @@ int linear_form_name(const LinearArgs& a, int dtype, int which, char* buf, size_
 {
     static const char* const tiles[] = {"tile64x64", "tile128x128", "tile256x256", "tile64x64_any", "tile128x128_any"};
     const int es = dtype_size(dtype);
-    const bool planes = dtype == CONV_F32, x16 = on_16(a.x, a.ldx, es), w16 = on_16(a.w, a.ldw, es);
+    const bool x16 = on_16(a.x, a.ldx, es), w16 = on_16(a.w, a.ldw, es);
     ProductPlan p;
     if (which == 0) {
         const LinearForm f = form_of(a.rows, a.N, a.K, dtype, x16 && w16);
@@ -616,11 +544,11 @@ int linear_form_name(const LinearArgs& a, int dtype, int which, char* buf, size_
         }
         p = f.tiles;
     } else if (which == 1) {
-        p = plan_product(a.rows, a.K, a.N, planes ? 6 : 1, planes || w16);
+        p = plan_product(a.rows, a.K, a.N, dtype, w16);
     } else {
-        p = plan_product(a.N, a.K, a.rows, planes ? 6 : 1, planes || x16);
+        p = plan_product(a.N, a.K, a.rows, dtype, x16);
     }
-    const int len = std::snprintf(buf, n, "%s%s", planes ? "planes_" : "", tiles[p.form]);
+    const int len = std::snprintf(buf, n, "%s%s", dtype == CONV_F32 ? "split_" : "", tiles[p.form]);
     return p.splits > 1 && len > 0 && (size_t)len < n ? std::snprintf(buf + len, n - len, "_split%d", p.splits) : len;
 }
 

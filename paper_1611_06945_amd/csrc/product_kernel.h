@@ -14,8 +14,7 @@
 //     the bounds check of the buffer descriptor, which moves along with the reduction, so that offsets stay below 2^31 however long it is.  A row's
 //     bytes past K belong to what follows and are cleared in both operands on the last step.  Otherwise pieces go
 //     through registers, from any address, and their ends are cleared on the way.
-//   * fp32 operands are sums of three bf16 planes each, of which six products count; a product over planes is a reduction of `segments` times
-//     the length, the smallest terms first.
+//   * An operand may be a sum of planes; a product over them is a reduction of `segments` times the length, the smallest terms first.
 #pragma once
 
 #include <algorithm>
@@ -208,6 +207,42 @@ struct ProductArgs {
     float* partial;               // sums of gridDim.z workgroups, [z][M][N]
 };
 
+// Consecutive workgroups go to different XCDs: each XCD takes a run of tiles.
+__device__ __forceinline__ int tile_in_order()
+{
+    const int total = gridDim.x, q = total / 8, r = total % 8, x = blockIdx.x % 8, i = blockIdx.x / 8;
+    return x * q + min(x, r) + i;
+}
+// ... in bands of eight tiles of n
+__device__ __forceinline__ void tile_of_block(int tiles_m, int tiles_n, int& tm, int& tn)
+{
+    const int tile = tile_in_order();
+    const int band = tile / (8 * tiles_m), in_band = tile - band * 8 * tiles_m;
+    const int width = min(8, tiles_n - band * 8);
+    tn = band * 8 + in_band % width, tm = in_band / width;
+}
+// ... of those with n >= m only: row tm has the tiles tm .. tiles - 1
+__device__ __forceinline__ void tile_above_diagonal(int tiles, int& tm, int& tn)
+{
+    int tile = tile_in_order();
+    tm = 0;
+    for (int left = tiles; tile >= left; --left) tile -= left, ++tm;
+    tn = tm + tile;
+}
+
+// A lane has four n 4 (lane / 16) .. of a block and m = lane % 16 of a block of rows.  Neighbouring groups of 16 lanes trade between two
+// blocks of n, so that a lane has eight n in a row: the groups 0 .. 3 those of the first block from 0, of the second from 0, of the first
+// from 8, of the second from 8.
+__device__ __forceinline__ void eight_in_a_row(const f32x4& first, const f32x4& second, float (&v)[8])
+{
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const float here = first[r], there = second[r];  // (a cast of a vector's element itself takes the first one)
+        const auto two = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, here), __builtin_bit_cast(uint32_t, there), false, false);
+        v[r] = __builtin_bit_cast(float, (uint32_t)two[0]), v[4 + r] = __builtin_bit_cast(float, (uint32_t)two[1]);
+    }
+}
+
 // Epi: what becomes of the sums.  symmetric: only the tiles with n >= m are formed.
 template <int DT, typename T, bool A_ACROSS, bool B_ACROSS, bool DIRECT, typename Epi>
 __global__ __launch_bounds__(T::NT) void product_kernel(ProductArgs g, typename Epi::Args e)
@@ -216,24 +251,9 @@ __global__ __launch_bounds__(T::NT) void product_kernel(ProductArgs g, typename 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wt = wave % T::WT, wn = wave / T::WT;
 
-    // consecutive workgroups go to different XCDs: each XCD takes a run of tiles, in bands of eight tiles of n
     int tm, tn;
-    {
-        const int total = gridDim.x;
-        int tile = blockIdx.x;
-        const int q = total / 8, r = total % 8, x = tile % 8, i = tile / 8;
-        tile = x * q + min(x, r) + i;
-        if constexpr (Epi::SYMMETRIC) {
-            // row tm has the tiles tm .. tiles_m - 1
-            tm = 0;
-            for (int left = g.tiles_m; tile >= left; --left) tile -= left, ++tm;
-            tn = tm + tile;
-        } else {
-            const int band = tile / (8 * g.tiles_m), in_band = tile - band * 8 * g.tiles_m;
-            const int width = min(8, g.tiles_n - band * 8);
-            tn = band * 8 + in_band % width, tm = in_band / width;
-        }
-    }
+    if constexpr (Epi::SYMMETRIC) tile_above_diagonal(g.tiles_m, tm, tn);
+    else tile_of_block(g.tiles_m, g.tiles_n, tm, tn);
     const int64_t m0 = (int64_t)tm * T::BT, n0 = (int64_t)tn * T::BN;
     const int ks0 = blockIdx.z * g.each, ks1 = min(ks0 + g.each, g.ksteps);
 
@@ -385,9 +405,6 @@ __global__ __launch_bounds__(T::NT) void product_kernel(ProductArgs g, typename 
         }
     }
 
-    // A lane has four n 4 (lane / 16) .. of a block and m = lane % 16 of a block of rows.  Neighbouring groups of 16 lanes trade between two
-    // blocks of n, so that a lane has eight n in a row: the groups 0 .. 3 those of block i from 0, of block i + 1 from 0, of block i from 8,
-    // of block i + 1 from 8.
     const int grp = lane >> 4;
 #pragma unroll
     for (int i = 0; i < T::FN; i += 2) {
@@ -396,12 +413,7 @@ __global__ __launch_bounds__(T::NT) void product_kernel(ProductArgs g, typename 
         for (int j = 0; j < T::FT; ++j) {
             const int ml = (wt * T::FT + j) * 16 + (lane & 15);
             float v[8];
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const float here = acc[i][j][r], there = acc[i + 1][j][r];  // (a cast of a vector's element itself takes the first one)
-                const auto two = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, here), __builtin_bit_cast(uint32_t, there), false, false);
-                v[r] = __builtin_bit_cast(float, (uint32_t)two[0]), v[4 + r] = __builtin_bit_cast(float, (uint32_t)two[1]);
-            }
+            eight_in_a_row(acc[i][j], acc[i + 1][j], v);
             if (ml < a.here && nl < b.here) Epi::finish(g, e, v, g.m_first + m0 + ml, n0 + nl, min(8, b.here - nl), bias + nl);
         }
         __builtin_amdgcn_sched_barrier(0);

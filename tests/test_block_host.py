@@ -79,7 +79,7 @@ def test_linear_bwd_pointers_that_are_refused():
 
 
 def test_linear_workspaces_that_are_refused():
-    d = B.make_linear_desc(8192, 8192, 4096)
+    d = B.make_linear_desc(256, 256, 1 << 16, B.CONV_BF16)  # a long reduction for few tiles, shared by workgroups
     for call, need in ((fwd, B.linear_workspace_bytes(d)), (bwd, B.linear_bwd_workspace_bytes(d))):
         assert need > 0
         assert call(d, ws=None, n=need) == B.CONV_EWORKSPACE
@@ -98,7 +98,7 @@ def test_linear_forms():
     names = {B.linear_form(B.make_linear_desc(r, n, k, B.CONV_BF16), 0, 0) for r, n, k in ((1, 4096, 4096), (2048, 2048, 2048), (8192, 8192, 8192), (1024, 1024, 1024))}
     assert names >= {"rows16", "tile256x256"} and len(names) >= 3
     assert B.linear_form(B.make_linear_desc(2048, 1001, 2048, B.CONV_BF16), 0, 2).endswith("_any")
-    assert B.linear_form(B.make_linear_desc(2048, 2048, 2048, B.CONV_F32)).startswith("planes_")
+    assert B.linear_form(B.make_linear_desc(2048, 2048, 2048, B.CONV_F32)).startswith("split_")
     assert "_split" in B.linear_form(B.make_linear_desc(65536, 256, 256, B.CONV_BF16), which=2)
 
 
