@@ -7,10 +7,25 @@ namespace convfwd {
 
 enum { ACT_NONE = 0, ACT_RELU = 1, ACT_GELU = 2, ACT_SILU = 3 };
 
+// The normal distribution Phi(z) and exp(-z^2 / 2), by the rational approximation 7.1.26 of Abramowitz and Stegun's handbook, which is off by
+// 1.5e-7 / 2 at most; erff() takes four times the instructions, 8 us of the 44 of 3380 x 384 x 1536.
+__device__ __forceinline__ float normal_distribution(float z, float& bell)
+{
+    const float x = fabsf(z) * 0.70710678118654752f, t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.3275911f, x, 1.0f));
+    bell = __expf(-x * x);
+    float p = __builtin_fmaf(1.061405429f, t, -1.453152027f);
+    p = __builtin_fmaf(p, t, 1.421413741f);
+    p = __builtin_fmaf(p, t, -0.284496736f);
+    p = __builtin_fmaf(p, t, 0.254829592f);
+    const float tail = 0.5f * p * t * bell;  // Phi(-|z|)
+    return z < 0.0f ? tail : 1.0f - tail;
+}
+
 __device__ __forceinline__ float act_of(float z, int act)
 {
+    float bell;
     if (act == ACT_RELU) return z < 0.0f ? 0.0f : z;  // a NaN stays
-    if (act == ACT_GELU) return 0.5f * z * (1.0f + erff(z * 0.70710678118654752f));
+    if (act == ACT_GELU) return z * normal_distribution(z, bell);
     if (act == ACT_SILU) return z / (1.0f + __expf(-z));
     return z;
 }
@@ -18,7 +33,11 @@ __device__ __forceinline__ float act_of(float z, int act)
 __device__ __forceinline__ float act_slope(float z, int act)
 {
     if (act == ACT_RELU) return z > 0.0f ? 1.0f : z <= 0.0f ? 0.0f : z;
-    if (act == ACT_GELU) return 0.5f * (1.0f + erff(z * 0.70710678118654752f)) + z * __expf(-0.5f * z * z) * 0.39894228040143268f;
+    if (act == ACT_GELU) {
+        float bell;
+        const float phi = normal_distribution(z, bell);
+        return __builtin_fmaf(z * bell, 0.39894228040143268f, phi);
+    }
     if (act == ACT_SILU) {
         const float p = 1.0f / (1.0f + __expf(-z));
         return p * (1.0f + z * (1.0f - p));
@@ -74,7 +93,7 @@ typedef ProductTile<4, 2, 1, 2, 2> Tile64Any;
 
 enum ProductLayout { LAYOUT_NT, LAYOUT_NN, LAYOUT_TN };  // which operand lies across the reduction: none, the second, both
 
-// The products of fp16, bf16 and fp32 rows (fp32: strides in elements of four bytes, tiles of 64 and 128).  splits > 1: partial sums to g.partial.
+// The products of fp16, bf16 and fp32 rows (fp32: strides in elements of four bytes, tiles of 64 x 64, 128 x 128 and 256 x 128).  splits > 1: partial sums to g.partial.
 hipError_t launch_product_f16(const ProductArgs& g, const LinearOut& e, ProductLayout layout, ProductForm form, int splits, hipStream_t s);
 hipError_t launch_product_bf16(const ProductArgs& g, const LinearOut& e, ProductLayout layout, ProductForm form, int splits, hipStream_t s);
 hipError_t launch_product_f32(const ProductArgs& g, const LinearOut& e, ProductLayout layout, ProductForm form, int splits, hipStream_t s);

@@ -260,8 +260,8 @@ struct TileCost {
     int bt, bn;
     double once, own, step;
 };
-constexpr TileCost kTiles[] = {{64, 64, 2.0, 1.2, 0.2}, {128, 128, 1.8, 1.5, 0.52}, {256, 256, 0, 11, 1.4}, {64, 64, 2.0, 1.5, 0.4}, {128, 128, 1.8, 1.5, 1.0}};
-constexpr TileCost kTilesF32[] = {{64, 64, 2.0, 1.2, 0.8}, {128, 128, 1.8, 1.5, 2.4}};
+constexpr TileCost kTiles[] = {{64, 64, 4.1, 1.0, 0.275}, {128, 128, 3.1, 1.7, 0.53}, {256, 256, 0, 6.4, 1.18}, {64, 64, 4.0, 0.4, 0.45}, {128, 128, 2.6, 2.4, 0.93}};
+constexpr TileCost kTilesF32[] = {{64, 64, 4.5, 0.5, 1.3}, {128, 128, 0, 6.2, 2.75}, {256, 128, 0, 8.1, 4.7}};
 
 struct ProductPlan {
     ProductForm form;
@@ -273,7 +273,7 @@ ProductPlan plan_product(int64_t M, int64_t N, int64_t K, int dtype, bool direct
     ProductPlan best = {P64, 1, 1e30};
     const int64_t ksteps = (K + 63) / 64;
     const bool f32 = dtype == CONV_F32;
-    for (int f = f32 || direct ? P64 : P64_ANY; f <= (f32 ? P128 : direct ? P256 : P128_ANY); ++f) {
+    for (int f = f32 || direct ? P64 : P64_ANY; f <= (f32 || direct ? P256 : P128_ANY); ++f) {
         const TileCost& c = f32 ? kTilesF32[f] : kTiles[f];
         const double tiles = (double)((M + c.bt - 1) / c.bt) * ((N + c.bn - 1) / c.bn);
         for (int splits = 1; splits <= 64; splits *= 2) {
@@ -548,7 +548,7 @@ int linear_form_name(const LinearArgs& a, int dtype, int which, char* buf, size_
     } else {
         p = plan_product(a.N, a.K, a.rows, dtype, x16);
     }
-    const int len = std::snprintf(buf, n, "%s%s", dtype == CONV_F32 ? "split_" : "", tiles[p.form]);
+    const int len = dtype == CONV_F32 ? std::snprintf(buf, n, "split_%s", p.form == P256 ? "tile256x128" : tiles[p.form]) : std::snprintf(buf, n, "%s", tiles[p.form]);
     return p.splits > 1 && len > 0 && (size_t)len < n ? std::snprintf(buf + len, n - len, "_split%d", p.splits) : len;
 }
 

@@ -4,9 +4,10 @@
 //
 // x = x0 + x1 + x2 with 8 bits each holds all 24 bits of an fp32 value; of the nine products of parts the six that count are formed: 1 1, 0 2 and 2 0 first,
 // then 0 1 and 1 0, then 0 0.  What is left out is below 2^-25 of a product.  Six products at the bf16 rate are 2.6 times as fast as the fp32 matrix
-// instructions.  An element is split once for a workgroup: pieces of eight go from memory to registers, one step ahead, and as three planes to
+// instructions.  An element is split once for a workgroup: pieces of eight go from memory to registers, D steps ahead, and as three planes to
 // LDS, so operands may start anywhere.  A stage has 32 of the reduction: 64 bytes of each row and plane (pieces at piece ^ (row / 4 % 4)), or 32 rows
-// across.  One stage only, so that two or three workgroups a CU fill each other's waits.
+// across.  There are two stages: the next one is split and written between the products of the present one, since splitting is as much vector work as half of
+// the products' time and a workgroup that did one after the other took 2.1 us a step of 128 x 128, whose products are 0.64.
 #pragma once
 
 #include "linear_common.h"
@@ -14,60 +15,43 @@
 
 namespace convfwd {
 
-template <int WT_, int WN_, int FT_, int FN_>
+template <int WT_, int WN_, int FT_, int FN_, int D_, int S_>
 struct SplitTile {
-    static constexpr int WT = WT_, WN = WN_, FT = FT_, FN = FN_;
+    static constexpr int S = S_;  // stages
+    static constexpr int WT = WT_, WN = WN_, FT = FT_, FN = FN_, D = D_;  // D: steps that are on their way
     static constexpr int BT = 16 * WT * FT, BN = 16 * WN * FN, NT = 64 * WT * WN, KE = 32;
     static constexpr int PLANE_A = BT * KE * 2, PLANE_B = BN * KE * 2;  // bytes of a plane of a stage
-    static constexpr size_t LDS = 3 * (PLANE_A + PLANE_B) + BN * 4;
+    static constexpr int STAGE = 3 * (PLANE_A + PLANE_B);
+    static constexpr size_t LDS = S * STAGE + BN * 4;
     static constexpr int LA = BT * 4 / NT, LB = BN * 4 / NT;            // pieces of eight a thread
     static_assert(LA * NT == BT * 4 && LB * NT == BN * 4 && FN % 2 == 0, "whole loads");
 };
 
 template <typename T, int W, int L, bool ACROSS>
 struct SplitOperand {
-    const float* from;  // the tile's first element of the next step
-    int64_t ld, left;   // left: of the reduction
-    int here;
-    float held[L][8];
+    typedef AnyPieces<float, T::NT, W, T::KE, L, ACROSS> Pieces;
+    Pieces pieces;
+    float held[T::D][L][8];
 
-    static __device__ __forceinline__ void place(int i, int& row, int& piece)
-    {
-        const int p = i * T::NT + (int)threadIdx.x;
-        row = ACROSS ? p / (W / 8) : p / 4, piece = ACROSS ? p % (W / 8) : p % 4;
-    }
-    __device__ __forceinline__ void begin(const float* p, int64_t stride, int64_t K, int64_t first, int64_t all, int64_t k0)
-    {
-        ld = stride, left = K - k0;
-        here = (int)min((int64_t)W, all - first);
-        from = p + (ACROSS ? first + k0 * stride : first * stride + k0);
-    }
+    template <int S>
     __device__ __forceinline__ void load()
     {
-        const bool whole = here == W && left >= T::KE;
-#pragma unroll
-        for (int i = 0; i < L; ++i) {
-            int row, piece;
-            place(i, row, piece);
-            const float* p = from + row * ld + piece * 8;
-            const int64_t n = ACROSS ? (row < left ? here - piece * 8 : 0) : (row < here ? left - piece * 8 : 0);
-            if (whole || n >= 8) {
-                __builtin_memcpy(held[i], p, 32);
-            } else {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) held[i][j] = j < n ? p[j] : 0.0f;
-            }
-        }
-        from += ACROSS ? T::KE * ld : (int64_t)T::KE;
-        left -= T::KE;
+        pieces.load(held[S]);
     }
-    __device__ __forceinline__ void commit(char* lds, int plane) const
+    template <int S>
+    __device__ __forceinline__ void clear()
+    {
+        pieces.clear(held[S]);
+    }
+    // pieces FROM .. TO - 1 of a step
+    template <int S, int FROM, int TO>
+    __device__ __forceinline__ void commit(char* lds, int plane)
     {
 #pragma unroll
-        for (int i = 0; i < L; ++i) {
+        for (int i = FROM; i < TO; ++i) {
             int row, piece;
-            place(i, row, piece);
-            const Split3 s = split3(held[i]);
+            Pieces::place(i, row, piece);
+            const Split3 s = split3(held[S][i]);
             char* to = lds + (ACROSS ? row * (W * 2) + (piece ^ across_swizzle<W>(row)) * 16 : row * 64 + ((piece ^ ((row >> 2) & 3)) << 4));
 #pragma unroll
             for (int q = 0; q < 3; ++q) *(uint4*)(to + q * plane) = s.p[q];
@@ -116,11 +100,10 @@ __global__ __launch_bounds__(T::NT) void product_f32_kernel(SplitArgs g, LinearO
 
     SplitOperand<T, T::BT, T::LA, A_ACROSS> a;
     SplitOperand<T, T::BN, T::LB, B_ACROSS> b;
-    a.begin(g.a, g.lda, k1, m0, g.M, k0);
-    b.begin(g.b, g.ldb, k1, n0, g.N, k0);
-    char *const lds_a = smem, *const lds_b = smem + 3 * T::PLANE_A;
-    float* const bias = (float*)(smem + 3 * (T::PLANE_A + T::PLANE_B));
-    if constexpr (!PARTIAL) LinearEpi<CONV_F32>::prepare(e, bias, n0, b.here, T::BN, T::NT);
+    a.pieces.begin(g.a, g.lda, k1, m0, g.M, k0);
+    b.pieces.begin(g.b, g.ldb, k1, n0, g.N, k0);
+    float* const bias = (float*)(smem + T::S * T::STAGE);
+    if constexpr (!PARTIAL) LinearEpi<CONV_F32>::prepare(e, bias, n0, b.pieces.here, T::BN, T::NT);
 
     f32x4 acc[T::FN][T::FT];
 #pragma unroll
@@ -128,28 +111,59 @@ __global__ __launch_bounds__(T::NT) void product_f32_kernel(SplitArgs g, LinearO
 #pragma unroll
         for (int j = 0; j < T::FT; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 
-    a.load(), b.load();
-    for (int64_t k = k0; k < k1; k += T::KE) {
-        __syncthreads();  // the stage has been read
-        a.commit(lds_a, T::PLANE_A), b.commit(lds_b, T::PLANE_B);
+    // (steps past the last load nothing: there is nothing left of the reduction)
+    typedef std::integral_constant<int, 0> Zero;
+    auto commit = [&](char* stage, auto slot, auto part) {  // part of FT
+        constexpr int S = decltype(slot)::value, P = decltype(part)::value;
+        if constexpr (P == 0) a.template clear<S>(), b.template clear<S>();
+        a.template commit<S, T::LA * P / T::FT, T::LA * (P + 1) / T::FT>(stage, T::PLANE_A);
+        b.template commit<S, T::LB * P / T::FT, T::LB * (P + 1) / T::FT>(stage + 3 * T::PLANE_A, T::PLANE_B);
+    };
+    count_to<T::D>([&](auto d) { a.template load<decltype(d)::value>(), b.template load<decltype(d)::value>(); });
+    if constexpr (T::S == 2) {
+        count_to<T::FT>([&](auto p) { commit(smem, Zero(), p); });
+        a.template load<0>(), b.template load<0>();
         __syncthreads();
-        if (k + T::KE < k1) a.load(), b.load();
-        u32x4 bv[T::FN][3];
+    }
+    int64_t k = k0;
+    for (int buf = 0; k < k1;) {
+        // step i is in stage i % S; two stages: step i + 1 in slot (i + 1) % D of the registers, one: step i in slot i % D
+        count_to<T::D>([&](auto d) {
+            constexpr int SLOT = (decltype(d)::value + T::S - 1) % T::D;
+            typedef std::integral_constant<int, SLOT> Slot;
+            if (k >= k1) return;
+            k += T::KE;
+            if constexpr (T::S == 1) {
+                __syncthreads();  // the stage has been read
+                count_to<T::FT>([&](auto p) { commit(smem, Slot(), p); });
+                __syncthreads();
+                a.template load<SLOT>(), b.template load<SLOT>();
+            }
+            const char *const at_a = smem + buf * T::STAGE, *const at_b = at_a + 3 * T::PLANE_A;
+            char* const next = smem + (buf ^ 1) * T::STAGE;
+            u32x4 bv[T::FN][3];
 #pragma unroll
-        for (int i = 0; i < T::FN; ++i)
+            for (int i = 0; i < T::FN; ++i)
 #pragma unroll
-            for (int q = 0; q < 3; ++q) bv[i][q] = b.fragment(lds_b + q * T::PLANE_B, wn * T::FN + i);
+                for (int q = 0; q < 3; ++q) bv[i][q] = b.fragment(at_b + q * T::PLANE_B, wn * T::FN + i);
+            count_to<T::FT>([&](auto part) {
+                constexpr int j = decltype(part)::value;
+                u32x4 av[3];
 #pragma unroll
-        for (int j = 0; j < T::FT; ++j) {
-            u32x4 av[3];
+                for (int q = 0; q < 3; ++q) av[q] = a.fragment(at_a + q * T::PLANE_A, wt * T::FT + j);
+                if (T::S == 2 && k < k1) commit(next, Slot(), part);
+                constexpr int PA[6] = {1, 0, 2, 0, 1, 0}, PB[6] = {1, 2, 0, 1, 0, 0};
 #pragma unroll
-            for (int q = 0; q < 3; ++q) av[q] = a.fragment(lds_a + q * T::PLANE_A, wt * T::FT + j);
-            constexpr int PA[6] = {1, 0, 2, 0, 1, 0}, PB[6] = {1, 2, 0, 1, 0, 0};
+                for (int t = 0; t < 6; ++t)
 #pragma unroll
-            for (int t = 0; t < 6; ++t)
-#pragma unroll
-                for (int i = 0; i < T::FN; ++i) acc[i][j] = multiply16<CONV_BF16>(bv[i][PB[t]], av[PA[t]], acc[i][j]);
-        }
+                    for (int i = 0; i < T::FN; ++i) acc[i][j] = multiply16<CONV_BF16>(bv[i][PB[t]], av[PA[t]], acc[i][j]);
+            });
+            if constexpr (T::S == 2) {
+                a.template load<SLOT>(), b.template load<SLOT>();
+                __syncthreads();
+                buf ^= 1;
+            }
+        });
     }
 
     // as in product_kernel: eight n in a row for each lane
@@ -162,8 +176,8 @@ __global__ __launch_bounds__(T::NT) void product_f32_kernel(SplitArgs g, LinearO
             const int ml = (wt * T::FT + j) * 16 + (lane & 15);
             float v[8];
             eight_in_a_row(acc[i][j], acc[i + 1][j], v);
-            if (ml < a.here && nl < b.here) {
-                const int have = min(8, b.here - nl);
+            if (ml < a.pieces.here && nl < b.pieces.here) {
+                const int have = min(8, b.pieces.here - nl);
                 const int64_t m = g.m_first + m0 + ml;
                 if constexpr (PARTIAL) put8<CONV_F32>(g.partial, ((int64_t)blockIdx.z * g.M + m) * g.N + n0 + nl, v, have);
                 else LinearEpi<CONV_F32>::finish(ProductArgs(), e, v, m, n0 + nl, have, bias + nl);

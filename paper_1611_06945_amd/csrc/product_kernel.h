@@ -76,6 +76,80 @@ __device__ __forceinline__ f32x4 multiply16(u32x4 b, u32x4 a, f32x4 c)
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, b), __builtin_bit_cast(bf16x8, a), c, 0, 0, 0);
 }
 
+// Pieces of eight elements from any address to registers, KE of the reduction a step, L pieces a thread.  Loads have no branch around them that lanes take apart: a wave
+// would wait there for all its loads, and a step take a trip to memory.  Instead a lane without a piece reads another one's, and what a
+// piece holds past the reduction's end is cleared where it is used.  Only a step in which a piece would pass the end of the whole operand
+// loads element by element.
+template <typename E, int NT, int W, int KE, int L, bool ACROSS>
+struct AnyPieces {
+    const E* from;  // the tile's first element of the next step
+    int64_t ld, left, used;  // left: of the reduction, for load; used: for clear
+    int here;                // rows (ALONG) or columns (ACROSS) of the tile that exist
+    bool last;               // ALONG: whether nothing follows the tile's last row; ACROSS: whether a piece passes the last column
+    int64_t off[L];
+
+    static __device__ __forceinline__ void place(int i, int& row, int& piece)
+    {
+        const int p = i * NT + (int)threadIdx.x;
+        row = ACROSS ? p / (W / 8) : p / (KE / 8), piece = ACROSS ? p % (W / 8) : p % (KE / 8);
+    }
+    __device__ __forceinline__ void begin(const E* p, int64_t stride, int64_t K, int64_t first, int64_t all, int64_t k0)
+    {
+        ld = stride, left = used = K - k0;
+        here = (int)min((int64_t)W, all - first);
+        last = ACROSS ? (here & 7) != 0 : first + here >= all || K < 8;
+        from = p + (ACROSS ? first + k0 * stride : first * stride + k0);
+#pragma unroll
+        for (int i = 0; i < L; ++i) {
+            int row, piece;
+            place(i, row, piece);
+            off[i] = ACROSS ? row * ld + (piece * 8 < here ? piece * 8 : 0) : min(row, here - 1) * ld + piece * 8;
+        }
+    }
+    __device__ __forceinline__ void load(E (&to)[L][8])
+    {
+        // (ACROSS: eight more rows hold the seven elements that a piece may pass its row's last column by, however short they are)
+        if (left >= KE + (ACROSS && last ? 8 : 0)) {
+#pragma unroll
+            for (int i = 0; i < L; ++i) __builtin_memcpy(to[i], from + off[i], 8 * sizeof(E));
+        } else if (left > 0) {
+#pragma unroll
+            for (int i = 0; i < L; ++i) {
+                int row, piece;
+                place(i, row, piece);
+                if (!last) {
+                    // (ALONG: a piece that passes its row's end goes on in the next row)
+                    const int64_t at = ACROSS ? min((int64_t)row, left - 1) * ld + (piece * 8 < here ? piece * 8 : 0)
+                                              : min(row, here - 1) * ld + (piece * 8 < left ? piece * 8 : 0);
+                    __builtin_memcpy(to[i], from + at, 8 * sizeof(E));
+                } else {
+                    const E* p = from + row * ld + piece * 8;
+                    const int64_t n = ACROSS ? (row < left ? here - piece * 8 : 0) : (row < here ? left - piece * 8 : 0);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) to[i][j] = j < n ? p[j] : (E)0;
+                }
+            }
+        }
+        from += ACROSS ? KE * ld : (int64_t)KE;
+        left -= KE;
+    }
+    // what is past the reduction's end becomes zeros; once for each load, in their order
+    __device__ __forceinline__ void clear(E (&v)[L][8])
+    {
+        if (used < KE) {
+#pragma unroll
+            for (int i = 0; i < L; ++i) {
+                int row, piece;
+                place(i, row, piece);
+                const int64_t n = ACROSS ? (row < used ? 8 : 0) : used - piece * 8;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[i][j] = j < n ? v[i][j] : (E)0;
+            }
+        }
+        used -= KE;
+    }
+};
+
 // 16 bytes a lane from offset `off` of a descriptor to LDS, the wave's 1024 bytes from `to`.  It is the instruction of
 // __builtin_amdgcn_raw_ptr_buffer_load_lds, written out because the compiler lets no transposing LDS read (a builtin that may read anything)
 // pass such a builtin without waiting for all of them: a step's loads would have a quarter of the step to arrive.  It has no
@@ -85,6 +159,34 @@ __device__ __forceinline__ void load_to_lds(u32x4 r, uint32_t to, uint32_t off)
     asm volatile("s_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"{m0}"(to), "v"(off), "s"(r));
 }
 
+// The matrix operand of block `block` (16 wide) for half s of a stage of 64 of the reduction.
+template <int W, bool ACROSS>
+__device__ __forceinline__ u32x4 fragment_of(const char* lds, int block, int s)
+{
+    const int lane = threadIdx.x & 63;
+    if constexpr (ACROSS) {
+        typedef short s16x4 __attribute__((ext_vector_type(4)));
+        typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+        const int k = (lane >> 4) * 8 + ((lane & 15) >> 2);
+        const char* p = lds + (s * 32 + k) * (W * 2) + ((block * 2) ^ across_swizzle<W>(k)) * 16 + (lane & 3) * 8;
+        union {
+            s16x4 h[2];
+            u32x4 v;
+        } u;
+        u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)p);
+        u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 4 * W * 2));
+        return u.v;
+    } else {
+        return *(const u32x4*)(lds + block * 2048 + (lane & 15) * 128 + (((s * 4 + (lane >> 4)) ^ ((lane >> 1) & 7)) << 4));
+    }
+}
+// Where a piece of such a stage lies: 16-byte piece `piece` of row `row` (of the operand ALONG, of the reduction ACROSS).
+template <int W, bool ACROSS>
+__device__ __forceinline__ int swizzled(int row, int piece)
+{
+    return ACROSS ? piece ^ across_swizzle<W>(row) : piece ^ ((row >> 1) & 7);
+}
+
 // One operand of a tile.  W: its width (BT or BN), L: pieces a thread and stage.
 template <typename T, int W, int L, bool ACROSS, bool DIRECT>
 struct Operand {
@@ -92,31 +194,18 @@ struct Operand {
     int64_t ld, plane, K;
     int here;              // rows (ALONG) or columns (ACROSS) of the tile that exist
     const uint16_t* from;  // the next step
-    int64_t left;          // DIRECT: bytes from there to the operand's end, in whole pieces; otherwise steps of the reduction
-    uint32_t off[DIRECT ? L : 1];
-    u32x4 held[DIRECT ? 1 : L];
+    int64_t left;          // bytes from there to the operand's end, in whole pieces
+    uint32_t off[L];
 
-    static __device__ __forceinline__ void place(int i, int& row, int& piece)
-    {
-        const int p = i * T::NT + (int)threadIdx.x;
-        if constexpr (ACROSS) {
-            row = p / (W / 8), piece = (p % (W / 8)) ^ across_swizzle<W>(row);
-        } else {
-            row = p / 8, piece = (p % 8) ^ ((row >> 1) & 7);
-        }
-    }
     __device__ __forceinline__ void begin(const uint16_t* p, int64_t stride, int64_t plane_, int64_t K_, int64_t first, int64_t all)
     {
         ld = stride, plane = plane_, K = K_;
         here = (int)min((int64_t)W, all - first);
         base = p + (ACROSS ? first : first * stride);
-        if constexpr (DIRECT) {
 #pragma unroll
-            for (int i = 0; i < L; ++i) {
-                int row, piece;
-                place(i, row, piece);
-                off[i] = (uint32_t)row * (uint32_t)(stride * 2) + piece * 16;
-            }
+        for (int i = 0; i < L; ++i) {
+            const int p = i * T::NT + (int)threadIdx.x, row = ACROSS ? p / (W / 8) : p / 8, piece = ACROSS ? p % (W / 8) : p % 8;
+            off[i] = (uint32_t)row * (uint32_t)(stride * 2) + swizzled<W, ACROSS>(row, piece) * 16;
         }
     }
     // the next step is step k of plane q
@@ -125,72 +214,57 @@ struct Operand {
         const int64_t k0 = (int64_t)k * T::KE;
         from = base + q * plane + (ACROSS ? k0 * ld : k0);
         // (the rows start on 16 bytes, so what the last piece holds past the end lies in the same 16 bytes as an element)
-        if constexpr (DIRECT) left = ((ACROSS ? (K - 1 - k0) * ld + here : (here - 1) * ld + (K - k0)) * 2 + 15) & ~(int64_t)15;
-        else left = K - k0;
+        left = ((ACROSS ? (K - 1 - k0) * ld + here : (here - 1) * ld + (K - k0)) * 2 + 15) & ~(int64_t)15;
     }
     __device__ __forceinline__ void advance()
     {
         const int64_t by = ACROSS ? T::KE * ld : T::KE;
         from += by;
-        left -= DIRECT ? by * 2 : T::KE;
+        left -= by * 2;
     }
-    // the next step to the stage at `lds` (DIRECT; no step: nothing but zeros), or to registers
+    // the next step to the stage at `lds` (no step: nothing but zeros)
     __device__ __forceinline__ void load(char* lds, bool step)
     {
-        if constexpr (DIRECT) {
-            const uint64_t at = (uint64_t)(uintptr_t)from;
-            const uint32_t bytes = !step || left <= 0 ? 0u : (uint32_t)min(left, (int64_t)0x7FFFFFF0);
-            const u32x4 r = {(uint32_t)at, (uint32_t)(at >> 32), bytes, 0x00020000u};
-            const uint32_t to = (uint32_t)(uintptr_t)(lds_void_t*)lds + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * 1024;
+        const uint64_t at = (uint64_t)(uintptr_t)from;
+        const uint32_t bytes = !step || left <= 0 ? 0u : (uint32_t)min(left, (int64_t)0x7FFFFFF0);
+        const u32x4 r = {(uint32_t)at, (uint32_t)(at >> 32), bytes, 0x00020000u};
+        const uint32_t to = (uint32_t)(uintptr_t)(lds_void_t*)lds + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * 1024;
 #pragma unroll
-            for (int i = 0; i < L; ++i) load_to_lds(r, to + i * T::NT * 16, off[i]);
-        } else {
-#pragma unroll
-            for (int i = 0; i < L; ++i) {
-                int row, piece;
-                place(i, row, piece);
-                const uint16_t* p = from + (int64_t)row * ld + piece * 8;
-                const int64_t n = !step ? 0 : ACROSS ? (row < left ? here - piece * 8 : 0) : (row < here ? left - piece * 8 : 0);
-                u32x4 v = {0, 0, 0, 0};
-                if (n >= 8) {
-                    __builtin_memcpy(&v, p, 16);
-                } else if (n > 0) {
-                    uint16_t e[8];
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) e[j] = j < n ? p[j] : (uint16_t)0;
-                    __builtin_memcpy(&v, e, 16);
-                }
-                held[i] = v;
-            }
-        }
+        for (int i = 0; i < L; ++i) load_to_lds(r, to + i * T::NT * 16, off[i]);
     }
-    __device__ __forceinline__ void commit(char* lds) const
+    static __device__ __forceinline__ u32x4 fragment(const char* lds, int block, int s) { return fragment_of<W, ACROSS>(lds, block, s); }
+};
+
+// ... that may start anywhere, through registers, of one plane
+template <typename T, int W, int L, bool ACROSS>
+struct Operand<T, W, L, ACROSS, false> {
+    typedef AnyPieces<uint16_t, T::NT, W, T::KE, L, ACROSS> Pieces;
+    Pieces pieces;
+    const uint16_t* start;
+    int64_t ld, K, first, all;
+    int here;
+    uint16_t held[L][8];
+
+    __device__ __forceinline__ void begin(const uint16_t* p, int64_t stride, int64_t, int64_t K_, int64_t first_, int64_t all_)
     {
-        if constexpr (!DIRECT) {
-#pragma unroll
-            for (int i = 0; i < L; ++i) *(u32x4*)(lds + (i * T::NT + (int)threadIdx.x) * 16) = held[i];
-        }
+        start = p, ld = stride, K = K_, first = first_, all = all_;
+        here = (int)min((int64_t)W, all - first);
     }
-    // the matrix operand of block `block` (16 wide) for half s of a stage
-    static __device__ __forceinline__ u32x4 fragment(const char* lds, int block, int s)
+    __device__ __forceinline__ void seek(int k, int) { pieces.begin(start, ld, K, first, all, (int64_t)k * T::KE); }
+    __device__ __forceinline__ void load() { pieces.load(held); }
+    __device__ __forceinline__ void commit(char* lds)
     {
-        const int lane = threadIdx.x & 63;
-        if constexpr (ACROSS) {
-            typedef short s16x4 __attribute__((ext_vector_type(4)));
-            typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-            const int k = (lane >> 4) * 8 + ((lane & 15) >> 2);
-            const char* p = lds + (s * 32 + k) * (W * 2) + ((block * 2) ^ across_swizzle<W>(k)) * 16 + (lane & 3) * 8;
-            union {
-                s16x4 h[2];
-                u32x4 v;
-            } u;
-            u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)p);
-            u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 4 * W * 2));
-            return u.v;
-        } else {
-            return *(const u32x4*)(lds + block * 16 * T::KB + (lane & 15) * T::KB + (((s * 4 + (lane >> 4)) ^ ((lane >> 1) & 7)) << 4));
+        pieces.clear(held);
+#pragma unroll
+        for (int i = 0; i < L; ++i) {
+            int row, piece;
+            Pieces::place(i, row, piece);
+            uint4 v;
+            __builtin_memcpy(&v, held[i], 16);
+            *(uint4*)(lds + (row * (ACROSS ? W / 8 : 8) + swizzled<W, ACROSS>(row, piece)) * 16) = v;
         }
     }
+    static __device__ __forceinline__ u32x4 fragment(const char* lds, int block, int s) { return fragment_of<W, ACROSS>(lds, block, s); }
 };
 
 struct ProductArgs {
@@ -265,24 +339,6 @@ __global__ __launch_bounds__(T::NT) void product_kernel(ProductArgs g, typename 
     Epi::prepare(e, bias, n0, b.here, T::BN, T::NT);
 
     const int steps = (ks1 - ks0) * g.segments;
-    int ks = ks0, seg = 0;  // the next step to load
-    a.seek(ks, g.seg_a & 3), b.seek(ks, g.seg_b & 3);
-    auto load = [&](int buf) {
-        char* const to = smem + buf * T::STAGE;
-        const bool step = ks < ks1;
-        a.load(to, step);
-        b.load(to + T::BT * T::KB, step);
-    };
-    auto move = [&]() {  // (apart from load(): its branch would end the stretch of code in which loads and products are interleaved)
-        ++ks;
-        if (ks == ks1 && seg + 1 < g.segments) {
-            ks = ks0, ++seg;
-            a.seek(ks, (g.seg_a >> (2 * seg)) & 3), b.seek(ks, (g.seg_b >> (2 * seg)) & 3);
-        } else {
-            a.advance(), b.advance();
-        }
-    };
-
     f32x4 acc[T::FN][T::FT];
 #pragma unroll
     for (int i = 0; i < T::FN; ++i)
@@ -313,6 +369,24 @@ __global__ __launch_bounds__(T::NT) void product_kernel(ProductArgs g, typename 
     typedef std::integral_constant<int, PHASES - 1> Last;
 
     if constexpr (DIRECT) {
+        int ks = ks0, seg = 0;  // the next step to load
+        a.seek(ks, g.seg_a & 3), b.seek(ks, g.seg_b & 3);
+        auto load = [&](int buf) {
+            char* const to = smem + buf * T::STAGE;
+            const bool step = ks < ks1;
+            a.load(to, step);
+            b.load(to + T::BT * T::KB, step);
+        };
+        auto move = [&]() {  // (apart from load(): its branch would end the stretch of code in which loads and products are interleaved)
+            ++ks;
+            if (ks == ks1 && seg + 1 < g.segments) {
+                ks = ks0, ++seg;
+                a.seek(ks, (g.seg_a >> (2 * seg)) & 3), b.seek(ks, (g.seg_b >> (2 * seg)) & 3);
+            } else {
+                a.advance(), b.advance();
+            }
+        };
+
         // Order of a phase of many products: after every few one of its LDS reads, then one of its loads, so that products begin at
         // once.  With few products the reads come first, or they would be late.
         constexpr bool MIXED = T::HB * T::FN >= 16;
@@ -386,9 +460,10 @@ __global__ __launch_bounds__(T::NT) void product_kernel(ProductArgs g, typename 
             a.commit(smem + buf * T::STAGE);
             b.commit(smem + buf * T::STAGE + T::BT * T::KB);
         };
-        load(0), move();
+        a.seek(ks0, 0), b.seek(ks0, 0);
+        a.load(), b.load();
         commit(0);
-        load(1), move();
+        a.load(), b.load();
         __syncthreads();
         for (int k = 0; k < steps; ++k) {
             fetch(k & 1, First());
@@ -399,7 +474,7 @@ __global__ __launch_bounds__(T::NT) void product_kernel(ProductArgs g, typename 
             });
             if (k + 1 < steps) {
                 commit((k + 1) & 1);
-                load(k & 1), move();
+                a.load(), b.load();
             }
             __syncthreads();
         }
