@@ -132,17 +132,6 @@ hipError_t launch_product_form(const ProductArgs& g, const typename Epi::Args& e
     }
 }
 
-// Planes always start on 16 bytes: no forms for other operands.
-template <int DT, bool A_ACROSS, bool B_ACROSS, typename Epi>
-hipError_t launch_product_direct(const ProductArgs& g, const typename Epi::Args& e, ProductForm form, int batch, int splits, hipStream_t s)
-{
-    switch (form) {
-        case P64: return launch_product_tiles<DT, Tile64, A_ACROSS, B_ACROSS, true, Epi>(g, e, batch, splits, s);
-        case P128: return launch_product_tiles<DT, Tile128, A_ACROSS, B_ACROSS, true, Epi>(g, e, batch, splits, s);
-        default: return launch_product_tiles<DT, Tile256, A_ACROSS, B_ACROSS, true, Epi>(g, e, batch, splits, s);
-    }
-}
-
 #define CONVFWD_PRODUCT_LAYOUTS(launch, DT, Epi)                                                   \
     switch (layout) {                                                                              \
         case LAYOUT_NT: return launch<DT, false, false, Epi>(g, arg, form, 1, splits, s);          \

@@ -364,7 +364,7 @@ hipError_t multiply(int dtype, ProductLayout layout, const Factor& a, const Fact
 {
     ProductArgs g = {};
     g.a = (const uint16_t*)a.p, g.b = (const uint16_t*)b.p, g.lda = a.ld, g.ldb = b.ld, g.M = M, g.N = N, g.K = K, g.partial = partial;
-    g.ksteps = (int)((K + 63) / 64), g.segments = 1;
+    g.ksteps = (int)((K + 63) / 64);
     const auto launch = dtype == CONV_F32 ? launch_product_f32 : dtype == CONV_F16 ? launch_product_f16 : launch_product_bf16;
     const hipError_t err = launch(g, e, layout, plan.form, plan.splits, s);
     if (err != hipSuccess || plan.splits == 1) return err;

@@ -5,10 +5,11 @@
 // A and B have the side of the shorter dimension n and are symmetric: only the tiles on and above the diagonal are multiplied, each written to both its
 // places, so a step takes n n (3 m + n) operations for the longer dimension m.  All products are those of product_kernel.h, on fp16 operands scaled by
 // 2^12 (X, A and B are small whole numbers at most and their elements of the size 1 / sqrt(n): scaled they keep all their bits).
-//   * X itself is kept in fp32 beside its fp16 form: weak directions grow by a in every step, and so would the roundings of an X kept in 16
-//     bits (a matrix of rank n / 8 in bf16: 3 % off, with X in fp32 0.08 %).  The errors of A, B and the X that B multiplies do not grow like that.
+//   * X itself is kept in more bits than it is multiplied in: weak directions grow by a in every step, and so would the roundings of an X kept in 16
+//     bits (a matrix of rank n / 8 in bf16: 3 % off, against 0.08 %).  The errors of A, B and the X that B multiplies do not grow like that.
 //   * bf16: the products take one fp16 plane of each operand, which has three bits more than the result (off by 1.2e-3 before the result's own
 //     rounding of 1.7e-3, 4096 x 4096).  fp16 and fp32: two planes, high and low, and three of their four products, 22 bits.
+//   * X beside its products: fp32 for fp32; for 16-bit types the high and the low plane together, 22 bits, which is less to read and write.
 #include <algorithm>
 #include <cmath>
 
@@ -75,7 +76,7 @@ __device__ __forceinline__ void get_scaled(const Planes& from, int planes, int64
 struct GramEpi {
     struct Args {
         Planes a;
-        int planes, shift;  // shift: log2 of the tiles' side
+        int planes, side;  // side of the tiles
     };
     static constexpr bool SYMMETRIC = true;
     static __device__ __forceinline__ void prepare(const Args&, float*, int64_t, int, int, int) {}
@@ -84,7 +85,7 @@ struct GramEpi {
 #pragma unroll
         for (int k = 0; k < 8; ++k) v[k] *= kUnplane;
         put_scaled(e.a, e.planes, m, n, v, have);
-        if (m >> e.shift != n >> e.shift) put_mirrored(e.a, e.planes, m, n, v, have);
+        if ((uint32_t)m / (uint32_t)e.side != (uint32_t)n / (uint32_t)e.side) put_mirrored(e.a, e.planes, m, n, v, have);
     }
 };
 
@@ -92,7 +93,7 @@ struct SquareEpi {
     struct Args {
         Planes a, b;
         float coef_b, coef_c;
-        int planes, shift;  // shift: log2 of the tiles' side
+        int planes, side;  // side of the tiles
     };
     static constexpr bool SYMMETRIC = true;
     static __device__ __forceinline__ void prepare(const Args&, float*, int64_t, int, int, int) {}
@@ -103,17 +104,16 @@ struct SquareEpi {
 #pragma unroll
         for (int k = 0; k < 8; ++k) v[k] = __builtin_fmaf(e.coef_b, a[k], e.coef_c * kUnplane * v[k]);
         put_scaled(e.b, e.planes, m, n, v, have);
-        if (m >> e.shift != n >> e.shift) put_mirrored(e.b, e.planes, m, n, v, have);
+        if ((uint32_t)m / (uint32_t)e.side != (uint32_t)n / (uint32_t)e.side) put_mirrored(e.b, e.planes, m, n, v, have);
     }
 };
 
 struct UpdateEpi {
     struct Args {
-        float* x;        // in fp32, [rows][ld of the planes]
+        float* x;        // in fp32, [rows][ld of the planes]; null: the planes hold it
         int64_t batch_x;
-        Planes to;
+        Planes from, to;
         float coef_a;
-        int planes;
         void* out;       // the last step's result, instead of the planes
         int64_t ldo, batch_o;
         int dtype;
@@ -123,15 +123,16 @@ struct UpdateEpi {
     static __device__ __forceinline__ void finish(const ProductArgs&, const Args& e, float (&v)[8], int64_t m, int64_t n, int have, const float*)
     {
         float* const x = e.x + blockIdx.y * e.batch_x;
-        float old[8];
-        get8<CONV_F32>(x, m * e.to.ld + n, old, have);
+        float old[8], scale = e.coef_a;
+        if (e.x) get8<CONV_F32>(x, m * e.to.ld + n, old, have);
+        else get_scaled(e.from, 2, m, n, old, have), scale *= kUnplane;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] = __builtin_fmaf(e.coef_a, old[k], kUnplane * kUnplane * v[k]);
+        for (int k = 0; k < 8; ++k) v[k] = __builtin_fmaf(scale, old[k], kUnplane * kUnplane * v[k]);
         if (!e.out) {
-            put8<CONV_F32>(x, m * e.to.ld + n, v, have);
+            if (e.x) put8<CONV_F32>(x, m * e.to.ld + n, v, have);
 #pragma unroll
             for (int k = 0; k < 8; ++k) v[k] *= kPlane;
-            put_scaled(e.to, e.planes, m, n, v, have);
+            put_scaled(e.to, 2, m, n, v, have);
         } else {
             const int64_t at = blockIdx.y * e.batch_o + m * e.ldo + n;
             if (e.dtype == CONV_F32) put8<CONV_F32>(e.out, at, v, have);
@@ -144,13 +145,12 @@ struct UpdateEpi {
 struct StartArgs {
     const void* x;
     int64_t ldx, stride_x;
-    int64_t rows, cols, side;      // side: of A and B
+    int64_t rows, cols;
     double* sums;                  // [batch][parts]
     int parts;
     float* x32;
     int64_t batch_x;
-    Planes x0, x1, a, b;
-    int planes;
+    Planes to;
     double eps;
 };
 
@@ -179,7 +179,7 @@ __global__ __launch_bounds__(256) void orthogonal_norm(StartArgs g)
     if (threadIdx.x == 0) g.sums[blockIdx.y * g.parts + blockIdx.x] = red[0];
 }
 
-// X in fp32 and in planes, and the zeros behind the rows of all planes, which products over two planes read.
+// X in planes, and in fp32 where it is kept so.
 template <int DT>
 __global__ __launch_bounds__(256) void orthogonal_start(StartArgs g)
 {
@@ -196,36 +196,25 @@ __global__ __launch_bounds__(256) void orthogonal_start(StartArgs g)
     const double inv = 1.0 / (sqrt(red[0]) + g.eps);
     const elem_t* x = (const elem_t*)g.x + blockIdx.y * g.stride_x;
     float* x32 = g.x32 + blockIdx.y * g.batch_x;
-    const int64_t ld = g.x0.ld, each = ld / 8, all = g.rows * each, step = (int64_t)gridDim.x * 256, first = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t ld = g.to.ld, each = ld / 8, all = g.rows * each, step = (int64_t)gridDim.x * 256, first = (int64_t)blockIdx.x * 256 + threadIdx.x;
     for (int64_t i = first; i < all; i += step) {
         const int64_t t = all <= UINT32_MAX ? (uint32_t)i / (uint32_t)each : i / each, j = (i - t * each) * 8;
-        float v[8];
-        get8<DT>(x, t * g.ldx + j, v, (int)min(g.cols - j, (int64_t)8));
         const int have = (int)min(g.cols - j, (int64_t)8);
+        float v[8];
+        get8<DT>(x, t * g.ldx + j, v, have);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] = k < have ? (float)(v[k] * inv) : 0.0f;
-        put8<CONV_F32>(x32, t * ld + j, v, 8);
+        for (int k = 0; k < 8; ++k) v[k] = (float)(v[k] * inv);
+        if (g.x32) put8<CONV_F32>(x32, t * ld + j, v, have);
 #pragma unroll
         for (int k = 0; k < 8; ++k) v[k] *= kPlane;
-        put_scaled(g.x0, g.planes, t, j, v, 8);
-        if (j + 8 > g.cols) {
-            const float none[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
-            put_scaled(g.x1, g.planes, t, j, none, 8);
-        }
-    }
-    const int64_t pad = g.a.ld - g.side / 8 * 8, pads = g.side * (pad / 8);
-    for (int64_t i = first; i < pads; i += step) {
-        const float none[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
-        const int64_t t = i / (pad / 8), j = g.a.ld - pad + i % (pad / 8) * 8;
-        put_scaled(g.a, g.planes, t, j, none, 8);
-        put_scaled(g.b, g.planes, t, j, none, 8);
+        put_scaled(g.to, 2, t, j, v, have);
     }
 }
 
 int64_t round_up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 
 int planes_of(int dtype) { return dtype == CONV_BF16 ? 1 : 2; }
-int parts_of(int64_t rows, int64_t cols) { return (int)std::max<int64_t>(1, std::min<int64_t>(256, rows * cols / 8192)); }
+int parts_of(int64_t rows, int64_t cols) { return (int)std::max<int64_t>(1, std::min<int64_t>(1024, rows * cols / 8192)); }
 
 struct Space {
     Planes x[2], a, b;
@@ -243,59 +232,78 @@ Space space_of(const OrthogonalArgs& g, int dtype, void* ws)
         s.bytes += (n + 255) & ~(size_t)255;
         return (void*)p;
     };
-    const int planes = planes_of(dtype);
-    auto matrix = [&](int64_t rows, int64_t cols) {
+    auto matrix = [&](int64_t rows, int64_t cols, int planes) {
         Planes p = {};
-        p.ld = round_up(cols, 64), p.plane = rows * p.ld, p.batch = p.plane * planes;
+        p.ld = round_up(cols, 8), p.plane = rows * p.ld, p.batch = p.plane * planes;
         p.p = (uint16_t*)take((size_t)g.batch * p.batch * 2);
         return p;
     };
     const int64_t side = std::min(g.rows, g.cols);
-    s.x[0] = matrix(g.rows, g.cols), s.x[1] = matrix(g.rows, g.cols);
-    s.a = matrix(side, side), s.b = matrix(side, side);
+    s.x[0] = matrix(g.rows, g.cols, 2), s.x[1] = matrix(g.rows, g.cols, 2);
+    s.a = matrix(side, side, planes_of(dtype)), s.b = matrix(side, side, planes_of(dtype));
     s.batch_x = g.rows * s.x[0].ld;
-    s.x32 = (float*)take((size_t)g.batch * s.batch_x * 4);
+    if (dtype == CONV_F32) s.x32 = (float*)take((size_t)g.batch * s.batch_x * 4);
     s.sums = (double*)take((size_t)g.batch * parts_of(g.rows, g.cols) * 8);
     return s;
 }
 
-// The tile with the least expected time, in us (see the linear layers' plan).
-ProductForm tile_of(int64_t M, int64_t N, int64_t K, int segments, int64_t batch, bool symmetric)
-{
-    struct Cost {
-        int side;
-        double once, own, step;
-    };
-    constexpr Cost costs[] = {{64, 2.0, 1.2, 0.2}, {128, 1.8, 1.5, 0.52}, {256, 0, 11, 1.4}};
-    ProductForm best = P64;
-    double least = 1e30;
-    for (int f = 0; f < 3; ++f) {
-        const Cost& c = costs[f];
-        const double tm = (double)((M + c.side - 1) / c.side), tn = (double)((N + c.side - 1) / c.side);
-        const double tiles = (symmetric ? tm * (tm + 1) / 2 : tm * tn) * batch, steps = (double)((K + 63) / 64) * segments;
-        const double us = c.once + std::ceil(tiles / 256) * (c.own + steps * c.step);
-        if (us < least) least = us, best = (ProductForm)f;
-    }
-    return best;
-}
-int shift_of(ProductForm f) { return f == P64 ? 6 : f == P128 ? 7 : 8; }
-int64_t tiles_of(ProductForm f, int64_t M, int64_t N) { return ((M - 1) >> shift_of(f)) * ((N - 1) >> shift_of(f)) + ((M - 1) >> shift_of(f)) + ((N - 1) >> shift_of(f)) + 1; }
+// Tiles of one plane, and of two, whose stages are twice as large.
+typedef ProductTile<4, 2, 3, 6, 3> Tile192;
+typedef ProductTile<4, 2, 1, 2, 3, 2> Tile64Two;
+typedef ProductTile<2, 4, 4, 2, 2, 2> Tile128Two;
+struct TileCost {
+    int side, planes;
+    double once, own, step;
+};
+constexpr TileCost kTiles[] = {{64, 1, 4.1, 1.0, 0.275}, {128, 1, 3.1, 1.7, 0.53}, {256, 1, 0, 6.4, 1.18}, {192, 1, 0, 5.0, 0.8}, {64, 2, 4.1, 1.0, 0.5}, {128, 2, 3.1, 3.0, 1.3}};
+enum TileId { T64, T128, T256, T192, T64_TWO, T128_TWO };
 
-ProductArgs product_of(const Planes& a, const Planes& b, int64_t M, int64_t N, int64_t K, int planes)
+// The tile with the least expected time, in us (see the linear layers' plan).
+TileId tile_of(int64_t M, int64_t N, int64_t K, int planes, int64_t batch, bool symmetric)
+{
+    int best = 0;
+    double least = 1e30;
+    for (int f = 0; f < (int)(sizeof(kTiles) / sizeof(kTiles[0])); ++f) {
+        const TileCost& c = kTiles[f];
+        if (c.planes != planes) continue;
+        const double tm = (double)((M + c.side - 1) / c.side), tn = (double)((N + c.side - 1) / c.side);
+        const double tiles = (symmetric ? tm * (tm + 1) / 2 : tm * tn) * batch, steps = (double)((K + 63) / 64);
+        const double us = c.once + std::ceil(tiles / 256) * (c.own + steps * c.step);
+        if (us < least) least = us, best = f;
+    }
+    return (TileId)best;
+}
+int64_t tiles_of(TileId f, int64_t M, int64_t N)
+{
+    const int side = kTiles[f].side;
+    return ((M + side - 1) / side) * ((N + side - 1) / side);
+}
+
+template <bool A_ACROSS, bool B_ACROSS, typename Epi>
+hipError_t multiply(const ProductArgs& g, const typename Epi::Args& e, TileId tile, int batch, hipStream_t s)
+{
+    switch (tile) {
+        case T64: return launch_product_tiles<CONV_F16, Tile64, A_ACROSS, B_ACROSS, true, Epi>(g, e, batch, 1, s);
+        case T128: return launch_product_tiles<CONV_F16, Tile128, A_ACROSS, B_ACROSS, true, Epi>(g, e, batch, 1, s);
+        case T192: return launch_product_tiles<CONV_F16, Tile192, A_ACROSS, B_ACROSS, true, Epi>(g, e, batch, 1, s);
+        case T256: return launch_product_tiles<CONV_F16, Tile256, A_ACROSS, B_ACROSS, true, Epi>(g, e, batch, 1, s);
+        case T64_TWO: return launch_product_tiles<CONV_F16, Tile64Two, A_ACROSS, B_ACROSS, true, Epi>(g, e, batch, 1, s);
+        default: return launch_product_tiles<CONV_F16, Tile128Two, A_ACROSS, B_ACROSS, true, Epi>(g, e, batch, 1, s);
+    }
+}
+
+ProductArgs product_of(const Planes& a, const Planes& b, int64_t M, int64_t N, int64_t K)
 {
     ProductArgs p = {};
     p.a = a.p, p.b = b.p, p.lda = a.ld, p.ldb = b.ld, p.plane_a = a.plane, p.plane_b = b.plane, p.batch_a = a.batch, p.batch_b = b.batch;
     p.M = M, p.N = N, p.K = K, p.ksteps = (int)((K + 63) / 64);
-    // low x high, high x low, high x high
-    p.segments = planes == 1 ? 1 : 3;
-    p.seg_a = planes == 1 ? 0 : 1, p.seg_b = planes == 1 ? 0 : 1 << 2;
     return p;
 }
 
 template <int DT>
 hipError_t start(const StartArgs& g, int64_t batch, hipStream_t s)
 {
-    const int64_t blocks = std::max<int64_t>(1, std::min<int64_t>(2048, g.rows * g.x0.ld / 2048));
+    const int64_t blocks = std::max<int64_t>(1, std::min<int64_t>(2048, g.rows * g.to.ld / 2048));
     hipLaunchKernelGGL((orthogonal_norm<DT>), dim3((unsigned)g.parts, (unsigned)batch), dim3(256), 0, s, g);
     hipLaunchKernelGGL((orthogonal_start<DT>), dim3((unsigned)blocks, (unsigned)batch), dim3(256), 0, s, g);
     return hipGetLastError();
@@ -308,10 +316,10 @@ size_t orthogonal_workspace(const OrthogonalArgs& g, int dtype) { return g.batch
 hipError_t launch_orthogonalize(const OrthogonalArgs& all, int dtype, hipStream_t s)
 {
     // gridDim.y is at most 65535, and a launch holds less than 2^32 threads: the batch goes in portions, tiles chosen for the largest
-    const int planes = planes_of(dtype), segments = planes == 1 ? 1 : 3, es = dtype_size(dtype);
+    const int planes = planes_of(dtype), es = dtype_size(dtype);
     const int64_t side = std::min(all.rows, all.cols), longer = std::max(all.rows, all.cols), most = std::min<int64_t>(all.batch, 32768);
-    const ProductForm gram = tile_of(side, side, longer, segments, most, true), square = tile_of(side, side, side, segments, most, true);
-    const ProductForm update = tile_of(all.rows, all.cols, side, segments, most, false);
+    const TileId gram = tile_of(side, side, longer, planes, most, true), square = tile_of(side, side, side, planes, most, true);
+    const TileId update = tile_of(all.rows, all.cols, side, planes, most, false);
     const int64_t tiles = std::max({tiles_of(gram, side, side), tiles_of(square, side, side), tiles_of(update, all.rows, all.cols)});
     const int64_t portion = std::max<int64_t>(1, std::min(most, ((int64_t)1 << 21) / tiles));
     for (int64_t skip = 0; skip < all.batch; skip += portion) {
@@ -321,24 +329,23 @@ hipError_t launch_orthogonalize(const OrthogonalArgs& all, int dtype, hipStream_
         const Space w = space_of(g, dtype, all.ws);
         const bool tall = g.rows > g.cols;
         StartArgs st = {};
-        st.x = g.x, st.ldx = g.ldx, st.stride_x = g.stride_x, st.rows = g.rows, st.cols = g.cols, st.side = side, st.sums = w.sums;
-        st.parts = parts_of(g.rows, g.cols), st.x32 = w.x32, st.batch_x = w.batch_x, st.x0 = w.x[0], st.x1 = w.x[1], st.a = w.a, st.b = w.b;
-        st.planes = planes, st.eps = g.eps;
+        st.x = g.x, st.ldx = g.ldx, st.stride_x = g.stride_x, st.rows = g.rows, st.cols = g.cols, st.sums = w.sums;
+        st.parts = parts_of(g.rows, g.cols), st.x32 = w.x32, st.batch_x = w.batch_x, st.to = w.x[0], st.eps = g.eps;
         hipError_t e = dtype == CONV_F32 ? start<CONV_F32>(st, g.batch, s) : dtype == CONV_F16 ? start<CONV_F16>(st, g.batch, s) : start<CONV_BF16>(st, g.batch, s);
         if (e != hipSuccess) return e;
         const int batch = (int)g.batch;
         for (int step = 0; step < g.steps; ++step) {
             const Planes &x = w.x[step & 1], &to = w.x[(step + 1) & 1];
-            const GramEpi::Args ge = {w.a, planes, shift_of(gram)};
-            const ProductArgs gp = product_of(x, x, side, side, longer, planes);
-            e = tall ? launch_product_direct<CONV_F16, true, true, GramEpi>(gp, ge, gram, batch, 1, s) : launch_product_direct<CONV_F16, false, false, GramEpi>(gp, ge, gram, batch, 1, s);
+            const GramEpi::Args ge = {w.a, planes, kTiles[gram].side};
+            const ProductArgs gp = product_of(x, x, side, side, longer);
+            e = tall ? multiply<true, true, GramEpi>(gp, ge, gram, batch, s) : multiply<false, false, GramEpi>(gp, ge, gram, batch, s);
             if (e != hipSuccess) return e;
-            const SquareEpi::Args se = {w.a, w.b, g.b, g.c, planes, shift_of(square)};
-            e = launch_product_direct<CONV_F16, false, false, SquareEpi>(product_of(w.a, w.a, side, side, side, planes), se, square, batch, 1, s);
+            const SquareEpi::Args se = {w.a, w.b, g.b, g.c, planes, kTiles[square].side};
+            e = multiply<false, false, SquareEpi>(product_of(w.a, w.a, side, side, side), se, square, batch, s);
             if (e != hipSuccess) return e;
-            const UpdateEpi::Args ue = {w.x32, w.batch_x, to, g.a, planes, step + 1 == g.steps ? g.out : nullptr, g.ldo, g.stride_o, dtype};
-            e = tall ? launch_product_direct<CONV_F16, false, false, UpdateEpi>(product_of(x, w.b, g.rows, g.cols, side, planes), ue, update, batch, 1, s)
-                     : launch_product_direct<CONV_F16, false, true, UpdateEpi>(product_of(w.b, x, g.rows, g.cols, side, planes), ue, update, batch, 1, s);
+            const UpdateEpi::Args ue = {w.x32, w.batch_x, x, to, g.a, step + 1 == g.steps ? g.out : nullptr, g.ldo, g.stride_o, dtype};
+            e = tall ? multiply<false, false, UpdateEpi>(product_of(x, w.b, g.rows, g.cols, side), ue, update, batch, s)
+                     : multiply<false, true, UpdateEpi>(product_of(w.b, x, g.rows, g.cols, side), ue, update, batch, s);
             if (e != hipSuccess) return e;
         }
     }

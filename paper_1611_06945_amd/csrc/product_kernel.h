@@ -14,7 +14,7 @@
 //     the bounds check of the buffer descriptor, which moves along with the reduction, so that offsets stay below 2^31 however long it is.  A row's
 //     bytes past K belong to what follows and are cleared in both operands on the last step.  Otherwise pieces go
 //     through registers, from any address, and their ends are cleared on the way.
-//   * An operand may be a sum of planes; a product over them is a reduction of `segments` times the length, the smallest terms first.
+//   * Operands may be sums of two planes, high and low (PL = 2), of which a step multiplies low x high, high x low and high x high.
 #pragma once
 
 #include <algorithm>
@@ -36,12 +36,13 @@ __device__ __forceinline__ void count_to(F f)
     }
 }
 
-template <int WT_, int WN_, int FT_, int FN_, int S_>
+template <int WT_, int WN_, int FT_, int FN_, int S_, int PL_ = 1>
 struct ProductTile {
+    static constexpr int PL = PL_;  // planes
     static constexpr int WT = WT_, WN = WN_, FT = FT_, FN = FN_, S = S_;  // waves and 16-wide blocks a wave, along m and n; stages
     static constexpr int BT = 16 * WT * FT, BN = 16 * WN * FN, NT = 64 * WT * WN;
     static constexpr int KB = 128, KE = KB / 2;  // of a step, bytes and elements
-    static constexpr int STAGE = (BT + BN) * KB;
+    static constexpr int PLANE_A = BT * KB, PLANE_B = BN * KB, STAGE = PL * (PLANE_A + PLANE_B);
     static constexpr size_t LDS = (size_t)S * STAGE + BN * 4;
     static constexpr int LA = BT * 8 / NT, LW = BN * 8 / NT;  // 16-byte loads a thread and stage
     static constexpr int H = FT > 4 ? 2 : 1, HB = FT / H;     // the blocks of m go in H portions
@@ -53,7 +54,7 @@ struct ProductTile {
 template <int W>
 __device__ __forceinline__ int across_swizzle(int k)
 {
-    return W >= 128 ? ((k & 3) | ((k >> 3) & 1) << 2) * 2 : (((k >> 1) & 1) | ((k >> 3) & 1) << 1) * 2;
+    return W % 128 == 0 ? ((k & 3) | ((k >> 3) & 1) << 2) * 2 : (((k >> 1) & 1) | ((k >> 3) & 1) << 1) * 2;
 }
 
 // The first `n` elements of 8 (n may be <= 0 or >= 8), the others zero.
@@ -190,31 +191,24 @@ __device__ __forceinline__ int swizzled(int row, int piece)
 // One operand of a tile.  W: its width (BT or BN), L: pieces a thread and stage.
 template <typename T, int W, int L, bool ACROSS, bool DIRECT>
 struct Operand {
-    const uint16_t* base;  // the tile's first element, k = 0, first plane
-    int64_t ld, plane, K;
+    int64_t ld, plane;
     int here;              // rows (ALONG) or columns (ACROSS) of the tile that exist
-    const uint16_t* from;  // the next step
+    const uint16_t* from;  // the next step, first plane
     int64_t left;          // bytes from there to the operand's end, in whole pieces
     uint32_t off[L];
 
-    __device__ __forceinline__ void begin(const uint16_t* p, int64_t stride, int64_t plane_, int64_t K_, int64_t first, int64_t all)
+    __device__ __forceinline__ void begin(const uint16_t* p, int64_t stride, int64_t plane_, int64_t K, int64_t first, int64_t all, int64_t k0)
     {
-        ld = stride, plane = plane_, K = K_;
+        ld = stride, plane = plane_;
         here = (int)min((int64_t)W, all - first);
-        base = p + (ACROSS ? first : first * stride);
+        from = p + (ACROSS ? first + k0 * ld : first * ld + k0);
+        // (the rows start on 16 bytes, so what the last piece holds past the end lies in the same 16 bytes as an element)
+        left = ((ACROSS ? (K - 1 - k0) * ld + here : (here - 1) * ld + (K - k0)) * 2 + 15) & ~(int64_t)15;
 #pragma unroll
         for (int i = 0; i < L; ++i) {
             const int p = i * T::NT + (int)threadIdx.x, row = ACROSS ? p / (W / 8) : p / 8, piece = ACROSS ? p % (W / 8) : p % 8;
             off[i] = (uint32_t)row * (uint32_t)(stride * 2) + swizzled<W, ACROSS>(row, piece) * 16;
         }
-    }
-    // the next step is step k of plane q
-    __device__ __forceinline__ void seek(int k, int q)
-    {
-        const int64_t k0 = (int64_t)k * T::KE;
-        from = base + q * plane + (ACROSS ? k0 * ld : k0);
-        // (the rows start on 16 bytes, so what the last piece holds past the end lies in the same 16 bytes as an element)
-        left = ((ACROSS ? (K - 1 - k0) * ld + here : (here - 1) * ld + (K - k0)) * 2 + 15) & ~(int64_t)15;
     }
     __device__ __forceinline__ void advance()
     {
@@ -222,15 +216,18 @@ struct Operand {
         from += by;
         left -= by * 2;
     }
-    // the next step to the stage at `lds` (no step: nothing but zeros)
+    // the next step to the stage at `lds`, plane behind plane (no step: nothing but zeros)
     __device__ __forceinline__ void load(char* lds, bool step)
     {
-        const uint64_t at = (uint64_t)(uintptr_t)from;
         const uint32_t bytes = !step || left <= 0 ? 0u : (uint32_t)min(left, (int64_t)0x7FFFFFF0);
-        const u32x4 r = {(uint32_t)at, (uint32_t)(at >> 32), bytes, 0x00020000u};
-        const uint32_t to = (uint32_t)(uintptr_t)(lds_void_t*)lds + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * 1024;
 #pragma unroll
-        for (int i = 0; i < L; ++i) load_to_lds(r, to + i * T::NT * 16, off[i]);
+        for (int q = 0; q < T::PL; ++q) {
+            const uint64_t at = (uint64_t)(uintptr_t)(from + q * plane);
+            const u32x4 r = {(uint32_t)at, (uint32_t)(at >> 32), bytes, 0x00020000u};
+            const uint32_t to = (uint32_t)(uintptr_t)(lds_void_t*)lds + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * 1024 + q * (W * T::KB);
+#pragma unroll
+            for (int i = 0; i < L; ++i) load_to_lds(r, to + i * T::NT * 16, off[i]);
+        }
     }
     static __device__ __forceinline__ u32x4 fragment(const char* lds, int block, int s) { return fragment_of<W, ACROSS>(lds, block, s); }
 };
@@ -240,17 +237,14 @@ template <typename T, int W, int L, bool ACROSS>
 struct Operand<T, W, L, ACROSS, false> {
     typedef AnyPieces<uint16_t, T::NT, W, T::KE, L, ACROSS> Pieces;
     Pieces pieces;
-    const uint16_t* start;
-    int64_t ld, K, first, all;
     int here;
     uint16_t held[L][8];
 
-    __device__ __forceinline__ void begin(const uint16_t* p, int64_t stride, int64_t, int64_t K_, int64_t first_, int64_t all_)
+    __device__ __forceinline__ void begin(const uint16_t* p, int64_t stride, int64_t, int64_t K, int64_t first, int64_t all, int64_t k0)
     {
-        start = p, ld = stride, K = K_, first = first_, all = all_;
-        here = (int)min((int64_t)W, all - first);
+        pieces.begin(p, stride, K, first, all, k0);
+        here = pieces.here;
     }
-    __device__ __forceinline__ void seek(int k, int) { pieces.begin(start, ld, K, first, all, (int64_t)k * T::KE); }
     __device__ __forceinline__ void load() { pieces.load(held); }
     __device__ __forceinline__ void commit(char* lds)
     {
@@ -273,9 +267,7 @@ struct ProductArgs {
     int64_t plane_a, plane_b;     // distance of an operand's planes
     int64_t M, N, K;
     int64_t m_first;              // what the first row of these M is in the whole product
-    uint32_t seg_a, seg_b;        // plane of each segment, two bits each
-    int segments;
-    int ksteps, each;             // steps of a segment, and of a workgroup that shares it with others (gridDim.z)
+    int ksteps, each;             // steps of the reduction, and of a workgroup that shares it with others (gridDim.z)
     int64_t batch_a, batch_b;     // distances of the batch's matrices (gridDim.y)
     int tiles_m, tiles_n;
     float* partial;               // sums of gridDim.z workgroups, [z][M][N]
@@ -333,66 +325,63 @@ __global__ __launch_bounds__(T::NT) void product_kernel(ProductArgs g, typename 
 
     Operand<T, T::BT, T::LA, A_ACROSS, DIRECT> a;
     Operand<T, T::BN, T::LW, B_ACROSS, DIRECT> b;
-    a.begin(g.a + blockIdx.y * g.batch_a, g.lda, g.plane_a, g.K, m0, g.M);
-    b.begin(g.b + blockIdx.y * g.batch_b, g.ldb, g.plane_b, g.K, n0, g.N);
+    a.begin(g.a + blockIdx.y * g.batch_a, g.lda, g.plane_a, g.K, m0, g.M, (int64_t)ks0 * T::KE);
+    b.begin(g.b + blockIdx.y * g.batch_b, g.ldb, g.plane_b, g.K, n0, g.N, (int64_t)ks0 * T::KE);
     float* const bias = (float*)(smem + T::S * T::STAGE);
     Epi::prepare(e, bias, n0, b.here, T::BN, T::NT);
 
-    const int steps = (ks1 - ks0) * g.segments;
+    const int steps = ks1 - ks0;
     f32x4 acc[T::FN][T::FT];
 #pragma unroll
     for (int i = 0; i < T::FN; ++i)
 #pragma unroll
         for (int j = 0; j < T::FT; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 
-    u32x4 av[2][T::HB], bv[2][T::FN];
+    u32x4 av[2][T::PL][T::HB], bv[2][T::PL][T::FN];
     // The operands of phase p of a stage (half p / H, portion p % H of the rows) to the registers of its parity.
     auto fetch = [&](int buf, auto phase) {
         constexpr int p = decltype(phase)::value, s = p / T::H, h = p % T::H;
-        const char* const at = smem + buf * T::STAGE;
-        if constexpr (h == 0) {
+        const char *const at_a = smem + buf * T::STAGE, *const at_b = at_a + T::PL * T::PLANE_A;
 #pragma unroll
-            for (int i = 0; i < T::FN; ++i) bv[s][i] = b.fragment(at + T::BT * T::KB, wn * T::FN + i, s);
+        for (int q = 0; q < T::PL; ++q) {
+            if constexpr (h == 0) {
+#pragma unroll
+                for (int i = 0; i < T::FN; ++i) bv[s][q][i] = b.fragment(at_b + q * T::PLANE_B, wn * T::FN + i, s);
+            }
+#pragma unroll
+            for (int j = 0; j < T::HB; ++j) av[p & 1][q][j] = a.fragment(at_a + q * T::PLANE_A, wt * T::FT + h * T::HB + j, s);
         }
-#pragma unroll
-        for (int j = 0; j < T::HB; ++j) av[p & 1][j] = a.fragment(at, wt * T::FT + h * T::HB + j, s);
     };
     auto products = [&](auto phase) {
         constexpr int p = decltype(phase)::value, s = p / T::H, h = p % T::H;
 #pragma unroll
-        for (int j = 0; j < T::HB; ++j)
+        for (int t = T::PL == 2 ? 0 : 2; t < 3; ++t)
 #pragma unroll
-            for (int i = 0; i < T::FN; ++i) acc[i][h * T::HB + j] = multiply16<DT>(bv[s][i], av[p & 1][j], acc[i][h * T::HB + j]);
+            for (int j = 0; j < T::HB; ++j)
+#pragma unroll
+                for (int i = 0; i < T::FN; ++i)
+                    acc[i][h * T::HB + j] = multiply16<DT>(bv[s][t == 1 ? 1 : 0][i], av[p & 1][t == 0 ? 1 : 0][j], acc[i][h * T::HB + j]);
     };
-    constexpr int PHASES = 2 * T::H, LOADS = T::LA + T::LW;
+    constexpr int PHASES = 2 * T::H, LOADS = T::PL * (T::LA + T::LW);
     typedef std::integral_constant<int, 0> First;
     typedef std::integral_constant<int, PHASES - 1> Last;
 
     if constexpr (DIRECT) {
-        int ks = ks0, seg = 0;  // the next step to load
-        a.seek(ks, g.seg_a & 3), b.seek(ks, g.seg_b & 3);
+        int ks = ks0;  // the next step to load
         auto load = [&](int buf) {
             char* const to = smem + buf * T::STAGE;
-            const bool step = ks < ks1;
-            a.load(to, step);
-            b.load(to + T::BT * T::KB, step);
-        };
-        auto move = [&]() {  // (apart from load(): its branch would end the stretch of code in which loads and products are interleaved)
+            a.load(to, ks < ks1);
+            b.load(to + T::PL * T::PLANE_A, ks < ks1);
             ++ks;
-            if (ks == ks1 && seg + 1 < g.segments) {
-                ks = ks0, ++seg;
-                a.seek(ks, (g.seg_a >> (2 * seg)) & 3), b.seek(ks, (g.seg_b >> (2 * seg)) & 3);
-            } else {
-                a.advance(), b.advance();
-            }
+            a.advance(), b.advance();
         };
 
         // Order of a phase of many products: after every few one of its LDS reads, then one of its loads, so that products begin at
         // once.  With few products the reads come first, or they would be late.
-        constexpr bool MIXED = T::HB * T::FN >= 16;
-        constexpr int READS_A = T::HB * (A_ACROSS ? 2 : 1), READS_B = T::FN * (B_ACROSS ? 2 : 1);
+        constexpr bool MIXED = T::HB * T::FN * (2 * T::PL - 1) >= 16;
+        constexpr int READS_A = T::PL * T::HB * (A_ACROSS ? 2 : 1), READS_B = T::PL * T::FN * (B_ACROSS ? 2 : 1);
         auto interleave = [&](auto reads, auto loads) {
-            constexpr int R = decltype(reads)::value, L = decltype(loads)::value, M = T::HB * T::FN, EACH = MIXED ? M / (R + L) : 1;
+            constexpr int R = decltype(reads)::value, L = decltype(loads)::value, M = T::HB * T::FN * (2 * T::PL - 1), EACH = MIXED ? M / (R + L) : 1;
             if constexpr (MIXED && EACH > 0) {
                 count_to<R>([&](auto) {
                     __builtin_amdgcn_sched_group_barrier(0x008, EACH, 0);  // products
@@ -411,7 +400,7 @@ __global__ __launch_bounds__(T::NT) void product_kernel(ProductArgs g, typename 
         };
         // Steps past the last are asked for as well, without a byte in range, so that the count of loads on their way is always the same.
 #pragma unroll
-        for (int k = 0; k < T::S; ++k) load(k), move();
+        for (int k = 0; k < T::S; ++k) load(k);
         asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((T::S - 1) * LOADS) : "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
@@ -434,33 +423,30 @@ __global__ __launch_bounds__(T::NT) void product_kernel(ProductArgs g, typename 
             reads_first();
             products(Last());
             interleave(std::integral_constant<int, READS_A + READS_B>(), std::integral_constant<int, LOADS>());
-            move();
             buf = next;
         }
-        // (planes end with zeros up to a whole step)
-        const int tail = g.segments > 1 || ks1 < g.ksteps ? T::KE : (int)(g.K - (int64_t)(g.ksteps - 1) * T::KE);
+        const int tail = ks1 < g.ksteps ? T::KE : (int)(g.K - (int64_t)(g.ksteps - 1) * T::KE);
         count_to<PHASES>([&](auto p) {
             constexpr int q = decltype(p)::value, s = q / T::H;
             if constexpr (q + 1 < PHASES) fetch(buf, std::integral_constant<int, q + 1>());
             const int left = tail - (s * 4 + (lane >> 4)) * 8;
             if constexpr (q % T::H == 0 && !B_ACROSS) {
 #pragma unroll
-                for (int i = 0; i < T::FN; ++i) bv[s][i] = first_elems(bv[s][i], left);
+                for (int i = 0; i < T::PL * T::FN; ++i) bv[s][i / T::FN][i % T::FN] = first_elems(bv[s][i / T::FN][i % T::FN], left);
             }
             if constexpr (!A_ACROSS) {
 #pragma unroll
-                for (int j = 0; j < T::HB; ++j) av[q & 1][j] = first_elems(av[q & 1][j], left);
+                for (int j = 0; j < T::PL * T::HB; ++j) av[q & 1][j / T::HB][j % T::HB] = first_elems(av[q & 1][j / T::HB][j % T::HB], left);
             }
             products(p);
         });
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // nothing may land in LDS after the end
     } else {
-        static_assert(DIRECT || T::S == 2, "one stage is multiplied, the other written");
+        static_assert(DIRECT || (T::S == 2 && T::PL == 1), "one stage is multiplied, the other written");
         auto commit = [&](int buf) {
             a.commit(smem + buf * T::STAGE);
-            b.commit(smem + buf * T::STAGE + T::BT * T::KB);
+            b.commit(smem + buf * T::STAGE + T::PLANE_A);
         };
-        a.seek(ks0, 0), b.seek(ks0, 0);
         a.load(), b.load();
         commit(0);
         a.load(), b.load();
