@@ -340,6 +340,7 @@ struct ResidualNormForm {
     int lanes, most, waves;              // lanes of a row (0: none hold it), elements a lane holds, forward waves a workgroup
     int64_t stretch, each, items;        // backward: as above, and workgroups
     int per, groups;
+    bool sums;                           // ... whether the column sums take a kernel of their own
 };
 hipError_t launch_residual_norm_fwd(const ResidualNormArgs& a, int dtype, hipStream_t s);
 hipError_t launch_residual_norm_bwd(ResidualNormArgs& a, int dtype, hipStream_t s);

@@ -133,60 +133,102 @@ __global__ __launch_bounds__(1024) void residual_norm_bwd_any(ResidualNormArgs a
     }
 }
 
-// The four column sums of each item: a thread a column.
+// The four column sums of each item where no registers held them: a thread eight columns.
 template <int DT>
-__global__ __launch_bounds__(256) void residual_norm_sums_any(ResidualNormArgs a)
+__global__ __launch_bounds__(256) void residual_norm_sums(ResidualNormArgs a)
 {
     typedef typename Prec<DT>::elem_t elem_t;
-    const int j = blockIdx.x * 256 + threadIdx.x;
+    const int64_t j = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;
     if (j >= a.cols) return;
-    float dg = 0.0f, db = 0.0f;
+    const int have = (int)min((int64_t)8, a.cols - j);
+    float gamma[8], dg[8], db[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) gamma[k] = a.gamma && k < have ? a.gamma[j + k] : 1.0f, dg[k] = db[k] = 0.0f;
     for (int64_t item = blockIdx.y; item < a.items; item += gridDim.y) {
         int64_t first, last;
         item_rows(a, item, first, last);
-        float s1 = 0.0f, s2 = 0.0f;
+        float s1[8], s2[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) s1[k] = s2[k] = 0.0f;
         for (int64_t t = first; t < last; ++t) {
             const float4 st = stats_of(a, t);
-            float q = grad_at<DT>(a, t, j, st, a.averages[t * 2], a.averages[t * 2 + 1]);
-            const float hv = Prec<DT>::to_f32(((const elem_t*)a.h)[t * a.ldh + j]);
-            if (a.gate && a.gate_rows == 1) q *= gate_of(Prec<DT>::to_f32(((const elem_t*)a.gate)[t * a.ldg + j]), a.sigmoid);
-            s1 += q, s2 = __builtin_fmaf(q, a.post ? (hv - st.x) * st.y : hv, s2);
-            if (a.dy) {
-                const float dy = Prec<DT>::to_f32(((const elem_t*)a.dy)[t * a.ldy + j]);
-                dg = __builtin_fmaf(dy, (Prec<DT>::to_f32(((const elem_t*)a.x)[t * a.ldr + j]) - st.z) * st.w, dg);
-                db += dy;
+            const float c1 = a.averages[t * 2], c2 = a.averages[t * 2 + 1];
+            float q[8], x[8], dy[8], h[8], g[8];
+            if (a.dr_out) get8<DT>(a.dr_out, t * a.ldr + j, q, have);
+            if (a.dy) get8<DT>(a.x, t * a.ldr + j, x, have), get8<DT>(a.dy, t * a.ldy + j, dy, have);
+            get8<DT>(a.h, t * a.ldh + j, h, have);
+            const bool own_gate = a.gate && a.gate_rows == 1;
+            if (own_gate) get8<DT>(a.gate, t * a.ldg + j, g, have);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                if (!a.dr_out) q[k] = 0.0f;
+                if (a.dy) {
+                    const float xh = (x[k] - st.z) * st.w;
+                    dg[k] = __builtin_fmaf(dy[k], xh, dg[k]), db[k] += dy[k];
+                    q[k] += st.w * (dy[k] * gamma[k] - c1 - xh * c2);
+                }
+                if (own_gate) q[k] *= gate_of(g[k], a.sigmoid);
+                s1[k] += q[k], s2[k] = __builtin_fmaf(q[k], a.post ? (h[k] - st.x) * st.y : h[k], s2[k]);
             }
         }
-        if (a.sums_h) a.sums_h[item * 2 * a.cols + j] = s1, a.sums_h[item * 2 * a.cols + a.cols + j] = s2;
+        if (a.sums_h) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if (k < have) a.sums_h[item * 2 * a.cols + j + k] = s1[k], a.sums_h[item * 2 * a.cols + a.cols + j + k] = s2[k];
+        }
     }
-    if (a.sums) a.sums[(int64_t)blockIdx.y * 2 * a.cols + j] = dg, a.sums[(int64_t)blockIdx.y * 2 * a.cols + a.cols + j] = db;
+    if (a.sums) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            if (k < have) a.sums[(int64_t)blockIdx.y * 2 * a.cols + j + k] = dg[k], a.sums[(int64_t)blockIdx.y * 2 * a.cols + a.cols + j + k] = db[k];
+    }
 }
 
 // ---- joins ----------------------------------------------------------------------------------------------------------------
 
-// Gates that rows share: their gradient from the sums of their rows, which then become those times the gate, at the gate's first item.
+// What the gates' gradient takes: scale, gamma_h and beta_h of a column.
+struct Column {
+    float s, ga, gb;
+    __device__ __forceinline__ Column(const ResidualNormArgs& a, int j)
+        : s(a.scale ? a.scale[j] : 1.0f), ga(a.post && a.gamma_h ? a.gamma_h[j] : 1.0f), gb(a.post && a.beta_h ? a.beta_h[j] : 0.0f)
+    {
+    }
+};
+// The gradient of gate row g, which rows share, from the sums of its runs; s1 and s2 become those of its rows times the gate.
+template <int DT>
+__device__ __forceinline__ void gate_row(const ResidualNormArgs& a, const Column& c, int64_t g, int j, float& s1, float& s2)
+{
+    typedef typename Prec<DT>::elem_t elem_t;
+    s1 = s2 = 0.0f;
+#pragma unroll 4
+    for (int p = 0; p < a.per; ++p) s1 += a.sums_h[(g * a.per + p) * 2 * a.cols + j], s2 += a.sums_h[(g * a.per + p) * 2 * a.cols + a.cols + j];
+    const float gate = gate_of(Prec<DT>::to_f32(((const elem_t*)a.gate)[g * a.ldg + j]), a.sigmoid);
+    if (a.dgate) {
+        float d = c.s * __builtin_fmaf(c.ga, s2, c.gb * s1);
+        if (a.sigmoid) d *= gate * (1.0f - gate);
+        ((elem_t*)a.dgate)[g * a.ldg + j] = Prec<DT>::from_f32(d);
+    }
+    s1 *= gate, s2 *= gate;
+}
+
+// Many gate rows: a kernel of their own, which leaves the sums times the gate at the gate's first run.
 template <int DT>
 __global__ __launch_bounds__(256) void residual_norm_gates(ResidualNormArgs a)
 {
-    typedef typename Prec<DT>::elem_t elem_t;
     const int j = blockIdx.x * 256 + threadIdx.x;
     if (j >= a.cols) return;
-    const float s = a.scale ? a.scale[j] : 1.0f, ga = a.post && a.gamma_h ? a.gamma_h[j] : 1.0f, gb = a.post && a.beta_h ? a.beta_h[j] : 0.0f;
+    const Column c(a, j);
     const int64_t gates = a.items / a.per;
     for (int64_t g = blockIdx.y; g < gates; g += gridDim.y) {
-        float s1 = 0.0f, s2 = 0.0f;
-        for (int p = 0; p < a.per; ++p) s1 += a.sums_h[(g * a.per + p) * 2 * a.cols + j], s2 += a.sums_h[(g * a.per + p) * 2 * a.cols + a.cols + j];
-        const float gate = gate_of(Prec<DT>::to_f32(((const elem_t*)a.gate)[g * a.ldg + j]), a.sigmoid);
-        if (a.dgate) {
-            float d = s * __builtin_fmaf(ga, s2, gb * s1);
-            if (a.sigmoid) d *= gate * (1.0f - gate);
-            ((elem_t*)a.dgate)[g * a.ldg + j] = Prec<DT>::from_f32(d);
-        }
-        a.sums_h[g * a.per * 2 * a.cols + j] = gate * s1, a.sums_h[g * a.per * 2 * a.cols + a.cols + j] = gate * s2;
+        float s1, s2;
+        gate_row<DT>(a, c, g, j, s1, s2);
+        a.sums_h[g * a.per * 2 * a.cols + j] = s1, a.sums_h[g * a.per * 2 * a.cols + a.cols + j] = s2;
     }
 }
 
-// Sums of `parts` and of `items`, 16 columns and 64 lanes of rows a workgroup, and from them the gradients of the vectors.
+// Sums of `parts` and of `items` (every `per`-th run, or GATES: gate rows), 16 columns and 64 lanes of rows a workgroup, and from them the gradients of the
+// vectors.
+template <int DT, bool GATES>
 __global__ __launch_bounds__(1024) void residual_norm_join(ResidualNormArgs a, int parts, int64_t items, int per)
 {
     __shared__ float red[4][64][16];
@@ -194,26 +236,37 @@ __global__ __launch_bounds__(1024) void residual_norm_join(ResidualNormArgs a, i
     const int j = blockIdx.x * 16 + l;
     float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
     if (j < a.cols) {
-        if (a.sums)
+        if (a.sums) {
+#pragma unroll 4
             for (int p = lane; p < parts; p += 64) s[0] += a.sums[(int64_t)p * 2 * a.cols + j], s[1] += a.sums[(int64_t)p * 2 * a.cols + a.cols + j];
-        if (a.sums_h)
+        }
+        if constexpr (GATES) {
+            const Column c(a, j);
+            for (int64_t g = lane; g < items; g += 64) {
+                float s1, s2;
+                gate_row<DT>(a, c, g, j, s1, s2);
+                s[2] += s1, s[3] += s2;
+            }
+        } else if (a.sums_h) {
+#pragma unroll 4
             for (int64_t p = lane; p < items; p += 64) s[2] += a.sums_h[p * per * 2 * a.cols + j], s[3] += a.sums_h[p * per * 2 * a.cols + a.cols + j];
+        }
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) red[i][lane][l] = s[i];
     __syncthreads();
     if (lane >= 4) return;
     float sum = 0.0f;  // lane i: sum i (one wave is left, so the four sums of a column are in its lanes)
-#pragma unroll 8
+#pragma unroll 16
     for (int p = 0; p < 64; ++p) sum += red[lane][p][l];
     const float dg = __shfl(sum, l), db = __shfl(sum, 16 + l), s1 = __shfl(sum, 32 + l), s2 = __shfl(sum, 48 + l);
     if (lane || j >= a.cols) return;
+    const Column c(a, j);
     if (a.dgamma) a.dgamma[j] = dg;
     if (a.dbeta) a.dbeta[j] = db;
-    const float scale = a.scale ? a.scale[j] : 1.0f;
-    if (a.dgamma_h) a.dgamma_h[j] = scale * s2;
-    if (a.dbeta_h) a.dbeta_h[j] = scale * s1;
-    if (a.dscale) a.dscale[j] = a.post ? __builtin_fmaf(a.gamma_h ? a.gamma_h[j] : 1.0f, s2, (a.beta_h ? a.beta_h[j] : 0.0f) * s1) : s2;
+    if (a.dgamma_h) a.dgamma_h[j] = c.s * s2;
+    if (a.dbeta_h) a.dbeta_h[j] = c.s * s1;
+    if (a.dscale) a.dscale[j] = __builtin_fmaf(c.ga, s2, c.gb * s1);
 }
 
 // ---- forms ----------------------------------------------------------------------------------------------------------------
@@ -243,11 +296,12 @@ ResidualNormForm bwd_form(int64_t rows, int cols, int64_t gate_rows, int dtype)
 {
     ResidualNormForm f = {};
     if (dtype == CONV_F32 && cols <= 32) f.lanes = 8, f.most = 4;
-    for (int lanes : {8, 16, 64, 256, 512})
-        for (int most : {8, 16})
-            if (cols <= lanes * most && !f.lanes && !(lanes == 512 && most == 8)) f.lanes = lanes, f.most = most;
-    const int here = f.lanes ? (f.lanes <= 16 ? 256 : 512) / f.lanes : 1;  // rows at once
-    const int64_t most = f.lanes ? (f.most <= 8 ? 4 * kCUs : 2 * kCUs) : 64;
+    for (int lanes = 8; lanes <= 1024 && !f.lanes; lanes *= 2)
+        if (cols <= lanes * 8) f.lanes = lanes, f.most = 8;
+    if (!f.lanes && cols <= 16384) f.lanes = 1024, f.most = 16;
+    f.sums = f.most == 16 || !f.lanes;  // the column sums by a kernel of their own
+    const int here = f.sums ? 1 : (f.lanes <= 256 ? 256 : f.lanes) / f.lanes;  // rows at once
+    const int64_t most = f.sums ? 128 : f.lanes == 1024 ? kCUs : f.lanes <= 16 ? 4 * kCUs : 2 * kCUs;
     f.stretch = gate_rows > 1 ? gate_rows : std::max<int64_t>(rows, 1);
     const int64_t stretches = (rows + f.stretch - 1) / f.stretch;
     // as many runs as workgroups, of whole rounds; at least eight rows each, lest their sums cost more than they
@@ -276,7 +330,7 @@ Space space_of(const ResidualNormForm& f, int64_t rows, int cols, void* ws)
     };
     s.sums = take((size_t)f.groups * 2 * cols * 4);
     s.sums_h = take((size_t)f.items * 2 * cols * 4);
-    if (!f.lanes) s.averages = take((size_t)rows * 2 * 4);
+    if (f.sums) s.averages = take((size_t)rows * 2 * 4);
     return s;
 }
 
@@ -289,15 +343,20 @@ hipError_t bwd(ResidualNormArgs a, const ResidualNormForm& f, hipStream_t s)
             if (e != hipSuccess) return e;
         } else {
             hipLaunchKernelGGL((residual_norm_bwd_any<DT>), dim3((unsigned)std::min<int64_t>(a.rows, 1 << 20)), dim3(1024), 0, s, a);
-            if (a.sums || a.sums_h) hipLaunchKernelGGL((residual_norm_sums_any<DT>), dim3((unsigned)((a.cols + 255) / 256), (unsigned)f.groups), dim3(256), 0, s, a);
         }
-        if (a.gate && a.gate_rows > 1 && a.sums_h)
-            hipLaunchKernelGGL((residual_norm_gates<DT>), dim3((unsigned)((a.cols + 255) / 256), (unsigned)std::min<int64_t>(f.items / f.per, 4096)), dim3(256), 0, s, a);
+        if (f.sums && (a.sums || a.sums_h)) hipLaunchKernelGGL((residual_norm_sums<DT>), dim3((unsigned)((a.cols + 2047) / 2048), (unsigned)f.groups), dim3(256), 0, s, a);
     }
-    if (a.dgamma || a.dbeta || a.dgamma_h || a.dbeta_h || a.dscale) {
-        const bool shared = a.gate && a.gate_rows > 1;
-        hipLaunchKernelGGL(residual_norm_join, dim3((unsigned)((a.cols + 15) / 16)), dim3(1024), 0, s, a, a.rows ? f.groups : 0, shared ? f.items / f.per : f.items,
-                           shared ? f.per : 1);
+    if (!a.sums && !a.sums_h) return hipGetLastError();
+    const dim3 grid((unsigned)((a.cols + 15) / 16));
+    const bool shared = a.rows && a.gate && a.gate_rows > 1 && a.sums_h;
+    const int parts = a.rows ? f.groups : 0;
+    // few gate rows in the join itself; many by a kernel that has more than a workgroup for 16 columns
+    if (shared && f.items / f.per <= 256) {
+        hipLaunchKernelGGL((residual_norm_join<DT, true>), grid, dim3(1024), 0, s, a, parts, f.items / f.per, f.per);
+    } else {
+        if (shared)
+            hipLaunchKernelGGL((residual_norm_gates<DT>), dim3((unsigned)((a.cols + 255) / 256), (unsigned)std::min<int64_t>(f.items / f.per, 4096)), dim3(256), 0, s, a);
+        hipLaunchKernelGGL((residual_norm_join<DT, false>), grid, dim3(1024), 0, s, a, parts, a.rows ? (shared ? f.items / f.per : f.items) : 0, shared ? f.per : 1);
     }
     return hipGetLastError();
 }

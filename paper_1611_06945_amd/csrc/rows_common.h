@@ -57,6 +57,50 @@ struct Piece {
     }
 };
 
+// Eight neighbouring elements (n of them exist), to or from a row that starts at any element.
+template <int DT>
+__device__ __forceinline__ void put8(void* row, int64_t at, const float (&v)[8], int n)
+{
+    typedef Piece<DT> P;
+    typename P::elem_t* p = (typename P::elem_t*)row + at;
+    constexpr int VEC = P::VEC;
+#pragma unroll
+    for (int c = 0; c < 8 / VEC; ++c) {
+        float part[VEC];
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) part[k] = v[c * VEC + k];
+        const uint4 u = P::narrow(part);
+        if (n >= (c + 1) * VEC) {
+            P::put(p + c * VEC, u);
+        } else {
+            typename P::elem_t e[VEC];
+            __builtin_memcpy(e, &u, 16);
+#pragma unroll
+            for (int k = 0; k < VEC; ++k)
+                if (c * VEC + k < n) p[c * VEC + k] = e[k];
+        }
+    }
+}
+template <int DT>
+__device__ __forceinline__ void get8(const void* row, int64_t at, float (&v)[8], int n)
+{
+    typedef Piece<DT> P;
+    const typename P::elem_t* p = (const typename P::elem_t*)row + at;
+    constexpr int VEC = P::VEC;
+#pragma unroll
+    for (int c = 0; c < 8 / VEC; ++c) {
+        if (n >= (c + 1) * VEC) {
+            float part[VEC];
+            P::widen(P::raw(p + c * VEC), part);
+#pragma unroll
+            for (int k = 0; k < VEC; ++k) v[c * VEC + k] = part[k];
+        } else {
+#pragma unroll
+            for (int k = 0; k < VEC; ++k) v[c * VEC + k] = c * VEC + k < n ? Prec<DT>::to_f32(p[c * VEC + k]) : 0.0f;
+        }
+    }
+}
+
 struct OpSum {
     static __device__ __forceinline__ float of(float a, float b) { return a + b; }
 };
