@@ -226,47 +226,60 @@ __global__ __launch_bounds__(256) void residual_norm_gates(ResidualNormArgs a)
     }
 }
 
-// Sums of `parts` and of `items` (every `per`-th run, or GATES: gate rows), 16 columns and 64 lanes of rows a workgroup, and from them the gradients of the
-// vectors.
-template <int DT, bool GATES>
+// Sums of `parts` and of `items` (every `per`-th run, or GATES: gate rows), C columns and 1024 / C lanes of rows a workgroup, and from them the gradients
+// of the vectors.
+template <int DT, bool GATES, int C>
 __global__ __launch_bounds__(1024) void residual_norm_join(ResidualNormArgs a, int parts, int64_t items, int per)
 {
-    __shared__ float red[4][64][16];
-    const int l = threadIdx.x & 15, lane = threadIdx.x >> 4;
-    const int j = blockIdx.x * 16 + l;
+    constexpr int LANES = 1024 / C;
+    __shared__ float red[4][LANES][C];
+    const int l = threadIdx.x % C, lane = threadIdx.x / C;
+    const int j = blockIdx.x * C + l;
     float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
     if (j < a.cols) {
         if (a.sums) {
 #pragma unroll 4
-            for (int p = lane; p < parts; p += 64) s[0] += a.sums[(int64_t)p * 2 * a.cols + j], s[1] += a.sums[(int64_t)p * 2 * a.cols + a.cols + j];
+            for (int p = lane; p < parts; p += LANES) s[0] += a.sums[(int64_t)p * 2 * a.cols + j], s[1] += a.sums[(int64_t)p * 2 * a.cols + a.cols + j];
         }
         if constexpr (GATES) {
             const Column c(a, j);
-            for (int64_t g = lane; g < items; g += 64) {
+            for (int64_t g = lane; g < items; g += LANES) {
                 float s1, s2;
                 gate_row<DT>(a, c, g, j, s1, s2);
                 s[2] += s1, s[3] += s2;
             }
         } else if (a.sums_h) {
 #pragma unroll 4
-            for (int64_t p = lane; p < items; p += 64) s[2] += a.sums_h[p * per * 2 * a.cols + j], s[3] += a.sums_h[p * per * 2 * a.cols + a.cols + j];
+            for (int64_t p = lane; p < items; p += LANES) s[2] += a.sums_h[p * per * 2 * a.cols + j], s[3] += a.sums_h[p * per * 2 * a.cols + a.cols + j];
         }
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) red[i][lane][l] = s[i];
     __syncthreads();
     if (lane >= 4) return;
-    float sum = 0.0f;  // lane i: sum i (one wave is left, so the four sums of a column are in its lanes)
+    float sum = 0.0f;  // lane i: sum i
 #pragma unroll 16
-    for (int p = 0; p < 64; ++p) sum += red[lane][p][l];
-    const float dg = __shfl(sum, l), db = __shfl(sum, 16 + l), s1 = __shfl(sum, 32 + l), s2 = __shfl(sum, 48 + l);
-    if (lane || j >= a.cols) return;
+    for (int p = 0; p < LANES; ++p) sum += red[lane][p][l];
+    if (j >= a.cols) return;
     const Column c(a, j);
-    if (a.dgamma) a.dgamma[j] = dg;
-    if (a.dbeta) a.dbeta[j] = db;
-    if (a.dgamma_h) a.dgamma_h[j] = c.s * s2;
-    if (a.dbeta_h) a.dbeta_h[j] = c.s * s1;
-    if (a.dscale) a.dscale[j] = __builtin_fmaf(c.ga, s2, c.gb * s1);
+    if (lane == 0 && a.dgamma) a.dgamma[j] = sum;
+    if (lane == 1 && a.dbeta) a.dbeta[j] = sum;
+    if (lane == 2 && a.dbeta_h) a.dbeta_h[j] = c.s * sum;
+    if (lane == 3 && a.dgamma_h) a.dgamma_h[j] = c.s * sum;
+    if (lane == 3 && a.dscale) {
+        float s1 = 0.0f;  // (the same sum as lane 2's)
+#pragma unroll 16
+        for (int p = 0; p < LANES; ++p) s1 += red[2][p][l];
+        a.dscale[j] = __builtin_fmaf(c.ga, sum, c.gb * s1);
+    }
+}
+
+// 64 columns a workgroup where that leaves some for every CU, else 16.
+template <int DT, bool GATES>
+void join(const ResidualNormArgs& a, int parts, int64_t items, int per, hipStream_t s)
+{
+    if (a.cols >= 16 * kCUs) hipLaunchKernelGGL((residual_norm_join<DT, GATES, 64>), dim3((unsigned)((a.cols + 63) / 64)), dim3(1024), 0, s, a, parts, items, per);
+    else hipLaunchKernelGGL((residual_norm_join<DT, GATES, 16>), dim3((unsigned)((a.cols + 15) / 16)), dim3(1024), 0, s, a, parts, items, per);
 }
 
 // ---- forms ----------------------------------------------------------------------------------------------------------------
@@ -301,7 +314,7 @@ ResidualNormForm bwd_form(int64_t rows, int cols, int64_t gate_rows, int dtype)
     if (!f.lanes && cols <= 16384) f.lanes = 1024, f.most = 16;
     f.sums = f.most == 16 || !f.lanes;  // the column sums by a kernel of their own
     const int here = f.sums ? 1 : (f.lanes <= 256 ? 256 : f.lanes) / f.lanes;  // rows at once
-    const int64_t most = f.sums ? 128 : f.lanes == 1024 ? kCUs : f.lanes <= 16 ? 4 * kCUs : 2 * kCUs;
+    const int64_t most = f.sums ? 128 : f.lanes >= 512 ? kCUs : f.lanes <= 16 ? 4 * kCUs : 2 * kCUs;
     f.stretch = gate_rows > 1 ? gate_rows : std::max<int64_t>(rows, 1);
     const int64_t stretches = (rows + f.stretch - 1) / f.stretch;
     // as many runs as workgroups, of whole rounds; at least eight rows each, lest their sums cost more than they
@@ -347,16 +360,15 @@ hipError_t bwd(ResidualNormArgs a, const ResidualNormForm& f, hipStream_t s)
         if (f.sums && (a.sums || a.sums_h)) hipLaunchKernelGGL((residual_norm_sums<DT>), dim3((unsigned)((a.cols + 2047) / 2048), (unsigned)f.groups), dim3(256), 0, s, a);
     }
     if (!a.sums && !a.sums_h) return hipGetLastError();
-    const dim3 grid((unsigned)((a.cols + 15) / 16));
     const bool shared = a.rows && a.gate && a.gate_rows > 1 && a.sums_h;
     const int parts = a.rows ? f.groups : 0;
     // few gate rows in the join itself; many by a kernel that has more than a workgroup for 16 columns
     if (shared && f.items / f.per <= 256) {
-        hipLaunchKernelGGL((residual_norm_join<DT, true>), grid, dim3(1024), 0, s, a, parts, f.items / f.per, f.per);
+        join<DT, true>(a, parts, f.items / f.per, f.per, s);
     } else {
         if (shared)
             hipLaunchKernelGGL((residual_norm_gates<DT>), dim3((unsigned)((a.cols + 255) / 256), (unsigned)std::min<int64_t>(f.items / f.per, 4096)), dim3(256), 0, s, a);
-        hipLaunchKernelGGL((residual_norm_join<DT, false>), grid, dim3(1024), 0, s, a, parts, a.rows ? (shared ? f.items / f.per : f.items) : 0, shared ? f.per : 1);
+        join<DT, false>(a, parts, a.rows ? (shared ? f.items / f.per : f.items) : 0, shared ? f.per : 1, s);
     }
     return hipGetLastError();
 }

@@ -32,6 +32,9 @@ __device__ __forceinline__ void item_rows(const ResidualNormArgs& a, int64_t ite
 
 __device__ __forceinline__ float gate_of(float g, int sigmoid) { return sigmoid ? __builtin_amdgcn_rcpf(1.0f + __expf(-g)) : g; }
 
+// A gate of each row's own, or one that rows share.
+enum { NO_GATE = 0, OWN_GATE = 1, SHARED_GATE = 2 };
+
 // PLAIN calls have all tensors and rows of whole pieces: without a branch for each tensor and a mask for each element the backward
 // kernel takes half the instructions, which bound it.  A lane's piece is then in the row or behind it.
 template <int N>
@@ -40,7 +43,7 @@ __device__ __forceinline__ void keep_if(bool live, uint4 (&raw)[N], int i)
     raw[i].x = live ? raw[i].x : 0, raw[i].y = live ? raw[i].y : 0, raw[i].z = live ? raw[i].z : 0, raw[i].w = live ? raw[i].w : 0;
 }
 
-template <int DT, int G, int NV, int MAXT, bool POST, bool GATE, bool PLAIN>
+template <int DT, int G, int NV, int MAXT, bool POST, int GATE, bool PLAIN>
 __global__ __launch_bounds__(MAXT) void residual_norm_fwd_rows(ResidualNormArgs a)
 {
     typedef Held<DT, G, NV> H;
@@ -56,7 +59,7 @@ __global__ __launch_bounds__(MAXT) void residual_norm_fwd_rows(ResidualNormArgs 
         t = t < a.rows ? t : a.rows - 1;
         H::load(nr, (const elem_t*)a.r + t * a.ldr, a.cols, l);
         H::load(nh, (const elem_t*)a.h + t * a.ldh, a.cols, l);
-        if constexpr (GATE) H::load(ng, (const elem_t*)a.gate + (int64_t)((uint32_t)t / (uint32_t)a.gate_rows) * a.ldg, a.cols, l);
+        if constexpr (GATE != NO_GATE) H::load(ng, (const elem_t*)a.gate + (int64_t)((uint32_t)t / (uint32_t)a.gate_rows) * a.ldg, a.cols, l);
     };
     constexpr bool AHEAD = NV * VEC < 16 || DT != CONV_F32;
     if (AHEAD) load(row);
@@ -133,12 +136,12 @@ __global__ __launch_bounds__(MAXT) void residual_norm_fwd_rows(ResidualNormArgs 
         float x[NV][VEC], u[NV][VEC], g[NV][VEC];
         clear(nr);
         clear(nh);
-        if constexpr (GATE) clear(ng);
+        if constexpr (GATE != NO_GATE) clear(ng);
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             H::P::widen(nr[i], x[i]);
             H::P::widen(nh[i], u[i]);
-            if constexpr (GATE) H::P::widen(ng[i], g[i]);
+            if constexpr (GATE != NO_GATE) H::P::widen(ng[i], g[i]);
         }
         if (AHEAD && first + step < a.rows) load(row + step);
         float mean_h = 0.0f, rstd_h = 1.0f, mean = 0.0f, rstd = 1.0f;
@@ -148,7 +151,7 @@ __global__ __launch_bounds__(MAXT) void residual_norm_fwd_rows(ResidualNormArgs 
 #pragma unroll
             for (int k = 0; k < VEC; ++k) {
                 float v = POST ? __builtin_fmaf(u[i][k] * rstd_h, ga[i][k], gb[i][k]) : u[i][k] * ga[i][k];
-                if constexpr (GATE) v *= gate_of(g[i][k], a.sigmoid);
+                if constexpr (GATE != NO_GATE) v *= gate_of(g[i][k], a.sigmoid);
                 x[i][k] += v;
             }
         const bool in = row < a.rows;
@@ -204,7 +207,7 @@ __device__ __forceinline__ void sets_sum(float (&x)[N], float (&y)[N], float* ld
 // Where a lane holds 16 elements (a workgroup of 1024 a row) there are no registers for the column sums: it leaves the averages of each
 // row, and residual_norm_sums reads the tensors again.
 // (Registers for three workgroups of 256 a CU, or one of 512 or 1024.)
-template <int DT, int G, int NV, int NT, bool POST, bool GATE, bool PLAIN>
+template <int DT, int G, int NV, int NT, bool POST, int GATE, bool PLAIN>
 __global__ __launch_bounds__(NT, NT == 256 ? 3 : 1) void residual_norm_bwd_rows(ResidualNormArgs a)
 {
     typedef Held<DT, G, NV> H;
@@ -217,7 +220,6 @@ __global__ __launch_bounds__(NT, NT == 256 ? 3 : 1) void residual_norm_bwd_rows(
     const float inv_cols = 1.0f / (float)a.cols;
     const int set = G <= 64 ? tid / 64 : tid / G;
     const bool holder = G >= 64 || (tid & 63) < G;
-    const bool shared_gate = GATE && a.gate_rows > 1;
 
     auto reduce2 = [&](float& s1, float& s2) {
         if constexpr (G <= 64) {
@@ -313,7 +315,7 @@ __global__ __launch_bounds__(NT, NT == 256 ? 3 : 1) void residual_norm_bwd_rows(
     };
     auto load_h = [&](int64_t t) {
         H::load(nh, (const elem_t*)a.h + t * a.ldh, a.cols, l);
-        if constexpr (GATE) H::load(ng, (const elem_t*)a.gate + (int64_t)((uint32_t)t / (uint32_t)a.gate_rows) * a.ldg, a.cols, l);
+        if constexpr (GATE != NO_GATE) H::load(ng, (const elem_t*)a.gate + (int64_t)((uint32_t)t / (uint32_t)a.gate_rows) * a.ldg, a.cols, l);
     };
     auto row_of = [&](int64_t at, int64_t end) { return min(at + tid / G, end - 1); };
     int64_t item = blockIdx.x, begin, end;
@@ -402,12 +404,12 @@ __global__ __launch_bounds__(NT, NT == 256 ? 3 : 1) void residual_norm_bwd_rows(
             float hh[NV][VEC], gates[NV][VEC];
             if constexpr (!PLAIN) {
                 H::clear(nh, a.cols, l);
-                if constexpr (GATE) H::clear(ng, a.cols, l);
+                if constexpr (GATE != NO_GATE) H::clear(ng, a.cols, l);
             }
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
                 H::P::widen(nh[i], hh[i]);
-                if constexpr (GATE) H::P::widen(ng[i], gates[i]);
+                if constexpr (GATE != NO_GATE) H::P::widen(ng[i], gates[i]);
             }
             if constexpr (AHEAD) load_h(ahead);
             float d1 = 0.0f, d2 = 0.0f;
@@ -419,14 +421,14 @@ __global__ __launch_bounds__(NT, NT == 256 ? 3 : 1) void residual_norm_bwd_rows(
                 for (int k = 0; k < VEC; ++k) {
                     if constexpr (POST) hh[i][k] = (hh[i][k] - st.x) * st.y;
                     float p = q[i][k], sum = p;
-                    if constexpr (GATE) {
+                    if constexpr (GATE != NO_GATE) {
                         const float gate = gate_of(g[k], a.sigmoid);
-                        if (!shared_gate) {
+                        if constexpr (GATE == OWN_GATE) {
                             dgate[k] = p * (POST ? __builtin_fmaf(hh[i][k], ga[i][k], gb[i][k]) : hh[i][k] * ga[i][k]);
                             if (a.sigmoid) dgate[k] *= gate * (1.0f - gate);
                         }
                         p *= gate;
-                        if (!shared_gate) sum = p;
+                        if constexpr (GATE == OWN_GATE) sum = p;
                     }
                     if constexpr (SUMS) {
                         if (in) {
@@ -440,7 +442,7 @@ __global__ __launch_bounds__(NT, NT == 256 ? 3 : 1) void residual_norm_bwd_rows(
                         d2 = __builtin_fmaf(q[i][k], hh[i][k], d2);
                     }
                 }
-                if (GATE && !shared_gate && in && (PLAIN || a.dgate)) store((elem_t*)a.dgate + row * a.ldg, dgate, i);
+                if (GATE == OWN_GATE && in && (PLAIN || a.dgate)) store((elem_t*)a.dgate + row * a.ldg, dgate, i);
             }
             if (PLAIN || a.dh) {
                 if constexpr (POST) reduce2(d1, d2);
@@ -472,7 +474,7 @@ __global__ __launch_bounds__(NT, NT == 256 ? 3 : 1) void residual_norm_bwd_rows(
     }
 }
 
-template <int DT, int G, int NV, bool POST, bool GATE, bool PLAIN>
+template <int DT, int G, int NV, bool POST, int GATE, bool PLAIN>
 void residual_norm_fwd_launch(const ResidualNormArgs& a, int waves, hipStream_t s)
 {
     constexpr int CUS = 256;
@@ -486,7 +488,7 @@ void residual_norm_fwd_launch(const ResidualNormArgs& a, int waves, hipStream_t 
 }
 
 // `most` elements a lane: 8 or 16, and one piece of fp32 in rows of eight lanes (Held loads rows shorter than a piece only there)
-template <int DT, int G, bool POST, bool GATE, bool PLAIN>
+template <int DT, int G, bool POST, int GATE, bool PLAIN>
 void residual_norm_fwd_pieces(const ResidualNormArgs& a, int most, int waves, hipStream_t s)
 {
     constexpr int VEC = DT == CONV_F32 ? 4 : 8;
@@ -498,7 +500,8 @@ void residual_norm_fwd_pieces(const ResidualNormArgs& a, int most, int waves, hi
 }
 
 struct FwdHeld {
-    template <int DT, bool POST, bool GATE, bool PLAIN>
+    static constexpr bool GATES_ALIKE = true;
+    template <int DT, bool POST, int GATE, bool PLAIN>
     static void run(const ResidualNormArgs& a, const ResidualNormForm& f, hipStream_t s)
     {
         if (f.lanes == 8) residual_norm_fwd_pieces<DT, 8, POST, GATE, PLAIN>(a, f.most, 4, s);
@@ -509,12 +512,13 @@ struct FwdHeld {
 };
 
 struct BwdHeld {
-    template <int DT, int G, int NV, int NT, bool POST, bool GATE, bool PLAIN>
+    static constexpr bool GATES_ALIKE = false;
+    template <int DT, int G, int NV, int NT, bool POST, int GATE, bool PLAIN>
     static void launch(const ResidualNormArgs& a, const ResidualNormForm& f, hipStream_t s)
     {
         hipLaunchKernelGGL((residual_norm_bwd_rows<DT, G, NV, NT, POST, GATE, PLAIN>), dim3((unsigned)f.groups), dim3(NT), 0, s, a);
     }
-    template <int DT, bool POST, bool GATE, bool PLAIN>
+    template <int DT, bool POST, int GATE, bool PLAIN>
     static void run(const ResidualNormArgs& a, const ResidualNormForm& f, hipStream_t s)
     {
         constexpr int VEC = DT == CONV_F32 ? 4 : 8;
@@ -540,13 +544,18 @@ template <int DT, typename F>
 hipError_t residual_norm_held(const ResidualNormArgs& a, const ResidualNormForm& f, bool all, hipStream_t s)
 {
     const bool plain = all && a.cols % (DT == CONV_F32 ? 4 : 8) == 0;
-    if (a.post) {
-        if (a.gate) plain ? F::template run<DT, true, true, true>(a, f, s) : F::template run<DT, true, true, false>(a, f, s);
-        else plain ? F::template run<DT, true, false, true>(a, f, s) : F::template run<DT, true, false, false>(a, f, s);
-    } else {
-        if (a.gate) plain ? F::template run<DT, false, true, true>(a, f, s) : F::template run<DT, false, true, false>(a, f, s);
-        else plain ? F::template run<DT, false, false, true>(a, f, s) : F::template run<DT, false, false, false>(a, f, s);
+    const int gate = !a.gate ? NO_GATE : a.gate_rows == 1 || F::GATES_ALIKE ? OWN_GATE : SHARED_GATE;
+#define CONVFWD_WITH(POST, GATE) \
+    if ((a.post != 0) == POST && gate == GATE) plain ? F::template run<DT, POST, GATE, true>(a, f, s) : F::template run<DT, POST, GATE, false>(a, f, s);
+    CONVFWD_WITH(true, NO_GATE)
+    CONVFWD_WITH(true, OWN_GATE)
+    CONVFWD_WITH(false, NO_GATE)
+    CONVFWD_WITH(false, OWN_GATE)
+    if constexpr (!F::GATES_ALIKE) {
+        CONVFWD_WITH(true, SHARED_GATE)
+        CONVFWD_WITH(false, SHARED_GATE)
     }
+#undef CONVFWD_WITH
     return hipGetLastError();
 }
 template <int DT>
