@@ -85,10 +85,11 @@ struct LinearEpi {
 };
 
 // Tiles of a product; the last two are for operands that start anywhere.
-enum ProductForm { P64, P128, P256, P64_ANY, P128_ANY };
+enum ProductForm { P64, P128, P256, P192, P64_ANY, P128_ANY };
 typedef ProductTile<4, 2, 1, 2, 4> Tile64;
 typedef ProductTile<2, 4, 4, 2, 2> Tile128;  // two workgroups a CU
 typedef ProductTile<4, 2, 4, 8, 2> Tile256;
+typedef ProductTile<4, 2, 3, 6, 3> Tile192;
 typedef ProductTile<4, 2, 1, 2, 2> Tile64Any;
 
 enum ProductLayout { LAYOUT_NT, LAYOUT_NN, LAYOUT_TN };  // which operand lies across the reduction: none, the second, both
@@ -106,7 +107,7 @@ hipError_t launch_product_tiles(ProductArgs g, const typename Epi::Args& e, int 
     const hipError_t err = ensure_dynamic_lds(f, T::LDS);
     if (err != hipSuccess) return err;
     g.tiles_n = (int)((g.N + T::BN - 1) / T::BN);
-    g.each = (g.ksteps + splits - 1) / splits;
+    g.each = (g.ksteps + splits - 1) / splits, g.splits = splits;
     // a launch holds less than 2^32 threads: the rows go in portions of so many tiles
     const int64_t all = g.M, bands = std::max<int64_t>(1, (1 << 21) / ((int64_t)g.tiles_n * batch * splits));
     for (int64_t skip = 0; skip < all; skip += bands * T::BT) {
@@ -115,7 +116,7 @@ hipError_t launch_product_tiles(ProductArgs g, const typename Epi::Args& e, int 
         p.a += A_ACROSS ? skip : skip * g.lda;
         p.tiles_m = (int)((p.M + T::BT - 1) / T::BT);
         const unsigned tiles = Epi::SYMMETRIC ? (unsigned)((int64_t)p.tiles_m * (p.tiles_m + 1) / 2) : (unsigned)p.tiles_m * (unsigned)p.tiles_n;
-        hipLaunchKernelGGL((product_kernel<DT, T, A_ACROSS, B_ACROSS, DIRECT, Epi>), dim3(tiles, (unsigned)batch, (unsigned)splits), dim3(T::NT), T::LDS, s, p, e);
+        hipLaunchKernelGGL((product_kernel<DT, T, A_ACROSS, B_ACROSS, DIRECT, Epi>), dim3(tiles * (unsigned)splits, (unsigned)batch), dim3(T::NT), T::LDS, s, p, e);
     }
     return hipGetLastError();
 }
@@ -127,6 +128,7 @@ hipError_t launch_product_form(const ProductArgs& g, const typename Epi::Args& e
         case P64: return launch_product_tiles<DT, Tile64, A_ACROSS, B_ACROSS, true, Epi>(g, e, batch, splits, s);
         case P128: return launch_product_tiles<DT, Tile128, A_ACROSS, B_ACROSS, true, Epi>(g, e, batch, splits, s);
         case P256: return launch_product_tiles<DT, Tile256, A_ACROSS, B_ACROSS, true, Epi>(g, e, batch, splits, s);
+        case P192: return launch_product_tiles<DT, Tile192, A_ACROSS, B_ACROSS, true, Epi>(g, e, batch, splits, s);
         case P64_ANY: return launch_product_tiles<DT, Tile64Any, A_ACROSS, B_ACROSS, false, Epi>(g, e, batch, splits, s);
         default: return launch_product_tiles<DT, Tile128, A_ACROSS, B_ACROSS, false, Epi>(g, e, batch, splits, s);
     }

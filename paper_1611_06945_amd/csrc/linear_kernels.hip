@@ -84,19 +84,23 @@ __global__ __launch_bounds__(64 * W) void linear_rows(LinearRows g)
     const __amdgpu_buffer_rsrc_t rw = make_rsrc(w, DIRECT ? (uint32_t)(((outs_here - 1) * g.ldw + g.K) * ES + 15) & ~15u : 0u);
     const uint32_t woff = DIRECT ? (uint32_t)row * (uint32_t)(g.ldw * ES) + piece * 16 : 0u;
     const uint32_t xoff = DIRECT ? (uint32_t)row * (uint32_t)(g.ldx * ES) + piece * 16 : 0u;
-    // a piece from any address
-    auto through = [&](const elem_t* p, bool in, int k, char* to) {
-        const int n = in ? g.K - k : 0;
-        u32x4 v = {0, 0, 0, 0};
-        if (n >= VEC) {
-            __builtin_memcpy(&v, p + k, 16);
-        } else if (n > 0) {
-            elem_t e[VEC];
+    // Pieces from any address: all of a run's are asked for, without a branch, before the first is written to LDS.  Lanes without a row read another one's;
+    // only the run that holds the reduction's end loads element by element.
+    auto pieces = [&](const elem_t* p, int64_t ld, int at, int here, int k, u32x4 (&v)[U]) {
+        const elem_t* from = p + (int64_t)min(at, here - 1) * ld + piece * VEC;
+        if (k + RUN <= g.K) {
 #pragma unroll
-            for (int j = 0; j < VEC; ++j) e[j] = j < n ? p[k + j] : (elem_t)0;
-            __builtin_memcpy(&v, e, 16);
+            for (int u = 0; u < U; ++u) __builtin_memcpy(&v[u], from + k + u * (64 / ES), 16);
+        } else {
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int first = k + u * (64 / ES), n = g.K - first - piece * VEC;
+                elem_t e[VEC];
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) e[j] = j < n ? from[first + j] : (elem_t)0;
+                __builtin_memcpy(&v[u], e, 16);
+            }
         }
-        *(u32x4*)(to + lane * 16) = v;
     };
 
     f32x4 acc[RB];
@@ -115,13 +119,14 @@ __global__ __launch_bounds__(64 * W) void linear_rows(LinearRows g)
                                                              (int)(xoff + (uint32_t)(j * 16) * (uint32_t)(g.ldx * ES) + (uint32_t)k * ES + u * 64), 0, 0, 0);
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         } else {
+u32x4 got[1 + RB][U];
+            pieces(w, g.ldw, row, outs_here, k, got[0]);
 #pragma unroll
-            for (int u = 0; u < U; ++u) through(w + (int64_t)row * g.ldw, row < outs_here, k + u * (64 / ES) + piece * VEC, own + u * 1024);
+            for (int j = 0; j < RB; ++j) pieces(x, g.ldx, j * 16 + row, rows_here, k, got[1 + j]);
 #pragma unroll
-            for (int j = 0; j < RB; ++j)
+            for (int j = 0; j < 1 + RB; ++j)
 #pragma unroll
-                for (int u = 0; u < U; ++u)
-                    through(x + (int64_t)(j * 16 + row) * g.ldx, j * 16 + row < rows_here, k + u * (64 / ES) + piece * VEC, own + ((1 + j) * U + u) * 1024);
+                for (int u = 0; u < U; ++u) *(u32x4*)(own + (j * U + u) * 1024 + lane * 16) = got[j][u];
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         }
         u32x4 wv[U], xv[RB][U];
@@ -260,30 +265,41 @@ struct TileCost {
     int bt, bn;
     double once, own, step;
 };
-constexpr TileCost kTiles[] = {{64, 64, 4.1, 1.0, 0.275}, {128, 128, 3.1, 1.7, 0.53}, {256, 256, 0, 6.4, 1.18}, {64, 64, 4.0, 0.4, 0.45}, {128, 128, 2.6, 2.4, 0.93}};
+constexpr TileCost kTiles[] = {{64, 64, 3.3, 1.1, 0.24}, {128, 128, 2.2, 1.95, 0.51}, {256, 256, 0, 6.6, 1.1}, {192, 192, 0, 5.6, 0.75}, {64, 64, 3.4, 0.5, 0.49}, {128, 128, 3.1, 2.1, 0.81}};
 constexpr TileCost kTilesF32[] = {{64, 64, 4.5, 0.5, 1.3}, {128, 128, 0, 6.2, 2.75}, {256, 128, 0, 8.1, 4.7}};
 
 struct ProductPlan {
     ProductForm form;
     int splits;
     double us;
+    int64_t rows;      // of the first launch; the rest, if any, by a second one
+    ProductForm rest;
+    int rest_splits;
 };
-ProductPlan plan_product(int64_t M, int64_t N, int64_t K, int dtype, bool direct)
+ProductPlan plan_product(int64_t M, int64_t N, int64_t K, int dtype, bool direct, bool whole = false)
 {
-    ProductPlan best = {P64, 1, 1e30};
+    ProductPlan best = {P64, 1, 1e30, M, P64, 1};
     const int64_t ksteps = (K + 63) / 64;
     const bool f32 = dtype == CONV_F32;
-    for (int f = f32 || direct ? P64 : P64_ANY; f <= (f32 || direct ? P256 : P128_ANY); ++f) {
+    for (int f = f32 || direct ? P64 : P64_ANY; f <= (f32 ? P256 : direct ? P192 : P128_ANY); ++f) {
         const TileCost& c = f32 ? kTilesF32[f] : kTiles[f];
-        const double tiles = (double)((M + c.bt - 1) / c.bt) * ((N + c.bn - 1) / c.bn);
+        const int64_t tm = (M + c.bt - 1) / c.bt, tn = (N + c.bn - 1) / c.bn;
+        const double tiles = (double)tm * tn;
         for (int splits = 1; splits <= 64; splits *= 2) {
             if (splits > 1 && (splits * 4 > ksteps || tiles * splits > 2048)) break;
             const int64_t each = (ksteps + splits - 1) / splits;
             const int shares = (int)((ksteps + each - 1) / each);  // none without a step
             double us = c.once + std::ceil(tiles * shares / 256) * (c.own + each * c.step);
             if (shares > 1) us += 5 + 8.0 * shares * M * N / 4e6;  // written, read and added by a second launch
-            if (us < best.us) best = {(ProductForm)f, shares, us};
+            if (us < best.us) best = {(ProductForm)f, shares, us, M, P64, 1};
         }
+        // Whole rounds of tiles, and what is left by smaller ones or with a shared reduction (50257 x 1024 x 2048: 788 tiles of 256 x 256 are
+        // three rounds and 20 tiles).
+        const int64_t rounds = (int64_t)(tiles / 256), first = rounds * 256 / tn;
+        if (whole || rounds < 1 || rounds > 16 || first < 1 || first >= tm) continue;
+        const ProductPlan rest = plan_product(M - first * c.bt, N, K, dtype, direct, true);
+        const double us = c.once + rounds * (c.own + ksteps * c.step) + rest.us;
+        if (us < best.us) best = {(ProductForm)f, 1, us, first * c.bt, rest.form, rest.splits};
     }
     return best;
 }
@@ -294,7 +310,7 @@ struct RowsPlan {
     int rb, splits;
     double us;
 };
-RowsPlan plan_rows(int64_t rows, int N, int K, int dtype)
+RowsPlan plan_rows(int64_t rows, int N, int K, int dtype, bool direct)
 {
     RowsPlan p;
     const double size = dtype_size(dtype);
@@ -302,7 +318,8 @@ RowsPlan plan_rows(int64_t rows, int N, int K, int dtype)
     const double groups = (double)((rows + 16 * p.rb - 1) / (16 * p.rb)) * ((N + 15) / 16);
     const double bytes = 16.0 * (1 + p.rb) * K * size, alone = bytes / 120e3 * std::ceil(groups / 256);
     p.splits = 1;
-    p.us = 2.8 + alone + std::max(groups * bytes / 33e6, groups / 256 * 0.16 * p.rb);
+    // (pieces that start anywhere: twice that for 64 rows, whose loads outweigh the weights')
+    p.us = 2.8 + (direct || p.rb < 4 ? 1 : 2) * (alone + std::max(groups * bytes / 33e6, groups / 256 * 0.16 * p.rb));
     if (groups <= 64) {
         const int most = std::min({16, (int)(256 / groups), (int)((K * size + 1023) / 1024)});
         if (alone - alone / most > 6) p.splits = most, p.us = 8 + alone / most;
@@ -322,7 +339,7 @@ LinearForm form_of(int64_t rows, int N, int K, int dtype, bool direct)
 {
     LinearForm f;
     f.direct = direct;
-    f.few = plan_rows(rows, N, K, dtype);
+    f.few = plan_rows(rows, N, K, dtype, direct);
     f.tiles = plan_product(rows, N, K, dtype, direct);
     f.rows = rows <= 16 || f.few.us <= f.tiles.us;
     return f;
@@ -354,7 +371,7 @@ hipError_t join(int dtype, const LinearOut& e, const float* partial, int64_t row
                              : dtype == CONV_F16 ? join_as<CONV_F16>(e, partial, rows, N, splits, s) : join_as<CONV_BF16>(e, partial, rows, N, splits, s);
 }
 
-// C = A B, and the join where a reduction is shared.
+// C = A B, in one launch or two, and the join where a reduction is shared.
 struct Factor {
     const void* p;
     int64_t ld;
@@ -366,11 +383,24 @@ hipError_t multiply(int dtype, ProductLayout layout, const Factor& a, const Fact
     g.a = (const uint16_t*)a.p, g.b = (const uint16_t*)b.p, g.lda = a.ld, g.ldb = b.ld, g.M = M, g.N = N, g.K = K, g.partial = partial;
     g.ksteps = (int)((K + 63) / 64);
     const auto launch = dtype == CONV_F32 ? launch_product_f32 : dtype == CONV_F16 ? launch_product_f16 : launch_product_bf16;
-    const hipError_t err = launch(g, e, layout, plan.form, plan.splits, s);
-    if (err != hipSuccess || plan.splits == 1) return err;
-    return join(dtype, e, partial, M, (int)N, plan.splits, s);
+    g.M = plan.rows;
+    hipError_t err = launch(g, e, layout, plan.form, plan.splits, s);
+    if (err == hipSuccess && plan.splits > 1) err = join(dtype, e, partial, g.M, (int)N, plan.splits, s);
+    if (err != hipSuccess || plan.rows == M) return err;
+    const int es = dtype_size(dtype);
+    LinearOut rest = e;
+    rest.out = (char*)e.out + plan.rows * e.ldo * es;
+    if (e.pre) rest.pre = (char*)e.pre + plan.rows * e.ldo * es;
+    if (e.residual) rest.residual = (const char*)e.residual + plan.rows * e.ldr * es;
+    g.a = (const uint16_t*)((const char*)a.p + plan.rows * (layout == LAYOUT_TN ? 1 : a.ld) * es), g.M = M - plan.rows;
+    err = launch(g, rest, layout, plan.rest, plan.rest_splits, s);
+    return err != hipSuccess || plan.rest_splits == 1 ? err : join(dtype, rest, partial, g.M, (int)N, plan.rest_splits, s);
 }
-size_t partial_bytes(const ProductPlan& p, int64_t M, int64_t N) { return p.splits > 1 ? (size_t)p.splits * M * N * 4 : 0; }
+size_t partial_bytes(const ProductPlan& p, int64_t M, int64_t N)
+{
+    const size_t first = p.splits > 1 ? (size_t)p.splits * p.rows * N * 4 : 0, rest = p.rest_splits > 1 ? (size_t)p.rest_splits * (M - p.rows) * N * 4 : 0;
+    return std::max(first, rest);
+}
 
 template <int DT, int RB, int W, int U, bool DIRECT>
 hipError_t launch_rows(const LinearRows& g, int splits, hipStream_t s)
@@ -423,8 +453,8 @@ int64_t dz_rows(int64_t rows, int N)
 }
 int dz_parts(int64_t rows, int N) { return rows == 0 ? 0 : (int)((rows + dz_rows(rows, N) - 1) / dz_rows(rows, N)); }
 
-// Rows of dz start on 16 bytes in 16-bit types.
-int64_t dz_stride(int N, int dtype) { return dtype == CONV_F32 ? N : round_up(N, 8); }
+// Rows of dz start on lines of 128 bytes in 16-bit types: a step's 128 bytes of a row would lie in two.
+int64_t dz_stride(int N, int dtype) { return dtype == CONV_F32 ? N : round_up(N, 64); }
 
 struct BwdSpace {
     void* dz;
@@ -532,7 +562,7 @@ hipError_t launch_linear_bwd(const LinearArgs& a, int dtype, hipStream_t s)
 
 int linear_form_name(const LinearArgs& a, int dtype, int which, char* buf, size_t n)
 {
-    static const char* const tiles[] = {"tile64x64", "tile128x128", "tile256x256", "tile64x64_any", "tile128x128_any"};
+    static const char* const tiles[] = {"tile64x64", "tile128x128", "tile256x256", "tile192x192", "tile64x64_any", "tile128x128_any"};
     const int es = dtype_size(dtype);
     const bool x16 = on_16(a.x, a.ldx, es), w16 = on_16(a.w, a.ldw, es);
     ProductPlan p;
@@ -548,8 +578,15 @@ int linear_form_name(const LinearArgs& a, int dtype, int which, char* buf, size_
     } else {
         p = plan_product(a.N, a.K, a.rows, dtype, x16);
     }
-    const int len = dtype == CONV_F32 ? std::snprintf(buf, n, "split_%s", p.form == P256 ? "tile256x128" : tiles[p.form]) : std::snprintf(buf, n, "%s", tiles[p.form]);
-    return p.splits > 1 && len > 0 && (size_t)len < n ? std::snprintf(buf + len, n - len, "_split%d", p.splits) : len;
+    auto one = [&](char* to, size_t room, ProductForm form, int splits) {
+        const char* const name = dtype == CONV_F32 && form == P256 ? "tile256x128" : tiles[form];
+        const char* const kind = dtype == CONV_F32 ? "split_" : "";
+        return splits > 1 ? std::snprintf(to, room, "%s%s_split%d", kind, name, splits) : std::snprintf(to, room, "%s%s", kind, name);
+    };
+    const int len = one(buf, n, p.form, p.splits);
+    if (p.rows == (which == 2 ? a.N : a.rows) || len < 0 || (size_t)len + 1 >= n) return len;
+    buf[len] = '+';
+    return len + 1 + one(buf + len + 1, n - len - 1, p.rest, p.rest_splits);
 }
 
 }  // namespace convfwd

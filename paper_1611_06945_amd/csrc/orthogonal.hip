@@ -248,7 +248,6 @@ Space space_of(const OrthogonalArgs& g, int dtype, void* ws)
 }
 
 // Tiles of one plane, and of two, whose stages are twice as large.
-typedef ProductTile<4, 2, 3, 6, 3> Tile192;
 typedef ProductTile<4, 2, 1, 2, 2, 2> Tile64Two;  // two workgroups a CU
 typedef ProductTile<2, 4, 4, 2, 2, 2> Tile128Two;
 struct TileCost {

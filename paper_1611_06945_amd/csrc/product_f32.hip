@@ -18,7 +18,7 @@ hipError_t launch_tiles(SplitArgs g, const LinearOut& e, int splits, hipStream_t
         p.M = std::min(bands * T::BT, all - skip), p.m_first = skip;
         p.a += A_ACROSS ? skip : skip * g.lda;
         p.tiles_m = (int)((p.M + T::BT - 1) / T::BT);
-        hipLaunchKernelGGL((product_f32_kernel<T, A_ACROSS, B_ACROSS, PARTIAL>), dim3((unsigned)p.tiles_m * (unsigned)p.tiles_n, 1, (unsigned)splits), dim3(T::NT), T::LDS, s,
+        hipLaunchKernelGGL((product_f32_kernel<T, A_ACROSS, B_ACROSS, PARTIAL>), dim3((unsigned)p.tiles_m * (unsigned)p.tiles_n * (unsigned)splits), dim3(T::NT), T::LDS, s,
                            p, e);
     }
     return hipGetLastError();
@@ -40,7 +40,7 @@ hipError_t launch_product_f32(const ProductArgs& g, const LinearOut& e, ProductL
 {
     SplitArgs p = {};
     p.a = (const float*)g.a, p.b = (const float*)g.b, p.lda = g.lda, p.ldb = g.ldb, p.M = g.M, p.N = g.N, p.K = g.K, p.partial = g.partial;
-    p.each = (int64_t)((g.ksteps + splits - 1) / splits) * 64;
+    p.each = (int64_t)((g.ksteps + splits - 1) / splits) * 64, p.splits = splits;
     typedef SplitTile<2, 2, 2, 2, 2, 2> Tile64;
     typedef SplitTile<2, 4, 4, 2, 1, 2> Tile128;
     typedef SplitTile<4, 2, 4, 4, 1, 2> Tile256;

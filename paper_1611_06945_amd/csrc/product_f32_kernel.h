@@ -82,8 +82,8 @@ struct SplitArgs {
     const float *a, *b;
     int64_t lda, ldb;
     int64_t M, N, K, m_first;
-    int64_t each;              // of the reduction, of a workgroup that shares it with others (gridDim.z): a multiple of the step
-    int tiles_m, tiles_n;
+    int64_t each;              // of the reduction, of each of the workgroups that share it: a multiple of the step
+    int tiles_m, tiles_n, splits;
     float* partial;
 };
 
@@ -93,10 +93,11 @@ __global__ __launch_bounds__(T::NT) void product_f32_kernel(SplitArgs g, LinearO
     extern __shared__ __attribute__((aligned(16))) char smem[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wt = wave % T::WT, wn = wave / T::WT;
-    int tm, tn;
-    tile_of_block(g.tiles_m, g.tiles_n, tm, tn);
+    int tile, tm, tn;
+    const int share = share_of_block(g.splits, tile);
+    place_of_tile(tile, g.tiles_m, g.tiles_n, tm, tn);
     const int64_t m0 = (int64_t)tm * T::BT, n0 = (int64_t)tn * T::BN;
-    const int64_t k0 = blockIdx.z * g.each, k1 = min(k0 + g.each, g.K);
+    const int64_t k0 = share * g.each, k1 = min(k0 + g.each, g.K);
 
     SplitOperand<T, T::BT, T::LA, A_ACROSS> a;
     SplitOperand<T, T::BN, T::LB, B_ACROSS> b;
@@ -179,7 +180,7 @@ __global__ __launch_bounds__(T::NT) void product_f32_kernel(SplitArgs g, LinearO
             if (ml < a.pieces.here && nl < b.pieces.here) {
                 const int have = min(8, b.pieces.here - nl);
                 const int64_t m = g.m_first + m0 + ml;
-                if constexpr (PARTIAL) put8<CONV_F32>(g.partial, ((int64_t)blockIdx.z * g.M + m) * g.N + n0 + nl, v, have);
+                if constexpr (PARTIAL) put8<CONV_F32>(g.partial, ((int64_t)share * g.M + m) * g.N + n0 + nl, v, have);
                 else LinearEpi<CONV_F32>::finish(ProductArgs(), e, v, m, n0 + nl, have, bias + nl);
             }
         }

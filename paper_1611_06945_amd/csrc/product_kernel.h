@@ -267,10 +267,10 @@ struct ProductArgs {
     int64_t plane_a, plane_b;     // distance of an operand's planes
     int64_t M, N, K;
     int64_t m_first;              // what the first row of these M is in the whole product
-    int ksteps, each;             // steps of the reduction, and of a workgroup that shares it with others (gridDim.z)
+    int ksteps, each, splits;     // steps of the reduction, and of each of the workgroups that share it
     int64_t batch_a, batch_b;     // distances of the batch's matrices (gridDim.y)
     int tiles_m, tiles_n;
-    float* partial;               // sums of gridDim.z workgroups, [z][M][N]
+    float* partial;               // sums of the workgroups that share a reduction, [splits][M][N]
 };
 
 // Consecutive workgroups go to different XCDs: each XCD takes a run of tiles.
@@ -279,18 +279,27 @@ __device__ __forceinline__ int tile_in_order()
     const int total = gridDim.x, q = total / 8, r = total % 8, x = blockIdx.x % 8, i = blockIdx.x / 8;
     return x * q + min(x, r) + i;
 }
-// ... in bands of eight tiles of n
-__device__ __forceinline__ void tile_of_block(int tiles_m, int tiles_n, int& tm, int& tn)
+// Where `splits` workgroups share a tile's reduction, consecutive workgroups take different shares of it, so that an XCD has all tiles of its
+// shares and reads only those parts of the operands (2048 x 1024 x 50257 in shares of 8: 260 us with the tiles dealt to the XCDs).
+__device__ __forceinline__ int share_of_block(int splits, int& tile)
 {
-    const int tile = tile_in_order();
+    if (splits == 1) {
+        tile = tile_in_order();
+        return 0;
+    }
+    tile = blockIdx.x / splits;
+    return blockIdx.x % splits;
+}
+// ... in bands of eight tiles of n
+__device__ __forceinline__ void place_of_tile(int tile, int tiles_m, int tiles_n, int& tm, int& tn)
+{
     const int band = tile / (8 * tiles_m), in_band = tile - band * 8 * tiles_m;
     const int width = min(8, tiles_n - band * 8);
     tn = band * 8 + in_band % width, tm = in_band / width;
 }
 // ... of those with n >= m only: row tm has the tiles tm .. tiles - 1
-__device__ __forceinline__ void tile_above_diagonal(int tiles, int& tm, int& tn)
+__device__ __forceinline__ void tile_above_diagonal(int tile, int tiles, int& tm, int& tn)
 {
-    int tile = tile_in_order();
     tm = 0;
     for (int left = tiles; tile >= left; --left) tile -= left, ++tm;
     tn = tm + tile;
@@ -317,11 +326,12 @@ __global__ __launch_bounds__(T::NT) void product_kernel(ProductArgs g, typename 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wt = wave % T::WT, wn = wave / T::WT;
 
-    int tm, tn;
-    if constexpr (Epi::SYMMETRIC) tile_above_diagonal(g.tiles_m, tm, tn);
-    else tile_of_block(g.tiles_m, g.tiles_n, tm, tn);
+    int tile, tm, tn;
+    const int share = share_of_block(g.splits, tile);
+    if constexpr (Epi::SYMMETRIC) tile_above_diagonal(tile, g.tiles_m, tm, tn);
+    else place_of_tile(tile, g.tiles_m, g.tiles_n, tm, tn);
     const int64_t m0 = (int64_t)tm * T::BT, n0 = (int64_t)tn * T::BN;
-    const int ks0 = blockIdx.z * g.each, ks1 = min(ks0 + g.each, g.ksteps);
+    const int ks0 = share * g.each, ks1 = min(ks0 + g.each, g.ksteps);
 
     Operand<T, T::BT, T::LA, A_ACROSS, DIRECT> a;
     Operand<T, T::BN, T::LW, B_ACROSS, DIRECT> b;
@@ -488,7 +498,7 @@ struct PartialSums {
     static __device__ __forceinline__ void prepare(const Args&, float*, int64_t, int, int, int) {}
     static __device__ __forceinline__ void finish(const ProductArgs& g, const Args&, const float (&v)[8], int64_t m, int64_t n, int have, const float*)
     {
-        put8<CONV_F32>(g.partial, ((int64_t)blockIdx.z * g.M + m) * g.N + n, v, have);
+        put8<CONV_F32>(g.partial, ((int64_t)(blockIdx.x % g.splits) * g.M + m) * g.N + n, v, have);
     }
 };
 
