@@ -7,26 +7,31 @@ namespace convfwd {
 
 enum { ACT_NONE = 0, ACT_RELU = 1, ACT_GELU = 2, ACT_SILU = 3 };
 
-// The normal distribution Phi(z) and exp(-z^2 / 2), by the rational approximation 7.1.26 of Abramowitz and Stegun's handbook, which is off by
-// 1.5e-7 / 2 at most; erff() takes four times the instructions, 8 us of the 44 of 3380 x 384 x 1536.
-__device__ __forceinline__ float normal_distribution(float z, float& bell)
+// Phi(-|z|), Phi the normal distribution, by the rational approximation 7.1.26 of Abramowitz and Stegun's handbook, which is off by 1.5e-7 / 2 at
+// most (erff() takes four times the instructions), and exp(-z^2 / 2).  What a tile's 65536 activations cost is a part of its time: 10 us of the 115 of a
+// tile of 8192 x 4096 x 8192 with another form of this, so divisions are reciprocals (off by a unit in the last place).
+__device__ __forceinline__ float normal_tail(float z, float& bell)
 {
-    const float x = fabsf(z) * 0.70710678118654752f, t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.3275911f, x, 1.0f));
-    bell = __expf(-x * x);
-    float p = __builtin_fmaf(1.061405429f, t, -1.453152027f);
-    p = __builtin_fmaf(p, t, 1.421413741f);
-    p = __builtin_fmaf(p, t, -0.284496736f);
-    p = __builtin_fmaf(p, t, 0.254829592f);
-    const float tail = 0.5f * p * t * bell;  // Phi(-|z|)
-    return z < 0.0f ? tail : 1.0f - tail;
+    const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.3275911f * 0.70710678118654752f, fabsf(z), 1.0f));
+    bell = __builtin_amdgcn_exp2f(z * z * (-0.5f * 1.44269504088896341f));
+    float p = __builtin_fmaf(0.5f * 1.061405429f, t, 0.5f * -1.453152027f);
+    p = __builtin_fmaf(p, t, 0.5f * 1.421413741f);
+    p = __builtin_fmaf(p, t, 0.5f * -0.284496736f);
+    p = __builtin_fmaf(p, t, 0.5f * 0.254829592f);
+    return p * t * bell;
 }
+// 1 / (1 + exp(-z))
+__device__ __forceinline__ float logistic(float z) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(z * -1.44269504088896341f)); }
 
 __device__ __forceinline__ float act_of(float z, int act)
 {
-    float bell;
     if (act == ACT_RELU) return z < 0.0f ? 0.0f : z;  // a NaN stays
-    if (act == ACT_GELU) return z * normal_distribution(z, bell);
-    if (act == ACT_SILU) return z / (1.0f + __expf(-z));
+    if (act == ACT_GELU) {
+        float bell;
+        const float tail = normal_tail(z, bell);
+        return __builtin_fmaf(-fabsf(z), tail, z < 0.0f ? 0.0f : z);  // z Phi(z) = max(z, 0) - |z| Phi(-|z|)
+    }
+    if (act == ACT_SILU) return z * logistic(z);
     return z;
 }
 // its derivative; 0 at the corner of ReLU
@@ -35,12 +40,12 @@ __device__ __forceinline__ float act_slope(float z, int act)
     if (act == ACT_RELU) return z > 0.0f ? 1.0f : z <= 0.0f ? 0.0f : z;
     if (act == ACT_GELU) {
         float bell;
-        const float phi = normal_distribution(z, bell);
-        return __builtin_fmaf(z * bell, 0.39894228040143268f, phi);
+        const float tail = normal_tail(z, bell);
+        return __builtin_fmaf(z * bell, 0.39894228040143268f, z < 0.0f ? tail : 1.0f - tail);
     }
     if (act == ACT_SILU) {
-        const float p = 1.0f / (1.0f + __expf(-z));
-        return p * (1.0f + z * (1.0f - p));
+        const float p = logistic(z);
+        return p * __builtin_fmaf(z, 1.0f - p, 1.0f);
     }
     return 1.0f;
 }
