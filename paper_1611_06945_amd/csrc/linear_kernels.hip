@@ -69,7 +69,7 @@ template <int DT, int RB, int W, int U, bool DIRECT>
 __global__ __launch_bounds__(64 * W) void linear_rows(LinearRows g)
 {
     typedef typename Prec<DT>::elem_t elem_t;
-    constexpr int NT = 64 * W, ES = sizeof(elem_t), VEC = 16 / ES, RUN = 64 * U / ES, OWN = (1 + RB) * U * 1024;
+    constexpr int NT = 64 * W, ES = sizeof(elem_t), VEC = 16 / ES, RUN = 64 * U / ES, SLOT = (1 + RB) * U * 1024, OWN = (DIRECT ? 2 : 1) * SLOT;
     extern __shared__ __attribute__((aligned(16))) char smem[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n0 = blockIdx.x * 16;
@@ -78,7 +78,7 @@ __global__ __launch_bounds__(64 * W) void linear_rows(LinearRows g)
     const elem_t *const x = (const elem_t*)g.x + t0 * g.ldx, *const w = (const elem_t*)g.w + (int64_t)n0 * g.ldw;
     const int row = lane >> 2, piece = (lane & 3) ^ ((row >> 2) & 3);
     char* const own = smem + wave * OWN;
-    const char* const mine = own + (lane & 15) * 64 + (((lane >> 4) ^ ((lane >> 2) & 3)) << 4);
+    const int mine = (lane & 15) * 64 + (((lane >> 4) ^ ((lane >> 2) & 3)) << 4);
     // (whole pieces: rows start on 16 bytes, so what the last one holds past the end lies in the same 16 bytes as an element)
     const __amdgpu_buffer_rsrc_t rx = make_rsrc(x, DIRECT ? (uint32_t)(((rows_here - 1) * g.ldx + g.K) * ES + 15) & ~15u : 0u);
     const __amdgpu_buffer_rsrc_t rw = make_rsrc(w, DIRECT ? (uint32_t)(((outs_here - 1) * g.ldw + g.K) * ES + 15) & ~15u : 0u);
@@ -106,20 +106,31 @@ __global__ __launch_bounds__(64 * W) void linear_rows(LinearRows g)
     f32x4 acc[RB];
 #pragma unroll
     for (int j = 0; j < RB; ++j) acc[j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    for (int k = (blockIdx.z * W + wave) * RUN; k < g.K; k += gridDim.z * W * RUN) {
-        if constexpr (DIRECT) {
+    // DIRECT: a run's loads, into one of two places
+    auto ask = [&](int k, char* slot) {
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rw, (lds_void_t*)(slot + u * 1024), 16, (int)(woff + (uint32_t)k * ES + u * 64), 0, 0, 0);
+#pragma unroll
+        for (int j = 0; j < RB; ++j)
 #pragma unroll
             for (int u = 0; u < U; ++u)
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(rw, (lds_void_t*)(own + u * 1024), 16, (int)(woff + (uint32_t)k * ES + u * 64), 0, 0, 0);
-#pragma unroll
-            for (int j = 0; j < RB; ++j)
-#pragma unroll
-                for (int u = 0; u < U; ++u)
-                    __builtin_amdgcn_raw_ptr_buffer_load_lds(rx, (lds_void_t*)(own + ((1 + j) * U + u) * 1024), 16,
-                                                             (int)(xoff + (uint32_t)(j * 16) * (uint32_t)(g.ldx * ES) + (uint32_t)k * ES + u * 64), 0, 0, 0);
-            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(rx, (lds_void_t*)(slot + ((1 + j) * U + u) * 1024), 16,
+                                                         (int)(xoff + (uint32_t)(j * 16) * (uint32_t)(g.ldx * ES) + (uint32_t)k * ES + u * 64), 0, 0, 0);
+    };
+    const int first = (blockIdx.z * W + wave) * RUN, step = gridDim.z * W * RUN;
+    char* slot = own;
+    if (DIRECT && first < g.K) ask(first, slot);
+    for (int k = first; k < g.K; k += step) {
+        if constexpr (DIRECT) {
+            if (k + step < g.K) {
+                ask(k + step, slot == own ? own + SLOT : own);
+                asm volatile("s_waitcnt vmcnt(%0)" ::"n"((1 + RB) * U) : "memory");
+            } else {
+                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            }
         } else {
-u32x4 got[1 + RB][U];
+            u32x4 got[1 + RB][U];
             pieces(w, g.ldw, row, outs_here, k, got[0]);
 #pragma unroll
             for (int j = 0; j < RB; ++j) pieces(x, g.ldx, j * 16 + row, rows_here, k, got[1 + j]);
@@ -131,12 +142,13 @@ u32x4 got[1 + RB][U];
         }
         u32x4 wv[U], xv[RB][U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) wv[u] = *(const u32x4*)(mine + u * 1024);
+        for (int u = 0; u < U; ++u) wv[u] = *(const u32x4*)(slot + mine + u * 1024);
 #pragma unroll
         for (int j = 0; j < RB; ++j)
 #pragma unroll
-            for (int u = 0; u < U; ++u) xv[j][u] = *(const u32x4*)(mine + ((1 + j) * U + u) * 1024);
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // read before the next run's loads may land
+            for (int u = 0; u < U; ++u) xv[j][u] = *(const u32x4*)(slot + mine + ((1 + j) * U + u) * 1024);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // read before the next but one run's loads may land
+        if (DIRECT) slot = slot == own ? own + SLOT : own;
         if (DIRECT && k + RUN > g.K) {
             // what follows a row's end is another row's, or nobody's
 #pragma unroll
@@ -405,7 +417,7 @@ size_t partial_bytes(const ProductPlan& p, int64_t M, int64_t N)
 template <int DT, int RB, int W, int U, bool DIRECT>
 hipError_t launch_rows(const LinearRows& g, int splits, hipStream_t s)
 {
-    constexpr size_t LDS = (size_t)W * (1 + RB) * U * 1024;
+    constexpr size_t LDS = (size_t)W * (1 + RB) * U * 1024 * (DIRECT ? 2 : 1);
     const hipError_t e = ensure_dynamic_lds((const void*)linear_rows<DT, RB, W, U, DIRECT>, LDS);
     if (e != hipSuccess) return e;
     // gridDim.y is at most 65535, and a launch holds less than 2^32 threads: the rows go in portions
@@ -432,9 +444,9 @@ hipError_t launch_rows(const LinearRows& g, const RowsPlan& p, hipStream_t s)
 {
     const bool narrow = (int64_t)g.K * (int)sizeof(typename Prec<DT>::elem_t) <= 1024;
     switch (p.rb) {
-        case 1: return narrow ? launch_rows<DT, 1, 4, 4, DIRECT>(g, p.splits, s) : launch_rows<DT, 1, 8, 4, DIRECT>(g, p.splits, s);
+        case 1: return narrow ? launch_rows<DT, 1, 4, 2, DIRECT>(g, p.splits, s) : launch_rows<DT, 1, 8, 2, DIRECT>(g, p.splits, s);
         case 2: return narrow ? launch_rows<DT, 2, 4, 2, DIRECT>(g, p.splits, s) : launch_rows<DT, 2, 8, 2, DIRECT>(g, p.splits, s);
-        default: return narrow ? launch_rows<DT, 4, 4, 2, DIRECT>(g, p.splits, s) : launch_rows<DT, 4, 8, 2, DIRECT>(g, p.splits, s);
+        default: return narrow || DIRECT ? launch_rows<DT, 4, 4, 2, DIRECT>(g, p.splits, s) : launch_rows<DT, 4, 8, 2, DIRECT>(g, p.splits, s);
     }
 }
 template <int DT>
