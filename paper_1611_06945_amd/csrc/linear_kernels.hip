@@ -438,14 +438,22 @@ hipError_t launch_rows(const LinearRows& g, int splits, hipStream_t s)
     }
     return hipGetLastError();
 }
-// Waves a workgroup: a wave has a run of 256 bytes or more up to 1024 and 2048 bytes.
+// Waves a workgroup, and 64-byte pieces of a row in a run: what is on its way to a CU is what counts, and LDS holds it.  Long rows: 8 waves, with runs of 256
+// bytes where there is about a workgroup a CU (1 x 4096 x 4096 fp16, weights from memory 8.7 -> 8.2 us), else of 128 in two workgroups.  12 waves for 32
+// rows were no better (24 x 6752 x 46704 fp32 329 us with 8, 337).
 template <int DT, bool DIRECT>
 hipError_t launch_rows(const LinearRows& g, const RowsPlan& p, hipStream_t s)
 {
-    const bool narrow = (int64_t)g.K * (int)sizeof(typename Prec<DT>::elem_t) <= 1024;
+    const int64_t bytes = (int64_t)g.K * (int)sizeof(typename Prec<DT>::elem_t);
+    const bool narrow = bytes <= 1024, alone = (int64_t)(g.N + 15) / 16 * p.splits <= 384 && bytes >= 4096;
     switch (p.rb) {
-        case 1: return narrow ? launch_rows<DT, 1, 4, 2, DIRECT>(g, p.splits, s) : launch_rows<DT, 1, 8, 2, DIRECT>(g, p.splits, s);
-        case 2: return narrow ? launch_rows<DT, 2, 4, 2, DIRECT>(g, p.splits, s) : launch_rows<DT, 2, 8, 2, DIRECT>(g, p.splits, s);
+        case 1:
+            if constexpr (DIRECT) {
+                if (alone) return launch_rows<DT, 1, 8, 4, DIRECT>(g, p.splits, s);
+            }
+            return narrow ? launch_rows<DT, 1, 4, 2, DIRECT>(g, p.splits, s) : launch_rows<DT, 1, 8, 2, DIRECT>(g, p.splits, s);
+        case 2:
+            return narrow ? launch_rows<DT, 2, 4, 2, DIRECT>(g, p.splits, s) : launch_rows<DT, 2, 8, 2, DIRECT>(g, p.splits, s);
         default: return narrow || DIRECT ? launch_rows<DT, 4, 4, 2, DIRECT>(g, p.splits, s) : launch_rows<DT, 4, 8, 2, DIRECT>(g, p.splits, s);
     }
 }
