@@ -508,7 +508,7 @@ int linear_form(const linear_desc* desc, const void* x, const void* w, int which
  * gamma, beta: fp32 [cols], NULL = ones, zeros, ones, ones, zeros.  y may be NULL (no norm behind).  stats: fp32 [rows][4], 16-byte aligned,
  * receives mean and rstd of h and mean and rstd of the sum (0 and 1 where there is no norm, 0 for means under RMS); may be NULL.
  * r_out may be r.  Row strides: ldr of r, r_out, dr, dr_out; ldh of h, dh; ldg of gate, dgate; ldy of y, dy.
- * CONV_EINVAL for rows or gate_rows < 0, cols < 1 or >= 2^30, strides below cols (ldg only with a gate), eps < 0, infinite or NaN, unknown flags, a gate without gate_rows
+ * CONV_EINVAL for rows or gate_rows < 0, cols < 1 or >= 2^27, strides below cols (ldg only with a gate), eps < 0, infinite or NaN, unknown flags, a gate without gate_rows
  * or the reverse, NULL or misaligned pointers, other outputs that are inputs.
  */
 #define RESIDUAL_NORM_RMS 1u

@@ -23,15 +23,16 @@ __device__ __forceinline__ float normal_tail(float z, float& bell)
 // 1 / (1 + exp(-z))
 __device__ __forceinline__ float logistic(float z) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(z * -1.44269504088896341f)); }
 
+// (Factors z beside a tail are clamped where the tail has vanished already: infinities give the limits, where they would give infinity times zero.)
 __device__ __forceinline__ float act_of(float z, int act)
 {
     if (act == ACT_RELU) return z < 0.0f ? 0.0f : z;  // a NaN stays
     if (act == ACT_GELU) {
         float bell;
         const float tail = normal_tail(z, bell);
-        return __builtin_fmaf(-fabsf(z), tail, z < 0.0f ? 0.0f : z);  // z Phi(z) = max(z, 0) - |z| Phi(-|z|)
+        return __builtin_fmaf(-fminf(fabsf(z), 16.0f), tail, z < 0.0f ? 0.0f : z);  // z Phi(z) = max(z, 0) - |z| Phi(-|z|)
     }
-    if (act == ACT_SILU) return z * logistic(z);
+    if (act == ACT_SILU) return fmaxf(z, -128.0f) * logistic(z);
     return z;
 }
 // its derivative; 0 at the corner of ReLU
@@ -41,11 +42,11 @@ __device__ __forceinline__ float act_slope(float z, int act)
     if (act == ACT_GELU) {
         float bell;
         const float tail = normal_tail(z, bell);
-        return __builtin_fmaf(z * bell, 0.39894228040143268f, z < 0.0f ? tail : 1.0f - tail);
+        return __builtin_fmaf(__builtin_amdgcn_fmed3f(z, -16.0f, 16.0f) * bell, 0.39894228040143268f, z < 0.0f ? tail : 1.0f - tail);
     }
     if (act == ACT_SILU) {
         const float p = logistic(z);
-        return p * __builtin_fmaf(z, 1.0f - p, 1.0f);
+        return p * __builtin_fmaf(__builtin_amdgcn_fmed3f(z, -128.0f, 128.0f), 1.0f - p, 1.0f);
     }
     return 1.0f;
 }
@@ -104,7 +105,6 @@ hipError_t launch_product_f16(const ProductArgs& g, const LinearOut& e, ProductL
 hipError_t launch_product_bf16(const ProductArgs& g, const LinearOut& e, ProductLayout layout, ProductForm form, int splits, hipStream_t s);
 hipError_t launch_product_f32(const ProductArgs& g, const LinearOut& e, ProductLayout layout, ProductForm form, int splits, hipStream_t s);
 
-// (DT: of the operands, ODT: of the result)
 template <int DT, typename T, bool A_ACROSS, bool B_ACROSS, bool DIRECT, typename Epi>
 hipError_t launch_product_tiles(ProductArgs g, const typename Epi::Args& e, int batch, int splits, hipStream_t s)
 {
@@ -113,8 +113,8 @@ hipError_t launch_product_tiles(ProductArgs g, const typename Epi::Args& e, int 
     if (err != hipSuccess) return err;
     g.tiles_n = (int)((g.N + T::BN - 1) / T::BN);
     g.each = (g.ksteps + splits - 1) / splits, g.splits = splits;
-    // a launch holds less than 2^32 threads: the rows go in portions of so many tiles
-    const int64_t all = g.M, bands = std::max<int64_t>(1, (1 << 21) / ((int64_t)g.tiles_n * batch * splits));
+    // a launch holds less than 2^32 threads: the rows go in portions of so many tiles (the triangle of a symmetric product, of a side up to 2^17, in one)
+    const int64_t all = g.M, bands = Epi::SYMMETRIC ? g.tiles_n : std::max<int64_t>(1, (1 << 21) / ((int64_t)g.tiles_n * batch * splits));
     for (int64_t skip = 0; skip < all; skip += bands * T::BT) {
         ProductArgs p = g;
         p.M = std::min(bands * T::BT, all - skip), p.m_first = skip;

@@ -79,7 +79,7 @@ int check_residual_norm(const residual_norm_desc* d)
 {
     if (!d) return CONV_EINVAL;
     if (!known(d->dtype)) return CONV_EDTYPE;
-    if (d->rows < 0 || d->rows > kMostRows || d->cols < 1 || d->cols >= (1 << 30) || d->gate_rows < 0) return CONV_EINVAL;
+    if (d->rows < 0 || d->rows > kMostRows || d->cols < 1 || d->cols >= (1 << 27) || d->gate_rows < 0) return CONV_EINVAL;
     const int es = dtype_size(d->dtype);
     for (const int64_t ld : {d->ldr, d->ldh, d->ldy})
         if (ld < d->cols || !spans(d->rows, ld, es)) return CONV_EINVAL;
@@ -316,7 +316,7 @@ int linear_fwd(const linear_desc* desc, const void* x, const void* w, const floa
     if (desc->rows == 0) return CONV_OK;
     const int es = dtype_size(desc->dtype);
     if (!x || !w || !out || !aligned(x, es) || !aligned(w, es) || !aligned(out, es) || !aligned(residual, es) || !aligned(pre, es) || !vec_ok(bias)) return CONV_EINVAL;
-    if (out == x || out == w || pre == x || pre == w || pre == out || (pre && pre == residual) || (residual == out && desc->ldr != desc->ldo)) return CONV_EINVAL;
+    if (overlaps({out, pre}, {x, w, bias}) || (pre && pre == residual) || (residual == out && desc->ldr != desc->ldo)) return CONV_EINVAL;
     const size_t need = linear_fwd_workspace(desc->rows, desc->N, desc->K, desc->dtype);
     if (need && (!workspace || workspace_bytes < need)) return CONV_EWORKSPACE;
     if (!aligned(workspace, 16)) return CONV_EINVAL;
@@ -341,7 +341,7 @@ int linear_bwd(const linear_desc* desc, const void* x, const void* w, const void
     if (!aligned(x, es) || !aligned(w, es) || !aligned(pre, es) || !aligned(dout, es) || !aligned(dx, es) || !aligned(dw, es) || !vec_ok(dbias)) return CONV_EINVAL;
     if (desc->rows > 0) {
         if (!dout || (dw && !x) || (dx && !w) || (a.act && !pre)) return CONV_EINVAL;
-        if ((dx && (dx == x || dx == w || dx == pre || dx == dout || dx == dw)) || (dw && (dw == x || dw == w || dw == pre || dw == dout))) return CONV_EINVAL;
+        if (overlaps({dx, dw, dbias}, {x, w, pre, dout})) return CONV_EINVAL;
         const size_t need = linear_bwd_workspace(desc->rows, desc->N, desc->K, desc->dtype);
         if (need && (!workspace || workspace_bytes < need)) return CONV_EWORKSPACE;
         if (!aligned(workspace, 16)) return CONV_EINVAL;
@@ -376,7 +376,7 @@ int residual_norm_fwd(const residual_norm_desc* desc, const void* r, const void*
     if (!a.post && (gamma_h || beta_h)) return CONV_EINVAL;
     if (desc->rows == 0) return CONV_OK;
     if (!r || !h || !r_out || (gate != nullptr) != (desc->gate_rows > 0)) return CONV_EINVAL;
-    if (overlaps({r_out, y, stats}, {h, gate}) || y == r || (const void*)stats == r) return CONV_EINVAL;
+    if (overlaps({r_out, y, stats}, {h, gate, gamma_h, beta_h, scale, gamma, beta}) || y == r || (const void*)stats == r) return CONV_EINVAL;
     a.r = r, a.h = h, a.gate = gate, a.gamma_h = gamma_h, a.beta_h = beta_h, a.scale = scale, a.gamma = gamma, a.beta = beta;
     a.r_out = r_out, a.y = y, a.stats_out = stats;
     return guarded("residual_norm_fwd", [&] { return launch_residual_norm_fwd(a, desc->dtype, (hipStream_t)stream); });

@@ -57,6 +57,7 @@ def test_linear_pointers_that_are_refused():
     assert fwd(d, bias=P + 2) == B.CONV_EINVAL
     assert fwd(d, out=P) == B.CONV_EINVAL and fwd(d, out=2 * P) == B.CONV_EINVAL and fwd(d, pre=4 * P) == B.CONV_EINVAL
     assert fwd(d, pre=P) == B.CONV_EINVAL and fwd(d, pre=2 * P) == B.CONV_EINVAL and fwd(d, pre=3 * P) == B.CONV_EINVAL
+    assert fwd(d, bias=4 * P) == B.CONV_EINVAL
     d.ldr = 9
     assert fwd(d, residual=4 * P) == B.CONV_EINVAL  # over the residual, other strides
     assert B.lib().linear_fwd(None, P, P, P, P, P, P, P, 0, None) == B.CONV_EINVAL
@@ -74,7 +75,7 @@ def test_linear_bwd_pointers_that_are_refused():
     assert bwd(d, dbias=P + 2) == B.CONV_EINVAL
     for taken in (P, 2 * P, 3 * P, 4 * P):
         assert bwd(d, dx=taken) == B.CONV_EINVAL and bwd(d, dw=taken) == B.CONV_EINVAL
-    assert bwd(d, dx=6 * P) == B.CONV_EINVAL
+    assert bwd(d, dx=6 * P) == B.CONV_EINVAL and bwd(d, dbias=6 * P) == B.CONV_EINVAL and bwd(d, dbias=4 * P) == B.CONV_EINVAL
     assert B.lib().linear_bwd(None, P, P, P, P, P, P, P, P, 0, None) == B.CONV_EINVAL
 
 
@@ -134,14 +135,14 @@ def nbwd(d, r_out=P, h=2 * P, gate=3 * P, gamma_h=P + 64, beta_h=P + 64, scale=P
                   ws, n, stream=0)
 
 
-@pytest.mark.parametrize("change", [dict(rows=-1), dict(rows=1 << 31), dict(cols=0), dict(cols=1 << 30), dict(ldr=7), dict(ldh=7), dict(ldy=7), dict(ldg=7), dict(gate_rows=-1),
+@pytest.mark.parametrize("change", [dict(rows=-1), dict(rows=1 << 31), dict(cols=0), dict(cols=1 << 27), dict(ldr=7), dict(ldh=7), dict(ldy=7), dict(ldg=7), dict(gate_rows=-1),
                                     dict(eps=-1.0), dict(eps=float("nan")), dict(eps=float("inf")), dict(flags=8), dict(ldr=1 << 62), dict(ldg=1 << 62)])
 def test_residual_norm_descriptors_that_are_refused(change):
     d = B.make_residual_norm_desc(4, 8, B.CONV_BF16, gate_rows=2)
     for k, v in change.items():
         setattr(d, k, v)
-    if change == dict(cols=1 << 30):
-        d.ldr = d.ldh = d.ldy = d.ldg = 1 << 30
+    if change == dict(cols=1 << 27):
+        d.ldr = d.ldh = d.ldy = d.ldg = 1 << 27
     assert nfwd(d) == B.CONV_EINVAL and nbwd(d) == B.CONV_EINVAL
     assert B.residual_norm_bwd_workspace_bytes(d) == 0
 

@@ -143,3 +143,153 @@ def test_strides_and_starts(dtype, pad, start):
 def test_gradients_that_are_asked_for(dtype, want):
     for act, pad in (("none", 0), ("none", 3), ("gelu", 0)):
         check_bwd(150, 72, 136, dtype, act, pad=(0, 0, pad), want=want)
+
+
+# (which product, rows, N, K, elements the first operand starts at) -> the form that has to be taken
+FORMS = {
+    "rows16": (0, 9, 40, 200, 0), "rows16_any": (0, 9, 41, 201, 1), "rows32": (0, 21, 40, 136, 0), "rows32_any": (0, 21, 41, 135, 1), "rows64": (0, 45, 72, 200, 0),
+    "rows64_any": (0, 45, 73, 201, 1), "rows32_split16": (0, 20, 8, 9000, 0), "rows32_any_split16": (0, 20, 8, 9000, 1), "rows64_split16": (0, 40, 8, 9000, 0),
+    "rows64_any_split12": (0, 130, 100, 9000, 1),
+}
+FORMS16 = {
+    "tile64x64": (0, 700, 1032, 40, 0), "tile128x128": (0, 1000, 1032, 72, 0), "tile192x192": (0, 2000, 2056, 136, 0), "tile256x256": (0, 3000, 3080, 72, 0),
+    "tile64x64_any": (0, 520, 640, 40, 1), "tile128x128_any": (0, 2000, 1032, 72, 1), "tile256x256+tile128x128": (0, 5200, 3080, 40, 0),
+    "tile256x256+tile192x192": (0, 5200, 4104, 24, 0), "tile64x64_any_split13": (0, 40, 8, 4104, 1), "tile128x128_split16": (0, 700, 136, 9000, 0),
+    "tile128x128_any_split7": (0, 130, 1400, 2056, 1),
+    "1 tile64x64": (1, 30, 40, 24, 0), "1 tile128x128": (1, 1000, 40, 1032, 0), "1 tile192x192": (1, 2000, 72, 2056, 0), "1 tile256x256": (1, 2600, 40, 4104, 0),
+    "1 tile256x256+tile128x128": (1, 4100, 40, 4104, 0), "1 tile128x128_any": (1, 2000, 40, 1032, 1), "1 tile64x64_any_split13": (1, 3, 4104, 16, 1),
+    "1 tile128x128_split13": (1, 1, 4104, 2056, 0), "2 tile64x64": (2, 40, 24, 72, 0), "2 tile128x128": (2, 40, 1000, 1032, 0), "2 tile192x192": (2, 72, 2056, 2056, 0),
+    "2 tile256x256": (2, 40, 3080, 4104, 0), "2 tile256x256+tile128x128": (2, 40, 4104, 4104, 0), "2 tile128x128_any": (2, 40, 1000, 2056, 1),
+    "2 tile64x64_any_split13": (2, 4100, 8, 16, 1), "2 tile128x128_split13": (2, 4100, 8, 2056, 0),
+}
+FORMS32 = {
+    "split_tile64x64": (0, 700, 1000, 40, 1), "split_tile128x128": (0, 2000, 1032, 72, 1), "split_tile256x128": (0, 3000, 2056, 136, 0),
+    "split_tile256x128+split_tile128x128": (0, 2600, 4104, 40, 0), "split_tile256x128+split_tile64x64": (0, 4100, 2056, 24, 1),
+    "1 split_tile64x64": (1, 30, 40, 24, 1), "1 split_tile128x128": (1, 2000, 40, 1032, 0), "1 split_tile256x128": (1, 2000, 72, 2056, 0),
+    "1 split_tile256x128+split_tile128x128": (1, 2600, 40, 4104, 1), "2 split_tile64x64": (2, 40, 24, 72, 0), "2 split_tile128x128": (2, 40, 1000, 2056, 1),
+    "2 split_tile256x128": (2, 40, 2056, 2056, 0), "2 split_tile256x128+split_tile64x64": (2, 40, 4104, 2056, 0),
+}
+
+
+@pytest.mark.parametrize("dtype,name", [(t, n) for t in DTYPES for n in {**FORMS, **(FORMS32 if t == wl.F32 else FORMS16)} if (t, n) != (wl.F32, "rows64_any_split12")])
+def test_every_form(dtype, name):
+    which, rows, N, K, start = {**FORMS, **FORMS16, **FORMS32}[name]
+    pad = -K % 8
+    if which == 0:
+        assert check_fwd(rows, N, K, dtype, "relu", residual=True, pre=True, inplace=True, pad=(pad, pad, -N % 8, -N % 8), start=start) == name
+    else:
+        got = check_bwd(rows, N, K, dtype, "relu", pad=(pad, pad, -N % 8), start=start, want=("dx",) if which == 1 else ("dw",))
+        assert got[which - 1] == name.split()[1]
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_infinities_at_activations_give_the_limits(dtype):
+    """A large sum rounds to an infinity in fp16: the slope there is the limit."""
+    torch = torch_mod()
+    inf, nan = float("inf"), float("nan")
+    z = np.array([inf, -inf, nan, 0.0, -0.0, 1e4, -1e4, 100.0, -100.0, 17.0, -17.0, 15.0, -15.0, 3.0, -3.0, 6e4], dtype=np.float32)
+    n = len(z)
+    limits = {"relu": ([inf, 0.0], [1.0, 0.0]), "gelu": ([inf, 0.0], [1.0, 0.0]), "silu": ([inf, 0.0], [1.0, 0.0])}
+    tt = torch_type(dtype)
+    for act, (values, slopes) in limits.items():
+        x, w = torch.ones(1, 1, dtype=tt, device="cuda"), torch.zeros(n, 1, dtype=tt, device="cuda")
+        d = B.make_linear_desc(1, n, 1, dtype, act)
+        out, pre = torch.empty(1, n, dtype=tt, device="cuda"), torch.empty(1, n, dtype=tt, device="cuda")
+        B.linear_fwd(d, x, w, vec(z), None, out, pre)
+        zs = stored(z, dtype)
+        assert np.array_equal(pre.double().cpu().numpy()[0], zs, equal_nan=True)
+        with np.errstate(invalid="ignore"):
+            want, _ = ro.activation(z.astype(np.float64), act)
+            _, slope = ro.activation(zs, act)
+        want[:2], slope[:2] = values, slopes
+        fin = np.where(np.isfinite(z), z, 0.0).astype(np.float64)
+        tol = act_tol(fin, 0.0)
+        assert_close(out.double().cpu().numpy()[0], want, tol + ROUND[dtype] * (np.abs(np.where(np.isfinite(want), want, 0.0)) + tol) + TINY[dtype], act)
+        db = nan_vec(n)
+        need = B.linear_bwd_workspace_bytes(d)
+        B.linear_bwd(d, None, None, pre, torch.ones_like(out), None, None, db, workspace(need), need)
+        assert_close(db.cpu().numpy(), slope, slope_tol(np.where(np.isfinite(zs), np.minimum(np.abs(zs), 20.0), 0.0)) + EPS32, "slope of " + act)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rows,N,K,start", [(9, 40, 72, 0), (9, 41, 73, 1), (60, 300, 264, 0), (700, 1032, 136, 0), (700, 1031, 136, 1), (2000, 2056, 72, 0)])
+def test_what_is_not_a_number_stays_in_its_row_and_column(dtype, rows, N, K, start):
+    torch = torch_mod()
+    tt, nan = torch_type(dtype), float("nan")
+    rng = np.random.default_rng(5)
+    X, W = Rows(rows, K, tt, K, start, nan).set(rng.normal(size=(rows, K))), Rows(N, K, tt, K, start, nan).set(rng.normal(size=(N, K)))
+    G = Rows(rows, N, tt, N, start, nan).set(rng.normal(size=(rows, N)))
+    at, col, k = rows // 2, N // 3, K - 1
+    X.view[at, k], W.view[col, 0] = nan, float("inf")
+    Y, DX, DW, DB = Rows(rows, N, tt, N, start, 7.0), Rows(rows, K, tt, K, start, 7.0), Rows(N, K, tt, K, start, 7.0), nan_vec(N)
+    d = B.make_linear_desc(rows, N, K, dtype)
+    need = B.linear_workspace_bytes(d)
+    B.linear_fwd(d, X.ptr, W.ptr, None, None, Y.ptr, None, workspace(need), need)
+    bad = ~np.isfinite(Y.host())
+    assert bad[at].all() and bad[:, col].all() and bad.sum() == rows + N - 1
+    G.view[at, 1] = nan
+    need = B.linear_bwd_workspace_bytes(d)
+    B.linear_bwd(d, X.ptr, W.ptr, None, G.ptr, DX.ptr, DW.ptr, DB, workspace(need), need)
+    bad = ~np.isfinite(DX.host())
+    assert bad[at].all() and bad[:, 0].all() and bad.sum() == rows + K - 1  # the row of the NaN, the column of the infinity
+    bad = ~np.isfinite(DW.host())
+    assert bad[1].all() and bad[:, k].all() and bad.sum() == N + K - 1
+    assert np.flatnonzero(~np.isfinite(DB.cpu().numpy())).tolist() == [1]
+
+
+def spread(rows, cols, tt, ld, values):
+    """A tensor whose rows lie `ld` apart, of `values`; nothing else of its memory is written."""
+    torch = torch_mod()
+    t = torch.empty(rows * ld, dtype=tt, device="cuda").as_strided((rows, cols), (ld, 1))
+    return t.copy_(torch.from_numpy(values).to(tt))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rows,N,K,ld", [(1100, 40, 24, (1 << 22) + 8), (1100, 264, 136, (1 << 22) + 3), (40, 1100, 72, (1 << 22) - 8), (1100, 1100, 40, (1 << 22) - 8)])
+def test_rows_far_apart(dtype, rows, N, K, ld):
+    """Offsets above 2^32 elements, in every tensor."""
+    torch = torch_mod()
+    tt = torch_type(dtype)
+    rng = np.random.default_rng(rows + N)
+    x, w, g = (stored(rng.normal(size=s), dtype) for s in ((rows, K), (N, K), (rows, N)))
+    X, W, R = spread(rows, K, tt, ld, x), spread(N, K, tt, ld, w), spread(rows, N, tt, ld, g)
+    out = spread(rows, N, tt, ld, np.zeros((rows, N)))
+    d = B.make_linear_desc(rows, N, K, dtype, "none", ld, ld, ld, ld)
+    need = B.linear_workspace_bytes(d)
+    B.linear_fwd(d, X, W, None, R, out, None, workspace(need), need)
+    v, z, size = ro.linear(x, w, None, g, "none")
+    tol = (K + 4) * EPS32 * (size + np.abs(g))
+    assert_close(out.double().cpu().numpy(), v, tol + ROUND[dtype] * (np.abs(v) + tol) + TINY[dtype], "out")
+    need = B.linear_bwd_workspace_bytes(d)
+    dw = spread(N, K, tt, ld, np.zeros((N, K)))
+    B.linear_bwd(d, X, W, None, R, out.as_strided((rows, K), (ld, 1)), dw, None, workspace(need), need)  # (dx where out was)
+    for got, ref, n, size in ((out.as_strided((rows, K), (ld, 1)), g @ w, N, np.abs(g) @ np.abs(w)), (dw, g.T @ x, rows, np.abs(g).T @ np.abs(x))):
+        tol = (n + 3) * EPS32 * size
+        assert_close(got.double().cpu().numpy(), ref, tol + ROUND[dtype] * (np.abs(ref) + tol) + TINY[dtype], "gradient")
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_gradients_without_rows(dtype):
+    torch = torch_mod()
+    d = B.make_linear_desc(0, 30, 70, dtype, "gelu", ldw=73)
+    DW, DB = Rows(30, 70, torch_type(dtype), 73, 1, 7.0), nan_vec(30)
+    B.linear_bwd(d, None, None, None, None, None, DW.ptr, DB)
+    assert not DW.host().any() and DW.untouched() and bool((DB == 0).all())
+
+
+def test_calls_give_the_same_bits():
+    """Sums are added in one order, shared reductions too."""
+    torch = torch_mod()
+    for rows, N, K, dtype in ((20, 1000, 4096, wl.F32), (700, 136, 9000, wl.BF16), (3000, 100, 200, wl.F16)):
+        tt = torch_type(dtype)
+        x, w, g = (torch.randn(s, device="cuda").to(tt) for s in ((rows, K), (N, K), (rows, N)))
+        d = B.make_linear_desc(rows, N, K, dtype, "gelu")
+        a, b = B.linear_workspace_bytes(d), B.linear_bwd_workspace_bytes(d)
+        results = []
+        for _ in range(3):
+            out, pre, dx, dw, db = torch.empty_like(g), torch.empty_like(g), torch.empty_like(x), torch.empty_like(w), nan_vec(N)
+            B.linear_fwd(d, x, w, None, None, out, pre, workspace(a), a)
+            B.linear_bwd(d, x, w, pre, g, dx, dw, db, workspace(b), b)
+            results.append((out, pre, dx, dw, db))
+        for again in results[1:]:
+            assert all(torch.equal(p, q) for p, q in zip(results[0], again))

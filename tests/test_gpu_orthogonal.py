@@ -128,3 +128,45 @@ def test_zeros_and_what_is_not_a_number():
     n = B.orthogonalize_workspace_bytes(d)
     B.orthogonalize(d, x, y, torch.empty(n, dtype=torch.uint8, device="cuda"), n)
     assert bool((y[0] == 0).all()) and bool(torch.isnan(y[1]).all()) and bool(torch.isnan(y[2]).all()) and bool(torch.isfinite(y[3]).all())
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_one_matrix_for_all_of_a_batch(dtype):
+    torch = torch_mod()
+    x = torch.randn(40, 24, generator=torch.Generator(device="cuda").manual_seed(4), device="cuda").to(torch_type(dtype))
+    y = torch.empty(5, 40, 24, dtype=x.dtype, device="cuda")
+    d = B.make_orthogonal_desc(40, 24, dtype, 5, stride_x=0)
+    n = B.orthogonalize_workspace_bytes(d)
+    B.orthogonalize(d, x, y, torch.empty(n, dtype=torch.uint8, device="cuda"), n)
+    want = ro.newton_schulz(x.double().cpu().numpy(), 5, STEP, 1e-7)
+    assert all(torch.equal(y[0], y[i]) for i in range(5))
+    assert np.linalg.norm(y[0].double().cpu().numpy() - want) <= bound(dtype, 40, 24, 5, STEP) * np.linalg.norm(want)
+
+
+def test_more_matrices_than_a_launch_takes():
+    torch = torch_mod()
+    batch = 33000
+    x = torch.randn(batch, 5, 9, generator=torch.Generator(device="cuda").manual_seed(6), device="cuda")
+    y = torch.empty_like(x)
+    d = B.make_orthogonal_desc(5, 9, wl.F32, batch)
+    n = B.orthogonalize_workspace_bytes(d)
+    B.orthogonalize(d, x, y, torch.empty(n, dtype=torch.uint8, device="cuda"), n)
+    for i in (0, 1, 32767, 32768, 32999):
+        want = ro.newton_schulz(x[i].double().cpu().numpy(), 5, STEP, 1e-7)
+        assert np.linalg.norm(y[i].double().cpu().numpy() - want) <= bound(wl.F32, 5, 9, 5, STEP) * np.linalg.norm(want)
+    assert bool(torch.isfinite(y).all())
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_rows_far_apart(dtype):
+    """Offsets above 2^32 elements."""
+    torch = torch_mod()
+    ld, rows, cols = (1 << 23) + 3, 600, 40
+    tt = torch_type(dtype)
+    x, y = (torch.empty(rows * ld, dtype=tt, device="cuda").as_strided((rows, cols), (ld, 1)) for _ in range(2))
+    x.copy_(torch.randn(rows, cols, generator=torch.Generator(device="cuda").manual_seed(8), device="cuda").to(tt))
+    d = B.make_orthogonal_desc(rows, cols, dtype, ldx=ld, ldo=ld)
+    n = B.orthogonalize_workspace_bytes(d)
+    B.orthogonalize(d, x, y, torch.empty(n, dtype=torch.uint8, device="cuda"), n)
+    want = ro.newton_schulz(x.double().cpu().numpy(), 5, STEP, 1e-7)
+    assert np.linalg.norm(y.double().cpu().numpy() - want) <= bound(dtype, rows, cols, 5, STEP) * np.linalg.norm(want)

@@ -253,3 +253,35 @@ def test_without_rows():
     outs = [nan_vec(100) for _ in range(5)]
     B.residual_norm_bwd(d, None, None, None, None, None, None, None, None, None, None, None, None, None, *outs, torch.empty(max(need, 16), dtype=torch.uint8, device="cuda"), need)
     assert all(bool((o == 0).all()) for o in outs)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("cols,gate_rows", [(200, 7), (200, 1), (3000, 0), (16400, 50)])
+def test_rows_far_apart(dtype, cols, gate_rows):
+    """Offsets above 2^32 elements give what neighbouring rows give."""
+    torch = torch_mod()
+    tt, rows, ld = torch_type(dtype), 1100, 4_000_037
+    g = torch.Generator(device="cuda").manual_seed(cols)
+    near = {k: torch.randn(rows, cols, generator=g, device="cuda").to(tt) for k in ("r", "h", "dr_out", "dy")}
+    gate = torch.randn(-(-rows // gate_rows), cols, generator=g, device="cuda").to(tt) if gate_rows else None
+    vectors = [torch.randn(cols, generator=g, device="cuda") for _ in range(5)]
+    # (three tensors far apart, each used twice)
+    far = [torch.empty(rows * ld, dtype=tt, device="cuda").as_strided((rows, cols), (ld, 1)) for _ in range(3)]
+    results = []
+    for apart in (False, True):
+        stride = ld if apart else None
+        new = lambda: torch.empty(rows, cols, dtype=tt, device="cuda")  # noqa: E731
+        r, h, y = far if apart else (new(), new(), new())
+        r.copy_(near["r"]), h.copy_(near["h"])
+        d = B.make_residual_norm_desc(rows, cols, dtype, EPS, False, True, gate_rows, True, stride, stride, cols if gate_rows else 0, stride)
+        st = torch.empty(rows, 4, device="cuda")
+        B.residual_norm_fwd(d, r, h, gate, *vectors, r, y, st)  # the sum over r
+        results.append([r.clone(), y.clone(), st])
+        need = B.residual_norm_bwd_workspace_bytes(d)
+        dgate = torch.empty_like(gate) if gate_rows else None
+        sums = [nan_vec(cols) for _ in range(5)]
+        y.copy_(near["dy"])
+        dh = torch.empty(rows * ld, dtype=tt, device="cuda").as_strided((rows, cols), (ld, 1)) if apart else new()
+        B.residual_norm_bwd(d, r, h, gate, *vectors[:4], st, None, y, None, dh, dgate, *sums, torch.empty(need, dtype=torch.uint8, device="cuda"), need)
+        results[-1] += [dh.clone(), *([dgate] if gate_rows else []), *sums]
+    assert all(torch.equal(a, b) for a, b in zip(*results))

@@ -1,0 +1,136 @@
+"""The training block and the orthogonal update without a GPU: what they hand to the library, and what they refuse before anything is launched.
+
+The binding's launching functions are replaced by ones that write down their arguments, so tensors can lie in host memory; descriptors and workspace
+sizes are the library's own."""
+import pytest
+import torch
+
+from paper_1611_06945_amd import binding as B
+from paper_1611_06945_amd import block as blk
+
+LAUNCHES = ("linear_fwd", "linear_bwd", "residual_norm_fwd", "residual_norm_bwd", "orthogonalize")
+ROWS, D, HIDDEN = 12, 16, 40
+
+
+@pytest.fixture
+def calls(monkeypatch):
+    made = []
+    monkeypatch.setattr(blk, "GPU", "cpu", raising=False)
+    for name in LAUNCHES:
+        monkeypatch.setattr(B, name, lambda *args, name=name: made.append((name, args)))
+    return made
+
+
+def block(dtype=torch.bfloat16, **kw):
+    return blk.TrainingBlock(ROWS, D, HIDDEN, dtype, device="cpu", **kw)
+
+
+def weights_of(b):
+    return {k: torch.ones(*s, dtype=b.dtype if k in blk.WEIGHTS else torch.float32) for k, s in b.shapes.items()}
+
+
+def rows_of(b, n=1):
+    return [torch.zeros(ROWS, D, dtype=b.dtype) for _ in range(n)]
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("kind", [dict(), dict(post=False, rms=True), dict(last=True), dict(gate_rows=5, sigmoid=True, act="silu")])
+def test_what_a_block_hands_on(calls, kind, dtype):
+    b = block(dtype, **kind)
+    p, (r, y) = weights_of(b), rows_of(b, 2)
+    gate = torch.zeros(3, D, dtype=dtype) if "gate_rows" in kind else None
+    out = b.forward(r, y, p, gate)
+    assert out == (b.r_out, b.y) and (b.y is None) == ("last" in kind)
+    assert [n for n, _ in calls] == ["linear_fwd", "linear_fwd", "residual_norm_fwd"]
+    first, second, norm = (a for _, a in calls)
+    assert first[1] is y and first[2] is p["w1"] and first[3] is p["b1"] and first[4] is None and first[5] is b.a and first[6] is b.pre
+    assert second[1] is b.a and second[2] is p["w2"] and second[5] is b.h and second[6] is None
+    assert norm[1] is r and norm[2] is b.h and norm[3] is gate and norm[9] is b.r_out and norm[10] is b.y
+    assert (norm[4] is None) == (kind.get("post") is False)
+    del calls[:]
+    (dr_out,) = rows_of(b)
+    assert b.backward(dr_out) == (b.dr, b.dy)
+    assert [n for n, _ in calls] == ["residual_norm_bwd", "linear_bwd", "linear_bwd"]
+    for name, a in calls:  # one workspace, large enough for every call
+        need = (B.residual_norm_bwd_workspace_bytes if name == "residual_norm_bwd" else B.linear_bwd_workspace_bytes)(a[0])
+        assert a[-3] is b.ws and a[-2] == b.ws.numel() >= need
+    assert set(b.grads) == set(b.shapes) and all(tuple(b.grads[k].shape) == s for k, s in b.shapes.items())
+    with pytest.raises(RuntimeError):
+        b.backward(dr_out)  # a second time
+
+
+def test_rows_that_are_refused(calls):
+    b = block()
+    p, (r, y) = weights_of(b), rows_of(b, 2)
+    for bad in (torch.zeros(ROWS, D), torch.zeros(ROWS - 1, D, dtype=b.dtype), torch.zeros(ROWS, 2 * D, dtype=b.dtype)[:, ::2], torch.zeros(D, ROWS, dtype=b.dtype).t(),
+                torch.zeros(ROWS, D, dtype=b.dtype, device="meta"), torch.zeros(ROWS, D, 1, dtype=b.dtype)):
+        with pytest.raises(ValueError):
+            b.forward(bad, y, p)
+        with pytest.raises(ValueError):
+            b.forward(r, bad, p)
+    with pytest.raises(ValueError):
+        b.forward(r, b.y, p)  # its own result: replaced before the gradient reads it
+    assert not calls
+    b.forward(r, y, p)
+    with pytest.raises(ValueError):
+        b.backward(torch.zeros(ROWS, D))
+    with pytest.raises(ValueError):
+        b.backward(*rows_of(b), torch.zeros(ROWS, D))
+    b.backward(*rows_of(b, 2))  # a refused call does not use the forward pass up
+    assert len(calls) == 6
+
+
+def test_weights_and_gates_that_are_refused(calls):
+    b = block(gate_rows=4)
+    r, y = rows_of(b, 2)
+    gate = torch.zeros(3, D, dtype=b.dtype)
+    for k in b.shapes:
+        p = weights_of(b)
+        for bad in (p[k].double(), p[k][..., :-1], torch.ones(*(2 * s for s in p[k].shape), dtype=p[k].dtype)[tuple(slice(None, None, 2) for _ in p[k].shape)]):
+            with pytest.raises(ValueError):
+                b.forward(r, y, {**p, k: bad}, gate)
+        del p[k]
+        with pytest.raises(ValueError):
+            b.forward(r, y, p, gate)
+    p = weights_of(b)
+    for bad in (None, gate[:2], gate.float(), torch.zeros(4, D, dtype=b.dtype)):
+        with pytest.raises(ValueError):
+            b.forward(r, y, p, bad)
+    with pytest.raises(ValueError):
+        block().forward(r, y, weights_of(block()), gate)
+    with pytest.raises(ValueError):
+        b.forward(r, y, {**p, "other": p["b1"]}, gate)
+    with pytest.raises(RuntimeError):
+        b.backward(*rows_of(b))  # no forward pass was accepted
+    last = block(last=True)
+    last.forward(r, y, weights_of(last))
+    with pytest.raises(ValueError):
+        last.backward(*rows_of(last, 2))
+    assert len(calls) == 3
+
+
+def test_places_and_types_that_are_refused():
+    with pytest.raises(ValueError):
+        blk.TrainingBlock(4, 8, 16, torch.float32, device="cpu")
+    with pytest.raises(ValueError):
+        blk.OrthogonalUpdate(2, 8, 16, torch.float32, device="cpu")
+
+
+@pytest.mark.parametrize("nesterov", [True, False])
+def test_momentum_of_the_update(calls, nesterov):
+    u = blk.OrthogonalUpdate(2, 3, 5, torch.float32, momentum=0.5, nesterov=nesterov, device="cpu")
+    g = torch.Generator().manual_seed(1)
+    total = torch.zeros(2, 3, 5)
+    for step in range(3):
+        grads = [torch.randn(3, 5, generator=g) for _ in range(2)]
+        assert u.step(grads) is u.direction
+        now = torch.stack(grads)
+        total = 0.5 * total + now
+        assert torch.allclose(u.sum, total) and torch.allclose(u.direction, 0.5 * total + now if nesterov else total)
+        name, a = calls[step]
+        assert name == "orthogonalize" and a[1] is a[2] is u.direction and a[4] == u.ws.numel() >= B.orthogonalize_workspace_bytes(a[0])
+    before = u.sum.clone()
+    for bad in ([grads[0]], [grads[0], grads[1].t()], [grads[0], grads[1].int()], [grads[0], grads[1].to("meta")]):
+        with pytest.raises(ValueError):
+            u.step(bad)
+    assert torch.equal(u.sum, before) and len(calls) == 3
