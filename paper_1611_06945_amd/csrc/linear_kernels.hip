@@ -277,8 +277,8 @@ struct TileCost {
     int bt, bn;
     double once, own, step;
 };
-constexpr TileCost kTiles[] = {{64, 64, 3.3, 1.1, 0.24}, {128, 128, 2.2, 1.95, 0.51}, {256, 256, 0, 6.6, 1.1}, {192, 192, 0, 5.6, 0.75}, {64, 64, 3.4, 0.5, 0.49}, {128, 128, 3.1, 2.1, 0.81}};
-constexpr TileCost kTilesF32[] = {{64, 64, 4.5, 0.5, 1.3}, {128, 128, 0, 6.2, 2.75}, {256, 128, 0, 8.1, 4.7}};
+constexpr TileCost kTiles[] = {{64, 64, 3.3, 1.1, 0.24}, {128, 128, 2.2, 1.95, 0.51}, {256, 256, 0, 6.6, 1.1}, {192, 192, 0, 5.6, 0.75}, {64, 64, 5.2, 1.7, 0.28}, {128, 128, 2.4, 5.7, 0.59}};
+constexpr TileCost kTilesF32[] = {{64, 64, 4.6, 0.75, 1.06}, {128, 128, 0, 6.4, 2.36}, {256, 128, 0, 7.8, 3.9}};
 
 struct ProductPlan {
     ProductForm form;

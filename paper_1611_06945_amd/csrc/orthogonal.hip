@@ -248,14 +248,16 @@ Space space_of(const OrthogonalArgs& g, int dtype, void* ws)
 }
 
 // Tiles of one plane, and of two, whose stages are twice as large.
-typedef ProductTile<4, 2, 1, 2, 2, 2> Tile64Two;  // two workgroups a CU
+typedef ProductTile<4, 2, 1, 2, 2, 2> Tile64Two;      // two workgroups a CU
+typedef ProductTile<4, 2, 1, 2, 4, 2> Tile64TwoDeep;  // one: three steps on their way (4 of 2048 x 512 fp16: 307 -> 268 us)
 typedef ProductTile<2, 4, 4, 2, 2, 2> Tile128Two;
 struct TileCost {
     int side, planes;
     double once, own, step;
+    bool alone;  // for a workgroup a CU at most, and more steps than it has stages (12 of 192 x 192: 114 us, with it 116)
 };
-constexpr TileCost kTiles[] = {{64, 1, 4.1, 1.0, 0.275}, {128, 1, 3.1, 1.7, 0.53}, {256, 1, 0, 6.4, 1.18}, {192, 1, 0, 5.0, 0.8}, {64, 2, 4.1, 1.0, 0.5}, {128, 2, 3.1, 3.0, 1.3}};
-enum TileId { T64, T128, T256, T192, T64_TWO, T128_TWO };
+constexpr TileCost kTiles[] = {{64, 1, 4.1, 1.0, 0.275}, {128, 1, 3.1, 1.7, 0.53}, {256, 1, 0, 6.4, 1.18}, {192, 1, 0, 5.0, 0.8}, {64, 2, 4.1, 1.0, 0.5}, {128, 2, 3.1, 3.0, 1.3}, {64, 2, 4.1, 1.0, 0.4, true}};
+enum TileId { T64, T128, T256, T192, T64_TWO, T128_TWO, T64_TWO_DEEP };
 
 // The tile with the least expected time, in us (see the linear layers' plan).
 TileId tile_of(int64_t M, int64_t N, int64_t K, int planes, int64_t batch, bool symmetric)
@@ -268,6 +270,7 @@ TileId tile_of(int64_t M, int64_t N, int64_t K, int planes, int64_t batch, bool 
         const double tm = (double)((M + c.side - 1) / c.side), tn = (double)((N + c.side - 1) / c.side);
         const double tiles = (symmetric ? tm * (tm + 1) / 2 : tm * tn) * batch, steps = (double)((K + 63) / 64);
         const double us = c.once + std::ceil(tiles / 256) * (c.own + steps * c.step);
+        if (c.alone && (tiles > 256 || steps <= 4)) continue;
         if (us < least) least = us, best = f;
     }
     return (TileId)best;
@@ -286,6 +289,7 @@ hipError_t multiply(const ProductArgs& g, const typename Epi::Args& e, TileId ti
         case T128: return launch_product_tiles<CONV_F16, Tile128, A_ACROSS, B_ACROSS, true, Epi>(g, e, batch, 1, s);
         case T192: return launch_product_tiles<CONV_F16, Tile192, A_ACROSS, B_ACROSS, true, Epi>(g, e, batch, 1, s);
         case T256: return launch_product_tiles<CONV_F16, Tile256, A_ACROSS, B_ACROSS, true, Epi>(g, e, batch, 1, s);
+        case T64_TWO_DEEP: return launch_product_tiles<CONV_F16, Tile64TwoDeep, A_ACROSS, B_ACROSS, true, Epi>(g, e, batch, 1, s);
         case T64_TWO: return launch_product_tiles<CONV_F16, Tile64Two, A_ACROSS, B_ACROSS, true, Epi>(g, e, batch, 1, s);
         default: return launch_product_tiles<CONV_F16, Tile128Two, A_ACROSS, B_ACROSS, true, Epi>(g, e, batch, 1, s);
     }

@@ -41,9 +41,9 @@ hipError_t launch_product_f32(const ProductArgs& g, const LinearOut& e, ProductL
     SplitArgs p = {};
     p.a = (const float*)g.a, p.b = (const float*)g.b, p.lda = g.lda, p.ldb = g.ldb, p.M = g.M, p.N = g.N, p.K = g.K, p.partial = g.partial;
     p.each = (int64_t)((g.ksteps + splits - 1) / splits) * 64, p.splits = splits;
-    typedef SplitTile<2, 2, 2, 2, 2, 2> Tile64;
-    typedef SplitTile<2, 4, 4, 2, 1, 2> Tile128;
-    typedef SplitTile<4, 2, 4, 4, 1, 2> Tile256;
+    typedef SplitTile<2, 2, 2, 2> Tile64;
+    typedef SplitTile<2, 4, 4, 2> Tile128;
+    typedef SplitTile<4, 2, 4, 4> Tile256;
     switch (form) {
         case P64: return splits > 1 ? launch_layout<Tile64, true>(p, e, layout, splits, s) : launch_layout<Tile64, false>(p, e, layout, splits, s);
         case P128: return splits > 1 ? launch_layout<Tile128, true>(p, e, layout, splits, s) : launch_layout<Tile128, false>(p, e, layout, splits, s);

@@ -4,10 +4,11 @@
 //
 // x = x0 + x1 + x2 with 8 bits each holds all 24 bits of an fp32 value; of the nine products of parts the six that count are formed: 1 1, 0 2 and 2 0 first,
 // then 0 1 and 1 0, then 0 0.  What is left out is below 2^-25 of a product.  Six products at the bf16 rate are 2.6 times as fast as the fp32 matrix
-// instructions.  An element is split once for a workgroup: pieces of eight go from memory to registers, D steps ahead, and as three planes to
+// instructions.  An element is split once for a workgroup: pieces of eight go from memory to registers and as three planes to
 // LDS, so operands may start anywhere.  A stage has 32 of the reduction: 64 bytes of each row and plane (pieces at piece ^ (row / 4 % 4)), or 32 rows
 // across.  There are two stages: the next one is split and written between the products of the present one, since splitting is as much vector work as half of
-// the products' time and a workgroup that did one after the other took 2.1 us a step of 128 x 128, whose products are 0.64.
+// the products' time and a workgroup that did one after the other took 2.1 us a step of 128 x 128, whose products are 0.64.  A piece is asked for anew as soon as it is
+// split, a whole step ahead (8192 x 4096 x 4096: 1413 us with a step's loads behind its products, 1295 so; 2048 x 2048 x 2048 105 and 96).
 #pragma once
 
 #include "linear_common.h"
@@ -15,10 +16,10 @@
 
 namespace convfwd {
 
-template <int WT_, int WN_, int FT_, int FN_, int D_, int S_>
+template <int WT_, int WN_, int FT_, int FN_>
 struct SplitTile {
-    static constexpr int S = S_;  // stages
-    static constexpr int WT = WT_, WN = WN_, FT = FT_, FN = FN_, D = D_;  // D: steps that are on their way
+    static constexpr int S = 2;  // stages
+    static constexpr int WT = WT_, WN = WN_, FT = FT_, FN = FN_;
     static constexpr int BT = 16 * WT * FT, BN = 16 * WN * FN, NT = 64 * WT * WN, KE = 32;
     static constexpr int PLANE_A = BT * KE * 2, PLANE_B = BN * KE * 2;  // bytes of a plane of a stage
     static constexpr int STAGE = 3 * (PLANE_A + PLANE_B);
@@ -31,27 +32,23 @@ template <typename T, int W, int L, bool ACROSS>
 struct SplitOperand {
     typedef AnyPieces<float, T::NT, W, T::KE, L, ACROSS> Pieces;
     Pieces pieces;
-    float held[T::D][L][8];
+    float held[L][8];  // the next step
 
-    template <int S>
-    __device__ __forceinline__ void load()
-    {
-        pieces.load(held[S]);
-    }
-    template <int S>
-    __device__ __forceinline__ void clear()
-    {
-        pieces.clear(held[S]);
-    }
     // pieces FROM .. TO - 1 of a step
-    template <int S, int FROM, int TO>
+    template <int FROM, int TO>
+    __device__ __forceinline__ void load_whole()
+    {
+#pragma unroll
+        for (int i = FROM; i < TO; ++i) pieces.load_whole(held[i], i);
+    }
+    template <int FROM, int TO>
     __device__ __forceinline__ void commit(char* lds, int plane)
     {
 #pragma unroll
         for (int i = FROM; i < TO; ++i) {
             int row, piece;
             Pieces::place(i, row, piece);
-            const Split3 s = split3(held[S][i]);
+            const Split3 s = split3(held[i]);
             char* to = lds + (ACROSS ? row * (W * 2) + (piece ^ across_swizzle<W>(row)) * 16 : row * 64 + ((piece ^ ((row >> 2) & 3)) << 4));
 #pragma unroll
             for (int q = 0; q < 3; ++q) *(uint4*)(to + q * plane) = s.p[q];
@@ -112,59 +109,69 @@ __global__ __launch_bounds__(T::NT) void product_f32_kernel(SplitArgs g, LinearO
 #pragma unroll
         for (int j = 0; j < T::FT; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 
-    // (steps past the last load nothing: there is nothing left of the reduction)
-    typedef std::integral_constant<int, 0> Zero;
-    auto commit = [&](char* stage, auto slot, auto part) {  // part of FT
-        constexpr int S = decltype(slot)::value, P = decltype(part)::value;
-        if constexpr (P == 0) a.template clear<S>(), b.template clear<S>();
-        a.template commit<S, T::LA * P / T::FT, T::LA * (P + 1) / T::FT>(stage, T::PLANE_A);
-        b.template commit<S, T::LB * P / T::FT, T::LB * (P + 1) / T::FT>(stage + 3 * T::PLANE_A, T::PLANE_B);
+    auto commit = [&](char* stage, auto part) {  // part of FT
+        constexpr int P = decltype(part)::value;
+        a.template commit<T::LA * P / T::FT, T::LA * (P + 1) / T::FT>(stage, T::PLANE_A);
+        b.template commit<T::LB * P / T::FT, T::LB * (P + 1) / T::FT>(stage + 3 * T::PLANE_A, T::PLANE_B);
     };
-    count_to<T::D>([&](auto d) { a.template load<decltype(d)::value>(), b.template load<decltype(d)::value>(); });
-    if constexpr (T::S == 2) {
-        count_to<T::FT>([&](auto p) { commit(smem, Zero(), p); });
-        a.template load<0>(), b.template load<0>();
+    // The products of the step in stage `buf`; between them the step that the registers hold, if there is one, is split and goes to the other
+    // stage, and each of its pieces may be asked for anew for the step after it.
+    int buf = 0;
+    auto step = [&](auto load, bool more) {
+        const char *const at_a = smem + buf * T::STAGE, *const at_b = at_a + 3 * T::PLANE_A;
+        char* const next = smem + (buf ^ 1) * T::STAGE;
+        u32x4 bv[T::FN][3];
+#pragma unroll
+        for (int i = 0; i < T::FN; ++i)
+#pragma unroll
+            for (int q = 0; q < 3; ++q) bv[i][q] = b.fragment(at_b + q * T::PLANE_B, wn * T::FN + i);
+        count_to<T::FT>([&](auto part) {
+            constexpr int j = decltype(part)::value;
+            u32x4 av[3];
+#pragma unroll
+            for (int q = 0; q < 3; ++q) av[q] = a.fragment(at_a + q * T::PLANE_A, wt * T::FT + j);
+            if (more) commit(next, part);
+            load(part);
+            constexpr int PA[6] = {1, 0, 2, 0, 1, 0}, PB[6] = {1, 2, 0, 1, 0, 0};
+#pragma unroll
+            for (int t = 0; t < 6; ++t)
+#pragma unroll
+                for (int i = 0; i < T::FN; ++i) acc[i][j] = multiply16<CONV_BF16>(bv[i][PB[t]], av[PA[t]], acc[i][j]);
+        });
+        buf ^= 1;
+    };
+
+    const int steps = (int)((k1 - k0 + T::KE - 1) / T::KE);
+    a.pieces.load(a.held), b.pieces.load(b.held);
+    a.pieces.clear(a.held), b.pieces.clear(b.held);
+    count_to<T::FT>([&](auto p) { commit(smem, p); });
+    // Whole steps: loads without a branch (behind one that may load or not a wave waits for all that is on its way), a step ahead.
+    const int whole = min(a.pieces.whole(), b.pieces.whole()) - 1;
+    auto load_whole = [&](auto part) {
+        constexpr int P = decltype(part)::value;
+        a.template load_whole<T::LA * P / T::FT, T::LA*(P + 1) / T::FT>();
+        b.template load_whole<T::LB * P / T::FT, T::LB*(P + 1) / T::FT>();
+    };
+    int k = 0;
+    if (whole > 0) {
+        count_to<T::FT>(load_whole);
+        a.pieces.advance(), b.pieces.advance();
+        __syncthreads();
+        for (; k < whole; ++k) {
+            a.pieces.keep(), b.pieces.keep();
+            step(load_whole, true);
+            a.pieces.advance(), b.pieces.advance();
+            __syncthreads();
+        }
+    } else {
+        a.pieces.load(a.held), b.pieces.load(b.held);
         __syncthreads();
     }
-    int64_t k = k0;
-    for (int buf = 0; k < k1;) {
-        // step i is in stage i % S; two stages: step i + 1 in slot (i + 1) % D of the registers, one: step i in slot i % D
-        count_to<T::D>([&](auto d) {
-            constexpr int SLOT = (decltype(d)::value + T::S - 1) % T::D;
-            typedef std::integral_constant<int, SLOT> Slot;
-            if (k >= k1) return;
-            k += T::KE;
-            if constexpr (T::S == 1) {
-                __syncthreads();  // the stage has been read
-                count_to<T::FT>([&](auto p) { commit(smem, Slot(), p); });
-                __syncthreads();
-                a.template load<SLOT>(), b.template load<SLOT>();
-            }
-            const char *const at_a = smem + buf * T::STAGE, *const at_b = at_a + 3 * T::PLANE_A;
-            char* const next = smem + (buf ^ 1) * T::STAGE;
-            u32x4 bv[T::FN][3];
-#pragma unroll
-            for (int i = 0; i < T::FN; ++i)
-#pragma unroll
-                for (int q = 0; q < 3; ++q) bv[i][q] = b.fragment(at_b + q * T::PLANE_B, wn * T::FN + i);
-            count_to<T::FT>([&](auto part) {
-                constexpr int j = decltype(part)::value;
-                u32x4 av[3];
-#pragma unroll
-                for (int q = 0; q < 3; ++q) av[q] = a.fragment(at_a + q * T::PLANE_A, wt * T::FT + j);
-                if (T::S == 2 && k < k1) commit(next, Slot(), part);
-                constexpr int PA[6] = {1, 0, 2, 0, 1, 0}, PB[6] = {1, 2, 0, 1, 0, 0};
-#pragma unroll
-                for (int t = 0; t < 6; ++t)
-#pragma unroll
-                    for (int i = 0; i < T::FN; ++i) acc[i][j] = multiply16<CONV_BF16>(bv[i][PB[t]], av[PA[t]], acc[i][j]);
-            });
-            if constexpr (T::S == 2) {
-                a.template load<SLOT>(), b.template load<SLOT>();
-                __syncthreads();
-                buf ^= 1;
-            }
-        });
+    for (; k < steps; ++k) {
+        if (k + 1 < steps) a.pieces.clear(a.held), b.pieces.clear(b.held);
+        step([](auto) {}, k + 1 < steps);
+        a.pieces.load(a.held), b.pieces.load(b.held);  // (past the last step: nothing)
+        __syncthreads();
     }
 
     // as in product_kernel: eight n in a row for each lane

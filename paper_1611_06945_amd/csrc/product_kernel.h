@@ -18,6 +18,7 @@
 #pragma once
 
 #include <algorithm>
+#include <climits>
 #include <cmath>
 #include <type_traits>
 
@@ -107,12 +108,21 @@ struct AnyPieces {
             off[i] = ACROSS ? row * ld + (piece * 8 < here ? piece * 8 : 0) : min(row, here - 1) * ld + piece * 8;
         }
     }
+    // Steps from here on that load whole pieces.  (ACROSS: eight more rows hold the seven elements that a piece may pass its row's last column
+    // by, however short they are)
+    __device__ __forceinline__ int whole() const { return (int)min(max((left - (ACROSS && last ? 8 : 0)) / KE, (int64_t)0), (int64_t)INT_MAX); }
+    // piece i of one of those; advance() after all of its pieces
+    __device__ __forceinline__ void load_whole(E (&to)[8], int i) { __builtin_memcpy(to, from + off[i], 8 * sizeof(E)); }
+    __device__ __forceinline__ void advance()
+    {
+        from += ACROSS ? KE * ld : (int64_t)KE;
+        left -= KE;
+    }
     __device__ __forceinline__ void load(E (&to)[L][8])
     {
-        // (ACROSS: eight more rows hold the seven elements that a piece may pass its row's last column by, however short they are)
         if (left >= KE + (ACROSS && last ? 8 : 0)) {
 #pragma unroll
-            for (int i = 0; i < L; ++i) __builtin_memcpy(to[i], from + off[i], 8 * sizeof(E));
+            for (int i = 0; i < L; ++i) load_whole(to[i], i);
         } else if (left > 0) {
 #pragma unroll
             for (int i = 0; i < L; ++i) {
@@ -131,10 +141,11 @@ struct AnyPieces {
                 }
             }
         }
-        from += ACROSS ? KE * ld : (int64_t)KE;
-        left -= KE;
+        advance();
     }
-    // what is past the reduction's end becomes zeros; once for each load, in their order
+    // a step of whole pieces within the reduction
+    __device__ __forceinline__ void keep() { used -= KE; }
+    // what is past the reduction's end becomes zeros; this or keep() once for each load, in their order
     __device__ __forceinline__ void clear(E (&v)[L][8])
     {
         if (used < KE) {
@@ -236,25 +247,36 @@ struct Operand {
 template <typename T, int W, int L, bool ACROSS>
 struct Operand<T, W, L, ACROSS, false> {
     typedef AnyPieces<uint16_t, T::NT, W, T::KE, L, ACROSS> Pieces;
+    // Steps on their way: a step of small tiles takes a fraction of a trip to memory (64 x 64 with 1 and 4: the gradient of x of 777 x 1283 x 1001 25.6 and 18.6 us;
+    // 128 x 128 with 1, 2 and 4: that of w 25.7, 21.3 and 23.2 us, for the registers that two workgroups a CU have).
+    static constexpr int D = L == 1 ? 4 : 2;
     Pieces pieces;
     int here;
-    uint16_t held[L][8];
+    uint16_t held[D][L][8];
 
     __device__ __forceinline__ void begin(const uint16_t* p, int64_t stride, int64_t, int64_t K, int64_t first, int64_t all, int64_t k0)
     {
         pieces.begin(p, stride, K, first, all, k0);
         here = pieces.here;
     }
-    __device__ __forceinline__ void load() { pieces.load(held); }
+    template <int S>
+    __device__ __forceinline__ void load_whole()
+    {
+#pragma unroll
+        for (int i = 0; i < L; ++i) pieces.load_whole(held[S][i], i);
+        pieces.advance();
+    }
+    template <int S, bool WHOLE>
     __device__ __forceinline__ void commit(char* lds)
     {
-        pieces.clear(held);
+        if constexpr (WHOLE) pieces.keep();
+        else pieces.clear(held[S]);
 #pragma unroll
         for (int i = 0; i < L; ++i) {
             int row, piece;
             Pieces::place(i, row, piece);
             uint4 v;
-            __builtin_memcpy(&v, held[i], 16);
+            __builtin_memcpy(&v, held[S][i], 16);
             *(uint4*)(lds + (row * (ACROSS ? W / 8 : 8) + swizzled<W, ACROSS>(row, piece)) * 16) = v;
         }
     }
@@ -453,26 +475,58 @@ __global__ __launch_bounds__(T::NT) void product_kernel(ProductArgs g, typename 
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // nothing may land in LDS after the end
     } else {
         static_assert(DIRECT || (T::S == 2 && T::PL == 1), "one stage is multiplied, the other written");
-        auto commit = [&](int buf) {
-            a.commit(smem + buf * T::STAGE);
-            b.commit(smem + buf * T::STAGE + T::PLANE_A);
+        constexpr int D = decltype(a)::D;
+        static_assert(D % 2 == 0, "step k lies in stage k % 2 and came by slot k % D");
+        auto load = [&](auto slot) { a.pieces.load(a.held[decltype(slot)::value]), b.pieces.load(b.held[decltype(slot)::value]); };
+        auto load_whole = [&](auto slot) { a.template load_whole<decltype(slot)::value>(), b.template load_whole<decltype(slot)::value>(); };
+        auto commit = [&](auto slot, auto whole) {
+            constexpr int S = decltype(slot)::value;
+            char* const to = smem + S % 2 * T::STAGE;
+            a.template commit<S, decltype(whole)::value>(to);
+            b.template commit<S, decltype(whole)::value>(to + T::PLANE_A);
         };
-        a.load(), b.load();
-        commit(0);
-        a.load(), b.load();
-        __syncthreads();
-        for (int k = 0; k < steps; ++k) {
-            fetch(k & 1, First());
+        auto multiply = [&](auto slot) {
+            constexpr int BUF = decltype(slot)::value % 2;
+            fetch(BUF, First());
             count_to<PHASES>([&](auto p) {
                 constexpr int q = decltype(p)::value;
-                if constexpr (q + 1 < PHASES) fetch(k & 1, std::integral_constant<int, q + 1>());
+                if constexpr (q + 1 < PHASES) fetch(BUF, std::integral_constant<int, q + 1>());
                 products(p);
             });
-            if (k + 1 < steps) {
-                commit((k + 1) & 1);
-                a.load(), b.load();
-            }
+        };
+        // Step k is in its stage, steps k + 1 .. k + D on their way.  The first loop's loads are of whole steps, without a branch: behind one that
+        // may load or not a wave waits for all that is on its way.
+        const int whole = min(steps, min(a.pieces.whole(), b.pieces.whole()));
+        int k = 0;
+        if (whole > 2 * D) {
+            count_to<D>(load_whole);
+            commit(First(), std::true_type());
+            load_whole(First());
             __syncthreads();
+            for (; k + 2 * D < whole; k += D) {
+                count_to<D>([&](auto u) {
+                    typedef std::integral_constant<int, (decltype(u)::value + 1) % D> Next;
+                    multiply(u);
+                    commit(Next(), std::true_type());
+                    load_whole(Next());
+                    __syncthreads();
+                });
+            }
+        } else {
+            count_to<D>(load);
+            commit(First(), std::false_type());
+            load(First());
+            __syncthreads();
+        }
+        while (k < steps) {
+            count_to<D>([&](auto u) {
+                typedef std::integral_constant<int, (decltype(u)::value + 1) % D> Next;
+                if (k >= steps) return;
+                multiply(u);
+                if (++k < steps) commit(Next(), std::false_type());
+                load(Next());  // (past the last step: nothing)
+                __syncthreads();
+            });
         }
     }
 

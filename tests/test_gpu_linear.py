@@ -153,9 +153,9 @@ FORMS = {
 }
 FORMS16 = {
     "tile64x64": (0, 700, 1032, 40, 0), "tile128x128": (0, 1000, 1032, 72, 0), "tile192x192": (0, 2000, 2056, 136, 0), "tile256x256": (0, 3000, 3080, 72, 0),
-    "tile64x64_any": (0, 520, 640, 40, 1), "tile128x128_any": (0, 2000, 1032, 72, 1), "tile256x256+tile128x128": (0, 5200, 3080, 40, 0),
+    "tile64x64_any": (0, 1100, 776, 40, 1), "tile128x128_any": (0, 2000, 1032, 72, 1), "tile256x256+tile128x128": (0, 5200, 3080, 40, 0),
     "tile256x256+tile192x192": (0, 5200, 4104, 24, 0), "tile64x64_any_split13": (0, 40, 8, 4104, 1), "tile128x128_split16": (0, 700, 136, 9000, 0),
-    "tile128x128_any_split7": (0, 130, 1400, 2056, 1),
+    "tile128x128_any_split13": (0, 200, 1032, 4104, 1),
     "1 tile64x64": (1, 30, 40, 24, 0), "1 tile128x128": (1, 1000, 40, 1032, 0), "1 tile192x192": (1, 2000, 72, 2056, 0), "1 tile256x256": (1, 2600, 40, 4104, 0),
     "1 tile256x256+tile128x128": (1, 4100, 40, 4104, 0), "1 tile128x128_any": (1, 2000, 40, 1032, 1), "1 tile64x64_any_split13": (1, 3, 4104, 16, 1),
     "1 tile128x128_split13": (1, 1, 4104, 2056, 0), "2 tile64x64": (2, 40, 24, 72, 0), "2 tile128x128": (2, 40, 1000, 1032, 0), "2 tile192x192": (2, 72, 2056, 2056, 0),
