@@ -7,8 +7,8 @@
 // 2^12 (X, A and B are small whole numbers at most and their elements of the size 1 / sqrt(n): scaled they keep all their bits).
 //   * X itself is kept in more bits than it is multiplied in: weak directions grow by a in every step, and so would the roundings of an X kept in 16
 //     bits (a matrix of rank n / 8 in bf16: 3 % off, against 0.08 %).  The errors of A, B and the X that B multiplies do not grow like that.
-//   * bf16: the products take one fp16 plane of each operand, which has three bits more than the result (off by 1.2e-3 before the result's own
-//     rounding of 1.7e-3, 4096 x 4096).  fp16 and fp32: two planes, high and low, and three of their four products, 22 bits.
+//   * bf16: the products take one fp16 plane of each operand, which has three bits more than the result, where that is enough (planes_of).  Others: two
+//     planes, high and low, and three of their four products, 22 bits.
 //   * X beside its products: fp32 for fp32; for 16-bit types the high and the low plane together, 22 bits, which is less to read and write.
 #include <algorithm>
 #include <cmath>
@@ -213,7 +213,15 @@ __global__ __launch_bounds__(256) void orthogonal_start(StartArgs g)
 
 int64_t round_up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 
-int planes_of(int dtype) { return dtype == CONV_BF16 ? 1 : 2; }
+// Planes that are multiplied.  One makes errors of some 2^-11 in a step, which count once the strongest directions, 1 / sqrt(n) at least at first
+// and a times that with every step, have come near one: up to three steps from there leave a bf16 result off by 1.3 times its own rounding at most (4096 x
+// 4096 in five steps 1.02, 256 x 256 1.23, in six of 512 x 512 1.37, of 166 x 30 1.8: those take two).
+int planes_of(const OrthogonalArgs& g, int dtype)
+{
+    const double side = (double)std::min(g.rows, g.cols), a = std::fabs((double)g.a);
+    const double before = a > 1.0 ? 0.5 * std::log(side) / std::log(a) : 0.0;
+    return dtype == CONV_BF16 && g.steps - before <= 3.0 ? 1 : 2;
+}
 int parts_of(int64_t rows, int64_t cols) { return (int)std::max<int64_t>(1, std::min<int64_t>(1024, rows * cols / 8192)); }
 
 struct Space {
@@ -240,7 +248,7 @@ Space space_of(const OrthogonalArgs& g, int dtype, void* ws)
     };
     const int64_t side = std::min(g.rows, g.cols);
     s.x[0] = matrix(g.rows, g.cols, 2), s.x[1] = matrix(g.rows, g.cols, 2);
-    s.a = matrix(side, side, planes_of(dtype)), s.b = matrix(side, side, planes_of(dtype));
+    s.a = matrix(side, side, planes_of(g, dtype)), s.b = matrix(side, side, planes_of(g, dtype));
     s.batch_x = g.rows * s.x[0].ld;
     if (dtype == CONV_F32) s.x32 = (float*)take((size_t)g.batch * s.batch_x * 4);
     s.sums = (double*)take((size_t)g.batch * parts_of(g.rows, g.cols) * 8);
@@ -319,7 +327,7 @@ size_t orthogonal_workspace(const OrthogonalArgs& g, int dtype) { return g.batch
 hipError_t launch_orthogonalize(const OrthogonalArgs& all, int dtype, hipStream_t s)
 {
     // gridDim.y is at most 65535, and a launch holds less than 2^32 threads: the batch goes in portions, tiles chosen for the largest
-    const int planes = planes_of(dtype), es = dtype_size(dtype);
+    const int planes = planes_of(all, dtype), es = dtype_size(dtype);
     const int64_t side = std::min(all.rows, all.cols), longer = std::max(all.rows, all.cols), most = std::min<int64_t>(all.batch, 32768);
     const TileId gram = tile_of(side, side, longer, planes, most, true), square = tile_of(side, side, side, planes, most, true);
     const TileId update = tile_of(all.rows, all.cols, side, planes, most, false);
