@@ -15,6 +15,9 @@
 //     bytes past K belong to what follows and are cleared in both operands on the last step.  Otherwise pieces go
 //     through registers, from any address, and their ends are cleared on the way.
 //   * Operands may be sums of two planes, high and low (PL = 2), of which a step multiplies low x high, high x low and high x high.
+// Bound by the matrix units and LDS together: a step of a tile of 256 x 256 takes 2048 clocks of products and 2048 of LDS, 1536 reading and 512 written to, so waves of
+// 64 x 128 with two a SIMD, each's products between the reads of its next operands.  8192 x 4096 x 8192 bf16 with GELU and the sum kept 475 to 483 us, 1.14 PFLOP/s, matrix
+// units busy 52 % of the clocks (the end of a tile, 45 us in all, has none); four waves of 128 x 128 with one a SIMD took 141 us for 4096 x 4096 x 4096 where this takes 100.
 #pragma once
 
 #include <algorithm>

@@ -13,7 +13,8 @@
 // Where rows share a gate, the sums S1 and S2 are formed for each gate row apart, without the gate: its gradient is scale (gamma_h S2 + beta_h S1)
 // then, and the sums over all rows are those times the gate.  A workgroup takes `items`: runs of rows, each within one gate row; a lane
 // adds up its columns in registers, a workgroup's lanes meet in LDS, and a second kernel adds the items, always in the same order.
-// Bound by memory: four tensors forward, six backward.
+// Bound by memory: four tensors forward (50176 x 768 bf16 with shared gates 76 us, 4.1 TB/s), six backward and with gates of their own eight (16384 x 4096 bf16 221 us,
+// 4.9 TB/s); few rows by two launches (3380 x 384 fp32 backward 11.2 us and 7.2 for the join).
 #pragma once
 
 #include <algorithm>
