@@ -485,15 +485,15 @@ int linear_fwd(const linear_desc* desc, const void* x, const void* w, const floa
  * Its gradients: with dz = dout * act'(pre) (the slope of ReLU at 0 is 0),
  *   dx[t][k] = sum_n dz[t][n] * w[n][k],   dw[n][k] = sum_t dz[t][n] * x[t][k],   dbias[n] = sum_t dz[t][n];
  * the residual's gradient is dout.  Any of dx (row stride ldx), dw (ldw) and dbias (fp32 [N]) may be NULL, not all; x is read for dw, w for dx, pre
- * where there is an activation: each may be NULL otherwise.  In 16-bit types dz is rounded to the type before the products (dbias adds it
- * unrounded).  rows = 0 gives zero dw and dbias.  `workspace`: linear_bwd_workspace_bytes(desc), as above.
+ * where there is an activation: each may be NULL otherwise.  dz is kept in as many bits as the results need: in 16-bit types as two values of the type (16 bits in bf16,
+ * 22 in fp16, none lost to fp16's range) behind GELU and SiLU, where no infinity in x or w passes to a result but as NaN.  rows = 0 gives zero dw and dbias.  `workspace`: linear_bwd_workspace_bytes(desc), as above.
  */
 size_t linear_bwd_workspace_bytes(const linear_desc* desc);
 int linear_bwd(const linear_desc* desc, const void* x, const void* w, const void* pre, const void* dout, void* dx, void* dw,
                float* dbias, void* workspace, size_t workspace_bytes, void* stream);
 
 /* Name of the form that a product takes for this descriptor and these operands' addresses (which count modulo 16), NUL-terminated in
- * buf[0..n), e.g. "rows16", "tile256x256" or "split_tile64x64_split4"; `which`: 0 the product of linear_fwd, 1 and 2 those of linear_bwd for dx and
+ * buf[0..n), e.g. "rows16", "tile256x256", "split_tile64x64_split4" or "parts_tile128x128" (of dz in two parts); `which`: 0 the product of linear_fwd, 1 and 2 those of linear_bwd for dx and
  * dw.  Empty for no rows.  Pure host code. */
 int linear_form(const linear_desc* desc, const void* x, const void* w, int which, char* buf, size_t n);
 

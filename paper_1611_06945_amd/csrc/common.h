@@ -314,7 +314,7 @@ struct LinearArgs {
 hipError_t launch_linear_fwd(const LinearArgs& a, int dtype, hipStream_t s);
 hipError_t launch_linear_bwd(const LinearArgs& a, int dtype, hipStream_t s);
 size_t linear_fwd_workspace(int64_t rows, int N, int K, int dtype);
-size_t linear_bwd_workspace(int64_t rows, int N, int K, int dtype);
+size_t linear_bwd_workspace(int64_t rows, int N, int K, int act, int dtype);
 int linear_form_name(const LinearArgs& a, int dtype, int which, char* buf, size_t n);  // as snprintf; which: out, dx, dw
 
 // The norms around a block, forward and backward.

@@ -104,11 +104,14 @@ enum ProductLayout { LAYOUT_NT, LAYOUT_NN, LAYOUT_TN };  // which operand lies a
 hipError_t launch_product_f16(const ProductArgs& g, const LinearOut& e, ProductLayout layout, ProductForm form, int splits, hipStream_t s);
 hipError_t launch_product_bf16(const ProductArgs& g, const LinearOut& e, ProductLayout layout, ProductForm form, int splits, hipStream_t s);
 hipError_t launch_product_f32(const ProductArgs& g, const LinearOut& e, ProductLayout layout, ProductForm form, int splits, hipStream_t s);
+// ... of a first operand in two parts (LAYOUT_NN and LAYOUT_TN: the gradients behind GELU and SiLU).
+hipError_t launch_product_parts_f16(const ProductArgs& g, const LinearOut& e, ProductLayout layout, ProductForm form, int splits, hipStream_t s);
+hipError_t launch_product_parts_bf16(const ProductArgs& g, const LinearOut& e, ProductLayout layout, ProductForm form, int splits, hipStream_t s);
 
-template <int DT, typename T, bool A_ACROSS, bool B_ACROSS, bool DIRECT, typename Epi>
+template <int DT, typename T, bool A_ACROSS, bool B_ACROSS, bool DIRECT, typename Epi, bool PARTS = false>
 hipError_t launch_product_tiles(ProductArgs g, const typename Epi::Args& e, int batch, int splits, hipStream_t s)
 {
-    const void* f = (const void*)product_kernel<DT, T, A_ACROSS, B_ACROSS, DIRECT, Epi>;
+    const void* f = (const void*)product_kernel<DT, T, A_ACROSS, B_ACROSS, DIRECT, Epi, PARTS>;
     const hipError_t err = ensure_dynamic_lds(f, T::LDS);
     if (err != hipSuccess) return err;
     g.tiles_n = (int)((g.N + T::BN - 1) / T::BN);
@@ -121,21 +124,21 @@ hipError_t launch_product_tiles(ProductArgs g, const typename Epi::Args& e, int 
         p.a += A_ACROSS ? skip : skip * g.lda;
         p.tiles_m = (int)((p.M + T::BT - 1) / T::BT);
         const unsigned tiles = Epi::SYMMETRIC ? (unsigned)((int64_t)p.tiles_m * (p.tiles_m + 1) / 2) : (unsigned)p.tiles_m * (unsigned)p.tiles_n;
-        hipLaunchKernelGGL((product_kernel<DT, T, A_ACROSS, B_ACROSS, DIRECT, Epi>), dim3(tiles * (unsigned)splits, (unsigned)batch), dim3(T::NT), T::LDS, s, p, e);
+        hipLaunchKernelGGL((product_kernel<DT, T, A_ACROSS, B_ACROSS, DIRECT, Epi, PARTS>), dim3(tiles * (unsigned)splits, (unsigned)batch), dim3(T::NT), T::LDS, s, p, e);
     }
     return hipGetLastError();
 }
 
-template <int DT, bool A_ACROSS, bool B_ACROSS, typename Epi>
+template <int DT, bool A_ACROSS, bool B_ACROSS, typename Epi, bool PARTS = false>
 hipError_t launch_product_form(const ProductArgs& g, const typename Epi::Args& e, ProductForm form, int batch, int splits, hipStream_t s)
 {
     switch (form) {
-        case P64: return launch_product_tiles<DT, Tile64, A_ACROSS, B_ACROSS, true, Epi>(g, e, batch, splits, s);
-        case P128: return launch_product_tiles<DT, Tile128, A_ACROSS, B_ACROSS, true, Epi>(g, e, batch, splits, s);
-        case P256: return launch_product_tiles<DT, Tile256, A_ACROSS, B_ACROSS, true, Epi>(g, e, batch, splits, s);
-        case P192: return launch_product_tiles<DT, Tile192, A_ACROSS, B_ACROSS, true, Epi>(g, e, batch, splits, s);
-        case P64_ANY: return launch_product_tiles<DT, Tile64Any, A_ACROSS, B_ACROSS, false, Epi>(g, e, batch, splits, s);
-        default: return launch_product_tiles<DT, Tile128, A_ACROSS, B_ACROSS, false, Epi>(g, e, batch, splits, s);
+        case P64: return launch_product_tiles<DT, Tile64, A_ACROSS, B_ACROSS, true, Epi, PARTS>(g, e, batch, splits, s);
+        case P128: return launch_product_tiles<DT, Tile128, A_ACROSS, B_ACROSS, true, Epi, PARTS>(g, e, batch, splits, s);
+        case P256: return launch_product_tiles<DT, Tile256, A_ACROSS, B_ACROSS, true, Epi, PARTS>(g, e, batch, splits, s);
+        case P192: return launch_product_tiles<DT, Tile192, A_ACROSS, B_ACROSS, true, Epi, PARTS>(g, e, batch, splits, s);
+        case P64_ANY: return launch_product_tiles<DT, Tile64Any, A_ACROSS, B_ACROSS, false, Epi, PARTS>(g, e, batch, splits, s);
+        default: return launch_product_tiles<DT, Tile128, A_ACROSS, B_ACROSS, false, Epi, PARTS>(g, e, batch, splits, s);
     }
 }
 
@@ -145,5 +148,9 @@ hipError_t launch_product_form(const ProductArgs& g, const typename Epi::Args& e
         case LAYOUT_NN: return launch<DT, false, true, Epi>(g, arg, form, 1, splits, s);           \
         default: return launch<DT, true, true, Epi>(g, arg, form, 1, splits, s);                   \
     }
+
+#define CONVFWD_PARTS_LAYOUTS(launch, DT, Epi)                                                       \
+    return layout == LAYOUT_NN ? launch<DT, false, true, Epi, true>(g, arg, form, 1, splits, s)      \
+                               : launch<DT, true, true, Epi, true>(g, arg, form, 1, splits, s);
 
 }  // namespace convfwd

@@ -203,10 +203,11 @@ __global__ __launch_bounds__(256) void linear_join(LinearOut e, const float* par
 // The gradient at the sum: dz = dout act'(pre), with its sums over the rows.  A workgroup has 256 columns and `each` rows, eight lanes of
 // rows; the sums are of the values before they are rounded.
 // Bound by memory: 200704 x 768 fp16 with GELU 194 us, 4.8 TB/s of two tensors read and one written.
-// TO: whether dz is written, in the storage type with the row stride ldz.
-template <int DT, bool TO>
+// TO: whether dz is written, with the row stride ldz: 1 in the storage type, where that holds it (no activation, or ReLU's, whose slopes are 0 and 1); 2 in two
+// parts, the low one `plane` elements behind the high one.  (In one part a gradient behind GELU was off by 1.4 times its own rounding, and an fp16 dz could become an infinity or zero.)
+template <int DT, int TO>
 __global__ __launch_bounds__(256) void linear_dz(const void* dout, const void* pre, int64_t ld, int64_t rows, int N, int act, void* dz, int64_t ldz,
-                                                 float* sums, int64_t each)
+                                                 int64_t plane, float* sums, int64_t each)
 {
     __shared__ float lds[8][32 * 8 + 8];
     const int col = threadIdx.x & 31, r = threadIdx.x >> 5;
@@ -231,7 +232,14 @@ __global__ __launch_bounds__(256) void linear_dz(const void* dout, const void* p
                 if (k >= have) v[k] = 0.0f;
                 sum[k] += v[k];
             }
-            if constexpr (TO) put8<DT>(dz, t * ldz + j, v, (int)min((int64_t)8, ldz - j));
+            const int room = (int)min((int64_t)8, ldz - j);
+            if constexpr (TO == 1) put8<DT>(dz, t * ldz + j, v, room);
+            if constexpr (TO == 2) {
+                float high[8], low[8];
+                Parts<DT>::split(v, high, low);
+                put8<DT>(dz, t * ldz + j, high, room);
+                put8<DT>(dz, plane + t * ldz + j, low, room);
+            }
         }
     }
     if (!sums) return;
@@ -279,7 +287,7 @@ constexpr int64_t kLongStride = 1 << 22;  // from here on a tile's offsets may p
 int64_t round_up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 
 // Tiles, and what a launch of them is expected to take, in us: `once` and for every round of 256 tiles `own` and `step` for every 64 of the
-// reduction.
+// reduction and every part of the first operand.
 struct TileCost {
     int bt, bn;
     double once, own, step;
@@ -295,7 +303,7 @@ struct ProductPlan {
     ProductForm rest;
     int rest_splits;
 };
-ProductPlan plan_product(int64_t M, int64_t N, int64_t K, int dtype, bool direct, bool whole = false)
+ProductPlan plan_product(int64_t M, int64_t N, int64_t K, int dtype, bool direct, int parts = 1, bool whole = false)
 {
     ProductPlan best = {P64, 1, 1e30, M, P64, 1};
     const int64_t ksteps = (K + 63) / 64;
@@ -308,7 +316,7 @@ ProductPlan plan_product(int64_t M, int64_t N, int64_t K, int dtype, bool direct
             if (splits > 1 && (splits * 4 > ksteps || tiles * splits > 2048)) break;
             const int64_t each = (ksteps + splits - 1) / splits;
             const int shares = (int)((ksteps + each - 1) / each);  // none without a step
-            double us = c.once + std::ceil(tiles * shares / 256) * (c.own + each * c.step);
+            double us = c.once + std::ceil(tiles * shares / 256) * (c.own + parts * each * c.step);
             if (shares > 1) us += 5 + 8.0 * shares * M * N / 4e6;  // written, read and added by a second launch
             if (us < best.us) best = {(ProductForm)f, shares, us, M, P64, 1};
         }
@@ -316,8 +324,8 @@ ProductPlan plan_product(int64_t M, int64_t N, int64_t K, int dtype, bool direct
         // three rounds and 20 tiles).
         const int64_t rounds = (int64_t)(tiles / 256), first = rounds * 256 / tn;
         if (whole || rounds < 1 || rounds > 16 || first < 1 || first >= tm) continue;
-        const ProductPlan rest = plan_product(M - first * c.bt, N, K, dtype, direct, true);
-        const double us = c.once + rounds * (c.own + ksteps * c.step) + rest.us;
+        const ProductPlan rest = plan_product(M - first * c.bt, N, K, dtype, direct, parts, true);
+        const double us = c.once + rounds * (c.own + parts * ksteps * c.step) + rest.us;
         if (us < best.us) best = {(ProductForm)f, 1, us, first * c.bt, rest.form, rest.splits};
     }
     return best;
@@ -390,18 +398,20 @@ hipError_t join(int dtype, const LinearOut& e, const float* partial, int64_t row
                              : dtype == CONV_F16 ? join_as<CONV_F16>(e, partial, rows, N, splits, s) : join_as<CONV_BF16>(e, partial, rows, N, splits, s);
 }
 
-// C = A B, in one launch or two, and the join where a reduction is shared.
+// C = A B, in one launch or two, and the join where a reduction is shared.  plane: where A's low part is, 0 if it has one part.
 struct Factor {
     const void* p;
-    int64_t ld;
+    int64_t ld, plane = 0;
 };
 hipError_t multiply(int dtype, ProductLayout layout, const Factor& a, const Factor& b, int64_t M, int64_t N, int64_t K, const LinearOut& e,
                     const ProductPlan& plan, float* partial, hipStream_t s)
 {
     ProductArgs g = {};
     g.a = (const uint16_t*)a.p, g.b = (const uint16_t*)b.p, g.lda = a.ld, g.ldb = b.ld, g.M = M, g.N = N, g.K = K, g.partial = partial;
-    g.ksteps = (int)((K + 63) / 64);
-    const auto launch = dtype == CONV_F32 ? launch_product_f32 : dtype == CONV_F16 ? launch_product_f16 : launch_product_bf16;
+    g.ksteps = (int)((K + 63) / 64), g.plane_a = a.plane;
+    const auto launch = dtype == CONV_F32   ? launch_product_f32
+                        : dtype == CONV_F16 ? (a.plane ? launch_product_parts_f16 : launch_product_f16)
+                                            : (a.plane ? launch_product_parts_bf16 : launch_product_bf16);
     g.M = plan.rows;
     hipError_t err = launch(g, e, layout, plan.form, plan.splits, s);
     if (err == hipSuccess && plan.splits > 1) err = join(dtype, e, partial, g.M, (int)N, plan.splits, s);
@@ -483,8 +493,12 @@ int dz_parts(int64_t rows, int N) { return rows == 0 ? 0 : (int)((rows + dz_rows
 // Rows of dz start on lines of 128 bytes in 16-bit types: a step's 128 bytes of a row would lie in two.
 int64_t dz_stride(int N, int dtype) { return dtype == CONV_F32 ? N : round_up(N, 64); }
 
+// Parts of dz: two where the activation's slope is none of 0 and 1.
+int dz_parts_of(int act, int dtype) { return dtype != CONV_F32 && act >= ACT_GELU ? 2 : 1; }
+
 struct BwdSpace {
     void* dz;
+    int64_t plane;  // elements of a part
     float *sums, *partial;
     size_t bytes;
 };
@@ -493,12 +507,14 @@ BwdSpace bwd_space(const LinearArgs& a, int dtype, void* ws)
 {
     BwdSpace s = {};
     Carve c(ws);
-    s.dz = c.take((size_t)(a.rows * dz_stride(a.N, dtype)) * dtype_size(dtype));
+    const int parts = dz_parts_of(a.act, dtype);
+    s.plane = a.rows * dz_stride(a.N, dtype);
+    s.dz = c.take((size_t)parts * s.plane * dtype_size(dtype));
     s.sums = (float*)c.take((size_t)dz_parts(a.rows, a.N) * a.N * 4);
     size_t most = 0;
     for (const bool direct : {true, false}) {
-        most = std::max(most, partial_bytes(plan_product(a.rows, a.K, a.N, dtype, direct), a.rows, a.K));
-        most = std::max(most, partial_bytes(plan_product(a.N, a.K, a.rows, dtype, direct), a.N, a.K));
+        most = std::max(most, partial_bytes(plan_product(a.rows, a.K, a.N, dtype, direct, parts), a.rows, a.K));
+        most = std::max(most, partial_bytes(plan_product(a.N, a.K, a.rows, dtype, direct, parts), a.N, a.K));
     }
     s.partial = (float*)c.take(most);
     s.bytes = c.used;
@@ -506,14 +522,14 @@ BwdSpace bwd_space(const LinearArgs& a, int dtype, void* ws)
 }
 
 template <int DT>
-hipError_t launch_dz(const LinearArgs& a, void* dz, int64_t ldz, float* sums, hipStream_t s)
+hipError_t launch_dz(const LinearArgs& a, void* dz, int64_t ldz, int64_t plane, float* sums, hipStream_t s)
 {
     const int64_t each = dz_rows(a.rows, a.N);
     const int parts = dz_parts(a.rows, a.N);
     const dim3 grid((unsigned)(((dz ? ldz : a.N) + 255) / 256), (unsigned)parts);
     float* const at = !a.dbias ? nullptr : parts == 1 ? a.dbias : sums;
-    if (dz) hipLaunchKernelGGL((linear_dz<DT, true>), grid, dim3(256), 0, s, a.dout, a.pre_in, a.ldo, a.rows, a.N, a.act, dz, ldz, at, each);
-    else hipLaunchKernelGGL((linear_dz<DT, false>), grid, dim3(256), 0, s, a.dout, a.pre_in, a.ldo, a.rows, a.N, a.act, dz, ldz, at, each);
+    const auto kernel = !dz ? linear_dz<DT, 0> : plane && DT != CONV_F32 ? linear_dz<DT, DT == CONV_F32 ? 1 : 2> : linear_dz<DT, 1>;
+    hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, a.dout, a.pre_in, a.ldo, a.rows, a.N, a.act, dz, ldz, plane, at, each);
     if (a.dbias && parts > 1) hipLaunchKernelGGL(linear_sums, dim3((unsigned)((a.N + 31) / 32)), dim3(1024), 0, s, sums, parts, a.N, a.dbias);
     return hipGetLastError();
 }
@@ -534,11 +550,11 @@ size_t linear_fwd_workspace(int64_t rows, int N, int K, int dtype)
     }
     return most;
 }
-size_t linear_bwd_workspace(int64_t rows, int N, int K, int dtype)
+size_t linear_bwd_workspace(int64_t rows, int N, int K, int act, int dtype)
 {
     if (rows == 0) return 0;
     LinearArgs a = {};
-    a.rows = rows, a.N = N, a.K = K;
+    a.rows = rows, a.N = N, a.K = K, a.act = act;
     return bwd_space(a, dtype, nullptr).bytes;
 }
 
@@ -567,20 +583,21 @@ hipError_t launch_linear_bwd(const LinearArgs& a, int dtype, hipStream_t s)
     Factor dz = {a.dout, a.ldo};
     // dout is dz where there is no activation and its rows start on 16 bytes (in fp32 anywhere)
     const bool make = (a.dx || a.dw) && (a.act || (dtype != CONV_F32 && !on_16(a.dout, a.ldo, es)));
-    if (make) dz = {space.dz, dz_stride(a.N, dtype)};
+    const int parts = dz_parts_of(a.act, dtype);
+    if (make) dz = {space.dz, dz_stride(a.N, dtype), parts == 2 ? space.plane : 0};
     if (make || a.dbias) {
         void* const to = make ? space.dz : nullptr;
-        const hipError_t e = dtype == CONV_F32 ? launch_dz<CONV_F32>(a, to, dz.ld, space.sums, s)
-                                               : dtype == CONV_F16 ? launch_dz<CONV_F16>(a, to, dz.ld, space.sums, s) : launch_dz<CONV_BF16>(a, to, dz.ld, space.sums, s);
+        const hipError_t e = dtype == CONV_F32 ? launch_dz<CONV_F32>(a, to, dz.ld, dz.plane, space.sums, s)
+                                               : dtype == CONV_F16 ? launch_dz<CONV_F16>(a, to, dz.ld, dz.plane, space.sums, s) : launch_dz<CONV_BF16>(a, to, dz.ld, dz.plane, space.sums, s);
         if (e != hipSuccess) return e;
     }
     if (a.dx) {
-        const ProductPlan p = plan_product(a.rows, a.K, a.N, dtype, on_16(w.p, w.ld, es) && on_16(dz.p, dz.ld, es));
+        const ProductPlan p = plan_product(a.rows, a.K, a.N, dtype, on_16(w.p, w.ld, es) && on_16(dz.p, dz.ld, es), parts);
         const hipError_t e = multiply(dtype, LAYOUT_NN, dz, w, a.rows, a.K, a.N, {nullptr, nullptr, nullptr, a.dx, 0, a.ldx, ACT_NONE}, p, space.partial, s);
         if (e != hipSuccess) return e;
     }
     if (a.dw) {
-        const ProductPlan p = plan_product(a.N, a.K, a.rows, dtype, on_16(x.p, x.ld, es) && on_16(dz.p, dz.ld, es));
+        const ProductPlan p = plan_product(a.N, a.K, a.rows, dtype, on_16(x.p, x.ld, es) && on_16(dz.p, dz.ld, es), parts);
         const hipError_t e = multiply(dtype, LAYOUT_TN, dz, x, a.N, a.K, a.rows, {nullptr, nullptr, nullptr, a.dw, 0, a.ldw, ACT_NONE}, p, space.partial, s);
         if (e != hipSuccess) return e;
     }
@@ -592,6 +609,7 @@ int linear_form_name(const LinearArgs& a, int dtype, int which, char* buf, size_
     static const char* const tiles[] = {"tile64x64", "tile128x128", "tile256x256", "tile192x192", "tile64x64_any", "tile128x128_any"};
     const int es = dtype_size(dtype);
     const bool x16 = on_16(a.x, a.ldx, es), w16 = on_16(a.w, a.ldw, es);
+    const int parts = which ? dz_parts_of(a.act, dtype) : 1;
     ProductPlan p;
     if (which == 0) {
         const LinearForm f = form_of(a.rows, a.N, a.K, dtype, x16 && w16);
@@ -601,13 +619,13 @@ int linear_form_name(const LinearArgs& a, int dtype, int which, char* buf, size_
         }
         p = f.tiles;
     } else if (which == 1) {
-        p = plan_product(a.rows, a.K, a.N, dtype, w16);
+        p = plan_product(a.rows, a.K, a.N, dtype, w16, parts);
     } else {
-        p = plan_product(a.N, a.K, a.rows, dtype, x16);
+        p = plan_product(a.N, a.K, a.rows, dtype, x16, parts);
     }
     auto one = [&](char* to, size_t room, ProductForm form, int splits) {
         const char* const name = dtype == CONV_F32 && form == P256 ? "tile256x128" : tiles[form];
-        const char* const kind = dtype == CONV_F32 ? "split_" : "";
+        const char* const kind = dtype == CONV_F32 ? "split_" : parts == 2 ? "parts_" : "";
         return splits > 1 ? std::snprintf(to, room, "%s%s_split%d", kind, name, splits) : std::snprintf(to, room, "%s%s", kind, name);
     };
     const int len = one(buf, n, p.form, p.splits);

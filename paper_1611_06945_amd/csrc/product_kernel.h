@@ -15,6 +15,9 @@
 //     bytes past K belong to what follows and are cleared in both operands on the last step.  Otherwise pieces go
 //     through registers, from any address, and their ends are cleared on the way.
 //   * Operands may be sums of two planes, high and low (PL = 2), of which a step multiplies low x high, high x low and high x high.
+//   * PARTS: A alone is a sum of two planes, what the storage type holds of it and what is left (Parts).  The reduction is gone through twice, for the low
+//     plane first, whose sums are scaled before those of the high one are added to them: LDS has no room for a third plane beside the largest tiles.  (The
+//     code of both passes is laid out: in a loop the tiles of 256 x 256 spilled some 30 registers.)
 // Bound by the matrix units and LDS together: a step of a tile of 256 x 256 takes 2048 clocks of products and 2048 of LDS, 1536 reading and 512 written to, so waves of
 // 64 x 128 with two a SIMD, each's products between the reads of its next operands.  8192 x 4096 x 8192 bf16 with GELU and the sum kept 475 to 483 us, 1.14 PFLOP/s, matrix
 // units busy 52 % of the clocks (the end of a tile, 45 us in all, has none); four waves of 128 x 128 with one a SIMD took 141 us for 4096 x 4096 x 4096 where this takes 100.
@@ -286,6 +289,23 @@ struct Operand<T, W, L, ACROSS, false> {
     static __device__ __forceinline__ u32x4 fragment(const char* lds, int block, int s) { return fragment_of<W, ACROSS>(lds, block, s); }
 };
 
+// A value v in two elements of a 16-bit type: high of v HIGH, low of what is left of that times LOW.  bf16 has fp32's exponents and needs neither
+// factor.  fp16: half of the largest value times the largest slope of an activation, 1.13, is no infinity yet, and what is left of a value that fp16 holds as a denormal
+// number or not at all is kept down to 2^-36.
+template <int DT>
+struct Parts {
+    static constexpr float HIGH = DT == CONV_F16 ? 0.5f : 1.0f, LOW = DT == CONV_F16 ? 0x1p11f : 1.0f;
+    static __device__ __forceinline__ void split(const float (&v)[8], float (&high)[8], float (&low)[8])
+    {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const float x = v[k] * HIGH;
+            high[k] = Prec<DT>::to_f32(Prec<DT>::from_f32(x));
+            low[k] = fabsf(high[k]) < INFINITY ? (x - high[k]) * LOW : 0.0f;  // an infinity stays one; a NaN is in the high part
+        }
+    }
+};
+
 struct ProductArgs {
     const uint16_t *a, *b;
     int64_t lda, ldb;             // of operands, in elements of 16 bits
@@ -344,7 +364,7 @@ __device__ __forceinline__ void eight_in_a_row(const f32x4& first, const f32x4& 
 }
 
 // Epi: what becomes of the sums.  symmetric: only the tiles with n >= m are formed.
-template <int DT, typename T, bool A_ACROSS, bool B_ACROSS, bool DIRECT, typename Epi>
+template <int DT, typename T, bool A_ACROSS, bool B_ACROSS, bool DIRECT, typename Epi, bool PARTS>
 __global__ __launch_bounds__(T::NT) void product_kernel(ProductArgs g, typename Epi::Args e)
 {
     extern __shared__ __attribute__((aligned(16))) char smem[];
@@ -360,8 +380,11 @@ __global__ __launch_bounds__(T::NT) void product_kernel(ProductArgs g, typename 
 
     Operand<T, T::BT, T::LA, A_ACROSS, DIRECT> a;
     Operand<T, T::BN, T::LW, B_ACROSS, DIRECT> b;
-    a.begin(g.a + blockIdx.y * g.batch_a, g.lda, g.plane_a, g.K, m0, g.M, (int64_t)ks0 * T::KE);
-    b.begin(g.b + blockIdx.y * g.batch_b, g.ldb, g.plane_b, g.K, n0, g.N, (int64_t)ks0 * T::KE);
+    auto begin = [&](int64_t plane) {
+        a.begin(g.a + blockIdx.y * g.batch_a + plane, g.lda, g.plane_a, g.K, m0, g.M, (int64_t)ks0 * T::KE);
+        b.begin(g.b + blockIdx.y * g.batch_b, g.ldb, g.plane_b, g.K, n0, g.N, (int64_t)ks0 * T::KE);
+    };
+    begin(PARTS ? g.plane_a : 0);
     float* const bias = (float*)(smem + T::S * T::STAGE);
     Epi::prepare(e, bias, n0, b.here, T::BN, T::NT);
 
@@ -401,136 +424,154 @@ __global__ __launch_bounds__(T::NT) void product_kernel(ProductArgs g, typename 
     typedef std::integral_constant<int, 0> First;
     typedef std::integral_constant<int, PHASES - 1> Last;
 
-    if constexpr (DIRECT) {
-        int ks = ks0;  // the next step to load
-        auto load = [&](int buf) {
-            char* const to = smem + buf * T::STAGE;
-            a.load(to, ks < ks1);
-            b.load(to + T::PL * T::PLANE_A, ks < ks1);
-            ++ks;
-            a.advance(), b.advance();
-        };
+    auto multiply_all = [&]() {
+        if constexpr (DIRECT) {
+            int ks = ks0;  // the next step to load
+            auto load = [&](int buf) {
+                char* const to = smem + buf * T::STAGE;
+                a.load(to, ks < ks1);
+                b.load(to + T::PL * T::PLANE_A, ks < ks1);
+                ++ks;
+                a.advance(), b.advance();
+            };
 
-        // Order of a phase of many products: after every few one of its LDS reads, then one of its loads, so that products begin at
-        // once.  With few products the reads come first, or they would be late.
-        constexpr bool MIXED = T::HB * T::FN * (2 * T::PL - 1) >= 16;
-        constexpr int READS_A = T::PL * T::HB * (A_ACROSS ? 2 : 1), READS_B = T::PL * T::FN * (B_ACROSS ? 2 : 1);
-        auto interleave = [&](auto reads, auto loads) {
-            constexpr int R = decltype(reads)::value, L = decltype(loads)::value, M = T::HB * T::FN * (2 * T::PL - 1), EACH = MIXED ? M / (R + L) : 1;
-            if constexpr (MIXED && EACH > 0) {
-                count_to<R>([&](auto) {
-                    __builtin_amdgcn_sched_group_barrier(0x008, EACH, 0);  // products
-                    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);     // an LDS read
-                });
-                count_to<L>([&](auto) {
-                    __builtin_amdgcn_sched_group_barrier(0x008, EACH, 0);
-                    __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);     // a load
-                });
-                if constexpr (M > EACH * (R + L)) __builtin_amdgcn_sched_group_barrier(0x008, M - EACH * (R + L), 0);
-            }
-            __builtin_amdgcn_sched_barrier(0);
-        };
-        auto reads_first = [&]() {
-            if constexpr (!MIXED) __builtin_amdgcn_sched_barrier(0);
-        };
-        // Steps past the last are asked for as well, without a byte in range, so that the count of loads on their way is always the same.
+            // Order of a phase of many products: after every few one of its LDS reads, then one of its loads, so that products begin at
+            // once.  With few products the reads come first, or they would be late.
+            constexpr bool MIXED = T::HB * T::FN * (2 * T::PL - 1) >= 16;
+            constexpr int READS_A = T::PL * T::HB * (A_ACROSS ? 2 : 1), READS_B = T::PL * T::FN * (B_ACROSS ? 2 : 1);
+            auto interleave = [&](auto reads, auto loads) {
+                constexpr int R = decltype(reads)::value, L = decltype(loads)::value, M = T::HB * T::FN * (2 * T::PL - 1), EACH = MIXED ? M / (R + L) : 1;
+                if constexpr (MIXED && EACH > 0) {
+                    count_to<R>([&](auto) {
+                        __builtin_amdgcn_sched_group_barrier(0x008, EACH, 0);  // products
+                        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);     // an LDS read
+                    });
+                    count_to<L>([&](auto) {
+                        __builtin_amdgcn_sched_group_barrier(0x008, EACH, 0);
+                        __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);     // a load
+                    });
+                    if constexpr (M > EACH * (R + L)) __builtin_amdgcn_sched_group_barrier(0x008, M - EACH * (R + L), 0);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            };
+            auto reads_first = [&]() {
+                if constexpr (!MIXED) __builtin_amdgcn_sched_barrier(0);
+            };
+            // Steps past the last are asked for as well, without a byte in range, so that the count of loads on their way is always the same.
 #pragma unroll
-        for (int k = 0; k < T::S; ++k) load(k);
-        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((T::S - 1) * LOADS) : "memory");
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
-        fetch(0, First());
-        int buf = 0;
-        for (int k = 0; k < steps - 1; ++k) {
-            count_to<PHASES - 1>([&](auto p) {
-                fetch(buf, std::integral_constant<int, decltype(p)::value + 1>());
-                reads_first();
-                products(p);
-                interleave(std::integral_constant<int, READS_A + ((decltype(p)::value + 1) % T::H == 0 ? READS_B : 0)>(), std::integral_constant<int, 0>());
-            });
-            // this wave's loads of the next stage have landed and its reads of the present one are done; then so are everybody's
-            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((T::S - 2) * LOADS) : "memory");
+            for (int k = 0; k < T::S; ++k) load(k);
+            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((T::S - 1) * LOADS) : "memory");
             __builtin_amdgcn_s_barrier();
             asm volatile("" ::: "memory");
-            const int next = buf + 1 == T::S ? 0 : buf + 1;
-            fetch(next, First());
-            load(buf);
-            reads_first();
-            products(Last());
-            interleave(std::integral_constant<int, READS_A + READS_B>(), std::integral_constant<int, LOADS>());
-            buf = next;
-        }
-        const int tail = ks1 < g.ksteps ? T::KE : (int)(g.K - (int64_t)(g.ksteps - 1) * T::KE);
-        count_to<PHASES>([&](auto p) {
-            constexpr int q = decltype(p)::value, s = q / T::H;
-            if constexpr (q + 1 < PHASES) fetch(buf, std::integral_constant<int, q + 1>());
-            const int left = tail - (s * 4 + (lane >> 4)) * 8;
-            if constexpr (q % T::H == 0 && !B_ACROSS) {
-#pragma unroll
-                for (int i = 0; i < T::PL * T::FN; ++i) bv[s][i / T::FN][i % T::FN] = first_elems(bv[s][i / T::FN][i % T::FN], left);
+            fetch(0, First());
+            int buf = 0;
+            for (int k = 0; k < steps - 1; ++k) {
+                count_to<PHASES - 1>([&](auto p) {
+                    fetch(buf, std::integral_constant<int, decltype(p)::value + 1>());
+                    reads_first();
+                    products(p);
+                    interleave(std::integral_constant<int, READS_A + ((decltype(p)::value + 1) % T::H == 0 ? READS_B : 0)>(), std::integral_constant<int, 0>());
+                });
+                // this wave's loads of the next stage have landed and its reads of the present one are done; then so are everybody's
+                asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((T::S - 2) * LOADS) : "memory");
+                __builtin_amdgcn_s_barrier();
+                asm volatile("" ::: "memory");
+                const int next = buf + 1 == T::S ? 0 : buf + 1;
+                fetch(next, First());
+                load(buf);
+                reads_first();
+                products(Last());
+                interleave(std::integral_constant<int, READS_A + READS_B>(), std::integral_constant<int, LOADS>());
+                buf = next;
             }
-            if constexpr (!A_ACROSS) {
-#pragma unroll
-                for (int j = 0; j < T::PL * T::HB; ++j) av[q & 1][j / T::HB][j % T::HB] = first_elems(av[q & 1][j / T::HB][j % T::HB], left);
-            }
-            products(p);
-        });
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // nothing may land in LDS after the end
-    } else {
-        static_assert(DIRECT || (T::S == 2 && T::PL == 1), "one stage is multiplied, the other written");
-        constexpr int D = decltype(a)::D;
-        static_assert(D % 2 == 0, "step k lies in stage k % 2 and came by slot k % D");
-        auto load = [&](auto slot) { a.pieces.load(a.held[decltype(slot)::value]), b.pieces.load(b.held[decltype(slot)::value]); };
-        auto load_whole = [&](auto slot) { a.template load_whole<decltype(slot)::value>(), b.template load_whole<decltype(slot)::value>(); };
-        auto commit = [&](auto slot, auto whole) {
-            constexpr int S = decltype(slot)::value;
-            char* const to = smem + S % 2 * T::STAGE;
-            a.template commit<S, decltype(whole)::value>(to);
-            b.template commit<S, decltype(whole)::value>(to + T::PLANE_A);
-        };
-        auto multiply = [&](auto slot) {
-            constexpr int BUF = decltype(slot)::value % 2;
-            fetch(BUF, First());
+            const int tail = ks1 < g.ksteps ? T::KE : (int)(g.K - (int64_t)(g.ksteps - 1) * T::KE);
             count_to<PHASES>([&](auto p) {
-                constexpr int q = decltype(p)::value;
-                if constexpr (q + 1 < PHASES) fetch(BUF, std::integral_constant<int, q + 1>());
+                constexpr int q = decltype(p)::value, s = q / T::H;
+                if constexpr (q + 1 < PHASES) fetch(buf, std::integral_constant<int, q + 1>());
+                const int left = tail - (s * 4 + (lane >> 4)) * 8;
+                if constexpr (q % T::H == 0 && !B_ACROSS) {
+#pragma unroll
+                    for (int i = 0; i < T::PL * T::FN; ++i) bv[s][i / T::FN][i % T::FN] = first_elems(bv[s][i / T::FN][i % T::FN], left);
+                }
+                if constexpr (!A_ACROSS) {
+#pragma unroll
+                    for (int j = 0; j < T::PL * T::HB; ++j) av[q & 1][j / T::HB][j % T::HB] = first_elems(av[q & 1][j / T::HB][j % T::HB], left);
+                }
                 products(p);
             });
-        };
-        // Step k is in its stage, steps k + 1 .. k + D on their way.  The first loop's loads are of whole steps, without a branch: behind one that
-        // may load or not a wave waits for all that is on its way.
-        const int whole = min(steps, min(a.pieces.whole(), b.pieces.whole()));
-        int k = 0;
-        if (whole > 2 * D) {
-            count_to<D>(load_whole);
-            commit(First(), std::true_type());
-            load_whole(First());
-            __syncthreads();
-            for (; k + 2 * D < whole; k += D) {
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // nothing may land in LDS after the end
+        } else {
+            static_assert(DIRECT || (T::S == 2 && T::PL == 1), "one stage is multiplied, the other written");
+            constexpr int D = decltype(a)::D;
+            static_assert(D % 2 == 0, "step k lies in stage k % 2 and came by slot k % D");
+            auto load = [&](auto slot) { a.pieces.load(a.held[decltype(slot)::value]), b.pieces.load(b.held[decltype(slot)::value]); };
+            auto load_whole = [&](auto slot) { a.template load_whole<decltype(slot)::value>(), b.template load_whole<decltype(slot)::value>(); };
+            auto commit = [&](auto slot, auto whole) {
+                constexpr int S = decltype(slot)::value;
+                char* const to = smem + S % 2 * T::STAGE;
+                a.template commit<S, decltype(whole)::value>(to);
+                b.template commit<S, decltype(whole)::value>(to + T::PLANE_A);
+            };
+            auto multiply = [&](auto slot) {
+                constexpr int BUF = decltype(slot)::value % 2;
+                fetch(BUF, First());
+                count_to<PHASES>([&](auto p) {
+                    constexpr int q = decltype(p)::value;
+                    if constexpr (q + 1 < PHASES) fetch(BUF, std::integral_constant<int, q + 1>());
+                    products(p);
+                });
+            };
+            // Step k is in its stage, steps k + 1 .. k + D on their way.  The first loop's loads are of whole steps, without a branch: behind one that
+            // may load or not a wave waits for all that is on its way.
+            const int whole = min(steps, min(a.pieces.whole(), b.pieces.whole()));
+            int k = 0;
+            if (whole > 2 * D) {
+                count_to<D>(load_whole);
+                commit(First(), std::true_type());
+                load_whole(First());
+                __syncthreads();
+                for (; k + 2 * D < whole; k += D) {
+                    count_to<D>([&](auto u) {
+                        typedef std::integral_constant<int, (decltype(u)::value + 1) % D> Next;
+                        multiply(u);
+                        commit(Next(), std::true_type());
+                        load_whole(Next());
+                        __syncthreads();
+                    });
+                }
+            } else {
+                count_to<D>(load);
+                commit(First(), std::false_type());
+                load(First());
+                __syncthreads();
+            }
+            while (k < steps) {
                 count_to<D>([&](auto u) {
                     typedef std::integral_constant<int, (decltype(u)::value + 1) % D> Next;
+                    if (k >= steps) return;
                     multiply(u);
-                    commit(Next(), std::true_type());
-                    load_whole(Next());
+                    if (++k < steps) commit(Next(), std::false_type());
+                    load(Next());  // (past the last step: nothing)
                     __syncthreads();
                 });
             }
-        } else {
-            count_to<D>(load);
-            commit(First(), std::false_type());
-            load(First());
-            __syncthreads();
         }
-        while (k < steps) {
-            count_to<D>([&](auto u) {
-                typedef std::integral_constant<int, (decltype(u)::value + 1) % D> Next;
-                if (k >= steps) return;
-                multiply(u);
-                if (++k < steps) commit(Next(), std::false_type());
-                load(Next());  // (past the last step: nothing)
-                __syncthreads();
-            });
-        }
+    };
+    auto scale = [&](float by) {
+#pragma unroll
+        for (int i = 0; i < T::FN; ++i)
+#pragma unroll
+            for (int j = 0; j < T::FT; ++j) acc[i][j] *= by;
+    };
+    if constexpr (PARTS) {
+        multiply_all();
+        scale(1.0f / Parts<DT>::LOW);
+        __syncthreads();  // every wave has read its last operands before others land in their place
+        begin(0);
+        multiply_all();
+        if constexpr (Parts<DT>::HIGH != 1.0f) scale(1.0f / Parts<DT>::HIGH);
+    } else {
+        multiply_all();
     }
 
     const int grp = lane >> 4;

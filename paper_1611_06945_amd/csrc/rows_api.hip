@@ -327,7 +327,7 @@ int linear_fwd(const linear_desc* desc, const void* x, const void* w, const floa
 
 size_t linear_bwd_workspace_bytes(const linear_desc* desc)
 {
-    return check_linear(desc) ? 0 : linear_bwd_workspace(desc->rows, desc->N, desc->K, desc->dtype);
+    return check_linear(desc) ? 0 : linear_bwd_workspace(desc->rows, desc->N, desc->K, linear_args(desc).act, desc->dtype);
 }
 
 int linear_bwd(const linear_desc* desc, const void* x, const void* w, const void* pre, const void* dout, void* dx, void* dw, float* dbias,
@@ -342,7 +342,7 @@ int linear_bwd(const linear_desc* desc, const void* x, const void* w, const void
     if (desc->rows > 0) {
         if (!dout || (dw && !x) || (dx && !w) || (a.act && !pre)) return CONV_EINVAL;
         if (overlaps({dx, dw, dbias}, {x, w, pre, dout})) return CONV_EINVAL;
-        const size_t need = linear_bwd_workspace(desc->rows, desc->N, desc->K, desc->dtype);
+        const size_t need = linear_bwd_workspace(desc->rows, desc->N, desc->K, linear_args(desc).act, desc->dtype);
         if (need && (!workspace || workspace_bytes < need)) return CONV_EWORKSPACE;
         if (!aligned(workspace, 16)) return CONV_EINVAL;
     }
