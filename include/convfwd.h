@@ -548,8 +548,8 @@ int residual_norm_bwd(const residual_norm_desc* desc, const void* r_out, const v
  *   X = x / (|x| + eps), |x| the root of the sum of the squares;  `steps` times  X <- a X + (b X X^T + c (X X^T)^2) X;  out = X.
  * The polynomial a s + b s^3 + c s^5 moves every singular value s of X towards one; e.g. 3.4445, -4.7750, 2.0315 and five steps.  Coefficients have to keep
  * the elements of X and of b X X^T + c (X X^T)^2 below 15 (any that keep the singular values below 1.5 with |b|, |c| <= 5 do); beyond, results may be infinite or NaN.
- * X is held in 22 bits or more and multiplied in fp16 with fp32 sums, in two parts of 11 bits (results off by some 2e-6 of their norm before the rounding to
- * the type), for bf16 in one part where the steps leave them off by less than the rounding to the type is (1.7e-3).  A matrix with a NaN or an infinity gives NaN; one of zeros stays zero where eps > 0.
+ * X is held in 22 bits or more and multiplied in two fp16 parts of 11 bits each with fp32 sums: results are off by some 2e-6 of their norm before the rounding to the type.  A
+ * matrix with a NaN or an infinity gives NaN; one of zeros stays zero where eps > 0.
  * Matrix i starts stride_x (stride_o) elements behind matrix i - 1, its rows ldx (ldo) apart; out may be x where the strides are the same.  `workspace`:
  * orthogonalize_workspace_bytes(desc), 16-byte aligned, CONV_EWORKSPACE if it is smaller.  batch = 0 enqueues nothing.
  * CONV_EINVAL for batch < 0 or >= 2^31, rows or cols outside [1, 2^20] or both above 2^17, steps outside [1, 100], strides below a row's length, matrices that overlap in out (stride_o below

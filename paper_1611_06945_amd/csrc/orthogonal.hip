@@ -7,8 +7,10 @@
 // 2^12 (X, A and B are small whole numbers at most and their elements of the size 1 / sqrt(n): scaled they keep all their bits).
 //   * X itself is kept in more bits than it is multiplied in: weak directions grow by a in every step, and so would the roundings of an X kept in 16
 //     bits (a matrix of rank n / 8 in bf16: 3 % off, against 0.08 %).  The errors of A, B and the X that B multiplies do not grow like that.
-//   * bf16: the products take one fp16 plane of each operand, which has three bits more than the result, where that is enough (planes_of).  Others: two
-//     planes, high and low, and three of their four products, 22 bits.
+//   * The products take two planes of each operand, high and low, and three of their four products: 22 bits.  One plane, 11 bits, is three times as fast, but leaves a
+//     bf16 result off by up to 2.1 times its own rounding, most where all singular values are alike (orthonormal 141 x 141 in five steps; normal ones 1.5; some strong directions
+//     above weak ones 1.1 to 1.3), and the steps' slopes let errors of early steps grow in late ones.  Even the first step alone in one plane counts where one
+//     direction is nearly all of x (700 x 700 of rank one 1.15).
 //   * Bound by the products where there are tiles for all CUs (4096 x 4096 bf16, five steps: 72, 75 and 134 us for the three products of a step, 1387 in all, 0.99 PFLOP/s), by
 //     17 launches one after the other where there are not (24 of 192 x 768 fp32: 11, 7 and 23 us a step, 215 in all).
 //   * X beside its products: fp32 for fp32; for 16-bit types the high and the low plane together, 22 bits, which is less to read and write.
@@ -38,20 +40,16 @@ __device__ __forceinline__ void split2(const float (&v)[8], float (&hi)[8], floa
         hi[k] = Prec<CONV_F16>::to_f32(h), lo[k] = v[k] - hi[k];
     }
 }
-__device__ __forceinline__ void put_scaled(const Planes& to, int planes, int64_t row, int64_t col, const float (&v)[8], int have)
+__device__ __forceinline__ void put_scaled(const Planes& to, int64_t row, int64_t col, const float (&v)[8], int have)
 {
     uint16_t* const p = to.p + blockIdx.y * to.batch;
-    if (planes == 1) {
-        put8<CONV_F16>(p, row * to.ld + col, v, have);
-    } else {
-        float hi[8], lo[8];
-        split2(v, hi, lo);
-        put8<CONV_F16>(p, row * to.ld + col, hi, have);
-        put8<CONV_F16>(p + to.plane, row * to.ld + col, lo, have);
-    }
+    float hi[8], lo[8];
+    split2(v, hi, lo);
+    put8<CONV_F16>(p, row * to.ld + col, hi, have);
+    put8<CONV_F16>(p + to.plane, row * to.ld + col, lo, have);
 }
 // ... and to the place mirrored at the diagonal: neighbouring lanes have neighbouring rows, which lie next to each other there
-__device__ __forceinline__ void put_mirrored(const Planes& to, int planes, int64_t row, int64_t col, const float (&v)[8], int have)
+__device__ __forceinline__ void put_mirrored(const Planes& to, int64_t row, int64_t col, const float (&v)[8], int have)
 {
     uint16_t* const p = to.p + blockIdx.y * to.batch + col * to.ld + row;
     float hi[8], lo[8];
@@ -60,25 +58,23 @@ __device__ __forceinline__ void put_mirrored(const Planes& to, int planes, int64
     for (int k = 0; k < 8; ++k)
         if (k < have) {
             p[k * to.ld] = Prec<CONV_F16>::from_f32(hi[k]);
-            if (planes > 1) p[to.plane + k * to.ld] = Prec<CONV_F16>::from_f32(lo[k]);
+            p[to.plane + k * to.ld] = Prec<CONV_F16>::from_f32(lo[k]);
         }
 }
-__device__ __forceinline__ void get_scaled(const Planes& from, int planes, int64_t row, int64_t col, float (&v)[8], int have)
+__device__ __forceinline__ void get_scaled(const Planes& from, int64_t row, int64_t col, float (&v)[8], int have)
 {
     const uint16_t* const p = from.p + blockIdx.y * from.batch;
+    float lo[8];
     get8<CONV_F16>(p, row * from.ld + col, v, have);
-    if (planes > 1) {
-        float lo[8];
-        get8<CONV_F16>(p + from.plane, row * from.ld + col, lo, have);
+    get8<CONV_F16>(p + from.plane, row * from.ld + col, lo, have);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] += lo[k];
-    }
+    for (int k = 0; k < 8; ++k) v[k] += lo[k];
 }
 
 struct GramEpi {
     struct Args {
         Planes a;
-        int planes, side;  // side of the tiles
+        int side;  // of the tiles
     };
     static constexpr bool SYMMETRIC = true;
     static __device__ __forceinline__ void prepare(const Args&, float*, int64_t, int, int, int) {}
@@ -86,8 +82,8 @@ struct GramEpi {
     {
 #pragma unroll
         for (int k = 0; k < 8; ++k) v[k] *= kUnplane;
-        put_scaled(e.a, e.planes, m, n, v, have);
-        if ((uint32_t)m / (uint32_t)e.side != (uint32_t)n / (uint32_t)e.side) put_mirrored(e.a, e.planes, m, n, v, have);
+        put_scaled(e.a, m, n, v, have);
+        if ((uint32_t)m / (uint32_t)e.side != (uint32_t)n / (uint32_t)e.side) put_mirrored(e.a, m, n, v, have);
     }
 };
 
@@ -95,18 +91,18 @@ struct SquareEpi {
     struct Args {
         Planes a, b;
         float coef_b, coef_c;
-        int planes, side;  // side of the tiles
+        int side;  // of the tiles
     };
     static constexpr bool SYMMETRIC = true;
     static __device__ __forceinline__ void prepare(const Args&, float*, int64_t, int, int, int) {}
     static __device__ __forceinline__ void finish(const ProductArgs&, const Args& e, float (&v)[8], int64_t m, int64_t n, int have, const float*)
     {
         float a[8];
-        get_scaled(e.a, e.planes, m, n, a, have);
+        get_scaled(e.a, m, n, a, have);
 #pragma unroll
         for (int k = 0; k < 8; ++k) v[k] = __builtin_fmaf(e.coef_b, a[k], e.coef_c * kUnplane * v[k]);
-        put_scaled(e.b, e.planes, m, n, v, have);
-        if ((uint32_t)m / (uint32_t)e.side != (uint32_t)n / (uint32_t)e.side) put_mirrored(e.b, e.planes, m, n, v, have);
+        put_scaled(e.b, m, n, v, have);
+        if ((uint32_t)m / (uint32_t)e.side != (uint32_t)n / (uint32_t)e.side) put_mirrored(e.b, m, n, v, have);
     }
 };
 
@@ -127,14 +123,14 @@ struct UpdateEpi {
         float* const x = e.x + blockIdx.y * e.batch_x;
         float old[8], scale = e.coef_a;
         if (e.x) get8<CONV_F32>(x, m * e.to.ld + n, old, have);
-        else get_scaled(e.from, 2, m, n, old, have), scale *= kUnplane;
+        else get_scaled(e.from, m, n, old, have), scale *= kUnplane;
 #pragma unroll
         for (int k = 0; k < 8; ++k) v[k] = __builtin_fmaf(scale, old[k], kUnplane * kUnplane * v[k]);
         if (!e.out) {
             if (e.x) put8<CONV_F32>(x, m * e.to.ld + n, v, have);
 #pragma unroll
             for (int k = 0; k < 8; ++k) v[k] *= kPlane;
-            put_scaled(e.to, 2, m, n, v, have);
+            put_scaled(e.to, m, n, v, have);
         } else {
             const int64_t at = blockIdx.y * e.batch_o + m * e.ldo + n;
             if (e.dtype == CONV_F32) put8<CONV_F32>(e.out, at, v, have);
@@ -209,21 +205,12 @@ __global__ __launch_bounds__(256) void orthogonal_start(StartArgs g)
         if (g.x32) put8<CONV_F32>(x32, t * ld + j, v, have);
 #pragma unroll
         for (int k = 0; k < 8; ++k) v[k] *= kPlane;
-        put_scaled(g.to, 2, t, j, v, have);
+        put_scaled(g.to, t, j, v, have);
     }
 }
 
 int64_t round_up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 
-// Planes that are multiplied.  One makes errors of some 2^-11 in a step, which count once the strongest directions, 1 / sqrt(n) at least at first
-// and a times that with every step, have come near one: up to three steps from there leave a bf16 result off by 1.3 times its own rounding at most (4096 x
-// 4096 in five steps 1.02, 256 x 256 1.23, in six of 512 x 512 1.37, of 166 x 30 1.8: those take two).
-int planes_of(const OrthogonalArgs& g, int dtype)
-{
-    const double side = (double)std::min(g.rows, g.cols), a = std::fabs((double)g.a);
-    const double before = a > 1.0 ? 0.5 * std::log(side) / std::log(a) : 0.0;
-    return dtype == CONV_BF16 && g.steps - before <= 3.0 ? 1 : 2;
-}
 int parts_of(int64_t rows, int64_t cols) { return (int)std::max<int64_t>(1, std::min<int64_t>(1024, rows * cols / 8192)); }
 
 struct Space {
@@ -242,41 +229,40 @@ Space space_of(const OrthogonalArgs& g, int dtype, void* ws)
         s.bytes += (n + 255) & ~(size_t)255;
         return (void*)p;
     };
-    auto matrix = [&](int64_t rows, int64_t cols, int planes) {
+    auto matrix = [&](int64_t rows, int64_t cols) {
         Planes p = {};
-        p.ld = round_up(cols, 8), p.plane = rows * p.ld, p.batch = p.plane * planes;
+        p.ld = round_up(cols, 8), p.plane = rows * p.ld, p.batch = p.plane * 2;
         p.p = (uint16_t*)take((size_t)g.batch * p.batch * 2);
         return p;
     };
     const int64_t side = std::min(g.rows, g.cols);
-    s.x[0] = matrix(g.rows, g.cols, 2), s.x[1] = matrix(g.rows, g.cols, 2);
-    s.a = matrix(side, side, planes_of(g, dtype)), s.b = matrix(side, side, planes_of(g, dtype));
+    s.x[0] = matrix(g.rows, g.cols), s.x[1] = matrix(g.rows, g.cols);
+    s.a = matrix(side, side), s.b = matrix(side, side);
     s.batch_x = g.rows * s.x[0].ld;
     if (dtype == CONV_F32) s.x32 = (float*)take((size_t)g.batch * s.batch_x * 4);
     s.sums = (double*)take((size_t)g.batch * parts_of(g.rows, g.cols) * 8);
     return s;
 }
 
-// Tiles of one plane, and of two, whose stages are twice as large.
+// Tiles of two planes.
 typedef ProductTile<4, 2, 1, 2, 2, 2> Tile64Two;      // two workgroups a CU
 typedef ProductTile<4, 2, 1, 2, 4, 2> Tile64TwoDeep;  // one: three steps on their way (4 of 2048 x 512 fp16: 307 -> 268 us)
 typedef ProductTile<2, 4, 4, 2, 2, 2> Tile128Two;
 struct TileCost {
-    int side, planes;
+    int side;
     double once, own, step;
     bool alone;  // for a workgroup a CU at most, and more steps than it has stages (12 of 192 x 192: 114 us, with it 116)
 };
-constexpr TileCost kTiles[] = {{64, 1, 4.1, 1.0, 0.275}, {128, 1, 3.1, 1.7, 0.53}, {256, 1, 0, 6.4, 1.18}, {192, 1, 0, 5.0, 0.8}, {64, 2, 4.1, 1.0, 0.5}, {128, 2, 3.1, 3.0, 1.3}, {64, 2, 4.1, 1.0, 0.4, true}};
-enum TileId { T64, T128, T256, T192, T64_TWO, T128_TWO, T64_TWO_DEEP };
+constexpr TileCost kTiles[] = {{64, 4.1, 1.0, 0.5, false}, {128, 3.1, 3.0, 1.3, false}, {64, 4.1, 1.0, 0.4, true}};
+enum TileId { T64, T128, T64_DEEP };
 
 // The tile with the least expected time, in us (see the linear layers' plan).
-TileId tile_of(int64_t M, int64_t N, int64_t K, int planes, int64_t batch, bool symmetric)
+TileId tile_of(int64_t M, int64_t N, int64_t K, int64_t batch, bool symmetric)
 {
     int best = 0;
     double least = 1e30;
     for (int f = 0; f < (int)(sizeof(kTiles) / sizeof(kTiles[0])); ++f) {
         const TileCost& c = kTiles[f];
-        if (c.planes != planes) continue;
         const double tm = (double)((M + c.side - 1) / c.side), tn = (double)((N + c.side - 1) / c.side);
         const double tiles = (symmetric ? tm * (tm + 1) / 2 : tm * tn) * batch, steps = (double)((K + 63) / 64);
         const double us = c.once + std::ceil(tiles / 256) * (c.own + steps * c.step);
@@ -295,13 +281,9 @@ template <bool A_ACROSS, bool B_ACROSS, typename Epi>
 hipError_t multiply(const ProductArgs& g, const typename Epi::Args& e, TileId tile, int batch, hipStream_t s)
 {
     switch (tile) {
-        case T64: return launch_product_tiles<CONV_F16, Tile64, A_ACROSS, B_ACROSS, true, Epi>(g, e, batch, 1, s);
-        case T128: return launch_product_tiles<CONV_F16, Tile128, A_ACROSS, B_ACROSS, true, Epi>(g, e, batch, 1, s);
-        case T192: return launch_product_tiles<CONV_F16, Tile192, A_ACROSS, B_ACROSS, true, Epi>(g, e, batch, 1, s);
-        case T256: return launch_product_tiles<CONV_F16, Tile256, A_ACROSS, B_ACROSS, true, Epi>(g, e, batch, 1, s);
-        case T64_TWO_DEEP: return launch_product_tiles<CONV_F16, Tile64TwoDeep, A_ACROSS, B_ACROSS, true, Epi>(g, e, batch, 1, s);
-        case T64_TWO: return launch_product_tiles<CONV_F16, Tile64Two, A_ACROSS, B_ACROSS, true, Epi>(g, e, batch, 1, s);
-        default: return launch_product_tiles<CONV_F16, Tile128Two, A_ACROSS, B_ACROSS, true, Epi>(g, e, batch, 1, s);
+        case T64: return launch_product_tiles<CONV_F16, Tile64Two, A_ACROSS, B_ACROSS, true, Epi>(g, e, batch, 1, s);
+        case T128: return launch_product_tiles<CONV_F16, Tile128Two, A_ACROSS, B_ACROSS, true, Epi>(g, e, batch, 1, s);
+        default: return launch_product_tiles<CONV_F16, Tile64TwoDeep, A_ACROSS, B_ACROSS, true, Epi>(g, e, batch, 1, s);
     }
 }
 
@@ -329,10 +311,10 @@ size_t orthogonal_workspace(const OrthogonalArgs& g, int dtype) { return g.batch
 hipError_t launch_orthogonalize(const OrthogonalArgs& all, int dtype, hipStream_t s)
 {
     // gridDim.y is at most 65535, and a launch holds less than 2^32 threads: the batch goes in portions, tiles chosen for the largest
-    const int planes = planes_of(all, dtype), es = dtype_size(dtype);
+    const int es = dtype_size(dtype);
     const int64_t side = std::min(all.rows, all.cols), longer = std::max(all.rows, all.cols), most = std::min<int64_t>(all.batch, 32768);
-    const TileId gram = tile_of(side, side, longer, planes, most, true), square = tile_of(side, side, side, planes, most, true);
-    const TileId update = tile_of(all.rows, all.cols, side, planes, most, false);
+    const TileId gram = tile_of(side, side, longer, most, true), square = tile_of(side, side, side, most, true);
+    const TileId update = tile_of(all.rows, all.cols, side, most, false);
     const int64_t tiles = std::max({tiles_of(gram, side, side), tiles_of(square, side, side), tiles_of(update, all.rows, all.cols)});
     const int64_t portion = std::max<int64_t>(1, std::min(most, ((int64_t)1 << 21) / tiles));
     for (int64_t skip = 0; skip < all.batch; skip += portion) {
@@ -349,11 +331,11 @@ hipError_t launch_orthogonalize(const OrthogonalArgs& all, int dtype, hipStream_
         const int batch = (int)g.batch;
         for (int step = 0; step < g.steps; ++step) {
             const Planes &x = w.x[step & 1], &to = w.x[(step + 1) & 1];
-            const GramEpi::Args ge = {w.a, planes, kTiles[gram].side};
+            const GramEpi::Args ge = {w.a, kTiles[gram].side};
             const ProductArgs gp = product_of(x, x, side, side, longer);
             e = tall ? multiply<true, true, GramEpi>(gp, ge, gram, batch, s) : multiply<false, false, GramEpi>(gp, ge, gram, batch, s);
             if (e != hipSuccess) return e;
-            const SquareEpi::Args se = {w.a, w.b, g.b, g.c, planes, kTiles[square].side};
+            const SquareEpi::Args se = {w.a, w.b, g.b, g.c, kTiles[square].side};
             e = multiply<false, false, SquareEpi>(product_of(w.a, w.a, side, side, side), se, square, batch, s);
             if (e != hipSuccess) return e;
             const UpdateEpi::Args ue = {w.x32, w.batch_x, x, to, g.a, step + 1 == g.steps ? g.out : nullptr, g.ldo, g.stride_o, dtype};
