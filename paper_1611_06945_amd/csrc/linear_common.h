@@ -7,41 +7,63 @@ namespace convfwd {
 
 enum { ACT_NONE = 0, ACT_RELU = 1, ACT_GELU = 2, ACT_SILU = 3 };
 
-// Phi(-|z|), Phi the normal distribution, by the rational approximation 7.1.26 of Abramowitz and Stegun's handbook, which is off by 1.5e-7 / 2 at
-// most (erff() takes four times the instructions), and exp(-z^2 / 2).  What a tile's 65536 activations cost is a part of its time: 10 us of the 115 of a
-// tile of 8192 x 4096 x 8192 with another form of this, so divisions are reciprocals (off by a unit in the last place).
+// Phi(-|z|), Phi the normal distribution, and exp(-z^2 / 2).  It is exp(-z^2 / 2) t P(t) with t = 1 / (1 + c |z|), the form of formula 7.1.26 of Abramowitz and Stegun's
+// handbook, with c and P fitted here for the least relative error; FINE up to |z| = 1 it is 1/2 - |z| Q(z^2).  (erff() takes four times the instructions.)  FINE is off by the roundings of
+// fp32: GELU over normal z 3.1e-8 of the norm, with 1 + erf() in fp32 3.7e-8.  Otherwise by 1.1e-5 of the value at most, a fortieth of a rounding to fp16, for results that are stored
+// in 16 bits; the handbook's own coefficients leave twice a rounding of fp16 at z = -3.5.  What a tile's 65536 activations cost is a part of its time (200704 x 192 x 768 fp16 with the
+// sum kept 283 us, FINE 315), so divisions are reciprocals, off by a unit in the last place.
+template <bool FINE>
 __device__ __forceinline__ float normal_tail(float z, float& bell)
 {
-    const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.3275911f * 0.70710678118654752f, fabsf(z), 1.0f));
-    bell = __builtin_amdgcn_exp2f(z * z * (-0.5f * 1.44269504088896341f));
-    float p = __builtin_fmaf(0.5f * 1.061405429f, t, 0.5f * -1.453152027f);
-    p = __builtin_fmaf(p, t, 0.5f * 1.421413741f);
-    p = __builtin_fmaf(p, t, 0.5f * -0.284496736f);
-    p = __builtin_fmaf(p, t, 0.5f * 0.254829592f);
-    return p * t * bell;
+    const float u = fabsf(z), w = z * z;
+    const float t = __builtin_amdgcn_rcpf(__builtin_fmaf((FINE ? 0.4f : 0.425f) * 0.70710678118654752f, u, 1.0f));
+    bell = __builtin_amdgcn_exp2f(w * (-0.5f * 1.44269504088896341f));
+    float p;
+    if constexpr (!FINE) {
+        p = __builtin_fmaf(-0.0769140348f, t, 0.213978097f);
+        p = __builtin_fmaf(p, t, -0.014909937f);
+        p = __builtin_fmaf(p, t, 0.143442242f);
+        p = __builtin_fmaf(p, t, 0.114141129f);
+        p = __builtin_fmaf(p, t, 0.120266527f);
+        return p * t * bell;
+    }
+    p = __builtin_fmaf(-0.0566013232f, t, 0.117606282f);
+    p = __builtin_fmaf(p, t, 0.00876443554f);
+    p = __builtin_fmaf(p, t, 0.103900433f);
+    p = __builtin_fmaf(p, t, 0.10019324f);
+    p = __builtin_fmaf(p, t, 0.113221332f);
+    p = __builtin_fmaf(p, t, 0.112821251f);
+    float q = __builtin_fmaf(-7.65420828e-06f, w, 0.000113486371f);
+    q = __builtin_fmaf(q, w, -0.00118632999f);
+    q = __builtin_fmaf(q, w, 0.00997332297f);
+    q = __builtin_fmaf(q, w, -0.0664903596f);
+    q = __builtin_fmaf(q, w, 0.398942292f);
+    return u < 1.0f ? __builtin_fmaf(-u, q, 0.5f) : p * t * bell;
 }
 // 1 / (1 + exp(-z))
 __device__ __forceinline__ float logistic(float z) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(z * -1.44269504088896341f)); }
 
 // (Factors z beside a tail are clamped where the tail has vanished already: infinities give the limits, where they would give infinity times zero.)
+// DT: what the value is stored as.
+template <int DT>
 __device__ __forceinline__ float act_of(float z, int act)
 {
     if (act == ACT_RELU) return z < 0.0f ? 0.0f : z;  // a NaN stays
     if (act == ACT_GELU) {
         float bell;
-        const float tail = normal_tail(z, bell);
+        const float tail = normal_tail<DT == CONV_F32>(z, bell);
         return __builtin_fmaf(-fminf(fabsf(z), 16.0f), tail, z < 0.0f ? 0.0f : z);  // z Phi(z) = max(z, 0) - |z| Phi(-|z|)
     }
     if (act == ACT_SILU) return fmaxf(z, -128.0f) * logistic(z);
     return z;
 }
-// its derivative; 0 at the corner of ReLU
+// its derivative, which goes into sums in fp32; 0 at the corner of ReLU
 __device__ __forceinline__ float act_slope(float z, int act)
 {
     if (act == ACT_RELU) return z > 0.0f ? 1.0f : z <= 0.0f ? 0.0f : z;
     if (act == ACT_GELU) {
         float bell;
-        const float tail = normal_tail(z, bell);
+        const float tail = normal_tail<true>(z, bell);
         return __builtin_fmaf(__builtin_amdgcn_fmed3f(z, -16.0f, 16.0f) * bell, 0.39894228040143268f, z < 0.0f ? tail : 1.0f - tail);
     }
     if (act == ACT_SILU) {
@@ -78,7 +100,7 @@ struct LinearEpi {
         if (e.pre) put8<DT>(e.pre, m * e.ldo + n, v, have);
         if (e.act) {
 #pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] = act_of(v[k], e.act);
+            for (int k = 0; k < 8; ++k) v[k] = act_of<DT>(v[k], e.act);
         }
         if (e.residual) {
             float r[8];

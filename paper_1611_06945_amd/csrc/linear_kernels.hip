@@ -25,7 +25,7 @@ __device__ __forceinline__ float finish_one(const LinearOut& e, float z, int64_t
     typedef typename Prec<DT>::elem_t elem_t;
     if (e.bias) z += e.bias[n];
     if (e.pre) ((elem_t*)e.pre)[t * e.ldo + n] = Prec<DT>::from_f32(z);
-    float v = act_of(z, e.act);
+    float v = act_of<DT>(z, e.act);
     if (e.residual) v += Prec<DT>::to_f32(((const elem_t*)e.residual)[t * e.ldr + n]);
     return v;
 }
