@@ -338,7 +338,7 @@ ResidualNormForm bwd_form(int64_t rows, int cols, int64_t gate_rows, int dtype)
     f.sums = f.most == 16 || !f.lanes;  // the column sums by a kernel of their own
     const int here = f.sums ? 1 : (f.lanes <= 256 ? 256 : f.lanes) / f.lanes;  // rows at once
     const int64_t most = f.sums ? 128 : f.lanes >= 512 ? kCUs : f.lanes <= 16 ? 4 * kCUs : 2 * kCUs;
-    f.stretch = gate_rows > 1 ? gate_rows : std::max<int64_t>(rows, 1);
+    f.stretch = std::max<int64_t>(gate_rows > 1 ? std::min(gate_rows, rows) : rows, 1);  // (a gate may stand for more rows than there are)
     const int64_t stretches = (rows + f.stretch - 1) / f.stretch;
     // as many runs as workgroups, of whole rounds; at least eight rows each, lest their sums cost more than they
     const int64_t want = stretches ? std::max<int64_t>(1, most / stretches) : 1;

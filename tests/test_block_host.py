@@ -256,3 +256,11 @@ def test_oracle_of_the_steps_against_singular_values():
     for _ in range(3):
         s = 3.4445 * s - 4.7750 * s ** 3 + 2.0315 * s ** 5
     assert np.allclose(ro.newton_schulz(x, 3, (3.4445, -4.7750, 2.0315), 0.0), u * s @ v, atol=1e-12)
+
+
+@pytest.mark.parametrize("dtype", [B.CONV_F32, B.CONV_F16, B.CONV_BF16])
+@pytest.mark.parametrize("rows,cols", [(1, 40), (100, 64), (4096, 1000), (300, 9000)])
+def test_a_gate_for_more_rows_than_there_are_is_one_for_all(rows, cols, dtype):
+    """Rows are shared out among workgroups by what there is of them, and so is the room for their sums."""
+    need = [B.residual_norm_bwd_workspace_bytes(B.make_residual_norm_desc(rows, cols, dtype, gate_rows=n)) for n in (max(2, rows), 2 * rows + 1, (1 << 31) - 1)]
+    assert need[0] == need[1] == need[2]

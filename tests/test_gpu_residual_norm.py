@@ -285,3 +285,25 @@ def test_rows_far_apart(dtype, cols, gate_rows):
         B.residual_norm_bwd(d, r, h, gate, *vectors[:4], st, None, y, None, dh, dgate, *sums, torch.empty(need, dtype=torch.uint8, device="cuda"), need)
         results[-1] += [dh.clone(), *([dgate] if gate_rows else []), *sums]
     assert all(torch.equal(a, b) for a, b in zip(*results))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rows,cols", [(1, 40), (1000, 64), (700, 1000), (300, 9000), (40, 16400)])
+def test_a_gate_for_more_rows_than_there_are(rows, cols, dtype):
+    for gate_rows in (rows + 1, (1 << 31) - 1):
+        kind = dict(gate_rows=gate_rows, sigmoid=True, post=cols % 3 != 0)
+        check_fwd(rows, cols, dtype, **kind)
+        # (the bound's roundings of a gate's sum: as many as it has rows)
+        check_bwd(rows, cols, dtype, gate_rows=max(2, rows), sigmoid=True, post=kind["post"])
+        torch = torch_mod()
+        g = torch.Generator(device="cuda").manual_seed(rows)
+        r, h, dro, dy = (torch.randn(rows, cols, generator=g, device="cuda").to(torch_type(dtype)) for _ in range(4))
+        gate, st = torch.randn(1, cols, generator=g, device="cuda").to(r.dtype), torch.rand(rows, 4, generator=g, device="cuda")
+        results = []
+        for n in (max(2, rows), gate_rows):
+            d = B.make_residual_norm_desc(rows, cols, dtype, EPS, gate_rows=n)
+            need = B.residual_norm_bwd_workspace_bytes(d)
+            dr, dh, dgate, sums = torch.empty_like(r), torch.empty_like(h), torch.empty_like(gate), [nan_vec(cols) for _ in range(5)]
+            B.residual_norm_bwd(d, r, h, gate, None, None, None, None, st, dro, dy, dr, dh, dgate, *sums, torch.empty(need, dtype=torch.uint8, device="cuda"), need)
+            results.append([dr, dh, dgate, *sums])
+        assert all(torch.equal(a, b) for a, b in zip(*results))
