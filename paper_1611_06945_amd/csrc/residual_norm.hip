@@ -375,7 +375,18 @@ hipError_t bwd(ResidualNormArgs a, const ResidualNormForm& f, hipStream_t s)
 {
     if (a.rows > 0) {
         if (f.lanes) {
-            const hipError_t e = DT == CONV_F32 ? residual_norm_bwd_f32(a, f, s) : DT == CONV_F16 ? residual_norm_bwd_f16(a, f, s) : residual_norm_bwd_bf16(a, f, s);
+            ResidualNormArgs rows = a;
+            ResidualNormForm form = f;
+            // Without column sums a workgroup's rows need be neither of one gate nor many: as many workgroups as CUs (the runs of the sums' kernel, 128 at most,
+            // left half of them idle)
+            if (f.sums) {
+                rows.stretch = a.rows, rows.each = (a.rows + kCUs - 1) / kCUs;
+                rows.items = (a.rows + rows.each - 1) / rows.each;
+                rows.per = form.groups = (int)rows.items;
+            }
+            const hipError_t e = DT == CONV_F32   ? residual_norm_bwd_f32(rows, form, s)
+                                 : DT == CONV_F16 ? residual_norm_bwd_f16(rows, form, s)
+                                                  : residual_norm_bwd_bf16(rows, form, s);
             if (e != hipSuccess) return e;
         } else {
             hipLaunchKernelGGL((residual_norm_bwd_any<DT>), dim3((unsigned)std::min<int64_t>(a.rows, 1 << 20)), dim3(1024), 0, s, a);

@@ -307,3 +307,11 @@ def test_a_gate_for_more_rows_than_there_are(rows, cols, dtype):
             B.residual_norm_bwd(d, r, h, gate, None, None, None, None, st, dro, dy, dr, dh, dgate, *sums, torch.empty(need, dtype=torch.uint8, device="cuda"), need)
             results.append([dr, dh, dgate, *sums])
         assert all(torch.equal(a, b) for a, b in zip(*results))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rows", [1, 7, 255, 256, 257, 600])
+@pytest.mark.parametrize("cols,kind", [(8200, dict(gate_rows=3)), (8193, dict(gate_rows=1, sigmoid=True)), (16384, dict(post=False, rms=True))])
+def test_wide_rows_in_every_share_of_the_workgroups(cols, kind, rows, dtype):
+    """Rows too wide for the column sums: as many workgroups as CUs take them in runs, whatever rows share a gate."""
+    check_bwd(rows, cols, dtype, **kind)
