@@ -60,7 +60,7 @@ class TrainingBlock:
         dev, f32 = self.h.device, self.torch.float32
         self._rows("r", r)
         self._rows("y", y)
-        if self.y is not None and y.data_ptr() == self.y.data_ptr():
+        if self.rows and self.y is not None and y.data_ptr() == self.y.data_ptr():
             raise ValueError("y is the block's own result, which this pass replaces before backward() reads it")
         if set(weights) != set(self.shapes):
             raise ValueError("weights must be %s; they are %s" % (sorted(self.shapes), sorted(weights)))

@@ -218,3 +218,15 @@ def test_the_command_runs():
     lines = []
     first, last = blk.demo(images=3, pixels=10, D=32, hidden=48, classes=7, steps=3, log=lines.append)
     assert len(lines) == 2 and np.isfinite([first, last]).all()
+
+
+def test_a_block_without_rows_has_gradients_of_zeros():
+    torch = torch_mod()
+    b = blk.TrainingBlock(0, D, HIDDEN, torch.bfloat16, gate_rows=3, sigmoid=True)
+    weights = {k: torch.ones(*s, dtype=b.dtype if k in blk.WEIGHTS else torch.float32, device="cuda") for k, s in b.shapes.items()}
+    for g in b.grads.values():
+        g.fill_(7.0)
+    none = torch.empty(0, D, dtype=b.dtype, device="cuda")
+    b.forward(none, none, weights, none)
+    b.backward(none, none)
+    assert all(not bool(g.any()) for g in b.grads.values())

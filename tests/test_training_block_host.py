@@ -134,3 +134,12 @@ def test_momentum_of_the_update(calls, nesterov):
         with pytest.raises(ValueError):
             u.step(bad)
     assert torch.equal(u.sum, before) and len(calls) == 3
+
+
+def test_a_block_without_rows(calls):
+    """All tensors of no rows have the address zero, the block's own result too."""
+    b = blk.TrainingBlock(0, D, HIDDEN, torch.float32, gate_rows=3, device="cpu")
+    r, y = torch.zeros(0, D), torch.zeros(0, D)
+    assert b.forward(r, y, weights_of(b), torch.zeros(0, D)) == (b.r_out, b.y)
+    assert b.backward(torch.zeros(0, D), torch.zeros(0, D)) == (b.dr, b.dy)
+    assert len(calls) == 6
