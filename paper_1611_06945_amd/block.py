@@ -90,12 +90,12 @@ class TrainingBlock:
         if dy_out is not None:
             self._rows("dy_out", dy_out)
         y, p, gate = self.saved
-        self.saved = None
         g, ws, n = self.grads, self.ws, self.ws.numel()
         B.residual_norm_bwd(self.norm, self.r_out, self.h, gate, p.get("gamma_h"), p.get("beta_h"), p["scale"], p.get("gamma"), self.stats, dr_out, dy_out, self.dr,
                             self.dh, self.dgate, g.get("gamma_h"), g.get("beta_h"), g["scale"], g.get("gamma"), g.get("beta"), ws, n, stream)
         B.linear_bwd(self.second, self.a, p["w2"], None, self.dh, self.da, g["w2"], g["b2"], ws, n, stream)
         B.linear_bwd(self.first, y, p["w1"], self.pre, self.da, self.dy, g["w1"], g["b1"], ws, n, stream)
+        self.saved = None
         return self.dr, self.dy
 
 

@@ -143,3 +143,21 @@ def test_a_block_without_rows(calls):
     assert b.forward(r, y, weights_of(b), torch.zeros(0, D)) == (b.r_out, b.y)
     assert b.backward(torch.zeros(0, D), torch.zeros(0, D)) == (b.dr, b.dy)
     assert len(calls) == 6
+
+
+def test_a_call_that_the_library_refuses_does_not_use_the_forward_pass_up(calls, monkeypatch):
+    """As when a gradient is handed in where the block writes one."""
+    b = block()
+    b.forward(*rows_of(b, 2), weights_of(b))
+
+    def refuse(*args):
+        raise B.ConvError(B.CONV_EINVAL, "residual_norm_bwd")
+
+    taken = B.residual_norm_bwd
+    monkeypatch.setattr(B, "residual_norm_bwd", refuse)
+    with pytest.raises(B.ConvError):
+        b.backward(b.dr)
+    monkeypatch.setattr(B, "residual_norm_bwd", taken)
+    assert b.backward(*rows_of(b, 2)) == (b.dr, b.dy)
+    with pytest.raises(RuntimeError):
+        b.backward(*rows_of(b, 2))
