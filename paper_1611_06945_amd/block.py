@@ -102,7 +102,8 @@ class TrainingBlock:
 class OrthogonalUpdate:
     def __init__(self, count: int, rows: int, cols: int, dtype, momentum: float = 0.95, nesterov: bool = True, steps: int = 5,
                  coefficients=(3.4445, -4.7750, 2.0315), eps: float = 1e-7, device="cuda"):
-        """For `count` weights [rows][cols]; the steps are computed on `dtype`, the momentum is kept in fp32."""
+        """For `count` weights [rows][cols]; the steps are computed on `dtype`, the momentum is kept in fp32.  fp16 is the result's type alone: gradients and their
+        momentum may leave its range, so the steps are computed on fp32."""
         import torch
 
         if torch.device(device).type != GPU:
@@ -111,7 +112,8 @@ class OrthogonalUpdate:
         shape = (count, rows, cols)
         self.sum = torch.zeros(*shape, dtype=torch.float32, device=device)
         self.direction = torch.empty(*shape, dtype=dtype, device=device)
-        self.desc = B.make_orthogonal_desc(rows, cols, _code(torch, dtype), count, steps, coefficients, eps)
+        self.x = torch.empty(*shape, dtype=torch.float32, device=device) if dtype == torch.float16 else self.direction
+        self.desc = B.make_orthogonal_desc(rows, cols, _code(torch, self.x.dtype), count, steps, coefficients, eps)
         self.ws = torch.empty(max(256, B.orthogonalize_workspace_bytes(self.desc)), dtype=torch.uint8, device=device)
 
     def step(self, grads):
@@ -125,8 +127,10 @@ class OrthogonalUpdate:
         self.sum.mul_(self.momentum)
         for i, g in enumerate(grads):
             self.sum[i].add_(g)
-            self.direction[i].copy_(self.sum[i].mul(self.momentum).add_(g) if self.nesterov else self.sum[i])
-        B.orthogonalize(self.desc, self.direction, self.direction, self.ws, self.ws.numel())
+            self.x[i].copy_(self.sum[i].mul(self.momentum).add_(g) if self.nesterov else self.sum[i])
+        B.orthogonalize(self.desc, self.x, self.x, self.ws, self.ws.numel())
+        if self.x is not self.direction:
+            self.direction.copy_(self.x)
         return self.direction
 
 

@@ -230,3 +230,18 @@ def test_a_block_without_rows_has_gradients_of_zeros():
     b.forward(none, none, weights, none)
     b.backward(none, none)
     assert all(not bool(g.any()) for g in b.grads.values())
+
+
+def test_fp16_directions_of_gradients_outside_the_types_range():
+    torch = torch_mod()
+    from oracle import rows_oracle as ro
+    from test_gpu_orthogonal import STEP
+    from test_gpu_orthogonal import bound as steps_bound
+
+    u = blk.OrthogonalUpdate(2, 24, 40, torch.float16, momentum=0.5, nesterov=False, eps=0.0)
+    grads = torch.randn(2, 24, 40, generator=torch.Generator(device="cuda").manual_seed(5), device="cuda") * torch.tensor([1e-9, 1e6], device="cuda").view(2, 1, 1)
+    got = u.step(list(grads)).double().cpu().numpy()
+    assert u.direction.dtype == torch.float16
+    for i in range(2):
+        want = ro.newton_schulz(grads[i].double().cpu().numpy(), 5, STEP, 0.0)
+        assert np.linalg.norm(got[i] - want) <= steps_bound(wl.F16, 24, 40, 5, STEP) * np.linalg.norm(want)

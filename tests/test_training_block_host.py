@@ -161,3 +161,22 @@ def test_a_call_that_the_library_refuses_does_not_use_the_forward_pass_up(calls,
     assert b.backward(*rows_of(b, 2)) == (b.dr, b.dy)
     with pytest.raises(RuntimeError):
         b.backward(*rows_of(b, 2))
+
+
+def test_the_momentum_may_leave_the_range_of_fp16(calls):
+    """Gradients of 1e-9 vanish in fp16, and twenty times one of 6e4, as the momentum adds them up, is an infinity there."""
+    u = blk.OrthogonalUpdate(2, 3, 5, torch.float16, device="cpu")
+    small, large = torch.full((3, 5), 1e-9), torch.full((3, 5), 6e4, dtype=torch.float16)
+    for _ in range(30):
+        out = u.step([small, large])
+    assert out.dtype == torch.float16 and out is u.direction
+    handed = calls[-1][1][1]
+    assert calls[-1][1][2] is handed and bool(torch.isfinite(handed).all()) and bool((handed != 0).all())
+    assert calls[-1][1][4] >= B.orthogonalize_workspace_bytes(calls[-1][1][0])
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float16, torch.bfloat16])
+def test_the_direction_has_the_updates_type(calls, dtype):
+    u = blk.OrthogonalUpdate(1, 3, 5, dtype, momentum=0.0, device="cpu")
+    g = torch.arange(15.0).view(3, 5)
+    assert torch.equal(u.step([g]), g[None].to(dtype)) and u.direction.dtype == dtype  # (the steps, which are not made here, work in place)
