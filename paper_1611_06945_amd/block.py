@@ -19,6 +19,12 @@ WEIGHTS = ("w1", "w2")
 VECTORS = ("b1", "b2", "gamma_h", "beta_h", "scale", "gamma", "beta")
 
 
+def _current(torch, device):
+    """Kernels are launched on the current device."""
+    if device.type == "cuda" and torch.cuda.current_device() != device.index:
+        raise ValueError("the buffers are on %s, the current device is %d" % (device, torch.cuda.current_device()))
+
+
 class TrainingBlock:
     def __init__(self, rows: int, D: int, hidden: int, dtype, act: str = "gelu", rms: bool = False, post: bool = True, gate_rows: int = 0,
                  sigmoid: bool = False, last: bool = False, eps: float = 1e-5, device="cuda"):
@@ -58,6 +64,7 @@ class TrainingBlock:
         where the block has their norms, gamma_h, beta_h, gamma, beta; gate: [gates][D] of the type, or None.  All dense.  -> (r_out, y_out), views of the
         block's own buffers; keeps what backward() needs."""
         dev, f32 = self.h.device, self.torch.float32
+        _current(self.torch, dev)
         self._rows("r", r)
         self._rows("y", y)
         if self.rows and self.y is not None and y.data_ptr() == self.y.data_ptr():
@@ -86,6 +93,7 @@ class TrainingBlock:
             raise RuntimeError("backward() needs a forward() of its own")
         if dy_out is not None and self.last:
             raise ValueError("a last block has no y")
+        _current(self.torch, self.h.device)
         self._rows("dr_out", dr_out)
         if dy_out is not None:
             self._rows("dy_out", dy_out)
@@ -124,6 +132,7 @@ class OrthogonalUpdate:
             if g.shape != self.sum.shape[1:] or g.device != self.sum.device or not g.is_floating_point():
                 raise ValueError("a gradient must be %s of a float type on %s; it is %s %s on %s" % (
                     list(self.sum.shape[1:]), self.sum.device, g.dtype, list(g.shape), g.device))
+        _current(self.torch, self.sum.device)
         self.sum.mul_(self.momentum)
         for i, g in enumerate(grads):
             self.sum[i].add_(g)

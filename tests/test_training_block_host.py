@@ -180,3 +180,27 @@ def test_the_direction_has_the_updates_type(calls, dtype):
     u = blk.OrthogonalUpdate(1, 3, 5, dtype, momentum=0.0, device="cpu")
     g = torch.arange(15.0).view(3, 5)
     assert torch.equal(u.step([g]), g[None].to(dtype)) and u.direction.dtype == dtype  # (the steps, which are not made here, work in place)
+
+
+def test_another_current_device_is_refused(calls, monkeypatch):
+    """Kernels are launched on the current device, which another one's memory is not for."""
+    current = [0]
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: current[0])
+    blk._current(torch, torch.device("cuda:0"))
+    with pytest.raises(ValueError):
+        blk._current(torch, torch.device("cuda:1"))
+    current[0] = 1
+    blk._current(torch, torch.device("cuda:1"))
+
+    def other(torch, device):
+        raise ValueError("another device")
+
+    b, u = block(), blk.OrthogonalUpdate(1, 3, 5, torch.float32, device="cpu")
+    b.forward(*rows_of(b, 2), weights_of(b))
+    del calls[:]
+    before = u.sum.clone()
+    monkeypatch.setattr(blk, "_current", other)
+    for call in (lambda: b.forward(*rows_of(b, 2), weights_of(b)), lambda: b.backward(*rows_of(b, 2)), lambda: u.step([torch.ones(3, 5)])):
+        with pytest.raises(ValueError):
+            call()
+    assert not calls and torch.equal(u.sum, before)
