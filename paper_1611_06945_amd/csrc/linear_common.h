@@ -91,24 +91,25 @@ struct LinearEpi {
     {
         for (int i = threadIdx.x; i < width; i += threads) bias[i] = e.bias && i < here ? e.bias[n0 + i] : 0.0f;
     }
-    static __device__ __forceinline__ void finish(const ProductArgs&, const Args& e, float (&v)[8], int64_t m, int64_t n, int have, const float* bias)
+    template <int W>
+    static __device__ __forceinline__ void finish(const ProductArgs&, const Args& e, float (&v)[W], int64_t m, int64_t n, int have, const float* bias)
     {
         if (e.bias) {
 #pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] += bias[k];
+            for (int k = 0; k < W; ++k) v[k] += bias[k];
         }
-        if (e.pre) put8<DT>(e.pre, m * e.ldo + n, v, have);
+        if (e.pre) put_pieces<DT, W>(e.pre, m * e.ldo + n, v, have);
         if (e.act) {
 #pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] = act_of<DT>(v[k], e.act);
+            for (int k = 0; k < W; ++k) v[k] = act_of<DT>(v[k], e.act);
         }
         if (e.residual) {
-            float r[8];
-            get8<DT>(e.residual, m * e.ldr + n, r, have);
+            float r[W];
+            get_pieces<DT, W>(e.residual, m * e.ldr + n, r, have);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] += r[k];
+            for (int k = 0; k < W; ++k) v[k] += r[k];
         }
-        put8<DT>(e.out, m * e.ldo + n, v, have);
+        put_pieces<DT, W>(e.out, m * e.ldo + n, v, have);
     }
 };
 

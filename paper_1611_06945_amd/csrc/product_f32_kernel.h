@@ -175,20 +175,18 @@ __global__ __launch_bounds__(T::NT) void product_f32_kernel(SplitArgs g, LinearO
         __syncthreads();
     }
 
-    // as in product_kernel: eight n in a row for each lane
-    const int grp = lane >> 4;
+    // a lane has four n in a row, 16 bytes
 #pragma unroll
-    for (int i = 0; i < T::FN; i += 2) {
-        const int nl = (wn * T::FN + i) * 16 + (grp & 1) * 16 + (grp >> 1) * 8;
+    for (int i = 0; i < T::FN; ++i) {
+        const int nl = (wn * T::FN + i) * 16 + (lane >> 4) * 4;
 #pragma unroll
         for (int j = 0; j < T::FT; ++j) {
             const int ml = (wt * T::FT + j) * 16 + (lane & 15);
-            float v[8];
-            eight_in_a_row(acc[i][j], acc[i + 1][j], v);
             if (ml < a.pieces.here && nl < b.pieces.here) {
-                const int have = min(8, b.pieces.here - nl);
+                float v[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
+                const int have = min(4, b.pieces.here - nl);
                 const int64_t m = g.m_first + m0 + ml;
-                if constexpr (PARTIAL) put8<CONV_F32>(g.partial, ((int64_t)share * g.M + m) * g.N + n0 + nl, v, have);
+                if constexpr (PARTIAL) put_pieces<CONV_F32, 4>(g.partial, ((int64_t)share * g.M + m) * g.N + n0 + nl, v, have);
                 else LinearEpi<CONV_F32>::finish(ProductArgs(), e, v, m, n0 + nl, have, bias + nl);
             }
         }

@@ -57,15 +57,15 @@ struct Piece {
     }
 };
 
-// Eight neighbouring elements (n of them exist), to or from a row that starts at any element.
-template <int DT>
-__device__ __forceinline__ void put8(void* row, int64_t at, const float (&v)[8], int n)
+// W neighbouring elements, whole pieces (n of them exist), to or from a row that starts at any element.
+template <int DT, int W>
+__device__ __forceinline__ void put_pieces(void* row, int64_t at, const float (&v)[W], int n)
 {
     typedef Piece<DT> P;
     typename P::elem_t* p = (typename P::elem_t*)row + at;
     constexpr int VEC = P::VEC;
 #pragma unroll
-    for (int c = 0; c < 8 / VEC; ++c) {
+    for (int c = 0; c < W / VEC; ++c) {
         float part[VEC];
 #pragma unroll
         for (int k = 0; k < VEC; ++k) part[k] = v[c * VEC + k];
@@ -81,14 +81,14 @@ __device__ __forceinline__ void put8(void* row, int64_t at, const float (&v)[8],
         }
     }
 }
-template <int DT>
-__device__ __forceinline__ void get8(const void* row, int64_t at, float (&v)[8], int n)
+template <int DT, int W>
+__device__ __forceinline__ void get_pieces(const void* row, int64_t at, float (&v)[W], int n)
 {
     typedef Piece<DT> P;
     const typename P::elem_t* p = (const typename P::elem_t*)row + at;
     constexpr int VEC = P::VEC;
 #pragma unroll
-    for (int c = 0; c < 8 / VEC; ++c) {
+    for (int c = 0; c < W / VEC; ++c) {
         if (n >= (c + 1) * VEC) {
             float part[VEC];
             P::widen(P::raw(p + c * VEC), part);
@@ -100,6 +100,12 @@ __device__ __forceinline__ void get8(const void* row, int64_t at, float (&v)[8],
         }
     }
 }
+
+// ... eight of them
+template <int DT>
+__device__ __forceinline__ void put8(void* row, int64_t at, const float (&v)[8], int n) { put_pieces<DT, 8>(row, at, v, n); }
+template <int DT>
+__device__ __forceinline__ void get8(const void* row, int64_t at, float (&v)[8], int n) { get_pieces<DT, 8>(row, at, v, n); }
 
 struct OpSum {
     static __device__ __forceinline__ float of(float a, float b) { return a + b; }
