@@ -332,7 +332,9 @@ ProductPlan plan_product(int64_t M, int64_t N, int64_t K, int dtype, bool direct
 }
 
 // Few rows: blocks of 16 rows a workgroup, workgroups that share a reduction, expected us.  A workgroup reads 120 KB in a us, all of them
-// 33 TB/s (from the caches mostly), and one takes 0.16 us of a CU a block at least; a second launch to add shares costs about 5 us of a call.
+// 33 TB/s (from the caches mostly), and one takes 0.16 us of a CU a block at least; a second launch to add shares costs about 5 us of a call.  The fp32 matrix
+// instructions, 0.61 MFLOP a us and CU, add half their time: without it 18000 x 576 x 160 took 64 rows a workgroup and 56 us, in tiles 38; 114048 x 576 x 45 122 and 76;
+// 24 x 6752 x 46704, which stays, 321 and 335.
 struct RowsPlan {
     int rb, splits;
     double us;
@@ -344,12 +346,13 @@ RowsPlan plan_rows(int64_t rows, int N, int K, int dtype, bool direct)
     p.rb = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
     const double groups = (double)((rows + 16 * p.rb - 1) / (16 * p.rb)) * ((N + 15) / 16);
     const double bytes = 16.0 * (1 + p.rb) * K * size, alone = bytes / 120e3 * std::ceil(groups / 256);
+    const double matrix = dtype == CONV_F32 ? 0.5 * 2 * 16 * 16 * p.rb * (double)K / 0.61e6 : 0.0;
     p.splits = 1;
     // (pieces that start anywhere: twice that for 64 rows, whose loads outweigh the weights')
-    p.us = 2.8 + (direct || p.rb < 4 ? 1 : 2) * (alone + std::max(groups * bytes / 33e6, groups / 256 * 0.16 * p.rb));
+    p.us = 2.8 + (direct || p.rb < 4 ? 1 : 2) * (alone + std::max(groups * bytes / 33e6, groups / 256 * 0.16 * p.rb)) + matrix * std::ceil(groups / 256);
     if (groups <= 64) {
         const int most = std::min({16, (int)(256 / groups), (int)((K * size + 1023) / 1024)});
-        if (alone - alone / most > 6) p.splits = most, p.us = 8 + alone / most;
+        if (alone - alone / most > 6) p.splits = most, p.us = 8 + (alone + matrix) / most;
     }
     return p;
 }

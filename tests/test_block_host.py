@@ -264,3 +264,13 @@ def test_a_gate_for_more_rows_than_there_are_is_one_for_all(rows, cols, dtype):
     """Rows are shared out among workgroups by what there is of them, and so is the room for their sums."""
     need = [B.residual_norm_bwd_workspace_bytes(B.make_residual_norm_desc(rows, cols, dtype, gate_rows=n)) for n in (max(2, rows), 2 * rows + 1, (1 << 31) - 1)]
     assert need[0] == need[1] == need[2]
+
+
+def test_fp32_rows_take_the_faster_form():
+    """fp32 matrix instructions are slow enough to count: many rows over few outputs go through tiles, few rows and very few outputs do not."""
+    form = lambda r, n, k: B.linear_form(B.make_linear_desc(r, n, k, B.CONV_F32), 0, 0)  # noqa: E731
+    for many in ((114048, 45, 576), (18000, 160, 576), (1744, 62, 3476)):
+        assert form(*many).startswith("split_tile"), many
+    assert form(24, 46704, 6752) == "rows32" and form(17, 4096, 4096) == "rows32"
+    for few in ((100000, 16, 256), (4000, 40, 300), (20000, 31, 1000), (128, 4096, 512), (200, 1000, 1000)):
+        assert form(*few).startswith("rows64"), few
