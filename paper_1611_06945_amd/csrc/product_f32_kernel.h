@@ -175,19 +175,24 @@ __global__ __launch_bounds__(T::NT) void product_f32_kernel(SplitArgs g, LinearO
         __syncthreads();
     }
 
-    // a lane has four n in a row, 16 bytes
+    // a lane has four n in a row, 16 bytes; the blocks of a row one after the other
+    float columns[T::FN][4];
+    if constexpr (!PARTIAL) {
 #pragma unroll
-    for (int i = 0; i < T::FN; ++i) {
-        const int nl = (wn * T::FN + i) * 16 + (lane >> 4) * 4;
+        for (int i = 0; i < T::FN; ++i) __builtin_memcpy(columns[i], bias + (wn * T::FN + i) * 16 + (lane >> 4) * 4, 16);
+    }
 #pragma unroll
-        for (int j = 0; j < T::FT; ++j) {
-            const int ml = (wt * T::FT + j) * 16 + (lane & 15);
+    for (int j = 0; j < T::FT; ++j) {
+        const int ml = (wt * T::FT + j) * 16 + (lane & 15);
+        const int64_t m = g.m_first + m0 + ml;
+#pragma unroll
+        for (int i = 0; i < T::FN; ++i) {
+            const int nl = (wn * T::FN + i) * 16 + (lane >> 4) * 4;
             if (ml < a.pieces.here && nl < b.pieces.here) {
                 float v[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
                 const int have = min(4, b.pieces.here - nl);
-                const int64_t m = g.m_first + m0 + ml;
                 if constexpr (PARTIAL) put_pieces<CONV_F32, 4>(g.partial, ((int64_t)share * g.M + m) * g.N + n0 + nl, v, have);
-                else LinearEpi<CONV_F32>::finish(ProductArgs(), e, v, m, n0 + nl, have, bias + nl);
+                else LinearEpi<CONV_F32>::finish(ProductArgs(), e, v, m, n0 + nl, have, columns[i]);
             }
         }
         __builtin_amdgcn_sched_barrier(0);
