@@ -274,3 +274,13 @@ def test_fp32_rows_take_the_faster_form():
     assert form(24, 46704, 6752) == "rows32" and form(17, 4096, 4096) == "rows32"
     for few in ((100000, 16, 256), (4000, 40, 300), (20000, 31, 1000), (128, 4096, 512), (200, 1000, 1000)):
         assert form(*few).startswith("rows64"), few
+
+
+def test_fp32_gradients_take_the_faster_form():
+    """Small tiles of operands that lie across the reduction are slower than larger ones that share it."""
+    form = lambda r, n, k, which: B.linear_form(B.make_linear_desc(r, n, k, B.CONV_F32), 0, 0, which)  # noqa: E731
+    for size in ((1024, 1024, 1024), (1300, 1111, 640)):
+        assert form(*size, 1).startswith("split_tile128x128_split") and form(*size, 2).startswith("split_tile128x128_split"), size
+    assert form(600, 1000, 1000, 1).startswith("split_tile128x128_split")
+    assert form(600, 1000, 1000, 2) == form(300, 700, 3000, 1) == form(300, 300, 300, 1) == form(300, 300, 300, 2) == "split_tile64x64"
+    assert form(1024, 1024, 1024, 0) == "split_tile64x64"

@@ -293,3 +293,10 @@ def test_calls_give_the_same_bits():
             results.append((out, pre, dx, dw, db))
         for again in results[1:]:
             assert all(torch.equal(p, q) for p, q in zip(results[0], again))
+
+
+@pytest.mark.parametrize("start", [0, 1])
+@pytest.mark.parametrize("rows,N,K", [(1024, 1024, 1024), (1300, 1111, 640), (600, 1000, 1000), (2, 4100, 3001)])
+def test_fp32_gradients_of_shared_reductions(rows, N, K, start):
+    forms = check_bwd(rows, N, K, wl.F32, "silu", start=start)
+    assert any("_split" in f[5:] for f in forms)
