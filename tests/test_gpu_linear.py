@@ -300,3 +300,27 @@ def test_calls_give_the_same_bits():
 def test_fp32_gradients_of_shared_reductions(rows, N, K, start):
     forms = check_bwd(rows, N, K, wl.F32, "silu", start=start)
     assert any("_split" in f[5:] for f in forms)
+
+
+def test_fp32_operands_that_parts_do_not_hold():
+    """As documented: of small operands what lies below 2^-126 counts as zero, and infinities give NaN in tiles, themselves in few rows."""
+    torch = torch_mod()
+    rng = np.random.default_rng(2)
+    inf = float("inf")
+    for rows, N, K in ((700, 1032, 40), (4, 40, 64)):
+        x, w = stored(2.0 ** -112 * rng.normal(size=(rows, K)), wl.F32), stored(rng.normal(size=(N, K)), wl.F32)
+        X, W = Rows(rows, K, torch.float32, fill=inf).set(x), Rows(N, K, torch.float32, fill=inf).set(w)
+        Y = Rows(rows, N, torch.float32, fill=7.0)
+        d = B.make_linear_desc(rows, N, K, wl.F32)
+        need = B.linear_workspace_bytes(d)
+        B.linear_fwd(d, X.ptr, W.ptr, None, None, Y.ptr, None, workspace(need), need)
+        _, z, size = ro.linear(x, w, None, None, "none")
+        # (each of x's three parts may lose as much as one that rounds to the smallest normal number)
+        assert_close(Y.host(), z, (K + 4) * EPS32 * size + 2 * 2.0 ** -126 * np.abs(w).sum(1), "small")
+        tiles = B.linear_form(d, X.ptr, W.ptr).startswith("split_")
+        assert tiles == (rows == 700)
+        X.set(np.ones((rows, K))), W.set(np.ones((N, K)))
+        X.view[1, 3] = inf
+        B.linear_fwd(d, X.ptr, W.ptr, None, None, Y.ptr, None, workspace(need), need)
+        got = Y.host()
+        assert (np.isnan(got[1]) if tiles else np.isposinf(got[1])).all() and (np.delete(got, 1, 0) == K).all()
