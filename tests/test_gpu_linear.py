@@ -307,7 +307,7 @@ def test_fp32_operands_that_parts_do_not_hold():
     torch = torch_mod()
     rng = np.random.default_rng(2)
     inf = float("inf")
-    for rows, N, K in ((700, 1032, 40), (4, 40, 64)):
+    for rows, N, K in ((3000, 2056, 136), (4, 40, 64)):
         x, w = stored(2.0 ** -112 * rng.normal(size=(rows, K)), wl.F32), stored(rng.normal(size=(N, K)), wl.F32)
         X, W = Rows(rows, K, torch.float32, fill=inf).set(x), Rows(N, K, torch.float32, fill=inf).set(w)
         Y = Rows(rows, N, torch.float32, fill=7.0)
@@ -318,7 +318,7 @@ def test_fp32_operands_that_parts_do_not_hold():
         # (each of x's three parts may lose as much as one that rounds to the smallest normal number)
         assert_close(Y.host(), z, (K + 4) * EPS32 * size + 2 * 2.0 ** -126 * np.abs(w).sum(1), "small")
         tiles = B.linear_form(d, X.ptr, W.ptr).startswith("split_")
-        assert tiles == (rows == 700)
+        assert tiles == (rows == 3000)
         X.set(np.ones((rows, K))), W.set(np.ones((N, K)))
         X.view[1, 3] = inf
         B.linear_fwd(d, X.ptr, W.ptr, None, None, Y.ptr, None, workspace(need), need)
