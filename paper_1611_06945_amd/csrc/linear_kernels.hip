@@ -303,24 +303,27 @@ struct ProductPlan {
     ProductForm rest;
     int rest_splits;
 };
-// across: operands that lie across the reduction, which cost small fp32 tiles more (1024 x 1024 x 1024 in tiles of 64 x 64: 22.5, 25.4 and 26.9 us with 0, 1 and 2 of them; of
-// 128 x 128 in four shares 23.8)
-ProductPlan plan_product(int64_t M, int64_t N, int64_t K, int dtype, bool direct, int across, int parts = 1, bool whole = false)
+// across: an operand lies across the reduction, which costs a lone fp32 tile of 64 x 64 more (1024 x 1024 x 1024: 22.5 and 24.3 us; of 128 x 128 in four
+// shares 23.7); a CU that has more of these tiles than one has several at a time, whose steps but the first take two thirds of the time (476 of 13 steps 31 us, 1024 of 32 124).
+ProductPlan plan_product(int64_t M, int64_t N, int64_t K, int dtype, bool direct, bool across, int parts = 1, bool whole = false)
 {
     ProductPlan best = {P64, 1, 1e30, M, P64, 1};
     const int64_t ksteps = (K + 63) / 64;
     const bool f32 = dtype == CONV_F32;
     for (int f = f32 || direct ? P64 : P64_ANY; f <= (f32 ? P256 : direct ? P192 : P128_ANY); ++f) {
         const TileCost& c = f32 ? kTilesF32[f] : kTiles[f];
-        const double step = c.step + (f32 && f == P64 ? 0.12 * across : 0.0);
+        const bool small_across = f32 && f == P64 && across;
+        const double step = c.step + (small_across ? 0.12 : 0.0), later = small_across ? 0.63 : 1.0;
+        const auto time_of = [&](double turns, int64_t steps) { return turns * (c.own + step) + ((1 + later * (turns - 1)) * (parts * steps - 1)) * step; };
         const int64_t tm = (M + c.bt - 1) / c.bt, tn = (N + c.bn - 1) / c.bn;
         const double tiles = (double)tm * tn;
         for (int splits = 1; splits <= 64; splits *= 2) {
             if (splits > 1 && (splits * 4 > ksteps || tiles * splits > 2048)) break;
             const int64_t each = (ksteps + splits - 1) / splits;
             const int shares = (int)((ksteps + each - 1) / each);  // none without a step
-            double us = c.once + std::ceil(tiles * shares / 256) * (c.own + parts * each * step);
-            if (shares > 1) us += f32 ? 2 + 5.5 * shares * M * N / 4e6 : 5 + 8.0 * shares * M * N / 4e6;  // written, read and added by a second launch
+            const double turns = std::ceil(tiles * shares / 256);
+            double us = c.once + time_of(turns, each);
+            if (shares > 1) us += f32 && across ? 4 + 6.0 * shares * M * N / 4e6 : 5 + 8.0 * shares * M * N / 4e6;  // written, read and added by a second launch
             if (us < best.us) best = {(ProductForm)f, shares, us, M, P64, 1};
         }
         // Whole rounds of tiles, and what is left by smaller ones or with a shared reduction (50257 x 1024 x 2048: 788 tiles of 256 x 256 are
@@ -328,7 +331,7 @@ ProductPlan plan_product(int64_t M, int64_t N, int64_t K, int dtype, bool direct
         const int64_t rounds = (int64_t)(tiles / 256), first = rounds * 256 / tn;
         if (whole || rounds < 1 || rounds > 16 || first < 1 || first >= tm) continue;
         const ProductPlan rest = plan_product(M - first * c.bt, N, K, dtype, direct, across, parts, true);
-        const double us = c.once + rounds * (c.own + parts * ksteps * step) + rest.us;
+        const double us = c.once + time_of(rounds, ksteps) + rest.us;
         if (us < best.us) best = {(ProductForm)f, 1, us, first * c.bt, rest.form, rest.splits};
     }
     return best;
@@ -373,7 +376,7 @@ LinearForm form_of(int64_t rows, int N, int K, int dtype, bool direct)
     LinearForm f;
     f.direct = direct;
     f.few = plan_rows(rows, N, K, dtype, direct);
-    f.tiles = plan_product(rows, N, K, dtype, direct, 0);
+    f.tiles = plan_product(rows, N, K, dtype, direct, false);
     f.rows = rows <= 16 || f.few.us <= f.tiles.us;
     return f;
 }
@@ -519,8 +522,8 @@ BwdSpace bwd_space(const LinearArgs& a, int dtype, void* ws)
     s.sums = (float*)c.take((size_t)dz_parts(a.rows, a.N) * a.N * 4);
     size_t most = 0;
     for (const bool direct : {true, false}) {
-        most = std::max(most, partial_bytes(plan_product(a.rows, a.K, a.N, dtype, direct, 1, parts), a.rows, a.K));
-        most = std::max(most, partial_bytes(plan_product(a.N, a.K, a.rows, dtype, direct, 2, parts), a.N, a.K));
+        most = std::max(most, partial_bytes(plan_product(a.rows, a.K, a.N, dtype, direct, true, parts), a.rows, a.K));
+        most = std::max(most, partial_bytes(plan_product(a.N, a.K, a.rows, dtype, direct, true, parts), a.N, a.K));
     }
     s.partial = (float*)c.take(most);
     s.bytes = c.used;
@@ -598,12 +601,12 @@ hipError_t launch_linear_bwd(const LinearArgs& a, int dtype, hipStream_t s)
         if (e != hipSuccess) return e;
     }
     if (a.dx) {
-        const ProductPlan p = plan_product(a.rows, a.K, a.N, dtype, on_16(w.p, w.ld, es) && on_16(dz.p, dz.ld, es), 1, parts);
+        const ProductPlan p = plan_product(a.rows, a.K, a.N, dtype, on_16(w.p, w.ld, es) && on_16(dz.p, dz.ld, es), true, parts);
         const hipError_t e = multiply(dtype, LAYOUT_NN, dz, w, a.rows, a.K, a.N, {nullptr, nullptr, nullptr, a.dx, 0, a.ldx, ACT_NONE}, p, space.partial, s);
         if (e != hipSuccess) return e;
     }
     if (a.dw) {
-        const ProductPlan p = plan_product(a.N, a.K, a.rows, dtype, on_16(x.p, x.ld, es) && on_16(dz.p, dz.ld, es), 2, parts);
+        const ProductPlan p = plan_product(a.N, a.K, a.rows, dtype, on_16(x.p, x.ld, es) && on_16(dz.p, dz.ld, es), true, parts);
         const hipError_t e = multiply(dtype, LAYOUT_TN, dz, x, a.N, a.K, a.rows, {nullptr, nullptr, nullptr, a.dw, 0, a.ldw, ACT_NONE}, p, space.partial, s);
         if (e != hipSuccess) return e;
     }
@@ -625,9 +628,9 @@ int linear_form_name(const LinearArgs& a, int dtype, int which, char* buf, size_
         }
         p = f.tiles;
     } else if (which == 1) {
-        p = plan_product(a.rows, a.K, a.N, dtype, w16, 1, parts);
+        p = plan_product(a.rows, a.K, a.N, dtype, w16, true, parts);
     } else {
-        p = plan_product(a.N, a.K, a.rows, dtype, x16, 2, parts);
+        p = plan_product(a.N, a.K, a.rows, dtype, x16, true, parts);
     }
     auto one = [&](char* to, size_t room, ProductForm form, int splits) {
         const char* const name = dtype == CONV_F32 && form == P256 ? "tile256x128" : tiles[form];

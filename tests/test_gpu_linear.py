@@ -296,7 +296,7 @@ def test_calls_give_the_same_bits():
 
 
 @pytest.mark.parametrize("start", [0, 1])
-@pytest.mark.parametrize("rows,N,K", [(1024, 1024, 1024), (1300, 1111, 640), (600, 1000, 1000), (2, 4100, 3001)])
+@pytest.mark.parametrize("rows,N,K", [(1000, 300, 2000), (1300, 1111, 640), (600, 1000, 1000), (2, 4100, 3001)])
 def test_fp32_gradients_of_shared_reductions(rows, N, K, start):
     forms = check_bwd(rows, N, K, wl.F32, "silu", start=start)
     assert any("_split" in f[5:] for f in forms)
