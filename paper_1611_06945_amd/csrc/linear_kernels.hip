@@ -60,22 +60,23 @@ __device__ __forceinline__ u32x4 first_of_piece(u32x4 v, int n)
     }
 }
 
-// A workgroup 16 outputs x 16 RB rows, its W waves share the reduction: wave w takes every W-th run of 64 U bytes.  The weights' stream is what
+// A workgroup 16 NB outputs x 16 RB rows, its W waves share the reduction: wave w takes every W-th run of 64 U bytes.  The weights' stream is what
 // counts, so loads are made of four lanes a 64-byte stretch of a row (a lane a row, as the matrix instruction wants them, is
 // served 16 bytes a clock), straight into LDS the wave has for itself, no barrier; a row's four pieces lie at piece ^ (row / 4 % 4) there, so
 // that no two of 16 lanes read a bank.  The waves' sums meet in LDS.  gridDim.z workgroups may share a long reduction (linear_join).
 // DIRECT: rows start on 16 bytes; otherwise pieces go through registers.  Bound by the weights' stream: 1 x 4096 x 4096 fp16 7.7 us, 4.4 TB/s from memory
-// (a launch, the first loads and the join of waves in it), 1 x 65536 x 4096 bf16 86 us, 6.2 TB/s, in part from the caches.
-template <int DT, int RB, int W, int U, bool DIRECT>
+// (a launch, the first loads and the join of waves in it), 1 x 65536 x 4096 bf16 86 us, 6.2 TB/s, in part from the caches.  In fp32 the rows of x, read again for every 16
+// outputs, take longer than the weights: NB > 1 where that leaves workgroups for most CUs (24 x 6752 x 46704 320 -> 226 us, 16 x 4099 x 16001 72 -> 54).
+template <int DT, int NB, int RB, int W, int U, bool DIRECT>
 __global__ __launch_bounds__(64 * W) void linear_rows(LinearRows g)
 {
     typedef typename Prec<DT>::elem_t elem_t;
-    constexpr int NT = 64 * W, ES = sizeof(elem_t), VEC = 16 / ES, RUN = 64 * U / ES, SLOT = (1 + RB) * U * 1024, OWN = (DIRECT ? 2 : 1) * SLOT;
+    constexpr int NT = 64 * W, ES = sizeof(elem_t), VEC = 16 / ES, RUN = 64 * U / ES, SLOT = (NB + RB) * U * 1024, OWN = (DIRECT ? 2 : 1) * SLOT;
     extern __shared__ __attribute__((aligned(16))) char smem[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int n0 = blockIdx.x * 16;
+    const int n0 = blockIdx.x * (16 * NB);
     const int64_t t0 = (int64_t)blockIdx.y * (16 * RB);
-    const int rows_here = (int)min((int64_t)(16 * RB), g.rows - t0), outs_here = min(16, g.N - n0);
+    const int rows_here = (int)min((int64_t)(16 * RB), g.rows - t0), outs_here = min(16 * NB, g.N - n0);
     const elem_t *const x = (const elem_t*)g.x + t0 * g.ldx, *const w = (const elem_t*)g.w + (int64_t)n0 * g.ldw;
     const int row = lane >> 2, piece = (lane & 3) ^ ((row >> 2) & 3);
     char* const own = smem + wave * OWN;
@@ -104,19 +105,24 @@ __global__ __launch_bounds__(64 * W) void linear_rows(LinearRows g)
         }
     };
 
-    f32x4 acc[RB];
+    f32x4 acc[NB][RB];
 #pragma unroll
-    for (int j = 0; j < RB; ++j) acc[j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int i = 0; i < NB; ++i)
+#pragma unroll
+        for (int j = 0; j < RB; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     // DIRECT: a run's loads, into one of two places
     auto ask = [&](int k, char* slot) {
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rw, (lds_void_t*)(slot + u * 1024), 16, (int)(woff + (uint32_t)k * ES + u * 64), 0, 0, 0);
+        for (int i = 0; i < NB; ++i)
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(rw, (lds_void_t*)(slot + (i * U + u) * 1024), 16,
+                                                         (int)(woff + (uint32_t)(i * 16) * (uint32_t)(g.ldw * ES) + (uint32_t)k * ES + u * 64), 0, 0, 0);
 #pragma unroll
         for (int j = 0; j < RB; ++j)
 #pragma unroll
             for (int u = 0; u < U; ++u)
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(rx, (lds_void_t*)(slot + ((1 + j) * U + u) * 1024), 16,
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(rx, (lds_void_t*)(slot + ((NB + j) * U + u) * 1024), 16,
                                                          (int)(xoff + (uint32_t)(j * 16) * (uint32_t)(g.ldx * ES) + (uint32_t)k * ES + u * 64), 0, 0, 0);
     };
     const int first = (blockIdx.z * W + wave) * RUN, step = gridDim.z * W * RUN;
@@ -126,28 +132,31 @@ __global__ __launch_bounds__(64 * W) void linear_rows(LinearRows g)
         if constexpr (DIRECT) {
             if (k + step < g.K) {
                 ask(k + step, slot == own ? own + SLOT : own);
-                asm volatile("s_waitcnt vmcnt(%0)" ::"n"((1 + RB) * U) : "memory");
+                asm volatile("s_waitcnt vmcnt(%0)" ::"n"((NB + RB) * U) : "memory");
             } else {
                 asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
             }
         } else {
-            u32x4 got[1 + RB][U];
-            pieces(w, g.ldw, row, outs_here, k, got[0]);
+            u32x4 got[NB + RB][U];
 #pragma unroll
-            for (int j = 0; j < RB; ++j) pieces(x, g.ldx, j * 16 + row, rows_here, k, got[1 + j]);
+            for (int i = 0; i < NB; ++i) pieces(w, g.ldw, i * 16 + row, outs_here, k, got[i]);
 #pragma unroll
-            for (int j = 0; j < 1 + RB; ++j)
+            for (int j = 0; j < RB; ++j) pieces(x, g.ldx, j * 16 + row, rows_here, k, got[NB + j]);
+#pragma unroll
+            for (int j = 0; j < NB + RB; ++j)
 #pragma unroll
                 for (int u = 0; u < U; ++u) *(u32x4*)(own + (j * U + u) * 1024 + lane * 16) = got[j][u];
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         }
-        u32x4 wv[U], xv[RB][U];
+        u32x4 wv[NB][U], xv[RB][U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) wv[u] = *(const u32x4*)(slot + mine + u * 1024);
+        for (int i = 0; i < NB; ++i)
+#pragma unroll
+            for (int u = 0; u < U; ++u) wv[i][u] = *(const u32x4*)(slot + mine + (i * U + u) * 1024);
 #pragma unroll
         for (int j = 0; j < RB; ++j)
 #pragma unroll
-            for (int u = 0; u < U; ++u) xv[j][u] = *(const u32x4*)(slot + mine + ((1 + j) * U + u) * 1024);
+            for (int u = 0; u < U; ++u) xv[j][u] = *(const u32x4*)(slot + mine + ((NB + j) * U + u) * 1024);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // read before the next but one run's loads may land
         if (DIRECT) slot = slot == own ? own + SLOT : own;
         if (DIRECT && k + RUN > g.K) {
@@ -155,7 +164,8 @@ __global__ __launch_bounds__(64 * W) void linear_rows(LinearRows g)
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const int n = g.K - k - u * (64 / ES) - (lane >> 4) * VEC;
-                wv[u] = first_of_piece<DT>(wv[u], n);
+#pragma unroll
+                for (int i = 0; i < NB; ++i) wv[i][u] = first_of_piece<DT>(wv[i][u], n);
 #pragma unroll
                 for (int j = 0; j < RB; ++j) xv[j][u] = first_of_piece<DT>(xv[j][u], n);
             }
@@ -163,19 +173,23 @@ __global__ __launch_bounds__(64 * W) void linear_rows(LinearRows g)
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
-            for (int j = 0; j < RB; ++j) acc[j] = multiply_pieces<DT>(wv[u], xv[j][u], acc[j]);
+            for (int i = 0; i < NB; ++i)
+#pragma unroll
+                for (int j = 0; j < RB; ++j) acc[i][j] = multiply_pieces<DT>(wv[i][u], xv[j][u], acc[i][j]);
     }
     __syncthreads();
     f32x4* const part = (f32x4*)smem;
 #pragma unroll
-    for (int j = 0; j < RB; ++j) part[(wave * RB + j) * 64 + lane] = acc[j];
+    for (int i = 0; i < NB; ++i)
+#pragma unroll
+        for (int j = 0; j < RB; ++j) part[((wave * NB + i) * RB + j) * 64 + lane] = acc[i][j];
     __syncthreads();
-    for (int o = threadIdx.x; o < 256 * RB; o += NT) {
-        const int n = n0 + (o & 15), r = o >> 4;  // output; row among the workgroup's
+    for (int o = threadIdx.x; o < 256 * NB * RB; o += NT) {
+        const int l = o % (16 * NB), n = n0 + l, r = o / (16 * NB);  // output; row among the workgroup's
         if (n >= g.N || r >= rows_here) continue;
         float sum = 0.0f;
 #pragma unroll
-        for (int v = 0; v < W; ++v) sum += ((const float*)&part[(v * RB + (r >> 4)) * 64 + ((o & 15) >> 2) * 16 + (r & 15)])[o & 3];
+        for (int v = 0; v < W; ++v) sum += ((const float*)&part[((v * NB + (l >> 4)) * RB + (r >> 4)) * 64 + ((l & 15) >> 2) * 16 + (r & 15)])[l & 3];
         if (gridDim.z > 1)
             g.partial[((int64_t)blockIdx.z * g.rows + t0 + r) * g.N + n] = sum;
         else
@@ -339,23 +353,33 @@ ProductPlan plan_product(int64_t M, int64_t N, int64_t K, int dtype, bool direct
 
 // Few rows: blocks of 16 rows a workgroup, workgroups that share a reduction, expected us.  A workgroup reads 120 KB in a us, all of them
 // 33 TB/s (from the caches mostly), and one takes 0.16 us of a CU a block at least; a second launch to add shares costs about 5 us of a call.  The fp32 matrix
-// instructions, 0.61 MFLOP a us and CU, add half their time: without it 18000 x 576 x 160 took 64 rows a workgroup and 56 us, in tiles 38; 114048 x 576 x 45 122 and 76;
-// 24 x 6752 x 46704, which stays, 321 and 335.
+// instructions, 0.61 MFLOP a us and CU, add half their time: without it 18000 x 576 x 160 took 64 rows a workgroup and 56 us, in tiles 38; 114048 x 576 x 45 122 and 76.
 struct RowsPlan {
-    int rb, splits;
+    int rb, nb, splits;
     double us;
 };
+// Blocks of 16 outputs a workgroup, in fp32: four, or two of rows that start anywhere, where that makes 192 workgroups or more (20 x 1024 x 8192 in 128 of
+// them takes 14 us, one block each 12); 16 rows on 16 bytes take one (57 us for 16 x 4096 x 16000, with two 59), and so do short sums of more than 32 rows (40 x 544 x 45824: 50, with four 53).
+int blocks_of_outputs(int64_t rows, int rb, int N, int K, int dtype, bool direct)
+{
+    const int nb = direct ? 4 : 2;
+    if (dtype != CONV_F32 || rows > 64 || K * 4 <= 1024 || N < 192 * 16 * nb) return 1;
+    if (rb == 1) return direct ? 1 : nb;
+    return rb == 4 && (!direct || K < 1024) ? 1 : nb;
+}
 RowsPlan plan_rows(int64_t rows, int N, int K, int dtype, bool direct)
 {
     RowsPlan p;
     const double size = dtype_size(dtype);
     p.rb = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
-    const double groups = (double)((rows + 16 * p.rb - 1) / (16 * p.rb)) * ((N + 15) / 16);
-    const double bytes = 16.0 * (1 + p.rb) * K * size, alone = bytes / 120e3 * std::ceil(groups / 256);
-    const double matrix = dtype == CONV_F32 ? 0.5 * 2 * 16 * 16 * p.rb * (double)K / 0.61e6 : 0.0;
+    p.nb = blocks_of_outputs(rows, p.rb, N, K, dtype, direct);
+    const double groups = (double)((rows + 16 * p.rb - 1) / (16 * p.rb)) * ((N + 16 * p.nb - 1) / (16 * p.nb));
+    const double bytes = 16.0 * (p.nb + p.rb) * K * size, alone = bytes / 120e3 * std::ceil(groups / 256);
+    const double matrix = dtype == CONV_F32 ? 0.5 * 2 * 16 * 16 * p.nb * p.rb * (double)K / 0.61e6 : 0.0;
     p.splits = 1;
     // (pieces that start anywhere: twice that for 64 rows, whose loads outweigh the weights')
     p.us = 2.8 + (direct || p.rb < 4 ? 1 : 2) * (alone + std::max(groups * bytes / 33e6, groups / 256 * 0.16 * p.rb)) + matrix * std::ceil(groups / 256);
+    if (p.nb > 1) p.us = std::max(p.us, 2.8 + N * (K * size) / 5.3e6 + matrix * std::ceil(groups / 256));  // ... and the weights come from memory
     if (groups <= 64) {
         const int most = std::min({16, (int)(256 / groups), (int)((K * size + 1023) / 1024)});
         if (alone - alone / most > 6) p.splits = most, p.us = 8 + (alone + matrix) / most;
@@ -377,6 +401,8 @@ LinearForm form_of(int64_t rows, int N, int K, int dtype, bool direct)
     f.direct = direct;
     f.few = plan_rows(rows, N, K, dtype, direct);
     f.tiles = plan_product(rows, N, K, dtype, direct, false);
+    // (few fp32 rows: tiles take the weights from memory at 3.2 TB/s)
+    if (dtype == CONV_F32 && rows <= 64) f.tiles.us = std::max(f.tiles.us, 4 + (double)N * K * 4 / 3.2e6);
     f.rows = rows <= 16 || f.few.us <= f.tiles.us;
     return f;
 }
@@ -440,14 +466,14 @@ size_t partial_bytes(const ProductPlan& p, int64_t M, int64_t N)
     return std::max(first, rest);
 }
 
-template <int DT, int RB, int W, int U, bool DIRECT>
+template <int DT, int NB, int RB, int W, int U, bool DIRECT>
 hipError_t launch_rows(const LinearRows& g, int splits, hipStream_t s)
 {
-    constexpr size_t LDS = (size_t)W * (1 + RB) * U * 1024 * (DIRECT ? 2 : 1);
-    const hipError_t e = ensure_dynamic_lds((const void*)linear_rows<DT, RB, W, U, DIRECT>, LDS);
+    constexpr size_t LDS = (size_t)W * (NB + RB) * U * 1024 * (DIRECT ? 2 : 1);
+    const hipError_t e = ensure_dynamic_lds((const void*)linear_rows<DT, NB, RB, W, U, DIRECT>, LDS);
     if (e != hipSuccess) return e;
     // gridDim.y is at most 65535, and a launch holds less than 2^32 threads: the rows go in portions
-    const int64_t across = (g.N + 15) / 16, portion = std::min<int64_t>(65535, std::max<int64_t>(1, (1 << 22) / across)) * (16 * RB);
+    const int64_t across = (g.N + 16 * NB - 1) / (16 * NB), portion = std::min<int64_t>(65535, std::max<int64_t>(1, (1 << 22) / across)) * (16 * RB);
     for (int64_t skip = 0; skip < g.rows; skip += portion) {
         LinearRows p = g;
         constexpr int ES = sizeof(typename Prec<DT>::elem_t);
@@ -455,7 +481,7 @@ hipError_t launch_rows(const LinearRows& g, int splits, hipStream_t s)
         p.x = (const char*)g.x + skip * g.ldx * ES, p.out.out = (char*)g.out.out + skip * g.out.ldo * ES;
         if (g.out.pre) p.out.pre = (char*)g.out.pre + skip * g.out.ldo * ES;
         if (g.out.residual) p.out.residual = (const char*)g.out.residual + skip * g.out.ldr * ES;
-        hipLaunchKernelGGL((linear_rows<DT, RB, W, U, DIRECT>), dim3((unsigned)((g.N + 15) / 16), (unsigned)((p.rows + 16 * RB - 1) / (16 * RB)), (unsigned)splits),
+        hipLaunchKernelGGL((linear_rows<DT, NB, RB, W, U, DIRECT>), dim3((unsigned)across, (unsigned)((p.rows + 16 * RB - 1) / (16 * RB)), (unsigned)splits),
                            dim3(64 * W), LDS, s, p);
         if (splits > 1) {
             const hipError_t j = join_as<DT>(p.out, g.partial, p.rows, g.N, splits, s);
@@ -472,15 +498,21 @@ hipError_t launch_rows(const LinearRows& g, const RowsPlan& p, hipStream_t s)
 {
     const int64_t bytes = (int64_t)g.K * (int)sizeof(typename Prec<DT>::elem_t);
     const bool narrow = bytes <= 1024, alone = (int64_t)(g.N + 15) / 16 * p.splits <= 384 && bytes >= 4096;
+    if constexpr (DT == CONV_F32) {
+        if (p.nb > 1) {
+            if constexpr (DIRECT) return p.rb == 2 ? launch_rows<DT, 4, 2, 4, 2, DIRECT>(g, p.splits, s) : launch_rows<DT, 4, 4, 4, 2, DIRECT>(g, p.splits, s);
+            else return p.rb == 1 ? launch_rows<DT, 2, 1, 4, 4, DIRECT>(g, p.splits, s) : launch_rows<DT, 2, 2, 4, 4, DIRECT>(g, p.splits, s);
+        }
+    }
     switch (p.rb) {
         case 1:
             if constexpr (DIRECT) {
-                if (alone) return launch_rows<DT, 1, 8, 4, DIRECT>(g, p.splits, s);
+                if (alone) return launch_rows<DT, 1, 1, 8, 4, DIRECT>(g, p.splits, s);
             }
-            return narrow ? launch_rows<DT, 1, 4, 2, DIRECT>(g, p.splits, s) : launch_rows<DT, 1, 8, 2, DIRECT>(g, p.splits, s);
+            return narrow ? launch_rows<DT, 1, 1, 4, 2, DIRECT>(g, p.splits, s) : launch_rows<DT, 1, 1, 8, 2, DIRECT>(g, p.splits, s);
         case 2:
-            return narrow ? launch_rows<DT, 2, 4, 2, DIRECT>(g, p.splits, s) : launch_rows<DT, 2, 8, 2, DIRECT>(g, p.splits, s);
-        default: return narrow || DIRECT ? launch_rows<DT, 4, 4, 2, DIRECT>(g, p.splits, s) : launch_rows<DT, 4, 8, 2, DIRECT>(g, p.splits, s);
+            return narrow ? launch_rows<DT, 1, 2, 4, 2, DIRECT>(g, p.splits, s) : launch_rows<DT, 1, 2, 8, 2, DIRECT>(g, p.splits, s);
+        default: return narrow || DIRECT ? launch_rows<DT, 1, 4, 4, 2, DIRECT>(g, p.splits, s) : launch_rows<DT, 1, 4, 8, 2, DIRECT>(g, p.splits, s);
     }
 }
 template <int DT>
@@ -623,7 +655,9 @@ int linear_form_name(const LinearArgs& a, int dtype, int which, char* buf, size_
     if (which == 0) {
         const LinearForm f = form_of(a.rows, a.N, a.K, dtype, x16 && w16);
         if (f.rows) {
-            const int len = std::snprintf(buf, n, "rows%d%s", 16 * f.few.rb, f.direct ? "" : "_any");
+            char outputs[8] = "";
+            if (f.few.nb > 1) std::snprintf(outputs, sizeof(outputs), "x%d", 16 * f.few.nb);
+            const int len = std::snprintf(buf, n, "rows%d%s%s", 16 * f.few.rb, outputs, f.direct ? "" : "_any");
             return f.few.splits > 1 && len > 0 && (size_t)len < n ? std::snprintf(buf + len, n - len, "_split%d", f.few.splits) : len;
         }
         p = f.tiles;

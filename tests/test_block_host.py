@@ -271,7 +271,7 @@ def test_fp32_rows_take_the_faster_form():
     form = lambda r, n, k: B.linear_form(B.make_linear_desc(r, n, k, B.CONV_F32), 0, 0)  # noqa: E731
     for many in ((114048, 45, 576), (18000, 160, 576), (1744, 62, 3476)):
         assert form(*many).startswith("split_tile"), many
-    assert form(24, 46704, 6752) == "rows32" and form(17, 4096, 4096) == "rows32"
+    assert form(24, 46704, 6752).startswith("rows32") and form(17, 4096, 4096) == "rows32"
     for few in ((100000, 16, 256), (4000, 40, 300), (20000, 31, 1000), (128, 4096, 512), (200, 1000, 1000)):
         assert form(*few).startswith("rows64"), few
 
@@ -283,3 +283,11 @@ def test_fp32_gradients_take_the_faster_form():
         assert form(*size, which).startswith("split_tile128x128_split"), size
     for size, which in (((600, 1000, 1000), 2), ((300, 700, 3000), 1), ((400, 3000, 400), 2), ((300, 300, 300), 1), ((1024, 1024, 1024), 0)):
         assert form(*size, which) == "split_tile64x64", size
+
+
+def test_few_fp32_rows_over_many_outputs_take_more_of_them_a_workgroup():
+    """x is read again for every workgroup's outputs, which takes longer than the weights."""
+    form = lambda r, n, k, at: B.linear_form(B.make_linear_desc(r, n, k, B.CONV_F32), at, at)  # noqa: E731
+    assert form(24, 46704, 6752, 0) == "rows32x64" and form(64, 16000, 4096, 0) == "rows64x64"
+    assert form(16, 16001, 4099, 4) == "rows16x32_any" and form(30, 16001, 4099, 4) == "rows32x32_any"
+    assert form(1, 16000, 4096, 0) == "rows16" and form(20, 8192, 1024, 0) == "rows32" and form(5, 4099, 999, 4) == "rows16_any"

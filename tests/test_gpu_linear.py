@@ -324,3 +324,17 @@ def test_fp32_operands_that_parts_do_not_hold():
         B.linear_fwd(d, X.ptr, W.ptr, None, None, Y.ptr, None, workspace(need), need)
         got = Y.host()
         assert (np.isnan(got[1]) if tiles else np.isposinf(got[1])).all() and (np.delete(got, 1, 0) == K).all()
+
+
+# rows, N, K, elements the operands start at -> the form that has to be taken
+WIDE = {"rows32x64": (21, 12305, 296, 0), "rows64x64": (45, 12345, 1032, 0), "rows16x32_any": (9, 6157, 301, 1), "rows32x32_any": (29, 6170, 273, 1)}
+
+
+@pytest.mark.parametrize("name", WIDE)
+def test_few_fp32_rows_over_many_outputs(name):
+    rows, N, K, start = WIDE[name]
+    for act, r in (("none", rows), ("silu", rows - 4)):
+        assert check_fwd(r, N, K, wl.F32, act, residual=True, pre=act == "silu", inplace=act == "none", pad=(0, 0, 3, 3), start=start, seed=r) == name
+    # ... and rows that lie apart
+    pad = 8 if start == 0 else 5
+    assert check_fwd(rows, N, K, wl.F32, "relu", pad=(pad, 2 * pad, 0, 1), start=start) == name
