@@ -105,11 +105,15 @@ __global__ __launch_bounds__(64 * W) void linear_rows(LinearRows g)
         }
     };
 
-    f32x4 acc[NB][RB];
+    // (fp32: two sums a wave, of every other 64 bytes, so that a wave's share of a long reduction is no longer chain than the library's)
+    constexpr int SUMS = DT == CONV_F32 ? 2 : 1;
+    f32x4 acc[SUMS][NB][RB];
 #pragma unroll
-    for (int i = 0; i < NB; ++i)
+    for (int a = 0; a < SUMS; ++a)
 #pragma unroll
-        for (int j = 0; j < RB; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        for (int i = 0; i < NB; ++i)
+#pragma unroll
+            for (int j = 0; j < RB; ++j) acc[a][i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     // DIRECT: a run's loads, into one of two places
     auto ask = [&](int k, char* slot) {
 #pragma unroll
@@ -175,14 +179,14 @@ __global__ __launch_bounds__(64 * W) void linear_rows(LinearRows g)
 #pragma unroll
             for (int i = 0; i < NB; ++i)
 #pragma unroll
-                for (int j = 0; j < RB; ++j) acc[i][j] = multiply_pieces<DT>(wv[i][u], xv[j][u], acc[i][j]);
+                for (int j = 0; j < RB; ++j) acc[u % SUMS][i][j] = multiply_pieces<DT>(wv[i][u], xv[j][u], acc[u % SUMS][i][j]);
     }
     __syncthreads();
     f32x4* const part = (f32x4*)smem;
 #pragma unroll
     for (int i = 0; i < NB; ++i)
 #pragma unroll
-        for (int j = 0; j < RB; ++j) part[((wave * NB + i) * RB + j) * 64 + lane] = acc[i][j];
+        for (int j = 0; j < RB; ++j) part[((wave * NB + i) * RB + j) * 64 + lane] = SUMS == 2 ? acc[0][i][j] + acc[SUMS - 1][i][j] : acc[0][i][j];
     __syncthreads();
     for (int o = threadIdx.x; o < 256 * NB * RB; o += NT) {
         const int l = o % (16 * NB), n = n0 + l, r = o / (16 * NB);  // output; row among the workgroup's

@@ -338,3 +338,19 @@ def test_few_fp32_rows_over_many_outputs(name):
     # ... and rows that lie apart
     pad = 8 if start == 0 else 5
     assert check_fwd(rows, N, K, wl.F32, "relu", pad=(pad, 2 * pad, 0, 1), start=start) == name
+
+
+@pytest.mark.parametrize("rows,N,K,start", [(1, 300, 16384, 0), (9, 6157, 4099, 1), (24, 12305, 4096, 0), (20, 400, 9001, 1), (48, 300, 4096, 0)])
+def test_long_fp32_sums_of_few_rows(rows, N, K, start):
+    """A sum is formed in eight chains of K / 8 terms or more of them.  At random signs the sums within a chain of n terms of size s grow as s sqrt(k), a rounding of which
+    is 2^-24 / sqrt(3) of it: 2^-24 s n / sqrt(6) in all, and for all chains 2^-24 sqrt(K / 8) / sqrt(6) of the result's norm."""
+    torch = torch_mod()
+    rng = np.random.default_rng(rows + K)
+    x, w = stored(rng.normal(size=(rows, K)), wl.F32), stored(rng.normal(size=(N, K)) * K ** -0.5, wl.F32)
+    X, W, Y = Rows(rows, K, torch.float32, start=start).set(x), Rows(N, K, torch.float32, start=start).set(w), torch.empty(rows, N, device="cuda")
+    d = B.make_linear_desc(rows, N, K, wl.F32)
+    need = B.linear_workspace_bytes(d)
+    B.linear_fwd(d, X.ptr, W.ptr, None, None, Y, None, workspace(need), need)
+    assert B.linear_form(d, X.ptr, W.ptr).startswith("rows")
+    want = x @ w.T
+    assert np.linalg.norm(Y.double().cpu().numpy() - want) <= EPS32 * (np.sqrt(K / 8) / np.sqrt(6) + 1) * np.linalg.norm(want)
