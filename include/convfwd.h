@@ -493,7 +493,7 @@ int linear_bwd(const linear_desc* desc, const void* x, const void* w, const void
                float* dbias, void* workspace, size_t workspace_bytes, void* stream);
 
 /* Name of the form that a product takes for this descriptor and these operands' addresses (which count modulo 16), NUL-terminated in
- * buf[0..n), e.g. "rows16", "tile256x256", "split_tile64x64_split4" or "parts_tile128x128" (of dz in two parts); `which`: 0 the product of linear_fwd, 1 and 2 those of linear_bwd for dx and
+ * buf[0..n), e.g. "rows16", "rows32x64" (rows x outputs), "tile256x256", "split_tile64x64_split4" or "parts_tile128x128" (of dz in two parts); `which`: 0 the product of linear_fwd, 1 and 2 those of linear_bwd for dx and
  * dw.  Empty for no rows.  Pure host code. */
 int linear_form(const linear_desc* desc, const void* x, const void* w, int which, char* buf, size_t n);
 

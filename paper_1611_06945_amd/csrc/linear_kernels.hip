@@ -202,7 +202,7 @@ __global__ __launch_bounds__(64 * W) void linear_rows(LinearRows g)
 }
 
 // Adds the sums of `splits` workgroups that shared a reduction, in their order, 16 of them on their way at a time (64 of 768 x 192: 17.5 us one after the
-// other, 7.4 so; 16 MB of results of two bytes from 64 MB 15 us).
+// other, 7.4 so; 4 MB of results of two bytes from 64 MB 15 us).
 template <int DT>
 __global__ __launch_bounds__(256) void linear_join(LinearOut e, const float* partial, int64_t rows, int N, int splits)
 {
@@ -220,7 +220,7 @@ __global__ __launch_bounds__(256) void linear_join(LinearOut e, const float* par
 
 // The gradient at the sum: dz = dout act'(pre), with its sums over the rows.  A workgroup has 256 columns and `each` rows, eight lanes of
 // rows; the sums are of the values before they are rounded.
-// Bound by memory: 200704 x 768 fp16 with GELU 194 us, 4.8 TB/s of two tensors read and one written.
+// Bound by memory: 200704 x 768 fp16 with GELU 258 us, 4.8 TB/s of two tensors read and two written.
 // TO: whether dz is written, with the row stride ldz: 1 in the storage type, where that holds it (no activation, or ReLU's, whose slopes are 0 and 1); 2 in two
 // parts, the low one `plane` elements behind the high one.  (In one part a gradient behind GELU was off by 1.4 times its own rounding, and an fp16 dz could become an infinity or zero.)
 template <int DT, int TO>

@@ -11,8 +11,8 @@
 //     bf16 result off by up to 2.1 times its own rounding, most where all singular values are alike (orthonormal 141 x 141 in five steps; normal ones 1.5; some strong directions
 //     above weak ones 1.1 to 1.3), and the steps' slopes let errors of early steps grow in late ones.  Even the first step alone in one plane counts where one
 //     direction is nearly all of x (700 x 700 of rank one 1.15).
-//   * Bound by the products where there are tiles for all CUs (4096 x 4096 bf16, five steps: 72, 75 and 134 us for the three products of a step, 1387 in all, 0.99 PFLOP/s), by
-//     17 launches one after the other where there are not (24 of 192 x 768 fp32: 11, 7 and 23 us a step, 215 in all).
+//   * Bound by the products where there are tiles for all CUs (4096 x 4096 bf16, five steps, traced: 241, 245 and 345 us for the three products of a step, 29 before them, 4184 in
+//     all; 4120 to 4220 without the trace, 0.99 PFLOP/s), by 17 launches one after the other where there are not (24 of 192 x 768 fp32: 11, 7 and 23 us a step, 213 in all).
 //   * X beside its products: fp32 for fp32; for 16-bit types the high and the low plane together, 22 bits, which is less to read and write.
 #include <algorithm>
 #include <cmath>

@@ -8,8 +8,8 @@
 // LDS, so operands may start anywhere.  A stage has 32 of the reduction: 64 bytes of each row and plane (pieces at piece ^ (row / 4 % 4)), or 32 rows
 // across.  There are two stages: the next one is split and written between the products of the present one, since splitting is as much vector work as half of
 // the products' time and a workgroup that did one after the other took 2.1 us a step of 128 x 128, whose products are 0.64.  A piece is asked for anew as soon as it is
-// split, a whole step ahead (8192 x 4096 x 4096: 1413 us with a step's loads behind its products, 1295 so, 212 TFLOP/s; 2048 x 2048 x 2048 105
-// and 96).  Bound by the splitting beside the products: vector work and matrix work are about as long, and two waves a SIMD overlap them in part.
+// split, a whole step ahead (8192 x 4096 x 4096: 1413 us with a step's loads behind its products, 1295 so; 2048 x 2048 x 2048 105
+// and 96).  Sums leave 16 bytes a lane, a row's blocks one after the other, so that lines are written whole (1196 us, 230 TFLOP/s; 91; 10824 x 80 x 1600 with sum and residual 112 -> 86).  Bound by the splitting beside the products: vector work and matrix work are about as long, and two waves a SIMD overlap them in part.
 #pragma once
 
 #include "linear_common.h"
