@@ -394,6 +394,11 @@ __global__ __launch_bounds__(T::NT) void product_kernel(ProductArgs g, typename 
     for (int i = 0; i < T::FN; ++i)
 #pragma unroll
         for (int j = 0; j < T::FT; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    // Two planes: the products with a low one add up apart, in small tiles also those of a step's second half, so that the large sums are of a third or a sixth as many
+    // terms: after six of the steps of orthogonal.hip fp32 matrices of 24 x 3168 are off by 1.9e-6 of the norm, with one sum 4.6e-6 (in fp32 products 1.6e-6).  (In tiles of 128 x
+    // 128 a third sum takes 5 to 8 % more time; the larger matrices that take those are off by 0.4 of what fp32 products are with two.)
+    constexpr bool APART = T::PL == 2, HALVES = APART && T::FN * T::FT <= 2;
+    f32x4 apart[HALVES ? 2 : 1][APART ? T::FN : 1][APART ? T::FT : 1] = {};
 
     u32x4 av[2][T::PL][T::HB], bv[2][T::PL][T::FN];
     // The operands of phase p of a stage (half p / H, portion p % H of the rows) to the registers of its parity.
@@ -417,8 +422,10 @@ __global__ __launch_bounds__(T::NT) void product_kernel(ProductArgs g, typename 
 #pragma unroll
             for (int j = 0; j < T::HB; ++j)
 #pragma unroll
-                for (int i = 0; i < T::FN; ++i)
-                    acc[i][h * T::HB + j] = multiply16<DT>(bv[s][t == 1 ? 1 : 0][i], av[p & 1][t == 0 ? 1 : 0][j], acc[i][h * T::HB + j]);
+                for (int i = 0; i < T::FN; ++i) {
+                    f32x4& sum = (APART && t < 2) || (HALVES && s == 1) ? apart[HALVES && t == 2 ? 1 : 0][APART ? i : 0][APART ? h * T::HB + j : 0] : acc[i][h * T::HB + j];
+                    sum = multiply16<DT>(bv[s][t == 1 ? 1 : 0][i], av[p & 1][t == 0 ? 1 : 0][j], sum);
+                }
     };
     constexpr int PHASES = 2 * T::H, LOADS = T::PL * (T::LA + T::LW);
     typedef std::integral_constant<int, 0> First;
@@ -574,6 +581,15 @@ __global__ __launch_bounds__(T::NT) void product_kernel(ProductArgs g, typename 
         multiply_all();
     }
 
+    if constexpr (APART) {
+#pragma unroll
+        for (int i = 0; i < T::FN; ++i)
+#pragma unroll
+            for (int j = 0; j < T::FT; ++j) {
+                if constexpr (HALVES) acc[i][j] += apart[1][i][j];
+                acc[i][j] += apart[0][i][j];
+            }
+    }
     const int grp = lane >> 4;
 #pragma unroll
     for (int i = 0; i < T::FN; i += 2) {

@@ -63,3 +63,20 @@ def test_bf16_results_are_off_by_their_rounding(rows, cols, steps, kind):
     assert off <= least + 2 * error_before_rounding(rows, cols, steps) * np.linalg.norm(want), off / least
     # (a tenth more at most where roundings of many elements make up the norm)
     assert kind == "spike" or off <= 1.1 * least, off / least
+
+
+@pytest.mark.parametrize("batch,rows,cols", [(12, 3168, 24), (2, 38, 3475), (3, 2500, 60)])
+def test_fp32_results_of_long_thin_matrices(batch, rows, cols):
+    """The squares that X X^T adds up are all positive: a sum in order is off by half a rounding for each instruction's worth of them, half that in the mean, and the
+    roundings of one sign add.  64 elements go to each of the two sums that one instruction in two adds to: K / 64 terms, K / 64 2^-26 of the element.  A step moves the singular values by
+    (b s^2 + 2 c s^4) times that, 3 at most, and later steps turn its sign.  Parts of 22 bits and the short products leave 1e-6 besides."""
+    torch = torch_mod()
+    long = max(rows, cols)
+    x = np.stack([stored(1e-3 * matrix(rows, cols, "mixed", i), wl.F32) for i in range(batch)])
+    t = torch.from_numpy(x).float().cuda()
+    y = torch.empty_like(t)
+    d = B.make_orthogonal_desc(rows, cols, wl.F32, batch, 6, STEP)
+    n = B.orthogonalize_workspace_bytes(d)
+    B.orthogonalize(d, t, y, torch.full((n,), 0xFF, dtype=torch.uint8, device="cuda"), n)
+    want = np.stack([ro.newton_schulz(m, 6, STEP, 1e-7) for m in x])
+    assert np.linalg.norm(y.double().cpu().numpy() - want) <= (3 * long / 64 * 2.0 ** -26 + 1e-6) * np.linalg.norm(want)
